@@ -13,6 +13,11 @@
  *                      the compacted cache.
  *   air_decode_attn    Eq.2 append + softmax(q K'^T / sqrt(d)) V' over the compacted cache.
  *
+ * Around it, for the model that makes the prompt's tensors (these calls need no context):
+ *
+ *   air_rope           per-head norm and position rotation of queries and keys, laid out for the calls above.
+ *   air_prompt_attn    causal attention of a prompt, a piece of one or a single token over the full cache.
+ *
  * Conventions
  *   - Every tensor pointer is DEVICE memory unless its comment says "host".  Descriptor
  *     arrays (air_layer[], air_seq[]) and getter outputs are HOST memory.
@@ -225,6 +230,91 @@ air_status air_decode_attn(air_ctx *ctx, void *stream, int32_t l0, int32_t l1, c
 air_status air_decode_attn_static(air_ctx *ctx, void *stream, int32_t l0, int32_t l1, const void *q_new,
                                   const void *k_new, const void *v_new, void *out);
 
+/* ---- in front of the compression: queries and keys of the prompt, and its attention ----
+ *
+ * These calls need no context.  They enqueue kernels only (no allocation, no copy, no memset, no host wait), so they can be
+ * recorded into a HIP graph; descriptors are read before they return.  Tensors, workspace and stream belong to the device that
+ * is current.  After an error air_last_error(NULL) gives the text of the calling thread's last failure here.  They keep
+ * no state: calls on different streams or threads may overlap as long as their outputs and workspaces do not.           */
+
+typedef enum {
+    AIR_ROPE_HALF = 0,       /* pair i of a head: elements i and i + pairs  */
+    AIR_ROPE_INTERLEAVED = 1 /* pair i of a head: elements 2 i and 2 i + 1  */
+} air_rope_layout;
+
+typedef struct {
+    int32_t n_q_heads, n_kv_heads, head_dim, dtype; /* heads of q / of k and v; head_dim 64 or 128; air_dtype           */
+    int32_t batch, n_tokens;                        /* rows: batch x n_tokens (either may be 0: nothing is done)           */
+    int32_t layout;                                 /* air_rope_layout                                                     */
+    int32_t n_axes;                                 /* position axes, 1..3 (3: time, row and column of image tokens)       */
+    int32_t axis_pairs[3];                          /* pairs that turn with axis 0, 1, 2, in the order of the pairs; their sum is a
+                                                       multiple of 8, at most head_dim / 2.  Twice that many leading elements of
+                                                       a head are rotated, the others pass through (0: norms and layout only)   */
+    float norm_eps;                                 /* of the norms, >= 0                                                  */
+    float scale;                                    /* factor of the rotated elements (1, or what air_rope_frequencies gives) */
+} air_rope_config;
+
+/* One tensor of air_rope: element strides of batch, head and token (the head_dim axis is contiguous), multiples of 16 bytes.
+ * dst == src with the same strides works in place; source and destination must not overlap in any other way.               */
+typedef struct {
+    const void *src;
+    void *dst;
+    const void *weight; /* [head_dim] of the RMS norm, in dtype; NULL: no norm.  Not for v */
+    int64_t src_b, src_h, src_t, dst_b, dst_h, dst_t;
+} air_rope_tensor;
+
+/* For every row x (one token, one head) of q and k:  y = x * weight / sqrt(mean(x^2) + norm_eps)  where a weight is given, and
+ * for pair i of y, turning with axis a:  angle = positions[a] * freqs[i],
+ *   (y_first, y_second) -> scale * (y_first cos - y_second sin, y_first sin + y_second cos).
+ * Rows of v are copied.  Any of q, k, v may be NULL (not all): that tensor is left out.  Computed in fp32 with angles reduced in
+ * fp64 (positions of a million turn as exactly as small ones) and rounded once.
+ * positions: device [n_axes][batch][n_tokens]; a row whose position on axis 0 is negative is padding: it is neither read nor
+ * written, whatever lies there.  NULL only without pairs.  freqs: device [sum of axis_pairs], radians per position.         */
+air_status air_rope(void *stream, const air_rope_config *cfg, const air_rope_tensor *q, const air_rope_tensor *k,
+                    const air_rope_tensor *v, const int32_t *positions, const double *freqs);
+
+/* How the frequencies are stretched for contexts longer than the model was trained on. */
+typedef enum {
+    AIR_ROPE_PLAIN = 0,   /* f_i = theta^(-i / n_pairs)                                                              */
+    AIR_ROPE_LINEAR = 1,  /* f_i / factor                                                                            */
+    AIR_ROPE_BY_PARTS = 2 /* pairs that turn at most slow_turns times in original_len positions are divided by factor, those
+                             that turn at least fast_turns times stay, linear in the number of turns between; the
+                             factor of the rotated elements becomes 0.1 ln(factor) + 1  (arxiv 2309.00071, Sec.3.2-3.4) */
+} air_rope_scaling;
+
+/* Host only: freqs[n_pairs] and *scale (for air_rope_config.scale; may be NULL).  theta > 0, factor >= 1; original_len, slow_turns and
+ * fast_turns (the paper: 1 and 32) are read with AIR_ROPE_BY_PARTS only: original_len >= 1, 0 <= slow_turns < fast_turns. */
+air_status air_rope_frequencies(int32_t n_pairs, double theta, int32_t scaling, double factor, int32_t original_len,
+                                double slow_turns, double fast_turns, double *freqs, float *scale);
+
+typedef struct {
+    int32_t n_q_heads, n_kv_heads, head_dim, dtype; /* head_dim 64 or 128; air_dtype of q, k, v and out                     */
+    float scale;                                    /* of the logits, > 0; 0: 1 / sqrt(head_dim)                           */
+    int64_t q_h, q_t, k_h, k_t, v_h, v_t, out_h, out_t; /* element strides of head and token, multiples of 16 bytes       */
+} air_prompt_config;
+
+/* One sequence: where its first query, key, value and output row lie (elements from the tensors' pointers, multiples of 16 bytes:
+ * sequences packed one behind the other, rows of a padded batch or pieces of larger buffers) and how many there are.  The queries are
+ * the last q_len of the kv_len positions.  Lengths may be 0. */
+typedef struct {
+    int64_t q_off, k_off, v_off, out_off;
+    int32_t q_len, kv_len;
+} air_prompt_seq;
+
+/* Bytes of device workspace the call needs (0: none, or an argument that air_prompt_attn refuses).  Calls with little work per sequence are
+ * split over the keys and leave partial results there. */
+size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs);
+
+/* For query head h and query t of a sequence:  out = sum_j p_j v_j,  p = softmax over the keys j <= t + kv_len - q_len of
+ * scale * q . k_j, with the keys and values of KV head h / (n_q_heads / n_kv_heads).  What lies at keys behind a row's own position, or
+ * behind kv_len, counts for nothing, whatever it holds (infinities and NaN included).  A row that sees no key (q_len > kv_len), or
+ * only logits of -inf, is zero.  Output rows outside the sequences are left as they are.  Logits, maxima, sums and products are
+ * held in fp32; with bf16 the probabilities are rounded to bf16 for the second product.  seqs: host array, n_seqs in 0..AIR_MAX_BATCH.
+ * workspace: 256-byte aligned, free for another call when this one's work has run; may be NULL where no bytes are needed.
+ * out must not overlap an input. */
+air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, const void *q,
+                           const void *k, const void *v, void *out, void *workspace, size_t workspace_bytes);
+
 /* ---- inspection (tests, debugging): these synchronise the device ---- */
 /* importance scores of layer l: host [B][H_kv][max_vis_len], the device buffer as it is (entries past a
  * sequence's vis_len are never written by the library: zero on a context that has seen one prompt) */
@@ -252,6 +342,7 @@ air_status air_get_lengths(air_ctx *ctx, int32_t *host);
 air_status air_get_cache(air_ctx *ctx, int32_t l, int32_t b, int32_t h, void *k_host, void *v_host,
                          int32_t max_rows);
 
+/* text of the last failure on ctx; NULL: of the calling thread's last failure in a call that needs no context */
 const char *air_last_error(const air_ctx *ctx);
 const char *air_version(void);
 

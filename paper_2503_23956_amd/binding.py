@@ -19,6 +19,8 @@ AIR_ERR_INVALID_ARG, AIR_ERR_SHAPE, AIR_ERR_WORKSPACE, AIR_ERR_STATE, AIR_ERR_HI
 AIR_F32, AIR_BF16 = 0, 1
 AIR_BUDGET_STRENGTH_SKEW, AIR_BUDGET_UNIFORM, AIR_BUDGET_STRENGTH, AIR_BUDGET_SKEW = 0, 1, 2, 3
 AIR_WINDOW_TEXT, AIR_WINDOW_VISUAL = 0, 1
+AIR_ROPE_HALF, AIR_ROPE_INTERLEAVED = 0, 1
+AIR_ROPE_PLAIN, AIR_ROPE_LINEAR, AIR_ROPE_BY_PARTS = 0, 1, 2
 _STATUS_NAMES = {0: "AIR_OK", 1: "AIR_ERR_INVALID_ARG", 2: "AIR_ERR_SHAPE", 3: "AIR_ERR_WORKSPACE",
                  4: "AIR_ERR_STATE", 5: "AIR_ERR_HIP"}
 
@@ -55,11 +57,30 @@ class air_strides(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("q_b", "q_h", "q_t", "kv_b", "kv_h", "kv_t")]
 
 
+class air_rope_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "dtype", "batch", "n_tokens", "layout", "n_axes")] + [
+        ("axis_pairs", C.c_int32 * 3), ("norm_eps", C.c_float), ("scale", C.c_float)]
+
+
+class air_rope_tensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("weight", C.c_void_p)] + [
+        (n, C.c_int64) for n in ("src_b", "src_h", "src_t", "dst_b", "dst_h", "dst_t")]
+
+
+class air_prompt_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "dtype")] + [("scale", C.c_float)] + [
+        (n, C.c_int64) for n in ("q_h", "q_t", "k_h", "k_t", "v_h", "v_t", "out_h", "out_t")]
+
+
+class air_prompt_seq(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("q_off", "k_off", "v_off", "out_off")] + [("q_len", C.c_int32), ("kv_len", C.c_int32)]
+
+
 EXPORTS = (
     "air_version", "air_workspace_bytes", "air_create", "air_destroy", "air_reset", "air_set_tuning", "air_score",
     "air_budget", "air_select_compact", "air_decode_attn", "air_decode_attn_static", "air_get_scores", "air_get_elite", "air_get_stats",
     "air_get_budgets", "air_set_budgets", "air_get_indices", "air_set_indices", "air_get_lengths", "air_get_cache",
-    "air_last_error",
+    "air_last_error", "air_rope", "air_rope_frequencies", "air_prompt_workspace_bytes", "air_prompt_attn",
 )
 
 _lib = None
@@ -103,8 +124,14 @@ def load_library(path: Optional[str] = None):
     lib.air_get_cache.argtypes = [vp, i32, i32, i32, vp, vp, i32]
     lib.air_last_error.argtypes = [vp]
     lib.air_last_error.restype = C.c_char_p
+    dbl = C.c_double
+    lib.air_rope.argtypes = [vp, C.POINTER(air_rope_config)] + [C.POINTER(air_rope_tensor)] * 3 + [vp, vp]
+    lib.air_rope_frequencies.argtypes = [i32, dbl, i32, dbl, i32, dbl, dbl, vp, C.POINTER(C.c_float)]
+    lib.air_prompt_workspace_bytes.argtypes = [C.POINTER(air_prompt_config), C.POINTER(air_prompt_seq), i32]
+    lib.air_prompt_workspace_bytes.restype = C.c_size_t
+    lib.air_prompt_attn.argtypes = [vp, C.POINTER(air_prompt_config), C.POINTER(air_prompt_seq), i32, vp, vp, vp, vp, vp, C.c_size_t]
     for name in EXPORTS:
-        if name not in ("air_version", "air_workspace_bytes", "air_last_error"):
+        if name not in ("air_version", "air_workspace_bytes", "air_prompt_workspace_bytes", "air_last_error"):
             getattr(lib, name).restype = C.c_int
     if path is None:
         _lib = lib
@@ -307,3 +334,147 @@ class AirCache:
         vv = np.zeros((max_rows, c.head_dim), dtype=dt)
         self._check(self.lib.air_get_cache(self.handle, l, b, h, kk.ctypes.data, vv.ctypes.data, max_rows))
         return kk, vv
+
+
+# -- calls without a context: norm and rotation of queries and keys, attention over a prompt -----------------------------
+def _refuse(msg: str):
+    raise AirError(AIR_ERR_INVALID_ARG, msg)
+
+
+def _dtype_of(t) -> int:
+    import torch
+
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        _refuse(f"tensors must be bfloat16 or float32, not {t.dtype}")
+    return AIR_BF16 if t.dtype == torch.bfloat16 else AIR_F32
+
+
+def _strides4(t):
+    """Element strides (batch, head, token) of a tensor indexed [B][H][T][d]; an axis of one entry has none."""
+    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
+        _refuse("tensors must be indexed [B][H][T][d] with a contiguous last axis")
+    return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+
+
+class PreparedCall:
+    """Marshalled arguments of one air_rope / air_prompt_attn call plus the tensors they point to; may be called any number of
+    times (the tensors' contents may change between calls)."""
+
+    def __init__(self, args, device, keepalive, workspace_bytes=0):
+        self.args, self.device, self.workspace_bytes, self._keepalive = args, device, workspace_bytes, keepalive
+
+
+def _enqueue(fn, p: PreparedCall, stream, *more):
+    """fn(stream, args, more) with the tensors' device current."""
+    import torch
+
+    if p.device.type != "cuda":
+        _refuse("tensors must be on a GPU")
+    index = p.device.index if p.device.index is not None else torch.cuda.current_device()
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return _enqueue(fn, p, stream, *more)
+    raw = int(torch.cuda.current_stream(index).cuda_stream) if stream is None else stream
+    st = fn(raw, *p.args, *more)
+    if st != AIR_OK:
+        raise AirError(st, load_library().air_last_error(None).decode())
+
+
+def air_rope_frequencies(n_pairs: int, theta: float, scaling=AIR_ROPE_PLAIN, factor=1.0, original_len=0, slow_turns=1.0, fast_turns=32.0):
+    """(frequencies as a float64 array [n_pairs], factor of the rotated elements): see include/aircache.h."""
+    lib = load_library()
+    out, scale = np.empty(max(0, n_pairs), dtype=np.float64), C.c_float(1.0)
+    st = lib.air_rope_frequencies(n_pairs, theta, scaling, factor, original_len, slow_turns, fast_turns, out.ctypes.data, C.byref(scale))
+    if st != AIR_OK:
+        raise AirError(st, lib.air_last_error(None).decode())
+    return out, scale.value
+
+
+def prepare_rope(q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, *, positions=None, freqs=None, axis_pairs=(),
+                 layout=AIR_ROPE_HALF, q_weight=None, k_weight=None, eps=1e-6, scale=1.0) -> PreparedCall:
+    """Tensors indexed [B][H][T][d], any memory order with contiguous d; an output left out means in place.  axis_pairs: pairs per
+    position axis (one to three).  positions: int32 [axes][B][T] ([B][T] with one axis), negative = padding, left as it is;
+    freqs: float64 [sum(axis_pairs)]; both contiguous on the tensors' device."""
+    import torch
+
+    given = [(x, x if o is None else o, w) for x, o, w in ((q, q_out, q_weight), (k, k_out, k_weight), (v, v_out, None))]
+    first = next((x for x, _, _ in given if x is not None), None)
+    if first is None:
+        _refuse("air_rope: one of q, k, v is needed")
+    first_dtype = _dtype_of(first)
+    _strides4(first)
+    B, T, d = first.shape[0], first.shape[2], first.shape[3]
+    n_axes, pairs = max(1, len(axis_pairs)), sum(axis_pairs)
+    if len(axis_pairs) > 3:
+        _refuse("air_rope: at most three position axes")
+    ts = []
+    for x, o, w in given:
+        if x is None:
+            if o is not None or w is not None:
+                _refuse("air_rope: an output or a weight without its tensor")
+            ts.append(None)
+            continue
+        if x.dtype != first.dtype or o.dtype != first.dtype or x.shape != o.shape or (x.shape[0], x.shape[2], x.shape[3]) != (B, T, d):
+            _refuse("air_rope: tensors must have one type, batch, length and head size, outputs their tensor's shape")
+        if w is not None and (w.dtype != first.dtype or tuple(w.shape) != (d,) or not w.is_contiguous()):
+            _refuse("air_rope: a weight must be a contiguous [head_dim] of the tensors' type")
+        if x.device != first.device or o.device != first.device or (w is not None and w.device != first.device):
+            _refuse("air_rope: tensors must be on one device")
+        ts.append(air_rope_tensor(_ptr(x), _ptr(o), _ptr(w), *_strides4(x), *_strides4(o)))
+    if k is not None and v is not None and k.shape[1] != v.shape[1]:
+        _refuse("air_rope: keys and values must have the same heads")
+    hkv = k.shape[1] if k is not None else v.shape[1] if v is not None else 0
+    hq = q.shape[1] if q is not None else hkv
+    if positions is not None:
+        if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.device != first.device or \
+                tuple(positions.shape) not in ((n_axes, B, T),) + (((B, T),) if n_axes == 1 else ()):
+            _refuse("air_rope: positions must be a contiguous int32 [axes][B][T] on the tensors' device")
+    if freqs is not None and (freqs.dtype != torch.float64 or not freqs.is_contiguous() or freqs.numel() < pairs or
+                              freqs.device != first.device):
+        _refuse("air_rope: freqs must be a contiguous float64 [sum(axis_pairs)] on the tensors' device")
+    cfg = air_rope_config(hq, hkv or hq, d, first_dtype, B, T, layout, n_axes, (C.c_int32 * 3)(*axis_pairs), eps, scale)
+    args = (C.byref(cfg), *(None if t is None else C.byref(t) for t in ts), _ptr(positions), _ptr(freqs))
+    return PreparedCall(args, first.device, (given, positions, freqs))
+
+
+def air_rope(*tensors, prepared: Optional[PreparedCall] = None, stream=None, **kw):
+    """prepared: result of prepare_rope (skips the marshalling); else its arguments.  stream: a raw HIP stream handle, default torch's
+    current stream on the tensors' device."""
+    _enqueue(load_library().air_rope, prepared or prepare_rope(*tensors, **kw), stream)
+
+
+def prepare_prompt_attn(q, k, v, out, spans=None, scale=0.0) -> PreparedCall:
+    """q, out [B][Hq][T][d], k, v [B][Hkv][S][d], any memory order with contiguous d.  spans: one (batch row, first query, queries, first
+    key, keys) per sequence; default: every batch row over its full length."""
+    dt = _dtype_of(q)
+    sq, sk, sv, so = (_strides4(t) for t in (q, k, v, out))
+    if any(t.dtype != q.dtype or t.device != q.device for t in (k, v, out)):
+        _refuse("air_prompt_attn: tensors must have one type and device")
+    if k.shape != v.shape or q.shape != out.shape or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
+        _refuse("air_prompt_attn: shapes of q and out, of k and v must agree")
+    if spans is None:
+        spans = [(b, 0, q.shape[2], 0, k.shape[2]) for b in range(q.shape[0])]
+    arr = (air_prompt_seq * max(1, len(spans)))()
+    for i, (b, q0, n, k0, m) in enumerate(spans):
+        if min(q0, n, k0, m) < 0 or not 0 <= b < q.shape[0] or q0 + n > q.shape[2] or k0 + m > k.shape[2]:
+            _refuse("air_prompt_attn: a span lies outside its tensors")
+        arr[i] = air_prompt_seq(b * sq[0] + q0 * sq[2], b * sk[0] + k0 * sk[2], b * sv[0] + k0 * sv[2], b * so[0] + q0 * so[2], n, m)
+    cfg = air_prompt_config(q.shape[1], k.shape[1], q.shape[3], dt, scale, sq[1], sq[2], sk[1], sk[2], sv[1], sv[2], so[1], so[2])
+    args = (C.byref(cfg), arr, len(spans), _ptr(q), _ptr(k), _ptr(v), _ptr(out))
+    nbytes = load_library().air_prompt_workspace_bytes(C.byref(cfg), arr, len(spans))
+    return PreparedCall(args, q.device, (q, k, v, out), nbytes)
+
+
+def air_prompt_attn(*tensors, prepared: Optional[PreparedCall] = None, workspace=None, stream=None, **kw):
+    """prepared: result of prepare_prompt_attn (skips the marshalling); else its arguments.  workspace: a uint8 tensor of at least
+    prepared.workspace_bytes; default: one allocated for the call on torch's current stream, which is then the only stream the call may go
+    to.  stream: a raw HIP stream handle, default torch's current stream on the tensors' device."""
+    import torch
+
+    p = prepared or prepare_prompt_attn(*tensors, **kw)
+    if workspace is None and p.workspace_bytes and p.device.type == "cuda":
+        if stream is not None:
+            _refuse("air_prompt_attn: a call on a stream of its own needs its workspace")
+        workspace = torch.empty(p.workspace_bytes, dtype=torch.uint8, device=p.device)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _enqueue(load_library().air_prompt_attn, p, stream, _ptr(workspace), nbytes)

@@ -21,6 +21,9 @@ SOURCES = {
     "air_budget.hip": ["-ffp-contract=off"],
     "air_select.hip": [],
     "air_decode.hip": [],
+    "air_front.hip": [],
+    "air_rope.hip": [],
+    "air_prompt.hip": [],
 }
 
 COMMON = [

@@ -289,7 +289,10 @@ air_status air_reset(air_ctx *ctx) {
     return AIR_OK;
 }
 
-const char *air_last_error(const air_ctx *ctx) { return ctx ? ctx->err.c_str() : "null context"; }
+const char *air_last_error(const air_ctx *ctx) {
+    if (ctx) return ctx->err.c_str();
+    return *thread_error() ? thread_error() : "null context";
+}
 
 // layers per launch of the kernels that take per-layer tensor pointers: the units of a launch are one grid dimension (<= 65535)
 static int layers_per_launch(const air_ctx *c) {

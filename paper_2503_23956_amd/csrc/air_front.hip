@@ -1,0 +1,154 @@
+// Entry points that need no context (norm and rotation of queries and keys, attention over a prompt): argument checks.
+#include <math.h>
+#include <stdarg.h>
+#include <stdio.h>
+
+#include "air_internal.h"
+
+namespace air {
+
+static thread_local char t_error[256];
+const char *thread_error() { return t_error; }
+
+static air_status refuse(air_status st, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(t_error, sizeof(t_error), fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+constexpr int kMaxHeads = 16384;  // runs of heads and (tile, head) pairs are grid dimensions
+
+static bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+static const char *geometry(int hq, int hkv, int d, int dtype) {
+    if (dtype != AIR_F32 && dtype != AIR_BF16) return "dtype must be AIR_F32 or AIR_BF16";
+    if (d != 64 && d != 128) return "head_dim must be 64 or 128";
+    if (hkv < 1 || hq < hkv || hq % hkv || hq > kMaxHeads) return "query heads must be a multiple of KV heads, at most 16384";
+    return nullptr;
+}
+
+}  // namespace air
+
+using namespace air;
+
+extern "C" {
+
+air_status air_rope(void *stream, const air_rope_config *cfg, const air_rope_tensor *q, const air_rope_tensor *k,
+                    const air_rope_tensor *v, const int32_t *positions, const double *freqs) {
+    if (!cfg || (!q && !k && !v)) return refuse(AIR_ERR_INVALID_ARG, "air_rope: null argument");
+    const air_rope_config &c = *cfg;
+    if (const char *bad = geometry(c.n_q_heads, c.n_kv_heads, c.head_dim, c.dtype)) return refuse(AIR_ERR_SHAPE, "air_rope: %s", bad);
+    if (c.batch < 0 || c.n_tokens < 0 || (int64_t)c.batch * c.n_tokens > 0x7fffffff)
+        return refuse(AIR_ERR_SHAPE, "air_rope: batch and n_tokens must not be negative, their product below 2^31");
+    if (c.layout != AIR_ROPE_HALF && c.layout != AIR_ROPE_INTERLEAVED) return refuse(AIR_ERR_INVALID_ARG, "air_rope: unknown layout");
+    if (c.n_axes < 1 || c.n_axes > 3) return refuse(AIR_ERR_INVALID_ARG, "air_rope: n_axes must be 1, 2 or 3");
+    int64_t pairs = 0;
+    for (int i = 0; i < c.n_axes; ++i) {
+        if (c.axis_pairs[i] < 0) return refuse(AIR_ERR_SHAPE, "air_rope: negative axis_pairs");
+        pairs += c.axis_pairs[i];
+    }
+    if (pairs % 8 || pairs > c.head_dim / 2)
+        return refuse(AIR_ERR_SHAPE, "air_rope: axis_pairs must add up to a multiple of 8, at most head_dim / 2");
+    if (!(c.norm_eps >= 0.f) || !isfinite(c.norm_eps) || !isfinite(c.scale))
+        return refuse(AIR_ERR_INVALID_ARG, "air_rope: norm_eps must be finite and not negative, scale finite");
+    const bool work = c.batch > 0 && c.n_tokens > 0;
+    if (work && pairs > 0 && (!positions || !freqs)) return refuse(AIR_ERR_INVALID_ARG, "air_rope: positions and freqs are needed");
+    if (!aligned(positions, 4) || !aligned(freqs, 8)) return refuse(AIR_ERR_INVALID_ARG, "air_rope: positions or freqs misaligned");
+    const air_rope_tensor *const t[3] = {q, k, v};
+    const int64_t vec = c.dtype == AIR_BF16 ? 8 : 4;
+    for (int i = 0; i < 3; ++i) {
+        if (!t[i]) continue;
+        const air_rope_tensor &x = *t[i];
+        const int heads = i == 0 ? c.n_q_heads : c.n_kv_heads;
+        if (work && (!x.src || !x.dst)) return refuse(AIR_ERR_INVALID_ARG, "air_rope: null tensor pointer");
+        if (!aligned(x.src, 16) || !aligned(x.dst, 16) || !aligned(x.weight, 16))
+            return refuse(AIR_ERR_INVALID_ARG, "air_rope: tensor pointers must be 16-byte aligned");
+        if (i == 2 && x.weight) return refuse(AIR_ERR_INVALID_ARG, "air_rope: values have no norm");
+        const int64_t st[6] = {x.src_b, x.src_h, x.src_t, x.dst_b, x.dst_h, x.dst_t};
+        for (int64_t s : st)
+            if (s < 0 || s % vec) return refuse(AIR_ERR_SHAPE, "air_rope: strides must be non-negative multiples of 16 bytes");
+        if ((c.batch > 1 && x.dst_b < c.head_dim) || (heads > 1 && x.dst_h < c.head_dim) || (c.n_tokens > 1 && x.dst_t < c.head_dim))
+            return refuse(AIR_ERR_SHAPE, "air_rope: rows of a destination overlap");
+        if (work && x.src == x.dst && ((c.batch > 1 && x.src_b != x.dst_b) || (heads > 1 && x.src_h != x.dst_h) || (c.n_tokens > 1 && x.src_t != x.dst_t)))
+            return refuse(AIR_ERR_SHAPE, "air_rope: in place needs the same strides on both sides");
+    }
+    if (!work) return AIR_OK;
+    const hipError_t e = launch_rope((hipStream_t)stream, c, t, positions, freqs);
+    if (e != hipSuccess) return refuse(AIR_ERR_HIP, "air_rope launch: %s", hipGetErrorString(e));
+    return AIR_OK;
+}
+
+air_status air_rope_frequencies(int32_t n_pairs, double theta, int32_t scaling, double factor, int32_t original_len,
+                                double slow_turns, double fast_turns, double *freqs, float *scale) {
+    if (n_pairs < 0 || (n_pairs > 0 && !freqs)) return refuse(AIR_ERR_INVALID_ARG, "air_rope_frequencies: null argument");
+    if (scaling < AIR_ROPE_PLAIN || scaling > AIR_ROPE_BY_PARTS) return refuse(AIR_ERR_INVALID_ARG, "air_rope_frequencies: unknown scaling");
+    if (!(theta > 0.0) || !isfinite(theta) || !(factor >= 1.0) || !isfinite(factor))
+        return refuse(AIR_ERR_INVALID_ARG, "air_rope_frequencies: theta must be positive, factor at least 1, both finite");
+    if (scaling == AIR_ROPE_BY_PARTS && (original_len < 1 || !(slow_turns >= 0.0) || !(fast_turns > slow_turns) || !isfinite(fast_turns)))
+        return refuse(AIR_ERR_INVALID_ARG, "air_rope_frequencies: need original_len >= 1 and 0 <= slow_turns < fast_turns");
+    constexpr double kTurn = 6.28318530717958647693;
+    for (int i = 0; i < n_pairs; ++i) {
+        const double f = pow(theta, -(double)i / n_pairs);
+        double keep = 1.0;  // share of the frequency that is not stretched
+        if (scaling == AIR_ROPE_LINEAR) keep = 0.0;
+        if (scaling == AIR_ROPE_BY_PARTS) keep = fmin(1.0, fmax(0.0, (original_len * f / kTurn - slow_turns) / (fast_turns - slow_turns)));
+        freqs[i] = f * keep + f / factor * (1.0 - keep);
+    }
+    if (scale) *scale = scaling == AIR_ROPE_BY_PARTS ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+    return AIR_OK;
+}
+
+// what both calls of the prompt attention refuse, but for the tensors
+static air_status check_prompt(const char *who, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n) {
+    if (!cfg || (n > 0 && !seqs)) return refuse(AIR_ERR_INVALID_ARG, "%s: null argument", who);
+    const air_prompt_config &c = *cfg;
+    if (const char *bad = geometry(c.n_q_heads, c.n_kv_heads, c.head_dim, c.dtype)) return refuse(AIR_ERR_SHAPE, "%s: %s", who, bad);
+    if (n < 0 || n > AIR_MAX_BATCH) return refuse(AIR_ERR_SHAPE, "%s: n_seqs must be in 0..%d", who, AIR_MAX_BATCH);
+    if (!(c.scale >= 0.f) || !isfinite(c.scale)) return refuse(AIR_ERR_INVALID_ARG, "%s: scale must be positive (or 0) and finite", who);
+    const int64_t vec = c.dtype == AIR_BF16 ? 8 : 4;
+    const int64_t st[8] = {c.q_h, c.q_t, c.k_h, c.k_t, c.v_h, c.v_t, c.out_h, c.out_t};
+    for (int64_t s : st)
+        if (s < 0 || s % vec) return refuse(AIR_ERR_SHAPE, "%s: strides must be non-negative multiples of 16 bytes", who);
+    int32_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        const air_prompt_seq &s = seqs[i];
+        if (s.q_len < 0 || s.kv_len < 0) return refuse(AIR_ERR_SHAPE, "%s: negative length", who);
+        const int64_t off[4] = {s.q_off, s.k_off, s.v_off, s.out_off};
+        for (int64_t o : off)
+            if (o < 0 || o % vec) return refuse(AIR_ERR_SHAPE, "%s: offsets must be non-negative multiples of 16 bytes", who);
+        if (s.q_len > most) most = s.q_len;
+    }
+    if ((c.n_q_heads > 1 && c.out_h < c.head_dim) || (most > 1 && c.out_t < c.head_dim))
+        return refuse(AIR_ERR_SHAPE, "%s: output rows overlap", who);
+    if (!prompt_grid_ok(c, seqs, n)) return refuse(AIR_ERR_SHAPE, "%s: too many rows for one call", who);
+    return AIR_OK;
+}
+
+size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs) {
+    if (check_prompt("air_prompt_workspace_bytes", cfg, seqs, n_seqs) != AIR_OK) return 0;
+    return prompt_workspace(*cfg, seqs, n_seqs);
+}
+
+air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, const void *q,
+                           const void *k, const void *v, void *out, void *workspace, size_t workspace_bytes) {
+    const air_status st = check_prompt("air_prompt_attn", cfg, seqs, n_seqs);
+    if (st != AIR_OK) return st;
+    bool rows = false, keys = false;
+    for (int i = 0; i < n_seqs; ++i) {
+        rows = rows || seqs[i].q_len > 0;
+        keys = keys || (seqs[i].q_len > 0 && seqs[i].kv_len > 0);
+    }
+    if ((rows && (!q || !out)) || (keys && (!k || !v))) return refuse(AIR_ERR_INVALID_ARG, "air_prompt_attn: null tensor pointer");
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16))
+        return refuse(AIR_ERR_INVALID_ARG, "air_prompt_attn: tensors must be 16-byte aligned");
+    const size_t need = prompt_workspace(*cfg, seqs, n_seqs);
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
+        return refuse(AIR_ERR_WORKSPACE, "air_prompt_attn: needs a 256-byte aligned workspace of %zu bytes", need);
+    const hipError_t e = launch_prompt((hipStream_t)stream, *cfg, seqs, n_seqs, q, k, v, out, workspace);
+    if (e != hipSuccess) return refuse(AIR_ERR_HIP, "air_prompt_attn launch: %s", hipGetErrorString(e));
+    return AIR_OK;
+}
+
+}  // extern "C"

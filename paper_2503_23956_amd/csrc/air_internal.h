@@ -132,6 +132,15 @@ hipError_t launch_decode(hipStream_t s, const Dims &dm, const DevTables &t, cons
 hipError_t static_exchange(DecodeExchange *x);
 hipError_t launch_zero_counters(hipStream_t s, int32_t *p, int n);
 
+// ---- calls without a context ----
+hipError_t launch_rope(hipStream_t s, const air_rope_config &c, const air_rope_tensor *const (&t)[3], const int32_t *positions,
+                       const double *freqs);
+hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const air_prompt_seq *seqs, int n, const void *q, const void *k,
+                         const void *v, void *out, void *workspace);
+size_t prompt_workspace(const air_prompt_config &c, const air_prompt_seq *seqs, int n);
+bool prompt_grid_ok(const air_prompt_config &c, const air_prompt_seq *seqs, int n);  // the launches' grids and 32-bit indexes hold the call
+const char *thread_error();  // text of the calling thread's last failure in a call without a context; empty: none
+
 // The cache is laid out so that the decode kernel can feed it to MFMA straight from global memory, every load
 // instruction of a wave reading 1 KB of consecutive memory, and so that one token touches few cache lines (appending a
 // token costs by the line it writes).  vec = elements in 16 bytes (8 bf16, 4 fp32).

@@ -1,0 +1,673 @@
+// air_prompt_attn: causal attention of prompts, pieces of prompts and single tokens over the full cache.
+//
+//   out_t = sum_j p_j v_j,   p = softmax over j <= t + kv_len - q_len of scale * q_t . k_j
+//
+// The rows of one (sequence, KV head) are its queries times the G query heads that share the KV head, token by token: row
+// m = t G + g.  K and V are then read once for all heads of the group, a tile of rows spans few tokens (little of the causal
+// triangle is wasted), and prompts, pieces and single tokens are one shape: rows x keys.
+//
+// Both products run on 32 x 32 tiles of the matrix unit, transposed: S^T = K Q^T leaves lane (n = lane % 32, h = lane / 32)
+// with query n's logits at the keys 8 (i / 4) + 4 h + i % 4, i = 0..15.  Maximum and sum of a query need one exchange between two
+// lanes, and registers 8 s .. 8 s + 7 are the operand P^T of O^T = V^T P^T as they are, when the operand V^T takes the keys in the same
+// order: no probability leaves its lane.  The accumulators O^T have query n in the same lanes, so that a new reference maximum
+// scales them with the lane's own factor.
+//
+// Softmax in the base-2 domain with a running reference per query; it is raised only when a logit lies more than kSlack above it.
+#include <math.h>
+#include <string.h>
+
+#include "air_device.h"
+#include "air_internal.h"
+#include "air_tile.h"
+
+namespace air {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+struct PromptSpan {
+    int64_t q_off, k_off, v_off, out_off;
+    int32_t q_len, kv_len;
+    int32_t tile0;  // first row tile of the sequence in the launch
+    int32_t row0;   // first row (query x query head of the group) of the sequence in the partial results
+};
+struct PromptArgs {
+    const void *q, *k, *v;
+    void *out;
+    float *part_o;    // [split][KV head][row][D]
+    float2 *part_ml;  // [split][KV head][row]
+    int64_t q_h, q_t, k_h, k_t, v_h, v_t, out_h, out_t;
+    float c;  // scale * log2(e)
+    int32_t G, Hkv, n_seqs, n_tiles, n_rows, splits;
+    PromptSpan s[AIR_MAX_BATCH];
+};
+
+// What the wave functions need of the storage type: CH 16-byte pieces of a row, slices of 32 bytes (one piece per lane half)
+template <typename T, int D>
+struct Row {
+    static constexpr int kVec = Elem<T>::kVec, kPieces = D / kVec, kSlices = kPieces / 2;
+    // Where piece p of key r lies in its tile.  K: read 16 bytes a lane, one row per lane: neighbouring rows' pieces in different
+    // banks.  V in bf16: read transposed, four rows x 32 bytes per 16 lanes: neighbouring rows' pairs of pieces in different banks; in
+    // fp32 a row at a time.
+    static __device__ __forceinline__ int k_at(int r, int p) { return r * kPieces + (p ^ (r & (kPieces < 16 ? kPieces - 1 : 15))); }
+    static __device__ __forceinline__ int v_at(int r, int p) {
+        return r * kPieces + (sizeof(T) == 2 ? p ^ ((r & (kPieces / 2 - 1)) << 1) : p);
+    }
+};
+
+__device__ __forceinline__ f32x16 mma32(const uint4 &a, const uint4 &b, f32x16 acc, bf16_t) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(const uint4 &a, const uint4 &b, f32x16 acc, float) {
+    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], acc, 0, 0, 0);
+    return acc;
+}
+
+// all exponent bits set in one of the elements
+__device__ __forceinline__ bool not_finite(const uint4 &x, bf16_t) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad = bad || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+}
+__device__ __forceinline__ bool not_finite(const uint4 &x, float) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad = bad || (w[i] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+}
+
+// orders the LDS accesses of the lanes of one wave
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// s * c rounded, less the reference (two operations, not one)
+__device__ __forceinline__ float rounded_exponent(float s, float c, float ref) {
+#pragma clang fp contract(off)
+    const float x = s * c;
+    return x - ref;
+}
+
+constexpr float kHuge = 0x1p26f;
+constexpr float kSlack = 8.0f;  // probabilities may be as large as 2^8: fp32 sums and bf16 operands hold them without loss
+
+// RT row tiles of 32 of one wave against KT key tiles of 32 in LDS
+template <typename T, int D, int RT, int KT>
+struct Attend {
+    using R = Row<T, D>;
+    static constexpr int ND = D / 32;  // output tiles of 32 columns
+    f32x16 acc[RT][ND];
+    float m[RT], l[RT];  // reference (scaled logits), this lane's part of the sum
+    uint4 q[RT][R::kSlices];
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[r][d][i] = 0.f;
+        }
+    }
+
+    // kb: first key of the tile in the sequence; last[r]: last key that the lane's query of row tile r sees (read when MASKED);
+    // by_hand: the tile has values that are not finite at keys that some row does not see
+    template <bool MASKED>
+    __device__ __forceinline__ void step(const uint4 *sk, const uint4 *sv, int kb, const int (&last)[RT], float c, bool by_hand,
+                                         float *scratch) {
+        const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+        f32x16 s[RT][KT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[r][kt][i] = 0.f;
+#pragma unroll
+        for (int sl = 0; sl < R::kSlices; ++sl)
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const uint4 a = sk[R::k_at(32 * kt + n, 2 * sl + h)];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) s[r][kt] = mma32(a, q[r][sl], s[r][kt], T());
+            }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            if (MASKED) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (kb + 32 * kt + 8 * (i >> 2) + 4 * h + (i & 3) > last[r]) s[r][kt][i] = -INFINITY;
+            }
+            float mx = s[r][0][0];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[r][kt][i]);
+            mx *= c;
+            if (__ballot(mx > m[r] + kSlack) != 0ull) {
+                const float m_new = fmaxf(m[r], fmaxf(mx, __shfl_xor(mx, 32, 64)));
+                const float f = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[r] - m_new);  // no logit but -inf yet: nothing to scale
+                l[r] *= f;
+                m[r] = m_new;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[r][d][i] *= f;
+            }
+            const float ref = m[r] == -INFINITY ? 0.f : m[r];
+            // The reference is a rounded product, the exponent an exact one minus it: the largest logit's exponent is off zero by half a
+            // step of the reference, the same for all keys of the row, so that it cancels.  Far beyond any trained model's logits that
+            // step leaves fp32's range of exponents: there the product is rounded as the reference was.
+            if (__ballot(fabsf(ref) > kHuge) == 0ull) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[r][kt][i] = __builtin_amdgcn_exp2f(fmaf(s[r][kt][i], c, -ref));
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[r][kt][i] = __builtin_amdgcn_exp2f(rounded_exponent(s[r][kt][i], c, ref));
+            }
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) l[r] += s[r][kt][i];
+        }
+        if (MASKED && by_hand) {  // (uniform over the wave) a product with 0 would be NaN: only what a row sees is added
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {  // 16 keys at a time
+                        wave_sync();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) scratch[32 * (8 * (i >> 2) + 4 * h + (i & 3)) + n] = s[r][kt][8 * half + i];
+                        wave_sync();
+                        for (int j = 0; j < 16; ++j) {
+                            const int key = 32 * kt + 16 * half + j;
+                            const bool sees = kb + key <= last[r];
+                            const float p = scratch[32 * j + n];
+                            const T *row = reinterpret_cast<const T *>(sv);
+#pragma unroll
+                            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const int col = 32 * d + 8 * (i >> 2) + 4 * h + (i & 3);
+                                    const float v = ldf(row + R::v_at(key, col / R::kVec) * R::kVec + col % R::kVec);
+                                    acc[r][d][i] = sees ? fmaf(p, v, acc[r][d][i]) : acc[r][d][i];
+                                }
+                        }
+                    }
+                }
+            return;
+        }
+        if constexpr (sizeof(T) == 2) {
+            // lane of the transposed read: row (lane % 16) / 4 of four keys, 8 bytes at columns 16 ((lane / 16) % 2) + 4 (lane % 4)
+            const int krow = 4 * h + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            const char *base = reinterpret_cast<const char *>(sv) + 8 * (lane & 1);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint4 p[RT];
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        bf16x8 x;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = (__bf16)s[r][kt][8 * half + i];
+                        p[r] = __builtin_bit_cast(uint4, x);
+                    }
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const char *at = base + 16 * R::v_at(32 * kt + 16 * half + krow, 4 * d + piece);
+                        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                        struct { s16x4 a, b; } v;
+                        v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+                        v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * D * sizeof(T)));
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) acc[r][d] = mma32(__builtin_bit_cast(uint4, v), p[r], acc[r][d], T());
+                    }
+                }
+        } else {
+            const float *base = reinterpret_cast<const float *>(sv) + 4 * h * D + n;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const float v = base[(32 * kt + 8 * (i >> 2) + (i & 3)) * D + 32 * d];
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+                            acc[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r][kt][i], acc[r][d], 0, 0, 0);
+                    }
+        }
+    }
+};
+
+// four consecutive output elements
+__device__ __forceinline__ void store4(bf16_t *p, const f32x4 &x) {
+    typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+    bf16x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (__bf16)x[i];
+    *reinterpret_cast<uint2 *>(p) = __builtin_bit_cast(uint2, v);
+}
+__device__ __forceinline__ void store4(float *p, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
+
+// sequence, row tile, KV head and split of a workgroup.  The KV head is the fastest index (with 1, 2, 4 or 8 of them every XCD, dealt
+// workgroups round-robin, works on one head's K and V); the tiles come last to first: the ones with the most keys first.
+struct Place {
+    int seq, tile, kvh, split;
+};
+__device__ __forceinline__ Place place_of(const PromptArgs &a, int w) {
+    Place p;
+    int x = w / a.Hkv;
+    p.kvh = w - x * a.Hkv;
+    const int y = x / a.splits;
+    p.split = x - y * a.splits;
+    const int tile = a.n_tiles - 1 - y;
+    int lo = 0, hi = a.n_seqs - 1;  // last sequence whose first tile is not behind `tile`
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.s[mid].tile0 <= tile) lo = mid;
+        else hi = mid - 1;
+    }
+    p.seq = lo;
+    p.tile = tile - a.s[lo].tile0;
+    return p;
+}
+
+// ---------------------------------------------------------------------------------------
+// Many rows: NW waves of 32 RT rows each over tiles of 32 KT keys in LDS, which all waves share.  The next tile's loads are in
+// flight while the present one is multiplied.
+// ---------------------------------------------------------------------------------------
+template <typename T, int D, int NW, int RT, int KT>
+__global__ __launch_bounds__(64 * NW) void prompt_kernel(PromptArgs a) {
+    using R = Row<T, D>;
+    constexpr int kRows = 32 * RT * NW, kKeys = 32 * KT, kThreads = 64 * NW;
+    constexpr int kLoads = kKeys * R::kPieces / kThreads, kRowStep = kThreads / R::kPieces;
+    static_assert(kLoads * kThreads == kKeys * R::kPieces && kRowStep >= 1, "whole rounds of loads");
+    __shared__ uint4 sk[2][kKeys * R::kPieces], sv[2][kKeys * R::kPieces];
+    __shared__ float scratch[NW][16 * 32];
+    __shared__ int s_bad;
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(a, blockIdx.x);
+    const PromptSpan &sp = a.s[pl.seq];
+    const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
+    const int row0 = pl.tile * kRows;
+    const int end_row = min(row0 + kRows, n_rows);
+    // keys that every row of the tile sees, and that any does
+    const int see_all = max(0, row0 / a.G + shift + 1), see_any = max(0, (end_row - 1) / a.G + shift + 1);
+    const int n_blocks = (see_any + kKeys - 1) / kKeys, n_full = see_all / kKeys;
+    const int per_split = (n_blocks + a.splits - 1) / a.splits;
+    const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
+
+    Attend<T, D, RT, KT> at;
+    at.clear();
+    int last[RT], head[RT], tok[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row = min(row0 + 32 * (RT * wave + r) + n, n_rows - 1);
+        tok[r] = row / a.G;
+        head[r] = pl.kvh * a.G + row - tok[r] * a.G;
+        last[r] = tok[r] + shift;
+        const T *q = (const T *)a.q + sp.q_off + tok[r] * a.q_t + head[r] * a.q_h;
+#pragma unroll
+        for (int sl = 0; sl < R::kSlices; ++sl) at.q[r][sl] = *reinterpret_cast<const uint4 *>(q + R::kVec * (2 * sl + h));
+    }
+
+    const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
+    const int piece = threadIdx.x % R::kPieces, lrow = threadIdx.x / R::kPieces;
+    uint4 kr[kLoads], vr[kLoads];
+    auto load = [&](int b) {
+        const int kb = b * kKeys, top = sp.kv_len - 1 - kb;  // rows past the last key re-read it
+        const T *kp = kg + kb * a.k_t + R::kVec * piece, *vp = vg + kb * a.v_t + R::kVec * piece;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = min(lrow + kRowStep * i, top);
+            kr[i] = *reinterpret_cast<const uint4 *>(kp + r * a.k_t);
+            vr[i] = *reinterpret_cast<const uint4 *>(vp + r * a.v_t);
+        }
+    };
+    auto keep = [&](int b) {
+        const int buf = b & 1;
+        if (b >= n_full) {  // some row does not see all of the tile
+            const int left = sp.kv_len - b * kKeys;
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if (lrow + kRowStep * i >= left) vr[i] = make_uint4(0, 0, 0, 0);
+                bad = bad || not_finite(vr[i], T());
+            }
+            if (bad) s_bad = 1;
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            sk[buf][R::k_at(lrow + kRowStep * i, piece)] = kr[i];
+            sv[buf][R::v_at(lrow + kRowStep * i, piece)] = vr[i];
+        }
+    };
+    if (threadIdx.x == 0) s_bad = 0;
+    __syncthreads();
+    if (b0 < b1) {
+        load(b0);
+        keep(b0);
+    }
+    __syncthreads();
+    for (int b = b0; b < b1; ++b) {
+        if (b + 1 < b1) load(b + 1);
+        if (b < n_full) at.template step<false>(sk[b & 1], sv[b & 1], b * kKeys, last, a.c, false, scratch[wave]);
+        else at.template step<true>(sk[b & 1], sv[b & 1], b * kKeys, last, a.c, __builtin_amdgcn_readfirstlane(s_bad) != 0, scratch[wave]);
+        if (b + 1 < b1) keep(b + 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const float l = at.l[r] + __shfl_xor(at.l[r], 32, 64);
+        const int row = row0 + 32 * (RT * wave + r) + n;
+        if (row >= n_rows) continue;
+        if (a.splits == 1) {
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            T *o = (T *)a.out + sp.out_off + tok[r] * a.out_t + head[r] * a.out_h;
+#pragma unroll
+            for (int d = 0; d < Attend<T, D, RT, KT>::ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 x;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : at.acc[r][d][4 * i + j] * inv;
+                    store4(o + 32 * d + 8 * i + 4 * h, x);
+                }
+        } else {
+            const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + sp.row0 + row;
+            if (h == 0) a.part_ml[slot] = make_float2(at.m[r], l);
+            float *o = a.part_o + slot * D;
+#pragma unroll
+            for (int d = 0; d < Attend<T, D, RT, KT>::ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 x;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = at.acc[r][d][4 * i + j];
+                    store4(o + 32 * d + 8 * i + 4 * h, x);
+                }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Few rows (at most 32 per KV head and sequence): bound by reading K and V.  Four waves share the rows and deal the key tiles of 32
+// among themselves; each moves its tiles through LDS of its own, the next tile's loads in flight, without a barrier.
+// ---------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
+    using R = Row<T, D>;
+    constexpr int kTile = 32 * R::kPieces, kLoads = kTile / 64, kRowStep = 64 / R::kPieces, NW = 4;
+    __shared__ uint4 tiles[NW][2][kTile];
+    __shared__ float scratch[NW][16 * 32];
+    __shared__ float s_m[NW][32], s_l[NW][32];
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(a, blockIdx.x);
+    const PromptSpan &sp = a.s[pl.seq];
+    const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
+    const int row0 = pl.tile * 32, end_row = min(row0 + 32, n_rows);
+    const int see_all = max(0, row0 / a.G + shift + 1), see_any = max(0, (end_row - 1) / a.G + shift + 1);
+    const int n_blocks = (see_any + 31) / 32, n_full = see_all / 32;
+    const int per_split = (n_blocks + a.splits - 1) / a.splits;
+    const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
+
+    Attend<T, D, 1, 1> at;
+    at.clear();
+    const int row = min(row0 + n, n_rows - 1), tok = row / a.G, head = pl.kvh * a.G + row - tok * a.G;
+    const int last[1] = {tok + shift};
+    {
+        const T *q = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
+#pragma unroll
+        for (int sl = 0; sl < R::kSlices; ++sl) at.q[0][sl] = *reinterpret_cast<const uint4 *>(q + R::kVec * (2 * sl + h));
+    }
+    const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
+    const int piece = lane % R::kPieces, lrow = lane / R::kPieces;
+    uint4 *sk = tiles[wave][0], *sv = tiles[wave][1];
+    uint4 kr[kLoads], vr[kLoads];
+    auto load = [&](int b) {
+        const int kb = b * 32, top = sp.kv_len - 1 - kb;
+        const T *kp = kg + kb * a.k_t + R::kVec * piece, *vp = vg + kb * a.v_t + R::kVec * piece;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) kr[i] = *reinterpret_cast<const uint4 *>(kp + min(lrow + kRowStep * i, top) * a.k_t);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) vr[i] = *reinterpret_cast<const uint4 *>(vp + min(lrow + kRowStep * i, top) * a.v_t);
+    };
+    int b = b0 + wave;
+    if (b < b1) load(b);
+    for (; b < b1; b += NW) {
+        bool bad = false;
+        if (b >= n_full) {
+            const int left = sp.kv_len - b * 32;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if (lrow + kRowStep * i >= left) vr[i] = make_uint4(0, 0, 0, 0);
+                bad = bad || not_finite(vr[i], T());
+            }
+            bad = __ballot(bad) != 0ull;
+        }
+        wave_sync();  // the wave's reads of the tile before are behind it
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            sk[R::k_at(lrow + kRowStep * i, piece)] = kr[i];
+            sv[R::v_at(lrow + kRowStep * i, piece)] = vr[i];
+        }
+        wave_sync();
+        if (b + NW < b1) load(b + NW);
+        if (b < n_full) at.template step<false>(sk, sv, b * 32, last, a.c, false, scratch[wave]);
+        else at.template step<true>(sk, sv, b * 32, last, a.c, bad, scratch[wave]);
+    }
+    // merge of the four waves: every wave brings its sums to the common reference and leaves them in LDS
+    const float l = at.l[0] + __shfl_xor(at.l[0], 32, 64);
+    if (h == 0) s_m[wave][n] = at.m[0];
+    __syncthreads();
+    float M = s_m[0][n];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][n]);
+    const float f = at.m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(at.m[0] - M);
+    if (h == 0) s_l[wave][n] = l * f;
+    constexpr int kQuads = D / 4;  // 16-byte pieces of a row of sums
+    static_assert(sizeof(tiles) >= NW * 32 * D * sizeof(float), "the tiles' memory holds the sums");
+    f32x4 *sums = reinterpret_cast<f32x4 *>(&tiles[0][0][0]);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4 x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = f == 0.f ? 0.f : at.acc[0][d][4 * i + j] * f;
+            sums[(wave * 32 + n) * kQuads + ((8 * d + 2 * i + h) ^ (n & 15))] = x;
+        }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < 32 * kQuads; idx += 256) {
+        const int r = idx / kQuads, c4 = idx % kQuads;
+        if (row0 + r >= n_rows) break;  // (rows ascend with idx)
+        f32x4 x = sums[r * kQuads + (c4 ^ (r & 15))];
+        float lt = s_l[0][r];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            x += sums[(w * 32 + r) * kQuads + (c4 ^ (r & 15))];
+            lt += s_l[w][r];
+        }
+        const int t = (row0 + r) / a.G, g = row0 + r - t * a.G;
+        if (a.splits == 1) {
+            const float inv = 1.0f / lt;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = lt == 0.f ? 0.f : x[j] * inv;
+            store4((T *)a.out + sp.out_off + t * a.out_t + (pl.kvh * a.G + g) * a.out_h + 4 * c4, x);
+        } else {
+            const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + sp.row0 + row0 + r;
+            if (c4 == 0) {
+                float mm = s_m[0][r];
+#pragma unroll
+                for (int w = 1; w < NW; ++w) mm = fmaxf(mm, s_m[w][r]);
+                a.part_ml[slot] = make_float2(mm, lt);
+            }
+            store4(a.part_o + slot * D + 4 * c4, x);
+        }
+    }
+}
+
+// Joins the splits of a row: one group of D / 4 lanes per (row, KV head)
+template <typename T, int D>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
+    constexpr int kQuads = D / 4;
+    const int c4 = threadIdx.x % kQuads;
+    const int64_t idx = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kQuads;
+    if (idx >= (int64_t)a.n_rows * a.Hkv) return;
+    const int kvh = (int)(idx / a.n_rows), row = (int)(idx - (int64_t)kvh * a.n_rows);
+    const int64_t stride = (int64_t)a.Hkv * a.n_rows;
+    float M = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, a.part_ml[s * stride + idx].x);
+    float l = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 ml = a.part_ml[s * stride + idx];
+        if (ml.y == 0.f) continue;  // a split that saw nothing
+        const float w = __builtin_amdgcn_exp2f(ml.x - M);
+        const f32x4 o = *reinterpret_cast<const f32x4 *>(a.part_o + (s * stride + idx) * D + 4 * c4);
+        l = fmaf(w, ml.y, l);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = fmaf(w, o[j], x[j]);
+    }
+    int seq = 0;
+    {
+        int lo = 0, hi = a.n_seqs - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (a.s[mid].row0 <= row) lo = mid;
+            else hi = mid - 1;
+        }
+        seq = lo;
+    }
+    const PromptSpan &sp = a.s[seq];
+    const int r = row - sp.row0, t = r / a.G, g = r - t * a.G;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : x[j] / l;
+    store4((T *)a.out + sp.out_off + t * a.out_t + (kvh * a.G + g) * a.out_h + 4 * c4, x);
+}
+
+// ---------------------------------------------------------------------------------------
+// The shape of a call: which kernel, how many splits, what the partial results take
+// ---------------------------------------------------------------------------------------
+struct PromptPlan {
+    bool few;
+    int tile_rows, splits;
+    int64_t n_tiles, n_rows;
+    size_t ml_bytes, bytes;
+};
+static PromptPlan plan_of(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
+    const int64_t G = c.n_q_heads / c.n_kv_heads;
+    PromptPlan p;
+    memset(&p, 0, sizeof(p));
+    int64_t most = 0, keys = 0;
+    for (int i = 0; i < n; ++i) {
+        if (seqs[i].q_len * G > most) most = seqs[i].q_len * G;
+        if (seqs[i].q_len > 0 && seqs[i].kv_len > keys) keys = seqs[i].kv_len;
+    }
+    p.few = most <= 32;
+    p.tile_rows = p.few ? 32 : 128;
+    for (int i = 0; i < n; ++i) {
+        p.n_tiles += (seqs[i].q_len * G + p.tile_rows - 1) / p.tile_rows;
+        p.n_rows += seqs[i].q_len * G;
+    }
+    p.splits = 1;
+    const int64_t wgs = p.n_tiles * c.n_kv_heads, per = p.few ? 128 : 512;
+    if (wgs > 0) {
+        while (p.splits < 64 && wgs * p.splits < kCUs && keys > p.splits * per) p.splits *= 2;
+    }
+    if (p.splits > 1) {
+        const size_t slots = (size_t)p.n_rows * c.n_kv_heads * p.splits;
+        p.ml_bytes = (slots * sizeof(float2) + 255) / 256 * 256;
+        p.bytes = p.ml_bytes + slots * c.head_dim * sizeof(float);
+    }
+    return p;
+}
+
+size_t prompt_workspace(const air_prompt_config &c, const air_prompt_seq *seqs, int n) { return plan_of(c, seqs, n).bytes; }
+
+bool prompt_grid_ok(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
+    const PromptPlan p = plan_of(c, seqs, n);
+    return p.n_rows * c.n_kv_heads < 0x7fffffffll / (c.head_dim / 4) && p.n_tiles * c.n_kv_heads * p.splits < 0x7fffffffll;
+}
+
+template <typename T, int D>
+static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &a) {
+    const dim3 grid((unsigned)(p.n_tiles * a.Hkv * p.splits));
+    if (p.few) hipLaunchKernelGGL((prompt_few_kernel<T, D>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((prompt_kernel<T, D, 4, 1, sizeof(T) == 4 ? 1 : 2>), grid, dim3(256), 0, s, a);
+    if (p.splits > 1) {
+        const int64_t threads = p.n_rows * a.Hkv * (D / 4);
+        hipLaunchKernelGGL((prompt_join_kernel<T, D>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
+    }
+}
+
+hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const air_prompt_seq *seqs, int n, const void *q, const void *k,
+                         const void *v, void *out, void *workspace) {
+    const PromptPlan p = plan_of(c, seqs, n);
+    if (p.n_rows == 0) return hipSuccess;
+    PromptArgs a;
+    memset(&a, 0, sizeof(a));
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = out;
+    a.part_ml = (float2 *)workspace;
+    a.part_o = (float *)((char *)workspace + p.ml_bytes);
+    a.q_h = c.q_h;
+    a.q_t = c.q_t;
+    a.k_h = c.k_h;
+    a.k_t = c.k_t;
+    a.v_h = c.v_h;
+    a.v_t = c.v_t;
+    a.out_h = c.out_h;
+    a.out_t = c.out_t;
+    a.G = c.n_q_heads / c.n_kv_heads;
+    a.Hkv = c.n_kv_heads;
+    a.c = (float)((c.scale > 0.f ? (double)c.scale : 1.0 / sqrt((double)c.head_dim)) * 1.4426950408889634);
+    a.splits = p.splits;
+    a.n_tiles = (int)p.n_tiles;
+    a.n_rows = (int)p.n_rows;
+    // sequences by rising length: the workgroups take the tiles from the last to the first, the longest first
+    int order[AIR_MAX_BATCH];
+    int m = 0;
+    for (int i = 0; i < n; ++i) {
+        if (seqs[i].q_len == 0) continue;
+        int at = m++;
+        for (; at > 0 && seqs[order[at - 1]].kv_len > seqs[i].kv_len; --at) order[at] = order[at - 1];
+        order[at] = i;
+    }
+    a.n_seqs = m;
+    int tile0 = 0, row0 = 0;
+    for (int i = 0; i < m; ++i) {
+        const air_prompt_seq &x = seqs[order[i]];
+        a.s[i] = PromptSpan{x.q_off, x.k_off, x.v_off, x.out_off, x.q_len, x.kv_len, tile0, row0};
+        const int rows = x.q_len * a.G;
+        tile0 += (rows + p.tile_rows - 1) / p.tile_rows;
+        row0 += rows;
+    }
+    if (c.dtype == AIR_BF16) c.head_dim == 128 ? prompt_launch<bf16_t, 128>(s, p, a) : prompt_launch<bf16_t, 64>(s, p, a);
+    else c.head_dim == 128 ? prompt_launch<float, 128>(s, p, a) : prompt_launch<float, 64>(s, p, a);
+    return hipGetLastError();
+}
+
+}  // namespace air
