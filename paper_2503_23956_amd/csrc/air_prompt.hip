@@ -81,6 +81,25 @@ __device__ __forceinline__ bool not_finite(const uint4 &x, float) {
     return bad;
 }
 
+// the elements that are finite, 0 in place of the others
+__device__ __forceinline__ u32x4 finite_part(u32x4 x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = (x[i] & 0x7f80u) == 0x7f80u ? 0u : x[i] & 0xffffu;
+        const uint32_t hi = (x[i] & 0x7f800000u) == 0x7f800000u ? 0u : x[i] & 0xffff0000u;
+        x[i] = lo | hi;
+    }
+    return x;
+}
+// the eight bf16 numbers of x added to sum
+__device__ __forceinline__ float sum_of(const uint4 &x, float sum) {
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), one, sum, false);
+    return sum;
+}
 // orders the LDS accesses of the lanes of one wave
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -410,6 +429,234 @@ __global__ __launch_bounds__(64 * NW) void prompt_kernel(PromptArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------
+// Many rows, bf16: 4 waves of 32 RT rows, key blocks of 64 in LDS (three buffers), two row tiles a wave so that what is read of
+// K and V from LDS serves 64 rows.  One wave per SIMD: the logits of the next 32 keys are formed (matrix unit) while the
+// exponentials of the present ones are (vector unit), in one run of instructions without a branch.
+// ---------------------------------------------------------------------------------------
+template <typename T, int D, int RT>
+__global__ __launch_bounds__(256, 1) void prompt_pipe_kernel(PromptArgs a) {
+    using R = Row<T, D>;
+    static_assert(sizeof(T) == 2, "bf16");
+    constexpr int NW = 4, kRows = 32 * RT * NW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
+    constexpr int kTile = kKeys * R::kPieces, kLoads = kTile / 256, kRowStep = 256 / R::kPieces;
+    __shared__ u32x4 sk[kBufs][kTile], sv[kBufs][kTile];
+    __shared__ int s_bad;
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(a, blockIdx.x);
+    const PromptSpan &sp = a.s[pl.seq];
+    const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
+    const int row0 = pl.tile * kRows, end_row = min(row0 + kRows, n_rows);
+    const int see_all = max(0, row0 / a.G + shift + 1), see_any = max(0, (end_row - 1) / a.G + shift + 1);
+    const int n_blocks = (see_any + kKeys - 1) / kKeys;
+    const int per_split = (n_blocks + a.splits - 1) / a.splits;
+    const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
+
+    f32x16 acc[RT][ND];
+    float l[RT], ref[RT], top[RT], mul[RT], sub[RT];  // top: the logit (scaled) from which on the reference is raised
+    uint4 q[RT][NS];
+    int last[RT], row[RT];
+    bool huge = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        l[r] = 0.f;
+        ref[r] = top[r] = -INFINITY;
+        mul[r] = a.c;
+        sub[r] = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[r][d][i] = 0.f;
+        row[r] = row0 + 32 * (RT * wave + r) + n;
+        const int m = min(row[r], n_rows - 1), t = m / a.G, g = m - t * a.G;
+        last[r] = t + shift;
+        const T *qp = (const T *)a.q + sp.q_off + t * a.q_t + (pl.kvh * a.G + g) * a.q_h;
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) q[r][sl] = *reinterpret_cast<const uint4 *>(qp + R::kVec * (2 * sl + h));
+    }
+
+    const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
+    const int piece = threadIdx.x % R::kPieces, lrow = threadIdx.x / R::kPieces;
+    const int64_t k_lane = lrow * a.k_t + R::kVec * piece, v_lane = lrow * a.v_t + R::kVec * piece;
+    u32x4 kr[kLoads], vr[kLoads];
+    auto load = [&](int b) {
+        const int kb = b * kKeys, end = sp.kv_len - 1 - kb;
+        const T *kp = kg + kb * a.k_t, *vp = vg + kb * a.v_t;
+        if (end >= kKeys - 1) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                kr[i] = *reinterpret_cast<const u32x4 *>(kp + i * (kRowStep * a.k_t) + k_lane);
+                vr[i] = *reinterpret_cast<const u32x4 *>(vp + i * (kRowStep * a.v_t) + v_lane);
+            }
+        } else {  // rows past the last key re-read it
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = min(lrow + kRowStep * i, end);
+                kr[i] = *reinterpret_cast<const u32x4 *>(kp + r * a.k_t + R::kVec * piece);
+                vr[i] = *reinterpret_cast<const u32x4 *>(vp + r * a.v_t + R::kVec * piece);
+            }
+        }
+    };
+    auto keep = [&](int b) {
+        const int buf = b % kBufs;
+        if ((b + 1) * kKeys > see_all) {
+            // Some row does not see all of the block, and its probability of 0 must not meet an infinity: values behind the last key become
+            // 0, and so does what is not finite (added at the end to the rows that see it)
+            const int left = sp.kv_len - b * kKeys;
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if (lrow + kRowStep * i >= left) vr[i] = (u32x4){0, 0, 0, 0};
+                if (not_finite(__builtin_bit_cast(uint4, vr[i]), T())) {
+                    bad = true;
+                    vr[i] = finite_part(vr[i]);
+                }
+            }
+            if (bad) s_bad = 1;
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            sk[buf][R::k_at(lrow + kRowStep * i, piece)] = kr[i];
+            sv[buf][R::v_at(lrow + kRowStep * i, piece)] = vr[i];
+        }
+    };
+    // logits of the 32 keys whose tile starts at sk_
+    auto logits = [&](f32x16(&s)[RT], const u32x4 *sk_) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[r][i] = 0.f;
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) {
+            const uint4 x = __builtin_bit_cast(uint4, sk_[R::k_at(n, 2 * sl + h)]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) s[r] = mma32(x, q[r][sl], s[r], T());
+        }
+    };
+    // masks, reference: what has to be known of the logits of the keys from kb on before their exponentials are formed
+    auto settle = [&](f32x16(&s)[RT], int kb) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            if (kb + 32 > see_all) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (kb + 8 * (i >> 2) + 4 * h + (i & 3) > last[r]) s[r][i] = -INFINITY;
+            }
+            float mx = s[r][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[r][i]);
+            mx *= a.c;
+            if (__ballot(mx > top[r]) != 0ull) {
+                const float now = fmaxf(ref[r], fmaxf(mx, __shfl_xor(mx, 32, 64)));
+                const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - now);  // no logit but -inf yet: nothing to scale
+                l[r] *= f;
+                ref[r] = now;
+                top[r] = now + kSlack;
+                sub[r] = now == -INFINITY ? 0.f : now;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[r][d][i] *= f;
+                huge = huge || __ballot(fabsf(sub[r]) > kHuge) != 0ull;
+            }
+            if (huge) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[r][i] = rounded_exponent(s[r][i], a.c, ref[r] == -INFINITY ? 0.f : ref[r]);
+                mul[r] = 1.f;
+                sub[r] = 0.f;
+            }
+        }
+    };
+    const int krow = 4 * h + ((lane & 15) >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    // the next 32 keys' logits into `next` while this 32 keys' values are weighed
+    auto turn = [&](f32x16(&s)[RT], f32x16(&next)[RT], const u32x4 *sk_next, const u32x4 *sv_) {
+        logits(next, sk_next);
+        uint4 p[RT][2];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                bf16x8 x;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[r][8 * half + i], mul[r], -sub[r]));
+                p[r][half] = __builtin_bit_cast(uint4, x);
+                // the sum of what the second product takes: the weights add up to one as they are used
+                l[r] = sum_of(p[r][half], l[r]);
+            }
+        const char *base = reinterpret_cast<const char *>(sv_) + 8 * (lane & 1);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const char *at = base + 16 * R::v_at(16 * half + krow, 4 * d + vpiece);
+                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                struct { s16x4 a, b; } v;
+                v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+                v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * D * sizeof(T)));
+#pragma unroll
+                for (int r = 0; r < RT; ++r) acc[r][d] = mma32(__builtin_bit_cast(uint4, v), p[r][half], acc[r][d], T());
+            }
+    };
+    if (threadIdx.x == 0) s_bad = 0;
+    __syncthreads();
+    if (b0 < b1) {
+        f32x16 sa[RT], sb[RT];
+        load(b0);
+        keep(b0);
+        if (b0 + 1 < b1) load(b0 + 1);
+        lds_barrier();
+        logits(sa, sk[b0 % kBufs]);
+        settle(sa, b0 * kKeys);
+        for (int b = b0; b < b1; ++b) {
+            const u32x4 *k_now = sk[b % kBufs], *v_now = sv[b % kBufs], *k_next = sk[(b + 1) % kBufs];
+            if (b + 1 < b1) keep(b + 1);
+            if (b + 2 < b1) load(b + 2);
+            turn(sa, sb, k_now + 32 * R::kPieces, v_now);
+            settle(sb, b * kKeys + 32);
+            lds_barrier();
+            turn(sb, sa, k_next, v_now + 32 * R::kPieces);  // (behind the last block: logits of whatever lies there, not used)
+            if (b + 1 < b1) settle(sa, (b + 1) * kKeys);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const float sum = l[r] + __shfl_xor(l[r], 32, 64);
+        if (row[r] >= n_rows) continue;
+        if (s_bad) {  // values that are not finite, at keys that some row does not see
+            for (int key = max(b0 * kKeys, see_all / kKeys * kKeys); key < min(b1 * kKeys, see_any); ++key) {
+                if (key > last[r]) continue;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float v = ldf(vg + key * a.v_t + 32 * d + 8 * (i >> 2) + 4 * h + (i & 3));
+                        if (!(fabsf(v) < INFINITY)) acc[r][d][i] += v;
+                    }
+            }
+        }
+        const int t = row[r] / a.G, head = pl.kvh * a.G + row[r] - t * a.G;
+        const bool whole = a.splits == 1;
+        const float inv = whole ? 1.0f / sum : 1.0f;
+        const bool none = whole && sum == 0.f;
+        const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + sp.row0 + row[r];
+        if (!whole && h == 0) a.part_ml[slot] = make_float2(ref[r], sum);
+        T *o = (T *)a.out + sp.out_off + t * a.out_t + head * a.out_h;
+        float *po = a.part_o + slot * D;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f32x4 x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = none ? 0.f : acc[r][d][4 * i + j] * inv;
+                const int col = 32 * d + 8 * i + 4 * h;
+                if (whole) store4(o + col, x);
+                else store4(po + col, x);
+            }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
 // Few rows (at most 32 per KV head and sequence): bound by reading K and V.  Four waves share the rows and deal the key tiles of 32
 // among themselves; each moves its tiles through LDS of its own, the next tile's loads in flight, without a barrier.
 // ---------------------------------------------------------------------------------------
@@ -585,7 +832,7 @@ static PromptPlan plan_of(const air_prompt_config &c, const air_prompt_seq *seqs
         if (seqs[i].q_len > 0 && seqs[i].kv_len > keys) keys = seqs[i].kv_len;
     }
     p.few = most <= 32;
-    p.tile_rows = p.few ? 32 : 128;
+    p.tile_rows = p.few ? 32 : (c.dtype == AIR_BF16 ? 256 : 128);
     for (int i = 0; i < n; ++i) {
         p.n_tiles += (seqs[i].q_len * G + p.tile_rows - 1) / p.tile_rows;
         p.n_rows += seqs[i].q_len * G;
@@ -614,7 +861,8 @@ template <typename T, int D>
 static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &a) {
     const dim3 grid((unsigned)(p.n_tiles * a.Hkv * p.splits));
     if (p.few) hipLaunchKernelGGL((prompt_few_kernel<T, D>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((prompt_kernel<T, D, 4, 1, sizeof(T) == 4 ? 1 : 2>), grid, dim3(256), 0, s, a);
+    else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 2>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((prompt_kernel<T, D, 4, 1, 1>), grid, dim3(256), 0, s, a);
     if (p.splits > 1) {
         const int64_t threads = p.n_rows * a.Hkv * (D / 4);
         hipLaunchKernelGGL((prompt_join_kernel<T, D>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
