@@ -433,12 +433,12 @@ __global__ __launch_bounds__(64 * NW) void prompt_kernel(PromptArgs a) {
 // K and V from LDS serves 64 rows.  One wave per SIMD: the logits of the next 32 keys are formed (matrix unit) while the
 // exponentials of the present ones are (vector unit), in one run of instructions without a branch.
 // ---------------------------------------------------------------------------------------
-template <typename T, int D, int RT>
-__global__ __launch_bounds__(256, 1) void prompt_pipe_kernel(PromptArgs a) {
+template <typename T, int D, int RT, int NW>
+__global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs a) {
     using R = Row<T, D>;
     static_assert(sizeof(T) == 2, "bf16");
-    constexpr int NW = 4, kRows = 32 * RT * NW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
-    constexpr int kTile = kKeys * R::kPieces, kLoads = kTile / 256, kRowStep = 256 / R::kPieces;
+    constexpr int kRows = 32 * RT * NW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
+    constexpr int kTile = kKeys * R::kPieces, kLoads = kTile / (64 * NW), kRowStep = 64 * NW / R::kPieces;
     __shared__ u32x4 sk[kBufs][kTile], sv[kBufs][kTile];
     __shared__ int s_bad;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(256, 1) void prompt_pipe_kernel(PromptArgs a) {
     auto settle = [&](f32x16(&s)[RT], int kb) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            if (kb + 32 > see_all) {
+            if (__builtin_expect(kb + 32 > see_all, 0)) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (kb + 8 * (i >> 2) + 4 * h + (i & 3) > last[r]) s[r][i] = -INFINITY;
@@ -546,7 +546,7 @@ __global__ __launch_bounds__(256, 1) void prompt_pipe_kernel(PromptArgs a) {
 #pragma unroll
             for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[r][i]);
             mx *= a.c;
-            if (__ballot(mx > top[r]) != 0ull) {
+            if (__builtin_expect(__ballot(mx > top[r]) != 0ull, 0)) {
                 const float now = fmaxf(ref[r], fmaxf(mx, __shfl_xor(mx, 32, 64)));
                 const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - now);  // no logit but -inf yet: nothing to scale
                 l[r] *= f;
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(256, 1) void prompt_pipe_kernel(PromptArgs a) {
                     for (int i = 0; i < 16; ++i) acc[r][d][i] *= f;
                 huge = huge || __ballot(fabsf(sub[r]) > kHuge) != 0ull;
             }
-            if (huge) {
+            if (__builtin_expect(huge, 0)) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[r][i] = rounded_exponent(s[r][i], a.c, ref[r] == -INFINITY ? 0.f : ref[r]);
                 mul[r] = 1.f;
@@ -861,7 +861,7 @@ template <typename T, int D>
 static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &a) {
     const dim3 grid((unsigned)(p.n_tiles * a.Hkv * p.splits));
     if (p.few) hipLaunchKernelGGL((prompt_few_kernel<T, D>), grid, dim3(256), 0, s, a);
-    else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 2>), grid, dim3(256), 0, s, a);
+    else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 1, 8>), grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL((prompt_kernel<T, D, 4, 1, 1>), grid, dim3(256), 0, s, a);
     if (p.splits > 1) {
         const int64_t threads = p.n_rows * a.Hkv * (D / 4);
