@@ -46,12 +46,14 @@ struct PromptArgs {
 template <typename T, int D>
 struct Row {
     static constexpr int kVec = Elem<T>::kVec, kPieces = D / kVec, kSlices = kPieces / 2;
-    // Where piece p of key r lies in its tile.  K: read 16 bytes a lane, one row per lane: neighbouring rows' pieces in different
-    // banks.  V in bf16: read transposed, four rows x 32 bytes per 16 lanes: neighbouring rows' pairs of pieces in different banks; in
-    // fp32 a row at a time.
-    static __device__ __forceinline__ int k_at(int r, int p) { return r * kPieces + (p ^ (r & (kPieces < 16 ? kPieces - 1 : 15))); }
+    // Where piece p of key r lies in its tile (64 banks of 4 bytes: 256 bytes of a tile are read at a time).
+    // K: 16 bytes a lane, a row per lane: 16 neighbouring rows' pieces p lie in different banks.  V in bf16: read transposed, 32 lanes take
+    // four rows x two neighbouring pairs of pieces: eight different pairs; in fp32 half a wave takes 128 bytes of row r, the
+    // other half those of row r + 4.
+    static __device__ __forceinline__ int k_at(int r, int p) { return r * kPieces + (p ^ (kPieces == 8 ? (r >> 1) & 7 : r & 15)); }
     static __device__ __forceinline__ int v_at(int r, int p) {
-        return r * kPieces + (sizeof(T) == 2 ? p ^ ((r & (kPieces / 2 - 1)) << 1) : p);
+        if (sizeof(T) == 4) return r * kPieces + (p ^ ((r & 4) << 1));
+        return r * kPieces + (p ^ (kPieces == 8 ? (r & 2) << 1 : ((r & 3) << 2) | ((r & 4) >> 1)));
     }
 };
 
@@ -260,14 +262,14 @@ struct Attend {
                     }
                 }
         } else {
-            const float *base = reinterpret_cast<const float *>(sv) + 4 * h * D + n;
+            const float *base = reinterpret_cast<const float *>(sv) + 4 * h * D;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
-                        const float v = base[(32 * kt + 8 * (i >> 2) + (i & 3)) * D + 32 * d];
+                        const float v = base[(32 * kt + 8 * (i >> 2) + (i & 3)) * D + ((32 * d + n) ^ (32 * h))];
 #pragma unroll
                         for (int r = 0; r < RT; ++r)
                             acc[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r][kt][i], acc[r][d], 0, 0, 0);
