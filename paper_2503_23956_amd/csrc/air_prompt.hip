@@ -522,34 +522,40 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
             sv[buf][R::v_at(lrow + kRowStep * i, piece)] = vr[i];
         }
     };
-    // logits of the 32 keys whose tile starts at sk_
-    auto logits = [&](f32x16(&s)[RT], const u32x4 *sk_) {
+    // operands of the logits of the 32 keys whose tile starts at sk_
+    auto read_k = [&](u32x4(&x)[NS], const u32x4 *sk_) {
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) x[sl] = sk_[R::k_at(n, 2 * sl + h)];
+    };
+    auto largest = [&](const f32x16 &s) {
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        return mx;
+    };
+    auto logits = [&](f32x16(&s)[RT], const u32x4(&x)[NS]) {
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[r][i] = 0.f;
 #pragma unroll
-        for (int sl = 0; sl < NS; ++sl) {
-            const uint4 x = __builtin_bit_cast(uint4, sk_[R::k_at(n, 2 * sl + h)]);
+        for (int sl = 0; sl < NS; ++sl)
 #pragma unroll
-            for (int r = 0; r < RT; ++r) s[r] = mma32(x, q[r][sl], s[r], T());
-        }
+            for (int r = 0; r < RT; ++r) s[r] = mma32(__builtin_bit_cast(uint4, x[sl]), q[r][sl], s[r], T());
     };
     // masks, reference: what has to be known of the logits of the keys from kb on before their exponentials are formed
-    auto settle = [&](f32x16(&s)[RT], int kb) {
+    auto settle = [&](f32x16(&s)[RT], float(&mx)[RT], int kb) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             if (__builtin_expect(kb + 32 > see_all, 0)) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (kb + 8 * (i >> 2) + 4 * h + (i & 3) > last[r]) s[r][i] = -INFINITY;
+                mx[r] = largest(s[r]);
             }
-            float mx = s[r][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[r][i]);
-            mx *= a.c;
-            if (__builtin_expect(__ballot(mx > top[r]) != 0ull, 0)) {
-                const float now = fmaxf(ref[r], fmaxf(mx, __shfl_xor(mx, 32, 64)));
+            mx[r] *= a.c;
+            if (__builtin_expect(__ballot(mx[r] > top[r]) != 0ull, 0)) {
+                const float now = fmaxf(ref[r], fmaxf(mx[r], __shfl_xor(mx[r], 32, 64)));
                 const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - now);  // no logit but -inf yet: nothing to scale
                 l[r] *= f;
                 ref[r] = now;
@@ -570,9 +576,25 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
         }
     };
     const int krow = 4 * h + ((lane & 15) >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    // the next 32 keys' logits into `next` while this 32 keys' values are weighed
-    auto turn = [&](f32x16(&s)[RT], f32x16(&next)[RT], const u32x4 *sk_next, const u32x4 *sv_) {
-        logits(next, sk_next);
+    auto read_v = [&](u32x4(&x)[ND], const u32x4 *sv_, int half) {
+        const char *base = reinterpret_cast<const char *>(sv_) + 8 * (lane & 1);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            const char *at = base + 16 * R::v_at(16 * half + krow, 4 * d + vpiece);
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            struct { s16x4 a, b; } v;
+            v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+            v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * D * sizeof(T)));
+            x[d] = __builtin_bit_cast(u32x4, v);
+        }
+    };
+    // The next 32 keys' logits into `next` (operands: kf) while this 32 keys' values are weighed; kf then takes the operands of the keys
+    // behind those.  `meet`: the tiles that k_after points to are whole only behind a barrier.
+    auto turn = [&](f32x16(&s)[RT], f32x16(&next)[RT], float(&mx)[RT], u32x4(&kf)[NS], const u32x4 *sv_, const u32x4 *k_after, bool meet) {
+        u32x4 vf[2][ND];
+        __builtin_amdgcn_s_setprio(1);
+        read_v(vf[0], sv_, 0);
+        logits(next, kf);
         uint4 p[RT][2];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
@@ -582,42 +604,65 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[r][8 * half + i], mul[r], -sub[r]));
                 p[r][half] = __builtin_bit_cast(uint4, x);
-                // the sum of what the second product takes: the weights add up to one as they are used
-                l[r] = sum_of(p[r][half], l[r]);
             }
-        const char *base = reinterpret_cast<const char *>(sv_) + 8 * (lane & 1);
+        read_v(vf[1], sv_, 1);
+        if (meet) lds_barrier();
+        read_k(kf, k_after);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                const char *at = base + 16 * R::v_at(16 * half + krow, 4 * d + vpiece);
-                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                struct { s16x4 a, b; } v;
-                v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-                v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * D * sizeof(T)));
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) acc[r][d] = mma32(__builtin_bit_cast(uint4, v), p[r][half], acc[r][d], T());
+                for (int r = 0; r < RT; ++r) acc[r][d] = mma32(__builtin_bit_cast(uint4, vf[half][d]), p[r][half], acc[r][d], T());
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            // the sum of what the second product takes: the weights add up to one as they are used
+            l[r] = sum_of(p[r][1], sum_of(p[r][0], l[r]));
+            mx[r] = largest(next[r]);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (!meet) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, RT, 0);
+                __builtin_amdgcn_sched_group_barrier(0x2, 40 / NS, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
+
+#pragma unroll
+            for (int i = 0; i < 2 * ND; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, RT, 0);
+                __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+        }
     };
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
     if (b0 < b1) {
         f32x16 sa[RT], sb[RT];
+        float mx[RT];
+        u32x4 kf[NS];
         load(b0);
         keep(b0);
         if (b0 + 1 < b1) load(b0 + 1);
         lds_barrier();
-        logits(sa, sk[b0 % kBufs]);
-        settle(sa, b0 * kKeys);
+        read_k(kf, sk[b0 % kBufs]);
+        logits(sa, kf);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) mx[r] = largest(sa[r]);
+        settle(sa, mx, b0 * kKeys);
+        read_k(kf, sk[b0 % kBufs] + 32 * R::kPieces);
         for (int b = b0; b < b1; ++b) {
-            const u32x4 *k_now = sk[b % kBufs], *v_now = sv[b % kBufs], *k_next = sk[(b + 1) % kBufs];
+            const u32x4 *v_now = sv[b % kBufs], *k_next = sk[(b + 1) % kBufs];
             if (b + 1 < b1) keep(b + 1);
             if (b + 2 < b1) load(b + 2);
-            turn(sa, sb, k_now + 32 * R::kPieces, v_now);
-            settle(sb, b * kKeys + 32);
-            lds_barrier();
-            turn(sb, sa, k_next, v_now + 32 * R::kPieces);  // (behind the last block: logits of whatever lies there, not used)
-            if (b + 1 < b1) settle(sa, (b + 1) * kKeys);
+            turn(sa, sb, mx, kf, v_now, k_next, true);
+            settle(sb, mx, b * kKeys + 32);
+            // (behind the last block: logits of whatever lies there, not used)
+            turn(sb, sa, mx, kf, v_now + 32 * R::kPieces, k_next + 32 * R::kPieces, false);
+            if (b + 1 < b1) settle(sa, mx, (b + 1) * kKeys);
         }
     }
 #pragma unroll
