@@ -821,43 +821,78 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     }
 }
 
-// Joins the splits of a row: one group of D / 4 lanes per (row, KV head)
+// Joins the splits of a row.  D / 4 lanes hold a row's columns; `groups` of them (a power of two) share its splits, so that the partial
+// results of a long row are all in flight at once.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
-    constexpr int kQuads = D / 4;
-    const int c4 = threadIdx.x % kQuads;
-    const int64_t idx = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kQuads;
-    if (idx >= (int64_t)a.n_rows * a.Hkv) return;
-    const int kvh = (int)(idx / a.n_rows), row = (int)(idx - (int64_t)kvh * a.n_rows);
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int groups) {
+    constexpr int kQuads = D / 4, kRound = 8;
+    __shared__ f32x4 s_x[256];
+    __shared__ float2 s_ml[256 / kQuads];
+    const int c4 = threadIdx.x % kQuads, team = threadIdx.x / kQuads, g = team & (groups - 1);
+    const int64_t idx = (int64_t)blockIdx.x * (256 / kQuads / groups) + team / groups;
+    const bool live = idx < (int64_t)a.n_rows * a.Hkv;
     const int64_t stride = (int64_t)a.Hkv * a.n_rows;
-    float M = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, a.part_ml[s * stride + idx].x);
-    float l = 0.f;
+    float m = -INFINITY, l = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 ml = a.part_ml[s * stride + idx];
-        if (ml.y == 0.f) continue;  // a split that saw nothing
-        const float w = __builtin_amdgcn_exp2f(ml.x - M);
-        const f32x4 o = *reinterpret_cast<const f32x4 *>(a.part_o + (s * stride + idx) * D + 4 * c4);
-        l = fmaf(w, ml.y, l);
+    for (int s0 = g; live && s0 < a.splits; s0 += kRound * groups) {
+        float2 ml[kRound];
+        f32x4 o[kRound];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = fmaf(w, o[j], x[j]);
-    }
-    int seq = 0;
-    {
-        int lo = 0, hi = a.n_seqs - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.s[mid].row0 <= row) lo = mid;
-            else hi = mid - 1;
+        for (int i = 0; i < kRound; ++i) {
+            const int64_t slot = min(s0 + i * groups, a.splits - 1) * stride + idx;
+            ml[i] = a.part_ml[slot];
+            o[i] = *reinterpret_cast<const f32x4 *>(a.part_o + slot * D + 4 * c4);
         }
-        seq = lo;
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) top = fmaxf(top, ml[i].x);
+        if (top == -INFINITY) top = 0.f;
+        const float f = __builtin_amdgcn_exp2f(m - top);
+        l *= f;
+        x *= f;
+        m = top;
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            if (s0 + i * groups >= a.splits || ml[i].y == 0.f) continue;  // (a split that saw nothing left nothing)
+            const float w = __builtin_amdgcn_exp2f(ml[i].x - m);
+            l = fmaf(w, ml[i].y, l);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = fmaf(w, o[i][j], x[j]);
+        }
     }
-    const PromptSpan &sp = a.s[seq];
-    const int r = row - sp.row0, t = r / a.G, g = r - t * a.G;
+    if (groups > 1) {
+        s_x[threadIdx.x] = x;
+        if (c4 == 0) s_ml[team] = make_float2(m, l);
+        __syncthreads();
+        if (g != 0) return;
+        float top = m;
+        for (int i = 1; i < groups; ++i) top = fmaxf(top, s_ml[team + i].x);
+        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        l *= f;
+        x *= f;
+        for (int i = 1; i < groups; ++i) {
+            const float2 ml = s_ml[team + i];
+            if (ml.y == 0.f) continue;
+            const float w = __builtin_amdgcn_exp2f(ml.x - top);
+            l = fmaf(w, ml.y, l);
+            const f32x4 o = s_x[threadIdx.x + i * kQuads];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = fmaf(w, o[j], x[j]);
+        }
+    }
+    if (!live) return;
+    const int kvh = (int)(idx / a.n_rows), row = (int)(idx - (int64_t)kvh * a.n_rows);
+    int lo = 0, hi = a.n_seqs - 1;  // last sequence whose first row is not behind `row`
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.s[mid].row0 <= row) lo = mid;
+        else hi = mid - 1;
+    }
+    const PromptSpan &sp = a.s[lo];
+    const int r = row - sp.row0, t = r / a.G, q = r - t * a.G;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : x[j] / l;
-    store4((T *)a.out + sp.out_off + t * a.out_t + (kvh * a.G + g) * a.out_h + 4 * c4, x);
+    store4((T *)a.out + sp.out_off + t * a.out_t + (kvh * a.G + q) * a.out_h + 4 * c4, x);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -911,8 +946,11 @@ static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &
     else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 1, 8>), grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL((prompt_kernel<T, D, 4, 1, 1>), grid, dim3(256), 0, s, a);
     if (p.splits > 1) {
-        const int64_t threads = p.n_rows * a.Hkv * (D / 4);
-        hipLaunchKernelGGL((prompt_join_kernel<T, D>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
+        constexpr int kMost = 256 / (D / 4);
+        int groups = 1;
+        while (groups < kMost && groups * 2 <= p.splits) groups *= 2;
+        const int64_t per = kMost / groups, rows = p.n_rows * a.Hkv;
+        hipLaunchKernelGGL((prompt_join_kernel<T, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, s, a, groups);
     }
 }
 
