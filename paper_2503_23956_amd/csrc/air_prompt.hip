@@ -28,8 +28,6 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 struct PromptSpan {
     int64_t q_off, k_off, v_off, out_off;
     int32_t q_len, kv_len;
-    int32_t tile0;  // first row tile of the sequence in the launch
-    int32_t row0;   // first row (query x query head of the group) of the sequence in the partial results
 };
 struct PromptArgs {
     const void *q, *k, *v;
@@ -39,8 +37,16 @@ struct PromptArgs {
     int64_t q_h, q_t, k_h, k_t, v_h, v_t, out_h, out_t;
     float c;  // scale * log2(e)
     int32_t G, Hkv, n_seqs, n_tiles, n_rows, splits;
+    int32_t tile0[AIR_MAX_BATCH];  // first row tile of a sequence in the launch; behind the last sequence: INT32_MAX
+    int32_t row0[AIR_MAX_BATCH];   // first row (query x query head of the group) in the partial results, likewise
     PromptSpan s[AIR_MAX_BATCH];
 };
+static_assert(AIR_MAX_BATCH == 64 && sizeof(PromptArgs) <= 4096, "one lane per sequence; the size of an argument block");
+
+// the last sequence whose first tile (row) is not behind x: one load for all sequences, not a chain of them
+__device__ __forceinline__ int sequence_of(const int32_t *first, int x) {
+    return __popcll(__ballot(first[threadIdx.x & 63] <= x)) - 1;
+}
 
 // What the wave functions need of the storage type: CH 16-byte pieces of a row, slices of 32 bytes (one piece per lane half)
 template <typename T, int D>
@@ -300,14 +306,8 @@ __device__ __forceinline__ Place place_of(const PromptArgs &a, int w) {
     const int y = x / a.splits;
     p.split = x - y * a.splits;
     const int tile = a.n_tiles - 1 - y;
-    int lo = 0, hi = a.n_seqs - 1;  // last sequence whose first tile is not behind `tile`
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.s[mid].tile0 <= tile) lo = mid;
-        else hi = mid - 1;
-    }
-    p.seq = lo;
-    p.tile = tile - a.s[lo].tile0;
+    p.seq = a.n_seqs == 1 ? 0 : sequence_of(a.tile0, tile);
+    p.tile = tile - (a.n_seqs == 1 ? 0 : a.tile0[p.seq]);
     return p;
 }
 
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(64 * NW) void prompt_kernel(PromptArgs a) {
                     store4(o + 32 * d + 8 * i + 4 * h, x);
                 }
         } else {
-            const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + sp.row0 + row;
+            const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + a.row0[pl.seq] + row;
             if (h == 0) a.part_ml[slot] = make_float2(at.m[r], l);
             float *o = a.part_o + slot * D;
 #pragma unroll
@@ -685,7 +685,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
         const bool whole = a.splits == 1;
         const float inv = whole ? 1.0f / sum : 1.0f;
         const bool none = whole && sum == 0.f;
-        const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + sp.row0 + row[r];
+        const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + a.row0[pl.seq] + row[r];
         if (!whole && h == 0) a.part_ml[slot] = make_float2(ref[r], sum);
         T *o = (T *)a.out + sp.out_off + t * a.out_t + head * a.out_h;
         float *po = a.part_o + slot * D;
@@ -809,7 +809,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
             for (int j = 0; j < 4; ++j) x[j] = lt == 0.f ? 0.f : x[j] * inv;
             store4((T *)a.out + sp.out_off + t * a.out_t + (pl.kvh * a.G + g) * a.out_h + 4 * c4, x);
         } else {
-            const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + sp.row0 + row0 + r;
+            const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + a.row0[pl.seq] + row0 + r;
             if (c4 == 0) {
                 float mm = s_m[0][r];
 #pragma unroll
@@ -882,14 +882,11 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
     }
     if (!live) return;
     const int kvh = (int)(idx / a.n_rows), row = (int)(idx - (int64_t)kvh * a.n_rows);
-    int lo = 0, hi = a.n_seqs - 1;  // last sequence whose first row is not behind `row`
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.s[mid].row0 <= row) lo = mid;
-        else hi = mid - 1;
-    }
-    const PromptSpan &sp = a.s[lo];
-    const int r = row - sp.row0, t = r / a.G, q = r - t * a.G;
+    int seq = 0;  // (lanes differ in their row: no vote here)
+    for (int step = 32; step > 0; step >>= 1)
+        if (a.row0[seq + step] <= row) seq += step;
+    const PromptSpan &sp = a.s[seq];
+    const int r = row - a.row0[seq], t = r / a.G, q = r - t * a.G;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : x[j] / l;
     store4((T *)a.out + sp.out_off + t * a.out_t + (kvh * a.G + q) * a.out_h + 4 * c4, x);
@@ -991,9 +988,12 @@ hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const air_pr
     }
     a.n_seqs = m;
     int tile0 = 0, row0 = 0;
+    for (int i = 0; i < AIR_MAX_BATCH; ++i) a.tile0[i] = a.row0[i] = 0x7fffffff;
     for (int i = 0; i < m; ++i) {
         const air_prompt_seq &x = seqs[order[i]];
-        a.s[i] = PromptSpan{x.q_off, x.k_off, x.v_off, x.out_off, x.q_len, x.kv_len, tile0, row0};
+        a.s[i] = PromptSpan{x.q_off, x.k_off, x.v_off, x.out_off, x.q_len, x.kv_len};
+        a.tile0[i] = tile0;
+        a.row0[i] = row0;
         const int rows = x.q_len * a.G;
         tile0 += (rows + p.tile_rows - 1) / p.tile_rows;
         row0 += rows;

@@ -72,7 +72,6 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     int pos[3] = {0, 0, 0};
     if (a.positions) {
         pos[0] = a.positions[row];
-        if (pos[0] < 0) return;  // padding
         if (a.n_axes > 1) pos[1] = a.positions[(int64_t)a.rows + row];
         if (a.n_axes > 2) pos[2] = a.positions[2 * (int64_t)a.rows + row];
     }
@@ -91,6 +90,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         x0[r] = *reinterpret_cast<const uint4 *>(s + kVec * p0);
         x1[r] = *reinterpret_cast<const uint4 *>(s + kVec * p1);
     }
+    if (pos[0] < 0) return;  // padding (the position was requested together with the row)
     if (which < 2) {
         float cs[kVec], sn[kVec], w0[kVec], w1[kVec];
         if (t.weight) {
@@ -163,7 +163,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 template <typename T, int D, bool HALF>
 static hipError_t rope_launch(hipStream_t s, RopeArgs &a) {
     constexpr int kLanes = D / (2 * Elem<T>::kVec), kRun = 4;
-    const bool few = a.rows < 64;
+    // runs of four heads once the launch then still has 1024 workgroups or so: fewer are bound by their latency
+    const bool few = a.rows * (int64_t)kLanes * (a.heads[0] + a.heads[1] + a.heads[2]) < (int64_t)kRun * 256 * 1024;
     const int threads = few ? 64 : 256, run = few ? 1 : kRun;
     int64_t runs = 0;
     for (int i = 0; i < 3; ++i) runs += a.runs[i] = (a.heads[i] + run - 1) / run;

@@ -85,7 +85,7 @@ def test_against_fp64(dtype, d, half, pairs):
         assert torch.equal(outs[2], v)
 
 
-def test_padding_rows_are_neither_read_nor_written():
+def test_padding_rows_are_left_as_they_are():
     import torch
 
     import paper_2503_23956_amd as A
