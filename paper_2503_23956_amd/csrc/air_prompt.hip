@@ -73,30 +73,19 @@ __device__ __forceinline__ f32x16 mma32(const uint4 &a, const uint4 &b, f32x16 a
     return acc;
 }
 
-// all exponent bits set in one of the elements
-__device__ __forceinline__ bool not_finite(const uint4 &x, bf16_t) {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) bad = bad || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-    return bad;
-}
-__device__ __forceinline__ bool not_finite(const uint4 &x, float) {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) bad = bad || (w[i] & 0x7f800000u) == 0x7f800000u;
-    return bad;
-}
-
 // the elements that are finite, 0 in place of the others
-__device__ __forceinline__ u32x4 finite_part(u32x4 x) {
+__device__ __forceinline__ u32x4 finite_part(u32x4 x, bf16_t) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t lo = (x[i] & 0x7f80u) == 0x7f80u ? 0u : x[i] & 0xffffu;
         const uint32_t hi = (x[i] & 0x7f800000u) == 0x7f800000u ? 0u : x[i] & 0xffff0000u;
         x[i] = lo | hi;
     }
+    return x;
+}
+__device__ __forceinline__ u32x4 finite_part(u32x4 x, float) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (x[i] & 0x7f800000u) == 0x7f800000u ? 0u : x[i];
     return x;
 }
 // the eight bf16 numbers of x added to sum
@@ -107,6 +96,12 @@ __device__ __forceinline__ float sum_of(const uint4 &x, float sum) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), one, sum, false);
     return sum;
+}
+__device__ __forceinline__ float largest(const f32x16 &s) {
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    return mx;
 }
 // orders the LDS accesses of the lanes of one wave
 __device__ __forceinline__ void wave_sync() {
@@ -121,168 +116,176 @@ __device__ __forceinline__ float rounded_exponent(float s, float c, float ref) {
     return x - ref;
 }
 
+// The reference is a rounded product, the exponent an exact one minus it: the largest logit's exponent is off zero by half a step of the
+// reference, the same for all keys of the row, so that it cancels.  Beyond kHuge (no trained model's logits) that step leaves fp32's
+// range of exponents: there the product is rounded as the reference was.
 constexpr float kHuge = 0x1p26f;
 constexpr float kSlack = 8.0f;  // probabilities may be as large as 2^8: fp32 sums and bf16 operands hold them without loss
 
-// RT row tiles of 32 of one wave against KT key tiles of 32 in LDS
-template <typename T, int D, int RT, int KT>
+// Operand V^T of output tile d for the keys 16 half .. 16 half + 15 of a tile, in the order that the logits' registers have: the transposed
+// read gives a lane four keys of a column; its address is that of row (lane % 16) / 4 of them, 8 bytes at columns
+// 16 ((lane / 16) % 2) + 4 (lane % 4).
+template <int D>
+__device__ __forceinline__ uint4 read_v(const char *sv, int half, int d) {
+    const int lane = threadIdx.x & 63;
+    const int row = 4 * (lane >> 5) + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const char *at = sv + 8 * (lane & 1) + 16 * Row<bf16_t, D>::v_at(16 * half + row, 4 * d + piece);
+    struct { s16x4 a, b; } v;
+    v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+    v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * D * sizeof(bf16_t)));
+    return __builtin_bit_cast(uint4, v);
+}
+
+// One row tile of 32 of a wave against a tile of 32 keys in LDS
+template <typename T, int D>
 struct Attend {
     using R = Row<T, D>;
     static constexpr int ND = D / 32;  // output tiles of 32 columns
-    f32x16 acc[RT][ND];
-    float m[RT], l[RT];  // reference (scaled logits), this lane's part of the sum
-    uint4 q[RT][R::kSlices];
+    f32x16 acc[ND];
+    float m, l;  // reference (scaled logits), this lane's part of the sum
+    uint4 q[R::kSlices];
 
     __device__ __forceinline__ void clear() {
+        m = -INFINITY;
+        l = 0.f;
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            m[r] = -INFINITY;
-            l[r] = 0.f;
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+    }
+
+    // last: last key of the tile that the lane's query sees, counted from the tile's first (read when masked, uniform over the wave)
+    __device__ __forceinline__ void step(const u32x4 *sk, const u32x4 *sv, bool masked, int last, float c) {
+        const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int sl = 0; sl < R::kSlices; ++sl) s = mma32(__builtin_bit_cast(uint4, sk[R::k_at(n, 2 * sl + h)]), q[sl], s, T());
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + 4 * h + (i & 3) > last) s[i] = -INFINITY;
+        }
+        const float mx = largest(s) * c;
+        if (__ballot(mx > m + kSlack) != 0ull) {
+            const float m_new = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32, 64)));
+            const float f = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);  // no logit but -inf yet: nothing to scale
+            l *= f;
+            m = m_new;
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[r][d][i] = 0.f;
+                for (int i = 0; i < 16; ++i) acc[d][i] *= f;
         }
-    }
-
-    // kb: first key of the tile in the sequence; last[r]: last key that the lane's query of row tile r sees (read when MASKED);
-    // by_hand: the tile has values that are not finite at keys that some row does not see
-    template <bool MASKED>
-    __device__ __forceinline__ void step(const uint4 *sk, const uint4 *sv, int kb, const int (&last)[RT], float c, bool by_hand,
-                                         float *scratch) {
-        const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-        f32x16 s[RT][KT];
+        const float ref = m == -INFINITY ? 0.f : m;
+        if (__builtin_expect(__ballot(fabsf(ref) > kHuge) == 0ull, 1)) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+            for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], c, -ref);
+        } else {
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[r][kt][i] = 0.f;
-#pragma unroll
-        for (int sl = 0; sl < R::kSlices; ++sl)
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const uint4 a = sk[R::k_at(32 * kt + n, 2 * sl + h)];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) s[r][kt] = mma32(a, q[r][sl], s[r][kt], T());
-            }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (MASKED) {
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (kb + 32 * kt + 8 * (i >> 2) + 4 * h + (i & 3) > last[r]) s[r][kt][i] = -INFINITY;
-            }
-            float mx = s[r][0][0];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[r][kt][i]);
-            mx *= c;
-            if (__ballot(mx > m[r] + kSlack) != 0ull) {
-                const float m_new = fmaxf(m[r], fmaxf(mx, __shfl_xor(mx, 32, 64)));
-                const float f = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[r] - m_new);  // no logit but -inf yet: nothing to scale
-                l[r] *= f;
-                m[r] = m_new;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[r][d][i] *= f;
-            }
-            const float ref = m[r] == -INFINITY ? 0.f : m[r];
-            // The reference is a rounded product, the exponent an exact one minus it: the largest logit's exponent is off zero by half a
-            // step of the reference, the same for all keys of the row, so that it cancels.  Far beyond any trained model's logits that
-            // step leaves fp32's range of exponents: there the product is rounded as the reference was.
-            if (__ballot(fabsf(ref) > kHuge) == 0ull) {
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[r][kt][i] = __builtin_amdgcn_exp2f(fmaf(s[r][kt][i], c, -ref));
-            } else {
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[r][kt][i] = __builtin_amdgcn_exp2f(rounded_exponent(s[r][kt][i], c, ref));
-            }
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) l[r] += s[r][kt][i];
+            for (int i = 0; i < 16; ++i) s[i] = rounded_exponent(s[i], c, ref);
         }
-        if (MASKED && by_hand) {  // (uniform over the wave) a product with 0 would be NaN: only what a row sees is added
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {  // 16 keys at a time
-                        wave_sync();
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) scratch[32 * (8 * (i >> 2) + 4 * h + (i & 3)) + n] = s[r][kt][8 * half + i];
-                        wave_sync();
-                        for (int j = 0; j < 16; ++j) {
-                            const int key = 32 * kt + 16 * half + j;
-                            const bool sees = kb + key <= last[r];
-                            const float p = scratch[32 * j + n];
-                            const T *row = reinterpret_cast<const T *>(sv);
-#pragma unroll
-                            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    const int col = 32 * d + 8 * (i >> 2) + 4 * h + (i & 3);
-                                    const float v = ldf(row + R::v_at(key, col / R::kVec) * R::kVec + col % R::kVec);
-                                    acc[r][d][i] = sees ? fmaf(p, v, acc[r][d][i]) : acc[r][d][i];
-                                }
-                        }
-                    }
-                }
-            return;
-        }
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
         if constexpr (sizeof(T) == 2) {
-            // lane of the transposed read: row (lane % 16) / 4 of four keys, 8 bytes at columns 16 ((lane / 16) % 2) + 4 (lane % 4)
-            const int krow = 4 * h + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            const char *base = reinterpret_cast<const char *>(sv) + 8 * (lane & 1);
+            const char *base = reinterpret_cast<const char *>(sv);
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+            for (int half = 0; half < 2; ++half) {
+                bf16x8 x;
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint4 p[RT];
+                for (int i = 0; i < 8; ++i) x[i] = (__bf16)s[8 * half + i];
+                const uint4 p = __builtin_bit_cast(uint4, x);
+                l = sum_of(p, l);
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        bf16x8 x;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = (__bf16)s[r][kt][8 * half + i];
-                        p[r] = __builtin_bit_cast(uint4, x);
-                    }
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        const char *at = base + 16 * R::v_at(32 * kt + 16 * half + krow, 4 * d + piece);
-                        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                        struct { s16x4 a, b; } v;
-                        v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-                        v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * D * sizeof(T)));
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) acc[r][d] = mma32(__builtin_bit_cast(uint4, v), p[r], acc[r][d], T());
-                    }
-                }
+                for (int d = 0; d < ND; ++d) acc[d] = mma32(read_v<D>(base, half, d), p, acc[d], T());
+            }
         } else {
             const float *base = reinterpret_cast<const float *>(sv) + 4 * h * D;
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+            for (int i = 0; i < 16; ++i) l += s[i];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 16; ++i)
 #pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        const float v = base[(32 * kt + 8 * (i >> 2) + (i & 3)) * D + ((32 * d + n) ^ (32 * h))];
-#pragma unroll
-                        for (int r = 0; r < RT; ++r)
-                            acc[r][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r][kt][i], acc[r][d], 0, 0, 0);
-                    }
+                for (int d = 0; d < ND; ++d) {
+                    const float v = base[(8 * (i >> 2) + (i & 3)) * D + ((32 * d + n) ^ (32 * h))];
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], acc[d], 0, 0, 0);
+                }
         }
     }
 };
+
+// What a thread loads of a tile of keys, kLoads rows apart by kRowStep, on its way to LDS
+template <typename T, int D, int THREADS, int KEYS>
+struct Stage {
+    using R = Row<T, D>;
+    static constexpr int kLoads = KEYS * R::kPieces / THREADS, kRowStep = THREADS / R::kPieces;
+    static_assert(kLoads >= 1 && kLoads * THREADS == KEYS * R::kPieces, "whole rounds of loads");
+    int piece, row;
+    int64_t k_lane, v_lane;
+    u32x4 k[kLoads], v[kLoads];
+
+    __device__ __forceinline__ void init(const PromptArgs &a, int thread) {
+        piece = thread % R::kPieces;
+        row = thread / R::kPieces;
+        k_lane = row * a.k_t + R::kVec * piece;
+        v_lane = row * a.v_t + R::kVec * piece;
+    }
+    // keys from kb on, of kv_len in all; kg, vg: the first key's and value's rows
+    __device__ __forceinline__ void load(const PromptArgs &a, const T *kg, const T *vg, int kb, int kv_len) {
+        const T *kp = kg + kb * a.k_t, *vp = vg + kb * a.v_t;
+        const int end = kv_len - 1 - kb;
+        if (end >= KEYS - 1) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) k[i] = *reinterpret_cast<const u32x4 *>(kp + i * (kRowStep * a.k_t) + k_lane);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) v[i] = *reinterpret_cast<const u32x4 *>(vp + i * (kRowStep * a.v_t) + v_lane);
+        } else {  // rows past the last key re-read it
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = min(row + kRowStep * i, end);
+                k[i] = *reinterpret_cast<const u32x4 *>(kp + r * a.k_t + R::kVec * piece);
+                v[i] = *reinterpret_cast<const u32x4 *>(vp + r * a.v_t + R::kVec * piece);
+            }
+        }
+    }
+    // Of a tile that some row does not see all of: that row's probability of 0 must not meet an infinity.  Values behind the last
+    // key (`left` are left from the tile's first) become 0, and so does what is not finite: true if there was any (add_not_finite
+    // gives it to the rows that see it)
+    __device__ __forceinline__ bool clean(int left) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (row + kRowStep * i >= left) v[i] = (u32x4){0, 0, 0, 0};
+            const u32x4 x = finite_part(v[i], T());
+#pragma unroll
+            for (int w = 0; w < 4; ++w) bad = bad || x[w] != v[i][w];
+            v[i] = x;
+        }
+        return bad;
+    }
+    __device__ __forceinline__ void store(u32x4 *sk, u32x4 *sv) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            sk[R::k_at(row + kRowStep * i, piece)] = k[i];
+            sv[R::v_at(row + kRowStep * i, piece)] = v[i];
+        }
+    }
+};
+
+// the values of keys [key0, key1) that are not finite, added to the accumulators of a row that sees the keys up to `last`
+template <typename T, int ND>
+__device__ __forceinline__ void add_not_finite(f32x16 (&acc)[ND], const T *vg, int64_t v_t, int key0, int key1, int last, int h) {
+    for (int key = key0; key < key1 && key <= last; ++key)
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float v = ldf(vg + key * v_t + 32 * d + 8 * (i >> 2) + 4 * h + (i & 3));
+                if (!(fabsf(v) < INFINITY)) acc[d][i] += v;
+            }
+}
 
 // four consecutive output elements
 __device__ __forceinline__ void store4(bf16_t *p, const f32x4 &x) {
@@ -312,125 +315,6 @@ __device__ __forceinline__ Place place_of(const PromptArgs &a, int w) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Many rows: NW waves of 32 RT rows each over tiles of 32 KT keys in LDS, which all waves share.  The next tile's loads are in
-// flight while the present one is multiplied.
-// ---------------------------------------------------------------------------------------
-template <typename T, int D, int NW, int RT, int KT>
-__global__ __launch_bounds__(64 * NW) void prompt_kernel(PromptArgs a) {
-    using R = Row<T, D>;
-    constexpr int kRows = 32 * RT * NW, kKeys = 32 * KT, kThreads = 64 * NW;
-    constexpr int kLoads = kKeys * R::kPieces / kThreads, kRowStep = kThreads / R::kPieces;
-    static_assert(kLoads * kThreads == kKeys * R::kPieces && kRowStep >= 1, "whole rounds of loads");
-    __shared__ uint4 sk[2][kKeys * R::kPieces], sv[2][kKeys * R::kPieces];
-    __shared__ float scratch[NW][16 * 32];
-    __shared__ int s_bad;
-    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place pl = place_of(a, blockIdx.x);
-    const PromptSpan &sp = a.s[pl.seq];
-    const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
-    const int row0 = pl.tile * kRows;
-    const int end_row = min(row0 + kRows, n_rows);
-    // keys that every row of the tile sees, and that any does
-    const int see_all = max(0, row0 / a.G + shift + 1), see_any = max(0, (end_row - 1) / a.G + shift + 1);
-    const int n_blocks = (see_any + kKeys - 1) / kKeys, n_full = see_all / kKeys;
-    const int per_split = (n_blocks + a.splits - 1) / a.splits;
-    const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
-
-    Attend<T, D, RT, KT> at;
-    at.clear();
-    int last[RT], head[RT], tok[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int row = min(row0 + 32 * (RT * wave + r) + n, n_rows - 1);
-        tok[r] = row / a.G;
-        head[r] = pl.kvh * a.G + row - tok[r] * a.G;
-        last[r] = tok[r] + shift;
-        const T *q = (const T *)a.q + sp.q_off + tok[r] * a.q_t + head[r] * a.q_h;
-#pragma unroll
-        for (int sl = 0; sl < R::kSlices; ++sl) at.q[r][sl] = *reinterpret_cast<const uint4 *>(q + R::kVec * (2 * sl + h));
-    }
-
-    const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
-    const int piece = threadIdx.x % R::kPieces, lrow = threadIdx.x / R::kPieces;
-    uint4 kr[kLoads], vr[kLoads];
-    auto load = [&](int b) {
-        const int kb = b * kKeys, top = sp.kv_len - 1 - kb;  // rows past the last key re-read it
-        const T *kp = kg + kb * a.k_t + R::kVec * piece, *vp = vg + kb * a.v_t + R::kVec * piece;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int r = min(lrow + kRowStep * i, top);
-            kr[i] = *reinterpret_cast<const uint4 *>(kp + r * a.k_t);
-            vr[i] = *reinterpret_cast<const uint4 *>(vp + r * a.v_t);
-        }
-    };
-    auto keep = [&](int b) {
-        const int buf = b & 1;
-        if (b >= n_full) {  // some row does not see all of the tile
-            const int left = sp.kv_len - b * kKeys;
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if (lrow + kRowStep * i >= left) vr[i] = make_uint4(0, 0, 0, 0);
-                bad = bad || not_finite(vr[i], T());
-            }
-            if (bad) s_bad = 1;
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            sk[buf][R::k_at(lrow + kRowStep * i, piece)] = kr[i];
-            sv[buf][R::v_at(lrow + kRowStep * i, piece)] = vr[i];
-        }
-    };
-    if (threadIdx.x == 0) s_bad = 0;
-    __syncthreads();
-    if (b0 < b1) {
-        load(b0);
-        keep(b0);
-    }
-    __syncthreads();
-    for (int b = b0; b < b1; ++b) {
-        if (b + 1 < b1) load(b + 1);
-        if (b < n_full) at.template step<false>(sk[b & 1], sv[b & 1], b * kKeys, last, a.c, false, scratch[wave]);
-        else at.template step<true>(sk[b & 1], sv[b & 1], b * kKeys, last, a.c, __builtin_amdgcn_readfirstlane(s_bad) != 0, scratch[wave]);
-        if (b + 1 < b1) keep(b + 1);
-        __syncthreads();
-    }
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const float l = at.l[r] + __shfl_xor(at.l[r], 32, 64);
-        const int row = row0 + 32 * (RT * wave + r) + n;
-        if (row >= n_rows) continue;
-        if (a.splits == 1) {
-            const float inv = l == 0.f ? 0.f : 1.0f / l;
-            T *o = (T *)a.out + sp.out_off + tok[r] * a.out_t + head[r] * a.out_h;
-#pragma unroll
-            for (int d = 0; d < Attend<T, D, RT, KT>::ND; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4 x;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : at.acc[r][d][4 * i + j] * inv;
-                    store4(o + 32 * d + 8 * i + 4 * h, x);
-                }
-        } else {
-            const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + a.row0[pl.seq] + row;
-            if (h == 0) a.part_ml[slot] = make_float2(at.m[r], l);
-            float *o = a.part_o + slot * D;
-#pragma unroll
-            for (int d = 0; d < Attend<T, D, RT, KT>::ND; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4 x;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] = at.acc[r][d][4 * i + j];
-                    store4(o + 32 * d + 8 * i + 4 * h, x);
-                }
-        }
-    }
-}
-
-// ---------------------------------------------------------------------------------------
 // Many rows, bf16: 4 waves of 32 RT rows, key blocks of 64 in LDS (three buffers), two row tiles a wave so that what is read of
 // K and V from LDS serves 64 rows.  One wave per SIMD: the logits of the next 32 keys are formed (matrix unit) while the
 // exponentials of the present ones are (vector unit), in one run of instructions without a branch.
@@ -440,7 +324,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
     using R = Row<T, D>;
     static_assert(sizeof(T) == 2, "bf16");
     constexpr int kRows = 32 * RT * NW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
-    constexpr int kTile = kKeys * R::kPieces, kLoads = kTile / (64 * NW), kRowStep = 64 * NW / R::kPieces;
+    constexpr int kTile = kKeys * R::kPieces;
     __shared__ u32x4 sk[kBufs][kTile], sv[kBufs][kTile];
     __shared__ int s_bad;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -478,60 +362,17 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
     }
 
     const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
-    const int piece = threadIdx.x % R::kPieces, lrow = threadIdx.x / R::kPieces;
-    const int64_t k_lane = lrow * a.k_t + R::kVec * piece, v_lane = lrow * a.v_t + R::kVec * piece;
-    u32x4 kr[kLoads], vr[kLoads];
-    auto load = [&](int b) {
-        const int kb = b * kKeys, end = sp.kv_len - 1 - kb;
-        const T *kp = kg + kb * a.k_t, *vp = vg + kb * a.v_t;
-        if (end >= kKeys - 1) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                kr[i] = *reinterpret_cast<const u32x4 *>(kp + i * (kRowStep * a.k_t) + k_lane);
-                vr[i] = *reinterpret_cast<const u32x4 *>(vp + i * (kRowStep * a.v_t) + v_lane);
-            }
-        } else {  // rows past the last key re-read it
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int r = min(lrow + kRowStep * i, end);
-                kr[i] = *reinterpret_cast<const u32x4 *>(kp + r * a.k_t + R::kVec * piece);
-                vr[i] = *reinterpret_cast<const u32x4 *>(vp + r * a.v_t + R::kVec * piece);
-            }
-        }
-    };
+    Stage<T, D, 64 * NW, kKeys> stage;
+    stage.init(a, threadIdx.x);
+    auto load = [&](int b) { stage.load(a, kg, vg, b * kKeys, sp.kv_len); };
     auto keep = [&](int b) {
-        const int buf = b % kBufs;
-        if ((b + 1) * kKeys > see_all) {
-            // Some row does not see all of the block, and its probability of 0 must not meet an infinity: values behind the last key become
-            // 0, and so does what is not finite (added at the end to the rows that see it)
-            const int left = sp.kv_len - b * kKeys;
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if (lrow + kRowStep * i >= left) vr[i] = (u32x4){0, 0, 0, 0};
-                if (not_finite(__builtin_bit_cast(uint4, vr[i]), T())) {
-                    bad = true;
-                    vr[i] = finite_part(vr[i]);
-                }
-            }
-            if (bad) s_bad = 1;
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            sk[buf][R::k_at(lrow + kRowStep * i, piece)] = kr[i];
-            sv[buf][R::v_at(lrow + kRowStep * i, piece)] = vr[i];
-        }
+        if ((b + 1) * kKeys > see_all && stage.clean(sp.kv_len - b * kKeys)) s_bad = 1;
+        stage.store(sk[b % kBufs], sv[b % kBufs]);
     };
     // operands of the logits of the 32 keys whose tile starts at sk_
     auto read_k = [&](u32x4(&x)[NS], const u32x4 *sk_) {
 #pragma unroll
         for (int sl = 0; sl < NS; ++sl) x[sl] = sk_[R::k_at(n, 2 * sl + h)];
-    };
-    auto largest = [&](const f32x16 &s) {
-        float mx = s[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-        return mx;
     };
     auto logits = [&](f32x16(&s)[RT], const u32x4(&x)[NS]) {
 #pragma unroll
@@ -575,25 +416,13 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
             }
         }
     };
-    const int krow = 4 * h + ((lane & 15) >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    auto read_v = [&](u32x4(&x)[ND], const u32x4 *sv_, int half) {
-        const char *base = reinterpret_cast<const char *>(sv_) + 8 * (lane & 1);
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            const char *at = base + 16 * R::v_at(16 * half + krow, 4 * d + vpiece);
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            struct { s16x4 a, b; } v;
-            v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-            v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * D * sizeof(T)));
-            x[d] = __builtin_bit_cast(u32x4, v);
-        }
-    };
     // The next 32 keys' logits into `next` (operands: kf) while this 32 keys' values are weighed; kf then takes the operands of the keys
     // behind those.  `meet`: the tiles that k_after points to are whole only behind a barrier.
     auto turn = [&](f32x16(&s)[RT], f32x16(&next)[RT], float(&mx)[RT], u32x4(&kf)[NS], const u32x4 *sv_, const u32x4 *k_after, bool meet) {
-        u32x4 vf[2][ND];
+        uint4 vf[2][ND];
         __builtin_amdgcn_s_setprio(1);
-        read_v(vf[0], sv_, 0);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) vf[0][d] = read_v<D>(reinterpret_cast<const char *>(sv_), 0, d);
         logits(next, kf);
         uint4 p[RT][2];
 #pragma unroll
@@ -605,7 +434,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
                 for (int i = 0; i < 8; ++i) x[i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[r][8 * half + i], mul[r], -sub[r]));
                 p[r][half] = __builtin_bit_cast(uint4, x);
             }
-        read_v(vf[1], sv_, 1);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) vf[1][d] = read_v<D>(reinterpret_cast<const char *>(sv_), 1, d);
         if (meet) lds_barrier();
         read_k(kf, k_after);
 #pragma unroll
@@ -613,7 +443,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) acc[r][d] = mma32(__builtin_bit_cast(uint4, vf[half][d]), p[r][half], acc[r][d], T());
+                for (int r = 0; r < RT; ++r) acc[r][d] = mma32(vf[half][d], p[r][half], acc[r][d], T());
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             // the sum of what the second product takes: the weights add up to one as they are used
@@ -669,18 +499,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
     for (int r = 0; r < RT; ++r) {
         const float sum = l[r] + __shfl_xor(l[r], 32, 64);
         if (row[r] >= n_rows) continue;
-        if (s_bad) {  // values that are not finite, at keys that some row does not see
-            for (int key = max(b0 * kKeys, see_all / kKeys * kKeys); key < min(b1 * kKeys, see_any); ++key) {
-                if (key > last[r]) continue;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float v = ldf(vg + key * a.v_t + 32 * d + 8 * (i >> 2) + 4 * h + (i & 3));
-                        if (!(fabsf(v) < INFINITY)) acc[r][d][i] += v;
-                    }
-            }
-        }
+        if (s_bad) add_not_finite(acc[r], vg, a.v_t, max(b0 * kKeys, see_all / kKeys * kKeys), min(b1 * kKeys, see_any), last[r], h);
         const int t = row[r] / a.G, head = pl.kvh * a.G + row[r] - t * a.G;
         const bool whole = a.splits == 1;
         const float inv = whole ? 1.0f / sum : 1.0f;
@@ -704,16 +523,17 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
 }
 
 // ---------------------------------------------------------------------------------------
-// Few rows (at most 32 per KV head and sequence): bound by reading K and V.  Four waves share the rows and deal the key tiles of 32
-// among themselves; each moves its tiles through LDS of its own, the next tile's loads in flight, without a barrier.
+// Few rows: 32 of one (sequence, KV head).  Four waves share the rows and deal the key tiles of 32 among themselves; each moves its
+// tiles through LDS of its own, the next tile's loads in flight, without a barrier.  (Also fp32 prompts: the fp32 matrix unit is so
+// much slower that re-reading K and V per 32 rows costs nothing.)
 // ---------------------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     using R = Row<T, D>;
-    constexpr int kTile = 32 * R::kPieces, kLoads = kTile / 64, kRowStep = 64 / R::kPieces, NW = 4;
-    __shared__ uint4 tiles[NW][2][kTile];
-    __shared__ float scratch[NW][16 * 32];
+    constexpr int kTile = 32 * R::kPieces, NW = 4;
+    __shared__ u32x4 tiles[NW][2][kTile];
     __shared__ float s_m[NW][32], s_l[NW][32];
+    __shared__ int s_bad;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place pl = place_of(a, blockIdx.x);
@@ -721,63 +541,45 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
     const int row0 = pl.tile * 32, end_row = min(row0 + 32, n_rows);
     const int see_all = max(0, row0 / a.G + shift + 1), see_any = max(0, (end_row - 1) / a.G + shift + 1);
-    const int n_blocks = (see_any + 31) / 32, n_full = see_all / 32;
+    const int n_blocks = (see_any + 31) / 32;
     const int per_split = (n_blocks + a.splits - 1) / a.splits;
     const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
 
-    Attend<T, D, 1, 1> at;
+    const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
+    Stage<T, D, 64, 32> stage;
+    stage.init(a, lane);
+    int b = b0 + wave;
+    if (b < b1) stage.load(a, kg, vg, b * 32, sp.kv_len);
+    Attend<T, D> at;
     at.clear();
     const int row = min(row0 + n, n_rows - 1), tok = row / a.G, head = pl.kvh * a.G + row - tok * a.G;
-    const int last[1] = {tok + shift};
+    const int last = tok + shift;
     {
         const T *q = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
 #pragma unroll
-        for (int sl = 0; sl < R::kSlices; ++sl) at.q[0][sl] = *reinterpret_cast<const uint4 *>(q + R::kVec * (2 * sl + h));
+        for (int sl = 0; sl < R::kSlices; ++sl) at.q[sl] = *reinterpret_cast<const uint4 *>(q + R::kVec * (2 * sl + h));
     }
-    const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
-    const int piece = lane % R::kPieces, lrow = lane / R::kPieces;
-    uint4 *sk = tiles[wave][0], *sv = tiles[wave][1];
-    uint4 kr[kLoads], vr[kLoads];
-    auto load = [&](int b) {
-        const int kb = b * 32, top = sp.kv_len - 1 - kb;
-        const T *kp = kg + kb * a.k_t + R::kVec * piece, *vp = vg + kb * a.v_t + R::kVec * piece;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) kr[i] = *reinterpret_cast<const uint4 *>(kp + min(lrow + kRowStep * i, top) * a.k_t);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) vr[i] = *reinterpret_cast<const uint4 *>(vp + min(lrow + kRowStep * i, top) * a.v_t);
-    };
-    int b = b0 + wave;
-    if (b < b1) load(b);
+    if (threadIdx.x == 0) s_bad = 0;
+    __syncthreads();
+    u32x4 *sk = tiles[wave][0], *sv = tiles[wave][1];
+#pragma unroll 1
     for (; b < b1; b += NW) {
-        bool bad = false;
-        if (b >= n_full) {
-            const int left = sp.kv_len - b * 32;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if (lrow + kRowStep * i >= left) vr[i] = make_uint4(0, 0, 0, 0);
-                bad = bad || not_finite(vr[i], T());
-            }
-            bad = __ballot(bad) != 0ull;
-        }
+        const bool masked = (b + 1) * 32 > see_all;
+        if (masked && stage.clean(sp.kv_len - b * 32)) s_bad = 1;
         wave_sync();  // the wave's reads of the tile before are behind it
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            sk[R::k_at(lrow + kRowStep * i, piece)] = kr[i];
-            sv[R::v_at(lrow + kRowStep * i, piece)] = vr[i];
-        }
+        stage.store(sk, sv);
         wave_sync();
-        if (b + NW < b1) load(b + NW);
-        if (b < n_full) at.template step<false>(sk, sv, b * 32, last, a.c, false, scratch[wave]);
-        else at.template step<true>(sk, sv, b * 32, last, a.c, bad, scratch[wave]);
+        if (b + NW < b1) stage.load(a, kg, vg, (b + NW) * 32, sp.kv_len);
+        at.step(sk, sv, masked, last - b * 32, a.c);
     }
     // merge of the four waves: every wave brings its sums to the common reference and leaves them in LDS
-    const float l = at.l[0] + __shfl_xor(at.l[0], 32, 64);
-    if (h == 0) s_m[wave][n] = at.m[0];
+    const float l = at.l + __shfl_xor(at.l, 32, 64);
+    if (h == 0) s_m[wave][n] = at.m;
     __syncthreads();
     float M = s_m[0][n];
 #pragma unroll
     for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][n]);
-    const float f = at.m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(at.m[0] - M);
+    const float f = at.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(at.m - M);
     if (h == 0) s_l[wave][n] = l * f;
     constexpr int kQuads = D / 4;  // 16-byte pieces of a row of sums
     static_assert(sizeof(tiles) >= NW * 32 * D * sizeof(float), "the tiles' memory holds the sums");
@@ -788,7 +590,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
         for (int i = 0; i < 4; ++i) {
             f32x4 x;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = f == 0.f ? 0.f : at.acc[0][d][4 * i + j] * f;
+            for (int j = 0; j < 4; ++j) x[j] = f == 0.f ? 0.f : at.acc[d][4 * i + j] * f;
             sums[(wave * 32 + n) * kQuads + ((8 * d + 2 * i + h) ^ (n & 15))] = x;
         }
     __syncthreads();
@@ -803,6 +605,14 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
             lt += s_l[w][r];
         }
         const int t = (row0 + r) / a.G, g = row0 + r - t * a.G;
+        if (s_bad) {  // values that are not finite, at keys that some row does not see
+            const int end = min(min(b1 * 32, see_any), t + shift + 1);
+            for (int key = max(b0, see_all / 32) * 32; key < end; ++key)
+                for (int j = 0; j < 4; ++j) {
+                    const float v = ldf(vg + key * a.v_t + 4 * c4 + j);
+                    if (!(fabsf(v) < INFINITY)) x[j] += v;
+                }
+        }
         if (a.splits == 1) {
             const float inv = 1.0f / lt;
 #pragma unroll
@@ -823,9 +633,9 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
 
 // Joins the splits of a row.  D / 4 lanes hold a row's columns; `groups` of them (a power of two) share its splits, so that the partial
 // results of a long row are all in flight at once.
-template <typename T, int D>
+template <typename T, int D, int kRound>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int groups) {
-    constexpr int kQuads = D / 4, kRound = 8;
+    constexpr int kQuads = D / 4;
     __shared__ f32x4 s_x[256];
     __shared__ float2 s_ml[256 / kQuads];
     const int c4 = threadIdx.x % kQuads, team = threadIdx.x / kQuads, g = team & (groups - 1);
@@ -846,8 +656,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
         float top = m;
 #pragma unroll
         for (int i = 0; i < kRound; ++i) top = fmaxf(top, ml[i].x);
-        if (top == -INFINITY) top = 0.f;
-        const float f = __builtin_amdgcn_exp2f(m - top);
+        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
         l *= f;
         x *= f;
         m = top;
@@ -910,8 +719,8 @@ static PromptPlan plan_of(const air_prompt_config &c, const air_prompt_seq *seqs
         if (seqs[i].q_len * G > most) most = seqs[i].q_len * G;
         if (seqs[i].q_len > 0 && seqs[i].kv_len > keys) keys = seqs[i].kv_len;
     }
-    p.few = most <= 32;
-    p.tile_rows = p.few ? 32 : (c.dtype == AIR_BF16 ? 256 : 128);
+    p.few = most <= 32 || c.dtype == AIR_F32;
+    p.tile_rows = p.few ? 32 : 256;
     for (int i = 0; i < n; ++i) {
         p.n_tiles += (seqs[i].q_len * G + p.tile_rows - 1) / p.tile_rows;
         p.n_rows += seqs[i].q_len * G;
@@ -939,15 +748,18 @@ bool prompt_grid_ok(const air_prompt_config &c, const air_prompt_seq *seqs, int 
 template <typename T, int D>
 static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &a) {
     const dim3 grid((unsigned)(p.n_tiles * a.Hkv * p.splits));
+    if constexpr (sizeof(T) == 2) {
+        if (!p.few) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 1, 8>), grid, dim3(512), 0, s, a);
+    }
     if (p.few) hipLaunchKernelGGL((prompt_few_kernel<T, D>), grid, dim3(256), 0, s, a);
-    else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 1, 8>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((prompt_kernel<T, D, 4, 1, 1>), grid, dim3(256), 0, s, a);
     if (p.splits > 1) {
         constexpr int kMost = 256 / (D / 4);
         int groups = 1;
         while (groups < kMost && groups * 2 <= p.splits) groups *= 2;
         const int64_t per = kMost / groups, rows = p.n_rows * a.Hkv;
-        hipLaunchKernelGGL((prompt_join_kernel<T, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, s, a, groups);
+        const dim3 join((unsigned)((rows + per - 1) / per));
+        if (p.splits <= groups) hipLaunchKernelGGL((prompt_join_kernel<T, D, 1>), join, dim3(256), 0, s, a, groups);
+        else hipLaunchKernelGGL((prompt_join_kernel<T, D, 8>), join, dim3(256), 0, s, a, groups);
     }
 }
 
