@@ -25,6 +25,20 @@ namespace air {
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
+// Division by a number that the host knows: x / d = (x m) >> s for 0 <= x < 2^31, with 2^(s - 32) < d <= 2^(s - 31) and
+// m = ceil(2^s / d) (m d - 2^s < d <= 2^(s - 31): the quotient is off by less than 1 / d)
+struct Div {
+    uint32_t m, s;
+    __device__ __forceinline__ int of(int x) const { return (int)(((uint64_t)(uint32_t)x * m) >> s); }
+};
+static Div div_by(int d) {
+    Div r;
+    r.s = 31;
+    while ((1ll << (r.s - 31)) < d) ++r.s;
+    r.m = (uint32_t)(((1ull << r.s) + (uint64_t)d - 1) / (uint64_t)d);
+    return r;
+}
+
 struct PromptSpan {
     int64_t q_off, k_off, v_off, out_off;
     int32_t q_len, kv_len;
@@ -37,6 +51,7 @@ struct PromptArgs {
     int64_t q_h, q_t, k_h, k_t, v_h, v_t, out_h, out_t;
     float c;  // scale * log2(e)
     int32_t G, Hkv, n_seqs, n_tiles, n_rows, splits;
+    Div by_g, by_hkv, by_splits, by_rows;
     int32_t tile0[AIR_MAX_BATCH];  // first row tile of a sequence in the launch; behind the last sequence: INT32_MAX
     int32_t row0[AIR_MAX_BATCH];   // first row (query x query head of the group) in the partial results, likewise
     PromptSpan s[AIR_MAX_BATCH];
@@ -304,9 +319,9 @@ struct Place {
 };
 __device__ __forceinline__ Place place_of(const PromptArgs &a, int w) {
     Place p;
-    int x = w / a.Hkv;
+    int x = a.by_hkv.of(w);
     p.kvh = w - x * a.Hkv;
-    const int y = x / a.splits;
+    const int y = a.by_splits.of(x);
     p.split = x - y * a.splits;
     const int tile = a.n_tiles - 1 - y;
     p.seq = a.n_seqs == 1 ? 0 : sequence_of(a.tile0, tile);
@@ -333,7 +348,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
     const PromptSpan &sp = a.s[pl.seq];
     const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
     const int row0 = pl.tile * kRows, end_row = min(row0 + kRows, n_rows);
-    const int see_all = max(0, row0 / a.G + shift + 1), see_any = max(0, (end_row - 1) / a.G + shift + 1);
+    const int see_all = max(0, a.by_g.of(row0) + shift + 1), see_any = max(0, a.by_g.of(end_row - 1) + shift + 1);
     const int n_blocks = (see_any + kKeys - 1) / kKeys;
     const int per_split = (n_blocks + a.splits - 1) / a.splits;
     const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
@@ -354,7 +369,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[r][d][i] = 0.f;
         row[r] = row0 + 32 * (RT * wave + r) + n;
-        const int m = min(row[r], n_rows - 1), t = m / a.G, g = m - t * a.G;
+        const int m = min(row[r], n_rows - 1), t = a.by_g.of(m), g = m - t * a.G;
         last[r] = t + shift;
         const T *qp = (const T *)a.q + sp.q_off + t * a.q_t + (pl.kvh * a.G + g) * a.q_h;
 #pragma unroll
@@ -500,7 +515,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
         const float sum = l[r] + __shfl_xor(l[r], 32, 64);
         if (row[r] >= n_rows) continue;
         if (s_bad) add_not_finite(acc[r], vg, a.v_t, max(b0 * kKeys, see_all / kKeys * kKeys), min(b1 * kKeys, see_any), last[r], h);
-        const int t = row[r] / a.G, head = pl.kvh * a.G + row[r] - t * a.G;
+        const int t = a.by_g.of(row[r]), head = pl.kvh * a.G + row[r] - t * a.G;
         const bool whole = a.splits == 1;
         const float inv = whole ? 1.0f / sum : 1.0f;
         const bool none = whole && sum == 0.f;
@@ -540,7 +555,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     const PromptSpan &sp = a.s[pl.seq];
     const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
     const int row0 = pl.tile * 32, end_row = min(row0 + 32, n_rows);
-    const int see_all = max(0, row0 / a.G + shift + 1), see_any = max(0, (end_row - 1) / a.G + shift + 1);
+    const int see_all = max(0, a.by_g.of(row0) + shift + 1), see_any = max(0, a.by_g.of(end_row - 1) + shift + 1);
     const int n_blocks = (see_any + 31) / 32;
     const int per_split = (n_blocks + a.splits - 1) / a.splits;
     const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
@@ -552,7 +567,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     if (b < b1) stage.load(a, kg, vg, b * 32, sp.kv_len);
     Attend<T, D> at;
     at.clear();
-    const int row = min(row0 + n, n_rows - 1), tok = row / a.G, head = pl.kvh * a.G + row - tok * a.G;
+    const int row = min(row0 + n, n_rows - 1), tok = a.by_g.of(row), head = pl.kvh * a.G + row - tok * a.G;
     const int last = tok + shift;
     {
         const T *q = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
@@ -604,7 +619,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
             x += sums[(w * 32 + r) * kQuads + (c4 ^ (r & 15))];
             lt += s_l[w][r];
         }
-        const int t = (row0 + r) / a.G, g = row0 + r - t * a.G;
+        const int t = a.by_g.of(row0 + r), g = row0 + r - t * a.G;
         if (s_bad) {  // values that are not finite, at keys that some row does not see
             const int end = min(min(b1 * 32, see_any), t + shift + 1);
             for (int key = max(b0, see_all / 32) * 32; key < end; ++key)
@@ -640,8 +655,17 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
     __shared__ float2 s_ml[256 / kQuads];
     const int c4 = threadIdx.x % kQuads, team = threadIdx.x / kQuads, g = team & (groups - 1);
     const int64_t idx = (int64_t)blockIdx.x * (256 / kQuads / groups) + team / groups;
-    const bool live = idx < (int64_t)a.n_rows * a.Hkv;
     const int64_t stride = (int64_t)a.Hkv * a.n_rows;
+    const bool live = idx < stride;
+    const int kvh = a.by_rows.of((int)min(idx, stride - 1)), row = (int)min(idx, stride - 1) - kvh * a.n_rows;
+    int seq = 0, seq_row = 0;
+    if (a.n_seqs > 1) {  // the last sequence whose first row is not behind `row`: every lane holds one sequence's
+        const int first = a.row0[threadIdx.x & 63];
+#pragma unroll
+        for (int step = 32; step > 0; step >>= 1)
+            if (__shfl(first, seq + step, 64) <= row) seq += step;
+        seq_row = __shfl(first, seq, 64);
+    }
     float m = -INFINITY, l = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = g; live && s0 < a.splits; s0 += kRound * groups) {
@@ -690,12 +714,8 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
         }
     }
     if (!live) return;
-    const int kvh = (int)(idx / a.n_rows), row = (int)(idx - (int64_t)kvh * a.n_rows);
-    int seq = 0;  // (lanes differ in their row: no vote here)
-    for (int step = 32; step > 0; step >>= 1)
-        if (a.row0[seq + step] <= row) seq += step;
     const PromptSpan &sp = a.s[seq];
-    const int r = row - a.row0[seq], t = r / a.G, q = r - t * a.G;
+    const int r = row - seq_row, t = a.by_g.of(r), q = r - t * a.G;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : x[j] / l;
     store4((T *)a.out + sp.out_off + t * a.out_t + (kvh * a.G + q) * a.out_h + 4 * c4, x);
@@ -785,6 +805,10 @@ hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const air_pr
     a.out_t = c.out_t;
     a.G = c.n_q_heads / c.n_kv_heads;
     a.Hkv = c.n_kv_heads;
+    a.by_g = div_by(a.G);
+    a.by_hkv = div_by(a.Hkv);
+    a.by_splits = div_by(p.splits);
+    a.by_rows = div_by((int)p.n_rows);
     a.c = (float)((c.scale > 0.f ? (double)c.scale : 1.0 / sqrt((double)c.head_dim)) * 1.4426950408889634);
     a.splits = p.splits;
     a.n_tiles = (int)p.n_tiles;
