@@ -330,57 +330,61 @@ __device__ __forceinline__ Place place_of(const PromptArgs &a, int w) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Many rows, bf16: 4 waves of 32 RT rows, key blocks of 64 in LDS (three buffers), two row tiles a wave so that what is read of
-// K and V from LDS serves 64 rows.  One wave per SIMD: the logits of the next 32 keys are formed (matrix unit) while the
-// exponentials of the present ones are (vector unit), in one run of instructions without a branch.
+// Many rows, bf16: eight waves of 32 rows, two a SIMD; key blocks of 64 in LDS (three buffers), the loads of the block after next in
+// flight.  A wave forms the logits of its next 32 keys (matrix unit) under the exponentials of the present ones (vector unit), in one run
+// of instructions without a branch; the operands of the logits after those are read from LDS meanwhile.
+// KW 1: 256 rows, every wave takes both halves of a block, one barrier a block.  KW 2: 128 rows, two waves share 32 rows and take a
+// half of every block each; their sums are joined at the end through LDS: twice the workgroups where a call has few rows.
+// (Two row tiles a wave, to halve the reads of LDS, need more than 256 registers: the accumulators then wander between the two
+// register files, 12.4 ms against 8.9 for 2 x 16910 tokens of 64 heads.)
 // ---------------------------------------------------------------------------------------
-template <typename T, int D, int RT, int NW>
-__global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs a) {
+template <typename T, int D, int KW>
+__global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
     using R = Row<T, D>;
     static_assert(sizeof(T) == 2, "bf16");
-    constexpr int kRows = 32 * RT * NW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
-    constexpr int kTile = kKeys * R::kPieces;
-    __shared__ u32x4 sk[kBufs][kTile], sv[kBufs][kTile];
+    constexpr int NW = 8, RW = NW / KW, kRows = 32 * RW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
+    constexpr int kTile = kKeys * R::kPieces, kHalf = 32 * R::kPieces;
+    __shared__ u32x4 tiles[2][kBufs][kTile];
+    __shared__ float2 s_ml[KW == 2 ? RW * 32 : 1];
     __shared__ int s_bad;
+    u32x4(&sk)[kBufs][kTile] = tiles[0], (&sv)[kBufs][kTile] = tiles[1];
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rw = wave % RW, kw = wave / RW;
     const Place pl = place_of(a, blockIdx.x);
     const PromptSpan &sp = a.s[pl.seq];
     const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
     const int row0 = pl.tile * kRows, end_row = min(row0 + kRows, n_rows);
+    // keys that every row of the tile sees, and that any does
     const int see_all = max(0, a.by_g.of(row0) + shift + 1), see_any = max(0, a.by_g.of(end_row - 1) + shift + 1);
     const int n_blocks = (see_any + kKeys - 1) / kKeys;
     const int per_split = (n_blocks + a.splits - 1) / a.splits;
     const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
 
-    f32x16 acc[RT][ND];
-    float l[RT], ref[RT], top[RT], mul[RT], sub[RT];  // top: the logit (scaled) from which on the reference is raised
-    uint4 q[RT][NS];
-    int last[RT], row[RT];
+    f32x16 acc[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+    float l = 0.f, ref = -INFINITY, top = -INFINITY, mul = a.c, sub = 0.f;  // top: the logit (scaled) from which on the reference is raised
     bool huge = false;
+    const int row = row0 + 32 * rw + n, m_row = min(row, n_rows - 1), tok = a.by_g.of(m_row), head = pl.kvh * a.G + m_row - tok * a.G;
+    const int last = tok + shift;  // last key that the lane's query sees
+    uint4 q[NS];
+    {
+        const T *qp = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        l[r] = 0.f;
-        ref[r] = top[r] = -INFINITY;
-        mul[r] = a.c;
-        sub[r] = 0.f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[r][d][i] = 0.f;
-        row[r] = row0 + 32 * (RT * wave + r) + n;
-        const int m = min(row[r], n_rows - 1), t = a.by_g.of(m), g = m - t * a.G;
-        last[r] = t + shift;
-        const T *qp = (const T *)a.q + sp.q_off + t * a.q_t + (pl.kvh * a.G + g) * a.q_h;
-#pragma unroll
-        for (int sl = 0; sl < NS; ++sl) q[r][sl] = *reinterpret_cast<const uint4 *>(qp + R::kVec * (2 * sl + h));
+        for (int sl = 0; sl < NS; ++sl) q[sl] = *reinterpret_cast<const uint4 *>(qp + R::kVec * (2 * sl + h));
     }
 
     const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
     Stage<T, D, 64 * NW, kKeys> stage;
     stage.init(a, threadIdx.x);
-    auto load = [&](int b) { stage.load(a, kg, vg, b * kKeys, sp.kv_len); };
+    auto load = [&](int b) {
+        if (b < b1) stage.load(a, kg, vg, b * kKeys, sp.kv_len);
+    };
     auto keep = [&](int b) {
+        if (b >= b1) return;
         if ((b + 1) * kKeys > see_all && stage.clean(sp.kv_len - b * kKeys)) s_bad = 1;
         stage.store(sk[b % kBufs], sv[b % kBufs]);
     };
@@ -389,66 +393,56 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
 #pragma unroll
         for (int sl = 0; sl < NS; ++sl) x[sl] = sk_[R::k_at(n, 2 * sl + h)];
     };
-    auto logits = [&](f32x16(&s)[RT], const u32x4(&x)[NS]) {
+    auto logits = [&](f32x16 &s, const u32x4(&x)[NS]) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[r][i] = 0.f;
-#pragma unroll
-        for (int sl = 0; sl < NS; ++sl)
-#pragma unroll
-            for (int r = 0; r < RT; ++r) s[r] = mma32(__builtin_bit_cast(uint4, x[sl]), q[r][sl], s[r], T());
+        for (int sl = 0; sl < NS; ++sl) s = mma32(__builtin_bit_cast(uint4, x[sl]), q[sl], s, T());
     };
     // masks, reference: what has to be known of the logits of the keys from kb on before their exponentials are formed
-    auto settle = [&](f32x16(&s)[RT], float(&mx)[RT], int kb) {
+    auto settle = [&](f32x16 &s, float mx, int kb) {
+        if (__builtin_expect(kb + 32 > see_all, 0)) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (__builtin_expect(kb + 32 > see_all, 0)) {
+            for (int i = 0; i < 16; ++i)
+                if (kb + 8 * (i >> 2) + 4 * h + (i & 3) > last) s[i] = -INFINITY;
+            mx = largest(s);
+        }
+        mx *= a.c;
+        if (__builtin_expect(__ballot(mx > top) != 0ull, 0)) {
+            const float now = fmaxf(ref, fmaxf(mx, __shfl_xor(mx, 32, 64)));
+            const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - now);  // no logit but -inf yet: nothing to scale
+            l *= f;
+            ref = now;
+            top = now + kSlack;
+            sub = now == -INFINITY ? 0.f : now;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (kb + 8 * (i >> 2) + 4 * h + (i & 3) > last[r]) s[r][i] = -INFINITY;
-                mx[r] = largest(s[r]);
-            }
-            mx[r] *= a.c;
-            if (__builtin_expect(__ballot(mx[r] > top[r]) != 0ull, 0)) {
-                const float now = fmaxf(ref[r], fmaxf(mx[r], __shfl_xor(mx[r], 32, 64)));
-                const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - now);  // no logit but -inf yet: nothing to scale
-                l[r] *= f;
-                ref[r] = now;
-                top[r] = now + kSlack;
-                sub[r] = now == -INFINITY ? 0.f : now;
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int d = 0; d < ND; ++d)
+                for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+            huge = huge || __ballot(fabsf(sub) > kHuge) != 0ull;
+        }
+        if (__builtin_expect(huge, 0)) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[r][d][i] *= f;
-                huge = huge || __ballot(fabsf(sub[r]) > kHuge) != 0ull;
-            }
-            if (__builtin_expect(huge, 0)) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[r][i] = rounded_exponent(s[r][i], a.c, ref[r] == -INFINITY ? 0.f : ref[r]);
-                mul[r] = 1.f;
-                sub[r] = 0.f;
-            }
+            for (int i = 0; i < 16; ++i) s[i] = rounded_exponent(s[i], a.c, ref == -INFINITY ? 0.f : ref);
+            mul = 1.f;
+            sub = 0.f;
         }
     };
-    // The next 32 keys' logits into `next` (operands: kf) while this 32 keys' values are weighed; kf then takes the operands of the keys
-    // behind those.  `meet`: the tiles that k_after points to are whole only behind a barrier.
-    auto turn = [&](f32x16(&s)[RT], f32x16(&next)[RT], float(&mx)[RT], u32x4(&kf)[NS], const u32x4 *sv_, const u32x4 *k_after, bool meet) {
-        uint4 vf[2][ND];
+    // The next 32 keys' logits into `next` (operands: kf), their largest into mx, while the values of this 32 keys are weighed; kf then
+    // takes the operands of the keys behind those.  meet: the tile that k_after points to is whole only behind a barrier.
+    auto turn = [&](f32x16 &s, f32x16 &next, float &mx, u32x4(&kf)[NS], const u32x4 *sv_, const u32x4 *k_after, bool meet) {
+        uint4 vf[2][ND], p[2];
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int d = 0; d < ND; ++d) vf[0][d] = read_v<D>(reinterpret_cast<const char *>(sv_), 0, d);
         logits(next, kf);
-        uint4 p[RT][2];
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+        for (int half = 0; half < 2; ++half) {
+            bf16x8 x;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                bf16x8 x;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[r][8 * half + i], mul[r], -sub[r]));
-                p[r][half] = __builtin_bit_cast(uint4, x);
-            }
+            for (int i = 0; i < 8; ++i) x[i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[8 * half + i], mul, -sub));
+            p[half] = __builtin_bit_cast(uint4, x);
+        }
 #pragma unroll
         for (int d = 0; d < ND; ++d) vf[1][d] = read_v<D>(reinterpret_cast<const char *>(sv_), 1, d);
         if (meet) lds_barrier();
@@ -456,28 +450,21 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) acc[r][d] = mma32(vf[half][d], p[r][half], acc[r][d], T());
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            // the sum of what the second product takes: the weights add up to one as they are used
-            l[r] = sum_of(p[r][1], sum_of(p[r][0], l[r]));
-            mx[r] = largest(next[r]);
-        }
+            for (int d = 0; d < ND; ++d) acc[d] = mma32(vf[half][d], p[half], acc[d], T());
+        l = sum_of(p[1], sum_of(p[0], l));  // the sum of what the second product takes: the weights add up to one as they are used
+        mx = largest(next);
         __builtin_amdgcn_s_setprio(0);
-        if (!meet) {
+        if (!meet) {  // the order of issue: products, vector instructions and reads of LDS taken in turn
             __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x8, RT, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x2, 40 / NS, 0);
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
-
 #pragma unroll
             for (int i = 0; i < 2 * ND; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x8, RT, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
                 __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             }
@@ -486,55 +473,95 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void prompt_pipe_kernel(PromptArgs
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
     if (b0 < b1) {
-        f32x16 sa[RT], sb[RT];
-        float mx[RT];
+        f32x16 sa, sb;
+        float mx;
         u32x4 kf[NS];
         load(b0);
         keep(b0);
-        if (b0 + 1 < b1) load(b0 + 1);
+        load(b0 + 1);
+        if constexpr (KW == 2) {
+            keep(b0 + 1);
+            load(b0 + 2);
+        }
         lds_barrier();
-        read_k(kf, sk[b0 % kBufs]);
+        read_k(kf, sk[b0 % kBufs] + kw * kHalf);
         logits(sa, kf);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) mx[r] = largest(sa[r]);
-        settle(sa, mx, b0 * kKeys);
-        read_k(kf, sk[b0 % kBufs] + 32 * R::kPieces);
-        for (int b = b0; b < b1; ++b) {
-            const u32x4 *v_now = sv[b % kBufs], *k_next = sk[(b + 1) % kBufs];
-            if (b + 1 < b1) keep(b + 1);
-            if (b + 2 < b1) load(b + 2);
-            turn(sa, sb, mx, kf, v_now, k_next, true);
-            settle(sb, mx, b * kKeys + 32);
-            // (behind the last block: logits of whatever lies there, not used)
-            turn(sb, sa, mx, kf, v_now + 32 * R::kPieces, k_next + 32 * R::kPieces, false);
-            if (b + 1 < b1) settle(sa, mx, (b + 1) * kKeys);
+        settle(sa, largest(sa), b0 * kKeys + 32 * kw);
+        // (behind the last block: logits of whatever lies there, not used)
+        if constexpr (KW == 1) {
+            read_k(kf, sk[b0 % kBufs] + kHalf);
+            for (int b = b0; b < b1; ++b) {
+                const u32x4 *v_now = sv[b % kBufs], *k_next = sk[(b + 1) % kBufs];
+                keep(b + 1);  // (into the buffer of block b - 2, which every wave has left before the last barrier)
+                load(b + 2);
+                turn(sa, sb, mx, kf, v_now, k_next, true);
+                settle(sb, mx, b * kKeys + 32);
+                turn(sb, sa, mx, kf, v_now + kHalf, k_next + kHalf, false);
+                if (b + 1 < b1) settle(sa, mx, (b + 1) * kKeys);
+            }
+        } else {
+            read_k(kf, sk[(b0 + 1) % kBufs] + kw * kHalf);
+            auto block = [&](int b, f32x16 &s, f32x16 &next) {
+                keep(b + 2);  // (into the buffer of block b - 1: its values were read before the last barrier)
+                load(b + 3);
+                turn(s, next, mx, kf, sv[b % kBufs] + kw * kHalf, sk[(b + 2) % kBufs] + kw * kHalf, true);
+                if (b + 1 < b1) settle(next, mx, (b + 1) * kKeys + 32 * kw);
+            };
+            for (int b = b0; b < b1; b += 2) {
+                block(b, sa, sb);
+                if (b + 1 < b1) block(b + 1, sb, sa);
+            }
         }
     }
+    l += __shfl_xor(l, 32, 64);
+    if constexpr (KW == 2) {  // the two waves of 32 rows: lane by lane
+        static_assert(sizeof(tiles) >= RW * 32 * D * sizeof(float), "the tiles' memory holds the sums of half the waves");
+        f32x4 *sums = reinterpret_cast<f32x4 *>(&tiles[0][0][0]) + rw * (4 * ND * 64) + lane;
+        lds_barrier();
+        if (kw == 1) {
+            if (h == 0) s_ml[rw * 32 + n] = make_float2(ref, l);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const float sum = l[r] + __shfl_xor(l[r], 32, 64);
-        if (row[r] >= n_rows) continue;
-        if (s_bad) add_not_finite(acc[r], vg, a.v_t, max(b0 * kKeys, see_all / kKeys * kKeys), min(b1 * kKeys, see_any), last[r], h);
-        const int t = a.by_g.of(row[r]), head = pl.kvh * a.G + row[r] - t * a.G;
-        const bool whole = a.splits == 1;
-        const float inv = whole ? 1.0f / sum : 1.0f;
-        const bool none = whole && sum == 0.f;
-        const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + a.row0[pl.seq] + row[r];
-        if (!whole && h == 0) a.part_ml[slot] = make_float2(ref[r], sum);
-        T *o = (T *)a.out + sp.out_off + t * a.out_t + head * a.out_h;
-        float *po = a.part_o + slot * D;
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sums[(4 * d + i) * 64] = (f32x4){acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+        }
+        lds_barrier();
+        if (kw == 1) return;
+        const float2 other = s_ml[rw * 32 + n];
+        const float now = fmaxf(ref, other.x);
+        const float f0 = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
+        const float f1 = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.x - now);
+        ref = now;
+        l = l * f0 + other.y * f1;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                f32x4 x;
+                const f32x4 x = sums[(4 * d + i) * 64];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = none ? 0.f : acc[r][d][4 * i + j] * inv;
-                const int col = 32 * d + 8 * i + 4 * h;
-                if (whole) store4(o + col, x);
-                else store4(po + col, x);
+                for (int j = 0; j < 4; ++j) acc[d][4 * i + j] = acc[d][4 * i + j] * f0 + x[j] * f1;
             }
     }
+    if (row >= n_rows) return;
+    if (s_bad) add_not_finite(acc, vg, a.v_t, max(b0 * kKeys, see_all / kKeys * kKeys), min(b1 * kKeys, see_any), last, h);
+    const bool whole = a.splits == 1;
+    const float inv = whole ? 1.0f / l : 1.0f;
+    const bool none = whole && l == 0.f;
+    const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + a.row0[pl.seq] + row;
+    if (!whole && h == 0) a.part_ml[slot] = make_float2(ref, l);
+    T *o = (T *)a.out + sp.out_off + tok * a.out_t + head * a.out_h;
+    float *po = a.part_o + slot * D;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4 x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = none ? 0.f : acc[d][4 * i + j] * inv;
+            const int col = 32 * d + 8 * i + 4 * h;
+            if (whole) store4(o + col, x);
+            else store4(po + col, x);
+        }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -730,46 +757,91 @@ struct PromptPlan {
     int64_t n_tiles, n_rows;
     size_t ml_bytes, bytes;
 };
+// What a launch takes, in us, by the kernel's tile (rows): a round of workgroups `start`, 128 keys of the longest workgroup `step`, and
+// of all workgroups together, spread over the CUs, `full` (the clock falls when every matrix unit works); `at_once`: workgroups that
+// run together.  Fitted to launches of 16 to 16000 tokens (7 query heads per KV head, 2 to 8 KV heads), alone in a graph, us as measured
+// for tiles of 32 / 128 / 256 rows, the choice in brackets.  Heads of 128 elements in bf16, 28 / 4 heads: prompts of 256 tokens
+// [9.8] / 12.4 / 15.6, 512 19.4 / [16.5] / 21.6, 1024 44 / [25] / 34, 2048 113 / [49] / 59, 3000 211 / 95 / [87], 7432 1026 / 437 /
+// [384]; heads of 64, 14 / 2: 1024 [12.6] / 17.9 / 23.6, 4096 74 / [57] / 76, 8000 235 / 189 / [146].
+// A split more: the join, its launch and the partial results written and read (4 TB/s).  One token of 28 / 4 heads with 1 / 4 / 16 / 64 splits:
+// 256 keys [7.4] / 8.9 / 9.8 / 10.1, 1024 14.6 / 10.8 / [10.1] / 10.1, 7432 73 / 26 / 14.5 / [11.3]; 64 tokens behind 15936 keys, tiles of
+// 128 rows, 4 / 16 / 64 splits: 71 / [34] / 65.
+struct TileCost {
+    int rows, at_once;
+    double start, step, full;
+};
+static const TileCost kCosts[3][3] = {
+    {{32, 256, 5.5, 1.32, 1.32}, {128, 256, 7.5, 1.89, 2.15}, {256, 256, 8.0, 2.97, 3.7}},   // bf16, heads of 128
+    {{32, 1024, 3.2, 0.83, 0.83}, {128, 256, 5.0, 1.45, 1.57}, {256, 256, 6.0, 2.15, 2.5}},  // bf16, heads of 64
+    {{32, 256, 5.5, 5.0, 6.2}, {0}, {0}},                                                    // fp32 (heads of 64: half the steps)
+};
+constexpr int kMostSplits = 64;
+
 static PromptPlan plan_of(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
     const int64_t G = c.n_q_heads / c.n_kv_heads;
-    PromptPlan p;
-    memset(&p, 0, sizeof(p));
-    int64_t most = 0, keys = 0;
+    const bool f32 = c.dtype == AIR_F32;
+    PromptPlan best;
+    memset(&best, 0, sizeof(best));
+    best.splits = 1;
+    best.tile_rows = 32;
+    int64_t longest = 0, n_rows = 0;
+    double bytes = 0.0;
     for (int i = 0; i < n; ++i) {
-        if (seqs[i].q_len * G > most) most = seqs[i].q_len * G;
-        if (seqs[i].q_len > 0 && seqs[i].kv_len > keys) keys = seqs[i].kv_len;
+        if (seqs[i].q_len == 0) continue;
+        n_rows += seqs[i].q_len * G;
+        bytes += 2.0 * seqs[i].kv_len * c.n_kv_heads * c.head_dim * (f32 ? 4 : 2);
+        if (seqs[i].kv_len > longest) longest = seqs[i].kv_len;
     }
-    p.few = most <= 32 || c.dtype == AIR_F32;
-    p.tile_rows = p.few ? 32 : 256;
-    for (int i = 0; i < n; ++i) {
-        p.n_tiles += (seqs[i].q_len * G + p.tile_rows - 1) / p.tile_rows;
-        p.n_rows += seqs[i].q_len * G;
+    double least = INFINITY;
+    for (const TileCost &k : kCosts[f32 ? 2 : (c.head_dim == 128 ? 0 : 1)]) {
+        if (k.rows == 0) continue;
+        const double scale = f32 && c.head_dim == 64 ? 0.5 : 1.0;
+        int64_t tiles = 0;
+        double keys = 0.0;  // of all tiles
+        for (int i = 0; i < n; ++i) {
+            const int64_t t = (seqs[i].q_len * G + k.rows - 1) / k.rows;
+            tiles += t;
+            keys += t * fmax(0.0, seqs[i].kv_len - 0.5 * seqs[i].q_len);
+        }
+        const double wgs = (double)tiles * c.n_kv_heads;
+        const double all = keys * c.n_kv_heads / kCUs / 128.0 * k.full * scale, read = bytes / 5.2e6;
+        // 1 to 8 splits, then four to every doubling
+        for (int s = 1; s <= kMostSplits && (s == 1 || longest > 64 * s); s += s < 8 ? 1 : (s < 16 ? 2 : (s < 32 ? 4 : 8))) {
+            const double work = fmax(ceil(longest / 128.0 / s) * k.step * scale, all);
+            double us = 1.0 + k.start * ceil(wgs * s / k.at_once) + sqrt(work * work + read * read);
+            if (s > 1) us += 3.3 + 2.0 * n_rows * c.n_kv_heads * s * (c.head_dim * 4 + 8) / 4e6;
+            if (us < least) {
+                least = us;
+                best.tile_rows = k.rows;
+                best.n_tiles = tiles;
+                best.splits = s;
+            }
+        }
     }
-    p.splits = 1;
-    const int64_t wgs = p.n_tiles * c.n_kv_heads, per = p.few ? 128 : 512;
-    if (wgs > 0) {
-        while (p.splits < 64 && wgs * p.splits < kCUs && keys > p.splits * per) p.splits *= 2;
+    best.few = best.tile_rows == 32;
+    best.n_rows = n_rows;
+    if (best.splits > 1) {
+        const size_t slots = (size_t)n_rows * c.n_kv_heads * best.splits;
+        best.ml_bytes = (slots * sizeof(float2) + 255) / 256 * 256;
+        best.bytes = best.ml_bytes + slots * c.head_dim * sizeof(float);
     }
-    if (p.splits > 1) {
-        const size_t slots = (size_t)p.n_rows * c.n_kv_heads * p.splits;
-        p.ml_bytes = (slots * sizeof(float2) + 255) / 256 * 256;
-        p.bytes = p.ml_bytes + slots * c.head_dim * sizeof(float);
-    }
-    return p;
+    return best;
 }
 
 size_t prompt_workspace(const air_prompt_config &c, const air_prompt_seq *seqs, int n) { return plan_of(c, seqs, n).bytes; }
 
 bool prompt_grid_ok(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
     const PromptPlan p = plan_of(c, seqs, n);
-    return p.n_rows * c.n_kv_heads < 0x7fffffffll / (c.head_dim / 4) && p.n_tiles * c.n_kv_heads * p.splits < 0x7fffffffll;
+    const int64_t rows = p.n_rows * c.n_kv_heads, wgs = p.n_tiles * c.n_kv_heads * p.splits;
+    return rows < (1 << 26) && wgs * 512 < (1ll << 32) && (p.splits == 1 || rows * 256 < (1ll << 32));
 }
 
 template <typename T, int D>
 static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &a) {
     const dim3 grid((unsigned)(p.n_tiles * a.Hkv * p.splits));
     if constexpr (sizeof(T) == 2) {
-        if (!p.few) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 1, 8>), grid, dim3(512), 0, s, a);
+        if (p.tile_rows == 256) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 1>), grid, dim3(512), 0, s, a);
+        else if (!p.few) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 2>), grid, dim3(512), 0, s, a);
     }
     if (p.few) hipLaunchKernelGGL((prompt_few_kernel<T, D>), grid, dim3(256), 0, s, a);
     if (p.splits > 1) {
@@ -779,6 +851,7 @@ static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &
         const int64_t per = kMost / groups, rows = p.n_rows * a.Hkv;
         const dim3 join((unsigned)((rows + per - 1) / per));
         if (p.splits <= groups) hipLaunchKernelGGL((prompt_join_kernel<T, D, 1>), join, dim3(256), 0, s, a, groups);
+        else if (p.splits <= 2 * groups) hipLaunchKernelGGL((prompt_join_kernel<T, D, 2>), join, dim3(256), 0, s, a, groups);
         else hipLaunchKernelGGL((prompt_join_kernel<T, D, 8>), join, dim3(256), 0, s, a, groups);
     }
 }
