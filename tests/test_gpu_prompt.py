@@ -101,6 +101,55 @@ def test_long_axes_are_split_and_joined(dtype, d, n, m):
     _check(q, k, v, spans, _run(A, q, k, v, spans))
 
 
+# The library chooses tiles of 32, 128 or 256 rows and a number of splits by the work of a call: shapes of every choice
+SHAPES = [(128, 28, 4, 1, 9000), (128, 28, 4, 7, 3001), (128, 28, 4, 200, 200), (128, 28, 4, 500, 500), (128, 28, 4, 61, 9001), (128, 28, 4, 1300, 1311),
+          (128, 28, 4, 3000, 3000), (128, 20, 5, 700, 5003), (128, 64, 8, 511, 12001), (64, 14, 2, 1, 20000), (64, 14, 2, 900, 900), (64, 14, 2, 130, 9000),
+          (64, 14, 2, 3500, 3500), (64, 14, 2, 5000, 6001), (64, 32, 8, 257, 15000)]
+
+
+@pytest.mark.parametrize("d,hq,hkv,n,m", SHAPES)
+def test_tiles_and_splits(d, hq, hkv, n, m):
+    """The result, and what is not finite: at a key behind the first rows of a tile and behind the sequence."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    q, k, v = _tensors(1, n, m + 20, hq, hkv, d, "bf16", n + m, order="token")
+    spans = [(0, 0, n, 0, m)]
+    _check(q, k, v, spans, _run(A, q, k, v, spans))
+    at = m - 1 - n // 3  # the first key that is not finite
+    v[:, :, at, 3], v[:, :, at, d - 1], v[:, :, m:] = math.inf, -math.inf, math.nan
+    k[:, :, m:] = math.nan
+    got = _run(A, q, k, v, spans)[0, :, :n].double()
+    v[:, :, at, 3], v[:, :, at, d - 1] = 0.0, 0.0
+    want, bound = _plain(q, k, v, spans)[0]
+    sees = torch.arange(n, device=q.device) + (m - n) >= at
+    assert bool((got[:, sees, 3] == math.inf).all()) and bool((got[:, sees, d - 1] == -math.inf).all())
+    got[:, sees, 3], got[:, sees, d - 1] = want[:, sees, 3], want[:, sees, d - 1]
+    assert bool(((got - want).abs() <= bound).all()), ((got - want).abs() - bound).max().item()
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+def test_prompts_pieces_and_tokens_in_one_call(dtype, d):
+    import paper_2503_23956_amd as A
+
+    pairs = [(700, 700), (1, 3000), (1, 5), (64, 2000), (0, 50), (33, 33), (1, 1), (3, 2999)]
+    spans, at, kt = [], 3, 1
+    for n, m in pairs:  # packed, with gaps between the sequences
+        spans.append((0, at, n, kt, m))
+        at, kt = at + n + 2, kt + m + 3
+    q, k, v = _tensors(1, at, kt, 12, 4, d, dtype, 77, order="token")
+    _check(q, k, v, spans, _run(A, q, k, v, spans))
+
+
+def test_sixty_four_sequences():
+    import paper_2503_23956_amd as A
+
+    spans = [(b, b % 3, 1 + (7 * b) % 40, b % 5, 1 + (7 * b) % 40 + (b % 4) * 150) for b in range(64)]
+    q, k, v = _tensors(64, 45, 600, 6, 3, 64, "bf16", 4)
+    _check(q, k, v, spans, _run(A, q, k, v, spans))
+
+
 @pytest.mark.parametrize("dtype,d", KINDS)
 def test_packed_sequences_of_a_projection_buffer(dtype, d):
     """Sequences one behind the other, q, k and v views of one [token][head][d] buffer, a scale of the caller's."""
