@@ -111,6 +111,7 @@ static air_status check_prompt(const char *who, const air_prompt_config *cfg, co
     const int64_t st[8] = {c.q_h, c.q_t, c.k_h, c.k_t, c.v_h, c.v_t, c.out_h, c.out_t};
     for (int64_t s : st)
         if (s < 0 || s % vec) return refuse(AIR_ERR_SHAPE, "%s: strides must be non-negative multiples of 16 bytes", who);
+    if (c.k_t >= (1 << 24) || c.v_t >= (1 << 24)) return refuse(AIR_ERR_SHAPE, "%s: token strides of k and v must be below 2^24 elements", who);
     int32_t most = 0;
     for (int i = 0; i < n; ++i) {
         const air_prompt_seq &s = seqs[i];

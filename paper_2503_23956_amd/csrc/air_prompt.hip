@@ -42,6 +42,8 @@ static Div div_by(int d) {
 struct PromptSpan {
     int64_t q_off, k_off, v_off, out_off;
     int32_t q_len, kv_len;
+    int32_t n_tiles;  // row tiles
+    int32_t row0;     // first row (query x query head of the group) in the partial results
 };
 struct PromptArgs {
     const void *q, *k, *v;
@@ -52,29 +54,30 @@ struct PromptArgs {
     float c;  // scale * log2(e)
     int32_t G, Hkv, n_seqs, n_tiles, n_rows, splits;
     Div by_g, by_hkv, by_splits, by_rows;
-    int32_t tile0[AIR_MAX_BATCH];  // first row tile of a sequence in the launch; behind the last sequence: INT32_MAX
-    int32_t row0[AIR_MAX_BATCH];   // first row (query x query head of the group) in the partial results, likewise
+    // The sequences lie in `s` by falling number of row tiles.  A launch takes the tiles by falling index inside their sequence, so that
+    // tiles of about equal length run side by side and the shortest at the end: of rank rank0[i] on, i + 1 sequences have a tile of the
+    // index in question (behind the last sequence: INT32_MAX)
+    int32_t rank0[AIR_MAX_BATCH];
+    int32_t row0[AIR_MAX_BATCH];  // PromptSpan::row0 (behind the last sequence: INT32_MAX)
     PromptSpan s[AIR_MAX_BATCH];
 };
-static_assert(AIR_MAX_BATCH == 64 && sizeof(PromptArgs) <= 4096, "one lane per sequence; the size of an argument block");
+static_assert(AIR_MAX_BATCH == 64 && sizeof(PromptArgs) <= 4096, "a lane per sequence; the size of an argument block");
 
-// the last sequence whose first tile (row) is not behind x: one load for all sequences, not a chain of them
-__device__ __forceinline__ int sequence_of(const int32_t *first, int x) {
-    return __popcll(__ballot(first[threadIdx.x & 63] <= x)) - 1;
-}
-
-// What the wave functions need of the storage type: CH 16-byte pieces of a row, slices of 32 bytes (one piece per lane half)
+// A tile of 32 keys in LDS, in units of 16 bytes (64 banks of 4 bytes: 256 bytes at a time).  Both layouts put what one instruction of a
+// wave reads side by side, so that no two lanes meet in a bank and the reads of a tile differ by constants only.
 template <typename T, int D>
 struct Row {
-    static constexpr int kVec = Elem<T>::kVec, kPieces = D / kVec, kSlices = kPieces / 2;
-    // Where piece p of key r lies in its tile (64 banks of 4 bytes: 256 bytes of a tile are read at a time).
-    // K: 16 bytes a lane, a row per lane: 16 neighbouring rows' pieces p lie in different banks.  V in bf16: read transposed, 32 lanes take
-    // four rows x two neighbouring pairs of pieces: eight different pairs; in fp32 half a wave takes 128 bytes of row r, the
-    // other half those of row r + 4.
-    static __device__ __forceinline__ int k_at(int r, int p) { return r * kPieces + (p ^ (kPieces == 8 ? (r >> 1) & 7 : r & 15)); }
+    static constexpr int kVec = Elem<T>::kVec, kPieces = D / kVec;  // 16-byte pieces of a row
+    static constexpr int kSlices = kPieces / 2;                     // slices of the contraction: two pieces, one per half of a wave
+    // K: [slice][row][2 pieces], lane (n, h) reads piece h of row n; slices apart by what spreads the rows of one store over the banks
+    static constexpr int kSlice = (1024 + 32 * (64 / kPieces) % 256) / 16;
+    static constexpr int kKTile = kSlices * kSlice, kVTile = 32 * kPieces;
+    static __device__ __forceinline__ int k_at(int r, int p) { return (p >> 1) * kSlice + 2 * r + (p & 1); }
+    // V: [32 columns][row][column].  bf16 is read transposed, eight rows x 64 bytes; fp32 as 128 bytes of row r (lanes 0..31) and of row
+    // r + 4 (lanes 32..63), which are neighbours
     static __device__ __forceinline__ int v_at(int r, int p) {
-        if (sizeof(T) == 4) return r * kPieces + (p ^ ((r & 4) << 1));
-        return r * kPieces + (p ^ (kPieces == 8 ? (r & 2) << 1 : ((r & 3) << 2) | ((r & 4) >> 1)));
+        if (sizeof(T) == 2) return (p >> 2) * 128 + 4 * r + (p & 3);
+        return (p >> 3) * 256 + 8 * ((r & 24) | (r & 3) << 1 | (r >> 2 & 1)) + (p & 7);
     }
 };
 
@@ -140,15 +143,15 @@ constexpr float kSlack = 8.0f;  // probabilities may be as large as 2^8: fp32 su
 // Operand V^T of output tile d for the keys 16 half .. 16 half + 15 of a tile, in the order that the logits' registers have: the transposed
 // read gives a lane four keys of a column; its address is that of row (lane % 16) / 4 of them, 8 bytes at columns
 // 16 ((lane / 16) % 2) + 4 (lane % 4).
-template <int D>
-__device__ __forceinline__ uint4 read_v(const char *sv, int half, int d) {
-    const int lane = threadIdx.x & 63;
-    const int row = 4 * (lane >> 5) + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+__device__ __forceinline__ int v_lane(int lane) {
+    return 64 * (4 * (lane >> 5) + ((lane & 15) >> 2)) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+}
+__device__ __forceinline__ uint4 read_v(const u32x4 *sv, int lane_bytes, int half, int d) {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const char *at = sv + 8 * (lane & 1) + 16 * Row<bf16_t, D>::v_at(16 * half + row, 4 * d + piece);
+    const char *at = reinterpret_cast<const char *>(sv) + lane_bytes + 2048 * d + 1024 * half;
     struct { s16x4 a, b; } v;
     v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-    v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * D * sizeof(bf16_t)));
+    v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 512));  // eight rows on
     return __builtin_bit_cast(uint4, v);
 }
 
@@ -205,7 +208,7 @@ struct Attend {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
         if constexpr (sizeof(T) == 2) {
-            const char *base = reinterpret_cast<const char *>(sv);
+            const int at = v_lane(lane);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 bf16x8 x;
@@ -214,17 +217,17 @@ struct Attend {
                 const uint4 p = __builtin_bit_cast(uint4, x);
                 l = sum_of(p, l);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) acc[d] = mma32(read_v<D>(base, half, d), p, acc[d], T());
+                for (int d = 0; d < ND; ++d) acc[d] = mma32(read_v(sv, at, half, d), p, acc[d], T());
             }
         } else {
-            const float *base = reinterpret_cast<const float *>(sv) + 4 * h * D;
+            const float *base = reinterpret_cast<const float *>(sv) + 32 * h + n;
 #pragma unroll
             for (int i = 0; i < 16; ++i) l += s[i];
 #pragma unroll
             for (int i = 0; i < 16; ++i)
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
-                    const float v = base[(8 * (i >> 2) + (i & 3)) * D + ((32 * d + n) ^ (32 * h))];
+                    const float v = base[1024 * d + 256 * (i >> 2) + 64 * (i & 3)];
                     acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], acc[d], 0, 0, 0);
                 }
         }
@@ -238,30 +241,31 @@ struct Stage {
     static constexpr int kLoads = KEYS * R::kPieces / THREADS, kRowStep = THREADS / R::kPieces;
     static_assert(kLoads >= 1 && kLoads * THREADS == KEYS * R::kPieces, "whole rounds of loads");
     int piece, row;
-    int64_t k_lane, v_lane;
+    uint32_t k_lane, v_lane;  // bytes from a tile's first row (token strides are below 2^24 elements)
     u32x4 k[kLoads], v[kLoads];
 
     __device__ __forceinline__ void init(const PromptArgs &a, int thread) {
         piece = thread % R::kPieces;
         row = thread / R::kPieces;
-        k_lane = row * a.k_t + R::kVec * piece;
-        v_lane = row * a.v_t + R::kVec * piece;
+        k_lane = (uint32_t)(row * (int)a.k_t + R::kVec * piece) * (uint32_t)sizeof(T);
+        v_lane = (uint32_t)(row * (int)a.v_t + R::kVec * piece) * (uint32_t)sizeof(T);
     }
     // keys from kb on, of kv_len in all; kg, vg: the first key's and value's rows
     __device__ __forceinline__ void load(const PromptArgs &a, const T *kg, const T *vg, int kb, int kv_len) {
-        const T *kp = kg + kb * a.k_t, *vp = vg + kb * a.v_t;
+        const char *kp = (const char *)(kg + kb * a.k_t), *vp = (const char *)(vg + kb * a.v_t);
         const int end = kv_len - 1 - kb;
         if (end >= KEYS - 1) {
+            const uint32_t k_step = kRowStep * (uint32_t)a.k_t * (uint32_t)sizeof(T), v_step = kRowStep * (uint32_t)a.v_t * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) k[i] = *reinterpret_cast<const u32x4 *>(kp + i * (kRowStep * a.k_t) + k_lane);
+            for (int i = 0; i < kLoads; ++i) k[i] = *reinterpret_cast<const u32x4 *>(kp + (uint64_t)i * k_step + k_lane);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) v[i] = *reinterpret_cast<const u32x4 *>(vp + i * (kRowStep * a.v_t) + v_lane);
+            for (int i = 0; i < kLoads; ++i) v[i] = *reinterpret_cast<const u32x4 *>(vp + (uint64_t)i * v_step + v_lane);
         } else {  // rows past the last key re-read it
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int r = min(row + kRowStep * i, end);
-                k[i] = *reinterpret_cast<const u32x4 *>(kp + r * a.k_t + R::kVec * piece);
-                v[i] = *reinterpret_cast<const u32x4 *>(vp + r * a.v_t + R::kVec * piece);
+                k[i] = *reinterpret_cast<const u32x4 *>(kp + (uint32_t)(r * (int)a.k_t + R::kVec * piece) * (uint32_t)sizeof(T));
+                v[i] = *reinterpret_cast<const u32x4 *>(vp + (uint32_t)(r * (int)a.v_t + R::kVec * piece) * (uint32_t)sizeof(T));
             }
         }
     }
@@ -283,8 +287,9 @@ struct Stage {
     __device__ __forceinline__ void store(u32x4 *sk, u32x4 *sv) const {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            sk[R::k_at(row + kRowStep * i, piece)] = k[i];
-            sv[R::v_at(row + kRowStep * i, piece)] = v[i];
+            const int r = row + kRowStep * i;
+            sk[(r >> 5) * R::kKTile + R::k_at(r & 31, piece)] = k[i];
+            sv[(r >> 5) * R::kVTile + R::v_at(r & 31, piece)] = v[i];
         }
     }
 };
@@ -312,20 +317,24 @@ __device__ __forceinline__ void store4(bf16_t *p, const f32x4 &x) {
 }
 __device__ __forceinline__ void store4(float *p, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
 
-// sequence, row tile, KV head and split of a workgroup.  The KV head is the fastest index (with 1, 2, 4 or 8 of them every XCD, dealt
-// workgroups round-robin, works on one head's K and V); the tiles come last to first: the ones with the most keys first.
+// Sequence, row tile and split of the workgroups with number y of a KV head.  The KV head itself is the fastest index of a launch: with 1,
+// 2, 4 or 8 of them every XCD, dealt workgroups round-robin, works on one head's K and V.
 struct Place {
-    int seq, tile, kvh, split;
+    int seq, tile, split;
 };
-__device__ __forceinline__ Place place_of(const PromptArgs &a, int w) {
+__device__ __forceinline__ Place place_of(const PromptArgs &a, int y) {
     Place p;
-    int x = a.by_hkv.of(w);
-    p.kvh = w - x * a.Hkv;
-    const int y = a.by_splits.of(x);
-    p.split = x - y * a.splits;
-    const int tile = a.n_tiles - 1 - y;
-    p.seq = a.n_seqs == 1 ? 0 : sequence_of(a.tile0, tile);
-    p.tile = tile - (a.n_seqs == 1 ? 0 : a.tile0[p.seq]);
+    const int rank = a.by_splits.of(y);
+    p.split = y - rank * a.splits;
+    p.seq = 0;
+    p.tile = a.s[0].n_tiles - 1 - rank;
+    if (a.n_seqs > 1) {
+        // one load for all sequences and a vote in place of a chain of loads
+        const int k = __popcll(__ballot(a.rank0[threadIdx.x & 63] <= rank));
+        const int off = rank - a.rank0[k - 1], level = off / k;
+        p.seq = __builtin_amdgcn_readfirstlane(off - level * k);
+        p.tile = __builtin_amdgcn_readfirstlane(a.s[k - 1].n_tiles - 1 - level);
+    }
     return p;
 }
 
@@ -343,15 +352,16 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
     using R = Row<T, D>;
     static_assert(sizeof(T) == 2, "bf16");
     constexpr int NW = 8, RW = NW / KW, kRows = 32 * RW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
-    constexpr int kTile = kKeys * R::kPieces, kHalf = 32 * R::kPieces;
-    __shared__ u32x4 tiles[2][kBufs][kTile];
+    __shared__ u32x4 tiles[2 * kBufs * (R::kKTile + R::kVTile)];
     __shared__ float2 s_ml[KW == 2 ? RW * 32 : 1];
     __shared__ int s_bad;
-    u32x4(&sk)[kBufs][kTile] = tiles[0], (&sv)[kBufs][kTile] = tiles[1];
+    auto sk = [&](int b) { return tiles + b % kBufs * (2 * R::kKTile); };  // the two tiles of block b
+    auto sv = [&](int b) { return tiles + 2 * kBufs * R::kKTile + b % kBufs * (2 * R::kVTile); };
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rw = wave % RW, kw = wave / RW;
-    const Place pl = place_of(a, blockIdx.x);
+    const int y = a.by_hkv.of(blockIdx.x), kvh = blockIdx.x - y * a.Hkv;
+    const Place pl = place_of(a, y);
     const PromptSpan &sp = a.s[pl.seq];
     const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
     const int row0 = pl.tile * kRows, end_row = min(row0 + kRows, n_rows);
@@ -368,7 +378,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
     float l = 0.f, ref = -INFINITY, top = -INFINITY, mul = a.c, sub = 0.f;  // top: the logit (scaled) from which on the reference is raised
     bool huge = false;
-    const int row = row0 + 32 * rw + n, m_row = min(row, n_rows - 1), tok = a.by_g.of(m_row), head = pl.kvh * a.G + m_row - tok * a.G;
+    const int row = row0 + 32 * rw + n, m_row = min(row, n_rows - 1), tok = a.by_g.of(m_row), head = kvh * a.G + m_row - tok * a.G;
     const int last = tok + shift;  // last key that the lane's query sees
     uint4 q[NS];
     {
@@ -377,7 +387,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
         for (int sl = 0; sl < NS; ++sl) q[sl] = *reinterpret_cast<const uint4 *>(qp + R::kVec * (2 * sl + h));
     }
 
-    const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
+    const T *kg = (const T *)a.k + sp.k_off + kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + kvh * a.v_h;
     Stage<T, D, 64 * NW, kKeys> stage;
     stage.init(a, threadIdx.x);
     auto load = [&](int b) {
@@ -386,7 +396,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
     auto keep = [&](int b) {
         if (b >= b1) return;
         if ((b + 1) * kKeys > see_all && stage.clean(sp.kv_len - b * kKeys)) s_bad = 1;
-        stage.store(sk[b % kBufs], sv[b % kBufs]);
+        stage.store(sk(b), sv(b));
     };
     // operands of the logits of the 32 keys whose tile starts at sk_
     auto read_k = [&](u32x4(&x)[NS], const u32x4 *sk_) {
@@ -428,13 +438,14 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
             sub = 0.f;
         }
     };
+    const int v_at = v_lane(lane);
     // The next 32 keys' logits into `next` (operands: kf), their largest into mx, while the values of this 32 keys are weighed; kf then
     // takes the operands of the keys behind those.  meet: the tile that k_after points to is whole only behind a barrier.
     auto turn = [&](f32x16 &s, f32x16 &next, float &mx, u32x4(&kf)[NS], const u32x4 *sv_, const u32x4 *k_after, bool meet) {
         uint4 vf[2][ND], p[2];
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) vf[0][d] = read_v<D>(reinterpret_cast<const char *>(sv_), 0, d);
+        for (int d = 0; d < ND; ++d) vf[0][d] = read_v(sv_, v_at, 0, d);
         logits(next, kf);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -444,7 +455,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
             p[half] = __builtin_bit_cast(uint4, x);
         }
 #pragma unroll
-        for (int d = 0; d < ND; ++d) vf[1][d] = read_v<D>(reinterpret_cast<const char *>(sv_), 1, d);
+        for (int d = 0; d < ND; ++d) vf[1][d] = read_v(sv_, v_at, 1, d);
         if (meet) lds_barrier();
         read_k(kf, k_after);
 #pragma unroll
@@ -484,27 +495,27 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
             load(b0 + 2);
         }
         lds_barrier();
-        read_k(kf, sk[b0 % kBufs] + kw * kHalf);
+        read_k(kf, sk(b0) + kw * R::kKTile);
         logits(sa, kf);
         settle(sa, largest(sa), b0 * kKeys + 32 * kw);
         // (behind the last block: logits of whatever lies there, not used)
         if constexpr (KW == 1) {
-            read_k(kf, sk[b0 % kBufs] + kHalf);
+            read_k(kf, sk(b0) + R::kKTile);
             for (int b = b0; b < b1; ++b) {
-                const u32x4 *v_now = sv[b % kBufs], *k_next = sk[(b + 1) % kBufs];
+                const u32x4 *v_now = sv(b), *k_next = sk(b + 1);
                 keep(b + 1);  // (into the buffer of block b - 2, which every wave has left before the last barrier)
                 load(b + 2);
                 turn(sa, sb, mx, kf, v_now, k_next, true);
                 settle(sb, mx, b * kKeys + 32);
-                turn(sb, sa, mx, kf, v_now + kHalf, k_next + kHalf, false);
+                turn(sb, sa, mx, kf, v_now + R::kVTile, k_next + R::kKTile, false);
                 if (b + 1 < b1) settle(sa, mx, (b + 1) * kKeys);
             }
         } else {
-            read_k(kf, sk[(b0 + 1) % kBufs] + kw * kHalf);
+            read_k(kf, sk(b0 + 1) + kw * R::kKTile);
             auto block = [&](int b, f32x16 &s, f32x16 &next) {
                 keep(b + 2);  // (into the buffer of block b - 1: its values were read before the last barrier)
                 load(b + 3);
-                turn(s, next, mx, kf, sv[b % kBufs] + kw * kHalf, sk[(b + 2) % kBufs] + kw * kHalf, true);
+                turn(s, next, mx, kf, sv(b) + kw * R::kVTile, sk(b + 2) + kw * R::kKTile, true);
                 if (b + 1 < b1) settle(next, mx, (b + 1) * kKeys + 32 * kw);
             };
             for (int b = b0; b < b1; b += 2) {
@@ -516,7 +527,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
     l += __shfl_xor(l, 32, 64);
     if constexpr (KW == 2) {  // the two waves of 32 rows: lane by lane
         static_assert(sizeof(tiles) >= RW * 32 * D * sizeof(float), "the tiles' memory holds the sums of half the waves");
-        f32x4 *sums = reinterpret_cast<f32x4 *>(&tiles[0][0][0]) + rw * (4 * ND * 64) + lane;
+        f32x4 *sums = reinterpret_cast<f32x4 *>(tiles) + rw * (4 * ND * 64) + lane;
         lds_barrier();
         if (kw == 1) {
             if (h == 0) s_ml[rw * 32 + n] = make_float2(ref, l);
@@ -542,26 +553,40 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
                 for (int j = 0; j < 4; ++j) acc[d][4 * i + j] = acc[d][4 * i + j] * f0 + x[j] * f1;
             }
     }
-    if (row >= n_rows) return;
     if (s_bad) add_not_finite(acc, vg, a.v_t, max(b0 * kKeys, see_all / kKeys * kKeys), min(b1 * kKeys, see_any), last, h);
-    const bool whole = a.splits == 1;
-    const float inv = whole ? 1.0f / l : 1.0f;
-    const bool none = whole && l == 0.f;
-    const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + a.row0[pl.seq] + row;
-    if (!whole && h == 0) a.part_ml[slot] = make_float2(ref, l);
-    T *o = (T *)a.out + sp.out_off + tok * a.out_t + head * a.out_h;
-    float *po = a.part_o + slot * D;
+    if (a.splits == 1) {
+        // through LDS (clear of the sums above), so that a row leaves in whole lines
+        const float inv = 1.0f / l;
+        if (KW == 1) lds_barrier();
+        u32x4 *rows = (rw < 4 ? sv(1) : sk(1)) + (rw & 3) * R::kVTile;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f32x4 x;
+            for (int i = 0; i < 4; ++i) {
+                f32x4 o;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = none ? 0.f : acc[d][4 * i + j] * inv;
-            const int col = 32 * d + 8 * i + 4 * h;
-            if (whole) store4(o + col, x);
-            else store4(po + col, x);
+                for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : acc[d][4 * i + j] * inv;
+                store4(reinterpret_cast<T *>(rows + n * R::kPieces + ((4 * d + i) ^ (n & (R::kPieces - 1)))) + 4 * h, o);
+            }
+        wave_sync();
+        T *out = (T *)a.out + sp.out_off + R::kVec * (lane % R::kPieces);
+#pragma unroll
+        for (int i = 0; i < R::kPieces / 2; ++i) {
+            const int r = lane / R::kPieces + (64 / R::kPieces) * i, m = row0 + 32 * rw + r;
+            const u32x4 o = rows[r * R::kPieces + ((lane % R::kPieces) ^ (r & (R::kPieces - 1)))];
+            const int to = a.by_g.of(m), hd = kvh * a.G + m - to * a.G;
+            if (m < n_rows) *reinterpret_cast<u32x4 *>(out + to * a.out_t + hd * a.out_h) = o;
         }
+    } else if (row < n_rows) {
+        const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + sp.row0 + row;
+        if (h == 0) a.part_ml[slot] = make_float2(ref, l);
+        float *po = a.part_o + slot * D + 4 * h;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store4(po + 32 * d + 8 * i, (f32x4){acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]});
+    }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -572,13 +597,14 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     using R = Row<T, D>;
-    constexpr int kTile = 32 * R::kPieces, NW = 4;
-    __shared__ u32x4 tiles[NW][2][kTile];
+    constexpr int NW = 4;
+    __shared__ u32x4 tiles[NW][R::kKTile + R::kVTile];
     __shared__ float s_m[NW][32], s_l[NW][32];
     __shared__ int s_bad;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place pl = place_of(a, blockIdx.x);
+    const int y = a.by_hkv.of(blockIdx.x), kvh = blockIdx.x - y * a.Hkv;
+    const Place pl = place_of(a, y);
     const PromptSpan &sp = a.s[pl.seq];
     const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
     const int row0 = pl.tile * 32, end_row = min(row0 + 32, n_rows);
@@ -587,14 +613,14 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     const int per_split = (n_blocks + a.splits - 1) / a.splits;
     const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
 
-    const T *kg = (const T *)a.k + sp.k_off + pl.kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + pl.kvh * a.v_h;
+    const T *kg = (const T *)a.k + sp.k_off + kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + kvh * a.v_h;
     Stage<T, D, 64, 32> stage;
     stage.init(a, lane);
     int b = b0 + wave;
     if (b < b1) stage.load(a, kg, vg, b * 32, sp.kv_len);
     Attend<T, D> at;
     at.clear();
-    const int row = min(row0 + n, n_rows - 1), tok = a.by_g.of(row), head = pl.kvh * a.G + row - tok * a.G;
+    const int row = min(row0 + n, n_rows - 1), tok = a.by_g.of(row), head = kvh * a.G + row - tok * a.G;
     const int last = tok + shift;
     {
         const T *q = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
@@ -603,7 +629,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     }
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
-    u32x4 *sk = tiles[wave][0], *sv = tiles[wave][1];
+    u32x4 *sk = tiles[wave], *sv = sk + R::kKTile;
 #pragma unroll 1
     for (; b < b1; b += NW) {
         const bool masked = (b + 1) * 32 > see_all;
@@ -625,7 +651,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     if (h == 0) s_l[wave][n] = l * f;
     constexpr int kQuads = D / 4;  // 16-byte pieces of a row of sums
     static_assert(sizeof(tiles) >= NW * 32 * D * sizeof(float), "the tiles' memory holds the sums");
-    f32x4 *sums = reinterpret_cast<f32x4 *>(&tiles[0][0][0]);
+    f32x4 *sums = reinterpret_cast<f32x4 *>(&tiles[0][0]);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -659,9 +685,9 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
             const float inv = 1.0f / lt;
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = lt == 0.f ? 0.f : x[j] * inv;
-            store4((T *)a.out + sp.out_off + t * a.out_t + (pl.kvh * a.G + g) * a.out_h + 4 * c4, x);
+            store4((T *)a.out + sp.out_off + t * a.out_t + (kvh * a.G + g) * a.out_h + 4 * c4, x);
         } else {
-            const int64_t slot = ((int64_t)pl.split * a.Hkv + pl.kvh) * a.n_rows + a.row0[pl.seq] + row0 + r;
+            const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + sp.row0 + row0 + r;
             if (c4 == 0) {
                 float mm = s_m[0][r];
 #pragma unroll
@@ -886,25 +912,28 @@ hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const air_pr
     a.splits = p.splits;
     a.n_tiles = (int)p.n_tiles;
     a.n_rows = (int)p.n_rows;
-    // sequences by rising length: the workgroups take the tiles from the last to the first, the longest first
     int order[AIR_MAX_BATCH];
     int m = 0;
     for (int i = 0; i < n; ++i) {
         if (seqs[i].q_len == 0) continue;
         int at = m++;
-        for (; at > 0 && seqs[order[at - 1]].kv_len > seqs[i].kv_len; --at) order[at] = order[at - 1];
+        for (; at > 0; --at) {
+            const air_prompt_seq &o = seqs[order[at - 1]];
+            if (o.q_len > seqs[i].q_len || (o.q_len == seqs[i].q_len && o.kv_len >= seqs[i].kv_len)) break;
+            order[at] = order[at - 1];
+        }
         order[at] = i;
     }
     a.n_seqs = m;
-    int tile0 = 0, row0 = 0;
-    for (int i = 0; i < AIR_MAX_BATCH; ++i) a.tile0[i] = a.row0[i] = 0x7fffffff;
+    for (int i = 0; i < AIR_MAX_BATCH; ++i) a.rank0[i] = a.row0[i] = 0x7fffffff;
+    int row0 = 0, rank0 = 0;
     for (int i = 0; i < m; ++i) {
         const air_prompt_seq &x = seqs[order[i]];
-        a.s[i] = PromptSpan{x.q_off, x.k_off, x.v_off, x.out_off, x.q_len, x.kv_len};
-        a.tile0[i] = tile0;
+        const int rows = x.q_len * a.G, tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+        if (i > 0) rank0 += i * (a.s[i - 1].n_tiles - tiles);
+        a.s[i] = PromptSpan{x.q_off, x.k_off, x.v_off, x.out_off, x.q_len, x.kv_len, tiles, row0};
+        a.rank0[i] = rank0;
         a.row0[i] = row0;
-        const int rows = x.q_len * a.G;
-        tile0 += (rows + p.tile_rows - 1) / p.tile_rows;
         row0 += rows;
     }
     if (c.dtype == AIR_BF16) c.head_dim == 128 ? prompt_launch<bf16_t, 128>(s, p, a) : prompt_launch<bf16_t, 64>(s, p, a);

@@ -85,7 +85,7 @@ def test_nothing_to_do_is_no_error():
     (SHAPE, dict(dtype=-1)), (SHAPE, dict(head_dim=80)), (SHAPE, dict(n_q_heads=3)), (SHAPE, dict(n_kv_heads=-2)),
     (SHAPE, dict(n=65)), (SHAPE, dict(n=-1)),
     (INVALID, dict(scale=-0.1)), (INVALID, dict(scale=float("nan"))), (INVALID, dict(scale=float("inf"))),
-    (SHAPE, dict(q_t=-512)), (SHAPE, dict(k_h=4)), (SHAPE, dict(out_t=120)), (SHAPE, dict(out_h=0)), (SHAPE, dict(out_t=0)),
+    (SHAPE, dict(q_t=-512)), (SHAPE, dict(k_h=4)), (SHAPE, dict(out_t=120)), (SHAPE, dict(k_t=1 << 24)), (SHAPE, dict(v_t=1 << 24)), (SHAPE, dict(out_h=0)), (SHAPE, dict(out_t=0)),
     (SHAPE, dict(seqs=((0, 0, 0, 0, -1, 3),))), (SHAPE, dict(seqs=((0, 0, 0, 0, 1, -3),))),
     (SHAPE, dict(seqs=((-8, 0, 0, 0, 1, 3),))), (SHAPE, dict(seqs=((0, 4, 0, 0, 1, 3),))), (SHAPE, dict(seqs=((0, 0, 0, 0, 1 << 29, 1),))),
     (WORKSPACE, dict(seqs=((0, 0, 0, 0, 1, 5000),))),
