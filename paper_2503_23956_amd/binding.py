@@ -360,24 +360,26 @@ class PreparedCall:
     """Marshalled arguments of one air_rope / air_prompt_attn call plus the tensors they point to; may be called any number of
     times (the tensors' contents may change between calls)."""
 
-    def __init__(self, args, device, keepalive, workspace_bytes=0):
-        self.args, self.device, self.workspace_bytes, self._keepalive = args, device, workspace_bytes, keepalive
+    def __init__(self, fn, args, device, keepalive, workspace_bytes=0):
+        import torch
 
+        self.torch, self.fn, self.args, self.device, self.workspace_bytes, self._keepalive = torch, fn, args, device, workspace_bytes, keepalive
+        self.on_gpu = device.type == "cuda"
+        self.index = device.index if device.index is not None else 0
+        # the current stream's handle without a stream object around it (0.1 us in place of 3), where torch offers it
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
-def _enqueue(fn, p: PreparedCall, stream, *more):
-    """fn(stream, args, more) with the tensors' device current."""
-    import torch
-
-    if p.device.type != "cuda":
-        _refuse("tensors must be on a GPU")
-    index = p.device.index if p.device.index is not None else torch.cuda.current_device()
-    if torch.cuda.current_device() != index:
-        with torch.cuda.device(index):
-            return _enqueue(fn, p, stream, *more)
-    raw = int(torch.cuda.current_stream(index).cuda_stream) if stream is None else stream
-    st = fn(raw, *p.args, *more)
-    if st != AIR_OK:
-        raise AirError(st, load_library().air_last_error(None).decode())
+    def __call__(self, stream=None, *more):
+        """Enqueues the call with the tensors' device current; stream: a raw HIP stream handle, default torch's current one there."""
+        if not self.on_gpu:
+            _refuse("tensors must be on a GPU")
+        cuda = self.torch.cuda
+        if cuda.current_device() != self.index:
+            with cuda.device(self.index):
+                return self(stream, *more)
+        st = self.fn(self.raw_stream(self.index) if stream is None else stream, *self.args, *more)
+        if st != AIR_OK:
+            raise AirError(st, load_library().air_last_error(None).decode())
 
 
 def air_rope_frequencies(n_pairs: int, theta: float, scaling=AIR_ROPE_PLAIN, factor=1.0, original_len=0, slow_turns=1.0, fast_turns=32.0):
@@ -434,13 +436,13 @@ def prepare_rope(q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, *, 
         _refuse("air_rope: freqs must be a contiguous float64 [sum(axis_pairs)] on the tensors' device")
     cfg = air_rope_config(hq, hkv or hq, d, first_dtype, B, T, layout, n_axes, (C.c_int32 * 3)(*axis_pairs), eps, scale)
     args = (C.byref(cfg), *(None if t is None else C.byref(t) for t in ts), _ptr(positions), _ptr(freqs))
-    return PreparedCall(args, first.device, (given, positions, freqs))
+    return PreparedCall(load_library().air_rope, args, first.device, (given, positions, freqs))
 
 
 def air_rope(*tensors, prepared: Optional[PreparedCall] = None, stream=None, **kw):
     """prepared: result of prepare_rope (skips the marshalling); else its arguments.  stream: a raw HIP stream handle, default torch's
     current stream on the tensors' device."""
-    _enqueue(load_library().air_rope, prepared or prepare_rope(*tensors, **kw), stream)
+    (prepared or prepare_rope(*tensors, **kw))(stream)
 
 
 def prepare_prompt_attn(q, k, v, out, spans=None, scale=0.0) -> PreparedCall:
@@ -461,20 +463,20 @@ def prepare_prompt_attn(q, k, v, out, spans=None, scale=0.0) -> PreparedCall:
         arr[i] = air_prompt_seq(b * sq[0] + q0 * sq[2], b * sk[0] + k0 * sk[2], b * sv[0] + k0 * sv[2], b * so[0] + q0 * so[2], n, m)
     cfg = air_prompt_config(q.shape[1], k.shape[1], q.shape[3], dt, scale, sq[1], sq[2], sk[1], sk[2], sv[1], sv[2], so[1], so[2])
     args = (C.byref(cfg), arr, len(spans), _ptr(q), _ptr(k), _ptr(v), _ptr(out))
-    nbytes = load_library().air_prompt_workspace_bytes(C.byref(cfg), arr, len(spans))
-    return PreparedCall(args, q.device, (q, k, v, out), nbytes)
+    lib = load_library()
+    nbytes = lib.air_prompt_workspace_bytes(C.byref(cfg), arr, len(spans))
+    return PreparedCall(lib.air_prompt_attn, args, q.device, (q, k, v, out), nbytes)
 
 
 def air_prompt_attn(*tensors, prepared: Optional[PreparedCall] = None, workspace=None, stream=None, **kw):
     """prepared: result of prepare_prompt_attn (skips the marshalling); else its arguments.  workspace: a uint8 tensor of at least
     prepared.workspace_bytes; default: one allocated for the call on torch's current stream, which is then the only stream the call may go
     to.  stream: a raw HIP stream handle, default torch's current stream on the tensors' device."""
-    import torch
-
     p = prepared or prepare_prompt_attn(*tensors, **kw)
-    if workspace is None and p.workspace_bytes and p.device.type == "cuda":
+    if workspace is None:
+        if not p.workspace_bytes or not p.on_gpu:
+            return p(stream, 0, 0)
         if stream is not None:
             _refuse("air_prompt_attn: a call on a stream of its own needs its workspace")
-        workspace = torch.empty(p.workspace_bytes, dtype=torch.uint8, device=p.device)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _enqueue(load_library().air_prompt_attn, p, stream, _ptr(workspace), nbytes)
+        workspace = p.torch.empty(p.workspace_bytes, dtype=p.torch.uint8, device=p.device)
+    p(stream, workspace.data_ptr(), workspace.numel() * workspace.element_size())

@@ -101,7 +101,7 @@ air_status air_rope_frequencies(int32_t n_pairs, double theta, int32_t scaling, 
 }
 
 // what both calls of the prompt attention refuse, but for the tensors
-static air_status check_prompt(const char *who, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n) {
+static air_status check_prompt(const char *who, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n, PromptPlan *plan) {
     if (!cfg || (n > 0 && !seqs)) return refuse(AIR_ERR_INVALID_ARG, "%s: null argument", who);
     const air_prompt_config &c = *cfg;
     if (const char *bad = geometry(c.n_q_heads, c.n_kv_heads, c.head_dim, c.dtype)) return refuse(AIR_ERR_SHAPE, "%s: %s", who, bad);
@@ -123,18 +123,20 @@ static air_status check_prompt(const char *who, const air_prompt_config *cfg, co
     }
     if ((c.n_q_heads > 1 && c.out_h < c.head_dim) || (most > 1 && c.out_t < c.head_dim))
         return refuse(AIR_ERR_SHAPE, "%s: output rows overlap", who);
-    if (!prompt_grid_ok(c, seqs, n)) return refuse(AIR_ERR_SHAPE, "%s: too many rows for one call", who);
+    *plan = prompt_plan(c, seqs, n);
+    if (!prompt_grid_ok(c, *plan)) return refuse(AIR_ERR_SHAPE, "%s: too many rows for one call", who);
     return AIR_OK;
 }
 
 size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs) {
-    if (check_prompt("air_prompt_workspace_bytes", cfg, seqs, n_seqs) != AIR_OK) return 0;
-    return prompt_workspace(*cfg, seqs, n_seqs);
+    PromptPlan plan;
+    return check_prompt("air_prompt_workspace_bytes", cfg, seqs, n_seqs, &plan) == AIR_OK ? plan.bytes : 0;
 }
 
 air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, const void *q,
                            const void *k, const void *v, void *out, void *workspace, size_t workspace_bytes) {
-    const air_status st = check_prompt("air_prompt_attn", cfg, seqs, n_seqs);
+    PromptPlan plan;
+    const air_status st = check_prompt("air_prompt_attn", cfg, seqs, n_seqs, &plan);
     if (st != AIR_OK) return st;
     bool rows = false, keys = false;
     for (int i = 0; i < n_seqs; ++i) {
@@ -144,10 +146,9 @@ air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air
     if ((rows && (!q || !out)) || (keys && (!k || !v))) return refuse(AIR_ERR_INVALID_ARG, "air_prompt_attn: null tensor pointer");
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16))
         return refuse(AIR_ERR_INVALID_ARG, "air_prompt_attn: tensors must be 16-byte aligned");
-    const size_t need = prompt_workspace(*cfg, seqs, n_seqs);
-    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
-        return refuse(AIR_ERR_WORKSPACE, "air_prompt_attn: needs a 256-byte aligned workspace of %zu bytes", need);
-    const hipError_t e = launch_prompt((hipStream_t)stream, *cfg, seqs, n_seqs, q, k, v, out, workspace);
+    if (plan.bytes > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < plan.bytes))
+        return refuse(AIR_ERR_WORKSPACE, "air_prompt_attn: needs a 256-byte aligned workspace of %zu bytes", plan.bytes);
+    const hipError_t e = launch_prompt((hipStream_t)stream, *cfg, plan, seqs, n_seqs, q, k, v, out, workspace);
     if (e != hipSuccess) return refuse(AIR_ERR_HIP, "air_prompt_attn launch: %s", hipGetErrorString(e));
     return AIR_OK;
 }

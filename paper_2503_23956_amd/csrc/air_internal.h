@@ -135,10 +135,17 @@ hipError_t launch_zero_counters(hipStream_t s, int32_t *p, int n);
 // ---- calls without a context ----
 hipError_t launch_rope(hipStream_t s, const air_rope_config &c, const air_rope_tensor *const (&t)[3], const int32_t *positions,
                        const double *freqs);
-hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const air_prompt_seq *seqs, int n, const void *q, const void *k,
-                         const void *v, void *out, void *workspace);
-size_t prompt_workspace(const air_prompt_config &c, const air_prompt_seq *seqs, int n);
-bool prompt_grid_ok(const air_prompt_config &c, const air_prompt_seq *seqs, int n);  // the launches' grids and 32-bit indexes hold the call
+// The shape of a prompt attention call: the row tiles' size, splits over the keys, what the partial results take
+struct PromptPlan {
+    bool few;  // tiles of 32 rows
+    int32_t tile_rows, splits;
+    int64_t n_tiles, n_rows;
+    size_t ml_bytes, bytes;  // workspace: (maximum, sum) pairs in front, all of it
+};
+PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, int n);
+bool prompt_grid_ok(const air_prompt_config &c, const PromptPlan &p);  // the launches' grids and 32-bit indexes hold the call
+hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const PromptPlan &p, const air_prompt_seq *seqs, int n, const void *q,
+                         const void *k, const void *v, void *out, void *workspace);
 const char *thread_error();  // text of the calling thread's last failure in a call without a context; empty: none
 
 // The cache is laid out so that the decode kernel can feed it to MFMA straight from global memory, every load

@@ -777,12 +777,6 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
 // ---------------------------------------------------------------------------------------
 // The shape of a call: which kernel, how many splits, what the partial results take
 // ---------------------------------------------------------------------------------------
-struct PromptPlan {
-    bool few;
-    int tile_rows, splits;
-    int64_t n_tiles, n_rows;
-    size_t ml_bytes, bytes;
-};
 // What a launch takes, in us, by the kernel's tile (rows): a round of workgroups `start`, 128 keys of the longest workgroup `step`, and
 // of all workgroups together, spread over the CUs, `full` (the clock falls when every matrix unit works); `at_once`: workgroups that
 // run together.  Fitted to launches of 16 to 16000 tokens (7 query heads per KV head, 2 to 8 KV heads), alone in a graph, us as measured
@@ -803,7 +797,7 @@ static const TileCost kCosts[3][3] = {
 };
 constexpr int kMostSplits = 64;
 
-static PromptPlan plan_of(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
+PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
     const int64_t G = c.n_q_heads / c.n_kv_heads;
     const bool f32 = c.dtype == AIR_F32;
     PromptPlan best;
@@ -854,10 +848,7 @@ static PromptPlan plan_of(const air_prompt_config &c, const air_prompt_seq *seqs
     return best;
 }
 
-size_t prompt_workspace(const air_prompt_config &c, const air_prompt_seq *seqs, int n) { return plan_of(c, seqs, n).bytes; }
-
-bool prompt_grid_ok(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
-    const PromptPlan p = plan_of(c, seqs, n);
+bool prompt_grid_ok(const air_prompt_config &c, const PromptPlan &p) {
     const int64_t rows = p.n_rows * c.n_kv_heads, wgs = p.n_tiles * c.n_kv_heads * p.splits;
     return rows < (1 << 26) && wgs * 512 < (1ll << 32) && (p.splits == 1 || rows * 256 < (1ll << 32));
 }
@@ -882,9 +873,8 @@ static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &
     }
 }
 
-hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const air_prompt_seq *seqs, int n, const void *q, const void *k,
-                         const void *v, void *out, void *workspace) {
-    const PromptPlan p = plan_of(c, seqs, n);
+hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const PromptPlan &p, const air_prompt_seq *seqs, int n, const void *q,
+                         const void *k, const void *v, void *out, void *workspace) {
     if (p.n_rows == 0) return hipSuccess;
     PromptArgs a;
     memset(&a, 0, sizeof(a));
