@@ -244,7 +244,7 @@ typedef enum {
 
 typedef struct {
     int32_t n_q_heads, n_kv_heads, head_dim, dtype; /* heads of q / of k and v; head_dim 64 or 128; air_dtype           */
-    int32_t batch, n_tokens;                        /* rows: batch x n_tokens (either may be 0: nothing is done)           */
+    int32_t batch, n_tokens;                        /* rows: batch x n_tokens, at most 2^27 (0: nothing is done)          */
     int32_t layout;                                 /* air_rope_layout                                                     */
     int32_t n_axes;                                 /* position axes, 1..3 (3: time, row and column of image tokens)       */
     int32_t axis_pairs[3];                          /* pairs that turn with axis 0, 1, 2, in the order of the pairs; their sum is a
@@ -296,7 +296,7 @@ typedef struct {
 
 /* One sequence: where its first query, key, value and output row lie (elements from the tensors' pointers, multiples of 16 bytes:
  * sequences packed one behind the other, rows of a padded batch or pieces of larger buffers) and how many there are.  The queries are
- * the last q_len of the kv_len positions.  Lengths may be 0. */
+ * the last q_len of the kv_len positions.  Lengths may be 0; kv_len at most 2^30, all sequences' queries times n_q_heads below 2^26. */
 typedef struct {
     int64_t q_off, k_off, v_off, out_off;
     int32_t q_len, kv_len;

@@ -40,8 +40,8 @@ air_status air_rope(void *stream, const air_rope_config *cfg, const air_rope_ten
     if (!cfg || (!q && !k && !v)) return refuse(AIR_ERR_INVALID_ARG, "air_rope: null argument");
     const air_rope_config &c = *cfg;
     if (const char *bad = geometry(c.n_q_heads, c.n_kv_heads, c.head_dim, c.dtype)) return refuse(AIR_ERR_SHAPE, "air_rope: %s", bad);
-    if (c.batch < 0 || c.n_tokens < 0 || (int64_t)c.batch * c.n_tokens > 0x7fffffff)
-        return refuse(AIR_ERR_SHAPE, "air_rope: batch and n_tokens must not be negative, their product below 2^31");
+    if (c.batch < 0 || c.n_tokens < 0 || (int64_t)c.batch * c.n_tokens > (1 << 27))
+        return refuse(AIR_ERR_SHAPE, "air_rope: batch and n_tokens must not be negative, their product at most 2^27");
     if (c.layout != AIR_ROPE_HALF && c.layout != AIR_ROPE_INTERLEAVED) return refuse(AIR_ERR_INVALID_ARG, "air_rope: unknown layout");
     if (c.n_axes < 1 || c.n_axes > 3) return refuse(AIR_ERR_INVALID_ARG, "air_rope: n_axes must be 1, 2 or 3");
     int64_t pairs = 0;
@@ -115,7 +115,7 @@ static air_status check_prompt(const char *who, const air_prompt_config *cfg, co
     int32_t most = 0;
     for (int i = 0; i < n; ++i) {
         const air_prompt_seq &s = seqs[i];
-        if (s.q_len < 0 || s.kv_len < 0) return refuse(AIR_ERR_SHAPE, "%s: negative length", who);
+        if (s.q_len < 0 || s.kv_len < 0 || s.kv_len > (1 << 30)) return refuse(AIR_ERR_SHAPE, "%s: a length is negative or above 2^30", who);
         const int64_t off[4] = {s.q_off, s.k_off, s.v_off, s.out_off};
         for (int64_t o : off)
             if (o < 0 || o % vec) return refuse(AIR_ERR_SHAPE, "%s: offsets must be non-negative multiples of 16 bytes", who);

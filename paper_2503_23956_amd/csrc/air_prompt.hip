@@ -63,21 +63,24 @@ struct PromptArgs {
 };
 static_assert(AIR_MAX_BATCH == 64 && sizeof(PromptArgs) <= 4096, "a lane per sequence; the size of an argument block");
 
-// A tile of 32 keys in LDS, in units of 16 bytes (64 banks of 4 bytes: 256 bytes at a time).  Both layouts put what one instruction of a
-// wave reads side by side, so that no two lanes meet in a bank and the reads of a tile differ by constants only.
+// A tile of 32 keys in LDS, in units of 16 bytes.  LDS serves 256 bytes at a time (64 banks of 4 bytes): both layouts put what one
+// instruction of a wave reads side by side, so that the reads of a tile differ by constants only, and the pieces of a row that 16 lanes
+// store together into different banks.
 template <typename T, int D>
 struct Row {
     static constexpr int kVec = Elem<T>::kVec, kPieces = D / kVec;  // 16-byte pieces of a row
     static constexpr int kSlices = kPieces / 2;                     // slices of the contraction: two pieces, one per half of a wave
-    // K: [slice][row][2 pieces], lane (n, h) reads piece h of row n; slices apart by what spreads the rows of one store over the banks
-    static constexpr int kSlice = (1024 + 32 * (64 / kPieces) % 256) / 16;
-    static constexpr int kKTile = kSlices * kSlice, kVTile = 32 * kPieces;
-    static __device__ __forceinline__ int k_at(int r, int p) { return (p >> 1) * kSlice + 2 * r + (p & 1); }
-    // V: [32 columns][row][column].  bf16 is read transposed, eight rows x 64 bytes; fp32 as 128 bytes of row r (lanes 0..31) and of row
-    // r + 4 (lanes 32..63), which are neighbours
+    // K: [piece][row]: lane (n, h) reads piece h of a slice of row n
+    static constexpr int kPiece = 32 + (kPieces == 8 ? 2 : 1);
+    // V: [32 columns][row][column].  bf16 is read transposed, 32 bytes of rows r and r + 4 together (lanes 0..15 and 32..47): the halves of
+    // rows 4..7 of every eight change places.  fp32 is read as 128 bytes of row r (lanes 0..31) and of row r + 4 (lanes 32..63):
+    // neighbours
+    static constexpr int kBlock = sizeof(T) == 2 ? (kPieces == 8 ? 136 : 132) : 264;
+    static constexpr int kKTile = kPieces * kPiece, kVTile = D / 32 * kBlock;
+    static __device__ __forceinline__ int k_at(int r, int p) { return p * kPiece + r; }
     static __device__ __forceinline__ int v_at(int r, int p) {
-        if (sizeof(T) == 2) return (p >> 2) * 128 + 4 * r + (p & 3);
-        return (p >> 3) * 256 + 8 * ((r & 24) | (r & 3) << 1 | (r >> 2 & 1)) + (p & 7);
+        if (sizeof(T) == 2) return (p >> 2) * kBlock + 4 * r + ((p & 3) ^ ((r >> 1) & 2));
+        return (p >> 3) * kBlock + 8 * ((r & 24) | (r & 3) << 1 | (r >> 2 & 1)) + (p & 7);
     }
 };
 
@@ -144,11 +147,12 @@ constexpr float kSlack = 8.0f;  // probabilities may be as large as 2^8: fp32 su
 // read gives a lane four keys of a column; its address is that of row (lane % 16) / 4 of them, 8 bytes at columns
 // 16 ((lane / 16) % 2) + 4 (lane % 4).
 __device__ __forceinline__ int v_lane(int lane) {
-    return 64 * (4 * (lane >> 5) + ((lane & 15) >> 2)) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    return 64 * (4 * (lane >> 5) + ((lane & 15) >> 2)) + 32 * (((lane >> 4) ^ (lane >> 5)) & 1) + 8 * (lane & 3);
 }
+template <int D>
 __device__ __forceinline__ uint4 read_v(const u32x4 *sv, int lane_bytes, int half, int d) {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const char *at = reinterpret_cast<const char *>(sv) + lane_bytes + 2048 * d + 1024 * half;
+    const char *at = reinterpret_cast<const char *>(sv) + lane_bytes + 16 * Row<bf16_t, D>::kBlock * d + 1024 * half;
     struct { s16x4 a, b; } v;
     v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
     v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 512));  // eight rows on
@@ -217,7 +221,7 @@ struct Attend {
                 const uint4 p = __builtin_bit_cast(uint4, x);
                 l = sum_of(p, l);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) acc[d] = mma32(read_v(sv, at, half, d), p, acc[d], T());
+                for (int d = 0; d < ND; ++d) acc[d] = mma32(read_v<D>(sv, at, half, d), p, acc[d], T());
             }
         } else {
             const float *base = reinterpret_cast<const float *>(sv) + 32 * h + n;
@@ -227,7 +231,7 @@ struct Attend {
             for (int i = 0; i < 16; ++i)
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
-                    const float v = base[1024 * d + 256 * (i >> 2) + 64 * (i & 3)];
+                    const float v = base[4 * R::kBlock * d + 256 * (i >> 2) + 64 * (i & 3)];
                     acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], acc[d], 0, 0, 0);
                 }
         }
@@ -445,7 +449,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
         uint4 vf[2][ND], p[2];
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) vf[0][d] = read_v(sv_, v_at, 0, d);
+        for (int d = 0; d < ND; ++d) vf[0][d] = read_v<D>(sv_, v_at, 0, d);
         logits(next, kf);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -455,7 +459,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
             p[half] = __builtin_bit_cast(uint4, x);
         }
 #pragma unroll
-        for (int d = 0; d < ND; ++d) vf[1][d] = read_v(sv_, v_at, 1, d);
+        for (int d = 0; d < ND; ++d) vf[1][d] = read_v<D>(sv_, v_at, 1, d);
         if (meet) lds_barrier();
         read_k(kf, k_after);
 #pragma unroll
@@ -558,7 +562,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
         // through LDS (clear of the sums above), so that a row leaves in whole lines
         const float inv = 1.0f / l;
         if (KW == 1) lds_barrier();
-        u32x4 *rows = (rw < 4 ? sv(1) : sk(1)) + (rw & 3) * R::kVTile;
+        u32x4 *rows = (rw < 4 ? sv(1) : sk(1)) + (rw & 3) * (32 * R::kPieces);
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll

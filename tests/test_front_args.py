@@ -55,7 +55,7 @@ INVALID, SHAPE, WORKSPACE = binding.AIR_ERR_INVALID_ARG, binding.AIR_ERR_SHAPE, 
     (INVALID, dict(pos=None)), (INVALID, dict(freqs=None)), (INVALID, dict(pos=P + 2)), (INVALID, dict(freqs=P + 4)),
     (SHAPE, dict(dtype=2)), (SHAPE, dict(head_dim=96)), (SHAPE, dict(n_q_heads=5)), (SHAPE, dict(n_kv_heads=0)),
     (SHAPE, dict(n_q_heads=32768, n_kv_heads=32768)),
-    (SHAPE, dict(batch=-1)), (SHAPE, dict(n_tokens=-1)), (SHAPE, dict(batch=1 << 16, n_tokens=1 << 16)),
+    (SHAPE, dict(batch=-1)), (SHAPE, dict(n_tokens=-1)), (SHAPE, dict(batch=1 << 16, n_tokens=1 << 16)), (SHAPE, dict(batch=3, n_tokens=1 << 26)),
     (INVALID, dict(layout=2)), (INVALID, dict(n_axes=0)), (INVALID, dict(n_axes=4)),
     (SHAPE, dict(axis_pairs=(60, 0, 0))), (SHAPE, dict(axis_pairs=(72, 0, 0))), (SHAPE, dict(axis_pairs=(-8, 0, 0))),
     (SHAPE, dict(n_axes=3, axis_pairs=(32, 40, -8))),
@@ -86,7 +86,8 @@ def test_nothing_to_do_is_no_error():
     (SHAPE, dict(n=65)), (SHAPE, dict(n=-1)),
     (INVALID, dict(scale=-0.1)), (INVALID, dict(scale=float("nan"))), (INVALID, dict(scale=float("inf"))),
     (SHAPE, dict(q_t=-512)), (SHAPE, dict(k_h=4)), (SHAPE, dict(out_t=120)), (SHAPE, dict(k_t=1 << 24)), (SHAPE, dict(v_t=1 << 24)), (SHAPE, dict(out_h=0)), (SHAPE, dict(out_t=0)),
-    (SHAPE, dict(seqs=((0, 0, 0, 0, -1, 3),))), (SHAPE, dict(seqs=((0, 0, 0, 0, 1, -3),))),
+    (SHAPE, dict(seqs=((0, 0, 0, 0, -1, 3),))), (SHAPE, dict(seqs=((0, 0, 0, 0, 1, -3),))), (SHAPE, dict(seqs=((0, 0, 0, 0, 1, (1 << 30) + 1),))),
+    (SHAPE, dict(seqs=((0, 0, 0, 0, 1 << 24, 1),))),
     (SHAPE, dict(seqs=((-8, 0, 0, 0, 1, 3),))), (SHAPE, dict(seqs=((0, 4, 0, 0, 1, 3),))), (SHAPE, dict(seqs=((0, 0, 0, 0, 1 << 29, 1),))),
     (WORKSPACE, dict(seqs=((0, 0, 0, 0, 1, 5000),))),
     (WORKSPACE, dict(seqs=((0, 0, 0, 0, 1, 5000),), ws=P, nbytes=256)),
