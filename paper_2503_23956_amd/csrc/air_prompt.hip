@@ -13,6 +13,10 @@
 // scales them with the lane's own factor.
 //
 // Softmax in the base-2 domain with a running reference per query; it is raised only when a logit lies more than kSlack above it.
+//
+// Measured (bf16, heads of 128): prompts of 7432 tokens, 28 / 4 heads, 385 us (1.03 PFLOP/s); 16910 + 16001 tokens, 64 / 8 heads, 8.08 ms (1.1
+// PFLOP/s, matrix unit busy 55 % of the clocks at 1.9 GHz; with inputs of zeros 1.34 PFLOP/s: bound by power); one token over 7432
+// keys 12.3 us, 10.8 in a graph (two launches).
 #include <math.h>
 #include <string.h>
 
@@ -469,21 +473,6 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
         l = sum_of(p[1], sum_of(p[0], l));  // the sum of what the second product takes: the weights add up to one as they are used
         mx = largest(next);
         __builtin_amdgcn_s_setprio(0);
-        if (!meet) {  // the order of issue: products, vector instructions and reads of LDS taken in turn
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x2, 40 / NS, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 2 * ND; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            }
-        }
     };
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
@@ -595,8 +584,9 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
 
 // ---------------------------------------------------------------------------------------
 // Few rows: 32 of one (sequence, KV head).  Four waves share the rows and deal the key tiles of 32 among themselves; each moves its
-// tiles through LDS of its own, the next tile's loads in flight, without a barrier.  (Also fp32 prompts: the fp32 matrix unit is so
-// much slower that re-reading K and V per 32 rows costs nothing.)
+// tiles through LDS of its own, the next tile's loads in flight, without a barrier: one wave takes in 32 keys in about 1.3 us, a launch of 16
+// tokens over 7432 keys each 244 MB in 44 us.  Also fp32 prompts (2048 tokens of 28 / 4 heads 363 us, 83 of the 146 TFLOP/s that a product of
+// matrices reaches): at the fp32 matrix unit's rate reading K and V again for every 32 rows costs nothing.
 // ---------------------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
