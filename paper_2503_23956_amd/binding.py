@@ -469,9 +469,9 @@ def prepare_prompt_attn(q, k, v, out, spans=None, scale=0.0) -> PreparedCall:
 
 
 def air_prompt_attn(*tensors, prepared: Optional[PreparedCall] = None, workspace=None, stream=None, **kw):
-    """prepared: result of prepare_prompt_attn (skips the marshalling); else its arguments.  workspace: a uint8 tensor of at least
-    prepared.workspace_bytes; default: one allocated for the call on torch's current stream, which is then the only stream the call may go
-    to.  stream: a raw HIP stream handle, default torch's current stream on the tensors' device."""
+    """prepared: result of prepare_prompt_attn (skips the marshalling); else its arguments.  workspace: a contiguous tensor of at least
+    prepared.workspace_bytes on the tensors' device; default: one allocated for the call on torch's current stream, which is then the only
+    stream the call may go to.  stream: a raw HIP stream handle, default torch's current stream on the tensors' device."""
     p = prepared or prepare_prompt_attn(*tensors, **kw)
     if workspace is None:
         if not p.workspace_bytes or not p.on_gpu:
@@ -479,4 +479,6 @@ def air_prompt_attn(*tensors, prepared: Optional[PreparedCall] = None, workspace
         if stream is not None:
             _refuse("air_prompt_attn: a call on a stream of its own needs its workspace")
         workspace = p.torch.empty(p.workspace_bytes, dtype=p.torch.uint8, device=p.device)
+    elif workspace.device != p.device or not workspace.is_contiguous():
+        _refuse("air_prompt_attn: the workspace must be contiguous, on the tensors' device")
     p(stream, workspace.data_ptr(), workspace.numel() * workspace.element_size())

@@ -175,3 +175,13 @@ def test_error_text_belongs_to_the_thread():
     t.start()
     t.join()
     assert seen == [b"null context"] and b"head_dim" in _lib().air_last_error(None)
+
+
+def test_workspace_that_is_not_one_piece_of_the_device():
+    torch = pytest.importorskip("torch")
+    q, k = torch.zeros(1, 4, 1, 64), torch.zeros(1, 2, 9000, 64)
+    call = A.prepare_prompt_attn(q, k, k, q.clone())
+    assert call.workspace_bytes > 0
+    for ws in (torch.empty(2 * call.workspace_bytes, dtype=torch.uint8)[::2], torch.empty(call.workspace_bytes, dtype=torch.uint8, device="meta")):
+        with pytest.raises(A.AirError, match="workspace"):
+            A.air_prompt_attn(prepared=call, workspace=ws)
