@@ -291,3 +291,107 @@ def test_same_bits_twice_on_streams_and_in_graphs():
     A.air_prompt_attn(prepared=call, stream=side.cuda_stream, workspace=ws)
     torch.cuda.synchronize()
     assert torch.equal(call._keepalive[3], outs[1])
+
+
+@pytest.mark.parametrize("d,hq,hkv,n,m", [(128, 28, 4, 1300, 600), (128, 28, 4, 3000, 2000), (64, 14, 2, 900, 70), (64, 14, 2, 5000, 4000), (128, 8, 8, 600, 1)])
+def test_more_rows_than_keys(d, hq, hkv, n, m):
+    """Whole tiles of rows that see no key, tiles whose last rows see some."""
+    import paper_2503_23956_amd as A
+
+    q, k, v = _tensors(1, n, m, hq, hkv, d, "bf16", n, order="token")
+    spans = [(0, 0, n, 0, m)]
+    out = _run(A, q, k, v, spans)
+    _check(q, k, v, spans, out)
+    assert bool((out[:, :, :n - m] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("n,m", [(1, 3000), (40, 40), (700, 700)])
+def test_broadcast_keys_and_outputs_inside_a_buffer(dtype, d, n, m):
+    """One head's keys and values for all KV heads and batch rows; output rows apart from each other."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    q, k, v = _tensors(2, n, m, 6, 3, d, dtype, n, order="token")
+    k, v = (x[:1, :1].expand(2, 3, m, d) for x in (k, v))
+    buf = torch.full((2, n, 7, d + 24), 42.0, dtype=q.dtype, device=q.device)
+    out = buf[:, :, :6, 8:d + 8].transpose(1, 2)
+    spans = [(b, 0, n, 0, m) for b in range(2)]
+    _check(q, k, v, spans, _run(A, q, k, v, spans, out=out))
+    out.fill_(42.0)
+    assert bool((buf == 42.0).all())
+
+
+def test_calls_without_work():
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    q, k, v = _tensors(2, 5, 9, 4, 2, 64, "bf16", 1)
+    assert bool((_run(A, q, k, v, []) == 42.0).all())
+    assert bool((_run(A, q, k, v, [(0, 5, 0, 9, 0), (1, 2, 0, 0, 9)]) == 42.0).all())
+    assert bool((_run(A, q, k[:, :, :0], v[:, :, :0], None) == 0.0).all())
+    _run(A, q[:, :, :0], k, v, None)
+    _run(A, q[:0], k[:0], v[:0], None)
+    with pytest.raises(A.AirError):
+        A.air_prompt_attn(q, k, v, torch.empty_like(q), spans=[(0, 0, 1, 0, 1)] * 65)
+    call = A.prepare_prompt_attn(q, k, v, torch.empty_like(q))
+    with pytest.raises(A.AirError, match="workspace"):
+        A.air_prompt_attn(prepared=call, workspace=torch.empty(1 << 20, dtype=torch.uint8))  # the host's
+
+
+def test_as_many_rows_as_a_call_takes():
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    n, m = 2 ** 26 - 1, 100  # 8.6 GB of queries, 100 of them see keys
+    q = torch.empty((1, 1, n, 64), dtype=torch.bfloat16, device="cuda:0")
+    out = torch.full_like(q, 42.0)
+    q[:, :, n - 1000:] = torch.randn((1, 1, 1000, 64), device="cuda:0").bfloat16()
+    _, k, v = _tensors(1, 1, m, 1, 1, 64, "bf16", 8)
+    _run(A, q, k, v, [(0, 0, n, 0, m)], out=out)
+    assert int(torch.count_nonzero(out[:, :, :n - m])) == 0
+    last = (0, 0, 1000, 0, m)
+    _check(q[:, :, n - 1000:], k, v, [last], out[:, :, n - 1000:])
+    with pytest.raises(A.AirError):
+        wide = q.expand(1, 2, n, 64)  # twice the rows
+        A.air_prompt_attn(wide, k, v, torch.empty((1, 2, 1, 64), dtype=q.dtype, device="cuda:0").expand(1, 2, n, 64))
+
+
+def test_two_calls_at_once_and_two_graphs_of_one_workspace():
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    q, k, v = _tensors(4, 260, 3000, 14, 2, 128, "bf16", 5)
+    jobs = [[(0, 0, 1, 0, 3000), (1, 0, 3, 0, 2900)], [(2, 0, 260, 0, 3000), (3, 0, 7, 0, 1000)]]
+    want = [_run(A, q, k, v, spans) for spans in jobs]
+    outs = [torch.zeros_like(w) for w in want]
+    calls = [A.prepare_prompt_attn(q, k, v, o, spans=spans) for o, spans in zip(outs, jobs)]
+    own = [torch.empty(c.workspace_bytes, dtype=torch.uint8, device="cuda:0") for c in calls]
+    assert all(c.workspace_bytes > 0 for c in calls)
+    sides = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for _ in range(10):  # side by side, each with its workspace
+        for c, ws, s in zip(calls, own, sides):
+            A.air_prompt_attn(prepared=c, workspace=ws, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for o, w, spans in zip(outs, want, jobs):
+        for b, q0, n, _, _ in spans:
+            assert torch.equal(o[b, :, q0:q0 + n], w[b, :, q0:q0 + n])
+    shared = torch.empty(max(c.workspace_bytes for c in calls), dtype=torch.uint8, device="cuda:0")
+    graphs = [torch.cuda.CUDAGraph() for _ in calls]
+    for g, c in zip(graphs, calls):
+        with torch.cuda.graph(g):
+            A.air_prompt_attn(prepared=c, workspace=shared)
+    for step in range(4):
+        for o in outs:
+            o.zero_()
+        for g in graphs if step % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        for o, w, spans in zip(outs, want, jobs):
+            for b, q0, n, _, _ in spans:
+                assert torch.equal(o[b, :, q0:q0 + n], w[b, :, q0:q0 + n])

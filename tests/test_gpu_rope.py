@@ -184,3 +184,46 @@ def test_graph_replays_and_other_streams():
             for o, w in zip(outs, want):
                 o[2] = 0
                 w[2] = 0
+
+
+def test_calls_without_work_and_broadcast_sources():
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    q, k, v = _inputs(2, 9, 4, 2, 64, torch.bfloat16, "token", 2)
+    freqs = torch.tensor(A.air_rope_frequencies(32, 1e4)[0], device="cuda:0")
+    pos = torch.arange(18, dtype=torch.int32, device="cuda:0").view(2, 9)
+    none = torch.zeros((2, 0), dtype=torch.int32, device="cuda:0")
+    A.air_rope(q[:, :, :0], k[:, :, :0], v[:, :, :0], positions=none, freqs=freqs, axis_pairs=(32,))
+    wide = k[:1, :1, :1].expand(2, 4, 9, 64)  # one row for all
+    kw = dict(positions=pos, freqs=freqs, axis_pairs=(32,))
+    outs = [torch.zeros((2, 4, 9, 64), dtype=q.dtype, device="cuda:0") for _ in range(2)]
+    A.air_rope(wide, q_out=outs[0], **kw)
+    A.air_rope(wide.contiguous(), q_out=outs[1], **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(*outs)
+    with pytest.raises(A.AirError):  # in place: the rows of the destination would overlap
+        A.air_rope(wide, **kw)
+
+
+def test_as_many_rows_as_a_call_takes():
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    n, tail = 2 ** 27, 5000  # 17 GB
+    x = torch.empty((1, 1, n, 64), dtype=torch.bfloat16, device="cuda:0")
+    x[:, :, n - tail:] = torch.randn((1, 1, tail, 64), device="cuda:0").bfloat16()
+    pos = torch.full((1, n), -1, dtype=torch.int32, device="cuda:0")
+    pos[0, n - tail:] = torch.arange(tail, dtype=torch.int32, device="cuda:0")
+    freqs = torch.tensor(A.air_rope_frequencies(32, 1e4)[0], device="cuda:0")
+    few = x[:, :, n - tail:].clone()
+    few_pos = pos[:, n - tail:].contiguous()
+    A.air_rope(x, positions=pos, freqs=freqs, axis_pairs=(32,))
+    A.air_rope(few, positions=few_pos, freqs=freqs, axis_pairs=(32,))
+    torch.cuda.synchronize()
+    assert torch.equal(x[:, :, n - tail:], few)
+    more = torch.empty((1, 1, 1, 64), dtype=torch.bfloat16, device="cuda:0").expand(1, 1, n + 1, 64)
+    with pytest.raises(A.AirError):
+        A.air_rope(more, q_out=more)
