@@ -583,10 +583,85 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------
+// Many rows, fp32: four waves of 32 rows share the key tiles of 32 in LDS (two buffers, one barrier a tile, the next tile's loads in flight).
+// The fp32 matrix unit sets the pace: 64 clocks a product of 32 x 32 x 2.  Two workgroups a CU, so that one's exponentials, stores and reads
+// of LDS run under the other's products.  28 / 4 heads of 128: 5000 tokens 1.42 ms, 126 of the 146 TFLOP/s that a product of matrices reaches (in
+// tiles of 32 rows, which read K and V from the L2 caches four times as often, 1.86 ms); 2048 tokens 290 us (356).
+// ---------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
+    using R = Row<T, D>;
+    constexpr int kRows = 128, ND = D / 32;
+    __shared__ u32x4 sk[2][R::kKTile], sv[2][R::kVTile];
+    __shared__ int s_bad;
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int y = a.by_hkv.of(blockIdx.x), kvh = blockIdx.x - y * a.Hkv;
+    const Place pl = place_of(a, y);
+    const PromptSpan &sp = a.s[pl.seq];
+    const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
+    const int row0 = pl.tile * kRows, end_row = min(row0 + kRows, n_rows);
+    const int see_all = max(0, a.by_g.of(row0) + shift + 1), see_any = max(0, a.by_g.of(end_row - 1) + shift + 1);
+    const int n_blocks = (see_any + 31) / 32;
+    const int per_split = (n_blocks + a.splits - 1) / a.splits;
+    const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
+
+    const T *kg = (const T *)a.k + sp.k_off + kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + kvh * a.v_h;
+    Stage<T, D, 256, 32> stage;
+    stage.init(a, threadIdx.x);
+    if (b0 < b1) stage.load(a, kg, vg, b0 * 32, sp.kv_len);
+    Attend<T, D> at;
+    at.clear();
+    const int row = row0 + 32 * wave + n, m_row = min(row, n_rows - 1), tok = a.by_g.of(m_row), head = kvh * a.G + m_row - tok * a.G;
+    const int last = tok + shift;
+    const int wave_last = a.by_g.of(min(row0 + 32 * wave + 31, n_rows - 1)) + shift;  // last key that a row of the wave sees
+    {
+        const T *q = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
+#pragma unroll
+        for (int sl = 0; sl < R::kSlices; ++sl) at.q[sl] = *reinterpret_cast<const uint4 *>(q + R::kVec * (2 * sl + h));
+    }
+    if (threadIdx.x == 0) s_bad = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) {
+        const bool masked = (b + 1) * 32 > see_all;
+        if (masked && stage.clean(sp.kv_len - b * 32)) s_bad = 1;
+        stage.store(sk[b & 1], sv[b & 1]);  // (read for block b - 2, which every wave has left before the last barrier)
+        lds_barrier();
+        if (b + 1 < b1) stage.load(a, kg, vg, (b + 1) * 32, sp.kv_len);
+        if (b * 32 <= wave_last) at.step(sk[b & 1], sv[b & 1], masked, last - b * 32, a.c);
+    }
+    const float l = at.l + __shfl_xor(at.l, 32, 64);
+    if (s_bad) add_not_finite(at.acc, vg, a.v_t, max(b0, see_all / 32) * 32, min(b1 * 32, see_any), last, h);
+    if (row >= n_rows) return;
+    if (a.splits == 1) {
+        const float inv = 1.0f / l;
+        T *o = (T *)a.out + sp.out_off + tok * a.out_t + head * a.out_h + 4 * h;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f32x4 x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : at.acc[d][4 * i + j] * inv;
+                store4(o + 32 * d + 8 * i, x);
+            }
+    } else {
+        const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + sp.row0 + row;
+        if (h == 0) a.part_ml[slot] = make_float2(at.m, l);
+        float *po = a.part_o + slot * D + 4 * h;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store4(po + 32 * d + 8 * i, (f32x4){at.acc[d][4 * i], at.acc[d][4 * i + 1], at.acc[d][4 * i + 2], at.acc[d][4 * i + 3]});
+    }
+}
+
+// ---------------------------------------------------------------------------------------
 // Few rows: 32 of one (sequence, KV head).  Four waves share the rows and deal the key tiles of 32 among themselves; each moves its
 // tiles through LDS of its own, the next tile's loads in flight, without a barrier: one wave takes in 32 keys in about 1.3 us, a launch of 16
-// tokens over 7432 keys each 244 MB in 44 us.  Also fp32 prompts (2048 tokens of 28 / 4 heads 363 us, 83 of the 146 TFLOP/s that a product of
-// matrices reaches): at the fp32 matrix unit's rate reading K and V again for every 32 rows costs nothing.
+// tokens over 7432 keys each 244 MB in 44 us.
 // ---------------------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
@@ -780,14 +855,17 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
 // A split more: the join, its launch and the partial results written and read (4 TB/s).  One token of 28 / 4 heads with 1 / 4 / 16 / 64 splits:
 // 256 keys [7.4] / 8.9 / 9.8 / 10.1, 1024 14.6 / 10.8 / [10.1] / 10.1, 7432 73 / 26 / 14.5 / [11.3]; 64 tokens behind 15936 keys, tiles of
 // 128 rows, 4 / 16 / 64 splits: 71 / [34] / 65.
+// fp32, tiles of 32 / 128 rows, each with its best splits.  Heads of 128, 28 / 4: 512 tokens [40] / 47, 1024 115 / [94], 2048 355 / [279], 5000 1860 /
+// [1414], 64 behind 7936 keys 96 / [82]; heads of 64, 14 / 2: 512 [17.0] / 21, 2048 98 / [91], 8000 1013 / [909].
 struct TileCost {
     int rows, at_once;
     double start, step, full;
 };
-static const TileCost kCosts[3][3] = {
+static const TileCost kCosts[4][3] = {
     {{32, 256, 5.5, 1.32, 1.32}, {128, 256, 7.5, 1.89, 2.15}, {256, 256, 8.0, 2.97, 3.7}},   // bf16, heads of 128
     {{32, 1024, 3.2, 0.83, 0.83}, {128, 256, 5.0, 1.45, 1.57}, {256, 256, 6.0, 2.15, 2.5}},  // bf16, heads of 64
-    {{32, 256, 5.5, 5.0, 6.2}, {0}, {0}},                                                    // fp32 (heads of 64: half the steps)
+    {{32, 256, 5.5, 5.0, 6.2}, {128, 512, 7.0, 16.7, 15.8}, {0}},                            // fp32, heads of 128
+    {{32, 512, 3.2, 2.8, 2.4}, {128, 768, 5.0, 9.2, 8.0}, {0}},                              // fp32, heads of 64
 };
 constexpr int kMostSplits = 64;
 
@@ -807,9 +885,8 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
         if (seqs[i].kv_len > longest) longest = seqs[i].kv_len;
     }
     double least = INFINITY;
-    for (const TileCost &k : kCosts[f32 ? 2 : (c.head_dim == 128 ? 0 : 1)]) {
+    for (const TileCost &k : kCosts[(f32 ? 2 : 0) + (c.head_dim == 128 ? 0 : 1)]) {
         if (k.rows == 0) continue;
-        const double scale = f32 && c.head_dim == 64 ? 0.5 : 1.0;
         int64_t tiles = 0;
         double keys = 0.0;  // of all tiles
         for (int i = 0; i < n; ++i) {
@@ -818,10 +895,13 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
             keys += t * fmax(0.0, seqs[i].kv_len - 0.5 * seqs[i].q_len);
         }
         const double wgs = (double)tiles * c.n_kv_heads;
-        const double all = keys * c.n_kv_heads / kCUs / 128.0 * k.full * scale, read = bytes / 5.2e6;
+        const double full = keys * c.n_kv_heads / kCUs / 128.0 * k.full, read = bytes / 5.2e6;
         // 1 to 8 splits, then four to every doubling
         for (int s = 1; s <= kMostSplits && (s == 1 || longest > 64 * s); s += s < 8 ? 1 : (s < 16 ? 2 : (s < 32 ? 4 : 8))) {
-            const double work = fmax(ceil(longest / 128.0 / s) * k.step * scale, all);
+            // fp32 workgroups are long: whole ones to a CU, and the longest shares its CU's matrix units once there is a second
+            const double deal = f32 ? fmax(1.0, wgs * s / kCUs) : 1.0;
+            const double all = full * ceil(deal) / deal, shared = deal > 1.0 ? 1.4 : 1.0;
+            const double work = fmax(ceil(longest / 128.0 / s) * k.step * shared, all);
             double us = 1.0 + k.start * ceil(wgs * s / k.at_once) + sqrt(work * work + read * read);
             if (s > 1) us += 3.3 + 2.0 * n_rows * c.n_kv_heads * s * (c.head_dim * 4 + 8) / 4e6;
             if (us < least) {
@@ -853,6 +933,9 @@ static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &
     if constexpr (sizeof(T) == 2) {
         if (p.tile_rows == 256) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 1>), grid, dim3(512), 0, s, a);
         else if (!p.few) hipLaunchKernelGGL((prompt_pipe_kernel<T, D, 2>), grid, dim3(512), 0, s, a);
+    }
+    if constexpr (sizeof(T) == 4) {
+        if (!p.few) hipLaunchKernelGGL((prompt_share_kernel<T, D>), grid, dim3(256), 0, s, a);
     }
     if (p.few) hipLaunchKernelGGL((prompt_few_kernel<T, D>), grid, dim3(256), 0, s, a);
     if (p.splits > 1) {

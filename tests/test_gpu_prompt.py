@@ -107,14 +107,18 @@ SHAPES = [(128, 28, 4, 1, 9000), (128, 28, 4, 7, 3001), (128, 28, 4, 200, 200), 
           (64, 14, 2, 3500, 3500), (64, 14, 2, 5000, 6001), (64, 32, 8, 257, 15000)]
 
 
-@pytest.mark.parametrize("d,hq,hkv,n,m", SHAPES)
-def test_tiles_and_splits(d, hq, hkv, n, m):
+F32_SHAPES = [(128, 28, 4, 61, 8001), (128, 28, 4, 700, 701), (128, 28, 4, 1500, 1500), (128, 20, 5, 300, 3001), (128, 3, 3, 1700, 1700),
+              (64, 14, 2, 2100, 2100), (64, 14, 2, 3500, 3600), (64, 32, 8, 257, 5000)]
+
+
+@pytest.mark.parametrize("dtype,d,hq,hkv,n,m", [("bf16", *s) for s in SHAPES] + [("f32", *s) for s in F32_SHAPES])
+def test_tiles_and_splits(dtype, d, hq, hkv, n, m):
     """The result, and what is not finite: at a key behind the first rows of a tile and behind the sequence."""
     import torch
 
     import paper_2503_23956_amd as A
 
-    q, k, v = _tensors(1, n, m + 20, hq, hkv, d, "bf16", n + m, order="token")
+    q, k, v = _tensors(1, n, m + 20, hq, hkv, d, dtype, n + m, order="token")
     spans = [(0, 0, n, 0, m)]
     _check(q, k, v, spans, _run(A, q, k, v, spans))
     at = m - 1 - n // 3  # the first key that is not finite
@@ -294,11 +298,12 @@ def test_same_bits_twice_on_streams_and_in_graphs():
 
 
 @pytest.mark.parametrize("d,hq,hkv,n,m", [(128, 28, 4, 1300, 600), (128, 28, 4, 3000, 2000), (64, 14, 2, 900, 70), (64, 14, 2, 5000, 4000), (128, 8, 8, 600, 1)])
-def test_more_rows_than_keys(d, hq, hkv, n, m):
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_rows_than_keys(dtype, d, hq, hkv, n, m):
     """Whole tiles of rows that see no key, tiles whose last rows see some."""
     import paper_2503_23956_amd as A
 
-    q, k, v = _tensors(1, n, m, hq, hkv, d, "bf16", n, order="token")
+    q, k, v = _tensors(1, n, m, hq, hkv, d, dtype, n, order="token")
     spans = [(0, 0, n, 0, m)]
     out = _run(A, q, k, v, spans)
     _check(q, k, v, spans, out)
