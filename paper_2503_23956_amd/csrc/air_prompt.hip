@@ -614,7 +614,8 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
     at.clear();
     const int row = row0 + 32 * wave + n, m_row = min(row, n_rows - 1), tok = a.by_g.of(m_row), head = kvh * a.G + m_row - tok * a.G;
     const int last = tok + shift;
-    const int wave_last = a.by_g.of(min(row0 + 32 * wave + 31, n_rows - 1)) + shift;  // last key that a row of the wave sees
+    // last key that a row of the wave sees
+    const int wave_last = row0 + 32 * wave < n_rows ? a.by_g.of(min(row0 + 32 * wave + 31, n_rows - 1)) + shift : -1;
     {
         const T *q = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
 #pragma unroll
