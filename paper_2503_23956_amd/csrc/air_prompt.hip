@@ -847,26 +847,27 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
 // ---------------------------------------------------------------------------------------
 // The shape of a call: which kernel, how many splits, what the partial results take
 // ---------------------------------------------------------------------------------------
-// What a launch takes, in us, by the kernel's tile (rows): a round of workgroups `start`, 128 keys of the longest workgroup `step`, and
-// of all workgroups together, spread over the CUs, `full` (the clock falls when every matrix unit works); `at_once`: workgroups that
-// run together.  Fitted to launches of 16 to 16000 tokens (7 query heads per KV head, 2 to 8 KV heads), alone in a graph, us as measured
-// for tiles of 32 / 128 / 256 rows, the choice in brackets.  Heads of 128 elements in bf16, 28 / 4 heads: prompts of 256 tokens
-// [9.8] / 12.4 / 15.6, 512 19.4 / [16.5] / 21.6, 1024 44 / [25] / 34, 2048 113 / [49] / 59, 3000 211 / 95 / [87], 7432 1026 / 437 /
-// [384]; heads of 64, 14 / 2: 1024 [12.6] / 17.9 / 23.6, 4096 74 / [57] / 76, 8000 235 / 189 / [146].
-// A split more: the join, its launch and the partial results written and read (4 TB/s).  One token of 28 / 4 heads with 1 / 4 / 16 / 64 splits:
-// 256 keys [7.4] / 8.9 / 9.8 / 10.1, 1024 14.6 / 10.8 / [10.1] / 10.1, 7432 73 / 26 / 14.5 / [11.3]; 64 tokens behind 15936 keys, tiles of
-// 128 rows, 4 / 16 / 64 splits: 71 / [34] / 65.
-// fp32, tiles of 32 / 128 rows, each with its best splits.  Heads of 128, 28 / 4: 512 tokens [40] / 47, 1024 115 / [94], 2048 355 / [279], 5000 1860 /
-// [1414], 64 behind 7936 keys 96 / [82]; heads of 64, 14 / 2: 512 [17.0] / 21, 2048 98 / [91], 8000 1013 / [909].
+// What a call takes, in us, by the kernel's tile (rows): its first workgroups `start`, each round of them after that `round` (`at_once`
+// workgroups run together); 128 keys of the longest workgroup `step` (keys are dealt by `grain`), and of all workgroups together,
+// spread over the CUs, `full` (the clock falls when every matrix unit works).  Splits: the join, its launch and the partial results written and
+// read.  Fitted to 880 calls of 1 to 17000 tokens, 1 to 33 sequences, 1 to 16 query heads per KV head, alone in a graph, every tile and split
+// measured; on 145 others the choice takes 1 % longer than the best of up to 60 on average, 11 % at worst.  Some, us in tiles of 32 / 128 / 256
+// rows, each with the splits that are chosen for it, the choice in brackets.
+// bf16, heads of 128, 28 / 4 of them: prompts of 256 tokens [9.8] / 11.5 / 13.4, 512 19 / [15.7] / 19.7, 1024 45 / [24] / 32, 2048 113 / [48] / 57,
+// 3000 215 / 95 / [88], 7432 1055 / 455 / [400]; heads of 64, 14 / 2: 1024 [12.4] / 16 / 23, 4096 79 / [52] / 60, 8000 246 / 177 / [154];
+// 33 prompts of 200 tokens, 16 / 1: 35 / 21 / [15].  One token of 28 / 4 heads of 128 with 1 / 4 / 16 / 64 splits: 7432 keys 75 / 26 / 13.9 / [11.0]; 1024
+// keys 14.6 without, [9.7] with; 256 keys [7.2].  64 tokens behind 15936 keys, tiles of 128 rows, 4 / 16 / 64 splits: 71 / 35 / 68 (chosen: 33.7).
+// fp32, tiles of 32 / 128 rows: heads of 128, 28 / 4: 512 tokens [40] / 47, 1024 114 / [94], 2048 356 / [291], 5000 1862 / [1466],
+// 64 behind 7936 keys 96 / [83]; heads of 64, 14 / 2: 512 [18] / 23, 2048 93 / [91], 8000 1017 / [916].
 struct TileCost {
-    int rows, at_once;
-    double start, step, full;
+    int rows, at_once, grain;
+    double start, round, step, full;
 };
 static const TileCost kCosts[4][3] = {
-    {{32, 256, 5.5, 1.32, 1.32}, {128, 256, 7.5, 1.89, 2.15}, {256, 256, 8.0, 2.97, 3.7}},   // bf16, heads of 128
-    {{32, 1024, 3.2, 0.83, 0.83}, {128, 256, 5.0, 1.45, 1.57}, {256, 256, 6.0, 2.15, 2.5}},  // bf16, heads of 64
-    {{32, 256, 5.5, 5.0, 6.2}, {128, 512, 7.0, 16.7, 15.8}, {0}},                            // fp32, heads of 128
-    {{32, 512, 3.2, 2.8, 2.4}, {128, 768, 5.0, 9.2, 8.0}, {0}},                              // fp32, heads of 64
+    {{32, 256, 128, 5.9, 3.9, 1.32, 1.57}, {128, 256, 64, 7.0, 4.5, 1.98, 2.3}, {256, 256, 64, 6.7, 3.6, 3.07, 3.46}},  // bf16, heads of 128
+    {{32, 512, 128, 5.1, 3.9, 0.77, 0.62}, {128, 256, 64, 5.8, 2.6, 1.34, 1.63}, {256, 256, 64, 5.6, 1.0, 2.26, 2.57}},  // bf16, heads of 64
+    {{32, 256, 128, 7.4, 7.6, 4.8, 5.6}, {128, 512, 32, 4.9, 1.7, 18.4, 15.2}, {0}},                                    // fp32, heads of 128
+    {{32, 512, 128, 5.6, 4.6, 2.9, 2.55}, {128, 768, 32, 3.8, 0.0, 11.9, 8.4}, {0}},                                    // fp32, heads of 64
 };
 constexpr int kMostSplits = 64;
 
@@ -899,12 +900,11 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
         const double full = keys * c.n_kv_heads / kCUs / 128.0 * k.full, read = bytes / 5.2e6;
         // 1 to 8 splits, then four to every doubling
         for (int s = 1; s <= kMostSplits && (s == 1 || longest > 64 * s); s += s < 8 ? 1 : (s < 16 ? 2 : (s < 32 ? 4 : 8))) {
-            // fp32 workgroups are long: whole ones to a CU, and the longest shares its CU's matrix units once there is a second
-            const double deal = f32 ? fmax(1.0, wgs * s / kCUs) : 1.0;
-            const double all = full * ceil(deal) / deal, shared = deal > 1.0 ? 1.4 : 1.0;
-            const double work = fmax(ceil(longest / 128.0 / s) * k.step * shared, all);
-            double us = 1.0 + k.start * ceil(wgs * s / k.at_once) + sqrt(work * work + read * read);
-            if (s > 1) us += 3.3 + 2.0 * n_rows * c.n_kv_heads * s * (c.head_dim * 4 + 8) / 4e6;
+            const double at_work = fmax(1.0, wgs * s / kCUs);  // workgroups a CU: part of a last, uneven deal is lost
+            const double all = full * (1.0 + 0.3 * (ceil(at_work) / at_work - 1.0));
+            const double work = fmax(ceil((double)longest / s / k.grain) * k.grain / 128.0 * k.step, all);
+            double us = k.start + k.round * (ceil(fmax(1.0, wgs * s / k.at_once)) - 1.0) + sqrt(work * work + read * read);
+            if (s > 1) us += 2.9 + 2.1 * n_rows * c.n_kv_heads * s * (c.head_dim * 4 + 8) / 4e6;
             if (us < least) {
                 least = us;
                 best.tile_rows = k.rows;
