@@ -146,6 +146,17 @@ def test_prompts_pieces_and_tokens_in_one_call(dtype, d):
     _check(q, k, v, spans, _run(A, q, k, v, spans))
 
 
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("hq,hkv,pairs", [(16, 1, [(20 + (11 * i) % 37, 20 + (11 * i) % 37 + (i % 4) * (i % 3) * 9) for i in range(33)]),
+                                          (28, 4, [(901, 901), (333, 400), (1, 1), (0, 0), (612, 612), (95, 1500), (1100, 800)])])
+def test_ragged_prompts(dtype, d, hq, hkv, pairs):
+    import paper_2503_23956_amd as A
+
+    spans = [(b, 0, n, 0, m) for b, (n, m) in enumerate(pairs)]
+    q, k, v = _tensors(len(pairs), max(n for n, _ in pairs), max(m for _, m in pairs), hq, hkv, d, dtype, hq + d, order="token")
+    _check(q, k, v, spans, _run(A, q, k, v, spans))
+
+
 def test_sixty_four_sequences():
     import paper_2503_23956_amd as A
 
