@@ -14,8 +14,8 @@
 //
 // Softmax in the base-2 domain with a running reference per query; it is raised only when a logit lies more than kSlack above it.
 //
-// Measured (bf16, heads of 128): prompts of 7432 tokens, 28 / 4 heads, 385 us (1.03 PFLOP/s); 16910 + 16001 tokens, 64 / 8 heads, 8.08 ms (1.1
-// PFLOP/s, matrix unit busy 55 % of the clocks at 1.9 GHz; with inputs of zeros 1.34 PFLOP/s: bound by power); one token over 7432
+// Measured (bf16, heads of 128): prompts of 7432 tokens, 28 / 4 heads, 385 us (1.03 PFLOP/s); 16910 + 16001 tokens, 64 / 8 heads, 8.08 ms (on
+// another card 405 and 8.48; 1.1 PFLOP/s, matrix unit busy 55 % of the clocks at 1.9 GHz; with inputs of zeros 1.34 PFLOP/s: bound by power); one token over 7432
 // keys 12.3 us, 10.8 in a graph (two launches).
 #include <math.h>
 #include <string.h>
