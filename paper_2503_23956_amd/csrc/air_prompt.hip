@@ -15,8 +15,8 @@
 // Softmax in the base-2 domain with a running reference per query; it is raised only when a logit lies more than kSlack above it.
 //
 // Measured (bf16, heads of 128): prompts of 7432 tokens, 28 / 4 heads, 385 us (1.03 PFLOP/s); 16910 + 16001 tokens, 64 / 8 heads, 8.08 ms (on
-// another card 405 and 8.48; 1.1 PFLOP/s, matrix unit busy 55 % of the clocks at 1.9 GHz; with inputs of zeros 1.34 PFLOP/s: bound by power); one token over 7432
-// keys 12.3 us, 10.8 in a graph (two launches).
+// another card 405 and 8.48; 1.1 PFLOP/s, matrix unit busy 55 % of the clocks at 1.9 GHz; with inputs of zeros 1.34 PFLOP/s: bound by power); one
+// token over 7432 keys 11.5 us (two launches).
 #include <math.h>
 #include <string.h>
 
@@ -325,23 +325,42 @@ __device__ __forceinline__ void store4(bf16_t *p, const f32x4 &x) {
 }
 __device__ __forceinline__ void store4(float *p, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
 
+// Brings the arguments that every workgroup needs into registers together: left to themselves, they are read where they are used, one wait for
+// memory behind the other (one token over 7432 keys 12.3 us so, 11.8 like this).
+__device__ __forceinline__ void fetch(const PromptArgs &a) {
+    asm volatile("" ::"s"(a.q), "s"(a.k), "s"(a.v), "s"(a.out), "s"(a.q_h), "s"(a.q_t), "s"(a.k_h), "s"(a.k_t), "s"(a.v_h), "s"(a.v_t), "s"(a.G),
+                 "s"(a.Hkv), "s"(a.n_seqs), "s"(a.splits), "s"(a.by_g.m), "s"(a.by_hkv.m), "s"(a.by_splits.m), "s"(a.s[0].q_off), "s"(a.s[0].k_off),
+                 "s"(a.s[0].v_off), "s"(a.s[0].q_len), "s"(a.s[0].n_tiles));
+}
+
 // Sequence, row tile and split of the workgroups with number y of a KV head.  The KV head itself is the fastest index of a launch: with 1,
 // 2, 4 or 8 of them every XCD, dealt workgroups round-robin, works on one head's K and V.
 struct Place {
-    int seq, tile, split;
+    int tile, split, q_len, kv_len, row0;
+    int64_t q_off, k_off, v_off, out_off;
 };
+__device__ __forceinline__ int64_t of_lane(int64_t x, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32);
+}
 __device__ __forceinline__ Place place_of(const PromptArgs &a, int y) {
     Place p;
     const int rank = a.by_splits.of(y);
     p.split = y - rank * a.splits;
-    p.seq = 0;
-    p.tile = a.s[0].n_tiles - 1 - rank;
-    if (a.n_seqs > 1) {
-        // one load for all sequences and a vote in place of a chain of loads
-        const int k = __popcll(__ballot(a.rank0[threadIdx.x & 63] <= rank));
-        const int off = rank - a.rank0[k - 1], level = off / k;
-        p.seq = __builtin_amdgcn_readfirstlane(off - level * k);
-        p.tile = __builtin_amdgcn_readfirstlane(a.s[k - 1].n_tiles - 1 - level);
+    if (a.n_seqs == 1) {
+        p.tile = a.s[0].n_tiles - 1 - rank;
+        p.q_len = a.s[0].q_len, p.kv_len = a.s[0].kv_len, p.row0 = a.s[0].row0;
+        p.q_off = a.s[0].q_off, p.k_off = a.s[0].k_off, p.v_off = a.s[0].v_off, p.out_off = a.s[0].out_off;
+    } else {
+        // every lane loads a sequence, all at once, and a vote finds the one, in place of a chain of loads
+        const int i = threadIdx.x & 63;
+        const int rank0 = a.rank0[i], n_tiles = a.s[i].n_tiles, q_len = a.s[i].q_len, kv_len = a.s[i].kv_len, row0 = a.s[i].row0;
+        const int64_t q_off = a.s[i].q_off, k_off = a.s[i].k_off, v_off = a.s[i].v_off, out_off = a.s[i].out_off;
+        const int k = __popcll(__ballot(rank0 <= rank));
+        const int off = rank - __builtin_amdgcn_readlane(rank0, k - 1), level = off / k, seq = __builtin_amdgcn_readfirstlane(off - level * k);
+        p.tile = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(n_tiles, k - 1) - 1 - level);
+        p.q_len = __builtin_amdgcn_readlane(q_len, seq), p.kv_len = __builtin_amdgcn_readlane(kv_len, seq);
+        p.row0 = __builtin_amdgcn_readlane(row0, seq);
+        p.q_off = of_lane(q_off, seq), p.k_off = of_lane(k_off, seq), p.v_off = of_lane(v_off, seq), p.out_off = of_lane(out_off, seq);
     }
     return p;
 }
@@ -357,6 +376,7 @@ __device__ __forceinline__ Place place_of(const PromptArgs &a, int y) {
 // ---------------------------------------------------------------------------------------
 template <typename T, int D, int KW>
 __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
+    fetch(a);
     using R = Row<T, D>;
     static_assert(sizeof(T) == 2, "bf16");
     constexpr int NW = 8, RW = NW / KW, kRows = 32 * RW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
@@ -370,8 +390,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
     const int rw = wave % RW, kw = wave / RW;
     const int y = a.by_hkv.of(blockIdx.x), kvh = blockIdx.x - y * a.Hkv;
     const Place pl = place_of(a, y);
-    const PromptSpan &sp = a.s[pl.seq];
-    const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
+    const int n_rows = pl.q_len * a.G, shift = pl.kv_len - pl.q_len;
     const int row0 = pl.tile * kRows, end_row = min(row0 + kRows, n_rows);
     // keys that every row of the tile sees, and that any does
     const int see_all = max(0, a.by_g.of(row0) + shift + 1), see_any = max(0, a.by_g.of(end_row - 1) + shift + 1);
@@ -390,20 +409,20 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
     const int last = tok + shift;  // last key that the lane's query sees
     uint4 q[NS];
     {
-        const T *qp = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
+        const T *qp = (const T *)a.q + pl.q_off + tok * a.q_t + head * a.q_h;
 #pragma unroll
         for (int sl = 0; sl < NS; ++sl) q[sl] = *reinterpret_cast<const uint4 *>(qp + R::kVec * (2 * sl + h));
     }
 
-    const T *kg = (const T *)a.k + sp.k_off + kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + kvh * a.v_h;
+    const T *kg = (const T *)a.k + pl.k_off + kvh * a.k_h, *vg = (const T *)a.v + pl.v_off + kvh * a.v_h;
     Stage<T, D, 64 * NW, kKeys> stage;
     stage.init(a, threadIdx.x);
     auto load = [&](int b) {
-        if (b < b1) stage.load(a, kg, vg, b * kKeys, sp.kv_len);
+        if (b < b1) stage.load(a, kg, vg, b * kKeys, pl.kv_len);
     };
     auto keep = [&](int b) {
         if (b >= b1) return;
-        if ((b + 1) * kKeys > see_all && stage.clean(sp.kv_len - b * kKeys)) s_bad = 1;
+        if ((b + 1) * kKeys > see_all && stage.clean(pl.kv_len - b * kKeys)) s_bad = 1;
         stage.store(sk(b), sv(b));
     };
     // operands of the logits of the 32 keys whose tile starts at sk_
@@ -562,7 +581,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
                 store4(reinterpret_cast<T *>(rows + n * R::kPieces + ((4 * d + i) ^ (n & (R::kPieces - 1)))) + 4 * h, o);
             }
         wave_sync();
-        T *out = (T *)a.out + sp.out_off + R::kVec * (lane % R::kPieces);
+        T *out = (T *)a.out + pl.out_off + R::kVec * (lane % R::kPieces);
 #pragma unroll
         for (int i = 0; i < R::kPieces / 2; ++i) {
             const int r = lane / R::kPieces + (64 / R::kPieces) * i, m = row0 + 32 * rw + r;
@@ -571,7 +590,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
             if (m < n_rows) *reinterpret_cast<u32x4 *>(out + to * a.out_t + hd * a.out_h) = o;
         }
     } else if (row < n_rows) {
-        const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + sp.row0 + row;
+        const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + pl.row0 + row;
         if (h == 0) a.part_ml[slot] = make_float2(ref, l);
         float *po = a.part_o + slot * D + 4 * h;
 #pragma unroll
@@ -590,6 +609,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
 // ---------------------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
+    fetch(a);
     using R = Row<T, D>;
     constexpr int kRows = 128, ND = D / 32;
     __shared__ u32x4 sk[2][R::kKTile], sv[2][R::kVTile];
@@ -598,18 +618,17 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int y = a.by_hkv.of(blockIdx.x), kvh = blockIdx.x - y * a.Hkv;
     const Place pl = place_of(a, y);
-    const PromptSpan &sp = a.s[pl.seq];
-    const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
+    const int n_rows = pl.q_len * a.G, shift = pl.kv_len - pl.q_len;
     const int row0 = pl.tile * kRows, end_row = min(row0 + kRows, n_rows);
     const int see_all = max(0, a.by_g.of(row0) + shift + 1), see_any = max(0, a.by_g.of(end_row - 1) + shift + 1);
     const int n_blocks = (see_any + 31) / 32;
     const int per_split = (n_blocks + a.splits - 1) / a.splits;
     const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
 
-    const T *kg = (const T *)a.k + sp.k_off + kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + kvh * a.v_h;
+    const T *kg = (const T *)a.k + pl.k_off + kvh * a.k_h, *vg = (const T *)a.v + pl.v_off + kvh * a.v_h;
     Stage<T, D, 256, 32> stage;
     stage.init(a, threadIdx.x);
-    if (b0 < b1) stage.load(a, kg, vg, b0 * 32, sp.kv_len);
+    if (b0 < b1) stage.load(a, kg, vg, b0 * 32, pl.kv_len);
     Attend<T, D> at;
     at.clear();
     const int row = row0 + 32 * wave + n, m_row = min(row, n_rows - 1), tok = a.by_g.of(m_row), head = kvh * a.G + m_row - tok * a.G;
@@ -617,7 +636,7 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
     // last key that a row of the wave sees
     const int wave_last = row0 + 32 * wave < n_rows ? a.by_g.of(min(row0 + 32 * wave + 31, n_rows - 1)) + shift : -1;
     {
-        const T *q = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
+        const T *q = (const T *)a.q + pl.q_off + tok * a.q_t + head * a.q_h;
 #pragma unroll
         for (int sl = 0; sl < R::kSlices; ++sl) at.q[sl] = *reinterpret_cast<const uint4 *>(q + R::kVec * (2 * sl + h));
     }
@@ -626,10 +645,10 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
 #pragma unroll 1
     for (int b = b0; b < b1; ++b) {
         const bool masked = (b + 1) * 32 > see_all;
-        if (masked && stage.clean(sp.kv_len - b * 32)) s_bad = 1;
+        if (masked && stage.clean(pl.kv_len - b * 32)) s_bad = 1;
         stage.store(sk[b & 1], sv[b & 1]);  // (read for block b - 2, which every wave has left before the last barrier)
         lds_barrier();
-        if (b + 1 < b1) stage.load(a, kg, vg, (b + 1) * 32, sp.kv_len);
+        if (b + 1 < b1) stage.load(a, kg, vg, (b + 1) * 32, pl.kv_len);
         if (b * 32 <= wave_last) at.step(sk[b & 1], sv[b & 1], masked, last - b * 32, a.c);
     }
     const float l = at.l + __shfl_xor(at.l, 32, 64);
@@ -637,7 +656,7 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
     if (row >= n_rows) return;
     if (a.splits == 1) {
         const float inv = 1.0f / l;
-        T *o = (T *)a.out + sp.out_off + tok * a.out_t + head * a.out_h + 4 * h;
+        T *o = (T *)a.out + pl.out_off + tok * a.out_t + head * a.out_h + 4 * h;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -648,7 +667,7 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
                 store4(o + 32 * d + 8 * i, x);
             }
     } else {
-        const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + sp.row0 + row;
+        const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + pl.row0 + row;
         if (h == 0) a.part_ml[slot] = make_float2(at.m, l);
         float *po = a.part_o + slot * D + 4 * h;
 #pragma unroll
@@ -666,6 +685,7 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
 // ---------------------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
+    fetch(a);
     using R = Row<T, D>;
     constexpr int NW = 4;
     __shared__ u32x4 tiles[NW][R::kKTile + R::kVTile];
@@ -675,25 +695,24 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int y = a.by_hkv.of(blockIdx.x), kvh = blockIdx.x - y * a.Hkv;
     const Place pl = place_of(a, y);
-    const PromptSpan &sp = a.s[pl.seq];
-    const int n_rows = sp.q_len * a.G, shift = sp.kv_len - sp.q_len;
+    const int n_rows = pl.q_len * a.G, shift = pl.kv_len - pl.q_len;
     const int row0 = pl.tile * 32, end_row = min(row0 + 32, n_rows);
     const int see_all = max(0, a.by_g.of(row0) + shift + 1), see_any = max(0, a.by_g.of(end_row - 1) + shift + 1);
     const int n_blocks = (see_any + 31) / 32;
     const int per_split = (n_blocks + a.splits - 1) / a.splits;
     const int b0 = pl.split * per_split, b1 = min(n_blocks, b0 + per_split);
 
-    const T *kg = (const T *)a.k + sp.k_off + kvh * a.k_h, *vg = (const T *)a.v + sp.v_off + kvh * a.v_h;
+    const T *kg = (const T *)a.k + pl.k_off + kvh * a.k_h, *vg = (const T *)a.v + pl.v_off + kvh * a.v_h;
     Stage<T, D, 64, 32> stage;
     stage.init(a, lane);
     int b = b0 + wave;
-    if (b < b1) stage.load(a, kg, vg, b * 32, sp.kv_len);
+    if (b < b1) stage.load(a, kg, vg, b * 32, pl.kv_len);
     Attend<T, D> at;
     at.clear();
     const int row = min(row0 + n, n_rows - 1), tok = a.by_g.of(row), head = kvh * a.G + row - tok * a.G;
     const int last = tok + shift;
     {
-        const T *q = (const T *)a.q + sp.q_off + tok * a.q_t + head * a.q_h;
+        const T *q = (const T *)a.q + pl.q_off + tok * a.q_t + head * a.q_h;
 #pragma unroll
         for (int sl = 0; sl < R::kSlices; ++sl) at.q[sl] = *reinterpret_cast<const uint4 *>(q + R::kVec * (2 * sl + h));
     }
@@ -703,11 +722,11 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
 #pragma unroll 1
     for (; b < b1; b += NW) {
         const bool masked = (b + 1) * 32 > see_all;
-        if (masked && stage.clean(sp.kv_len - b * 32)) s_bad = 1;
+        if (masked && stage.clean(pl.kv_len - b * 32)) s_bad = 1;
         wave_sync();  // the wave's reads of the tile before are behind it
         stage.store(sk, sv);
         wave_sync();
-        if (b + NW < b1) stage.load(a, kg, vg, (b + NW) * 32, sp.kv_len);
+        if (b + NW < b1) stage.load(a, kg, vg, (b + NW) * 32, pl.kv_len);
         at.step(sk, sv, masked, last - b * 32, a.c);
     }
     // merge of the four waves: every wave brings its sums to the common reference and leaves them in LDS
@@ -755,9 +774,9 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
             const float inv = 1.0f / lt;
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = lt == 0.f ? 0.f : x[j] * inv;
-            store4((T *)a.out + sp.out_off + t * a.out_t + (kvh * a.G + g) * a.out_h + 4 * c4, x);
+            store4((T *)a.out + pl.out_off + t * a.out_t + (kvh * a.G + g) * a.out_h + 4 * c4, x);
         } else {
-            const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + sp.row0 + row0 + r;
+            const int64_t slot = ((int64_t)pl.split * a.Hkv + kvh) * a.n_rows + pl.row0 + row0 + r;
             if (c4 == 0) {
                 float mm = s_m[0][r];
 #pragma unroll
@@ -773,6 +792,8 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
 // results of a long row are all in flight at once.
 template <typename T, int D, int kRound>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int groups) {
+    asm volatile("" ::"s"(a.part_o), "s"(a.part_ml), "s"(a.out), "s"(a.out_t), "s"(a.out_h), "s"(a.Hkv), "s"(a.n_rows), "s"(a.splits), "s"(a.n_seqs),
+                 "s"(a.G), "s"(a.by_g.m), "s"(a.by_rows.m), "s"(a.s[0].out_off));  // as in fetch
     constexpr int kQuads = D / 4;
     __shared__ f32x4 s_x[256];
     __shared__ float2 s_ml[256 / kQuads];
@@ -782,12 +803,15 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
     const bool live = idx < stride;
     const int kvh = a.by_rows.of((int)min(idx, stride - 1)), row = (int)min(idx, stride - 1) - kvh * a.n_rows;
     int seq = 0, seq_row = 0;
+    int64_t out_off = a.s[0].out_off;
     if (a.n_seqs > 1) {  // the last sequence whose first row is not behind `row`: every lane holds one sequence's
         const int first = a.row0[threadIdx.x & 63];
+        const int64_t out_first = a.s[threadIdx.x & 63].out_off;
 #pragma unroll
         for (int step = 32; step > 0; step >>= 1)
             if (__shfl(first, seq + step, 64) <= row) seq += step;
         seq_row = __shfl(first, seq, 64);
+        out_off = __shfl((long long)out_first, seq, 64);
     }
     float m = -INFINITY, l = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -837,11 +861,10 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
         }
     }
     if (!live) return;
-    const PromptSpan &sp = a.s[seq];
     const int r = row - seq_row, t = a.by_g.of(r), q = r - t * a.G;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : x[j] / l;
-    store4((T *)a.out + sp.out_off + t * a.out_t + (kvh * a.G + q) * a.out_h + 4 * c4, x);
+    store4((T *)a.out + out_off + t * a.out_t + (kvh * a.G + q) * a.out_h + 4 * c4, x);
 }
 
 // ---------------------------------------------------------------------------------------
