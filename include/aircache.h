@@ -266,8 +266,8 @@ typedef struct {
 /* For every row x (one token, one head) of q and k:  y = x * weight / sqrt(mean(x^2) + norm_eps)  where a weight is given, and
  * for pair i of y, turning with axis a:  angle = positions[a] * freqs[i],
  *   (y_first, y_second) -> scale * (y_first cos - y_second sin, y_first sin + y_second cos).
- * Rows of v are copied.  Any of q, k, v may be NULL (not all): that tensor is left out.  Computed in fp32 with angles reduced in
- * fp64 (positions of a million turn as exactly as small ones) and rounded once.
+ * Rows of v are copied.  Any of q, k, v may be NULL (not all): that tensor is left out.  Computed in fp32 (a norm's squares too: elements
+ * below 2^60) with angles reduced in fp64 (positions of a million turn as exactly as small ones) and rounded once.
  * positions: device [n_axes][batch][n_tokens]; a row whose position on axis 0 is negative is padding: nothing is written there,
  * whatever lies in its source.  NULL only without pairs.  freqs: device [sum of axis_pairs], radians per position.         */
 air_status air_rope(void *stream, const air_rope_config *cfg, const air_rope_tensor *q, const air_rope_tensor *k,
@@ -310,7 +310,8 @@ size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt
  * scale * q . k_j, with the keys and values of KV head h / (n_q_heads / n_kv_heads).  What lies at keys behind a row's own position, or
  * behind kv_len, counts for nothing, whatever it holds (infinities and NaN included).  A row that sees no key (q_len > kv_len), or
  * only logits of -inf, is zero.  Output rows outside the sequences are left as they are.  Logits, maxima, sums and products are
- * held in fp32; with bf16 the probabilities are rounded to bf16 for the second product.  seqs: host array, n_seqs in 0..AIR_MAX_BATCH.
+ * held in fp32, the products with the values before they are divided by the sum (values below 2^120 / kv_len cannot overflow there);
+ * with bf16 the probabilities are rounded to bf16 for the second product.  seqs: host array, n_seqs in 0..AIR_MAX_BATCH.
  * workspace: 256-byte aligned, free for another call when this one's work has run; may be NULL where no bytes are needed.
  * out must not overlap an input. */
 air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, const void *q,

@@ -411,3 +411,13 @@ def test_two_calls_at_once_and_two_graphs_of_one_workspace():
         for o, w, spans in zip(outs, want, jobs):
             for b, q0, n, _, _ in spans:
                 assert torch.equal(o[b, :, q0:q0 + n], w[b, :, q0:q0 + n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv", [(16384, 1), (16384, 16384), (16383, 3)])
+def test_as_many_heads_as_a_call_takes(dtype, hq, hkv):
+    import paper_2503_23956_amd as A
+
+    spans = [(0, 0, 3, 0, 40), (1, 1, 1, 2, 9), (1, 2, 1, 0, 70)]
+    q, k, v = _tensors(2, 3, 70, hq, hkv, 64, dtype, hkv)
+    _check(q, k, v, spans, _run(A, q, k, v, spans))

@@ -227,3 +227,24 @@ def test_as_many_rows_as_a_call_takes():
     more = torch.empty((1, 1, 1, 64), dtype=torch.bfloat16, device="cuda:0").expand(1, 1, n + 1, 64)
     with pytest.raises(A.AirError):
         A.air_rope(more, q_out=more)
+
+
+@pytest.mark.parametrize("tokens", [1, 70])
+def test_as_many_heads_as_a_call_takes(tokens):
+    """Heads are independent: the same rows whether 16384 heads are one call's or eight calls'."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    q, k, v = (torch.randn((1, 16384, tokens, 64), device="cuda:0").bfloat16() for _ in range(3))
+    pos = torch.arange(tokens, dtype=torch.int32, device="cuda:0").view(1, tokens) + 5
+    kw = dict(positions=pos, freqs=torch.tensor(A.air_rope_frequencies(32, 1e4)[0], device="cuda:0"), axis_pairs=(32,))
+    outs = [torch.zeros_like(x) for x in (q, k, v)]
+    A.air_rope(q, k, v, *outs, **kw)
+    parts = [torch.zeros_like(x) for x in (q, k, v)]
+    for i in range(0, 16384, 2048):
+        A.air_rope(*(x[:, i:i + 2048] for x in (q, k, v)), *(x[:, i:i + 2048] for x in parts), **kw)
+    torch.cuda.synchronize()
+    for a, b in zip(outs, parts):
+        assert torch.equal(a, b)
+    assert torch.equal(outs[2], v)
