@@ -124,7 +124,7 @@ static air_status check_prompt(const char *who, const air_prompt_config *cfg, co
     if ((c.n_q_heads > 1 && c.out_h < c.head_dim) || (most > 1 && c.out_t < c.head_dim))
         return refuse(AIR_ERR_SHAPE, "%s: output rows overlap", who);
     *plan = prompt_plan(c, seqs, n);
-    if (!prompt_grid_ok(c, *plan)) return refuse(AIR_ERR_SHAPE, "%s: too many rows for one call", who);
+    if (plan->splits == 0) return refuse(AIR_ERR_SHAPE, "%s: too many rows for one call", who);
     return AIR_OK;
 }
 

@@ -138,12 +138,11 @@ hipError_t launch_rope(hipStream_t s, const air_rope_config &c, const air_rope_t
 // The shape of a prompt attention call: the row tiles' size, splits over the keys, what the partial results take
 struct PromptPlan {
     bool few;  // tiles of 32 rows
-    int32_t tile_rows, splits;
+    int32_t tile_rows, splits;  // splits 0: more rows than one call takes
     int64_t n_tiles, n_rows;
     size_t ml_bytes, bytes;  // workspace: (maximum, sum) pairs in front, all of it
 };
 PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, int n);
-bool prompt_grid_ok(const air_prompt_config &c, const PromptPlan &p);  // the launches' grids and 32-bit indexes hold the call
 hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const PromptPlan &p, const air_prompt_seq *seqs, int n, const void *q,
                          const void *k, const void *v, void *out, void *workspace);
 const char *thread_error();  // text of the calling thread's last failure in a call without a context; empty: none

@@ -894,13 +894,26 @@ static const TileCost kCosts[4][3] = {
 };
 constexpr int kMostSplits = 64;
 
+// groups of D / 4 lanes that share the splits of a row in the join, and the join's workgroups
+static int join_groups(int splits, int d) {
+    int groups = 1;
+    while (groups < 256 / (d / 4) && groups * 2 <= splits) groups *= 2;
+    return groups;
+}
+static int64_t join_blocks(int64_t rows, int splits, int d) {
+    const int64_t per = 256 / (d / 4) / join_groups(splits, d);
+    return (rows + per - 1) / per;
+}
+// a launch has fewer than 2^32 work items
+static bool launchable(int64_t wgs, int64_t rows, int splits, int d) {
+    return wgs * 512 < (1ll << 32) && (splits == 1 || join_blocks(rows, splits, d) * 256 < (1ll << 32));
+}
+
 PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
     const int64_t G = c.n_q_heads / c.n_kv_heads;
     const bool f32 = c.dtype == AIR_F32;
     PromptPlan best;
     memset(&best, 0, sizeof(best));
-    best.splits = 1;
-    best.tile_rows = 32;
     int64_t longest = 0, n_rows = 0;
     double bytes = 0.0;
     for (int i = 0; i < n; ++i) {
@@ -909,6 +922,8 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
         bytes += 2.0 * seqs[i].kv_len * c.n_kv_heads * c.head_dim * (f32 ? 4 : 2);
         if (seqs[i].kv_len > longest) longest = seqs[i].kv_len;
     }
+    best.n_rows = n_rows;
+    if (n_rows * c.n_kv_heads >= (1 << 26)) return best;  // indexes of 32 bits
     double least = INFINITY;
     for (const TileCost &k : kCosts[(f32 ? 2 : 0) + (c.head_dim == 128 ? 0 : 1)]) {
         if (k.rows == 0) continue;
@@ -923,6 +938,7 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
         const double full = keys * c.n_kv_heads / kCUs / 128.0 * k.full, read = bytes / 5.2e6;
         // 1 to 8 splits, then four to every doubling
         for (int s = 1; s <= kMostSplits && (s == 1 || longest > 64 * s); s += s < 8 ? 1 : (s < 16 ? 2 : (s < 32 ? 4 : 8))) {
+            if (!launchable(tiles * c.n_kv_heads * s, n_rows * c.n_kv_heads, s, c.head_dim)) break;
             const double at_work = fmax(1.0, wgs * s / kCUs);  // workgroups a CU: part of a last, uneven deal is lost
             const double all = full * (1.0 + 0.3 * (ceil(at_work) / at_work - 1.0));
             const double work = fmax(ceil((double)longest / s / k.grain) * k.grain / 128.0 * k.step, all);
@@ -937,18 +953,12 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
         }
     }
     best.few = best.tile_rows == 32;
-    best.n_rows = n_rows;
     if (best.splits > 1) {
         const size_t slots = (size_t)n_rows * c.n_kv_heads * best.splits;
         best.ml_bytes = (slots * sizeof(float2) + 255) / 256 * 256;
         best.bytes = best.ml_bytes + slots * c.head_dim * sizeof(float);
     }
     return best;
-}
-
-bool prompt_grid_ok(const air_prompt_config &c, const PromptPlan &p) {
-    const int64_t rows = p.n_rows * c.n_kv_heads, wgs = p.n_tiles * c.n_kv_heads * p.splits;
-    return rows < (1 << 26) && wgs * 512 < (1ll << 32) && (p.splits == 1 || rows * 256 < (1ll << 32));
 }
 
 template <typename T, int D>
@@ -963,11 +973,8 @@ static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &
     }
     if (p.few) hipLaunchKernelGGL((prompt_few_kernel<T, D>), grid, dim3(256), 0, s, a);
     if (p.splits > 1) {
-        constexpr int kMost = 256 / (D / 4);
-        int groups = 1;
-        while (groups < kMost && groups * 2 <= p.splits) groups *= 2;
-        const int64_t per = kMost / groups, rows = p.n_rows * a.Hkv;
-        const dim3 join((unsigned)((rows + per - 1) / per));
+        const int groups = join_groups(p.splits, D);
+        const dim3 join((unsigned)join_blocks(p.n_rows * a.Hkv, p.splits, D));
         if (p.splits <= groups) hipLaunchKernelGGL((prompt_join_kernel<T, D, 1>), join, dim3(256), 0, s, a, groups);
         else if (p.splits <= 2 * groups) hipLaunchKernelGGL((prompt_join_kernel<T, D, 2>), join, dim3(256), 0, s, a, groups);
         else hipLaunchKernelGGL((prompt_join_kernel<T, D, 8>), join, dim3(256), 0, s, a, groups);

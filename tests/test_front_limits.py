@@ -1,0 +1,73 @@
+"""What the header of air_rope and air_prompt_attn allows is accepted, and what it does not is refused for the reason that it gives.  Host only:
+nothing here reaches a GPU."""
+import ctypes as C
+import random
+
+import pytest
+
+import paper_2503_23956_amd as A
+from test_front_args import SHAPE, _attn, _lib
+
+
+def _config(dtype, d, hq, hkv, **kw):
+    """Token-major tensors."""
+    return dict(dict(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, dtype=A.AIR_F32 if dtype == "f32" else A.AIR_BF16, scale=0.0,
+                     q_h=d, q_t=hq * d, k_h=d, k_t=hkv * d, v_h=d, v_t=hkv * d, out_h=d, out_t=hq * d), **kw)
+
+
+def _workspace(cfg, seqs):
+    """(bytes, text of the refusal or None) of air_prompt_workspace_bytes, which checks what air_prompt_attn checks but the pointers."""
+    arr = (A.air_prompt_seq * max(1, len(seqs)))(*(A.air_prompt_seq(*s) for s in seqs))
+    lib = _lib()
+    assert lib.air_prompt_workspace_bytes(None, None, 0) == 0
+    before = lib.air_last_error(None)
+    nbytes = lib.air_prompt_workspace_bytes(C.byref(A.air_prompt_config(**cfg)), arr, len(seqs))
+    text = lib.air_last_error(None)
+    return nbytes, None if text == before else text.decode()
+
+
+def _prompts(cfg, lens):
+    """Sequences one behind the other."""
+    out, q0, k0 = [], 0, 0
+    for n, m in lens:
+        out.append((q0 * cfg["q_t"], k0 * cfg["k_t"], k0 * cfg["v_t"], q0 * cfg["out_t"], n, m))
+        q0, k0 = q0 + n, k0 + m
+    return out
+
+
+def _log_int(rng, lo, hi):
+    return int(round(2.0 ** rng.uniform(lo, hi)))
+
+
+@pytest.mark.parametrize("dtype,d,hq,hkv,lens", [
+    ("f32", 128, 40, 5, [(463172, 924067)]), ("f32", 64, 16, 2, [(1051463, 1051463)]), ("bf16", 128, 64, 8, [((1 << 20) - 1, 1 << 30)]),
+    ("bf16", 64, 1, 1, [((1 << 26) - 1, 1 << 30)]), ("f32", 128, 16384, 16384, [(63, 1 << 20)] * 64), ("bf16", 64, 16384, 1, [(4095, 4095)]),
+])
+def test_calls_at_the_limits_are_accepted(dtype, d, hq, hkv, lens):
+    cfg = _config(dtype, d, hq, hkv)
+    assert _workspace(cfg, _prompts(cfg, lens))[1] is None
+
+
+def test_no_call_inside_the_limits_is_refused():
+    rng = random.Random(3)
+    for _ in range(3000):
+        hkv = rng.choice([1, 2, 4, 5, 8, 16, 128, 16384])
+        hq = min(16384 // hkv, rng.choice([1, 2, 5, 7, 8, 16, 64])) * hkv
+        most = ((1 << 26) - 1) // hq
+        n_seqs = rng.choice([1, 1, 2, 7, 33, 64])
+        lens = [(min(_log_int(rng, 0, 26), most // n_seqs), _log_int(rng, 0, 30)) for _ in range(n_seqs)]
+        cfg = _config(rng.choice(["bf16", "f32"]), rng.choice([64, 128]), hq, hkv)
+        if cfg["k_t"] < 1 << 24:
+            assert _workspace(cfg, _prompts(cfg, lens))[1] is None, (cfg, lens)
+
+
+def test_more_rows_than_a_call_takes():
+    for dtype, d, hq, hkv, lens in (("bf16", 64, 2, 1, [((1 << 26) - 1, 100)]), ("bf16", 64, 1, 1, [(1 << 26, 100)]), ("f32", 128, 16384, 1, [(1, 1)] * 64),
+                                    ("f32", 128, 28, 4, [(1 << 21, 1 << 21)] * 2), ("bf16", 128, 16384, 16384, [((1 << 31) - 1, 1)] * 64)):
+        cfg = _config(dtype, d, hq, hkv)
+        rows = sum(n for n, _ in lens) * hq
+        _, text = _workspace(cfg, _prompts(cfg, lens))
+        assert (text is not None and "too many rows" in text) == (rows >= 1 << 26), (text, rows)
+    # with out rows of their own, so that the number of rows is what is refused
+    status, _ = _attn(seqs=((0, 0, 0, 0, 1 << 24, 1),))
+    assert status == SHAPE and b"too many rows" in _lib().air_last_error(None)
