@@ -893,6 +893,13 @@ static const TileCost kCosts[4][3] = {
     {{32, 512, 128, 5.6, 4.6, 2.9, 2.55}, {128, 768, 32, 3.8, 0.0, 11.9, 8.4}, {0}},                                    // fp32, heads of 64
 };
 constexpr int kMostSplits = 64;
+// Splits have to be worth their partial results: by 2 % of the modelled time, more than the model is off on average, and in no more than
+// 256 MiB.  Without either bound, fp32 prompts of 97499 tokens over 258675 keys, 64 / 8 heads, took 6.5 GB for a modelled 0.004 %; with both, of 6000
+// calls of 1 to 10^6 tokens 103 are chosen otherwise, the worst of them 2.9 % slower in the model (a bound of 128 MiB: 5.5 %, of 64 MiB: 38 %).
+// Every plan can be launched: without splits there are fewer than 2^21 + 2^20 workgroups of 512 (2^26 rows in tiles of 32, and 64 sequences
+// of 16384 heads with a tile that is not whole), with them and in the join no more than the 2^19 slots that 256 MiB hold.
+constexpr double kSplitGain = 0.02;
+constexpr size_t kMostPartBytes = 256u << 20;
 
 // groups of D / 4 lanes that share the splits of a row in the join, and the join's workgroups
 static int join_groups(int splits, int d) {
@@ -904,9 +911,10 @@ static int64_t join_blocks(int64_t rows, int splits, int d) {
     const int64_t per = 256 / (d / 4) / join_groups(splits, d);
     return (rows + per - 1) / per;
 }
-// a launch has fewer than 2^32 work items
-static bool launchable(int64_t wgs, int64_t rows, int splits, int d) {
-    return wgs * 512 < (1ll << 32) && (splits == 1 || join_blocks(rows, splits, d) * 256 < (1ll << 32));
+// partial results of a call: (maximum, sum) pairs in front, sums behind them
+static size_t ml_bytes(int64_t rows, int splits) { return ((size_t)rows * splits * sizeof(float2) + 255) / 256 * 256; }
+static size_t part_bytes(int64_t rows, int splits, int d) {
+    return splits == 1 ? 0 : ml_bytes(rows, splits) + (size_t)rows * splits * d * sizeof(float);
 }
 
 PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
@@ -923,8 +931,14 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
         if (seqs[i].kv_len > longest) longest = seqs[i].kv_len;
     }
     best.n_rows = n_rows;
-    if (n_rows * c.n_kv_heads >= (1 << 26)) return best;  // indexes of 32 bits
-    double least = INFINITY;
+    const int64_t all_rows = n_rows * c.n_kv_heads;
+    if (all_rows >= (1 << 26)) return best;  // indexes of 32 bits
+    // the best choice without splits and with them: rows of a tile, tiles, splits, us
+    struct Choice {
+        int rows, splits;
+        int64_t tiles;
+        double us;
+    } whole = {0, 0, 0, INFINITY}, split = whole;
     for (const TileCost &k : kCosts[(f32 ? 2 : 0) + (c.head_dim == 128 ? 0 : 1)]) {
         if (k.rows == 0) continue;
         int64_t tiles = 0;
@@ -938,26 +952,23 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
         const double full = keys * c.n_kv_heads / kCUs / 128.0 * k.full, read = bytes / 5.2e6;
         // 1 to 8 splits, then four to every doubling
         for (int s = 1; s <= kMostSplits && (s == 1 || longest > 64 * s); s += s < 8 ? 1 : (s < 16 ? 2 : (s < 32 ? 4 : 8))) {
-            if (!launchable(tiles * c.n_kv_heads * s, n_rows * c.n_kv_heads, s, c.head_dim)) break;
+            if (part_bytes(all_rows, s, c.head_dim) > kMostPartBytes) break;
             const double at_work = fmax(1.0, wgs * s / kCUs);  // workgroups a CU: part of a last, uneven deal is lost
             const double all = full * (1.0 + 0.3 * (ceil(at_work) / at_work - 1.0));
             const double work = fmax(ceil((double)longest / s / k.grain) * k.grain / 128.0 * k.step, all);
             double us = k.start + k.round * (ceil(fmax(1.0, wgs * s / k.at_once)) - 1.0) + sqrt(work * work + read * read);
-            if (s > 1) us += 2.9 + 2.1 * n_rows * c.n_kv_heads * s * (c.head_dim * 4 + 8) / 4e6;
-            if (us < least) {
-                least = us;
-                best.tile_rows = k.rows;
-                best.n_tiles = tiles;
-                best.splits = s;
-            }
+            if (s > 1) us += 2.9 + 2.1 * all_rows * s * (c.head_dim * 4 + 8) / 4e6;
+            Choice &to = s == 1 ? whole : split;
+            if (us < to.us) to = Choice{k.rows, s, tiles, us};
         }
     }
-    best.few = best.tile_rows == 32;
-    if (best.splits > 1) {
-        const size_t slots = (size_t)n_rows * c.n_kv_heads * best.splits;
-        best.ml_bytes = (slots * sizeof(float2) + 255) / 256 * 256;
-        best.bytes = best.ml_bytes + slots * c.head_dim * sizeof(float);
-    }
+    const Choice &taken = split.us < (1.0 - kSplitGain) * whole.us ? split : whole;
+    best.tile_rows = taken.rows;
+    best.few = taken.rows == 32;
+    best.n_tiles = taken.tiles;
+    best.splits = taken.splits;
+    best.ml_bytes = taken.splits == 1 ? 0 : ml_bytes(all_rows, taken.splits);
+    best.bytes = part_bytes(all_rows, taken.splits, c.head_dim);
     return best;
 }
 

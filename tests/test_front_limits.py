@@ -71,3 +71,20 @@ def test_more_rows_than_a_call_takes():
     # with out rows of their own, so that the number of rows is what is refused
     status, _ = _attn(seqs=((0, 0, 0, 0, 1 << 24, 1),))
     assert status == SHAPE and b"too many rows" in _lib().air_last_error(None)
+
+
+def test_splits_are_worth_their_workspace():
+    """Long prompts take none, and no call takes more than 256 MiB; few rows over many keys, which need splits, still have them."""
+    for dtype, d, hq, hkv, n, m in (("bf16", 128, 64, 8, 21839, 249226), ("f32", 128, 64, 8, 97499, 258675), ("f32", 128, 28, 4, 131295, 250773)):
+        cfg = _config(dtype, d, hq, hkv)
+        assert _workspace(cfg, _prompts(cfg, [(n, m)])) == (0, None)
+    rng = random.Random(4)
+    for _ in range(3000):
+        hkv = rng.choice([1, 2, 3, 4, 8])
+        cfg = _config(rng.choice(["bf16", "f32"]), rng.choice([64, 128]), hkv * rng.choice([1, 2, 5, 7, 8, 16]), hkv)
+        lens = [(_log_int(rng, 0, 18), _log_int(rng, 0, 22)) for _ in range(rng.choice([1, 1, 2, 8, 33]))]
+        assert _workspace(cfg, _prompts(cfg, lens))[0] <= 256 << 20, (cfg, lens)
+    for dtype, d, hq, hkv, lens in (("bf16", 128, 28, 4, [(1, 7432)]), ("bf16", 64, 14, 2, [(1, 7432), (1, 33), (1, 4000)]), ("f32", 64, 4, 2, [(656, 656)]),
+                                    ("bf16", 128, 64, 8, [(512, 16910)]), ("bf16", 128, 64, 8, [(1, 1 << 20)] * 8)):
+        cfg = _config(dtype, d, hq, hkv)
+        assert _workspace(cfg, _prompts(cfg, lens))[0] > 0
