@@ -255,7 +255,8 @@ typedef struct {
 } air_rope_config;
 
 /* One tensor of air_rope: element strides of batch, head and token (the head_dim axis is contiguous), multiples of 16 bytes.
- * dst == src with the same strides works in place; source and destination must not overlap in any other way.               */
+ * dst == src with the same strides works in place; source and destination must not overlap in any other way, nor one
+ * tensor's destination another's.  A destination whose own rows overlap, whatever the strides, is refused (AIR_ERR_SHAPE).    */
 typedef struct {
     const void *src;
     void *dst;
@@ -313,7 +314,7 @@ size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt
  * held in fp32, the products with the values before they are divided by the sum (values below 2^120 / kv_len cannot overflow there);
  * with bf16 the probabilities are rounded to bf16 for the second product.  seqs: host array, n_seqs in 0..AIR_MAX_BATCH.
  * workspace: 256-byte aligned, free for another call when this one's work has run; may be NULL where no bytes are needed.
- * out must not overlap an input. */
+ * out must not overlap an input.  Output rows that overlap, of one sequence or of two, are refused (AIR_ERR_SHAPE). */
 air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, const void *q,
                            const void *k, const void *v, void *out, void *workspace, size_t workspace_bytes);
 

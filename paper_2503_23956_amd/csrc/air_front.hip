@@ -3,6 +3,8 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <algorithm>
+
 #include "air_internal.h"
 
 namespace air {
@@ -27,6 +29,119 @@ static const char *geometry(int hq, int hkv, int d, int dtype) {
     if (d != 64 && d != 128) return "head_dim must be 64 or 128";
     if (hkv < 1 || hq < hkv || hq % hkv || hq > kMaxHeads) return "query heads must be a multiple of KV heads, at most 16384";
     return nullptr;
+}
+
+// ---- do rows that a call writes overlap?  Rows of `d` elements start at sum_i x_i stride_i; two of them overlap if their starts are less than d
+// apart.  Exact, for any strides, by Euclid's algorithm: no loop over rows.
+typedef __int128 wide;
+
+static wide floor_div(wide a, wide b) { return a / b - (a % b != 0 && (a < 0) != (b < 0)); }
+
+// the smallest k >= 0 with low <= (a k mod m) <= high, for 0 <= low <= high < m; -1: none
+static wide first_in(wide a, wide m, wide low, wide high) {
+    if (low == 0) return 0;
+    a %= m;
+    if (a == 0) return -1;
+    wide k = (low + a - 1) / a;
+    if (a * k <= high) return k;
+    // no multiple of a in between: the j-th turn around m has one when (m j mod a) lies between -high and -low (mod a)
+    const wide j = first_in(m % a, a, (a - high % a) % a, (a - low % a) % a);
+    return j < 0 ? -1 : (low + m * j + a - 1) / a;
+}
+
+struct Axis {
+    int64_t stride, low, high;  // steps from low to high along it
+};
+// is |c + x a.stride + y b.stride| < d for some steps x, y?  An axis with steps has a stride of at least d.
+static bool rows_meet(wide c, Axis a, Axis b, int64_t d) {
+    if (a.low > a.high || b.low > b.high) return false;
+    if (a.stride > b.stride) std::swap(a, b);
+    if (b.low == b.high) {  // (then y is known; the axis with steps takes its place)
+        c += (wide)b.low * b.stride;
+        if (a.low == a.high) {
+            c += (wide)a.low * a.stride;
+            return c > -d && c < d;
+        }
+        std::swap(a, b);
+        a = Axis{0, 0, 0};
+    }
+    const wide m = b.stride;
+    for (int side = 0; side < 2; ++side) {  // starts 0 .. d - 1 apart, 1 .. d - 1 the other way
+        const wide from = side ? 1 - d : 0, length = side ? d - 2 : d - 1;
+        // w = c - from + x a.stride has to lie within `length` above a multiple -y m of m
+        const wide w0 = c - from, w_low = -(wide)b.high * m, w_high = -(wide)b.low * m + m - 1;
+        wide x0 = a.low, x1 = a.high;
+        if (a.stride == 0) {
+            if (w0 < w_low || w0 > w_high) continue;
+            x1 = x0;
+        } else {
+            x0 = std::max(x0, -floor_div(w0 - w_low, a.stride));
+            x1 = std::min(x1, floor_div(w_high - w0, a.stride));
+            if (x0 > x1) continue;
+        }
+        const wide at = w0 + x0 * a.stride, rest = at - floor_div(at, m) * m;
+        if (rest <= length) return true;
+        const wide k = first_in(a.stride, m, m - rest, m - rest + length);
+        if (k >= 0 && x0 + k <= x1) return true;
+    }
+    return false;
+}
+
+// rows of up to three axes (extent, stride): does one of them overlap another?
+static bool rows_overlap(int64_t (&n)[3], int64_t (&stride)[3], int64_t d) {
+    int order[3] = {0, 1, 2};
+    if (n[0] == 0 || n[1] == 0 || n[2] == 0) return false;
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] <= 1) stride[i] = 0;
+        else if (stride[i] < d) return true;
+    }
+    // every axis outside all that lies within its step, as tensors have it
+    std::sort(order, order + 3, [&](int i, int j) { return stride[i] < stride[j]; });
+    wide span = d;
+    bool nested = true;
+    for (int i : order) {
+        if (n[i] <= 1) continue;
+        nested = nested && stride[i] >= span;
+        span += (wide)(n[i] - 1) * stride[i];
+    }
+    if (nested) return false;
+    std::sort(order, order + 3, [&](int i, int j) { return n[i] < n[j]; });
+    const int o = order[0], a = order[1], b = order[2];
+    if (rows_meet(0, Axis{stride[a], 1, n[a] - 1}, Axis{stride[b], 1 - n[b], n[b] - 1}, d)) return true;
+    for (int64_t x = 1; x < n[o]; ++x)  // (the shortest axis: at most 13003 steps in 2^27 x 2^14 rows)
+        if (rows_meet((wide)x * stride[o], Axis{stride[a], 1 - n[a], n[a] - 1}, Axis{stride[b], 1 - n[b], n[b] - 1}, d)) return true;
+    return false;
+}
+
+// do two sequences of a prompt attention write the same elements?
+static bool sequences_overlap(const air_prompt_config &c, const air_prompt_seq *seqs, int n) {
+    // what a sequence's rows span, in all and of one head, and (heads outside tokens, sequences packed along the tokens) where they start
+    // inside a head's stride
+    int64_t low[AIR_MAX_BATCH], span[AIR_MAX_BATCH], run[AIR_MAX_BATCH], start[AIR_MAX_BATCH], len[AIR_MAX_BATCH];
+    const int64_t step = c.n_q_heads > 1 ? c.out_h : 0;
+    const auto bounded = [](wide x) { return (int64_t)std::min(x, (wide)INT64_MAX); };
+    int m = 0;
+    for (int i = 0; i < n; ++i) {
+        const air_prompt_seq &s = seqs[i];
+        if (s.q_len == 0) continue;
+        const wide tokens = (wide)(s.q_len - 1) * c.out_t + c.head_dim;
+        low[m] = s.out_off;
+        span[m] = bounded(tokens + (wide)(c.n_q_heads - 1) * c.out_h);
+        run[m] = bounded(tokens);
+        start[m] = step > 0 ? s.out_off % step : 0;
+        len[m++] = s.q_len;
+    }
+    for (int i = 0; i < m; ++i)
+        for (int j = 0; j < i; ++j) {
+            if (low[j] - low[i] >= span[i] || low[i] - low[j] >= span[j]) continue;
+            if (step > 0) {
+                const int64_t x = start[j] - start[i] + (start[j] < start[i] ? step : 0);  // from i's rows on to j's, within a step
+                if (x >= run[i] && run[j] <= step - x) continue;
+            }
+            if (rows_meet((wide)low[j] - low[i], Axis{c.out_h, 1 - c.n_q_heads, c.n_q_heads - 1}, Axis{c.out_t, 1 - len[i], len[j] - 1}, c.head_dim))
+                return true;
+        }
+    return false;
 }
 
 }  // namespace air
@@ -69,8 +184,8 @@ air_status air_rope(void *stream, const air_rope_config *cfg, const air_rope_ten
         const int64_t st[6] = {x.src_b, x.src_h, x.src_t, x.dst_b, x.dst_h, x.dst_t};
         for (int64_t s : st)
             if (s < 0 || s % vec) return refuse(AIR_ERR_SHAPE, "air_rope: strides must be non-negative multiples of 16 bytes");
-        if ((c.batch > 1 && x.dst_b < c.head_dim) || (heads > 1 && x.dst_h < c.head_dim) || (c.n_tokens > 1 && x.dst_t < c.head_dim))
-            return refuse(AIR_ERR_SHAPE, "air_rope: rows of a destination overlap");
+        int64_t n[3] = {c.batch, heads, c.n_tokens}, step[3] = {x.dst_b, x.dst_h, x.dst_t};
+        if (rows_overlap(n, step, c.head_dim)) return refuse(AIR_ERR_SHAPE, "air_rope: rows of a destination overlap");
         if (work && x.src == x.dst && ((c.batch > 1 && x.src_b != x.dst_b) || (heads > 1 && x.src_h != x.dst_h) || (c.n_tokens > 1 && x.src_t != x.dst_t)))
             return refuse(AIR_ERR_SHAPE, "air_rope: in place needs the same strides on both sides");
     }
@@ -121,8 +236,9 @@ static air_status check_prompt(const char *who, const air_prompt_config *cfg, co
             if (o < 0 || o % vec) return refuse(AIR_ERR_SHAPE, "%s: offsets must be non-negative multiples of 16 bytes", who);
         if (s.q_len > most) most = s.q_len;
     }
-    if ((c.n_q_heads > 1 && c.out_h < c.head_dim) || (most > 1 && c.out_t < c.head_dim))
-        return refuse(AIR_ERR_SHAPE, "%s: output rows overlap", who);
+    int64_t extent[3] = {1, c.n_q_heads, most}, step[3] = {0, c.out_h, c.out_t};
+    if (rows_overlap(extent, step, c.head_dim)) return refuse(AIR_ERR_SHAPE, "%s: output rows overlap", who);
+    if (sequences_overlap(c, seqs, n)) return refuse(AIR_ERR_SHAPE, "%s: output rows of two sequences overlap", who);
     *plan = prompt_plan(c, seqs, n);
     if (plan->splits == 0) return refuse(AIR_ERR_SHAPE, "%s: too many rows for one call", who);
     return AIR_OK;

@@ -2,10 +2,13 @@
 nothing here reaches a GPU."""
 import ctypes as C
 import random
+import time
 
 import pytest
+import torch
 
 import paper_2503_23956_amd as A
+from paper_2503_23956_amd import binding
 from test_front_args import SHAPE, _attn, _lib
 
 
@@ -88,3 +91,76 @@ def test_splits_are_worth_their_workspace():
                                     ("bf16", 128, 64, 8, [(512, 16910)]), ("bf16", 128, 64, 8, [(1, 1 << 20)] * 8)):
         cfg = _config(dtype, d, hq, hkv)
         assert _workspace(cfg, _prompts(cfg, lens))[0] > 0
+
+
+def _rows_overlap(rows, d):
+    rows = sorted(rows)
+    return any(b - a < d for a, b in zip(rows, rows[1:]))
+
+
+def test_output_rows_that_overlap_are_refused():
+    cfg = _config("bf16", 128, 4, 2)
+    assert "output rows overlap" in _workspace(dict(cfg, out_h=128, out_t=128), [(0, 0, 0, 0, 3, 3)])[1]  # head 1 of a token is head 0 of the next
+    same = [(0, 0, 0, 0, 3, 3)] * 2  # an output that is expanded over the batch
+    assert "two sequences" in _workspace(cfg, same)[1]
+    assert "two sequences" in _workspace(cfg, [(0, 0, 0, 0, 3, 3), (0, 0, 0, 2 * 512, 3, 3)])[1]
+    assert _workspace(cfg, [(0, 0, 0, 0, 3, 3), (0, 0, 0, 3 * 512, 3, 3)])[1] is None
+    assert _workspace(cfg, [(0, 0, 0, 0, 0, 3), (0, 0, 0, 0, 3, 3)])[1] is None  # no queries, no rows
+    assert "output rows overlap" in _workspace(dict(cfg, out_h=2 ** 61, out_t=2 ** 61), [(0, 0, 0, 0, 3, 3)])[1]
+    assert _workspace(dict(cfg, out_h=2 ** 62, out_t=2 ** 61), [(2 ** 62, 0, 0, 2 ** 62, 1, 3)])[1] is None
+
+
+def test_output_rows_of_any_layout():
+    """Against the rows themselves: heads inside tokens, tokens inside heads, strides that are no multiples of each other."""
+    rng = random.Random(5)
+    seen = [0, 0]
+    for _ in range(6000):
+        d = rng.choice([64, 128])
+        heads, n_seqs = rng.choice([1, 2, 3, 5, 8]), rng.choice([1, 1, 2, 3])
+        unit = 8 * rng.choice([1, 1, 2, 4, 8])
+        out_h, out_t = (rng.choice([unit * rng.randint(1, 900 // unit * 2), d * rng.randint(1, 9)]) for _ in range(2))
+        seqs = [(0, 0, 0, unit * rng.randint(0, rng.choice([10, 4000 // unit])), rng.choice([0, 1, 2, 3, 7, 12]), 5) for _ in range(n_seqs)]
+        rows = [o + h * out_h + t * out_t for _, _, _, o, n, _ in seqs for h in range(heads) for t in range(n)]
+        text = _workspace(_config("bf16", d, heads, 1, out_h=out_h, out_t=out_t), seqs)[1]
+        want = _rows_overlap(rows, d)
+        assert (text is not None and "overlap" in text) == want, (d, heads, out_h, out_t, seqs, text)
+        seen[want] += 1
+    assert min(seen) > 1000
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="made-up pointers: what is accepted would run")
+def test_rotated_rows_of_any_layout():
+    rng = random.Random(6)
+    seen = [0, 0]
+    for i in range(4000):
+        d = rng.choice([64, 128])
+        n = [rng.choice([1, 2, 3, 5, 9]) for _ in range(3)]
+        unit = 8 * rng.choice([1, 1, 2, 8])
+        s = [rng.choice([unit * rng.randint(1, 2400 // unit), d * rng.randint(1, 30)]) for _ in range(3)]
+        if i % 4 == 0:  # nested in some order
+            at = d
+            for j in rng.sample(range(3), 3):
+                s[j] = at + 8 * rng.choice([0, 0, 1, 5])
+                at = s[j] * n[j]
+        rows = [a * s[0] + b * s[1] + c * s[2] for a in range(n[0]) for b in range(n[1]) for c in range(n[2])]
+        cfg = A.air_rope_config(n[1], n[1], d, A.AIR_BF16, n[0], n[2], 0, 1, (C.c_int32 * 3)(0, 0, 0), 1e-6, 1.0)
+        t = A.air_rope_tensor(4096, 8192, None, 0, 0, 0, *s)
+        status = _lib().air_rope(None, C.byref(cfg), None, C.byref(t), None, None, None)
+        want = _rows_overlap(rows, d)
+        assert status == (SHAPE if want else binding.AIR_ERR_HIP), (d, n, s, want)  # (no GPU here: what is accepted stops at the launch)
+        seen[want] += 1
+    assert min(seen) > 800
+
+
+def test_overlap_in_large_calls_takes_no_time():
+    t = A.air_rope_tensor(4096, 8192, None, 0, 0, 0, 11616 * 64 + 8, 11584 * 64, 11600 * 64)
+    cfg = A.air_rope_config(11585, 11585, 64, A.AIR_BF16, 11585, 11585, 0, 1, (C.c_int32 * 3)(0, 0, 0), 1e-6, 1.0)
+    start = time.perf_counter()
+    assert _lib().air_rope(None, C.byref(cfg), None, C.byref(t), None, None, None) == SHAPE
+    assert time.perf_counter() - start < 0.5
+    cfg = _config("bf16", 128, 28, 4, out_h=128 * 64, out_t=128)  # 64 decoded tokens, head-major
+    seqs = [(0, 0, 0, 128 * i, 1, 500) for i in range(64)]
+    start = time.perf_counter()
+    for _ in range(100):
+        assert _workspace(cfg, seqs)[1] is None
+    assert time.perf_counter() - start < 0.5
