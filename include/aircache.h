@@ -290,7 +290,7 @@ air_status air_rope_frequencies(int32_t n_pairs, double theta, int32_t scaling, 
 
 typedef struct {
     int32_t n_q_heads, n_kv_heads, head_dim, dtype; /* head_dim 64 or 128; air_dtype of q, k, v and out                     */
-    float scale;                                    /* of the logits, > 0; 0: 1 / sqrt(head_dim)                           */
+    float scale;                                    /* of the logits, > 0, at most 2^127; 0: 1 / sqrt(head_dim)            */
     int64_t q_h, q_t, k_h, k_t, v_h, v_t, out_h, out_t; /* element strides of head and token, multiples of 16 bytes; k_t and
                                                            v_t below 2^24                                              */
 } air_prompt_config;

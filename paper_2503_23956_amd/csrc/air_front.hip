@@ -221,7 +221,7 @@ static air_status check_prompt(const char *who, const air_prompt_config *cfg, co
     const air_prompt_config &c = *cfg;
     if (const char *bad = geometry(c.n_q_heads, c.n_kv_heads, c.head_dim, c.dtype)) return refuse(AIR_ERR_SHAPE, "%s: %s", who, bad);
     if (n < 0 || n > AIR_MAX_BATCH) return refuse(AIR_ERR_SHAPE, "%s: n_seqs must be in 0..%d", who, AIR_MAX_BATCH);
-    if (!(c.scale >= 0.f) || !isfinite(c.scale)) return refuse(AIR_ERR_INVALID_ARG, "%s: scale must be positive (or 0) and finite", who);
+    if (!(c.scale >= 0.f) || !isfinite(prompt_factor(c))) return refuse(AIR_ERR_INVALID_ARG, "%s: scale must be positive (or 0), at most 2^127", who);
     const int64_t vec = c.dtype == AIR_BF16 ? 8 : 4;
     const int64_t st[8] = {c.q_h, c.q_t, c.k_h, c.k_t, c.v_h, c.v_t, c.out_h, c.out_t};
     for (int64_t s : st)

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -142,6 +143,10 @@ struct PromptPlan {
     int64_t n_tiles, n_rows;
     size_t ml_bytes, bytes;  // workspace: (maximum, sum) pairs in front, all of it
 };
+// factor of the logits in the base-2 domain
+inline float prompt_factor(const air_prompt_config &c) {
+    return (float)((c.scale > 0.f ? (double)c.scale : 1.0 / sqrt((double)c.head_dim)) * 1.4426950408889634);
+}
 PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, int n);
 hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const PromptPlan &p, const air_prompt_seq *seqs, int n, const void *q,
                          const void *k, const void *v, void *out, void *workspace);

@@ -1017,7 +1017,7 @@ hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const Prompt
     a.by_hkv = div_by(a.Hkv);
     a.by_splits = div_by(p.splits);
     a.by_rows = div_by((int)p.n_rows);
-    a.c = (float)((c.scale > 0.f ? (double)c.scale : 1.0 / sqrt((double)c.head_dim)) * 1.4426950408889634);
+    a.c = prompt_factor(c);
     a.splits = p.splits;
     a.n_tiles = (int)p.n_tiles;
     a.n_rows = (int)p.n_rows;

@@ -164,3 +164,9 @@ def test_overlap_in_large_calls_takes_no_time():
     for _ in range(100):
         assert _workspace(cfg, seqs)[1] is None
     assert time.perf_counter() - start < 0.5
+
+
+def test_scales_whose_base_2_factor_overflows_are_refused():
+    for scale, text in ((2.0 ** 127, None), (2.4e38, "scale must be"), (3.4e38, "scale must be"), (float("inf"), "scale must be"), (1e-45, None)):
+        got = _workspace(_config("bf16", 64, 4, 2, scale=scale), [(0, 0, 0, 0, 1, 9)])[1]
+        assert got is None if text is None else text in got, (scale, got)
