@@ -358,9 +358,9 @@ def _strides4(t):
 
 class PreparedCall:
     """Marshalled arguments of one air_rope / air_prompt_attn call plus the tensors they point to; may be called any number of
-    times (the tensors' contents may change between calls)."""
+    times (the tensors' contents may change between calls).  workspace_bytes: what an attention call needs, None for a rotation."""
 
-    def __init__(self, fn, args, device, keepalive, workspace_bytes=0):
+    def __init__(self, fn, args, device, keepalive, workspace_bytes=None):
         import torch
 
         self.torch, self.fn, self.args, self.device, self.workspace_bytes, self._keepalive = torch, fn, args, device, workspace_bytes, keepalive
@@ -369,14 +369,30 @@ class PreparedCall:
         # the current stream's handle without a stream object around it (0.1 us in place of 3), where torch offers it
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
-    def __call__(self, stream=None, *more):
-        """Enqueues the call with the tensors' device current; stream: a raw HIP stream handle, default torch's current one there."""
+    def __call__(self, stream=None, workspace=None):
+        """Enqueues the call with the tensors' device current; stream: a raw HIP stream handle, default torch's current one there.
+        workspace (attention): a contiguous tensor of at least workspace_bytes on the tensors' device; default: one allocated for the call on
+        torch's current stream, which is then the only stream the call may go to."""
+        more = ()
+        if workspace is not None:
+            if self.workspace_bytes is None:
+                _refuse("air_rope: takes no workspace")
+            if workspace.device != self.device or not workspace.is_contiguous():
+                _refuse("air_prompt_attn: the workspace must be contiguous, on the tensors' device")
+            more = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
         if not self.on_gpu:
             _refuse("tensors must be on a GPU")
         cuda = self.torch.cuda
         if cuda.current_device() != self.index:
             with cuda.device(self.index):
-                return self(stream, *more)
+                return self(stream, workspace)
+        if self.workspace_bytes == 0 and workspace is None:
+            more = (0, 0)
+        elif self.workspace_bytes and workspace is None:
+            if stream is not None:
+                _refuse("air_prompt_attn: a call on a stream of its own needs its workspace")
+            workspace = self.torch.empty(self.workspace_bytes, dtype=self.torch.uint8, device=self.device)
+            more = (workspace.data_ptr(), self.workspace_bytes)
         st = self.fn(self.raw_stream(self.index) if stream is None else stream, *self.args, *more)
         if st != AIR_OK:
             raise AirError(st, load_library().air_last_error(None).decode())
@@ -472,13 +488,4 @@ def air_prompt_attn(*tensors, prepared: Optional[PreparedCall] = None, workspace
     """prepared: result of prepare_prompt_attn (skips the marshalling); else its arguments.  workspace: a contiguous tensor of at least
     prepared.workspace_bytes on the tensors' device; default: one allocated for the call on torch's current stream, which is then the only
     stream the call may go to.  stream: a raw HIP stream handle, default torch's current stream on the tensors' device."""
-    p = prepared or prepare_prompt_attn(*tensors, **kw)
-    if workspace is None:
-        if not p.workspace_bytes or not p.on_gpu:
-            return p(stream, 0, 0)
-        if stream is not None:
-            _refuse("air_prompt_attn: a call on a stream of its own needs its workspace")
-        workspace = p.torch.empty(p.workspace_bytes, dtype=p.torch.uint8, device=p.device)
-    elif workspace.device != p.device or not workspace.is_contiguous():
-        _refuse("air_prompt_attn: the workspace must be contiguous, on the tensors' device")
-    p(stream, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    (prepared or prepare_prompt_attn(*tensors, **kw))(stream, workspace)

@@ -170,3 +170,32 @@ def test_scales_whose_base_2_factor_overflows_are_refused():
     for scale, text in ((2.0 ** 127, None), (2.4e38, "scale must be"), (3.4e38, "scale must be"), (float("inf"), "scale must be"), (1e-45, None)):
         got = _workspace(_config("bf16", 64, 4, 2, scale=scale), [(0, 0, 0, 0, 1, 9)])[1]
         assert got is None if text is None else text in got, (scale, got)
+
+
+class _OnGpu:
+    """What PreparedCall asks of torch, without a GPU."""
+
+    def __init__(self):
+        self.made = []
+
+    class cuda:
+        current_device = staticmethod(lambda: 0)
+
+    uint8 = torch.uint8
+
+    def empty(self, n, dtype, device):
+        self.made.append(torch.empty(n, dtype=dtype))
+        return self.made[-1]
+
+
+def test_a_prepared_attention_may_be_called():
+    q, k = torch.zeros(1, 4, 1, 64), torch.zeros(1, 2, 9000, 64)
+    lib = _lib()
+    for m in (9000, 3):
+        call = A.prepare_prompt_attn(q, k, k, q.clone(), spans=[(0, 0, 1, 0, m)])
+        seen = []
+        call.torch, call.on_gpu, call.raw_stream = _OnGpu(), True, lambda i: 77
+        call.fn = C.CFUNCTYPE(C.c_int, *lib.air_prompt_attn.argtypes)(lambda *args: seen.append((args[0], args[8], args[9])) or 0)
+        call()
+        made = call.torch.made
+        assert seen == [(77, made[0].data_ptr(), made[0].numel())] if m == 9000 else seen == [(77, None, 0)] and not made
