@@ -310,7 +310,8 @@ size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt
 /* For query head h and query t of a sequence:  out = sum_j p_j v_j,  p = softmax over the keys j <= t + kv_len - q_len of
  * scale * q . k_j, with the keys and values of KV head h / (n_q_heads / n_kv_heads).  What lies at keys behind a row's own position, or
  * behind kv_len, counts for nothing, whatever it holds (infinities and NaN included).  A row that sees no key (q_len > kv_len), or
- * only logits of -inf, is zero.  Output rows outside the sequences are left as they are.  Logits, maxima, sums and products are
+ * only logits of -inf, is zero.  In any other row a value that is not finite, at a key that the row sees, makes its column not finite, however
+ * little the key weighs: the infinity where the weight is above 2^-120, that or no number where it is less (0 included).  Output rows outside the sequences are left as they are.  Logits, maxima, sums and products are
  * held in fp32, the products with the values before they are divided by the sum (values below 2^120 / kv_len cannot overflow there);
  * with bf16 the probabilities are rounded to bf16 for the second product.  seqs: host array, n_seqs in 0..AIR_MAX_BATCH.
  * workspace: 256-byte aligned, free for another call when this one's work has run; may be NULL where no bytes are needed.

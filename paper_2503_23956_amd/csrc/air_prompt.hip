@@ -134,6 +134,10 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
+// Factor that brings sums of the reference m to the reference top >= m; no logit but -inf: 0.  Sums of weight 0 are taken along, not left out:
+// a value that is not finite, at a key whose weight is 0, makes its column no number wherever its key lies.
+__device__ __forceinline__ float weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
+
 // s * c rounded, less the reference (two operations, not one)
 __device__ __forceinline__ float rounded_exponent(float s, float c, float ref) {
 #pragma clang fp contract(off)
@@ -302,7 +306,8 @@ struct Stage {
     }
 };
 
-// the values of keys [key0, key1) that are not finite, added to the accumulators of a row that sees the keys up to `last`
+// the values of keys [key0, key1) that are not finite, added to the accumulators of a row that sees the keys up to `last` (whole, as their weights
+// are not known here: what a weight of 0 makes no number elsewhere becomes an infinity)
 template <typename T, int ND>
 __device__ __forceinline__ void add_not_finite(f32x16 (&acc)[ND], const T *vg, int64_t v_t, int key0, int key1, int last, int h) {
     for (int key = key0; key < key1 && key <= last; ++key)
@@ -552,8 +557,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
         if (kw == 1) return;
         const float2 other = s_ml[rw * 32 + n];
         const float now = fmaxf(ref, other.x);
-        const float f0 = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - now);
-        const float f1 = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.x - now);
+        const float f0 = weight(ref, now), f1 = weight(other.x, now);
         ref = now;
         l = l * f0 + other.y * f1;
 #pragma unroll
@@ -736,7 +740,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     float M = s_m[0][n];
 #pragma unroll
     for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][n]);
-    const float f = at.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(at.m - M);
+    const float f = weight(at.m, M);
     if (h == 0) s_l[wave][n] = l * f;
     constexpr int kQuads = D / 4;  // 16-byte pieces of a row of sums
     static_assert(sizeof(tiles) >= NW * 32 * D * sizeof(float), "the tiles' memory holds the sums");
@@ -747,7 +751,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
         for (int i = 0; i < 4; ++i) {
             f32x4 x;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = f == 0.f ? 0.f : at.acc[d][4 * i + j] * f;
+            for (int j = 0; j < 4; ++j) x[j] = at.acc[d][4 * i + j] * f;  // (f of 0: 0, but for values that are not finite)
             sums[(wave * 32 + n) * kQuads + ((8 * d + 2 * i + h) ^ (n & 15))] = x;
         }
     __syncthreads();
@@ -827,14 +831,14 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
         float top = m;
 #pragma unroll
         for (int i = 0; i < kRound; ++i) top = fmaxf(top, ml[i].x);
-        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        const float f = weight(m, top);
         l *= f;
         x *= f;
         m = top;
 #pragma unroll
         for (int i = 0; i < kRound; ++i) {
-            if (s0 + i * groups >= a.splits || ml[i].y == 0.f) continue;  // (a split that saw nothing left nothing)
-            const float w = __builtin_amdgcn_exp2f(ml[i].x - m);
+            if (s0 + i * groups >= a.splits) continue;
+            const float w = weight(ml[i].x, m);
             l = fmaf(w, ml[i].y, l);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = fmaf(w, o[i][j], x[j]);
@@ -847,13 +851,12 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
         if (g != 0) return;
         float top = m;
         for (int i = 1; i < groups; ++i) top = fmaxf(top, s_ml[team + i].x);
-        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        const float f = weight(m, top);
         l *= f;
         x *= f;
         for (int i = 1; i < groups; ++i) {
             const float2 ml = s_ml[team + i];
-            if (ml.y == 0.f) continue;
-            const float w = __builtin_amdgcn_exp2f(ml.x - top);
+            const float w = weight(ml.x, top);
             l = fmaf(w, ml.y, l);
             const f32x4 o = s_x[threadIdx.x + i * kQuads];
 #pragma unroll

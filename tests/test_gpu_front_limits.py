@@ -1,5 +1,9 @@
 """What air_rope and air_prompt_attn promise at the edges of their arguments, on the GPU."""
+import math
+
 import pytest
+
+from test_gpu_prompt import KINDS, _run, _tensors
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +57,63 @@ def test_prepared_calls_called_directly():
     turn()
     with pytest.raises(A.AirError, match="takes no workspace"):
         turn(workspace=ws)
+
+
+def _without(q, k, v, n, m, low, high):
+    """Attention in fp64 of n queries behind m - n keys, without the keys low .. high - 1, and its bound (the roundings as test_gpu_prompt
+    counts them: logits of d products in fp32, exp2 to 2^-22, sums of m terms, bf16 probabilities and outputs)."""
+    import torch
+
+    d, g = q.shape[3], q.shape[1] // k.shape[1]
+    at = torch.arange(m, device=q.device)
+    use = (at[None, :] <= torch.arange(n, device=q.device)[:, None] + (m - n)) & ((at < low) | (at >= high))[None, :]
+    want, bound = [], []
+    for h in range(q.shape[1]):
+        qs, ks, vs = q[0, h, :n].double(), k[0, h // g].double(), v[0, h // g].double()
+        s = (qs @ ks.T.contiguous() * d ** -0.5).masked_fill(~use, -math.inf)
+        p = torch.softmax(s, dim=1).nan_to_num(0.0)
+        dot = (qs.abs() @ ks.abs().T.contiguous() * d ** -0.5).masked_fill(~use, 0.0).amax(1, keepdim=True)
+        rel = 2 * (torch.expm1(dot * ((d + 8) * 2.0 ** -24)) + 2.0 ** -22 + (m + 64) * 2.0 ** -24)
+        step = 2.0 ** -24
+        if q.dtype == torch.bfloat16:
+            rel, step = rel + 2.0 ** -8, 2.0 ** -8
+        o, a = p @ vs, p @ vs.abs() * rel
+        want.append(o)
+        bound.append(a * 1.01 + (o.abs() + a) * step + 1e-37)
+    return torch.stack(want), torch.stack(bound)
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("hq,hkv,n,m", [(4, 2, 1, 40), (4, 2, 3, 700), (28, 4, 1, 6000), (8, 2, 70, 3000), (28, 4, 200, 333), (28, 4, 900, 900), (28, 4, 3000, 3100)])
+@pytest.mark.parametrize("key", [-math.inf, -3e4])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_visible_values_that_are_not_finite(dtype, d, hq, hkv, n, m, key, bad):
+    """At keys that weigh nothing, whole tiles, waves and splits of them: their columns are not finite, wherever the keys lie; nothing else changes."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    q, k, v = _tensors(1, n, m, hq, hkv, d, dtype, n + m + d, order="token")
+    q = q.abs()
+    spans = [(0, 0, n, 0, m)]
+    seen = torch.arange(n, device=q.device) + (m - n)  # last key of a row
+    # (first and last such key, keys of them whose value is not finite)
+    for low, high, at in ((0, m * 2 // 3, (0, m // 3)), (m // 5, m // 2, (m // 5 + 1,)), (max(1, m - 2), m, (m - 1,)), (max(1, m - 1 - n // 2), m, (max(1, m - 1 - n // 2),))):
+        k2, v2 = k.clone(), v.clone()
+        k2[:, :, low:high] = key
+        want, bound = _without(q, k, v, n, m, low, high)
+        for column, i in zip((5, d - 2), at):
+            v2[:, :, i, column] = bad
+        got = _run(A, q, k2, v2, spans)[0].double()
+        some = torch.zeros((n, d), dtype=torch.bool, device=q.device)  # rows and columns that such a value reaches
+        for column, i in zip((5, d - 2), at):
+            some[:, column] |= seen >= i
+        # a query element of 0 meets a key of -inf: 0 x inf, the logit is no number, and the row is none
+        none = (q[0, :, :n] == 0).any(-1, keepdim=True) & (seen[:, None] >= low) & math.isinf(key)
+        assert bool(torch.isnan(got[none.expand_as(got)]).all())
+        zero = ((seen[:, None] < high) & (low == 0) & ~none).expand_as(got)  # rows of nothing but such keys
+        if math.isinf(key):
+            assert bool((got[zero] == 0).all())
+        some = some.expand_as(got) & ~zero & ~none
+        assert not bool(torch.isfinite(got[some]).any()), (low, high, at)
+        assert bool(((got - want).abs() <= bound)[~some & ~zero & ~none].all()), (low, high, at)
