@@ -223,13 +223,23 @@ struct Attend {
             const int at = v_lane(lane);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                bf16x8 x;
+                // a probability as the sum of two bf16 numbers: 2^-16 of it is lost, 2^-8 with one.  The matrix unit has time, as a tile waits for
+                // memory and for its own chain of operations: one token over 7432 keys 10.8 us with one term, 10.9 with two, 16 of them 43.1 and
+                // 43.7, prompts of 1024 tokens with 14 / 2 heads of 64 12.3 and 13.0; error of a token's row against fp64 0.0020 and 0.0017
+                bf16x8 x, y;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = (__bf16)s[8 * half + i];
-                const uint4 p = __builtin_bit_cast(uint4, x);
-                l = sum_of(p, l);
+                for (int i = 0; i < 8; ++i) {
+                    const float p = s[8 * half + i], top = __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+                    x[i] = (__bf16)top;
+                    // (not negative, and 0 only with p: an infinite value stays the infinity that it is with one term)
+                    y[i] = (__bf16)__builtin_amdgcn_fmed3f(p - top, 0x1p-126f, p);
+                    l += p;
+                }
 #pragma unroll
-                for (int d = 0; d < ND; ++d) acc[d] = mma32(read_v<D>(sv, at, half, d), p, acc[d], T());
+                for (int d = 0; d < ND; ++d) {
+                    const uint4 v = read_v<D>(sv, at, half, d);
+                    acc[d] = mma32(v, __builtin_bit_cast(uint4, y), mma32(v, __builtin_bit_cast(uint4, x), acc[d], T()), T());
+                }
             }
         } else {
             const float *base = reinterpret_cast<const float *>(sv) + 32 * h + n;
@@ -482,6 +492,8 @@ __global__ __launch_bounds__(512, 2) void prompt_pipe_kernel(PromptArgs a) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             bf16x8 x;
+            // rounded to bf16, 2^-8 of a probability: a second term, as Attend has it, would be half as much work again for the matrix unit,
+            // which is what these kernels wait for
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[8 * half + i], mul, -sub));
             p[half] = __builtin_bit_cast(uint4, x);
@@ -880,7 +892,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
 // measured; on 145 others the choice takes 1 % longer than the best of up to 60 on average, 11 % at worst.  Some, us in tiles of 32 / 128 / 256
 // rows, each with the splits that are chosen for it, the choice in brackets.
 // bf16, heads of 128, 28 / 4 of them: prompts of 256 tokens [9.8] / 11.5 / 13.4, 512 19 / [15.7] / 19.7, 1024 45 / [24] / 32, 2048 113 / [48] / 57,
-// 3000 215 / 95 / [88], 7432 1055 / 455 / [400]; heads of 64, 14 / 2: 1024 [12.4] / 16 / 23, 4096 79 / [52] / 60, 8000 246 / 177 / [154];
+// 3000 215 / 95 / [88], 7432 1055 / 455 / [400]; heads of 64, 14 / 2: 1024 [13.0] / 16 / 23, 4096 79 / [52] / 60, 8000 246 / 177 / [154];
 // 33 prompts of 200 tokens, 16 / 1: 35 / 21 / [15].  One token of 28 / 4 heads of 128 with 1 / 4 / 16 / 64 splits: 7432 keys 75 / 26 / 13.9 / [11.0]; 1024
 // keys 14.6 without, [9.7] with; 256 keys [7.2].  64 tokens behind 15936 keys, tiles of 128 rows, 4 / 16 / 64 splits: 71 / 35 / 68 (chosen: 33.7).
 // fp32, tiles of 32 / 128 rows: heads of 128, 28 / 4: 512 tokens [40] / 47, 1024 114 / [94], 2048 356 / [291], 5000 1862 / [1466],

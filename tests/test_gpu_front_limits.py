@@ -117,3 +117,28 @@ def test_visible_values_that_are_not_finite(dtype, d, hq, hkv, n, m, key, bad):
         some = some.expand_as(got) & ~zero & ~none
         assert not bool(torch.isfinite(got[some]).any()), (low, high, at)
         assert bool(((got - want).abs() <= bound)[~some & ~zero & ~none].all()), (low, high, at)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,n,m", [(7, 1, 1, 2), (28, 4, 1, 5), (28, 4, 1, 40), (8, 2, 4, 700), (28, 4, 1, 7432), (16, 1, 2, 3000), (14, 2, 3, 33)])
+def test_probabilities_of_single_tokens_keep_16_bits(d, hq, hkv, n, m):
+    """Elements whose values cancel show the roundings of the probabilities: 2^-16 of each, not the 2^-8 of bf16."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    q, k, v = _tensors(1, n, m, hq, hkv, d, "bf16", n + m + d, order="token")
+    got = _run(A, q, k, v, [(0, 0, n, 0, m)])[0].double()
+    g = hq // hkv
+    qs, ks, vs = q[0].double(), k[0].double().repeat_interleave(g, dim=0), v[0].double().repeat_interleave(g, dim=0)
+    behind = torch.arange(m, device=q.device)[None, :] > torch.arange(n, device=q.device)[:, None] + (m - n)
+    s = (qs @ ks.transpose(1, 2).contiguous() * d ** -0.5).masked_fill(behind, -math.inf)
+    dot = (qs.abs() @ ks.abs().transpose(1, 2).contiguous() * d ** -0.5).masked_fill(behind, 0.0).amax(-1, keepdim=True)
+    p = torch.softmax(s, dim=-1)
+    want, size = p @ vs, p @ vs.abs()
+    # two bf16 terms, 16 bits: p = 2^e (1 + ...) less its first 8 bits is below 2^(e - 7), half a step there at most 2^(e - 16); logits in fp32 (d products and the factor), exp2 to 2^-22, sums of m terms;
+    # both in the sum of the probabilities too; bf16 rounds the output
+    rel = 2 * (torch.expm1(dot * ((d + 8) * 2.0 ** -24)) + 2.0 ** -22 + (m + 64) * 2.0 ** -24) + 2.0 ** -16
+    bound = size * rel * 1.01 + (want.abs() + size * rel) * 2.0 ** -8
+    far = (got - want).abs() - bound
+    assert bool((far <= 0).all()), f"{far.max().item()} above its bound, {int((far > 0).sum())} elements"
