@@ -268,7 +268,7 @@ typedef struct {
  * for pair i of y, turning with axis a:  angle = positions[a] * freqs[i],
  *   (y_first, y_second) -> scale * (y_first cos - y_second sin, y_first sin + y_second cos).
  * Rows of v are copied.  Any of q, k, v may be NULL (not all): that tensor is left out.  Computed in fp32 (a norm's squares too: elements
- * below 2^60) with angles reduced in fp64 (positions of a million turn as exactly as small ones) and rounded once.
+ * below 2^60) with angles reduced in fp64 (to 2^-28 turns at any position below 2^51 turns) and rounded once.
  * positions: device [n_axes][batch][n_tokens]; a row whose position on axis 0 is negative is padding: nothing is written there,
  * whatever lies in its source.  NULL only without pairs.  freqs: device [sum of axis_pairs], radians per position.         */
 air_status air_rope(void *stream, const air_rope_config *cfg, const air_rope_tensor *q, const air_rope_tensor *k,

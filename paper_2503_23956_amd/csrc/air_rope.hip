@@ -3,7 +3,7 @@
 // One read and one write of every element, bound by memory: a row (one token, one head) belongs to a group of
 // head_dim / (2 kVec) lanes, a lane holds two 16-byte pieces that contain both halves of its pairs in either layout, so the
 // rotation needs no exchange between lanes and the norm one sum over the group.  A group takes a run of heads of one token:
-// the angles of its pairs (one fp64 product and one sine and cosine each) are formed once for the run.
+// the angles of its pairs (a chain of fp64 operations, a sine and a cosine each) are formed once for the run.
 // 7432 tokens of 28 / 4 heads of 128 elements in bf16, values with them: 29 us, 4.7 TB/s (a plain copy 4.9); 32911 tokens of 64 / 8 heads with norms
 // 292 us, 4.6 TB/s; one token 3.4 us in a graph, what any launch takes.
 #include <math.h>
@@ -50,6 +50,25 @@ __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = f[i];
     return __builtin_bit_cast(uint4, v);
+}
+
+// Cosine and sine of p f radians.  The product and 2 / pi are taken in two parts each, so that what is left when whole quarter turns are dropped
+// is right to 2^-53 of a turn and 2^-100 of all turns: the same for positions of 2^31 as for small ones (in one part each, 2^-24 turns were
+// lost there).  The rest z, rounded to fp32 once, is at most pi / 4: the series to z^9 and z^10 leave 2e-9 and 2e-10.
+__device__ __forceinline__ void turn_by(double p, double f, float &cs, float &sn) {
+#pragma clang fp contract(off)  // t less its quarters: of t as it was rounded, whose rest t_low holds
+    constexpr double kHigh = 0x1.45f306dc9c883p-1, kLow = -0x1.6b01ec5417056p-55;  // 2 / pi
+    const double x = p * f, x_low = fma(p, f, -x);
+    const double t = x * kHigh, t_low = fma(x, kHigh, -t) + fma(x, kLow, x_low * kHigh);
+    const double n = rint(t);
+    const float z = (float)(((t - n) + t_low) * 1.5707963267948966), zz = z * z;
+    const int k = __double2loint(n + 0x1.8p52);  // the quarters' last two bits
+    const float s = fmaf(z * zz, fmaf(zz, fmaf(zz, fmaf(zz, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), z);
+    const float c = fmaf(zz, fmaf(zz, fmaf(zz, fmaf(zz, fmaf(zz, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+    cs = k & 1 ? s : c;
+    sn = k & 1 ? c : s;
+    if ((k + 1) & 2) cs = -cs;
+    if (k & 2) sn = -sn;
 }
 
 // RUN: heads of one token that a group of lanes takes, their loads in flight together
@@ -104,10 +123,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
             for (int i = 0; i < kVec; ++i) {
                 const int pair = kVec * lane + i;
                 const int p = pair < a.end0 ? pos[0] : (pair < a.end1 ? pos[1] : pos[2]);
-                // whole turns are dropped in fp64: what is left is a fraction of a turn to 2^-25, at any position
-                const double turn = (double)p * a.freqs[pair] * 0.15915494309189533577;  // 1 / (2 pi)
-                const float part = (float)(turn - rint(turn));
-                sincospif(2.0f * part, &sn[i], &cs[i]);
+                turn_by((double)p, a.freqs[pair], cs[i], sn[i]);
                 cs[i] *= a.scale;
                 sn[i] *= a.scale;
             }

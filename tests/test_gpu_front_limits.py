@@ -142,3 +142,38 @@ def test_probabilities_of_single_tokens_keep_16_bits(d, hq, hkv, n, m):
     bound = size * rel * 1.01 + (want.abs() + size * rel) * 2.0 ** -8
     far = (got - want).abs() - bound
     assert bool((far <= 0).all()), f"{far.max().item()} above its bound, {int((far > 0).sum())} elements"
+
+
+@pytest.mark.parametrize("low,high", [(0, 5000), (10 ** 6, 10 ** 6 + 5000), (2 ** 30, 2 ** 31 - 1)])
+def test_angles_at_any_position(low, high):
+    """Cosine and sine of position x frequency, against the fraction of a turn in whole numbers: 2 pi to 200 bits."""
+    import random
+    from fractions import Fraction
+
+    import numpy as np
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    rng = random.Random(low)
+    inverse = Fraction("0.159154943091895335768883763372514362034459645740456448747667344058896797634226535090113802766253085956")  # 1 / (2 pi)
+    scaled = int(inverse * 2 ** 300)
+    T, pairs = 4000, 32
+    pos = [rng.randint(low, high) for _ in range(T - 2)] + [low, high]
+    freqs = [1.0, 0.5, 8.0, 2 * math.pi / 64] + [rng.uniform(0.5, 1.0) for _ in range(pairs - 4)]
+    turns = np.empty((T, pairs))
+    for j, f in enumerate(freqs):
+        top, bottom = f.as_integer_ratio()
+        mod = bottom << 300
+        for i, p in enumerate(pos):
+            turns[i, j] = float(Fraction(p * top * scaled % mod, mod))
+    q = torch.zeros((1, 1, T, 64), device="cuda:0")
+    q[..., :pairs] = 1.0  # the first of every pair: the result is (cos, sin)
+    A.air_rope(q, positions=torch.tensor([[pos]], dtype=torch.int32, device="cuda:0"), freqs=torch.tensor(freqs, dtype=torch.float64, device="cuda:0"),
+               axis_pairs=(pairs,))
+    torch.cuda.synchronize()
+    got = q[0, 0].double().cpu().numpy()
+    # the rest of a turn to 2^-28 of one (2 pi 2^-28 rad); sine and cosine to 4 units of 2^-24; products with 1 and 0 are exact
+    bound = 2 * math.pi * 2.0 ** -28 + 4 * 2.0 ** -24
+    far = np.maximum(abs(got[:, :pairs] - np.cos(2 * math.pi * turns)), abs(got[:, pairs:] - np.sin(2 * math.pi * turns)))
+    assert far.max() <= bound, (far.max(), bound)
