@@ -268,7 +268,7 @@ typedef struct {
  * for pair i of y, turning with axis a:  angle = positions[a] * freqs[i],
  *   (y_first, y_second) -> scale * (y_first cos - y_second sin, y_first sin + y_second cos).
  * Rows of v are copied.  Any of q, k, v may be NULL (not all): that tensor is left out.  Computed in fp32 (a norm's squares too: elements
- * below 2^60) with angles reduced in fp64 (to 2^-28 turns at any position below 2^51 turns) and rounded once.
+ * below 2^60, and with norm_eps 0 their root mean square above 2^-60) with angles reduced in fp64 (to 2^-28 turns up to 2^49 turns) and rounded once.
  * positions: device [n_axes][batch][n_tokens]; a row whose position on axis 0 is negative is padding: nothing is written there,
  * whatever lies in its source.  NULL only without pairs.  freqs: device [sum of axis_pairs], radians per position.         */
 air_status air_rope(void *stream, const air_rope_config *cfg, const air_rope_tensor *q, const air_rope_tensor *k,
@@ -345,6 +345,10 @@ air_status air_get_lengths(air_ctx *ctx, int32_t *host);
  * order, element type = cfg.dtype: host [max_rows][d] each; fails if length > max_rows */
 air_status air_get_cache(air_ctx *ctx, int32_t l, int32_t b, int32_t h, void *k_host, void *v_host,
                          int32_t max_rows);
+
+/* how air_prompt_attn would run a call: rows of a tile (32, 128 or 256) and splits over the keys.  Host only; refuses what air_prompt_attn
+ * refuses of these arguments */
+air_status air_prompt_plan(const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, int32_t *tile_rows, int32_t *splits);
 
 /* text of the last failure on ctx; NULL: of the calling thread's last failure in a call that needs no context */
 const char *air_last_error(const air_ctx *ctx);

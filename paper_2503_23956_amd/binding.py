@@ -80,7 +80,7 @@ EXPORTS = (
     "air_version", "air_workspace_bytes", "air_create", "air_destroy", "air_reset", "air_set_tuning", "air_score",
     "air_budget", "air_select_compact", "air_decode_attn", "air_decode_attn_static", "air_get_scores", "air_get_elite", "air_get_stats",
     "air_get_budgets", "air_set_budgets", "air_get_indices", "air_set_indices", "air_get_lengths", "air_get_cache",
-    "air_last_error", "air_rope", "air_rope_frequencies", "air_prompt_workspace_bytes", "air_prompt_attn",
+    "air_last_error", "air_rope", "air_rope_frequencies", "air_prompt_workspace_bytes", "air_prompt_attn", "air_prompt_plan",
 )
 
 _lib = None
@@ -129,6 +129,7 @@ def load_library(path: Optional[str] = None):
     lib.air_rope_frequencies.argtypes = [i32, dbl, i32, dbl, i32, dbl, dbl, vp, C.POINTER(C.c_float)]
     lib.air_prompt_workspace_bytes.argtypes = [C.POINTER(air_prompt_config), C.POINTER(air_prompt_seq), i32]
     lib.air_prompt_workspace_bytes.restype = C.c_size_t
+    lib.air_prompt_plan.argtypes = [C.POINTER(air_prompt_config), C.POINTER(air_prompt_seq), i32, C.POINTER(i32), C.POINTER(i32)]
     lib.air_prompt_attn.argtypes = [vp, C.POINTER(air_prompt_config), C.POINTER(air_prompt_seq), i32, vp, vp, vp, vp, vp, C.c_size_t]
     for name in EXPORTS:
         if name not in ("air_version", "air_workspace_bytes", "air_prompt_workspace_bytes", "air_last_error"):
@@ -489,3 +490,13 @@ def air_prompt_attn(*tensors, prepared: Optional[PreparedCall] = None, workspace
     prepared.workspace_bytes on the tensors' device; default: one allocated for the call on torch's current stream, which is then the only
     stream the call may go to.  stream: a raw HIP stream handle, default torch's current stream on the tensors' device."""
     (prepared or prepare_prompt_attn(*tensors, **kw))(stream, workspace)
+
+
+def air_prompt_plan(prepared: PreparedCall):
+    """(rows of a tile, splits over the keys) with which a result of prepare_prompt_attn runs."""
+    lib = load_library()
+    rows, splits = C.c_int32(), C.c_int32()
+    st = lib.air_prompt_plan(*prepared.args[:3], C.byref(rows), C.byref(splits))
+    if st != AIR_OK:
+        raise AirError(st, lib.air_last_error(None).decode())
+    return rows.value, splits.value

@@ -249,6 +249,16 @@ size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt
     return check_prompt("air_prompt_workspace_bytes", cfg, seqs, n_seqs, &plan) == AIR_OK ? plan.bytes : 0;
 }
 
+air_status air_prompt_plan(const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, int32_t *tile_rows, int32_t *splits) {
+    PromptPlan plan;
+    if (!tile_rows || !splits) return refuse(AIR_ERR_INVALID_ARG, "air_prompt_plan: null argument");
+    const air_status st = check_prompt("air_prompt_plan", cfg, seqs, n_seqs, &plan);
+    if (st != AIR_OK) return st;
+    *tile_rows = plan.tile_rows;
+    *splits = plan.splits;
+    return AIR_OK;
+}
+
 air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, const void *q,
                            const void *k, const void *v, void *out, void *workspace, size_t workspace_bytes) {
     PromptPlan plan;

@@ -199,3 +199,61 @@ def test_a_prepared_attention_may_be_called():
         call()
         made = call.torch.made
         assert seen == [(77, made[0].data_ptr(), made[0].numel())] if m == 9000 else seen == [(77, None, 0)] and not made
+
+
+# calls of several sequences, unequal lengths, more keys than queries and fewer, one without queries: one of every kernel, without splits and with
+MIXED = [(dt, d, hq, hkv, [*pairs, (0, 5), (9, 4)], rows, split) for dt, d, hq, hkv, pairs, rows, split in (
+    ("bf16", 128, 8, 8, [(40, 41), (77, 77)], 32, False),
+    ("bf16", 128, 8, 8, [(40, 540), (77, 1077)], 32, True),
+    ("bf16", 128, 16, 1, [(40, 40), (77, 90), (114, 114), (151, 200), (188, 188)], 128, False),
+    ("bf16", 128, 8, 8, [(40, 3040), (77, 6077), (114, 3114)], 128, True),
+    ("bf16", 128, 64, 8, [(40, 40), (77, 90), (114, 114), (151, 200), (188, 188)], 256, False),
+    ("bf16", 128, 28, 4, [(901, 901), (1333, 1400), (612, 1000), (1100, 1107)], 256, False),
+    ("bf16", 128, 16, 2, [(200, 3100), (237, 6137), (274, 3174), (311, 6211), (248, 3248)], 256, True),
+    ("bf16", 64, 8, 8, [(40, 41), (77, 77)], 32, False),
+    ("bf16", 64, 8, 8, [(40, 540), (77, 1077)], 32, True),
+    ("bf16", 64, 64, 8, [(100, 110), (137, 137), (174, 200)], 128, False),
+    ("bf16", 64, 14, 2, [(300, 3100), (200, 4000)], 128, True),
+    ("bf16", 64, 64, 8, [(40, 40), (77, 90), (114, 114), (151, 200), (188, 188)], 256, False),
+    ("bf16", 64, 16, 1, [(40, 3040), (77, 6077), (114, 3114), (151, 6151), (188, 3188)], 256, True),
+    ("f32", 128, 8, 8, [(40, 40), (77, 77)], 32, False),
+    ("f32", 128, 8, 8, [(40, 71), (77, 139)], 32, True),
+    ("f32", 128, 64, 8, [(100, 110), (137, 137), (174, 200)], 128, False),
+    ("f32", 128, 14, 2, [(40, 540), (77, 1077), (114, 614)], 128, True),
+    ("f32", 64, 8, 8, [(40, 41), (77, 77)], 32, False),
+    ("f32", 64, 8, 8, [(40, 540), (77, 1077)], 32, True),
+    ("f32", 64, 64, 8, [(40, 71), (77, 139), (114, 145), (151, 213), (188, 219)], 128, False),
+    ("f32", 64, 8, 8, [(400, 900), (437, 1437), (474, 974)], 128, True),
+)]
+
+
+@pytest.mark.parametrize("dtype,d,hq,hkv,pairs,rows,split", MIXED)
+def test_plans_of_mixed_calls(dtype, d, hq, hkv, pairs, rows, split):
+    cfg = _config(dtype, d, hq, hkv)
+    seqs = _prompts(cfg, pairs)
+    arr = (A.air_prompt_seq * len(seqs))(*(A.air_prompt_seq(*s) for s in seqs))
+    got, splits = C.c_int32(), C.c_int32()
+    assert _lib().air_prompt_plan(C.byref(A.air_prompt_config(**cfg)), arr, len(seqs), C.byref(got), C.byref(splits)) == 0
+    assert (got.value, splits.value > 1) == (rows, split), splits.value
+    assert (_workspace(cfg, seqs)[0] > 0) == split
+
+
+def test_plans_are_refused_as_calls_are():
+    lib, n = _lib(), C.c_int32()
+    cfg = A.air_prompt_config(**_config("bf16", 64, 4, 2))
+    arr = (A.air_prompt_seq * 1)(A.air_prompt_seq(0, 0, 0, 0, -1, 3))
+    assert lib.air_prompt_plan(C.byref(cfg), arr, 1, C.byref(n), C.byref(n)) == SHAPE and b"length" in lib.air_last_error(None)
+    assert lib.air_prompt_plan(C.byref(cfg), arr, 0, None, C.byref(n)) == binding.AIR_ERR_INVALID_ARG
+    assert lib.air_prompt_plan(None, arr, 1, C.byref(n), C.byref(n)) == binding.AIR_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("text,kw", [
+    ("dtype", dict(dtype=-1)), ("head_dim", dict(head_dim=80)), ("multiple of KV heads", dict(n_q_heads=3)), ("multiple of KV heads", dict(n_kv_heads=-2)),
+    ("n_seqs", dict(n=65)), ("n_seqs", dict(n=-1)), ("strides must be", dict(q_t=-512)), ("strides must be", dict(k_h=4)), ("output rows overlap", dict(out_t=120)),
+    ("token strides", dict(k_t=1 << 24)), ("token strides", dict(v_t=1 << 24)), ("output rows overlap", dict(out_h=0)),
+    ("a length", dict(seqs=((0, 0, 0, 0, -1, 3),))), ("a length", dict(seqs=((0, 0, 0, 0, 1, (1 << 30) + 1),))),
+    ("offsets", dict(seqs=((-8, 0, 0, 0, 1, 3),))), ("offsets", dict(seqs=((0, 4, 0, 0, 1, 3),))), ("too many rows", dict(seqs=((0, 0, 0, 0, 1 << 24, 1),))),
+])
+def test_refusals_name_their_reason(text, kw):
+    assert _attn(**kw)[0] == SHAPE
+    assert text in _lib().air_last_error(None).decode()

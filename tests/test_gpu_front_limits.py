@@ -3,7 +3,8 @@ import math
 
 import pytest
 
-from test_gpu_prompt import KINDS, _run, _tensors
+from test_front_limits import MIXED
+from test_gpu_prompt import KINDS, _check, _run, _tensors
 
 pytestmark = pytest.mark.gpu
 
@@ -177,3 +178,31 @@ def test_angles_at_any_position(low, high):
     bound = 2 * math.pi * 2.0 ** -28 + 4 * 2.0 ** -24
     far = np.maximum(abs(got[:, :pairs] - np.cos(2 * math.pi * turns)), abs(got[:, pairs:] - np.sin(2 * math.pi * turns)))
     assert far.max() <= bound, (far.max(), bound)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype,d,hq,hkv,pairs,rows,split", MIXED)
+def test_mixed_calls_of_every_kernel(dtype, d, hq, hkv, pairs, rows, split, packed):
+    """Sequences in rows of a padded batch or behind each other with gaps; what lies behind a sequence's keys is no number."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    nq, nk = max(n for n, _ in pairs), max(m for _, m in pairs)
+    if packed:
+        spans, q0, k0 = [], 2, 1
+        for n, m in pairs:
+            spans.append((0, q0, n, k0, m))
+            q0, k0 = q0 + n + 3, k0 + m + 2
+        q, k, v = _tensors(1, q0, k0, hq, hkv, d, dtype, d + hq + rows, order="head")
+    else:
+        spans = [(b, 0, n, 0, m) for b, (n, m) in enumerate(pairs)]
+        q, k, v = _tensors(len(pairs), nq, nk, hq, hkv, d, dtype, d + hq + rows, order="token")
+    used = torch.zeros((k.shape[0], k.shape[2]), dtype=torch.bool, device=k.device)
+    for b, _, _, k0, m in spans:
+        used[b, k0:k0 + m] = True
+    for x in (k, v):
+        x.masked_fill_(~used[:, None, :, None], math.nan)
+    tile, splits = A.air_prompt_plan(A.prepare_prompt_attn(q, k, v, torch.empty_like(q), spans=spans))
+    assert (tile, splits > 1) == (rows, split)
+    _check(q, k, v, spans, _run(A, q, k, v, spans))
