@@ -908,9 +908,10 @@ static const TileCost kCosts[4][3] = {
     {{32, 512, 128, 5.6, 4.6, 2.9, 2.55}, {128, 768, 32, 3.8, 0.0, 11.9, 8.4}, {0}},                                    // fp32, heads of 64
 };
 constexpr int kMostSplits = 64;
-// Splits have to be worth their partial results: by 2 % of the modelled time, more than the model is off on average, and in no more than
-// 256 MiB.  Without either bound, fp32 prompts of 97499 tokens over 258675 keys, 64 / 8 heads, took 6.5 GB for a modelled 0.004 %; with both, of 6000
-// calls of 1 to 10^6 tokens 103 are chosen otherwise, the worst of them 2.9 % slower in the model (a bound of 128 MiB: 5.5 %, of 64 MiB: 38 %).
+// Splits have to be worth their partial results: these are at most 256 MiB, and that much has to gain 2 % of the modelled time (less as much less:
+// a gain of half a percent in the model for 59 MB is 13 % on the card, fp32, 14 / 2 heads of 64, 8000 tokens: 912 us, 1048 without).
+// Without the bound, fp32 prompts of 97499 tokens over 258675 keys, 64 / 8 heads, took 6.5 GB for a modelled 0.004 %; with it, of 6000 calls of 1
+// to 10^6 tokens 88 are chosen otherwise, the worst of them 2.9 % slower in the model (a bound of 128 MiB: 5.5 %, of 64 MiB: 38 %).
 // Every plan can be launched: without splits there are fewer than 2^21 + 2^20 workgroups of 512 (2^26 rows in tiles of 32, and 64 sequences
 // of 16384 heads with a tile that is not whole), with them and in the join no more than the 2^19 slots that 256 MiB hold.
 constexpr double kSplitGain = 0.02;
@@ -948,12 +949,7 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
     best.n_rows = n_rows;
     const int64_t all_rows = n_rows * c.n_kv_heads;
     if (all_rows >= (1 << 26)) return best;  // indexes of 32 bits
-    // the best choice without splits and with them: rows of a tile, tiles, splits, us
-    struct Choice {
-        int rows, splits;
-        int64_t tiles;
-        double us;
-    } whole = {0, 0, 0, INFINITY}, split = whole;
+    double least = INFINITY;
     for (const TileCost &k : kCosts[(f32 ? 2 : 0) + (c.head_dim == 128 ? 0 : 1)]) {
         if (k.rows == 0) continue;
         int64_t tiles = 0;
@@ -967,23 +963,25 @@ PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, i
         const double full = keys * c.n_kv_heads / kCUs / 128.0 * k.full, read = bytes / 5.2e6;
         // 1 to 8 splits, then four to every doubling
         for (int s = 1; s <= kMostSplits && (s == 1 || longest > 64 * s); s += s < 8 ? 1 : (s < 16 ? 2 : (s < 32 ? 4 : 8))) {
-            if (part_bytes(all_rows, s, c.head_dim) > kMostPartBytes) break;
+            const size_t part = part_bytes(all_rows, s, c.head_dim);
+            if (part > kMostPartBytes) break;
             const double at_work = fmax(1.0, wgs * s / kCUs);  // workgroups a CU: part of a last, uneven deal is lost
             const double all = full * (1.0 + 0.3 * (ceil(at_work) / at_work - 1.0));
             const double work = fmax(ceil((double)longest / s / k.grain) * k.grain / 128.0 * k.step, all);
             double us = k.start + k.round * (ceil(fmax(1.0, wgs * s / k.at_once)) - 1.0) + sqrt(work * work + read * read);
             if (s > 1) us += 2.9 + 2.1 * all_rows * s * (c.head_dim * 4 + 8) / 4e6;
-            Choice &to = s == 1 ? whole : split;
-            if (us < to.us) to = Choice{k.rows, s, tiles, us};
+            us *= 1.0 + kSplitGain * part / kMostPartBytes;
+            if (us < least) {
+                least = us;
+                best.tile_rows = k.rows;
+                best.n_tiles = tiles;
+                best.splits = s;
+                best.bytes = part;
+            }
         }
     }
-    const Choice &taken = split.us < (1.0 - kSplitGain) * whole.us ? split : whole;
-    best.tile_rows = taken.rows;
-    best.few = taken.rows == 32;
-    best.n_tiles = taken.tiles;
-    best.splits = taken.splits;
-    best.ml_bytes = taken.splits == 1 ? 0 : ml_bytes(all_rows, taken.splits);
-    best.bytes = part_bytes(all_rows, taken.splits, c.head_dim);
+    best.few = best.tile_rows == 32;
+    best.ml_bytes = best.splits > 1 ? ml_bytes(all_rows, best.splits) : 0;
     return best;
 }
 

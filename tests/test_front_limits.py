@@ -87,7 +87,7 @@ def test_splits_are_worth_their_workspace():
         cfg = _config(rng.choice(["bf16", "f32"]), rng.choice([64, 128]), hkv * rng.choice([1, 2, 5, 7, 8, 16]), hkv)
         lens = [(_log_int(rng, 0, 18), _log_int(rng, 0, 22)) for _ in range(rng.choice([1, 1, 2, 8, 33]))]
         assert _workspace(cfg, _prompts(cfg, lens))[0] <= 256 << 20, (cfg, lens)
-    for dtype, d, hq, hkv, lens in (("bf16", 128, 28, 4, [(1, 7432)]), ("bf16", 64, 14, 2, [(1, 7432), (1, 33), (1, 4000)]), ("f32", 64, 4, 2, [(656, 656)]),
+    for dtype, d, hq, hkv, lens in (("bf16", 128, 28, 4, [(1, 7432)]), ("bf16", 64, 14, 2, [(1, 7432), (1, 33), (1, 4000)]), ("f32", 64, 4, 2, [(656, 656)]), ("f32", 64, 14, 2, [(8000, 8000)]),
                                     ("bf16", 128, 64, 8, [(512, 16910)]), ("bf16", 128, 64, 8, [(1, 1 << 20)] * 8)):
         cfg = _config(dtype, d, hq, hkv)
         assert _workspace(cfg, _prompts(cfg, lens))[0] > 0
