@@ -311,9 +311,10 @@ size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt
  * scale * q . k_j, with the keys and values of KV head h / (n_q_heads / n_kv_heads).  What lies at keys behind a row's own position, or
  * behind kv_len, counts for nothing, whatever it holds (infinities and NaN included).  A row that sees no key (q_len > kv_len), or
  * only logits of -inf, is zero.  In any other row a value that is not finite, at a key that the row sees, makes its column not finite, however
- * little the key weighs: the infinity where the weight is above 2^-120, that or no number where it is less (0 included).  Output rows outside the sequences are left as they are.  Logits, maxima, sums and products are
- * held in fp32, the products with the values before they are divided by the sum (values below 2^120 / kv_len cannot overflow there);
- * with bf16 and many rows the probabilities are rounded to bf16 for the second product, with few rows (single tokens, short prompts) to 2^-16.  seqs: host array, n_seqs in 0..AIR_MAX_BATCH.
+ * little the key weighs: the infinity where the weight is above 2^-120, that or no number where it is less (0 included).  Output rows
+ * outside the sequences are left as they are.  Logits, maxima, sums and products are held in fp32, the products with the values before they are divided by the sum (values below 2^120 / kv_len cannot overflow there);
+ * with bf16 the probabilities are rounded to bf16 for the second product; sequences of at most 32 rows (queries x query heads per KV head: single
+ * tokens, steps) lose only 2^-16 of them in calls that run in tiles of 32 rows.  seqs: host array, n_seqs in 0..AIR_MAX_BATCH.
  * workspace: 256-byte aligned, free for another call when this one's work has run; may be NULL where no bytes are needed.
  * out must not overlap an input.  Output rows that overlap, of one sequence or of two, are refused (AIR_ERR_SHAPE). */
 air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, const void *q,

@@ -185,8 +185,10 @@ struct Attend {
             for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
     }
 
-    // last: last key of the tile that the lane's query sees, counted from the tile's first (read when masked, uniform over the wave)
-    __device__ __forceinline__ void step(const u32x4 *sk, const u32x4 *sv, bool masked, int last, float c) {
+    // last: last key of the tile that the lane's query sees, counted from the tile's first (read when masked, uniform over the wave).
+    // two (bf16, uniform over the workgroup): probabilities of the second product as the sum of two bf16 numbers, of which 2^-16 is lost,
+    // not 2^-8 as with one
+    __device__ __forceinline__ void step(const u32x4 *sk, const u32x4 *sv, bool masked, bool two, int last, float c) {
         const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
         f32x16 s;
 #pragma unroll
@@ -223,22 +225,31 @@ struct Attend {
             const int at = v_lane(lane);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                // a probability as the sum of two bf16 numbers: 2^-16 of it is lost, 2^-8 with one.  The matrix unit has time, as a tile waits for
-                // memory and for its own chain of operations: one token over 7432 keys 10.8 us with one term, 10.9 with two, 16 of them 43.1 and
-                // 43.7, prompts of 1024 tokens with 14 / 2 heads of 64 12.3 and 13.0; error of a token's row against fp64 0.0020 and 0.0017
                 bf16x8 x, y;
+                if (two) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float p = s[8 * half + i], top = __uint_as_float(__float_as_uint(p) & 0xffff0000u);
-                    x[i] = (__bf16)top;
-                    // (not negative, and 0 only with p: an infinite value stays the infinity that it is with one term)
-                    y[i] = (__bf16)__builtin_amdgcn_fmed3f(p - top, 0x1p-126f, p);
-                    l += p;
+                    for (int i = 0; i < 8; ++i) {
+                        const float p = s[8 * half + i], top = __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+                        x[i] = (__bf16)top;
+                        // (not negative, and 0 only with p: an infinite value stays the infinity that it is with one term)
+                        y[i] = (__bf16)__builtin_amdgcn_fmed3f(p - top, 0x1p-126f, p);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = (__bf16)s[8 * half + i];
                 }
+                const uint4 p = __builtin_bit_cast(uint4, x);
+                uint4 v[ND];
 #pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const uint4 v = read_v<D>(sv, at, half, d);
-                    acc[d] = mma32(v, __builtin_bit_cast(uint4, y), mma32(v, __builtin_bit_cast(uint4, x), acc[d], T()), T());
+                for (int d = 0; d < ND; ++d) v[d] = read_v<D>(sv, at, half, d);
+                l = sum_of(p, l);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) acc[d] = mma32(v[d], p, acc[d], T());
+                if (two) {
+                    const uint4 rest = __builtin_bit_cast(uint4, y);
+                    l = sum_of(rest, l);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) acc[d] = mma32(v[d], rest, acc[d], T());
                 }
             }
         } else {
@@ -665,7 +676,7 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
         stage.store(sk[b & 1], sv[b & 1]);  // (read for block b - 2, which every wave has left before the last barrier)
         lds_barrier();
         if (b + 1 < b1) stage.load(a, kg, vg, (b + 1) * 32, pl.kv_len);
-        if (b * 32 <= wave_last) at.step(sk[b & 1], sv[b & 1], masked, last - b * 32, a.c);
+        if (b * 32 <= wave_last) at.step(sk[b & 1], sv[b & 1], masked, false, last - b * 32, a.c);
     }
     const float l = at.l + __shfl_xor(at.l, 32, 64);
     if (s_bad) add_not_finite(at.acc, vg, a.v_t, max(b0, see_all / 32) * 32, min(b1 * 32, see_any), last, h);
@@ -697,9 +708,14 @@ __global__ __launch_bounds__(256, 2) void prompt_share_kernel(PromptArgs a) {
 // ---------------------------------------------------------------------------------------
 // Few rows: 32 of one (sequence, KV head).  Four waves share the rows and deal the key tiles of 32 among themselves; each moves its
 // tiles through LDS of its own, the next tile's loads in flight, without a barrier: one wave takes in 32 keys in about 1.3 us, a launch of 16
-// tokens over 7432 keys each 244 MB in 44 us.
+// tokens over 7432 keys each 244 MB in 39 us (the join 5 more).
+// TWO (bf16): where a sequence has one tile of rows (tokens, steps, pieces of a few queries), its probabilities are the sum of two bf16 numbers.
+// Such a sequence reads K and V for one tile only and waits for them, not for the matrix unit: one token over 7432 keys 10.9 us with one term and
+// 10.9 with two, 16 of them 43.1 to 43.9 and 43.4 to 43.7, the error of their rows against fp64 0.0020 and 0.0017.  A prompt's tiles keep the
+// matrix unit busy: 2048 tokens with 14 / 2 heads of 64 take 25.7 us with one term, 28.9 with two; calls without a sequence of one tile run
+// a kernel that does not ask (26.6 where it asks).
 // ---------------------------------------------------------------------------------------
-template <typename T, int D>
+template <typename T, int D, bool TWO>
 __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     fetch(a);
     using R = Row<T, D>;
@@ -734,6 +750,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
     }
     if (threadIdx.x == 0) s_bad = 0;
     __syncthreads();
+    const bool two = TWO && n_rows <= 32;
     u32x4 *sk = tiles[wave], *sv = sk + R::kKTile;
 #pragma unroll 1
     for (; b < b1; b += NW) {
@@ -743,7 +760,7 @@ __global__ __launch_bounds__(256) void prompt_few_kernel(PromptArgs a) {
         stage.store(sk, sv);
         wave_sync();
         if (b + NW < b1) stage.load(a, kg, vg, (b + NW) * 32, pl.kv_len);
-        at.step(sk, sv, masked, last - b * 32, a.c);
+        at.step(sk, sv, masked, two, last - b * 32, a.c);
     }
     // merge of the four waves: every wave brings its sums to the common reference and leaves them in LDS
     const float l = at.l + __shfl_xor(at.l, 32, 64);
@@ -892,7 +909,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
 // measured; on 145 others the choice takes 1 % longer than the best of up to 60 on average, 11 % at worst.  Some, us in tiles of 32 / 128 / 256
 // rows, each with the splits that are chosen for it, the choice in brackets.
 // bf16, heads of 128, 28 / 4 of them: prompts of 256 tokens [9.8] / 11.5 / 13.4, 512 19 / [15.7] / 19.7, 1024 45 / [24] / 32, 2048 113 / [48] / 57,
-// 3000 215 / 95 / [88], 7432 1055 / 455 / [400]; heads of 64, 14 / 2: 1024 [13.0] / 16 / 23, 4096 79 / [52] / 60, 8000 246 / 177 / [154];
+// 3000 215 / 95 / [88], 7432 1055 / 455 / [400]; heads of 64, 14 / 2: 1024 [12.4] / 16 / 23, 4096 79 / [52] / 60, 8000 246 / 177 / [154];
 // 33 prompts of 200 tokens, 16 / 1: 35 / 21 / [15].  One token of 28 / 4 heads of 128 with 1 / 4 / 16 / 64 splits: 7432 keys 75 / 26 / 13.9 / [11.0]; 1024
 // keys 14.6 without, [9.7] with; 256 keys [7.2].  64 tokens behind 15936 keys, tiles of 128 rows, 4 / 16 / 64 splits: 71 / 35 / 68 (chosen: 33.7).
 // fp32, tiles of 32 / 128 rows: heads of 128, 28 / 4: 512 tokens [40] / 47, 1024 114 / [94], 2048 356 / [291], 5000 1862 / [1466],
@@ -995,7 +1012,11 @@ static void prompt_launch(hipStream_t s, const PromptPlan &p, const PromptArgs &
     if constexpr (sizeof(T) == 4) {
         if (!p.few) hipLaunchKernelGGL((prompt_share_kernel<T, D>), grid, dim3(256), 0, s, a);
     }
-    if (p.few) hipLaunchKernelGGL((prompt_few_kernel<T, D>), grid, dim3(256), 0, s, a);
+    if (p.few) {
+        const bool two = sizeof(T) == 2 && a.s[a.n_seqs - 1].q_len * a.G <= 32;  // (the last sequence has the fewest queries)
+        if (two) hipLaunchKernelGGL((prompt_few_kernel<T, D, sizeof(T) == 2>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((prompt_few_kernel<T, D, false>), grid, dim3(256), 0, s, a);
+    }
     if (p.splits > 1) {
         const int groups = join_groups(p.splits, D);
         const dim3 join((unsigned)join_blocks(p.n_rows * a.Hkv, p.splits, D));
