@@ -14,9 +14,9 @@
 //
 // Softmax in the base-2 domain with a running reference per query; it is raised only when a logit lies more than kSlack above it.
 //
-// Measured (bf16, heads of 128): prompts of 7432 tokens, 28 / 4 heads, 385 us (1.03 PFLOP/s); 16910 + 16001 tokens, 64 / 8 heads, 8.08 ms (on
-// another card 405 and 8.48; 1.1 PFLOP/s, matrix unit busy 55 % of the clocks at 1.9 GHz; with inputs of zeros 1.34 PFLOP/s: bound by power); one
-// token over 7432 keys 11.5 us (two launches).
+// Measured (bf16, heads of 128): prompts of 7432 tokens, 28 / 4 heads, 384 to 407 us by card (1 PFLOP/s, matrix unit busy 47 % of the clocks at 2.05
+// GHz); 16910 + 16001 tokens, 64 / 8 heads, 7.79 to 8.48 ms (1.1 PFLOP/s, matrix unit busy 55 % at 1.92 GHz; with inputs of zeros 1.34 PFLOP/s: bound by
+// power); one token over 7432 keys 11 us (two launches).
 #include <math.h>
 #include <string.h>
 
@@ -906,7 +906,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, int grou
 // workgroups run together); 128 keys of the longest workgroup `step` (keys are dealt by `grain`), and of all workgroups together,
 // spread over the CUs, `full` (the clock falls when every matrix unit works).  Splits: the join, its launch and the partial results written and
 // read.  Fitted to 880 calls of 1 to 17000 tokens, 1 to 33 sequences, 1 to 16 query heads per KV head, alone in a graph, every tile and split
-// measured; on 145 others the choice takes 1 % longer than the best of up to 60 on average, 11 % at worst.  Some, us in tiles of 32 / 128 / 256
+// measured; on 800 others the choice takes 1.1 % longer than the best of up to 60 on average, nine in ten at most 3.1 %, the worst 46 %.  Some, us in tiles of 32 / 128 / 256
 // rows, each with the splits that are chosen for it, the choice in brackets.
 // bf16, heads of 128, 28 / 4 of them: prompts of 256 tokens [9.8] / 11.5 / 13.4, 512 19 / [15.7] / 19.7, 1024 45 / [24] / 32, 2048 113 / [48] / 57,
 // 3000 215 / 95 / [88], 7432 1055 / 455 / [400]; heads of 64, 14 / 2: 1024 [12.4] / 16 / 23, 4096 79 / [52] / 60, 8000 246 / 177 / [154];

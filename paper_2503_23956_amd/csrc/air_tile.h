@@ -1,6 +1,6 @@
 // MFMA operands and the layouts of the compacted cache, for both storage types and head sizes.
 //
-// Every matrix product of the library has 16 x 16 output tiles.  A lane (n = lane % 16, c = lane / 16) supplies 16 bytes
+// Every matrix product of the compressed path has 16 x 16 output tiles (those of prompts: air_prompt.hip).  A lane (n = lane % 16, c = lane / 16) supplies 16 bytes
 // of an operand at a time: of row (or column) n, the c-th quarter of a slice of kSlice contraction indices:
 //   bf16  8 elements a lane, slices of 32: one v_mfma_f32_16x16x32_bf16
 //   fp32  4 elements a lane, slices of 16: four v_mfma_f32_16x16x4_f32 (element i of every lane's 16 bytes in product i;
