@@ -18,6 +18,12 @@
  *   air_rope           per-head norm and position rotation of queries and keys, laid out for the calls above.
  *   air_prompt_attn    causal attention of a prompt, a piece of one or a single token over the full cache.
  *
+ * Behind it, for long generation (no context either):
+ *
+ *   air_quant_append   rows of K and V into a cache held in 4 bits; air_quant_read: what it stands for.
+ *   air_quant_attn     attention over that cache: tokens, windows and pieces; what every slot was attended to.
+ *   air_evict          drops the least attended tokens of a cache (4 bits, or rows of any type) in place.
+ *
  * Conventions
  *   - Every tensor pointer is DEVICE memory unless its comment says "host".  Descriptor
  *     arrays (air_layer[], air_seq[]) and getter outputs are HOST memory.
@@ -319,6 +325,107 @@ size_t air_prompt_workspace_bytes(const air_prompt_config *cfg, const air_prompt
  * out must not overlap an input.  Output rows that overlap, of one sequence or of two, are refused (AIR_ERR_SHAPE). */
 air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air_prompt_seq *seqs, int32_t n_seqs, const void *q,
                            const void *k, const void *v, void *out, void *workspace, size_t workspace_bytes);
+
+/* ---- behind the compression: a cache in 4 bits, attention over it, eviction by attention weight ----
+ *
+ * As above: no context, kernels only (recordable), tensors, workspace and stream of the current device, air_last_error(NULL).  What a
+ * cache holds is counted in DEVICE memory by the caller (`lens`), so that a recorded step serves every length: the calls read it when
+ * they run, never change it, and clamp it to 0..capacity.                                                                     */
+
+/* K and V in 4 bits.  Groups of `group` elements of a row share
+ *   lo   = the least element, rounded down to bf16,
+ *   step = (greatest - lo) / 15, rounded up to bf16; 0 where that is below 2^-120 (all codes are 0 then)
+ *   code = (x - lo) / step rounded to the nearest whole number (ties to even), in 0..15
+ * (difference, division by 15 and quotient rounded to fp32 each) and stand for lo + step code: off by at most step / 2 and 2^-22 of the
+ * largest magnitude.  A group with an element that is not finite, or of 2^126 and more, stands for NaN throughout.
+ * Memory, per (sequence, KV head, slot): codes head_dim / 2 bytes; scales head_dim / group pairs (lo, step) of bf16.
+ *   V: element c in byte c / 2, even elements in the low half.  K: elements 8 p .. 8 p + 7 (p = 4 m + n, n < 4) in the four bytes
+ *   from head_dim / 8 n + 4 m, element 8 p + i in the low half of byte i for i < 4, in the high half of byte i - 4 above. */
+typedef struct {
+    int32_t batch, n_kv_heads, capacity; /* batch x n_kv_heads at most 65535; capacity slots per (sequence, KV head), 1..2^24 */
+    int32_t head_dim, group;             /* 64 or 128; 32 or 64                                                                */
+    int32_t dtype;                       /* air_dtype of the rows that go in and come out, of queries and outputs              */
+    void *k_codes, *v_codes;   /* [batch][n_kv_heads][capacity][head_dim / 2] bytes, 16-byte aligned                         */
+    void *k_scales, *v_scales; /* [batch][n_kv_heads][capacity][head_dim / group][2] bf16, 16-byte aligned                   */
+} air_quant_cache;
+
+/* Rows [batch][n_kv_heads][n_tokens] of K and V.  Strides in elements, non-negative multiples of 16 bytes.  Row t of sequence b belongs
+ * to slot lens[b] + t.  Rows t >= counts[b] (NULL: n_tokens everywhere) are padding, and so are those whose slot lies outside the
+ * capacity: neither the cache nor what lies at them is touched. */
+typedef struct {
+    void *k, *v;
+    int64_t k_b, k_h, k_t, v_b, v_h, v_t;
+    int32_t n_tokens;          /* batch x n_tokens at most 2^27 (0: nothing is done)                                          */
+    const int32_t *lens;       /* device [batch]: slot of row 0; NULL: 0                                                      */
+    const int32_t *counts;     /* device [batch]; NULL: n_tokens                                                              */
+    int32_t *positions;        /* device [batch][n_kv_heads][capacity] or NULL: the slot's position, for air_evict            */
+    const int32_t *first_positions; /* device [batch], with positions: of row 0 (row t: first + t)                            */
+    float *weights;            /* device [batch][n_kv_heads][capacity] or NULL: the slot's weight, which starts at 0          */
+} air_quant_rows;
+
+/* Writes rows of k and v (read, not changed) into the cache, and positions and weights of their slots where given. */
+air_status air_quant_append(void *stream, const air_quant_cache *cache, const air_quant_rows *rows);
+
+/* Writes what the slots stand for to k and v (either may be NULL), rounded once.  positions, first_positions and weights must be NULL.  Rows of
+ * k and of v that overlap are refused (AIR_ERR_SHAPE). */
+air_status air_quant_read(void *stream, const air_quant_cache *cache, const air_quant_rows *rows);
+
+typedef struct {
+    int32_t n_q_heads, n_tokens; /* a multiple of the KV heads, at most 16384; queries of a sequence, with padding (0: nothing is done).
+                                    n_tokens x n_q_heads below 2^26                                                             */
+    int32_t causal;              /* 0: every query sees all slots held; 1: query t of n sees all but the last n - 1 - t        */
+    int32_t max_len;             /* most slots that a sequence will hold when the call runs: only the launch's shape goes by it; 0: capacity */
+    float scale;                 /* of the logits, > 0, at most 2^127; 0: 1 / sqrt(head_dim)                                  */
+    const void *q;               /* [batch][n_q_heads][n_tokens][head_dim]                                                     */
+    void *out;                   /* the same, or NULL: weights only                                                            */
+    int64_t q_b, q_h, q_t, out_b, out_h, out_t; /* element strides, non-negative multiples of 16 bytes                        */
+    const int32_t *lens;         /* device [batch]: slots held before the call                                                */
+    const int32_t *counts;       /* device [batch]: queries of a sequence; NULL: n_tokens.  Rows behind them are left as they are */
+    float *weights;              /* device [batch][n_kv_heads][capacity] or NULL                                               */
+} air_quant_query;
+
+/* Bytes of device workspace the call needs (0: none, or an argument that air_quant_attn refuses). */
+size_t air_quant_workspace_bytes(const air_quant_cache *cache, const air_quant_query *query);
+
+/* With `append` (its n_tokens, lens and counts those of the query) the call first does air_quant_append: the sequence then holds
+ * lens + counts slots, else lens.  For query head h (KV head h / (n_q_heads / n_kv_heads)) and query t:
+ *   out = sum_j p_j v_j,  p = softmax over the slots j that it sees of scale * q . k_j
+ * and, with weights, weights[b][KV head][j] += sum of p_j over the queries and the query heads of the KV head, in a fixed order.
+ * A query that sees no slot gives zero.  What lies in slots that a query does not see counts for nothing, whatever it stands for; a group
+ * of NaN in a slot that it sees makes its part of the output (V) or all of it (K) NaN.  Products of codes are exact; logits,
+ * sums and outputs are held in fp32 (with bf16 the factor of a code, p step, keeps 16 bits), outputs rounded once.
+ * Causal queries belong to the last counts slots of the sequence: after air_evict slots have no order, so a call of
+ * more than one causal query appends its own rows.  workspace: 256-byte aligned, free for another call when this one's work has run.
+ * out must not overlap an input; output rows that overlap are refused (AIR_ERR_SHAPE). */
+air_status air_quant_attn(void *stream, const air_quant_cache *cache, const air_quant_query *query, const air_quant_rows *append,
+                          void *workspace, size_t workspace_bytes);
+
+#define AIR_MAX_PLANES 8
+/* Rows that belong to slots: [batch][n_heads][capacity] rows of row_bytes bytes (a multiple of 4, at most 1024, 4-byte aligned; strides
+ * in bytes, non-negative multiples of 4; capacity x row_bytes at most 2^33).  Rows of all planes must not overlap. */
+typedef struct {
+    void *rows;
+    int64_t b, h, t;
+    int32_t row_bytes;
+} air_evict_plane;
+
+typedef struct {
+    int32_t batch, n_heads, capacity; /* batch x n_heads at most 65535; capacity 1..2^24                                  */
+    int32_t keep, limit;              /* sequences with more than `limit` slots keep `keep`; 1 <= keep <= limit                */
+    int32_t first, recent;            /* tokens that stay whatever they weigh; >= 0, together at most keep                     */
+    int32_t n_planes;                 /* 0..AIR_MAX_PLANES                                                                     */
+    air_evict_plane planes[AIR_MAX_PLANES];
+} air_evict_config;
+
+/* For every (sequence, head) with n = lens[b] > limit slots, which of them stay: first the tokens whose position is below `first`
+ * or among the `recent` positions up to the largest one there; then those of the largest weights (NaN before every number, ties to the lower
+ * slot), `keep` in all.  The i-th slot below `keep` that is given up takes what the i-th staying slot from `keep` on has: its rows of
+ * all planes, its weight and its position.  Slots from `keep` on are left as they are.  lens_out[b] = keep, or lens[b] where
+ * nothing is given up (not lens itself, which other calls of the launch's time may read).  positions: may be NULL with first =
+ * recent = 0.  weights, positions: device [batch][n_heads][capacity].  workspace: 256-byte aligned, air_evict_workspace_bytes (0: none). */
+air_status air_evict(void *stream, const air_evict_config *cfg, float *weights, int32_t *positions, const int32_t *lens, int32_t *lens_out,
+                     void *workspace, size_t workspace_bytes);
+size_t air_evict_workspace_bytes(const air_evict_config *cfg);
 
 /* ---- inspection (tests, debugging): these synchronise the device ---- */
 /* importance scores of layer l: host [B][H_kv][max_vis_len], the device buffer as it is (entries past a

@@ -76,11 +76,39 @@ class air_prompt_seq(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("q_off", "k_off", "v_off", "out_off")] + [("q_len", C.c_int32), ("kv_len", C.c_int32)]
 
 
+class air_quant_cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_kv_heads", "capacity", "head_dim", "group", "dtype")] + [
+        (n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales")]
+
+
+class air_quant_rows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(n, C.c_int64) for n in ("k_b", "k_h", "k_t", "v_b", "v_h", "v_t")] + [
+        ("n_tokens", C.c_int32)] + [(n, C.c_void_p) for n in ("lens", "counts", "positions", "first_positions", "weights")]
+
+
+class air_quant_query(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_tokens", "causal", "max_len")] + [("scale", C.c_float), ("q", C.c_void_p), ("out", C.c_void_p)] + [
+        (n, C.c_int64) for n in ("q_b", "q_h", "q_t", "out_b", "out_h", "out_t")] + [(n, C.c_void_p) for n in ("lens", "counts", "weights")]
+
+
+AIR_MAX_PLANES = 8
+
+
+class air_evict_plane(C.Structure):
+    _fields_ = [("rows", C.c_void_p), ("b", C.c_int64), ("h", C.c_int64), ("t", C.c_int64), ("row_bytes", C.c_int32)]
+
+
+class air_evict_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_heads", "capacity", "keep", "limit", "first", "recent", "n_planes")] + [
+        ("planes", air_evict_plane * AIR_MAX_PLANES)]
+
+
 EXPORTS = (
     "air_version", "air_workspace_bytes", "air_create", "air_destroy", "air_reset", "air_set_tuning", "air_score",
     "air_budget", "air_select_compact", "air_decode_attn", "air_decode_attn_static", "air_get_scores", "air_get_elite", "air_get_stats",
     "air_get_budgets", "air_set_budgets", "air_get_indices", "air_set_indices", "air_get_lengths", "air_get_cache",
     "air_last_error", "air_rope", "air_rope_frequencies", "air_prompt_workspace_bytes", "air_prompt_attn", "air_prompt_plan",
+    "air_quant_append", "air_quant_read", "air_quant_workspace_bytes", "air_quant_attn", "air_evict_workspace_bytes", "air_evict",
 )
 
 _lib = None
@@ -131,8 +159,17 @@ def load_library(path: Optional[str] = None):
     lib.air_prompt_workspace_bytes.restype = C.c_size_t
     lib.air_prompt_plan.argtypes = [C.POINTER(air_prompt_config), C.POINTER(air_prompt_seq), i32, C.POINTER(i32), C.POINTER(i32)]
     lib.air_prompt_attn.argtypes = [vp, C.POINTER(air_prompt_config), C.POINTER(air_prompt_seq), i32, vp, vp, vp, vp, vp, C.c_size_t]
+    lib.air_quant_append.argtypes = [vp, C.POINTER(air_quant_cache), C.POINTER(air_quant_rows)]
+    lib.air_quant_read.argtypes = [vp, C.POINTER(air_quant_cache), C.POINTER(air_quant_rows)]
+    lib.air_quant_workspace_bytes.argtypes = [C.POINTER(air_quant_cache), C.POINTER(air_quant_query)]
+    lib.air_quant_workspace_bytes.restype = C.c_size_t
+    lib.air_quant_attn.argtypes = [vp, C.POINTER(air_quant_cache), C.POINTER(air_quant_query), C.POINTER(air_quant_rows), vp, C.c_size_t]
+    lib.air_evict_workspace_bytes.argtypes = [C.POINTER(air_evict_config)]
+    lib.air_evict_workspace_bytes.restype = C.c_size_t
+    lib.air_evict.argtypes = [vp, C.POINTER(air_evict_config), vp, vp, vp, vp, vp, C.c_size_t]
     for name in EXPORTS:
-        if name not in ("air_version", "air_workspace_bytes", "air_prompt_workspace_bytes", "air_last_error"):
+        if name not in ("air_version", "air_workspace_bytes", "air_prompt_workspace_bytes", "air_quant_workspace_bytes",
+                        "air_evict_workspace_bytes", "air_last_error"):
             getattr(lib, name).restype = C.c_int
     if path is None:
         _lib = lib
@@ -358,12 +395,14 @@ def _strides4(t):
 
 
 class PreparedCall:
-    """Marshalled arguments of one air_rope / air_prompt_attn call plus the tensors they point to; may be called any number of
-    times (the tensors' contents may change between calls).  workspace_bytes: what an attention call needs, None for a rotation."""
+    """Marshalled arguments of one call without a context plus the tensors they point to; may be called any number of
+    times (the tensors' contents may change between calls).  workspace_bytes: what an attention or eviction call needs, None for calls
+    that take no workspace."""
 
     def __init__(self, fn, args, device, keepalive, workspace_bytes=None):
         import torch
 
+        self.name = fn.__name__
         self.torch, self.fn, self.args, self.device, self.workspace_bytes, self._keepalive = torch, fn, args, device, workspace_bytes, keepalive
         self.on_gpu = device.type == "cuda"
         self.index = device.index if device.index is not None else 0
@@ -372,14 +411,14 @@ class PreparedCall:
 
     def __call__(self, stream=None, workspace=None):
         """Enqueues the call with the tensors' device current; stream: a raw HIP stream handle, default torch's current one there.
-        workspace (attention): a contiguous tensor of at least workspace_bytes on the tensors' device; default: one allocated for the call on
+        workspace (attention, eviction): a contiguous tensor of at least workspace_bytes on the tensors' device; default: one allocated for the call on
         torch's current stream, which is then the only stream the call may go to."""
         more = ()
         if workspace is not None:
             if self.workspace_bytes is None:
-                _refuse("air_rope: takes no workspace")
+                _refuse(f"{self.name}: takes no workspace")
             if workspace.device != self.device or not workspace.is_contiguous():
-                _refuse("air_prompt_attn: the workspace must be contiguous, on the tensors' device")
+                _refuse(f"{self.name}: the workspace must be contiguous, on the tensors' device")
             more = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
         if not self.on_gpu:
             _refuse("tensors must be on a GPU")
@@ -391,7 +430,7 @@ class PreparedCall:
             more = (0, 0)
         elif self.workspace_bytes and workspace is None:
             if stream is not None:
-                _refuse("air_prompt_attn: a call on a stream of its own needs its workspace")
+                _refuse(f"{self.name}: a call on a stream of its own needs its workspace")
             workspace = self.torch.empty(self.workspace_bytes, dtype=self.torch.uint8, device=self.device)
             more = (workspace.data_ptr(), self.workspace_bytes)
         st = self.fn(self.raw_stream(self.index) if stream is None else stream, *self.args, *more)
@@ -500,3 +539,152 @@ def air_prompt_plan(prepared: PreparedCall):
     if st != AIR_OK:
         raise AirError(st, lib.air_last_error(None).decode())
     return rows.value, splits.value
+
+
+# -- a cache that is generated into: 4-bit rows, attention over them, eviction by attention weight ------------------------
+class QuantCache:
+    """K and V of up to `capacity` slots per (sequence, KV head) in 4 bits; dtype: of the rows that go in, of queries and outputs.  The
+    memory (`planes`: codes of K and V, scales of K and V, each [B][H][capacity][...]) is torch's; what it holds is counted by the
+    caller, in an int32 tensor [B] on the same device that every call takes as `lens`."""
+
+    def __init__(self, batch, n_kv_heads, capacity, head_dim, dtype=AIR_BF16, group=32, device="cuda:0"):
+        import torch
+
+        if head_dim not in (64, 128) or group not in (32, 64) or min(batch, n_kv_heads, capacity) < 1:
+            raise AirError(AIR_ERR_SHAPE, "QuantCache: head_dim must be 64 or 128, group 32 or 64, sizes positive")
+        self.batch, self.n_kv_heads, self.capacity, self.head_dim, self.dtype, self.group = batch, n_kv_heads, capacity, head_dim, dtype, group
+        self.torch_dtype = torch.bfloat16 if dtype == AIR_BF16 else torch.float32
+        self.device = torch.device(device)
+        shape = (batch, n_kv_heads, capacity)
+        codes = [torch.empty((*shape, head_dim // 2), dtype=torch.uint8, device=self.device) for _ in range(2)]
+        scales = [torch.empty((*shape, 2 * head_dim // group), dtype=torch.bfloat16, device=self.device) for _ in range(2)]
+        self.planes = (*codes, *scales)
+        self.device = codes[0].device  # (with its index)
+        self.struct = air_quant_cache(batch, n_kv_heads, capacity, head_dim, group, dtype, *(_ptr(p) for p in self.planes))
+
+
+def _table(who, name, t, dtype, shape, device):
+    """Address of an optional contiguous tensor of one type, shape and device."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        _refuse(f"{who}: {name} must be a contiguous {dtype} {list(shape)} on the tensors' device")
+    return _ptr(t)
+
+
+def _cache_tensor(who, name, cache, t, heads):
+    """Strides of a tensor [B][heads][T][d] of the cache's type and device."""
+    if t.dtype != cache.torch_dtype or t.device != cache.device:
+        _refuse(f"{who}: {name} must have the cache's type and device")
+    st = _strides4(t)
+    if t.shape[0] != cache.batch or t.shape[3] != cache.head_dim or (heads is not None and t.shape[1] != heads):
+        _refuse(f"{who}: {name} must be indexed [B][H][T][d] as the cache is")
+    return st
+
+
+def _quant_rows(who, cache, k, v, lens, counts, positions=None, first_positions=None, weights=None):
+    import torch
+
+    first = k if k is not None else v
+    if first is None:
+        _refuse(f"{who}: one of k and v is needed")
+    st = [_cache_tensor(who, n, cache, t, cache.n_kv_heads) if t is not None else [0, 0, 0] for n, t in (("k", k), ("v", v))]
+    if k is not None and v is not None and k.shape != v.shape:
+        _refuse(f"{who}: k and v must have one shape")
+    B, cells, dev = (cache.batch,), (cache.batch, cache.n_kv_heads, cache.capacity), cache.device
+    return air_quant_rows(_ptr(k), _ptr(v), *st[0], *st[1], first.shape[2], _table(who, "lens", lens, torch.int32, B, dev),
+                          _table(who, "counts", counts, torch.int32, B, dev), _table(who, "positions", positions, torch.int32, cells, dev),
+                          _table(who, "first_positions", first_positions, torch.int32, B, dev),
+                          _table(who, "weights", weights, torch.float32, cells, dev))
+
+
+def prepare_quant_append(cache: QuantCache, k, v, *, lens=None, counts=None, positions=None, first_positions=None, weights=None) -> PreparedCall:
+    """k, v [B][Hkv][T][d], any memory order with contiguous d.  lens, counts, first_positions: int32 [B]; positions: int32, weights:
+    float32 [B][Hkv][capacity]; all on the cache's device.  Row t of sequence b goes to slot lens[b] + t, for t < counts[b]."""
+    if k is None or v is None:
+        _refuse("air_quant_append: k and v are needed")
+    rows = _quant_rows("air_quant_append", cache, k, v, lens, counts, positions, first_positions, weights)
+    return PreparedCall(load_library().air_quant_append, (C.byref(cache.struct), C.byref(rows)), cache.device,
+                        (cache, k, v, lens, counts, positions, first_positions, weights))
+
+
+def air_quant_append(*args, prepared: Optional[PreparedCall] = None, stream=None, **kw):
+    """prepared: result of prepare_quant_append (skips the marshalling); else its arguments.  stream: a raw HIP stream handle, default
+    torch's current stream on the cache's device."""
+    (prepared or prepare_quant_append(*args, **kw))(stream)
+
+
+def prepare_quant_read(cache: QuantCache, k=None, v=None, *, starts=None, counts=None) -> PreparedCall:
+    """What slots starts[b] .. starts[b] + counts[b] - 1 stand for, into k and v [B][Hkv][T][d]; either may be left out."""
+    rows = _quant_rows("air_quant_read", cache, k, v, starts, counts)
+    return PreparedCall(load_library().air_quant_read, (C.byref(cache.struct), C.byref(rows)), cache.device, (cache, k, v, starts, counts))
+
+
+def air_quant_read(*args, prepared: Optional[PreparedCall] = None, stream=None, **kw):
+    """prepared: result of prepare_quant_read; else its arguments.  stream as in air_quant_append."""
+    (prepared or prepare_quant_read(*args, **kw))(stream)
+
+
+def prepare_quant_attn(cache: QuantCache, q, out, *, lens, counts=None, k=None, v=None, causal=True, scale=0.0, weights=None, positions=None,
+                       first_positions=None, max_len=0) -> PreparedCall:
+    """q, out [B][Hq][T][d] (out may be None: weights only); k, v [B][Hkv][T][d]: the queries' own rows, which go into the cache
+    first (with positions, where given).  weights float32 [B][Hkv][capacity] grow by what every slot is attended to.  max_len: most slots a sequence
+    will hold when the call runs (the launch's shape goes by it; 0: capacity)."""
+    import torch
+
+    who, B = "air_quant_attn", (cache.batch,)
+    sq = _cache_tensor(who, "q", cache, q, None)
+    so = _cache_tensor(who, "out", cache, out, q.shape[1]) if out is not None else [0, 0, 0]
+    if out is not None and out.shape != q.shape:
+        _refuse("air_quant_attn: shapes of q and out must agree")
+    if lens is None:
+        _refuse("air_quant_attn: lens are needed")
+    if (k is None) != (v is None):
+        _refuse("air_quant_attn: k and v go together")
+    rows = None
+    if k is not None:
+        rows = _quant_rows(who, cache, k, v, lens, counts, positions, first_positions, weights)
+    elif positions is not None or first_positions is not None:
+        _refuse("air_quant_attn: positions without rows to append")
+    query = air_quant_query(q.shape[1], q.shape[2], int(causal), max_len, scale, _ptr(q), _ptr(out), *sq, *so,
+                            _table(who, "lens", lens, torch.int32, B, cache.device), _table(who, "counts", counts, torch.int32, B, cache.device),
+                            _table(who, "weights", weights, torch.float32, (*B, cache.n_kv_heads, cache.capacity), cache.device))
+    lib = load_library()
+    nbytes = lib.air_quant_workspace_bytes(C.byref(cache.struct), C.byref(query))
+    return PreparedCall(lib.air_quant_attn, (C.byref(cache.struct), C.byref(query), C.byref(rows) if rows is not None else None), cache.device,
+                        (cache, q, out, lens, counts, k, v, weights, positions, first_positions), nbytes)
+
+
+def air_quant_attn(*args, prepared: Optional[PreparedCall] = None, workspace=None, stream=None, **kw):
+    """prepared: result of prepare_quant_attn; else its arguments.  workspace and stream as in air_prompt_attn."""
+    (prepared or prepare_quant_attn(*args, **kw))(stream, workspace)
+
+
+def prepare_evict(planes, weights, *, lens, lens_out, keep, limit=None, positions=None, first=0, recent=0) -> PreparedCall:
+    """planes: tensors [B][H][capacity][n] whose rows belong to the slots (K and V as they are, or QuantCache.planes), any strides with a
+    contiguous last axis.  weights float32, positions int32 [B][H][capacity]; lens, lens_out int32 [B].  limit: default keep."""
+    import torch
+
+    who = "air_evict"
+    if weights is None or lens is None or lens_out is None:
+        _refuse("air_evict: weights, lens and lens_out are needed")
+    if weights.dim() != 3 or len(planes) > AIR_MAX_PLANES:
+        _refuse(f"air_evict: weights must be [B][H][capacity], planes at most {AIR_MAX_PLANES}")
+    B, H, cap = weights.shape
+    arr = (air_evict_plane * AIR_MAX_PLANES)()
+    for i, p in enumerate(planes):
+        if p.device != weights.device or tuple(p.shape[:3]) != (B, H, cap):
+            _refuse("air_evict: planes must be [B][H][capacity][n] on the weights' device")
+        arr[i] = air_evict_plane(_ptr(p), *(s * p.element_size() for s in _strides4(p)), p.shape[3] * p.element_size())
+    cfg = air_evict_config(B, H, cap, keep, keep if limit is None else limit, first, recent, len(planes), arr)
+    args = (C.byref(cfg), _table(who, "weights", weights, torch.float32, (B, H, cap), weights.device),
+            _table(who, "positions", positions, torch.int32, (B, H, cap), weights.device),
+            _table(who, "lens", lens, torch.int32, (B,), weights.device), _table(who, "lens_out", lens_out, torch.int32, (B,), weights.device))
+    lib = load_library()
+    return PreparedCall(lib.air_evict, args, weights.device, (planes, weights, lens, lens_out, positions),
+                        lib.air_evict_workspace_bytes(C.byref(cfg)))
+
+
+def air_evict(*args, prepared: Optional[PreparedCall] = None, workspace=None, stream=None, **kw):
+    """prepared: result of prepare_evict; else its arguments.  workspace and stream as in air_prompt_attn."""
+    (prepared or prepare_evict(*args, **kw))(stream, workspace)

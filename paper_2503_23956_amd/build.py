@@ -24,6 +24,10 @@ SOURCES = {
     "air_front.hip": [],
     "air_rope.hip": [],
     "air_prompt.hip": [],
+    "air_cache.hip": [],
+    "air_quant.hip": [],
+    "air_quant_attn.hip": [],
+    "air_evict.hip": [],
 }
 
 COMMON = [

@@ -12,7 +12,7 @@ namespace air {
 static thread_local char t_error[256];
 const char *thread_error() { return t_error; }
 
-static air_status refuse(air_status st, const char *fmt, ...) {
+air_status refuse(air_status st, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(t_error, sizeof(t_error), fmt, ap);
@@ -22,9 +22,7 @@ static air_status refuse(air_status st, const char *fmt, ...) {
 
 constexpr int kMaxHeads = 16384;  // runs of heads and (tile, head) pairs are grid dimensions
 
-static bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-
-static const char *geometry(int hq, int hkv, int d, int dtype) {
+const char *geometry(int hq, int hkv, int d, int dtype) {
     if (dtype != AIR_F32 && dtype != AIR_BF16) return "dtype must be AIR_F32 or AIR_BF16";
     if (d != 64 && d != 128) return "head_dim must be 64 or 128";
     if (hkv < 1 || hq < hkv || hq % hkv || hq > kMaxHeads) return "query heads must be a multiple of KV heads, at most 16384";
@@ -88,7 +86,7 @@ static bool rows_meet(wide c, Axis a, Axis b, int64_t d) {
 }
 
 // rows of up to three axes (extent, stride): does one of them overlap another?
-static bool rows_overlap(int64_t (&n)[3], int64_t (&stride)[3], int64_t d) {
+bool rows_overlap(int64_t (&n)[3], int64_t (&stride)[3], int64_t d) {
     int order[3] = {0, 1, 2};
     if (n[0] == 0 || n[1] == 0 || n[2] == 0) return false;
     for (int i = 0; i < 3; ++i) {

@@ -19,6 +19,20 @@ constexpr int kCacheRowAlign = 32;    // layer regions of the compacted cache st
 constexpr int kFinishChunks = 4;      // chunks finished (and summed into one moment entry) per workgroup of the finish kernels
 constexpr int kStashRows = 32;        // window rows per unit up to which air_score stashes exponentials (one pass over K_v)
 
+// Division by a number that the host knows: x / d = (x m) >> s for 0 <= x < 2^31, with 2^(s - 32) < d <= 2^(s - 31) and
+// m = ceil(2^s / d) (m d - 2^s < d <= 2^(s - 31): the quotient is off by less than 1 / d)
+struct Div {
+    uint32_t m, s;
+    __device__ __forceinline__ int of(int x) const { return (int)(((uint64_t)(uint32_t)x * m) >> s); }
+};
+inline Div div_by(int d) {
+    Div r;
+    r.s = 31;
+    while ((1ll << (r.s - 31)) < d) ++r.s;
+    r.m = (uint32_t)(((1ull << r.s) + (uint64_t)d - 1) / (uint64_t)d);
+    return r;
+}
+
 struct LayerPtrs {
     const void *q, *k, *v;
 };
@@ -143,13 +157,44 @@ struct PromptPlan {
     int64_t n_tiles, n_rows;
     size_t ml_bytes, bytes;  // workspace: (maximum, sum) pairs in front, all of it
 };
-// factor of the logits in the base-2 domain
-inline float prompt_factor(const air_prompt_config &c) {
-    return (float)((c.scale > 0.f ? (double)c.scale : 1.0 / sqrt((double)c.head_dim)) * 1.4426950408889634);
+// factor of the logits in the base-2 domain, by a call's scale (0: 1 / sqrt(head_dim))
+inline float logit_factor(float scale, int head_dim) {
+    return (float)((scale > 0.f ? (double)scale : 1.0 / sqrt((double)head_dim)) * 1.4426950408889634);
 }
+inline float prompt_factor(const air_prompt_config &c) { return logit_factor(c.scale, c.head_dim); }
 PromptPlan prompt_plan(const air_prompt_config &c, const air_prompt_seq *seqs, int n);
 hipError_t launch_prompt(hipStream_t s, const air_prompt_config &c, const PromptPlan &p, const air_prompt_seq *seqs, int n, const void *q,
                          const void *k, const void *v, void *out, void *workspace);
+
+// Where the rows of a call on a cache in 4 bits lie, and the cache
+struct QuantAppendArgs {
+    uint8_t *codes[2];    // K, V
+    uint32_t *scales[2];  // (lo, step) pairs
+    void *rows[2];
+    int64_t row_b[2], row_h[2], row_t[2];
+    const int32_t *lens, *counts, *first;
+    int32_t *positions;
+    float *weights;
+    int32_t capacity, n_tokens, Hkv, batch;
+};
+hipError_t launch_quant_rows(hipStream_t s, const air_quant_cache &c, const air_quant_rows &r, bool append);
+// The shape of a quant attention call
+struct QuantPlan {
+    int32_t row_tiles, row_blocks, splits;  // row tiles of 16 per wave, workgroups along the rows, along the slots
+    int32_t finish;                         // workgroups per (sequence, KV head) of the second launch; 0: none
+    size_t ml_bytes, bytes;                 // workspace: (maximum, sum) pairs in front, all of it
+};
+QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q);
+hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const QuantPlan &p, const air_quant_query &q, bool appended, void *workspace);
+size_t evict_bytes(const air_evict_config &c);
+hipError_t launch_evict(hipStream_t s, const air_evict_config &c, float *weights, int32_t *positions, const int32_t *lens, int32_t *lens_out,
+                        void *workspace);
+
+// ---- argument checks of those calls (air_front.hip) ----
+air_status refuse(air_status st, const char *fmt, ...);  // leaves the text for thread_error
+const char *geometry(int hq, int hkv, int d, int dtype);  // null: supported
+bool rows_overlap(int64_t (&n)[3], int64_t (&stride)[3], int64_t d);  // rows of d elements along three axes (extent, stride)
+inline bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 const char *thread_error();  // text of the calling thread's last failure in a call without a context; empty: none
 
 // The cache is laid out so that the decode kernel can feed it to MFMA straight from global memory, every load

@@ -29,20 +29,6 @@ namespace air {
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
-// Division by a number that the host knows: x / d = (x m) >> s for 0 <= x < 2^31, with 2^(s - 32) < d <= 2^(s - 31) and
-// m = ceil(2^s / d) (m d - 2^s < d <= 2^(s - 31): the quotient is off by less than 1 / d)
-struct Div {
-    uint32_t m, s;
-    __device__ __forceinline__ int of(int x) const { return (int)(((uint64_t)(uint32_t)x * m) >> s); }
-};
-static Div div_by(int d) {
-    Div r;
-    r.s = 31;
-    while ((1ll << (r.s - 31)) < d) ++r.s;
-    r.m = (uint32_t)(((1ull << r.s) + (uint64_t)d - 1) / (uint64_t)d);
-    return r;
-}
-
 struct PromptSpan {
     int64_t q_off, k_off, v_off, out_off;
     int32_t q_len, kv_len;

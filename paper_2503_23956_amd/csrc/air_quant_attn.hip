@@ -1,0 +1,637 @@
+// air_quant_attn: attention over a cache held in 4 bits, and what every slot was attended to.
+//
+// The rows of one (sequence, KV head) are its queries times the G query heads that share the KV head, token by token: row t G + i.  A wave takes
+// 64 slots at a time, for 16 or 32 rows.  S = Q K^T by 16 x 16 products of codes, one group at a time; each group's product is
+// scaled by the slot's step, and one product more adds sum(q)_g lo_g (three bf16 terms of the sums).  A lane (n, c) then has the logits of slots
+// 16 t + n, t = 0..3, and rows 4 c .. 4 c + 3.  Probabilities go through LDS in fp32, slot 16 t + n at place 4 n + t, and come back as the
+// operand of the second product: lane (n, c) takes row n and 16 places from 16 c on, times the group's steps, as bf16 terms.  The codes
+// of V go to LDS as they lie in memory and come back transposed (ds_read_b64_tr_b4: 16 slots of one element per lane), the places' order
+// and that of the codes in an operand in the lanes' row addresses.  sum_j p_j lo_j is kept per lane, for its own slots.
+//
+// Waves share nothing until their ends: each deals itself every (4 splits)-th run of 64 slots, requested one run ahead, and the four
+// partial results of a workgroup are joined in LDS.
+#include "air_device.h"
+#include "air_internal.h"
+#include "air_quant_dev.h"
+
+namespace air {
+
+struct QuantAttnArgs {
+    const uint8_t *kc, *vc;
+    const uint32_t *ks, *vs;
+    const void *q;
+    void *out;
+    float *part_o;    // [pair][split][row][D]
+    float2 *part_ml;  // [pair][split][row]
+    float *weights;
+    int64_t q_b, q_h, q_t, out_b, out_h, out_t;
+    const int32_t *lens, *counts;
+    float c;  // scale * log2(e)
+    int32_t Hkv, G, n_tokens, capacity, n_rows, splits, causal, appended;
+    Div by_g, by_hkv, by_splits;
+};
+
+constexpr int kRun = 64;  // slots that a wave takes at a time
+
+// What a sequence holds and asks
+struct QuantSpan {
+    int b, h, count, held, rows;
+    __device__ __forceinline__ QuantSpan(const QuantAttnArgs &a, int pair) {
+        b = a.by_hkv.of(pair);
+        h = pair - b * a.Hkv;
+        const int n = a.counts ? a.counts[b] : a.n_tokens;
+        count = n < 0 ? 0 : n > a.n_tokens ? a.n_tokens : n;
+        const int64_t all = (int64_t)a.lens[b] + (a.appended ? count : 0);
+        held = all < 0 ? 0 : all > a.capacity ? a.capacity : (int)all;
+        rows = count * a.G;
+    }
+    // slots that row r sees (r < rows)
+    __device__ __forceinline__ int seen(const QuantAttnArgs &a, int r) const {
+        if (!a.causal) return held;
+        const int s = held - count + 1 + a.by_g.of(r);
+        return s < 0 ? 0 : s;
+    }
+};
+
+template <int D, int GR, typename T>
+struct QuantShape {
+    static constexpr int NG = D / GR, KM = D / 32, KG = GR / 32, NT = D / 16;
+    static constexpr bool kF32 = sizeof(T) == 4;
+    static constexpr int QT = kF32 ? 3 : 1, PT = kF32 ? 3 : 2;  // bf16 terms of a query's elements; of p step
+    static constexpr int kRowBytes = D / 2, kVStride = kRowBytes + 8;  // (rows of V in LDS: 8 bytes more, 32 rows on different banks)
+    static constexpr int kPStride = 68;                                // floats
+    static constexpr int kVBytes = kRun * kVStride, kPBytes = 16 * kPStride * 4, kSBytes = NG * kRun * 4;
+    static constexpr int kWave = kVBytes + kPBytes + kSBytes;
+    static constexpr int kLds = 4 * kWave > 4 * 16 * D * 4 + 4 * 16 * 8 ? 4 * kWave : 4 * 16 * D * 4 + 4 * 16 * 8;
+};
+
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+template <int N>
+struct Words {
+    uint32_t w[N];
+};
+template <int N>
+__device__ __forceinline__ Words<N> load_words(const void *p) {
+    Words<N> r;
+    if (N == 4) *reinterpret_cast<uint4 *>(&r) = *static_cast<const uint4 *>(p);
+    else if (N == 2) *reinterpret_cast<uint2 *>(&r) = *static_cast<const uint2 *>(p);
+    else r.w[0] = *static_cast<const uint32_t *>(p);
+    return r;
+}
+
+// 16 rows of queries as operands: elements 32 m + 8 c .. + 7 of row n in lane (n, c), and the sums of their groups for the product with lo
+template <int D, int GR, typename T>
+struct QueryTile {
+    using S = QuantShape<D, GR, T>;
+    uint4 e[S::QT][S::KM], sums;
+
+    __device__ __forceinline__ void load(const QuantAttnArgs &a, const QuantSpan &sp, int row) {
+        const int c = (threadIdx.x >> 4) & 3;
+        float part[S::NG] = {};
+        const bool real = row < sp.rows;
+        const int t = a.by_g.of(real ? row : 0), i = (real ? row : 0) - t * a.G;
+        const T *q = static_cast<const T *>(a.q) + sp.b * a.q_b + ((int64_t)sp.h * a.G + i) * a.q_h + t * a.q_t + 8 * c;
+#pragma unroll
+        for (int m = 0; m < S::KM; ++m) {
+            uint4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+            if (real) x = *reinterpret_cast<const uint4 *>(q + 32 * m);
+            if (S::kF32 && real) y = *reinterpret_cast<const uint4 *>(q + 32 * m + 4);
+            float sum = 0.0f;
+            if constexpr (S::kF32) {
+                const f32x4 u = __builtin_bit_cast(f32x4, x), v = __builtin_bit_cast(f32x4, y);
+                uint32_t w[4][S::QT];
+                split_pair<S::QT>(u[0], u[1], w[0]);
+                split_pair<S::QT>(u[2], u[3], w[1]);
+                split_pair<S::QT>(v[0], v[1], w[2]);
+                split_pair<S::QT>(v[2], v[3], w[3]);
+#pragma unroll
+                for (int k = 0; k < S::QT; ++k) e[k][m] = uint4{w[0][k], w[1][k], w[2][k], w[3][k]};
+                sum = ((u[0] + u[1]) + (u[2] + u[3])) + ((v[0] + v[1]) + (v[2] + v[3]));
+            } else {
+                e[0][m] = x;
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum += __uint_as_float(w[k] << 16) + __uint_as_float(w[k] & 0xffff0000u);
+            }
+            part[m / S::KG] += sum;
+        }
+        uint32_t t3[S::NG][3];  // bf16 terms of the sums, in the low halves
+#pragma unroll
+        for (int g = 0; g < S::NG; ++g) {
+            part[g] += __shfl_xor(part[g], 16, 64);
+            part[g] += __shfl_xor(part[g], 32, 64);
+            split_pair<3>(part[g], 0.0f, t3[g]);
+        }
+        // contraction indices 8 c .. 8 c + 7 of the product with lo, whose other operand repeats (lo_0, lo_1), (lo_2, lo_3): terms one and two
+        // in lanes c = 0, three in c = 1 (four groups); all three in c = 0 (two groups, one group beside its step)
+        if (S::NG == 4) {
+            const uint32_t a01 = t3[0][0] | t3[1 % S::NG][0] << 16, a23 = t3[2 % S::NG][0] | t3[3 % S::NG][0] << 16;
+            const uint32_t b01 = t3[0][1] | t3[1 % S::NG][1] << 16, b23 = t3[2 % S::NG][1] | t3[3 % S::NG][1] << 16;
+            const uint32_t c01 = t3[0][2] | t3[1 % S::NG][2] << 16, c23 = t3[2 % S::NG][2] | t3[3 % S::NG][2] << 16;
+            sums = c == 0 ? uint4{a01, a23, b01, b23} : c == 1 ? uint4{c01, c23, 0, 0} : uint4{0, 0, 0, 0};
+        } else {
+            uint32_t w[3];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) w[k] = S::NG == 2 ? t3[0][k] | t3[S::NG - 1][k] << 16 : t3[0][k] & 0xffffu;
+            sums = c == 0 ? uint4{w[0], w[1], w[2], 0} : uint4{0, 0, 0, 0};
+        }
+    }
+};
+
+// the other operand of the product with sum(q): slot n's lo, as the queries' sums lie
+template <int NG>
+__device__ __forceinline__ uint4 lo_operand(const Words<NG> &pairs) {
+    if (NG == 4) {
+        const uint32_t a = __builtin_amdgcn_perm(pairs.w[1 % NG], pairs.w[0], 0x05040100u);
+        const uint32_t b = __builtin_amdgcn_perm(pairs.w[3 % NG], pairs.w[2 % NG], 0x05040100u);
+        return uint4{a, b, a, b};
+    }
+    const uint32_t a = NG == 2 ? __builtin_amdgcn_perm(pairs.w[NG - 1], pairs.w[0], 0x05040100u) : pairs.w[0] & 0xffffu;
+    return uint4{a, a, a, a};
+}
+
+// logits (before the factor) of rows 4 c .. 4 c + 3 at slot n of a tile
+template <int D, int GR, typename T>
+__device__ __forceinline__ f32x4 logits(const QueryTile<D, GR, T> &q, const uint4 (&k)[D / 32], const Words<D / GR> &pairs, const uint4 &lo) {
+    using S = QuantShape<D, GR, T>;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    f32x4 s = mma<bf16_t>(q.sums, lo, zero);
+#pragma unroll
+    for (int g = 0; g < S::NG; ++g) {
+        f32x4 x = zero;
+#pragma unroll
+        for (int j = 0; j < S::KG; ++j)
+#pragma unroll
+            for (int k3 = 0; k3 < S::QT; ++k3) x = mma<bf16_t>(q.e[k3][g * S::KG + j], k[g * S::KG + j], x);
+        const float step = step_of(pairs.w[g]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = fmaf(step, x[i], s[i]);
+    }
+    return s;
+}
+
+// What a wave requests ahead: 64 slots
+template <int D, int GR>
+struct KeyRun {
+    Words<D / 32> code[4];
+    Words<D / GR> pair[4];
+    // row: of the pair's first slot; slots from `held` on are read as the last one
+    __device__ __forceinline__ void load(const uint8_t *codes, const uint32_t *pairs, int slot0, int held) {
+        const int n = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int at = slot0 + 16 * t + n, slot = at < held ? at : held - 1;
+            code[t] = load_words<D / 32>(codes + (size_t)(uint32_t)slot * (D / 2) + D / 8 * c);
+            pair[t] = load_words<D / GR>(pairs + (size_t)(uint32_t)slot * (D / GR));
+        }
+    }
+};
+template <int D, int GR>
+struct ValueRun {
+    static constexpr int kPieces = D / 32;  // 16-byte pieces of a row; of a lane
+    uint4 code[kPieces];
+    Words<D / GR> pair[4];
+    __device__ __forceinline__ void load(const uint8_t *codes, const uint32_t *pairs, int slot0, int held) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int at = slot0 + i * (64 / kPieces) + lane / kPieces, slot = at < held ? at : held - 1;
+            code[i] = *reinterpret_cast<const uint4 *>(codes + (size_t)(uint32_t)slot * (D / 2) + 16 * (lane % kPieces));
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int at = slot0 + 16 * t + (lane & 15), slot = at < held ? at : held - 1;
+            pair[t] = load_words<D / GR>(pairs + (size_t)(uint32_t)slot * (D / GR));
+        }
+    }
+};
+
+// weight of sums taken against the reference m in sums against top
+__device__ __forceinline__ float part_weight(float m, float l, float top, float c) {
+    if (m == -INFINITY) return l == 0.0f ? 0.0f : 1.0f;  // (no finite logit: nothing, or NaN that stays)
+    return __builtin_amdgcn_exp2f((m - top) * c);
+}
+
+__device__ __forceinline__ void put(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put(bf16_t *p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
+
+template <int D, int GR, typename T, int RT>
+__global__ __launch_bounds__(256) void quant_attn_kernel(QuantAttnArgs a) {
+    using S = QuantShape<D, GR, T>;
+    constexpr int NG = S::NG;
+    __shared__ __align__(16) uint8_t lds[S::kLds];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
+    const int pair = blockIdx.y, block = a.by_splits.of(blockIdx.x), split = blockIdx.x - block * a.splits;
+    const QuantSpan sp(a, pair);
+    const int row0 = block * 16 * RT;
+    if (row0 >= sp.rows) return;
+    const int row_end = row0 + 16 * RT < sp.rows ? row0 + 16 * RT : sp.rows;
+    const int most = sp.seen(a, row_end - 1), least = sp.seen(a, row0);
+
+    uint8_t *vb = lds + wave * S::kWave;
+    float *pb = reinterpret_cast<float *>(vb + S::kVBytes), *sb = reinterpret_cast<float *>(vb + S::kVBytes + S::kPBytes);
+    // rows of V that the lane gives to the transposed reads: place x of a group of 16 lanes is slot 16 (k & 3) + (k >> 2) with
+    // k = 16 c + 8 (x >> 3) + the place of code x & 7 in an operand
+    const int k_of = 16 * c + (n & 8) + ((n & 1) ? 4 + ((n & 7) >> 1) : (n & 7) >> 1);
+    const uint8_t *v_read = vb + (16 * (k_of & 3) + (k_of >> 2)) * S::kVStride;
+
+    QueryTile<D, GR, T> q[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) q[r].load(a, sp, row0 + 16 * r + n);
+
+    f32x4 acc[RT][S::NT];
+    float m[RT][4], l[RT][4], al[RT][4][NG];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+#pragma unroll
+        for (int i = 0; i < S::NT; ++i) acc[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[r][i] = -INFINITY;
+            l[r][i] = 0.0f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) al[r][i][g] = 0.0f;
+        }
+    }
+
+    const size_t base = (size_t)pair * a.capacity;
+    const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
+    const uint32_t *ks = a.ks + base * NG, *vs = a.vs + base * NG;
+    const int runs = (most + kRun - 1) / kRun, stride = 4 * a.splits;
+    int u = split * 4 + wave;
+    KeyRun<D, GR> key;
+    ValueRun<D, GR> val;
+    if (u < runs) {
+        key.load(kc, ks, u * kRun, sp.held);
+        val.load(vc, vs, u * kRun, sp.held);
+    }
+    for (; u < runs; u += stride) {
+        const bool masked = (u + 1) * kRun > least;
+        const int next = u + stride < runs ? u + stride : u;
+        // ---- logits
+        f32x4 s[RT][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            uint4 k[S::KM];
+#pragma unroll
+            for (int i = 0; i < S::KM; ++i) k[i] = operand_of(key.code[t].w[i]);
+            const uint4 lo = lo_operand<NG>(key.pair[t]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) s[r][t] = logits<D, GR, T>(q[r], k, key.pair[t], lo);
+        }
+        key.load(kc, ks, next * kRun, sp.held);
+        // ---- V to LDS, its steps beside it (group g by lanes c = g)
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < S::KM; ++i) {
+            uint2 *to = reinterpret_cast<uint2 *>(vb + (i * (64 / S::KM) + lane / S::KM) * S::kVStride + 16 * (lane % S::KM));
+            to[0] = uint2{val.code[i].x, val.code[i].y};
+            to[1] = uint2{val.code[i].z, val.code[i].w};
+        }
+        Words<NG> vp[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) vp[t] = val.pair[t];
+        val.load(vc, vs, next * kRun, sp.held);
+        if (masked) {  // slots that are not held: no step, no lo, whatever lies there
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) vp[t].w[g] = u * kRun + 16 * t + n < sp.held ? vp[t].w[g] : 0u;
+        }
+        if (c < NG) {
+            f32x4 st;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                uint32_t w = vp[t].w[0];
+#pragma unroll
+                for (int g = 1; g < NG; ++g) w = c == g ? vp[t].w[g] : w;
+                st[t] = step_of(w);
+            }
+            *reinterpret_cast<f32x4 *>(sb + c * kRun + 4 * n) = st;
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            // ---- softmax against a running reference
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = row0 + 16 * r + 4 * c + i, seen = row < sp.rows ? sp.seen(a, row) : sp.held;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) s[r][t][i] = u * kRun + 16 * t + n < seen ? s[r][t][i] : -INFINITY;
+                }
+            }
+            float top[4];
+            bool raise = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                top[i] = max16(fmaxf(fmaxf(s[r][0][i], s[r][1][i]), fmaxf(s[r][2][i], s[r][3][i])));
+                raise = raise || top[i] > m[r][i];
+            }
+            if (__any(raise)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool up = top[i] > m[r][i];
+                    const float f = up ? __builtin_amdgcn_exp2f((m[r][i] - top[i]) * a.c) : 1.0f;
+                    m[r][i] = up ? top[i] : m[r][i];
+                    l[r][i] *= f;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) al[r][i][g] *= f;
+#pragma unroll
+                    for (int j = 0; j < S::NT; ++j) acc[r][j][i] *= f;
+                }
+            }
+            wave_sync();  // (the probabilities of the tile in front have been read)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float ref = m[r][i] == -INFINITY ? 0.0f : m[r][i];
+                f32x4 p;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    p[t] = __builtin_amdgcn_exp2f((s[r][t][i] - ref) * a.c);
+                    l[r][i] += p[t];
+                }
+                if (masked) {
+                    // a lo of NaN counts only where the row sees it
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) al[r][i][g] = fmaf(p[t], s[r][t][i] == -INFINITY ? 0.0f : lo_of(vp[t].w[g]), al[r][i][g]);
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) al[r][i][g] = fmaf(p[t], lo_of(vp[t].w[g]), al[r][i][g]);
+                }
+                *reinterpret_cast<f32x4 *>(pb + (4 * c + i) * S::kPStride + 4 * n) = p;
+            }
+            wave_sync();
+            // ---- second product: two halves of 32 places
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float *pr = pb + n * S::kPStride + 16 * c + 8 * j;
+                const f32x4 p0 = *reinterpret_cast<const f32x4 *>(pr), p1 = *reinterpret_cast<const f32x4 *>(pr + 4);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const float *sr = sb + g * kRun + 16 * c + 8 * j;
+                    const f32x4 s0 = *reinterpret_cast<const f32x4 *>(sr), s1 = *reinterpret_cast<const f32x4 *>(sr + 4);
+                    uint32_t w[4][S::PT];
+                    split_pair<S::PT>(p0[0] * s0[0], p0[1] * s0[1], w[0]);
+                    split_pair<S::PT>(p0[2] * s0[2], p0[3] * s0[3], w[1]);
+                    split_pair<S::PT>(p1[0] * s1[0], p1[1] * s1[1], w[2]);
+                    split_pair<S::PT>(p1[2] * s1[2], p1[3] * s1[3], w[3]);
+#pragma unroll
+                    for (int x = 0; x < GR / 16; ++x) {
+                        const int tile = g * (GR / 16) + x;
+                        typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+                        const i32x2 code = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(v_read + 8 * tile));
+                        const uint4 v = operand_of((uint32_t)(j ? code.y : code.x));
+#pragma unroll
+                        for (int k = 0; k < S::PT; ++k) acc[r][tile] = mma<bf16_t>(uint4{w[0][k], w[1][k], w[2][k], w[3][k]}, v, acc[r][tile]);
+                    }
+                }
+            }
+        }
+    }
+
+    // ---- the lanes' sums, then the four waves'
+    __syncthreads();
+    float *ob = reinterpret_cast<float *>(lds);  // [wave][row][D]
+    float2 *mlb = reinterpret_cast<float2 *>(lds + 4 * 16 * D * 4);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        if (r > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            l[r][i] = sum16(l[r][i]);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) al[r][i][g] = sum16(al[r][i][g]);
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j) ob[(wave * 16 + 4 * c + i) * D + 16 * j + n] = acc[r][j][i] + al[r][i][j / (GR / 16)];
+            if (n == 0) mlb[wave * 16 + 4 * c + i] = float2{m[r][i], l[r][i]};
+        }
+        __syncthreads();
+        const int x = threadIdx.x >> 4, row = row0 + 16 * r + x;
+        if (row < sp.rows) {
+            float top = -INFINITY, f[4], sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, mlb[w * 16 + x].x);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                f[w] = part_weight(mlb[w * 16 + x].x, mlb[w * 16 + x].y, top, a.c);
+                sum += f[w] * mlb[w * 16 + x].y;
+            }
+            const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
+            if (a.part_ml && n == 0) a.part_ml[part] = float2{top, sum};
+            if (a.splits > 1 || a.out) {
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                const int t = a.by_g.of(row);
+                T *to = static_cast<T *>(a.out) + sp.b * a.out_b + ((int64_t)sp.h * a.G + row - t * a.G) * a.out_h + t * a.out_t;
+#pragma unroll
+                for (int j = 0; j < S::NT; ++j) {
+                    float o = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) o = f[w] == 0.0f ? o : fmaf(f[w], ob[(w * 16 + x) * D + 16 * j + n], o);
+                    if (a.splits > 1) a.part_o[part * D + 16 * j + n] = o;
+                    else put(to + 16 * j + n, o * inv);
+                }
+            }
+        }
+    }
+}
+
+// Second launch of a (sequence, KV head): rows joined over the splits, and what every slot was attended to - the logits once more, now against
+// every row's maximum and sum.
+template <int D, int GR, typename T>
+__global__ __launch_bounds__(256) void quant_finish_kernel(QuantAttnArgs a) {
+    using S = QuantShape<D, GR, T>;
+    constexpr int NG = S::NG, kTiles = S::kF32 ? 4 : 8, kOperands = S::QT * S::KM + 1;
+    __shared__ uint4 ql[kTiles][kOperands][64];
+    __shared__ float2 rl[kTiles * 16];  // (maximum, 1 / sum) of the rows
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
+    const int pair = blockIdx.y;
+    const QuantSpan sp(a, pair);
+    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
+
+    if (a.splits > 1 && a.out) {
+        constexpr int kRows = 256 / D;
+        for (int row = blockIdx.x * kRows + threadIdx.x / D; row < sp.rows; row += gridDim.x * kRows) {
+            const int e = threadIdx.x & (D - 1);
+            const float *o = a.part_o + ((size_t)pair * a.splits * a.n_rows + row) * D + e;
+            float top = -INFINITY, sum = 0.0f, x = 0.0f;
+            for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[(size_t)s * a.n_rows + row].x);
+            for (int s = 0; s < a.splits; ++s) {
+                const float2 v = ml[(size_t)s * a.n_rows + row];
+                const float f = part_weight(v.x, v.y, top, a.c);
+                sum += f * v.y;
+                x = f == 0.0f ? x : fmaf(f, o[(size_t)s * a.n_rows * D], x);
+            }
+            const int t = a.by_g.of(row);
+            T *to = static_cast<T *>(a.out) + sp.b * a.out_b + ((int64_t)sp.h * a.G + row - t * a.G) * a.out_h + t * a.out_t;
+            put(to + e, sum == 0.0f ? 0.0f : x / sum);
+        }
+    }
+    if (!a.weights || sp.rows == 0) return;
+
+    const size_t base = (size_t)pair * a.capacity;
+    const uint8_t *kc = a.kc + base * (D / 2);
+    const uint32_t *ks = a.ks + base * NG;
+    float *weights = a.weights + base;
+    const int runs = (sp.held + kRun - 1) / kRun;
+    if ((int)blockIdx.x * 4 >= runs) return;
+    for (int row0 = 0; row0 < sp.rows; row0 += 16 * kTiles) {
+        const int tiles = (sp.rows - row0 + 15) / 16 < kTiles ? (sp.rows - row0 + 15) / 16 : kTiles;
+        __syncthreads();
+        for (int r = wave; r < tiles; r += 4) {
+            QueryTile<D, GR, T> q;
+            q.load(a, sp, row0 + 16 * r + n);
+#pragma unroll
+            for (int k = 0; k < S::QT; ++k)
+#pragma unroll
+                for (int i = 0; i < S::KM; ++i) ql[r][k * S::KM + i][lane] = q.e[k][i];
+            ql[r][kOperands - 1][lane] = q.sums;
+        }
+        for (int x = threadIdx.x; x < 16 * tiles; x += 256) {
+            const int row = row0 + x;
+            float top = -INFINITY, sum = 0.0f;
+            if (row < sp.rows) {
+                for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[(size_t)s * a.n_rows + row].x);
+                for (int s = 0; s < a.splits; ++s) {
+                    const float2 v = ml[(size_t)s * a.n_rows + row];
+                    sum += part_weight(v.x, v.y, top, a.c) * v.y;
+                }
+            }
+            rl[x] = float2{top == -INFINITY ? 0.0f : top, sum == 0.0f ? 0.0f : 1.0f / sum};
+        }
+        __syncthreads();
+        for (int u = blockIdx.x * 4 + wave; u < runs; u += gridDim.x * 4) {
+            KeyRun<D, GR> key;
+            key.load(kc, ks, u * kRun, sp.held);
+            uint4 k[4][S::KM], lo[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int i = 0; i < S::KM; ++i) k[t][i] = operand_of(key.code[t].w[i]);
+                lo[t] = lo_operand<NG>(key.pair[t]);
+            }
+            float w[4] = {};
+            for (int r = 0; r < tiles; ++r) {
+                QueryTile<D, GR, T> q;
+#pragma unroll
+                for (int k3 = 0; k3 < S::QT; ++k3)
+#pragma unroll
+                    for (int i = 0; i < S::KM; ++i) q.e[k3][i] = ql[r][k3 * S::KM + i][lane];
+                q.sums = ql[r][kOperands - 1][lane];
+                float2 ref[4];
+                int seen[4];
+                const int row = row0 + 16 * r + 4 * c;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    ref[i] = rl[16 * r + 4 * c + i];
+                    seen[i] = row + i < sp.rows ? sp.seen(a, row + i) : 0;
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const f32x4 s = logits<D, GR, T>(q, k[t], key.pair[t], lo[t]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = __builtin_amdgcn_exp2f((s[i] - ref[i].x) * a.c) * ref[i].y;
+                        w[t] += u * kRun + 16 * t + n < seen[i] ? p : 0.0f;
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                w[t] += __shfl_xor(w[t], 16, 64);
+                w[t] += __shfl_xor(w[t], 32, 64);
+                const int slot = u * kRun + 16 * t + n;
+                if (c == t && slot < sp.held) weights[slot] += w[t];
+            }
+        }
+    }
+}
+
+QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
+    QuantPlan p{};
+    const int64_t pairs = (int64_t)c.batch * c.n_kv_heads, rows = (int64_t)q.n_tokens * (q.n_q_heads / c.n_kv_heads);
+    if (pairs == 0 || rows == 0) return p;
+    const int64_t len = q.max_len > 0 && q.max_len < c.capacity ? q.max_len : c.capacity;
+    p.row_tiles = rows > 16 && c.dtype == AIR_BF16 ? 2 : 1;  // (two tiles of fp32 queries, three terms each, do not fit the registers)
+    p.row_blocks = (int)((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
+    const int64_t runs = (len + 4 * kRun - 1) / (4 * kRun), wanted = 512 / (pairs * p.row_blocks);  // two workgroups a CU
+    p.splits = (int)(wanted < 1 ? 1 : wanted < runs ? wanted : runs);
+    if (p.splits > 64) p.splits = 64;
+    if (p.splits > 1 || q.weights) {
+        const size_t cells = (size_t)pairs * p.splits * rows;
+        p.ml_bytes = (cells * sizeof(float2) + 255) / 256 * 256;
+        p.bytes = p.ml_bytes + (p.splits > 1 ? cells * c.head_dim * sizeof(float) : 0);
+        int64_t n = (rows * c.head_dim + 255) / 256;
+        if (q.weights) n = runs;
+        const int64_t most = (1024 + pairs - 1) / pairs;
+        p.finish = (int)(n < most ? n : most);
+    }
+    return p;
+}
+
+template <int D, int GR, typename T>
+static hipError_t run_quant_attn(hipStream_t s, const QuantAttnArgs &a, const QuantPlan &p, int pairs) {
+    const dim3 grid((unsigned)(p.splits * p.row_blocks), (unsigned)pairs);
+    if constexpr (sizeof(T) == 2) {
+        if (p.row_tiles == 2) quant_attn_kernel<D, GR, T, 2><<<grid, 256, 0, s>>>(a);
+    }
+    if (p.row_tiles == 1) quant_attn_kernel<D, GR, T, 1><<<grid, 256, 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.finish == 0) return e;
+    quant_finish_kernel<D, GR, T><<<dim3((unsigned)p.finish, (unsigned)pairs), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const QuantPlan &p, const air_quant_query &q, bool appended, void *workspace) {
+    QuantAttnArgs a;
+    a.kc = static_cast<const uint8_t *>(c.k_codes);
+    a.vc = static_cast<const uint8_t *>(c.v_codes);
+    a.ks = static_cast<const uint32_t *>(c.k_scales);
+    a.vs = static_cast<const uint32_t *>(c.v_scales);
+    a.q = q.q;
+    a.out = q.out;
+    a.part_ml = p.bytes ? static_cast<float2 *>(workspace) : nullptr;
+    a.part_o = p.splits > 1 ? reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.ml_bytes) : nullptr;
+    a.weights = q.weights;
+    a.q_b = q.q_b;
+    a.q_h = q.q_h;
+    a.q_t = q.q_t;
+    a.out_b = q.out_b;
+    a.out_h = q.out_h;
+    a.out_t = q.out_t;
+    a.lens = q.lens;
+    a.counts = q.counts;
+    a.c = logit_factor(q.scale, c.head_dim);
+    a.Hkv = c.n_kv_heads;
+    a.G = q.n_q_heads / c.n_kv_heads;
+    a.n_tokens = q.n_tokens;
+    a.capacity = c.capacity;
+    a.n_rows = q.n_tokens * a.G;
+    a.splits = p.splits;
+    a.causal = q.causal;
+    a.appended = appended;
+    a.by_g = div_by(a.G);
+    a.by_hkv = div_by(a.Hkv);
+    a.by_splits = div_by(p.splits);
+    const int pairs = c.batch * c.n_kv_heads;
+#define AIR_CASE(D, GR, T, F) \
+    if (c.head_dim == D && c.group == GR && c.dtype == F) return run_quant_attn<D, GR, T>(s, a, p, pairs);
+    AIR_CASE(128, 32, bf16_t, AIR_BF16)
+    AIR_CASE(128, 64, bf16_t, AIR_BF16)
+    AIR_CASE(64, 32, bf16_t, AIR_BF16)
+    AIR_CASE(64, 64, bf16_t, AIR_BF16)
+    AIR_CASE(128, 32, float, AIR_F32)
+    AIR_CASE(128, 64, float, AIR_F32)
+    AIR_CASE(64, 32, float, AIR_F32)
+    AIR_CASE(64, 64, float, AIR_F32)
+#undef AIR_CASE
+    return hipErrorInvalidValue;
+}
+
+}  // namespace air

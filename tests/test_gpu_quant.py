@@ -1,0 +1,394 @@
+"""Rows in 4 bits and attention over them against the definitions in fp64, with bounds derived from the roundings they make."""
+import math
+
+import pytest
+
+from quant_util import attention, unpacked, values_of
+
+pytestmark = pytest.mark.gpu
+
+KINDS = [(dt, d, g) for dt in ("bf16", "f32") for d in (64, 128) for g in (32, 64)]
+
+
+def _type(dtype):
+    import torch
+
+    return torch.bfloat16 if dtype == "bf16" else torch.float32
+
+
+def _ints(x):
+    import torch
+
+    return torch.tensor(x, dtype=torch.int32, device="cuda:0")
+
+
+def _randn(seed, *shape):
+    import torch
+
+    return torch.randn(shape, generator=torch.Generator(device="cuda:0").manual_seed(seed), device="cuda:0")
+
+
+def _new(A, B, H, cap, d, dtype, group):
+    """A cache whose memory holds what no call may look at: NaN steps, all codes set."""
+    c = A.QuantCache(B, H, cap, d, A.AIR_BF16 if dtype == "bf16" else A.AIR_F32, group=group)
+    for p in c.planes[:2]:
+        p.fill_(255)
+    for p in c.planes[2:]:
+        p.fill_(math.nan)
+    return c
+
+
+def _filled(A, B, H, cap, d, dtype, group, held, seed, spread=1.0):
+    c = _new(A, B, H, cap, d, dtype, group)
+    n = max(held)
+    if n:
+        offset = 2.0 * _randn(seed + 2, 1, H, 1, d) * (_randn(seed + 3, 1, H, 1, d) > 1.5)
+        k, v = ((_randn(seed + i, B, H, n, d) * spread + (offset if i == 0 else 0.5)).to(_type(dtype)) for i in range(2))
+        A.air_quant_append(c, k, v, counts=_ints(held))
+    return c
+
+
+# ---- rows ------------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d,group", KINDS)
+@pytest.mark.parametrize("order", ["head", "token", "broadcast"])
+def test_rows_there_and_back(dtype, d, group, order):
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    dt, B, H, T, cap = _type(dtype), 3, 2, 37, 60
+    x = [_randn(i, B, H, T, d) * torch.exp(_randn(9 + i, B, H, T, 1)) + _randn(20 + i, 1, H, 1, d) for i in range(2)]
+    x[0][0, 0, 3] = 0.0
+    x[0][0, 1, 4] = 7.25
+    x[1][1, 0, 5, : group] = -3e-39  # a step below 2^-120
+    x[1][1, 1, 6, 1] = 5e37
+    x[0][2, 0, 0, : group] = torch.arange(group, device="cuda:0") % 16  # whole codes
+    x[0][2, 0, 1, : group] = (torch.arange(group, device="cuda:0") % 31) / 2  # ties
+    x = [y.to(dt) for y in x]
+    if order == "token":
+        both = torch.cat(x, dim=1).transpose(1, 2).contiguous().transpose(1, 2)
+        x = [both[:, :H], both[:, H:]]
+    elif order == "broadcast":
+        x = [y[:1, :, :1].expand(B, H, T, d) for y in x]
+    lens, counts = [0, 23, 5], [37, 30, 0]
+    cache = _new(A, B, H, cap, d, dtype, group)
+    A.air_quant_append(cache, *x, lens=_ints(lens), counts=_ints(counts))
+    out = [torch.full((B, T, H, d), 42.0, dtype=dt, device="cuda:0").transpose(1, 2) for _ in range(2)]
+    A.air_quant_read(cache, *out, starts=_ints(lens), counts=_ints(counts))
+    raw = unpacked(cache)
+    for y, o, (lo, up) in zip(x, out, raw):
+        want, step = values_of(y, group)
+        for b, (at, n) in enumerate(zip(lens, counts)):
+            assert torch.equal((lo + up)[b, :, at:at + n], want[b, :, :n])  # the memory, as the header has it
+            assert torch.equal(o[b, :, :n].double(), want[b, :, :n].float().to(dt).double())
+            assert bool((o[b, :, n:] == 42.0).all())
+            assert bool(torch.isnan(lo[b, :, :at]).all()) and bool(torch.isnan(lo[b, :, at + n:]).all())  # other slots untouched
+            far = (want[b, :, :n] - y[b, :, :n].double()).abs()
+            assert bool((far <= step[b, :, :n] / 2 + y[b, :, :n].double().abs().amax(-1, keepdim=True) * 2.0 ** -22 + 15 * 2.0 ** -120).all())
+    one = torch.full_like(out[1], 42.0)
+    A.air_quant_read(cache, None, one, starts=_ints(lens), counts=_ints(counts))
+    assert torch.equal(one, out[1])
+
+
+@pytest.mark.parametrize("dtype,d,group", KINDS)
+def test_rows_that_are_not_numbers(dtype, d, group):
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    x = [_randn(i, 1, 1, 6, d) for i in range(2)]
+    for i, bad in enumerate((math.nan, math.inf, -math.inf, 2.0 ** 126, -2.0 ** 127)):
+        x[i % 2][0, 0, i, 5] = bad
+    x = [y.to(_type(dtype)) for y in x]
+    cache = _new(A, 1, 1, 6, d, dtype, group)
+    A.air_quant_append(cache, *x)
+    out = [torch.empty_like(y) for y in x]
+    A.air_quant_read(cache, *out)
+    for y, o in zip(x, out):
+        want, _ = values_of(y, group)
+        assert torch.equal(torch.isnan(o), torch.isnan(want))
+        assert torch.equal(torch.nan_to_num(o.double()), torch.nan_to_num(want.float().to(o.dtype).double()))
+
+
+def test_rows_outside_the_capacity_are_dropped():
+    """Lengths and counts from device memory that make no sense reach no memory outside the cache."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    x = [_randn(i, 4, 2, 9, 64) for i in range(2)]
+    cache = _new(A, 4, 2, 12, 64, "f32", 32)
+    pos, w = torch.full((4, 2, 12), -7, dtype=torch.int32, device="cuda:0"), torch.full((4, 2, 12), 3.0, device="cuda:0")
+    lens, counts = [8, -3, 2 ** 31 - 1, 12], [9, 2 ** 31 - 1, 9, -5]
+    A.air_quant_append(cache, *x, lens=_ints(lens), counts=_ints(counts), positions=pos, first_positions=_ints([100, 200, 300, 400]), weights=w)
+    (lo, up), _ = unpacked(cache)
+    want, _ = values_of(x[0], 32)
+    got = lo + up
+    assert torch.equal(got[0, :, 8:], want[0, :, :4]) and torch.equal(got[1, :, :6], want[1, :, 3:])
+    assert bool(torch.isnan(got[0, :, :8]).all()) and bool(torch.isnan(got[1, :, 6:]).all()) and bool(torch.isnan(got[2:]).all())
+    assert pos[0, 1].tolist() == [-7] * 8 + [100, 101, 102, 103] and pos[1, 0].tolist() == [203, 204, 205, 206, 207, 208] + [-7] * 6
+    assert bool((pos[2:] == -7).all()) and bool((w[2:] == 3.0).all())
+    assert w[0, 0].tolist() == [3.0] * 8 + [0.0] * 4 and w[1, 1].tolist() == [0.0] * 6 + [3.0] * 6
+    out = [torch.full_like(y, 42.0) for y in x]
+    A.air_quant_read(cache, *out, starts=_ints(lens), counts=_ints(counts))
+    assert torch.equal(out[0][0, :, :4].double(), want[0, :, :4].float().double()) and bool((out[0][0, :, 4:] == 42.0).all())
+    assert torch.equal(out[0][1, :, 3:].double(), want[1, :, 3:].float().double()) and bool((out[0][1, :, :3] == 42.0).all())
+    assert bool((out[0][2:] == 42.0).all())
+
+
+# ---- attention -------------------------------------------------------------------------------------------------------------------
+def _check(A, cache, q, held, counts, causal, seed=0, weigh=True, scale=0.0, lens=None, k=None, v=None, with_out=True, **kw):
+    """One call against the definition; `held`: slots after it."""
+    import torch
+
+    B, _, T, d = q.shape
+    out = torch.full((B, T, q.shape[1], d), 42.0, dtype=q.dtype, device="cuda:0").transpose(1, 2)
+    w0 = torch.exp(_randn(seed + 50, B, cache.n_kv_heads, cache.capacity))
+    w = w0.clone()
+    A.air_quant_attn(cache, q, out if with_out else None, lens=_ints(held if lens is None else lens), counts=_ints(counts), causal=causal, scale=scale,
+                     weights=w if weigh else None, k=k, v=v, **kw)
+    torch.cuda.synchronize()
+    for b, (o, bound, ww, wb) in enumerate(attention(cache, q, held, counts, causal, scale or None)):
+        c, n = counts[b], held[b]
+        if with_out:
+            far = (out[b, :, :c].double() - o).abs()
+            assert bool((far <= bound).all()), f"sequence {b} ({c} over {n}): {(far - bound).max().item()} above its bound, {far.max().item()} off"
+            assert bool((out[b, :, c:] == 42.0).all())
+        if weigh:
+            was = w0[b].double()
+            if lens is not None and lens[b] < n:
+                was[:, lens[b]:n] = 0.0
+            far = (w[b, :, :n].double() - was[:, :n] - ww).abs()
+            assert bool((far <= wb + (was[:, :n] + ww) * 2.0 ** -23).all()), f"sequence {b}: weights {far.max().item()} off"
+            assert torch.equal(w[b, :, n:], w0[b, :, n:])
+    return out, w
+
+
+@pytest.mark.parametrize("dtype,d,group", KINDS)
+@pytest.mark.parametrize("hq,hkv", [(4, 4), (7, 1), (6, 2), (17, 1)])
+def test_tokens(dtype, d, group, hq, hkv):
+    """A token a sequence over none, one and many slots, at and around the runs' borders."""
+    import paper_2503_23956_amd as A
+
+    held = [1, 0, 2, 15, 16, 17, 63, 64, 65, 255, 256, 257, 700, 1031]
+    B, cap = len(held), 1040
+    cache = _filled(A, B, hkv, cap, d, dtype, group, held, 1)
+    q = (_randn(7, B, hq, 1, d) * 2.0).to(_type(dtype))
+    _check(A, cache, q, held, [1] * B, True)
+    _check(A, cache, q, held, [1] * B, False, weigh=False, max_len=1031)
+    _check(A, cache, q, held, [1, 1, 0, 1] * 3 + [0, 1], True, with_out=False)
+
+
+@pytest.mark.parametrize("dtype,d,group", KINDS)
+@pytest.mark.parametrize("causal", [False, True])
+def test_windows_and_pieces(dtype, d, group, causal):
+    """Many queries, more of them than slots, ragged counts, one of the batch empty."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    held, counts, hq, hkv = [300, 70, 5, 64, 0, 129], [33, 70, 21, 1, 3, 0], 6, 2
+    cache = _filled(A, 6, hkv, 311, d, dtype, group, held, 3)
+    q = (_randn(8, 6, 70, hq, d) * 2.0).to(_type(dtype)).transpose(1, 2)
+    out, w = _check(A, cache, q, held, counts, causal, seed=4)
+    if causal:
+        assert bool((out[2, :, :16] == 0.0).all())  # queries in front of every slot
+    again, w2 = _check(A, cache, q, held, counts, causal, seed=4)
+    assert torch.equal(out, again) and torch.equal(w, w2)
+
+
+@pytest.mark.parametrize("dtype,d,group", KINDS)
+def test_append_and_attend(dtype, d, group):
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    lens, counts, hq, hkv, T = [130, 0, 63, 500], [3, 7, 1, 0], 8, 2, 7
+    held = [a + b for a, b in zip(lens, counts)]
+    cache = _filled(A, 4, hkv, 510, d, dtype, group, lens, 5)
+    q = (_randn(9, 4, hq, T, d) * 2.0).to(_type(dtype))
+    k, v = (_randn(10 + i, 4, hkv, T, d).to(_type(dtype)) for i in range(2))
+    pos = torch.full((4, hkv, 510), -1, dtype=torch.int32, device="cuda:0")
+    _check(A, cache, q, held, counts, True, lens=lens, k=k, v=v, positions=pos, first_positions=_ints([1000, 0, 5, 9]))
+    (lo, up), (vlo, vup) = unpacked(cache)
+    for x, got in ((k, lo + up), (v, vlo + vup)):
+        want, _ = values_of(x, group)
+        for b, (at, n) in enumerate(zip(lens, counts)):
+            assert torch.equal(got[b, :, at:at + n], want[b, :, :n])
+    assert pos[0, 1, 128:135].tolist() == [-1, -1, 1000, 1001, 1002, -1, -1] and pos[3].max().item() == -1
+
+
+@pytest.mark.parametrize("dtype,d,group", KINDS)
+def test_slots_that_are_not_seen_count_for_nothing(dtype, d, group):
+    """Groups of NaN behind the causal border, and behind the slots held, reach no row; those that a row sees do, however little they weigh."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    held, c = 140, 20
+    cache = _filled(A, 2, 2, 150, d, dtype, group, [held, held], 6)
+    cache.planes[2][0, :, held - 1] = math.nan  # the last key of sequence 0, which the last query alone sees
+    cache.planes[3][1, :, held - 3, 0] = math.nan  # lo of the first group of a value of sequence 1
+    q = (_randn(12, 2, 4, c, d) * 2.0).to(_type(dtype))
+    out = torch.zeros_like(q)
+    w = torch.zeros((2, 2, 150), device="cuda:0")
+    A.air_quant_attn(cache, q, out, lens=_ints([held, held]), counts=_ints([c, c]), weights=w)
+    nan = torch.isnan(out)
+    assert bool(nan[0, :, c - 1].all()) and not bool(nan[0, :, : c - 1].any())
+    assert bool(nan[1, :, c - 3:, :group].all()) and not bool(nan[1, :, c - 3:, group:].any()) and not bool(nan[1, :, : c - 3].any())
+    assert bool(torch.isnan(w[0, :, :held]).all()) and not bool(torch.isnan(w[1]).any())
+    # a weight of 0 (the logits lie a thousand apart) times a value of NaN
+    one = _filled(A, 1, 1, 64, d, dtype, group, [64], 7, spread=0.01)
+    k = torch.zeros((1, 1, 1, d), dtype=_type(dtype), device="cuda:0")
+    k[..., 0] = 1000.0
+    A.air_quant_append(one, k, k, lens=_ints([10]))
+    one.planes[3][0, 0, 20] = math.nan
+    q1 = torch.zeros((1, 1, 1, d), dtype=_type(dtype), device="cuda:0")
+    q1[..., 0] = 100.0
+    o1 = torch.zeros_like(q1)
+    A.air_quant_attn(one, q1, o1, lens=_ints([64]))
+    assert bool(torch.isnan(o1).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_and_large_logits(dtype):
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    cache = _filled(A, 1, 2, 400, 128, dtype, 32, [390], 8)
+    q = (_randn(13, 1, 4, 3, 128) * 2.0).to(_type(dtype))
+    _check(A, cache, q, [390], [3], True, scale=0.7)
+    _check(A, cache, q, [390], [3], True, scale=1e-6)
+    # equal logits of any size share the weight equally
+    same = _new(A, 1, 1, 100, 64, dtype, 32)
+    k = torch.full((1, 1, 100, 64), 3.0, dtype=_type(dtype), device="cuda:0")
+    v = _randn(14, 1, 1, 100, 64).to(_type(dtype))
+    A.air_quant_append(same, k, v)
+    big = torch.full((1, 1, 1, 64), 1e6, dtype=_type(dtype), device="cuda:0")
+    o, w = torch.zeros_like(big), torch.zeros((1, 1, 100), device="cuda:0")
+    A.air_quant_attn(same, big, o, lens=_ints([100]), weights=w)
+    assert float((w - 0.01).abs().max()) < 1e-8
+    want = values_of(v, 32)[0].mean(2)
+    assert float((o.double()[0, :, 0] - want[0]).abs().max()) < 2.0 ** -8 * float(want.abs().max()) + 1e-6
+
+
+def test_lengths_that_make_no_sense():
+    """Lengths outside the capacity are clamped: no access leaves the cache."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    cache = _filled(A, 4, 2, 90, 64, "bf16", 32, [90] * 4, 9)
+    q = _randn(15, 4, 4, 2, 64).bfloat16()
+    outs = []
+    for lens in ([90, 0, 90, 0], [91, -1, 2 ** 31 - 1, -2 ** 31]):
+        out, w = torch.full_like(q, 42.0), torch.zeros((4, 2, 90), device="cuda:0")
+        A.air_quant_attn(cache, q, out, lens=_ints(lens), causal=False, weights=w)
+        outs.append((out, w))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    assert bool((outs[0][0][1] == 0).all()) and bool((outs[0][1][3] == 0).all())
+    out = torch.full_like(q, 42.0)
+    A.air_quant_attn(cache, q, out, lens=_ints([90] * 4), counts=_ints([-1, 2 ** 31 - 1, 0, 1]), causal=False)
+    assert bool((out[0] == 42.0).all()) and torch.equal(out[1], _check(A, cache, q, [90] * 4, [2] * 4, False)[0][1])
+    assert bool((out[2] == 42.0).all()) and bool((out[3, :, 1] == 42.0).all())
+
+
+def test_more_than_32_bits_of_cache():
+    """Codes of 6.4 GB a tensor, a capacity of 2^22: the last sequence's last slots."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    cap, H = 1 << 22, 24
+    cache = A.QuantCache(1, H, cap, 128)
+    at = cap - 200
+    k, v = (_randn(i, 1, H, 200, 128).bfloat16() for i in range(2))
+    A.air_quant_append(cache, k, v, lens=_ints([at]))
+    got = [torch.empty_like(k) for _ in range(2)]
+    A.air_quant_read(cache, *got, starts=_ints([at]))
+    for x, o in zip((k, v), got):
+        assert torch.equal(o.double(), values_of(x, 32)[0].float().bfloat16().double())
+    # the slots in front weigh nothing: their keys lie a thousand lower
+    for p in cache.planes[:2]:
+        p[0, H - 1, :at] = 0
+    cache.planes[2][0, H - 1, :at] = 0.0
+    cache.planes[2][0, H - 1, :at, 0] = -1000.0
+    cache.planes[3][0, H - 1, :at] = 0.0
+    small = A.QuantCache(1, H, 200, 128)
+    A.air_quant_append(small, k, v)
+    q = _randn(3, 1, H, 1, 128).bfloat16()
+    q[..., 0] = 8.0
+    a, b = torch.zeros_like(q), torch.zeros_like(q)
+    for p in cache.planes[2:]:
+        p[0, : H - 1] = 0.0
+    A.air_quant_attn(cache, q, a, lens=_ints([cap]))
+    A.air_quant_attn(small, q, b, lens=_ints([200]))
+    assert float((a[0, -1].double() - b[0, -1].double()).abs().max()) < 2.0 ** -7 * float(b[0, -1].abs().max())
+
+
+# ---- streams, graphs, workspaces ------------------------------------------------------------------------------------------------------
+def test_other_streams_workspaces_and_two_calls_at_once():
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    cache = _filled(A, 2, 2, 3000, 128, "bf16", 32, [2900, 1500], 10)
+    qs = [_randn(16 + i, 2, 14, 1, 128).bfloat16() for i in range(2)]
+    want = [torch.zeros_like(q) for q in qs]
+    lens = _ints([2900, 1500])
+    for q, o in zip(qs, want):
+        A.air_quant_attn(cache, q, o, lens=lens)
+    calls, outs = [], [torch.zeros_like(q) for q in qs]
+    for q, o in zip(qs, outs):
+        calls.append(A.prepare_quant_attn(cache, q, o, lens=lens))
+    assert calls[0].workspace_bytes > 0
+    with pytest.raises(A.AirError):
+        calls[0](stream=torch.cuda.Stream().cuda_stream)
+    with pytest.raises(A.AirError):
+        calls[0](workspace=torch.empty(calls[0].workspace_bytes - 1, dtype=torch.uint8, device="cuda:0"))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [torch.empty(c.workspace_bytes, dtype=torch.uint8, device="cuda:0") for c in calls]
+    for _ in range(20):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for c, s, ws in zip(calls, streams, spaces):
+            c(stream=s.cuda_stream, workspace=ws)
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_recorded_steps_grow_with_the_lengths(dtype):
+    """One recorded step, replayed while lengths in device memory advance, two graphs on one workspace; every replay against the eager call."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    B, hq, hkv, d, cap = 2, 8, 2, 64, 700
+    a, b = (_filled(A, B, hkv, cap, d, dtype, 32, [600, 3], 11) for _ in range(2))
+    dt = _type(dtype)
+    q, k, v = (torch.zeros((B, h, 1, d), dtype=dt, device="cuda:0") for h in (hq, hkv, hkv))
+    lens = {c: _ints([600, 3]) for c in (a, b)}
+    out = {c: torch.zeros((B, hq, 1, d), dtype=dt, device="cuda:0") for c in (a, b)}
+    w = {c: torch.zeros((B, hkv, cap), device="cuda:0") for c in (a, b)}
+    calls = {c: A.prepare_quant_attn(c, q, out[c], lens=lens[c], k=k, v=v, weights=w[c]) for c in (a, b)}
+    space = torch.empty(calls[a].workspace_bytes, dtype=torch.uint8, device="cuda:0")
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    torch.cuda.synchronize()
+    for g in graphs:
+        with torch.cuda.graph(g):
+            calls[a](workspace=space)
+            lens[a].add_(1)
+    for step in range(12):
+        for i, x in enumerate((q, k, v)):
+            x.copy_(_randn(100 * step + i, *x.shape).to(dt))
+        graphs[step % 2].replay()
+        calls[b]()
+        lens[b].add_(1)
+        torch.cuda.synchronize()
+        assert torch.equal(out[a], out[b]) and torch.equal(w[a], w[b]) and torch.equal(lens[a], lens[b])
+    assert lens[a].tolist() == [612, 15]
