@@ -8,7 +8,7 @@
 // of V go to LDS as they lie in memory and come back transposed (ds_read_b64_tr_b4: 16 slots of one element per lane), the places' order
 // and that of the codes in an operand in the lanes' row addresses.  sum_j p_j lo_j is kept per lane, for its own slots.
 //
-// Waves share nothing until their ends: each deals itself every (4 splits)-th run of 64 slots, requested one run ahead, and the four
+// Waves share nothing until their ends: each deals itself every (4 splits)-th run of 64 slots, K requested one run ahead, and the four
 // partial results of a workgroup are joined in LDS.
 #include "air_device.h"
 #include "air_internal.h"
@@ -217,9 +217,14 @@ __device__ __forceinline__ float part_weight(float m, float l, float top, float 
 
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16_t *p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
+__device__ __forceinline__ void put4(float *p, const f32x4 &v) { *reinterpret_cast<f32x4 *>(p) = v; }
+__device__ __forceinline__ void put4(bf16_t *p, const f32x4 &v) {
+    const bf16x2 a = {(__bf16)v[0], (__bf16)v[1]}, b = {(__bf16)v[2], (__bf16)v[3]};
+    *reinterpret_cast<uint2 *>(p) = uint2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+}
 
 template <int D, int GR, typename T, int RT>
-__global__ __launch_bounds__(256) void quant_attn_kernel(QuantAttnArgs a) {
+__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantAttnArgs a) {
     using S = QuantShape<D, GR, T>;
     constexpr int NG = S::NG;
     __shared__ __align__(16) uint8_t lds[S::kLds];
@@ -263,12 +268,10 @@ __global__ __launch_bounds__(256) void quant_attn_kernel(QuantAttnArgs a) {
     const int runs = (most + kRun - 1) / kRun, stride = 4 * a.splits;
     int u = split * 4 + wave;
     KeyRun<D, GR> key;
-    ValueRun<D, GR> val;
-    if (u < runs) {
-        key.load(kc, ks, u * kRun, sp.held);
-        val.load(vc, vs, u * kRun, sp.held);
-    }
+    if (u < runs) key.load(kc, ks, u * kRun, sp.held);
     for (; u < runs; u += stride) {
+        ValueRun<D, GR> val;  // (on its way during the first product)
+        val.load(vc, vs, u * kRun, sp.held);
         const bool masked = (u + 1) * kRun > least;
         const int next = u + stride < runs ? u + stride : u;
         // ---- logits
@@ -281,6 +284,7 @@ __global__ __launch_bounds__(256) void quant_attn_kernel(QuantAttnArgs a) {
             const uint4 lo = lo_operand<NG>(key.pair[t]);
 #pragma unroll
             for (int r = 0; r < RT; ++r) s[r][t] = logits<D, GR, T>(q[r], k, key.pair[t], lo);
+            if (NG == 4) __builtin_amdgcn_sched_barrier(0);  // (operands of all four tiles at once do not fit the registers)
         }
         key.load(kc, ks, next * kRun, sp.held);
         // ---- V to LDS, its steps beside it (group g by lanes c = g)
@@ -291,10 +295,7 @@ __global__ __launch_bounds__(256) void quant_attn_kernel(QuantAttnArgs a) {
             to[0] = uint2{val.code[i].x, val.code[i].y};
             to[1] = uint2{val.code[i].z, val.code[i].w};
         }
-        Words<NG> vp[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) vp[t] = val.pair[t];
-        val.load(vc, vs, next * kRun, sp.held);
+        Words<NG> (&vp)[4] = val.pair;
         if (masked) {  // slots that are not held: no step, no lo, whatever lies there
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -443,46 +444,110 @@ __global__ __launch_bounds__(256) void quant_attn_kernel(QuantAttnArgs a) {
 }
 
 // Second launch of a (sequence, KV head): rows joined over the splits, and what every slot was attended to - the logits once more, now against
-// every row's maximum and sum.
-template <int D, int GR, typename T>
-__global__ __launch_bounds__(256) void quant_finish_kernel(QuantAttnArgs a) {
+// every row's maximum and sum.  The partial results of a row are requested all at once: a lane per split for (maximum, sum), and
+// for the outputs D / 4 lanes a split.
+template <int D, typename T>
+__device__ __forceinline__ void join_rows(const QuantAttnArgs &a, const QuantSpan &sp, int pair, float4 *lds) {
+    constexpr int kLanes = D / 4, kPlaces = 256 / kLanes;  // places: splits of a row side by side, and rows
+    int groups = 1;
+    while (groups < a.splits && groups < kPlaces) groups *= 2;
+    const int place = threadIdx.x / kLanes, x = threadIdx.x % kLanes, group = place & (groups - 1), lane = threadIdx.x & 63;
+    const int rows = kPlaces / groups;
+    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
+    for (int first = blockIdx.x * rows; first < sp.rows; first += gridDim.x * rows) {
+        const int row = first + place / groups, r = row < sp.rows ? row : sp.rows - 1;
+        const float4 *o = reinterpret_cast<const float4 *>(a.part_o + ((size_t)pair * a.splits * a.n_rows + r) * D) + x;
+        const size_t step = (size_t)a.n_rows * (D / 4);
+        float4 sum = {0.f, 0.f, 0.f, 0.f};
+        float top = -INFINITY, l = 0.0f;
+        float4 part[8];
+        float2 v[8];
+        for (int s0 = group; s0 < a.splits; s0 += 8 * groups) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int s = s0 + k * groups;
+                v[k] = float2{-INFINITY, 0.f};
+                part[k] = float4{0.f, 0.f, 0.f, 0.f};
+                if (s < a.splits) {
+                    v[k] = ml[(size_t)s * a.n_rows + r];
+                    part[k] = o[s * step];
+                }
+            }
+            float most = top;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) most = fmaxf(most, v[k].x);
+            const float f0 = part_weight(top, l, most, a.c);
+            sum.x *= f0, sum.y *= f0, sum.z *= f0, sum.w *= f0;
+            l *= f0;
+            top = most;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float f = part_weight(v[k].x, v[k].y, top, a.c);
+                l = fmaf(f, v[k].y, l);
+                sum.x = fmaf(f, part[k].x, sum.x);
+                sum.y = fmaf(f, part[k].y, sum.y);
+                sum.z = fmaf(f, part[k].z, sum.z);
+                sum.w = fmaf(f, part[k].w, sum.w);
+            }
+        }
+        if (groups > 1) {
+            __syncthreads();
+            lds[threadIdx.x] = sum;
+            float2 *lds_ml = reinterpret_cast<float2 *>(lds + 256);
+            if (x == 0) lds_ml[place] = float2{top, l};
+            __syncthreads();
+            if (group == 0) {
+                float most = top;
+                for (int k = 1; k < groups; ++k) most = fmaxf(most, lds_ml[place + k].x);
+                const float f0 = part_weight(top, l, most, a.c);
+                sum.x *= f0, sum.y *= f0, sum.z *= f0, sum.w *= f0;
+                l *= f0;
+                for (int k = 1; k < groups; ++k) {
+                    const float2 w = lds_ml[place + k];
+                    const float4 y = lds[threadIdx.x + k * kLanes];
+                    const float f = part_weight(w.x, w.y, most, a.c);
+                    l = fmaf(f, w.y, l);
+                    sum.x = fmaf(f, y.x, sum.x);
+                    sum.y = fmaf(f, y.y, sum.y);
+                    sum.z = fmaf(f, y.z, sum.z);
+                    sum.w = fmaf(f, y.w, sum.w);
+                }
+            }
+        }
+        if (group == 0 && row < sp.rows) {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const int t = a.by_g.of(row);
+            T *to = static_cast<T *>(a.out) + sp.b * a.out_b + ((int64_t)sp.h * a.G + row - t * a.G) * a.out_h + t * a.out_t + 4 * x;
+            put4(to, f32x4{sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv});
+        }
+    }
+}
+
+template <int D, int GR, typename T, int TILES>
+__global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
     using S = QuantShape<D, GR, T>;
-    constexpr int NG = S::NG, kTiles = S::kF32 ? 4 : 8, kOperands = S::QT * S::KM + 1;
-    __shared__ uint4 ql[kTiles][kOperands][64];
-    __shared__ float2 rl[kTiles * 16];  // (maximum, 1 / sum) of the rows
+    constexpr int NG = S::NG, kOperands = S::QT * S::KM + 1;
+    __shared__ uint4 ql[TILES][kOperands][64];
+    __shared__ float2 rl[TILES * 16];  // (maximum, 1 / sum) of the rows
+    __shared__ float4 jl[256 + 8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
     const int pair = blockIdx.y;
     const QuantSpan sp(a, pair);
-    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
-
-    if (a.splits > 1 && a.out) {
-        constexpr int kRows = 256 / D;
-        for (int row = blockIdx.x * kRows + threadIdx.x / D; row < sp.rows; row += gridDim.x * kRows) {
-            const int e = threadIdx.x & (D - 1);
-            const float *o = a.part_o + ((size_t)pair * a.splits * a.n_rows + row) * D + e;
-            float top = -INFINITY, sum = 0.0f, x = 0.0f;
-            for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[(size_t)s * a.n_rows + row].x);
-            for (int s = 0; s < a.splits; ++s) {
-                const float2 v = ml[(size_t)s * a.n_rows + row];
-                const float f = part_weight(v.x, v.y, top, a.c);
-                sum += f * v.y;
-                x = f == 0.0f ? x : fmaf(f, o[(size_t)s * a.n_rows * D], x);
-            }
-            const int t = a.by_g.of(row);
-            T *to = static_cast<T *>(a.out) + sp.b * a.out_b + ((int64_t)sp.h * a.G + row - t * a.G) * a.out_h + t * a.out_t;
-            put(to + e, sum == 0.0f ? 0.0f : x / sum);
-        }
-    }
-    if (!a.weights || sp.rows == 0) return;
-
+    if (sp.rows == 0) return;
     const size_t base = (size_t)pair * a.capacity;
     const uint8_t *kc = a.kc + base * (D / 2);
     const uint32_t *ks = a.ks + base * NG;
-    float *weights = a.weights + base;
-    const int runs = (sp.held + kRun - 1) / kRun;
+    const int runs = a.weights ? (sp.held + kRun - 1) / kRun : 0, stride = gridDim.x * 4;
+    const int u0 = blockIdx.x * 4 + wave;
+    KeyRun<D, GR> key;
+    if (u0 < runs) key.load(kc, ks, u0 * kRun, sp.held);
+    if (a.splits > 1 && a.out) join_rows<D, T>(a, sp, pair, jl);
     if ((int)blockIdx.x * 4 >= runs) return;
-    for (int row0 = 0; row0 < sp.rows; row0 += 16 * kTiles) {
-        const int tiles = (sp.rows - row0 + 15) / 16 < kTiles ? (sp.rows - row0 + 15) / 16 : kTiles;
+
+    float *weights = a.weights + base;
+    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
+    for (int row0 = 0; row0 < sp.rows; row0 += 16 * TILES) {
+        const int left = (sp.rows - row0 + 15) / 16, tiles = left < TILES ? left : TILES;
         __syncthreads();
         for (int r = wave; r < tiles; r += 4) {
             QueryTile<D, GR, T> q;
@@ -493,29 +558,35 @@ __global__ __launch_bounds__(256) void quant_finish_kernel(QuantAttnArgs a) {
                 for (int i = 0; i < S::KM; ++i) ql[r][k * S::KM + i][lane] = q.e[k][i];
             ql[r][kOperands - 1][lane] = q.sums;
         }
-        for (int x = threadIdx.x; x < 16 * tiles; x += 256) {
+        for (int x = threadIdx.x >> 4; x < 16 * tiles; x += 16) {  // 16 lanes a row
             const int row = row0 + x;
+            float2 v[4];
             float top = -INFINITY, sum = 0.0f;
-            if (row < sp.rows) {
-                for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[(size_t)s * a.n_rows + row].x);
-                for (int s = 0; s < a.splits; ++s) {
-                    const float2 v = ml[(size_t)s * a.n_rows + row];
-                    sum += part_weight(v.x, v.y, top, a.c) * v.y;
-                }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[k] = float2{-INFINITY, 0.f};
+                if (n + 16 * k < a.splits && row < sp.rows) v[k] = ml[(size_t)(n + 16 * k) * a.n_rows + row];
+                top = fmaxf(top, v[k].x);
             }
-            rl[x] = float2{top == -INFINITY ? 0.0f : top, sum == 0.0f ? 0.0f : 1.0f / sum};
+            top = max16(top);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top, a.c) * v[k].y;
+            sum = sum16(sum);
+            if (n == 0) rl[x] = float2{top == -INFINITY ? 0.0f : top, sum == 0.0f ? 0.0f : 1.0f / sum};
         }
         __syncthreads();
-        for (int u = blockIdx.x * 4 + wave; u < runs; u += gridDim.x * 4) {
-            KeyRun<D, GR> key;
-            key.load(kc, ks, u * kRun, sp.held);
+        for (int u = u0; u < runs; u += stride) {
             uint4 k[4][S::KM], lo[4];
+            Words<NG> pairs[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
 #pragma unroll
                 for (int i = 0; i < S::KM; ++i) k[t][i] = operand_of(key.code[t].w[i]);
                 lo[t] = lo_operand<NG>(key.pair[t]);
+                pairs[t] = key.pair[t];
             }
+            // the run after this one; behind the last one the first again, for the next rows
+            key.load(kc, ks, (u + stride < runs ? u + stride : u0) * kRun, sp.held);
             float w[4] = {};
             for (int r = 0; r < tiles; ++r) {
                 QueryTile<D, GR, T> q;
@@ -534,7 +605,7 @@ __global__ __launch_bounds__(256) void quant_finish_kernel(QuantAttnArgs a) {
                 }
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    const f32x4 s = logits<D, GR, T>(q, k[t], key.pair[t], lo[t]);
+                    const f32x4 s = logits<D, GR, T>(q, k[t], pairs[t], lo[t]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float p = __builtin_amdgcn_exp2f((s[i] - ref[i].x) * a.c) * ref[i].y;
@@ -567,8 +638,11 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
         const size_t cells = (size_t)pairs * p.splits * rows;
         p.ml_bytes = (cells * sizeof(float2) + 255) / 256 * 256;
         p.bytes = p.ml_bytes + (p.splits > 1 ? cells * c.head_dim * sizeof(float) : 0);
-        int64_t n = (rows * c.head_dim + 255) / 256;
-        if (q.weights) n = runs;
+        const int places = 1024 / c.head_dim;  // rows of join_rows beside each other, times the splits taken side by side
+        int groups = 1;
+        while (groups < p.splits && groups < places) groups *= 2;
+        int64_t n = p.splits > 1 ? (rows + places / groups - 1) / (places / groups) : 1;
+        if (q.weights && runs > n) n = runs;
         const int64_t most = (1024 + pairs - 1) / pairs;
         p.finish = (int)(n < most ? n : most);
     }
@@ -584,7 +658,9 @@ static hipError_t run_quant_attn(hipStream_t s, const QuantAttnArgs &a, const Qu
     if (p.row_tiles == 1) quant_attn_kernel<D, GR, T, 1><<<grid, 256, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.finish == 0) return e;
-    quant_finish_kernel<D, GR, T><<<dim3((unsigned)p.finish, (unsigned)pairs), 256, 0, s>>>(a);
+    const dim3 finish((unsigned)p.finish, (unsigned)pairs);
+    if (a.n_rows <= 16) quant_finish_kernel<D, GR, T, 1><<<finish, 256, 0, s>>>(a);
+    else quant_finish_kernel<D, GR, T, sizeof(T) == 4 ? 4 : 8><<<finish, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
