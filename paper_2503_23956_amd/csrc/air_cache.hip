@@ -139,9 +139,7 @@ air_status air_quant_attn(void *stream, const air_quant_cache *cache, const air_
     if (!work) return AIR_OK;
     if (plan.bytes > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < plan.bytes))
         return refuse(AIR_ERR_WORKSPACE, "air_quant_attn: needs a 256-byte aligned workspace of %zu bytes", plan.bytes);
-    hipError_t e = hipSuccess;
-    if (rows) e = launch_quant_rows((hipStream_t)stream, *cache, *append, true);
-    if (e == hipSuccess) e = launch_quant_attn((hipStream_t)stream, *cache, plan, q, append != nullptr, workspace);
+    const hipError_t e = launch_quant_attn((hipStream_t)stream, *cache, plan, q, append, workspace);
     return e == hipSuccess ? AIR_OK : refuse(AIR_ERR_HIP, "air_quant_attn launch: %s", hipGetErrorString(e));
 }
 

@@ -177,15 +177,19 @@ struct QuantAppendArgs {
     float *weights;
     int32_t capacity, n_tokens, Hkv, batch;
 };
+QuantAppendArgs quant_row_args(const air_quant_cache &c, const air_quant_rows &r);
 hipError_t launch_quant_rows(hipStream_t s, const air_quant_cache &c, const air_quant_rows &r, bool append);
 // The shape of a quant attention call
 struct QuantPlan {
     int32_t row_tiles, row_blocks, splits;  // row tiles of 16 per wave, workgroups along the rows, along the slots
+    bool few;                               // the kernel for few rows, which appends by itself
+    int32_t max_runs;                       // runs of 64 slots per (sequence, KV head) whose logits are kept; 0: none
     int32_t finish;                         // workgroups per (sequence, KV head) of the second launch; 0: none
-    size_t ml_bytes, bytes;                 // workspace: (maximum, sum) pairs in front, all of it
+    size_t ml_bytes, kept_at, bytes;        // workspace: (maximum, sum) pairs in front, where the logits lie, all of it
 };
 QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q);
-hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const QuantPlan &p, const air_quant_query &q, bool appended, void *workspace);
+hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const QuantPlan &p, const air_quant_query &q, const air_quant_rows *append,
+                             void *workspace);
 size_t evict_bytes(const air_evict_config &c);
 hipError_t launch_evict(hipStream_t s, const air_evict_config &c, float *weights, int32_t *positions, const int32_t *lens, int32_t *lens_out,
                         void *workspace);

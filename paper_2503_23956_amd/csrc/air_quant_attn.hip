@@ -29,19 +29,26 @@ struct QuantAttnArgs {
     float c;  // scale * log2(e)
     int32_t Hkv, G, n_tokens, capacity, n_rows, splits, causal, appended;
     Div by_g, by_hkv, by_splits;
+    float4 *kept;      // [pair][run][2][lane]: logits, for the weights of calls with few rows; null: formed again
+    int32_t max_runs;  // runs of a pair there
+    QuantAppendArgs rows;  // what the first launch appends (few rows), else rows[0] null
 };
 
 constexpr int kRun = 64;  // slots that a wave takes at a time
+constexpr float kSlack = 8.0f;  // how far (base 2) a logit may lie above the reference of its row
+constexpr int kFewRows = 8;
 
 // What a sequence holds and asks
 struct QuantSpan {
     int b, h, count, held, rows;
+    int held_before;  // where the call appends its first row
     __device__ __forceinline__ QuantSpan(const QuantAttnArgs &a, int pair) {
         b = a.by_hkv.of(pair);
         h = pair - b * a.Hkv;
         const int n = a.counts ? a.counts[b] : a.n_tokens;
         count = n < 0 ? 0 : n > a.n_tokens ? a.n_tokens : n;
-        const int64_t all = (int64_t)a.lens[b] + (a.appended ? count : 0);
+        held_before = a.lens[b];
+        const int64_t all = (int64_t)held_before + (a.appended ? count : 0);
         held = all < 0 ? 0 : all > a.capacity ? a.capacity : (int)all;
         rows = count * a.G;
     }
@@ -315,7 +322,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
         }
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            // ---- softmax against a running reference
+            // ---- softmax against a running reference, raised when a logit lies more than kSlack above it
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -329,7 +336,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 top[i] = max16(fmaxf(fmaxf(s[r][0][i], s[r][1][i]), fmaxf(s[r][2][i], s[r][3][i])));
-                raise = raise || top[i] > m[r][i];
+                raise = raise || (top[i] - m[r][i]) * a.c > kSlack;
             }
             if (__any(raise)) {
 #pragma unroll
@@ -523,6 +530,24 @@ __device__ __forceinline__ void join_rows(const QuantAttnArgs &a, const QuantSpa
     }
 }
 
+// (maximum, 1 / sum) of a row over the splits; by 16 lanes, n of them
+__device__ __forceinline__ void row_reference(const QuantAttnArgs &a, const QuantSpan &sp, int pair, int row, int n, float2 *to) {
+    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
+    float2 v[4];
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        v[k] = float2{-INFINITY, 0.f};
+        if (n + 16 * k < a.splits && row < sp.rows) v[k] = ml[(size_t)(n + 16 * k) * a.n_rows + row];
+        top = fmaxf(top, v[k].x);
+    }
+    top = max16(top);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top, a.c) * v[k].y;
+    sum = sum16(sum);
+    if (n == 0) *to = float2{top == -INFINITY ? 0.0f : top, sum == 0.0f ? 0.0f : 1.0f / sum};
+}
+
 template <int D, int GR, typename T, int TILES>
 __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
     using S = QuantShape<D, GR, T>;
@@ -545,7 +570,6 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
     if ((int)blockIdx.x * 4 >= runs) return;
 
     float *weights = a.weights + base;
-    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
     for (int row0 = 0; row0 < sp.rows; row0 += 16 * TILES) {
         const int left = (sp.rows - row0 + 15) / 16, tiles = left < TILES ? left : TILES;
         __syncthreads();
@@ -559,20 +583,7 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
             ql[r][kOperands - 1][lane] = q.sums;
         }
         for (int x = threadIdx.x >> 4; x < 16 * tiles; x += 16) {  // 16 lanes a row
-            const int row = row0 + x;
-            float2 v[4];
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[k] = float2{-INFINITY, 0.f};
-                if (n + 16 * k < a.splits && row < sp.rows) v[k] = ml[(size_t)(n + 16 * k) * a.n_rows + row];
-                top = fmaxf(top, v[k].x);
-            }
-            top = max16(top);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top, a.c) * v[k].y;
-            sum = sum16(sum);
-            if (n == 0) rl[x] = float2{top == -INFINITY ? 0.0f : top, sum == 0.0f ? 0.0f : 1.0f / sum};
+            row_reference(a, sp, pair, row0 + x, n, rl + x);
         }
         __syncthreads();
         for (int u = u0; u < runs; u += stride) {
@@ -624,11 +635,334 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
     }
 }
 
+// ---------------------------------------------------------------------------------------
+// At most eight rows (a token of up to eight query heads per KV head, a few tokens of fewer): half of a 16 x 16 product's rows would be
+// idle.  The first product's are; its logits of slots 32 .. 63 of a run then move to the idle lanes, so that softmax, sums and steps are formed
+// once per logit: lane (n, c) has rows 4 (c & 1) + i at slots 16 t + 32 (c >> 1) + n, t = 0, 1.  The factors p step are formed there,
+// and go through LDS as bf16 terms, the first one in rows 0 .. 7 of the second product's operand and the second one in rows 8 .. 15
+// (fp32: the third one in a product of its own): one product for both, joined at the end.
+//
+// The wave whose run has slots that the call appends writes them first.
+// ---------------------------------------------------------------------------------------
+template <int D, int GR, typename T>
+struct FewShape {
+    using S = QuantShape<D, GR, T>;
+    static constexpr int kWStride = 144, kWRows = S::kF32 ? 24 : 16;  // bytes: 64 places of bf16 and 16 more, 16 rows on different banks
+    static constexpr int kWBytes = S::NG * kWRows * kWStride, kWave = S::kVBytes + kWBytes;
+    static constexpr int kLds = 4 * kWave > 4 * 8 * D * 4 + 4 * 8 * 8 ? 4 * kWave : 4 * 8 * D * 4 + 4 * 8 * 8;
+};
+
+// (x of lanes 0 .. 31, y of lanes 0 .. 31)
+__device__ __forceinline__ float lower_halves(float x, float y) {
+    return __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false)[0]);
+}
+__device__ __forceinline__ float max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float add_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// the wave's rows of slots slot0 .. slot0 + 63 that the call appends
+template <int D, int GR, typename T>
+__device__ __forceinline__ void append_run(const QuantAttnArgs &a, const QuantSpan &sp, int slot0) {
+    constexpr int kLanes = D / 8;
+    const int lane = threadIdx.x & 63, p = lane & (kLanes - 1);
+    const int64_t len = (int64_t)sp.held_before;
+    for (int64_t t = slot0 - len + lane / kLanes; t < slot0 + kRun - len; t += 64 / kLanes) {
+        if (t < 0 || t >= sp.count || len + t >= sp.held) continue;
+        const int64_t cell = ((int64_t)sp.b * a.Hkv + sp.h) * a.capacity + len + t;
+        append_row<D, GR, T, true>(static_cast<const T *>(a.rows.rows[0]) + sp.b * a.rows.row_b[0] + sp.h * a.rows.row_h[0] + t * a.rows.row_t[0],
+                                   reinterpret_cast<uint32_t *>(a.rows.codes[0] + cell * (D / 2)), a.rows.scales[0] + cell * (D / GR), p);
+        append_row<D, GR, T, false>(static_cast<const T *>(a.rows.rows[1]) + sp.b * a.rows.row_b[1] + sp.h * a.rows.row_h[1] + t * a.rows.row_t[1],
+                                    reinterpret_cast<uint32_t *>(a.rows.codes[1] + cell * (D / 2)), a.rows.scales[1] + cell * (D / GR), p);
+        if (p == 0) {
+            if (a.rows.positions) a.rows.positions[cell] = a.rows.first[sp.b] + (int)t;
+            if (a.rows.weights) a.rows.weights[cell] = 0.0f;
+        }
+    }
+    // in this XCD's L2 before the wave reads them, and nothing older in the first-level cache
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+}
+
+template <int D, int GR, typename T>
+__global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
+    using S = QuantShape<D, GR, T>;
+    using F = FewShape<D, GR, T>;
+    constexpr int NG = S::NG;
+    __shared__ __align__(16) uint8_t lds[F::kLds];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4, upper = c >> 1, rc = c & 1;
+    const int pair = blockIdx.y, split = blockIdx.x;
+    const QuantSpan sp(a, pair);
+    const bool append = a.rows.rows[0] != nullptr;
+    if (sp.rows == 0) return;
+    const int most = sp.seen(a, sp.rows - 1), least = sp.seen(a, 0);
+
+    uint8_t *vb = lds + wave * F::kWave, *wb = vb + S::kVBytes;
+    const int k_of = 16 * c + (n & 8) + ((n & 1) ? 4 + ((n & 7) >> 1) : (n & 7) >> 1);  // (as in the kernel for more rows)
+    const uint8_t *v_read = vb + (16 * (k_of & 3) + (k_of >> 2)) * S::kVStride;
+
+    const size_t base = (size_t)pair * a.capacity;
+    const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
+    const uint32_t *ks = a.ks + base * NG, *vs = a.vs + base * NG;
+    const int runs = (most + kRun - 1) / kRun, stride = 4 * a.splits;
+    int u = split * 4 + wave;
+    KeyRun<D, GR> key;
+    if (u < runs) {
+        if (append && (u + 1) * kRun > sp.held_before) append_run<D, GR, T>(a, sp, u * kRun);
+        key.load(kc, ks, u * kRun, sp.held);
+    }
+    QueryTile<D, GR, T> q;
+    q.load(a, sp, n);
+
+    f32x4 acc[S::NT];
+    float m[4], l[4], al[4][NG];
+#pragma unroll
+    for (int i = 0; i < S::NT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m[i] = -INFINITY;
+        l[i] = 0.0f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) al[i][g] = 0.0f;
+    }
+
+    for (; u < runs; u += stride) {
+        // V on its way during the first product: the codes, and the pairs of the lane's two tiles
+        constexpr int kPieces = D / 32;
+        uint4 code[kPieces];
+        Words<NG> vp[2];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int at = u * kRun + i * (64 / kPieces) + lane / kPieces, slot = at < sp.held ? at : sp.held - 1;
+            code[i] = *reinterpret_cast<const uint4 *>(vc + (size_t)(uint32_t)slot * (D / 2) + 16 * (lane % kPieces));
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int at = u * kRun + 16 * t + 32 * upper + n, slot = at < sp.held ? at : sp.held - 1;
+            vp[t] = load_words<NG>(vs + (size_t)(uint32_t)slot * NG);
+        }
+        const bool masked = (u + 1) * kRun > least;
+        const int next = u + stride < runs ? u + stride : u;
+        // ---- logits
+        f32x4 s4[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            uint4 k[S::KM];
+#pragma unroll
+            for (int i = 0; i < S::KM; ++i) k[i] = operand_of(key.code[t].w[i]);
+            s4[t] = logits<D, GR, T>(q, k, key.pair[t], lo_operand<NG>(key.pair[t]));
+            if (t & 1) __builtin_amdgcn_sched_barrier(0);  // (operands of all four tiles at once do not fit the registers)
+        }
+        if (append && next > u && (next + 1) * kRun > sp.held_before) append_run<D, GR, T>(a, sp, next * kRun);
+        key.load(kc, ks, next * kRun, sp.held);
+        f32x4 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[t][i] = lower_halves(s4[t][i], s4[t + 2][i]);
+        if (masked) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int slot = u * kRun + 16 * t + 32 * upper + n;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) vp[t].w[g] = slot < sp.held ? vp[t].w[g] : 0u;  // (whatever lies there)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = 4 * rc + i, seen = row < sp.rows ? sp.seen(a, row) : sp.held;
+                    s[t][i] = slot < seen ? s[t][i] : -INFINITY;
+                }
+            }
+        }
+        if (a.kept) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) a.kept[(((size_t)pair * a.max_runs + u) * 2 + t) * 64 + lane] = float4{s[t][0], s[t][1], s[t][2], s[t][3]};
+        }
+        // ---- V to LDS
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            uint2 *to = reinterpret_cast<uint2 *>(vb + (i * (64 / kPieces) + lane / kPieces) * S::kVStride + 16 * (lane % kPieces));
+            to[0] = uint2{code[i].x, code[i].y};
+            to[1] = uint2{code[i].z, code[i].w};
+        }
+        // ---- softmax against a running reference, raised when a logit lies more than kSlack above it
+        float top[4];
+        bool raise = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            top[i] = max_halves(max16(fmaxf(s[0][i], s[1][i])));
+            raise = raise || (top[i] - m[i]) * a.c > kSlack;
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool up = top[i] > m[i];
+                const float f = up ? __builtin_amdgcn_exp2f((m[i] - top[i]) * a.c) : 1.0f;
+                m[i] = up ? top[i] : m[i];
+                l[i] *= f;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) al[i][g] *= f;
+#pragma unroll
+                for (int j = 0; j < S::NT; ++j) acc[j][i] *= f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float ref = m[i] == -INFINITY ? 0.0f : m[i];
+            float p[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                p[t] = __builtin_amdgcn_exp2f((s[t][i] - ref) * a.c);
+                l[i] += p[t];
+            }
+            uint8_t *to = wb + (4 * rc + i) * F::kWStride + 8 * n + 4 * upper;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    float lo = lo_of(vp[t].w[g]);
+                    if (masked) lo = s[t][i] == -INFINITY ? 0.0f : lo;  // (a lo of NaN counts only where the row sees it)
+                    al[i][g] = fmaf(p[t], lo, al[i][g]);
+                }
+                uint32_t w[S::PT];
+                split_pair<S::PT>(p[0] * step_of(vp[0].w[g]), p[1] * step_of(vp[1].w[g]), w);
+#pragma unroll
+                for (int k = 0; k < S::PT; ++k) *reinterpret_cast<uint32_t *>(to + (g * F::kWRows + 8 * k) * F::kWStride) = w[k];
+            }
+        }
+        wave_sync();
+        __builtin_amdgcn_sched_barrier(0);
+        // ---- second product: two halves of 32 places
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + n) * F::kWStride + 32 * c + 16 * j);
+                uint4 w3 = {0, 0, 0, 0};
+                if (S::kF32 && n < 8) w3 = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + 16 + n) * F::kWStride + 32 * c + 16 * j);
+#pragma unroll
+                for (int x = 0; x < GR / 16; ++x) {
+                    const int tile = g * (GR / 16) + x;
+                    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+                    const i32x2 vcode = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(v_read + 8 * tile));
+                    const uint4 v = operand_of((uint32_t)(j ? vcode.y : vcode.x));
+                    acc[tile] = mma<bf16_t>(w, v, acc[tile]);
+                    if (S::kF32) acc[tile] = mma<bf16_t>(w3, v, acc[tile]);
+                }
+            }
+        }
+    }
+
+    // ---- the lanes' sums, then the four waves'
+    __syncthreads();
+    float *ob = reinterpret_cast<float *>(lds);  // [wave][8 rows][D]
+    float2 *mlb = reinterpret_cast<float2 *>(lds + 4 * 8 * D * 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        l[i] = add_halves(sum16(l[i]));
+#pragma unroll
+        for (int g = 0; g < NG; ++g) al[i][g] = add_halves(sum16(al[i][g]));
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j) {
+            const float o = add_halves(acc[j][i]) + al[i][j / (GR / 16)];
+            if (upper == 0) ob[(wave * 8 + 4 * rc + i) * D + 16 * j + n] = o;
+        }
+        if (n == 0 && upper == 0) mlb[wave * 8 + 4 * rc + i] = float2{m[i], l[i]};
+    }
+    __syncthreads();
+    const int row = threadIdx.x >> 5, x = threadIdx.x & 31;
+    if (row < sp.rows) {
+        float high = -INFINITY, f[4], sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) high = fmaxf(high, mlb[w * 8 + row].x);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            f[w] = part_weight(mlb[w * 8 + row].x, mlb[w * 8 + row].y, high, a.c);
+            sum = fmaf(f[w], mlb[w * 8 + row].y, sum);
+        }
+        const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
+        if (a.part_ml && x == 0) a.part_ml[part] = float2{high, sum};
+        if (a.splits > 1 || a.out) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const int t = a.by_g.of(row);
+            T *to = static_cast<T *>(a.out) + sp.b * a.out_b + ((int64_t)sp.h * a.G + row - t * a.G) * a.out_h + t * a.out_t;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                float o = 0.0f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) o = fmaf(f[w], ob[(w * 8 + row) * D + 32 * j + x], o);
+                if (a.splits > 1) a.part_o[part * D + 32 * j + x] = o;
+                else put(to + 32 * j + x, o * inv);
+            }
+        }
+    }
+}
+
+// Second launch behind it: rows joined, and the slots' weights out of the logits that were kept
+template <int D, typename T>
+__global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) {
+    __shared__ float4 jl[256 + 8];
+    __shared__ float2 rl[8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
+    const int pair = blockIdx.y;
+    const QuantSpan sp(a, pair);
+    if (sp.rows == 0) return;
+    // (all rows together see all slots that the last one sees)
+    const int runs = a.weights ? (sp.seen(a, sp.rows - 1) + kRun - 1) / kRun : 0, stride = gridDim.x * 4;
+    const float4 *kept = a.kept + (size_t)pair * a.max_runs * 128 + lane;
+    float *weights = a.weights + (size_t)pair * a.capacity;
+    int u = blockIdx.x * 4 + wave;
+    float4 s[2] = {};
+    float was[2] = {};
+    const auto request = [&](int run) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = kept[((size_t)run * 2 + t) * 64];
+            const int slot = run * kRun + 16 * t + 32 * (c >> 1) + n;
+            was[t] = (c & 1) == t && slot < sp.held ? weights[slot] : 0.0f;
+        }
+    };
+    if (u < runs) request(u);
+    if (a.splits > 1 && a.out) join_rows<D, T>(a, sp, pair, jl);
+    if ((int)blockIdx.x * 4 >= runs) return;
+    if (threadIdx.x < 128) {  // 16 lanes a row
+        const int row = threadIdx.x >> 4;
+        row_reference(a, sp, pair, row, n, rl + row);
+    }
+    __syncthreads();
+    float2 ref[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ref[i] = rl[4 * (c & 1) + i];
+    for (; u < runs; u += stride) {
+        float w[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const float x[4] = {s[t].x, s[t].y, s[t].z, s[t].w};
+            w[t] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (4 * (c & 1) + i < sp.rows) w[t] = fmaf(__builtin_amdgcn_exp2f((x[i] - ref[i].x) * a.c), ref[i].y, w[t]);
+            w[t] += __shfl_xor(w[t], 16, 64);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int slot = u * kRun + 16 * t + 32 * (c >> 1) + n;
+            if ((c & 1) == t && slot < sp.held) weights[slot] = was[t] + w[t];
+        }
+        if (u + stride < runs) request(u + stride);
+    }
+}
+
 QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     QuantPlan p{};
     const int64_t pairs = (int64_t)c.batch * c.n_kv_heads, rows = (int64_t)q.n_tokens * (q.n_q_heads / c.n_kv_heads);
     if (pairs == 0 || rows == 0) return p;
     const int64_t len = q.max_len > 0 && q.max_len < c.capacity ? q.max_len : c.capacity;
+    p.few = rows <= kFewRows;
     p.row_tiles = rows > 16 && c.dtype == AIR_BF16 ? 2 : 1;  // (two tiles of fp32 queries, three terms each, do not fit the registers)
     p.row_blocks = (int)((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
     const int64_t runs = (len + 4 * kRun - 1) / (4 * kRun), wanted = 512 / (pairs * p.row_blocks);  // two workgroups a CU
@@ -637,7 +971,12 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     if (p.splits > 1 || q.weights) {
         const size_t cells = (size_t)pairs * p.splits * rows;
         p.ml_bytes = (cells * sizeof(float2) + 255) / 256 * 256;
-        p.bytes = p.ml_bytes + (p.splits > 1 ? cells * c.head_dim * sizeof(float) : 0);
+        p.bytes = p.ml_bytes + (p.splits > 1 ? (cells * c.head_dim * sizeof(float) + 255) / 256 * 256 : 0);
+        if (p.few && q.weights) {
+            p.max_runs = (int)((c.capacity + kRun - 1) / kRun);
+            p.kept_at = p.bytes;
+            p.bytes += (size_t)pairs * p.max_runs * kRun * kFewRows * sizeof(float);
+        }
         const int places = 1024 / c.head_dim;  // rows of join_rows beside each other, times the splits taken side by side
         int groups = 1;
         while (groups < p.splits && groups < places) groups *= 2;
@@ -651,21 +990,37 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
 
 template <int D, int GR, typename T>
 static hipError_t run_quant_attn(hipStream_t s, const QuantAttnArgs &a, const QuantPlan &p, int pairs) {
-    const dim3 grid((unsigned)(p.splits * p.row_blocks), (unsigned)pairs);
+    const dim3 grid((unsigned)(p.splits * p.row_blocks), (unsigned)pairs), finish((unsigned)p.finish, (unsigned)pairs);
+    if (p.few) {
+        quant_few_kernel<D, GR, T><<<grid, 256, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || p.finish == 0) return e;
+        quant_few_finish_kernel<D, T><<<finish, 256, 0, s>>>(a);
+        return hipGetLastError();
+    }
     if constexpr (sizeof(T) == 2) {
         if (p.row_tiles == 2) quant_attn_kernel<D, GR, T, 2><<<grid, 256, 0, s>>>(a);
     }
     if (p.row_tiles == 1) quant_attn_kernel<D, GR, T, 1><<<grid, 256, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.finish == 0) return e;
-    const dim3 finish((unsigned)p.finish, (unsigned)pairs);
     if (a.n_rows <= 16) quant_finish_kernel<D, GR, T, 1><<<finish, 256, 0, s>>>(a);
     else quant_finish_kernel<D, GR, T, sizeof(T) == 4 ? 4 : 8><<<finish, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
-hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const QuantPlan &p, const air_quant_query &q, bool appended, void *workspace) {
+hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const QuantPlan &p, const air_quant_query &q, const air_quant_rows *append,
+                             void *workspace) {
     QuantAttnArgs a;
+    a.rows = QuantAppendArgs{};
+    if (append && p.few) {
+        a.rows = quant_row_args(c, *append);
+    } else if (append) {
+        const hipError_t e = launch_quant_rows(s, c, *append, true);
+        if (e != hipSuccess) return e;
+    }
+    a.kept = p.max_runs ? reinterpret_cast<float4 *>(static_cast<uint8_t *>(workspace) + p.kept_at) : nullptr;
+    a.max_runs = p.max_runs;
     a.kc = static_cast<const uint8_t *>(c.k_codes);
     a.vc = static_cast<const uint8_t *>(c.v_codes);
     a.ks = static_cast<const uint32_t *>(c.k_scales);
@@ -691,7 +1046,7 @@ hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const Quan
     a.n_rows = q.n_tokens * a.G;
     a.splits = p.splits;
     a.causal = q.causal;
-    a.appended = appended;
+    a.appended = append != nullptr;
     a.by_g = div_by(a.G);
     a.by_hkv = div_by(a.Hkv);
     a.by_splits = div_by(p.splits);

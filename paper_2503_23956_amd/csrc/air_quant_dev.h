@@ -44,4 +44,103 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&t)[TERMS
     t[TERMS - 1] = __builtin_bit_cast(uint32_t, last);
 }
 
+// ---- rows: a lane has eight elements
+__device__ __forceinline__ void load8(const bf16_t *p, float (&x)[8]) {
+    const uint4 v = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = a[i];
+        x[4 + i] = b[i];
+    }
+}
+__device__ __forceinline__ void store8(bf16_t *p, const float (&x)[8]) {
+    bf16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
+    *reinterpret_cast<uint4 *>(p) = __builtin_bit_cast(uint4, v);
+}
+__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
+    *reinterpret_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+
+__device__ __forceinline__ float min_f(float a, float b) { return fminf(a, b); }
+// over the 4 (LANES = 4) or 8 consecutive lanes of a group
+template <int LANES>
+__device__ __forceinline__ void range_of(float &low, float &high) {
+    low = AIR_DPP_STEP(min_f, low, 0xB1);
+    high = AIR_DPP_STEP(fmaxf, high, 0xB1);
+    low = AIR_DPP_STEP(min_f, low, 0x4E);
+    high = AIR_DPP_STEP(fmaxf, high, 0x4E);
+    if (LANES == 8) {
+        low = AIR_DPP_STEP(min_f, low, 0x141);
+        high = AIR_DPP_STEP(fmaxf, high, 0x141);
+    }
+}
+
+// (lo, step) of a group from its least and greatest element
+__device__ __forceinline__ uint32_t pair_of(float low, float high) {
+    // (a NaN does not pass a minimum or maximum: the caller has put an infinity in its place)
+    if (!(fmaxf(-low, high) < 0x1p126f)) return 0x7fc0u;  // NaN, step 0
+    const uint32_t u = __float_as_uint(low);
+    const uint32_t lo = (u + (u >> 31 ? 0xffffu : 0u)) & 0xffff0000u;  // down: away from zero below it
+    const float width = (high - __uint_as_float(lo)) / 15.0f;
+    const uint32_t step = (__float_as_uint(width) + 0xffffu) & 0xffff0000u;
+    return (__uint_as_float(step) < 0x1p-120f ? 0u : step) | lo >> 16;
+}
+
+// which dword of a row holds elements 8 p .. 8 p + 7
+template <int D, bool K>
+__device__ __forceinline__ int dword_of(int p) {
+    return K ? D / 32 * (p & 3) + (p >> 2) : p;
+}
+
+template <int D, int GR, typename T, bool K>
+__device__ __forceinline__ void append_row(const T *src, uint32_t *codes, uint32_t *scales, int p) {
+    float x[8];
+    load8(src + 8 * p, x);
+    float low = x[0], high = x[0];
+    bool number = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        low = fminf(low, x[i]);
+        high = fmaxf(high, x[i]);
+        number = number && x[i] == x[i];
+    }
+    if (!number) high = INFINITY;
+    range_of<GR / 8>(low, high);
+    const uint32_t pair = pair_of(low, high);
+    const float lo = lo_of(pair), step = step_of(pair), inv = 1.0f / step;
+    uint32_t code = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // the quotient, rounded correctly: the product with the rounded reciprocal, mended once by what it leaves (Markstein)
+        const float d = x[i] - lo, q = d * inv;
+        const float s = fmaf(fmaf(-q, step, d), inv, q);
+        const uint32_t c = step > 0.0f ? (uint32_t)fminf(rintf(s), 15.0f) : 0u;
+        code |= c << (K ? (i & 3) * 8 + (i & 4) : 4 * i);
+    }
+    codes[dword_of<D, K>(p)] = code;
+    if ((p & (GR / 8 - 1)) == 0) scales[p / (GR / 8)] = pair;
+}
+
+template <int D, int GR, typename T, bool K>
+__device__ __forceinline__ void read_row(T *dst, const uint32_t *codes, const uint32_t *scales, int p) {
+    const uint32_t code = codes[dword_of<D, K>(p)], pair = scales[p / (GR / 8)];
+    const float lo = lo_of(pair), step = step_of(pair);
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = fmaf(step, (float)(code >> (K ? (i & 3) * 8 + (i & 4) : 4 * i) & 15u), lo);
+    store8(dst + 8 * p, x);
+}
+
 }  // namespace air
