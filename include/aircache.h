@@ -340,7 +340,7 @@ air_status air_prompt_attn(void *stream, const air_prompt_config *cfg, const air
  * largest magnitude.  A group with an element that is not finite, or of 2^126 and more, stands for NaN throughout.
  * Memory, per (sequence, KV head, slot): codes head_dim / 2 bytes; scales head_dim / group pairs (lo, step) of bf16.
  *   V: element c in byte c / 2, even elements in the low half.  K: elements 8 p .. 8 p + 7 (p = 4 m + n, n < 4) in the four bytes
- *   from head_dim / 8 n + 4 m, element 8 p + i in the low half of byte i for i < 4, in the high half of byte i - 4 above. */
+ *   from head_dim / 8 n + 4 m, of which (low half, high half) hold the elements (0, 2), (4, 6), (1, 3), (5, 7). */
 typedef struct {
     int32_t batch, n_kv_heads, capacity; /* batch x n_kv_heads at most 65535; capacity slots per (sequence, KV head), 1..2^24 */
     int32_t head_dim, group;             /* 64 or 128; 32 or 64                                                                */

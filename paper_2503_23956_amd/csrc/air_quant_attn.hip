@@ -16,6 +16,9 @@
 
 namespace air {
 
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+
 struct QuantAttnArgs {
     const uint8_t *kc, *vc;
     const uint32_t *ks, *vs;
@@ -28,7 +31,7 @@ struct QuantAttnArgs {
     const int32_t *lens, *counts;
     float c;  // scale * log2(e)
     int32_t Hkv, G, n_tokens, capacity, n_rows, splits, causal, appended;
-    Div by_g, by_hkv, by_splits;
+    Div by_g, by_hkv, by_splits, by_stride;  // by_stride: 4 splits
     float4 *kept;      // [pair][run][2][lane]: logits, for the weights of calls with few rows; null: formed again
     int32_t max_runs;  // runs of a pair there
     QuantAppendArgs rows;  // what the first launch appends (few rows), else rows[0] null
@@ -110,10 +113,11 @@ struct QueryTile {
             if constexpr (S::kF32) {
                 const f32x4 u = __builtin_bit_cast(f32x4, x), v = __builtin_bit_cast(f32x4, y);
                 uint32_t w[4][S::QT];
-                split_pair<S::QT>(u[0], u[1], w[0]);
-                split_pair<S::QT>(u[2], u[3], w[1]);
-                split_pair<S::QT>(v[0], v[1], w[2]);
-                split_pair<S::QT>(v[2], v[3], w[3]);
+                // (the order in which operand_of gives K's codes)
+                split_pair<S::QT>(u[0], v[0], w[0]);
+                split_pair<S::QT>(u[1], v[1], w[1]);
+                split_pair<S::QT>(u[2], v[2], w[2]);
+                split_pair<S::QT>(u[3], v[3], w[3]);
 #pragma unroll
                 for (int k = 0; k < S::QT; ++k) e[k][m] = uint4{w[0][k], w[1][k], w[2][k], w[3][k]};
                 sum = ((u[0] + u[1]) + (u[2] + u[3])) + ((v[0] + v[1]) + (v[2] + v[3]));
@@ -125,39 +129,43 @@ struct QueryTile {
             }
             part[m / S::KG] += sum;
         }
+        // lanes c = 2, 3 take the bias off: their operand has the steps in the place of lo
         uint32_t t3[S::NG][3];  // bf16 terms of the sums, in the low halves
 #pragma unroll
         for (int g = 0; g < S::NG; ++g) {
             part[g] += __shfl_xor(part[g], 16, 64);
             part[g] += __shfl_xor(part[g], 32, 64);
-            split_pair<3>(part[g], 0.0f, t3[g]);
+            split_pair<3>(c < 2 ? part[g] : S::kF32 ? 0.0f : -kCodeBias * part[g], 0.0f, t3[g]);
         }
         // contraction indices 8 c .. 8 c + 7 of the product with lo, whose other operand repeats (lo_0, lo_1), (lo_2, lo_3): terms one and two
-        // in lanes c = 0, three in c = 1 (four groups); all three in c = 0 (two groups, one group beside its step)
+        // in even lanes c, three in odd ones (four groups); all three in even ones (two groups, one group beside a zero)
+        const bool even = (c & 1) == 0;
         if (S::NG == 4) {
             const uint32_t a01 = t3[0][0] | t3[1 % S::NG][0] << 16, a23 = t3[2 % S::NG][0] | t3[3 % S::NG][0] << 16;
             const uint32_t b01 = t3[0][1] | t3[1 % S::NG][1] << 16, b23 = t3[2 % S::NG][1] | t3[3 % S::NG][1] << 16;
             const uint32_t c01 = t3[0][2] | t3[1 % S::NG][2] << 16, c23 = t3[2 % S::NG][2] | t3[3 % S::NG][2] << 16;
-            sums = c == 0 ? uint4{a01, a23, b01, b23} : c == 1 ? uint4{c01, c23, 0, 0} : uint4{0, 0, 0, 0};
+            sums = even ? uint4{a01, a23, b01, b23} : uint4{c01, c23, 0, 0};
         } else {
             uint32_t w[3];
 #pragma unroll
             for (int k = 0; k < 3; ++k) w[k] = S::NG == 2 ? t3[0][k] | t3[S::NG - 1][k] << 16 : t3[0][k] & 0xffffu;
-            sums = c == 0 ? uint4{w[0], w[1], w[2], 0} : uint4{0, 0, 0, 0};
+            sums = even ? uint4{w[0], w[1], w[2], 0} : uint4{0, 0, 0, 0};
         }
     }
 };
 
-// the other operand of the product with sum(q): slot n's lo, as the queries' sums lie
+// the other operand of the product with sum(q), as the queries' sums lie: slot n's lo; its steps in lanes c = 2, 3
 template <int NG>
 __device__ __forceinline__ uint4 lo_operand(const Words<NG> &pairs) {
-    if (NG == 4) {
-        const uint32_t a = __builtin_amdgcn_perm(pairs.w[1 % NG], pairs.w[0], 0x05040100u);
-        const uint32_t b = __builtin_amdgcn_perm(pairs.w[3 % NG], pairs.w[2 % NG], 0x05040100u);
-        return uint4{a, b, a, b};
-    }
-    const uint32_t a = NG == 2 ? __builtin_amdgcn_perm(pairs.w[NG - 1], pairs.w[0], 0x05040100u) : pairs.w[0] & 0xffffu;
-    return uint4{a, a, a, a};
+    const uint32_t pick = threadIdx.x & 32 ? (NG == 1 ? 0x0c0c0302u : 0x07060302u) : (NG == 1 ? 0x0c0c0100u : 0x05040100u);
+    const uint32_t a = __builtin_amdgcn_perm(pairs.w[1 % NG], pairs.w[0], pick);
+    if (NG < 4) return uint4{a, a, a, a};
+    const uint32_t b = __builtin_amdgcn_perm(pairs.w[3 % NG], pairs.w[2 % NG], pick);
+    return uint4{a, b, a, b};
+}
+template <bool F32>
+__device__ __forceinline__ uint4 key_operand(uint32_t codes) {
+    return F32 ? operand_of(codes) : biased_of(codes);
 }
 
 // logits (before the factor) of rows 4 c .. 4 c + 3 at slot n of a tile
@@ -180,6 +188,24 @@ __device__ __forceinline__ f32x4 logits(const QueryTile<D, GR, T> &q, const uint
     return s;
 }
 
+// ---- references.  A row's reference is a number `ref` in the base-2 domain, the same in all of its exponents 2^(s c - ref): that it is a rounded
+// maximum cancels when the row is divided by its sum.  Beyond kHuge the exponents' own products are rounded like it: equal logits
+// stay equal.
+constexpr float kHuge = 0x1p20f;
+__device__ __forceinline__ float exponent(float s, float c, float ref, bool huge) {
+    if (__builtin_expect(huge, 0)) {
+        float x = s * c;
+        asm volatile("" : "+v"(x));  // (rounded by itself)
+        return x - ref;
+    }
+    return fmaf(s, c, -ref);
+}
+// the logit above which a reference `top`, of the logit `high`, is raised: kSlack further on, to 0.2 (base 2); at once beyond kHuge
+__device__ __forceinline__ float limit_of(float high, float top, float c) {
+    return fabsf(top) > kHuge ? high : (top + kSlack) * (1.0f / c);
+}
+__device__ __forceinline__ float finite_or_zero(float ref) { return ref == -INFINITY ? 0.0f : ref; }
+
 // What a wave requests ahead: 64 slots
 template <int D, int GR>
 struct KeyRun {
@@ -191,8 +217,8 @@ struct KeyRun {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const int at = slot0 + 16 * t + n, slot = at < held ? at : held - 1;
-            code[t] = load_words<D / 32>(codes + (size_t)(uint32_t)slot * (D / 2) + D / 8 * c);
-            pair[t] = load_words<D / GR>(pairs + (size_t)(uint32_t)slot * (D / GR));
+            code[t] = load_words<D / 32>(codes + ((uint32_t)slot * (D / 2) + D / 8 * c));
+            pair[t] = load_words<D / GR>(reinterpret_cast<const uint8_t *>(pairs) + (uint32_t)slot * (D / GR * 4));
         }
     }
 };
@@ -206,20 +232,20 @@ struct ValueRun {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int at = slot0 + i * (64 / kPieces) + lane / kPieces, slot = at < held ? at : held - 1;
-            code[i] = *reinterpret_cast<const uint4 *>(codes + (size_t)(uint32_t)slot * (D / 2) + 16 * (lane % kPieces));
+            code[i] = *reinterpret_cast<const uint4 *>(codes + ((uint32_t)slot * (D / 2) + 16 * (lane % kPieces)));
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const int at = slot0 + 16 * t + (lane & 15), slot = at < held ? at : held - 1;
-            pair[t] = load_words<D / GR>(pairs + (size_t)(uint32_t)slot * (D / GR));
+            pair[t] = load_words<D / GR>(reinterpret_cast<const uint8_t *>(pairs) + (uint32_t)slot * (D / GR * 4));
         }
     }
 };
 
 // weight of sums taken against the reference m in sums against top
-__device__ __forceinline__ float part_weight(float m, float l, float top, float c) {
+__device__ __forceinline__ float part_weight(float m, float l, float top) {
     if (m == -INFINITY) return l == 0.0f ? 0.0f : 1.0f;  // (no finite logit: nothing, or NaN that stays)
-    return __builtin_amdgcn_exp2f((m - top) * c);
+    return __builtin_amdgcn_exp2f(m - top);
 }
 
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
@@ -256,13 +282,15 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
 
     f32x4 acc[RT][S::NT];
     float m[RT][4], l[RT][4], al[RT][4][NG];
+    float limit[RT][4];  // the logit above which the reference is raised
+    bool huge = false;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) acc[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            m[r][i] = -INFINITY;
+            m[r][i] = limit[r][i] = -INFINITY;
             l[r][i] = 0.0f;
 #pragma unroll
             for (int g = 0; g < NG; ++g) al[r][i][g] = 0.0f;
@@ -287,7 +315,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
         for (int t = 0; t < 4; ++t) {
             uint4 k[S::KM];
 #pragma unroll
-            for (int i = 0; i < S::KM; ++i) k[i] = operand_of(key.code[t].w[i]);
+            for (int i = 0; i < S::KM; ++i) k[i] = key_operand<S::kF32>(key.code[t].w[i]);
             const uint4 lo = lo_operand<NG>(key.pair[t]);
 #pragma unroll
             for (int r = 0; r < RT; ++r) s[r][t] = logits<D, GR, T>(q[r], k, key.pair[t], lo);
@@ -331,34 +359,37 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
                     for (int t = 0; t < 4; ++t) s[r][t][i] = u * kRun + 16 * t + n < seen ? s[r][t][i] : -INFINITY;
                 }
             }
-            float top[4];
             bool raise = false;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                top[i] = max16(fmaxf(fmaxf(s[r][0][i], s[r][1][i]), fmaxf(s[r][2][i], s[r][3][i])));
-                raise = raise || (top[i] - m[r][i]) * a.c > kSlack;
-            }
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) raise = raise || s[r][t][i] > limit[r][i];
             if (__any(raise)) {
+                bool big = false;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool up = top[i] > m[r][i];
-                    const float f = up ? __builtin_amdgcn_exp2f((m[r][i] - top[i]) * a.c) : 1.0f;
-                    m[r][i] = up ? top[i] : m[r][i];
+                    const float high = max16(fmaxf(fmaxf(s[r][0][i], s[r][1][i]), fmaxf(s[r][2][i], s[r][3][i]))), top = high * a.c;
+                    const bool up = top > m[r][i];
+                    const float f = up ? __builtin_amdgcn_exp2f(m[r][i] - top) : 1.0f;
+                    m[r][i] = up ? top : m[r][i];
+                    if (up) limit[r][i] = limit_of(high, top, a.c);
+                    big = big || fabsf(finite_or_zero(m[r][i])) > kHuge;
                     l[r][i] *= f;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) al[r][i][g] *= f;
 #pragma unroll
                     for (int j = 0; j < S::NT; ++j) acc[r][j][i] *= f;
                 }
+                huge = huge || __any(big);
             }
             wave_sync();  // (the probabilities of the tile in front have been read)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float ref = m[r][i] == -INFINITY ? 0.0f : m[r][i];
+                const float ref = finite_or_zero(m[r][i]);
                 f32x4 p;
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    p[t] = __builtin_amdgcn_exp2f((s[r][t][i] - ref) * a.c);
+                    p[t] = __builtin_amdgcn_exp2f(exponent(s[r][t][i], a.c, ref, huge));
                     l[r][i] += p[t];
                 }
                 if (masked) {
@@ -428,7 +459,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
             for (int w = 0; w < 4; ++w) top = fmaxf(top, mlb[w * 16 + x].x);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                f[w] = part_weight(mlb[w * 16 + x].x, mlb[w * 16 + x].y, top, a.c);
+                f[w] = part_weight(mlb[w * 16 + x].x, mlb[w * 16 + x].y, top);
                 sum += f[w] * mlb[w * 16 + x].y;
             }
             const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
@@ -483,13 +514,13 @@ __device__ __forceinline__ void join_rows(const QuantAttnArgs &a, const QuantSpa
             float most = top;
 #pragma unroll
             for (int k = 0; k < 8; ++k) most = fmaxf(most, v[k].x);
-            const float f0 = part_weight(top, l, most, a.c);
+            const float f0 = part_weight(top, l, most);
             sum.x *= f0, sum.y *= f0, sum.z *= f0, sum.w *= f0;
             l *= f0;
             top = most;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float f = part_weight(v[k].x, v[k].y, top, a.c);
+                const float f = part_weight(v[k].x, v[k].y, top);
                 l = fmaf(f, v[k].y, l);
                 sum.x = fmaf(f, part[k].x, sum.x);
                 sum.y = fmaf(f, part[k].y, sum.y);
@@ -506,13 +537,13 @@ __device__ __forceinline__ void join_rows(const QuantAttnArgs &a, const QuantSpa
             if (group == 0) {
                 float most = top;
                 for (int k = 1; k < groups; ++k) most = fmaxf(most, lds_ml[place + k].x);
-                const float f0 = part_weight(top, l, most, a.c);
+                const float f0 = part_weight(top, l, most);
                 sum.x *= f0, sum.y *= f0, sum.z *= f0, sum.w *= f0;
                 l *= f0;
                 for (int k = 1; k < groups; ++k) {
                     const float2 w = lds_ml[place + k];
                     const float4 y = lds[threadIdx.x + k * kLanes];
-                    const float f = part_weight(w.x, w.y, most, a.c);
+                    const float f = part_weight(w.x, w.y, most);
                     l = fmaf(f, w.y, l);
                     sum.x = fmaf(f, y.x, sum.x);
                     sum.y = fmaf(f, y.y, sum.y);
@@ -543,9 +574,9 @@ __device__ __forceinline__ void row_reference(const QuantAttnArgs &a, const Quan
     }
     top = max16(top);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top, a.c) * v[k].y;
+    for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top) * v[k].y;
     sum = sum16(sum);
-    if (n == 0) *to = float2{top == -INFINITY ? 0.0f : top, sum == 0.0f ? 0.0f : 1.0f / sum};
+    if (n == 0) *to = float2{finite_or_zero(top), sum == 0.0f ? 0.0f : 1.0f / sum};
 }
 
 template <int D, int GR, typename T, int TILES>
@@ -592,7 +623,7 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
 #pragma unroll
-                for (int i = 0; i < S::KM; ++i) k[t][i] = operand_of(key.code[t].w[i]);
+                for (int i = 0; i < S::KM; ++i) k[t][i] = key_operand<S::kF32>(key.code[t].w[i]);
                 lo[t] = lo_operand<NG>(key.pair[t]);
                 pairs[t] = key.pair[t];
             }
@@ -614,12 +645,13 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
                     ref[i] = rl[16 * r + 4 * c + i];
                     seen[i] = row + i < sp.rows ? sp.seen(a, row + i) : 0;
                 }
+                const bool huge = __any(fmaxf(fmaxf(fabsf(ref[0].x), fabsf(ref[1].x)), fmaxf(fabsf(ref[2].x), fabsf(ref[3].x))) > kHuge);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const f32x4 s = logits<D, GR, T>(q, k[t], pairs[t], lo[t]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float p = __builtin_amdgcn_exp2f((s[i] - ref[i].x) * a.c) * ref[i].y;
+                        const float p = __builtin_amdgcn_exp2f(exponent(s[i], a.c, ref[i].x, huge)) * ref[i].y;
                         w[t] += u * kRun + 16 * t + n < seen[i] ? p : 0.0f;
                     }
                 }
@@ -639,15 +671,16 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
 // At most eight rows (a token of up to eight query heads per KV head, a few tokens of fewer): half of a 16 x 16 product's rows would be
 // idle.  The first product's are; its logits of slots 32 .. 63 of a run then move to the idle lanes, so that softmax, sums and steps are formed
 // once per logit: lane (n, c) has rows 4 (c & 1) + i at slots 16 t + 32 (c >> 1) + n, t = 0, 1.  The factors p step are formed there,
-// and go through LDS as bf16 terms, the first one in rows 0 .. 7 of the second product's operand and the second one in rows 8 .. 15
-// (fp32: the third one in a product of its own): one product for both, joined at the end.
+// and go through LDS.  bf16: as fp16 numbers, 11 bits, of a group's steps divided by a power of two that follows the greatest step the
+// wave has met (fp16 ends at 2^16).  fp32: as three bf16 terms, the first one in rows 0 .. 7 of the second product's operand, the second one in
+// rows 8 .. 15, the third one in a product of its own, joined at the end.
 //
 // The wave whose run has slots that the call appends writes them first.
 // ---------------------------------------------------------------------------------------
 template <int D, int GR, typename T>
 struct FewShape {
     using S = QuantShape<D, GR, T>;
-    static constexpr int kWStride = 144, kWRows = S::kF32 ? 24 : 16;  // bytes: 64 places of bf16 and 16 more, 16 rows on different banks
+    static constexpr int kWStride = 144, kWRows = S::kF32 ? 24 : 8;  // bytes: 64 places of 16 bits and 16 more, 16 rows on different banks
     static constexpr int kWBytes = S::NG * kWRows * kWStride, kWave = S::kVBytes + kWBytes;
     static constexpr int kLds = 4 * kWave > 4 * 8 * D * 4 + 4 * 8 * 8 ? 4 * kWave : 4 * 8 * D * 4 + 4 * 8 * 8;
 };
@@ -711,20 +744,31 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
     const int runs = (most + kRun - 1) / kRun, stride = 4 * a.splits;
     int u = split * 4 + wave;
     KeyRun<D, GR> key;
-    if (u < runs) {
-        if (append && (u + 1) * kRun > sp.held_before) append_run<D, GR, T>(a, sp, u * kRun);
-        key.load(kc, ks, u * kRun, sp.held);
+    if (append) {  // at most two runs have slots of its rows
+        const int first = sp.held_before < 0 ? 0 : sp.held_before / kRun;
+        for (int r = first; r < runs && r < first + 2; ++r)
+            if (r - a.by_stride.of(r) * stride == u) append_run<D, GR, T>(a, sp, r * kRun);
     }
+    if (u < runs) key.load(kc, ks, u * kRun, sp.held);
     QueryTile<D, GR, T> q;
     q.load(a, sp, n);
 
     f32x4 acc[S::NT];
-    float m[4], l[4], al[4][NG];
+    float m[4], limit[4], l[4], al[4][NG];
+    bool huge = false;
+    // bf16: (p step) is held times scale[g], a power of two; most[g]: the greatest step (a pair, its lower half set) that it is right for
+    float scale[NG];
+    uint32_t most_step[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        scale[g] = 1.0f;
+        most_step[g] = 0xffffu;
+    }
 #pragma unroll
     for (int i = 0; i < S::NT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        m[i] = -INFINITY;
+        m[i] = limit[i] = -INFINITY;
         l[i] = 0.0f;
 #pragma unroll
         for (int g = 0; g < NG; ++g) al[i][g] = 0.0f;
@@ -753,11 +797,10 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         for (int t = 0; t < 4; ++t) {
             uint4 k[S::KM];
 #pragma unroll
-            for (int i = 0; i < S::KM; ++i) k[i] = operand_of(key.code[t].w[i]);
+            for (int i = 0; i < S::KM; ++i) k[i] = key_operand<S::kF32>(key.code[t].w[i]);
             s4[t] = logits<D, GR, T>(q, k, key.pair[t], lo_operand<NG>(key.pair[t]));
-            if (t & 1) __builtin_amdgcn_sched_barrier(0);  // (operands of all four tiles at once do not fit the registers)
+            __builtin_amdgcn_sched_barrier(0);  // (operands of all four tiles at once do not fit the registers)
         }
-        if (append && next > u && (next + 1) * kRun > sp.held_before) append_run<D, GR, T>(a, sp, next * kRun);
         key.load(kc, ks, next * kRun, sp.held);
         f32x4 s[2];
 #pragma unroll
@@ -790,48 +833,101 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
             to[1] = uint2{code[i].z, code[i].w};
         }
         // ---- softmax against a running reference, raised when a logit lies more than kSlack above it
-        float top[4];
         bool raise = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            top[i] = max_halves(max16(fmaxf(s[0][i], s[1][i])));
-            raise = raise || (top[i] - m[i]) * a.c > kSlack;
-        }
+        for (int i = 0; i < 4; ++i) raise = raise || s[0][i] > limit[i] || s[1][i] > limit[i];
         if (__any(raise)) {
+            bool big = false;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool up = top[i] > m[i];
-                const float f = up ? __builtin_amdgcn_exp2f((m[i] - top[i]) * a.c) : 1.0f;
-                m[i] = up ? top[i] : m[i];
+                const float high = max_halves(max16(fmaxf(s[0][i], s[1][i]))), top = high * a.c;
+                const bool up = top > m[i];
+                const float f = up ? __builtin_amdgcn_exp2f(m[i] - top) : 1.0f;
+                m[i] = up ? top : m[i];
+                if (up) limit[i] = limit_of(high, top, a.c);
+                big = big || fabsf(finite_or_zero(m[i])) > kHuge;
                 l[i] *= f;
 #pragma unroll
                 for (int g = 0; g < NG; ++g) al[i][g] *= f;
 #pragma unroll
                 for (int j = 0; j < S::NT; ++j) acc[j][i] *= f;
             }
+            huge = huge || __any(big);
         }
+        if (!S::kF32) {
+            bool more = false;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) more = more || vp[0].w[g] > most_step[g] || vp[1].w[g] > most_step[g];
+            if (__any(more)) {
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const float greatest = max_halves(max16(fmaxf(step_of(vp[0].w[g]), step_of(vp[1].w[g]))));
+                    const bool up = __float_as_uint(greatest) > most_step[g];
+                    // times 2^-e: below 2; up to 32 times as much is right
+                    const int e = (int)(__float_as_uint(greatest) >> 23) - 127;
+                    const float next_scale = ldexpf(1.0f, -e), f = up ? next_scale / scale[g] : 1.0f;
+                    scale[g] = up ? next_scale : scale[g];
+                    most_step[g] = up ? __float_as_uint(greatest * 32.0f) | 0xffffu : most_step[g];
+#pragma unroll
+                    for (int j = g * (GR / 16); j < (g + 1) * (GR / 16); ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[j][i] *= f;
+                }
+            }
+        }
+        bool odd = false;  // a lo of NaN in a run that some row does not see all of: it counts only where the row sees it
+        if (masked) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) odd = odd || (vp[t].w[g] & 0x7f80u) == 0x7f80u;
+            odd = __any(odd);
+        }
+        float p[4][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float ref = m[i] == -INFINITY ? 0.0f : m[i];
-            float p[2];
+            const float ref = finite_or_zero(m[i]);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                p[t] = __builtin_amdgcn_exp2f((s[t][i] - ref) * a.c);
-                l[i] += p[t];
+                p[i][t] = __builtin_amdgcn_exp2f(exponent(s[t][i], a.c, ref, huge));
+                l[i] += p[i][t];
             }
-            uint8_t *to = wb + (4 * rc + i) * F::kWStride + 8 * n + 4 * upper;
+        }
+        if (__builtin_expect(odd, 0)) {
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    float lo = lo_of(vp[t].w[g]);
-                    if (masked) lo = s[t][i] == -INFINITY ? 0.0f : lo;  // (a lo of NaN counts only where the row sees it)
-                    al[i][g] = fmaf(p[t], lo, al[i][g]);
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) al[i][g] = fmaf(p[i][t], s[t][i] == -INFINITY ? 0.0f : lo_of(vp[t].w[g]), al[i][g]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) al[i][g] = fmaf(p[i][t], lo_of(vp[t].w[g]), al[i][g]);
+        }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            float step[2] = {step_of(vp[0].w[g]), step_of(vp[1].w[g])};
+            if (!S::kF32) {
+                step[0] *= scale[g];
+                step[1] *= scale[g];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint8_t *to = wb + (g * F::kWRows + 4 * rc + i) * F::kWStride + 8 * n + 4 * upper;
+                const float w0 = p[i][0] * step[0], w1 = p[i][1] * step[1];
+                if constexpr (S::kF32) {
+                    uint32_t w[3];
+                    split_pair<3>(w0, w1, w);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t *>(to + 8 * k * F::kWStride) = w[k];
+                } else {
+                    const f16x2 w = {(_Float16)w0, (_Float16)w1};
+                    *reinterpret_cast<uint32_t *>(to) = __builtin_bit_cast(uint32_t, w);
                 }
-                uint32_t w[S::PT];
-                split_pair<S::PT>(p[0] * step_of(vp[0].w[g]), p[1] * step_of(vp[1].w[g]), w);
-#pragma unroll
-                for (int k = 0; k < S::PT; ++k) *reinterpret_cast<uint32_t *>(to + (g * F::kWRows + 8 * k) * F::kWStride) = w[k];
             }
         }
         wave_sync();
@@ -841,7 +937,9 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + n) * F::kWStride + 32 * c + 16 * j);
+                if (g > 0) __builtin_amdgcn_sched_barrier(0);
+                // (bf16: rows 8 .. 15 are rows 0 .. 7 again)
+                const uint4 w = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + (S::kF32 ? n : n & 7)) * F::kWStride + 32 * c + 16 * j);
                 uint4 w3 = {0, 0, 0, 0};
                 if (S::kF32 && n < 8) w3 = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + 16 + n) * F::kWStride + 32 * c + 16 * j);
 #pragma unroll
@@ -849,9 +947,14 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
                     const int tile = g * (GR / 16) + x;
                     typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
                     const i32x2 vcode = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(v_read + 8 * tile));
-                    const uint4 v = operand_of((uint32_t)(j ? vcode.y : vcode.x));
-                    acc[tile] = mma<bf16_t>(w, v, acc[tile]);
-                    if (S::kF32) acc[tile] = mma<bf16_t>(w3, v, acc[tile]);
+                    if constexpr (S::kF32) {
+                        const uint4 v = operand_of((uint32_t)(j ? vcode.y : vcode.x));
+                        acc[tile] = mma<bf16_t>(w, v, acc[tile]);
+                        acc[tile] = mma<bf16_t>(w3, v, acc[tile]);
+                    } else {
+                        const uint4 v = operand16_of((uint32_t)(j ? vcode.y : vcode.x));
+                        acc[tile] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, v), acc[tile], 0, 0, 0);
+                    }
                 }
             }
         }
@@ -868,7 +971,7 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         for (int g = 0; g < NG; ++g) al[i][g] = add_halves(sum16(al[i][g]));
 #pragma unroll
         for (int j = 0; j < S::NT; ++j) {
-            const float o = add_halves(acc[j][i]) + al[i][j / (GR / 16)];
+            const float o = (S::kF32 ? add_halves(acc[j][i]) : acc[j][i] / scale[j / (GR / 16)]) + al[i][j / (GR / 16)];
             if (upper == 0) ob[(wave * 8 + 4 * rc + i) * D + 16 * j + n] = o;
         }
         if (n == 0 && upper == 0) mlb[wave * 8 + 4 * rc + i] = float2{m[i], l[i]};
@@ -881,7 +984,7 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         for (int w = 0; w < 4; ++w) high = fmaxf(high, mlb[w * 8 + row].x);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            f[w] = part_weight(mlb[w * 8 + row].x, mlb[w * 8 + row].y, high, a.c);
+            f[w] = part_weight(mlb[w * 8 + row].x, mlb[w * 8 + row].y, high);
             sum = fmaf(f[w], mlb[w * 8 + row].y, sum);
         }
         const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
@@ -935,8 +1038,13 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
     }
     __syncthreads();
     float2 ref[4];
+    bool huge = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ref[i] = rl[4 * (c & 1) + i];
+    for (int i = 0; i < 4; ++i) {
+        ref[i] = rl[4 * (c & 1) + i];
+        huge = huge || fabsf(ref[i].x) > kHuge;
+    }
+    huge = __any(huge);
     for (; u < runs; u += stride) {
         float w[2];
 #pragma unroll
@@ -945,7 +1053,7 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
             w[t] = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (4 * (c & 1) + i < sp.rows) w[t] = fmaf(__builtin_amdgcn_exp2f((x[i] - ref[i].x) * a.c), ref[i].y, w[t]);
+                if (4 * (c & 1) + i < sp.rows) w[t] = fmaf(__builtin_amdgcn_exp2f(exponent(x[i], a.c, ref[i].x, huge)), ref[i].y, w[t]);
             w[t] += __shfl_xor(w[t], 16, 64);
         }
 #pragma unroll
@@ -1050,6 +1158,7 @@ hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const Quan
     a.by_g = div_by(a.G);
     a.by_hkv = div_by(a.Hkv);
     a.by_splits = div_by(p.splits);
+    a.by_stride = div_by(4 * p.splits);
     const int pairs = c.batch * c.n_kv_heads;
 #define AIR_CASE(D, GR, T, F) \
     if (c.head_dim == D && c.group == GR && c.dtype == F) return run_quant_attn<D, GR, T>(s, a, p, pairs);

@@ -17,7 +17,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 __device__ __forceinline__ float lo_of(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float step_of(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
-// Eight codes as a matrix operand: the low halves of bytes 0..3, then the high ones.  A byte below 16 read as e4m3 is its value times 2^-9 (an
+// Eight codes as a matrix operand, halves of bytes in the order 0 2 4 6 1 3 5 7 (half 2 i: the low one of byte i).  A byte below 16 read as e4m3 is its value times 2^-9 (an
 // eighth's steps of 2^-6, below and above the least normal number alike), so that the conversion with a scale of 2^9 is exact.
 __device__ __forceinline__ uint4 operand_of(uint32_t codes) {
     const uint32_t lo = codes & 0x0f0f0f0fu, hi = (codes >> 4) & 0x0f0f0f0fu;
@@ -27,6 +27,34 @@ __device__ __forceinline__ uint4 operand_of(uint32_t codes) {
     r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, false));
     r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 512.0f, true));
     return r;
+}
+
+// The same in fp16
+__device__ __forceinline__ uint4 operand16_of(uint32_t codes) {
+    const uint32_t lo = codes & 0x0f0f0f0fu, hi = (codes >> 4) & 0x0f0f0f0fu;
+    uint4 r;
+    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.0f, false));
+    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.0f, true));
+    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, false));
+    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, true));
+    return r;
+}
+// Eight codes of K as the bf16 numbers 16 + code, elements in order: a code three bits up in the mantissa of 16.  Eight full-rate instructions where
+// the exact conversion takes three and four of half the rate; what the product has too much, 16 sum(q), is taken off by the product with
+// the sums.
+constexpr float kCodeBias = 16.0f;
+__device__ __forceinline__ uint4 biased_of(uint32_t codes) {
+    uint4 r;
+    r.x = (codes << 3 & 0x00780078u) | 0x41804180u;
+    r.y = (codes >> 1 & 0x00780078u) | 0x41804180u;
+    r.z = (codes >> 5 & 0x00780078u) | 0x41804180u;
+    r.w = (codes >> 9 & 0x00780078u) | 0x41804180u;
+    return r;
+}
+// bit of code i in a dword of eight: V in order; K in the order of biased_of
+template <bool K>
+__device__ __forceinline__ int code_shift(int i) {
+    return K ? 4 * (i >> 1) + 16 * (i & 1) : 4 * i;
 }
 
 // Two floats as TERMS packed pairs of bf16 whose sum they are: all terms but the last cut off behind eight bits, so that three are exact and
@@ -127,7 +155,7 @@ __device__ __forceinline__ void append_row(const T *src, uint32_t *codes, uint32
         const float d = x[i] - lo, q = d * inv;
         const float s = fmaf(fmaf(-q, step, d), inv, q);
         const uint32_t c = step > 0.0f ? (uint32_t)fminf(rintf(s), 15.0f) : 0u;
-        code |= c << (K ? (i & 3) * 8 + (i & 4) : 4 * i);
+        code |= c << code_shift<K>(i);
     }
     codes[dword_of<D, K>(p)] = code;
     if ((p & (GR / 8 - 1)) == 0) scales[p / (GR / 8)] = pair;
@@ -139,7 +167,7 @@ __device__ __forceinline__ void read_row(T *dst, const uint32_t *codes, const ui
     const float lo = lo_of(pair), step = step_of(pair);
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fmaf(step, (float)(code >> (K ? (i & 3) * 8 + (i & 4) : 4 * i) & 15u), lo);
+    for (int i = 0; i < 8; ++i) x[i] = fmaf(step, (float)(code >> code_shift<K>(i) & 15u), lo);
     store8(dst + 8 * p, x);
 }
 

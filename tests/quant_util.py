@@ -26,7 +26,7 @@ def values_of(x, group):
 
 
 def unpacked(cache):
-    """(lo, step code) of K and of V, fp64 [B][H][capacity][d], out of the cache's memory as the header lays it out."""
+    """(lo, step code, step) of K and of V, fp64 [B][H][capacity][d], out of the cache's memory as the header lays it out."""
     import torch
 
     out, d = [], cache.head_dim
@@ -35,35 +35,37 @@ def unpacked(cache):
         if i == 0:
             p = torch.arange(d // 8, device=codes.device)
             byte = (d // 8 * (p % 4) + 4 * (p // 4))[:, None] + torch.arange(4, device=codes.device)
-            c = c[..., byte, :].transpose(-1, -2).flatten(-3)  # [..., p, half, 4]
+            c = c[..., byte, :].flatten(-2)[..., [0, 4, 1, 5, 2, 6, 3, 7]].flatten(-2)  # [..., p, element]
         else:
             c = c.flatten(-2)
         pair = scales.double().unflatten(-1, (-1, 2))
         lo, step = (pair[..., j].repeat_interleave(cache.group, dim=-1) for j in range(2))
-        out.append((lo, step * c.double()))
+        out.append((lo, step * c.double(), step))
     return out
 
 
 def attention(cache, q, held, counts, causal, scale=None):
     """(out, its bound, weights, their bound) of every sequence, fp64: lists over the batch of [Hq][count][d] and [H][held].
 
-    Bounds: a logit is a sum of d products step q code and as many q lo, each exact or rounded to fp32, whose sums round once per term;
-    the exponent and the power of two (2^-22); sums of `held` terms; the factor p step keeps 16 bits (bf16: 2^-15) or 24; outputs are
-    rounded once."""
+    Bounds: a logit is a sum of d products step q code and as many q lo, each exact or rounded to fp32, whose sums round once per term (bf16:
+    codes have 16 added, and taken off again: 16 step q twice more); the exponent and the power of two (2^-22); sums of `held` terms; the factor
+    p step keeps 11 bits (bf16: half a step 2^-11, and of numbers below 2^-14 the absolute 2^-25, in units of at most the greatest step of the
+    group in the sequence, times a code) or 24; outputs are rounded once."""
     import torch
 
     d, H = cache.head_dim, cache.n_kv_heads
     g = q.shape[1] // H
     scale = scale or d ** -0.5
     half = 2.0 ** -8 if q.dtype == torch.bfloat16 else 2.0 ** -24
-    (klo, kst), (vlo, vst) = unpacked(cache)
+    (klo, kst, kstep), (vlo, vst, vstep) = unpacked(cache)
+    extra = 32.0 * kstep if q.dtype == torch.bfloat16 else 0.0 * kstep
     result = []
     for b, (n, c) in enumerate(zip(held, counts)):
         qs = q[b, :, :c].double()
-        kl, ks, vl, vs = (x[b, :, :n].repeat_interleave(g, dim=0) for x in (klo, kst, vlo, vst))
+        kl, ks, vl, vs, ke, vst1 = (x[b, :, :n].repeat_interleave(g, dim=0) for x in (klo, kst, vlo, vst, extra, vstep))
         t = lambda x: x.transpose(1, 2).contiguous()  # noqa: E731
         s = qs @ t(kl + ks) * scale
-        size = qs.abs() @ t(kl.abs() + ks) * scale
+        size = qs.abs() @ t(kl.abs() + ks + ke) * scale
         seen = torch.ones((c, n), dtype=torch.bool, device=q.device)
         if causal:
             seen = torch.arange(n, device=q.device)[None] <= torch.arange(c, device=q.device)[:, None] + (n - c)
@@ -76,8 +78,11 @@ def attention(cache, q, held, counts, causal, scale=None):
         rel = 2 * (torch.expm1(off) + 2.0 ** -22 + (n + 64) * 2.0 ** -24)
         vl_seen = torch.where(torch.isfinite(vl), vl, 0.0) if not bool(seen.all()) else vl
         o, a = p @ (vl_seen + vs), p @ (vl_seen.abs() + vs)
-        factor = 2.0 ** -15 if q.dtype == torch.bfloat16 else 2.0 ** -22
-        bound = (a * (rel + factor)) * 1.01 + (o.abs() + a * (rel + factor)) * half + 1e-37
+        low = half > 2.0 ** -20  # bf16
+        err = a * (rel + (2.0 ** -11 if low else 2.0 ** -22))
+        if low and n:
+            err = err + vst1.amax(1, keepdim=True) * (n * 15 * 2.0 ** -25)
+        bound = err * 1.01 + (o.abs() + err) * half + 1e-37
         w = p.reshape(H, g * c, n).sum(1)
         wb = (p * rel).reshape(H, g * c, n).sum(1) * 1.01 + w * (g * c + 8) * 2.0 ** -24 + 1e-37
         result.append((o, bound, w, wb))

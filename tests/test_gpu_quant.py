@@ -76,7 +76,7 @@ def test_rows_there_and_back(dtype, d, group, order):
     out = [torch.full((B, T, H, d), 42.0, dtype=dt, device="cuda:0").transpose(1, 2) for _ in range(2)]
     A.air_quant_read(cache, *out, starts=_ints(lens), counts=_ints(counts))
     raw = unpacked(cache)
-    for y, o, (lo, up) in zip(x, out, raw):
+    for y, o, (lo, up, _) in zip(x, out, raw):
         want, step = values_of(y, group)
         for b, (at, n) in enumerate(zip(lens, counts)):
             assert torch.equal((lo + up)[b, :, at:at + n], want[b, :, :n])  # the memory, as the header has it
@@ -121,7 +121,7 @@ def test_rows_outside_the_capacity_are_dropped():
     pos, w = torch.full((4, 2, 12), -7, dtype=torch.int32, device="cuda:0"), torch.full((4, 2, 12), 3.0, device="cuda:0")
     lens, counts = [8, -3, 2 ** 31 - 1, 12], [9, 2 ** 31 - 1, 9, -5]
     A.air_quant_append(cache, *x, lens=_ints(lens), counts=_ints(counts), positions=pos, first_positions=_ints([100, 200, 300, 400]), weights=w)
-    (lo, up), _ = unpacked(cache)
+    (lo, up, _), _ = unpacked(cache)
     want, _ = values_of(x[0], 32)
     got = lo + up
     assert torch.equal(got[0, :, 8:], want[0, :, :4]) and torch.equal(got[1, :, :6], want[1, :, 3:])
@@ -210,7 +210,7 @@ def test_append_and_attend(dtype, d, group):
     k, v = (_randn(10 + i, 4, hkv, T, d).to(_type(dtype)) for i in range(2))
     pos = torch.full((4, hkv, 510), -1, dtype=torch.int32, device="cuda:0")
     _check(A, cache, q, held, counts, True, lens=lens, k=k, v=v, positions=pos, first_positions=_ints([1000, 0, 5, 9]))
-    (lo, up), (vlo, vup) = unpacked(cache)
+    (lo, up, _), (vlo, vup, _) = unpacked(cache)
     for x, got in ((k, lo + up), (v, vlo + vup)):
         want, _ = values_of(x, group)
         for b, (at, n) in enumerate(zip(lens, counts)):
