@@ -372,7 +372,7 @@ air_status air_quant_read(void *stream, const air_quant_cache *cache, const air_
 
 typedef struct {
     int32_t n_q_heads, n_tokens; /* a multiple of the KV heads, at most 16384; queries of a sequence, with padding (0: nothing is done).
-                                    n_tokens x n_q_heads below 2^26                                                             */
+                                    n_tokens x n_q_heads below 2^26, times batch below 2^31                                     */
     int32_t causal;              /* 0: every query sees all slots held; 1: query t of n sees all but the last n - 1 - t        */
     int32_t max_len;             /* most slots that a sequence will hold when the call runs: only the launch's shape goes by it; 0: capacity */
     float scale;                 /* of the logits, > 0, at most 2^127; 0: 1 / sqrt(head_dim)                                  */
@@ -392,8 +392,9 @@ size_t air_quant_workspace_bytes(const air_quant_cache *cache, const air_quant_q
  *   out = sum_j p_j v_j,  p = softmax over the slots j that it sees of scale * q . k_j
  * and, with weights, weights[b][KV head][j] += sum of p_j over the queries and the query heads of the KV head, in a fixed order.
  * A query that sees no slot gives zero.  What lies in slots that a query does not see counts for nothing, whatever it stands for; a group
- * of NaN in a slot that it sees makes its part of the output (V) or all of it (K) NaN.  Products of codes are exact; logits,
- * sums and outputs are held in fp32 (with bf16 the factor of a code, p step, keeps 16 bits), outputs rounded once.
+ * of NaN in a slot that it sees makes its part of the output (V) or all of it (K) NaN.  fp32: products of codes are exact, everything
+ * else is held in fp32.  bf16: the same logits and sums, and factors p step of 11 to 16 bits for the second product; calls of 65 rows (queries
+ * x query heads per KV head) and more round what K stands for to 11 bits, what V stands for and the probabilities to bf16.  Outputs are rounded once.
  * Causal queries belong to the last counts slots of the sequence: after air_evict slots have no order, so a call of
  * more than one causal query appends its own rows.  workspace: 256-byte aligned, free for another call when this one's work has run.
  * out must not overlap an input; output rows that overlap are refused (AIR_ERR_SHAPE). */

@@ -27,6 +27,7 @@ SOURCES = {
     "air_cache.hip": [],
     "air_quant.hip": [],
     "air_quant_attn.hip": [],
+    "air_quant_many.hip": [],
     "air_evict.hip": [],
 }
 

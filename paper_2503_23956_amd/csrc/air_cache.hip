@@ -69,6 +69,8 @@ static air_status check_query(const char *who, const air_quant_cache *cache, con
     if (const char *bad = geometry(q.n_q_heads, cache->n_kv_heads, cache->head_dim, cache->dtype)) return refuse(AIR_ERR_SHAPE, "%s: %s", who, bad);
     if (q.n_tokens < 0 || (int64_t)q.n_tokens * q.n_q_heads >= (1 << 26))
         return refuse(AIR_ERR_SHAPE, "%s: n_tokens must not be negative, n_tokens x n_q_heads below 2^26", who);
+    if ((int64_t)q.n_tokens * q.n_q_heads * cache->batch >= (1ll << 31))
+        return refuse(AIR_ERR_SHAPE, "%s: batch x n_tokens x n_q_heads must be below 2^31", who);
     if (q.causal != 0 && q.causal != 1) return refuse(AIR_ERR_INVALID_ARG, "%s: causal must be 0 or 1", who);
     if (q.max_len < 0) return refuse(AIR_ERR_INVALID_ARG, "%s: max_len must not be negative", who);
     if (!(q.scale >= 0.f) || !isfinite(logit_factor(q.scale, cache->head_dim)))

@@ -10,58 +10,12 @@
 //
 // Waves share nothing until their ends: each deals itself every (4 splits)-th run of 64 slots, K requested one run ahead, and the four
 // partial results of a workgroup are joined in LDS.
-#include "air_device.h"
-#include "air_internal.h"
-#include "air_quant_dev.h"
+#include "air_quant_attn.h"
 
 namespace air {
 
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-
-struct QuantAttnArgs {
-    const uint8_t *kc, *vc;
-    const uint32_t *ks, *vs;
-    const void *q;
-    void *out;
-    float *part_o;    // [pair][split][row][D]
-    float2 *part_ml;  // [pair][split][row]
-    float *weights;
-    int64_t q_b, q_h, q_t, out_b, out_h, out_t;
-    const int32_t *lens, *counts;
-    float c;  // scale * log2(e)
-    int32_t Hkv, G, n_tokens, capacity, n_rows, splits, causal, appended;
-    Div by_g, by_hkv, by_splits, by_stride;  // by_stride: 4 splits
-    float4 *kept;      // [pair][run][2][lane]: logits, for the weights of calls with few rows; null: formed again
-    int32_t max_runs;  // runs of a pair there
-    QuantAppendArgs rows;  // what the first launch appends (few rows), else rows[0] null
-};
-
-constexpr int kRun = 64;  // slots that a wave takes at a time
+constexpr int kManyRows = 65;  // bf16: tiles of 128 and 256 rows from here on
 constexpr float kSlack = 8.0f;  // how far (base 2) a logit may lie above the reference of its row
-constexpr int kFewRows = 8;
-
-// What a sequence holds and asks
-struct QuantSpan {
-    int b, h, count, held, rows;
-    int held_before;  // where the call appends its first row
-    __device__ __forceinline__ QuantSpan(const QuantAttnArgs &a, int pair) {
-        b = a.by_hkv.of(pair);
-        h = pair - b * a.Hkv;
-        const int n = a.counts ? a.counts[b] : a.n_tokens;
-        count = n < 0 ? 0 : n > a.n_tokens ? a.n_tokens : n;
-        held_before = a.lens[b];
-        const int64_t all = (int64_t)held_before + (a.appended ? count : 0);
-        held = all < 0 ? 0 : all > a.capacity ? a.capacity : (int)all;
-        rows = count * a.G;
-    }
-    // slots that row r sees (r < rows)
-    __device__ __forceinline__ int seen(const QuantAttnArgs &a, int r) const {
-        if (!a.causal) return held;
-        const int s = held - count + 1 + a.by_g.of(r);
-        return s < 0 ? 0 : s;
-    }
-};
 
 template <int D, int GR, typename T>
 struct QuantShape {
@@ -204,7 +158,6 @@ __device__ __forceinline__ float exponent(float s, float c, float ref, bool huge
 __device__ __forceinline__ float limit_of(float high, float top, float c) {
     return fabsf(top) > kHuge ? high : (top + kSlack) * (1.0f / c);
 }
-__device__ __forceinline__ float finite_or_zero(float ref) { return ref == -INFINITY ? 0.0f : ref; }
 
 // What a wave requests ahead: 64 slots
 template <int D, int GR>
@@ -241,20 +194,6 @@ struct ValueRun {
         }
     }
 };
-
-// weight of sums taken against the reference m in sums against top
-__device__ __forceinline__ float part_weight(float m, float l, float top) {
-    if (m == -INFINITY) return l == 0.0f ? 0.0f : 1.0f;  // (no finite logit: nothing, or NaN that stays)
-    return __builtin_amdgcn_exp2f(m - top);
-}
-
-__device__ __forceinline__ void put(float *p, float v) { *p = v; }
-__device__ __forceinline__ void put(bf16_t *p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
-__device__ __forceinline__ void put4(float *p, const f32x4 &v) { *reinterpret_cast<f32x4 *>(p) = v; }
-__device__ __forceinline__ void put4(bf16_t *p, const f32x4 &v) {
-    const bf16x2 a = {(__bf16)v[0], (__bf16)v[1]}, b = {(__bf16)v[2], (__bf16)v[3]};
-    *reinterpret_cast<uint2 *>(p) = uint2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-}
 
 template <int D, int GR, typename T, int RT>
 __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantAttnArgs a) {
@@ -479,104 +418,6 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
             }
         }
     }
-}
-
-// Second launch of a (sequence, KV head): rows joined over the splits, and what every slot was attended to - the logits once more, now against
-// every row's maximum and sum.  The partial results of a row are requested all at once: a lane per split for (maximum, sum), and
-// for the outputs D / 4 lanes a split.
-template <int D, typename T>
-__device__ __forceinline__ void join_rows(const QuantAttnArgs &a, const QuantSpan &sp, int pair, float4 *lds) {
-    constexpr int kLanes = D / 4, kPlaces = 256 / kLanes;  // places: splits of a row side by side, and rows
-    int groups = 1;
-    while (groups < a.splits && groups < kPlaces) groups *= 2;
-    const int place = threadIdx.x / kLanes, x = threadIdx.x % kLanes, group = place & (groups - 1), lane = threadIdx.x & 63;
-    const int rows = kPlaces / groups;
-    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
-    for (int first = blockIdx.x * rows; first < sp.rows; first += gridDim.x * rows) {
-        const int row = first + place / groups, r = row < sp.rows ? row : sp.rows - 1;
-        const float4 *o = reinterpret_cast<const float4 *>(a.part_o + ((size_t)pair * a.splits * a.n_rows + r) * D) + x;
-        const size_t step = (size_t)a.n_rows * (D / 4);
-        float4 sum = {0.f, 0.f, 0.f, 0.f};
-        float top = -INFINITY, l = 0.0f;
-        float4 part[8];
-        float2 v[8];
-        for (int s0 = group; s0 < a.splits; s0 += 8 * groups) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int s = s0 + k * groups;
-                v[k] = float2{-INFINITY, 0.f};
-                part[k] = float4{0.f, 0.f, 0.f, 0.f};
-                if (s < a.splits) {
-                    v[k] = ml[(size_t)s * a.n_rows + r];
-                    part[k] = o[s * step];
-                }
-            }
-            float most = top;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) most = fmaxf(most, v[k].x);
-            const float f0 = part_weight(top, l, most);
-            sum.x *= f0, sum.y *= f0, sum.z *= f0, sum.w *= f0;
-            l *= f0;
-            top = most;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float f = part_weight(v[k].x, v[k].y, top);
-                l = fmaf(f, v[k].y, l);
-                sum.x = fmaf(f, part[k].x, sum.x);
-                sum.y = fmaf(f, part[k].y, sum.y);
-                sum.z = fmaf(f, part[k].z, sum.z);
-                sum.w = fmaf(f, part[k].w, sum.w);
-            }
-        }
-        if (groups > 1) {
-            __syncthreads();
-            lds[threadIdx.x] = sum;
-            float2 *lds_ml = reinterpret_cast<float2 *>(lds + 256);
-            if (x == 0) lds_ml[place] = float2{top, l};
-            __syncthreads();
-            if (group == 0) {
-                float most = top;
-                for (int k = 1; k < groups; ++k) most = fmaxf(most, lds_ml[place + k].x);
-                const float f0 = part_weight(top, l, most);
-                sum.x *= f0, sum.y *= f0, sum.z *= f0, sum.w *= f0;
-                l *= f0;
-                for (int k = 1; k < groups; ++k) {
-                    const float2 w = lds_ml[place + k];
-                    const float4 y = lds[threadIdx.x + k * kLanes];
-                    const float f = part_weight(w.x, w.y, most);
-                    l = fmaf(f, w.y, l);
-                    sum.x = fmaf(f, y.x, sum.x);
-                    sum.y = fmaf(f, y.y, sum.y);
-                    sum.z = fmaf(f, y.z, sum.z);
-                    sum.w = fmaf(f, y.w, sum.w);
-                }
-            }
-        }
-        if (group == 0 && row < sp.rows) {
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            const int t = a.by_g.of(row);
-            T *to = static_cast<T *>(a.out) + sp.b * a.out_b + ((int64_t)sp.h * a.G + row - t * a.G) * a.out_h + t * a.out_t + 4 * x;
-            put4(to, f32x4{sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv});
-        }
-    }
-}
-
-// (maximum, 1 / sum) of a row over the splits; by 16 lanes, n of them
-__device__ __forceinline__ void row_reference(const QuantAttnArgs &a, const QuantSpan &sp, int pair, int row, int n, float2 *to) {
-    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
-    float2 v[4];
-    float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        v[k] = float2{-INFINITY, 0.f};
-        if (n + 16 * k < a.splits && row < sp.rows) v[k] = ml[(size_t)(n + 16 * k) * a.n_rows + row];
-        top = fmaxf(top, v[k].x);
-    }
-    top = max16(top);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top) * v[k].y;
-    sum = sum16(sum);
-    if (n == 0) *to = float2{finite_or_zero(top), sum == 0.0f ? 0.0f : 1.0f / sum};
 }
 
 template <int D, int GR, typename T, int TILES>
@@ -1073,6 +914,27 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     p.few = rows <= kFewRows;
     p.row_tiles = rows > 16 && c.dtype == AIR_BF16 ? 2 : 1;  // (two tiles of fp32 queries, three terms each, do not fit the registers)
     p.row_blocks = (int)((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
+    p.max_len = (int)len;
+    if (rows >= kManyRows && c.dtype == AIR_BF16) {
+        const int64_t wgs256 = pairs * ((rows + 255) / 256);
+        p.tile_rows = wgs256 >= 256 ? 256 : 128;
+        p.row_blocks = (int)((rows + p.tile_rows - 1) / p.tile_rows);
+        const int64_t blocks = (len + 63) / 64, wgs = pairs * p.row_blocks, most = blocks / 4;
+        int64_t splits = wgs >= 256 ? 1 : 256 / wgs;
+        splits = splits > most ? most : splits;
+        p.splits = (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+        const size_t cells = (size_t)pairs * p.splits * rows;
+        if (p.splits > 1 || q.weights) p.ml_bytes = (cells * sizeof(float2) + 255) / 256 * 256;
+        p.l2_at = p.ml_bytes + (p.splits > 1 ? (cells * c.head_dim * sizeof(float) + 255) / 256 * 256 : 0);
+        p.bytes = p.l2_at + (q.weights ? (cells * sizeof(float) + 255) / 256 * 256 : 0);
+        p.max_len = c.capacity;
+        const int places = 1024 / c.head_dim;
+        int groups = 1;
+        while (groups < p.splits && groups < places) groups *= 2;
+        const int64_t n = (rows + places / groups - 1) / (places / groups), most_wgs = (4096 + pairs - 1) / pairs;
+        p.finish = (int)(n < most_wgs ? n : most_wgs);
+        return p;
+    }
     const int64_t runs = (len + 4 * kRun - 1) / (4 * kRun), wanted = 512 / (pairs * p.row_blocks);  // two workgroups a CU
     p.splits = (int)(wanted < 1 ? 1 : wanted < runs ? wanted : runs);
     if (p.splits > 64) p.splits = 64;
@@ -1136,7 +998,7 @@ hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const Quan
     a.q = q.q;
     a.out = q.out;
     a.part_ml = p.bytes ? static_cast<float2 *>(workspace) : nullptr;
-    a.part_o = p.splits > 1 ? reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.ml_bytes) : nullptr;
+    a.part_o = p.splits > 1 && workspace ? reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.ml_bytes) : nullptr;
     a.weights = q.weights;
     a.q_b = q.q_b;
     a.q_h = q.q_h;
@@ -1160,6 +1022,10 @@ hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const Quan
     a.by_splits = div_by(p.splits);
     a.by_stride = div_by(4 * p.splits);
     const int pairs = c.batch * c.n_kv_heads;
+    a.pairs = pairs;
+    a.by_pairs = div_by(pairs);
+    a.part_l2 = p.tile_rows ? reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.l2_at) : nullptr;
+    if (p.tile_rows) return launch_quant_many(s, a, p, c.head_dim, c.group, pairs);
 #define AIR_CASE(D, GR, T, F) \
     if (c.head_dim == D && c.group == GR && c.dtype == F) return run_quant_attn<D, GR, T>(s, a, p, pairs);
     AIR_CASE(128, 32, bf16_t, AIR_BF16)

@@ -1,0 +1,595 @@
+// air_quant_attn, bf16 calls of many rows (windows of queries, pieces of prompts): codes become 16-bit tiles in LDS once for 128 or 256 rows.
+//
+// The products are those of a prompt's attention: eight waves of 32 rows, transposed 32 x 32 tiles (S^T = K Q^T, O^T = V^T P^T: a row's logits,
+// probabilities and accumulators stay in two lanes), key blocks of 64 in three buffers, the codes of the block after next on their way, a
+// wave's next logits formed under the exponentials of its present ones.  What differs is how a block gets into LDS: a thread turns 16
+// codes of K and 16 of V into numbers, lo + step code in fp32, rounded once:
+//   K to fp16, 11 bits (bf16's 8 would cost a logit 2^-9 of sum |q k|).  Queries go to fp16 too, exactly: rows of either whose greatest
+//   magnitude lies outside 2^-6 .. 2^14 are held divided by a power of two, and their logits multiplied by it;
+//   V to bf16, like the probabilities, which have to hold any magnitude.
+// Per 32 x 64 logits a wave issues 16 + 16 products of 32 clocks; dequantising costs about 70 vector instructions a wave and block.
+#include "air_block.h"
+#include "air_quant_attn.h"
+
+namespace air {
+
+constexpr float kLeast = 0x1p-6f, kMost = 0x1p14f;  // magnitudes held as they are
+
+__device__ __forceinline__ f32x16 mma32_f16(const uint4 &a, const uint4 &b, f32x16 acc) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
+}
+// the power of two that brings a greatest magnitude outside the bounds to 1 .. 2; else 1
+__device__ __forceinline__ float unit_of(float greatest) {
+    if (!(greatest > kMost || greatest < kLeast) || greatest == 0.0f) return 1.0f;
+    const int e = (int)(__float_as_uint(greatest) >> 23);  // (a subnormal number counts as 2^-126, an infinity as 2^126)
+    return __uint_as_float((uint32_t)(e < 1 ? 1 : e > 253 ? 253 : e) << 23);
+}
+// eight elements of a query divided by the row's unit
+__device__ __forceinline__ uint4 to_f16(const uint4 &x, float inv) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f16x2 v = {(_Float16)(__uint_as_float(w[i] << 16) * inv), (_Float16)(__uint_as_float(w[i] & 0xffff0000u) * inv)};
+        r[i] = __builtin_bit_cast(uint32_t, v);
+    }
+    return uint4{r[0], r[1], r[2], r[3]};
+}
+__device__ __forceinline__ float greatest_of(const uint4 &x, float most) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+    return most;
+}
+__device__ __forceinline__ float byte_of(uint32_t x, int i) { return (float)(x >> (8 * i) & 0xffu); }  // (one conversion)
+// what eight codes of K stand for, in fp16
+__device__ __forceinline__ uint4 key_values(uint32_t codes, float lo, float step) {
+    const uint32_t a = codes & 0x0f0f0f0fu, b = codes >> 4 & 0x0f0f0f0fu;  // elements 0 4 1 5 and 2 6 3 7
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[(i >> 1) + 4 * (i & 1)] = fmaf(step, byte_of(a, i), lo);
+        x[2 + (i >> 1) + 4 * (i & 1)] = fmaf(step, byte_of(b, i), lo);
+    }
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f16x2 v = {(_Float16)x[2 * i], (_Float16)x[2 * i + 1]};
+        r[i] = __builtin_bit_cast(uint32_t, v);
+    }
+    return uint4{r[0], r[1], r[2], r[3]};
+}
+// what eight codes of V stand for, in bf16
+__device__ __forceinline__ uint4 values(uint32_t codes, float lo, float step) {
+    const uint32_t a = codes & 0x0f0f0f0fu, b = codes >> 4 & 0x0f0f0f0fu;  // even and odd elements
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bf16x2 v = {(__bf16)fmaf(step, byte_of(a, i), lo), (__bf16)fmaf(step, byte_of(b, i), lo)};
+        r[i] = __builtin_bit_cast(uint32_t, v);
+    }
+    return uint4{r[0], r[1], r[2], r[3]};
+}
+
+// A thread's part of a block of 64 slots: slot thread / 8, and of its rows the piece thread % 8 (8 bytes of codes, 4 with heads of 64)
+template <int D, int GR>
+struct CodeStage {
+    using R = Row<bf16_t, D>;
+    static constexpr int kWords = D / 64, kPairs = GR == 32 ? kWords : 1;  // dwords of codes; pairs of K that belong to them
+    int key, piece;
+    uint32_t k[kWords], v[kWords], kp[kPairs], vp;
+
+    __device__ __forceinline__ void init(int thread) {
+        key = thread >> 3;
+        piece = thread & 7;
+    }
+    // group of K's dword w: elements 32 m + ..., m = w % (D / 32)
+    __device__ __forceinline__ int key_group() const { return D == 128 ? (GR == 32 ? 2 * (piece & 1) : piece & 1) : (GR == 32 ? piece & 1 : 0); }
+    __device__ __forceinline__ int value_group() const { return (D == 128 ? 16 : 8) * piece / GR; }
+    __device__ __forceinline__ void load(const uint8_t *kc, const uint8_t *vc, const uint32_t *ks, const uint32_t *vs, int slot0, int held) {
+        const int at = slot0 + key;
+        const uint32_t slot = at < held ? at : held - 1;
+        if (kWords == 2) {
+            const uint2 a = *reinterpret_cast<const uint2 *>(kc + (slot * (D / 2) + 8 * piece)), b = *reinterpret_cast<const uint2 *>(vc + (slot * (D / 2) + 8 * piece));
+            k[0] = a.x, k[kWords - 1] = a.y, v[0] = b.x, v[kWords - 1] = b.y;
+        } else {
+            k[0] = *reinterpret_cast<const uint32_t *>(kc + (slot * (D / 2) + 4 * piece));
+            v[0] = *reinterpret_cast<const uint32_t *>(vc + (slot * (D / 2) + 4 * piece));
+        }
+        const uint32_t *pairs = ks + slot * (D / GR) + key_group();
+        if (kPairs == 2) {
+            const uint2 p = *reinterpret_cast<const uint2 *>(pairs);
+            kp[0] = p.x, kp[kPairs - 1] = p.y;
+        } else {
+            kp[0] = *pairs;
+        }
+        vp = vs[slot * (D / GR) + value_group()];
+    }
+    // Into LDS; unit[key]: what the key was divided by (true: some key by more than 1).  Of a block that some row does not see all of, `left` slots from
+    // its first are held: values behind them and of groups of NaN become 0 (bad: there were some)
+    __device__ __forceinline__ bool store(u32x4 *sk, u32x4 *sv, float *unit, bool part, int left, bool &bad) {
+        float lo[kPairs], step[kPairs], most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            lo[i] = lo_of(kp[i]);
+            step[i] = step_of(kp[i]);
+            most = fmaxf(most, fmaxf(fabsf(lo[i]), fabsf(fmaf(15.0f, step[i], lo[i]))));
+        }
+        most = max8(most);
+        const float u = unit_of(most);
+        if (u != 1.0f) {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                lo[i] /= u;
+                step[i] /= u;
+            }
+        }
+        if (piece == 0) unit[key] = u;
+        u32x4 *tk = sk + (key >> 5) * R::kKTile, *tv = sv + (key >> 5) * R::kVTile;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const int w = kWords * piece + i, nq = w / (D / 32), m = w % (D / 32);
+            tk[R::k_at(key & 31, 4 * m + nq)] = __builtin_bit_cast(u32x4, key_values(k[i], lo[i % kPairs], step[i % kPairs]));
+        }
+        float vlo = lo_of(vp), vstep = step_of(vp);
+        if (part) {
+            const bool nan = (vp & 0x7f80u) == 0x7f80u && key < left;
+            bad = bad || nan;
+            if (nan || key >= left) vlo = vstep = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) tv[R::v_at(key & 31, kWords * piece + i)] = __builtin_bit_cast(u32x4, values(v[i], vlo, vstep));
+        return u != 1.0f;
+    }
+};
+
+// KW 1: 256 rows, every wave takes both halves of a block.  KW 2: 128 rows, two waves share 32 rows and take a half of every block each.
+// WEIGH: a second sum, of the probabilities as they were before they were rounded, for the weights of the slots.
+template <int D, int GR, int KW, bool WEIGH>
+__global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
+    using R = Row<bf16_t, D>;
+    constexpr int NW = 8, RW = NW / KW, kRows = 32 * RW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
+    __shared__ u32x4 tiles[2 * kBufs * (R::kKTile + R::kVTile)];
+    __shared__ float units[kBufs][kKeys];
+    __shared__ float2 s_ml[KW == 2 ? RW * 32 : 1];
+    __shared__ float s_l2[KW == 2 ? RW * 32 : 1];
+    __shared__ int s_bad, s_units;
+    auto sk = [&](int b) { return tiles + b % kBufs * (2 * R::kKTile); };  // the two tiles of block b
+    auto sv = [&](int b) { return tiles + 2 * kBufs * R::kKTile + b % kBufs * (2 * R::kVTile); };
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rw = wave % RW, kw = wave / RW;
+    const int y = a.by_pairs.of(blockIdx.x), pair = blockIdx.x - y * a.pairs;  // (pairs fastest: an XCD's workgroups share K and V)
+    const QuantSpan sp(a, pair);
+    const int rank = a.by_splits.of(y), split = y - rank * a.splits;
+    const int n_tiles = (sp.rows + kRows - 1) / kRows, tile = n_tiles - 1 - rank;  // (the longest first)
+    if (tile < 0) return;
+    const int row0 = tile * kRows, end_row = min(row0 + kRows, sp.rows);
+    const int see_all = sp.seen(a, row0), see_any = sp.seen(a, end_row - 1);
+    const int n_blocks = (see_any + kKeys - 1) / kKeys;
+    const int per_split = (n_blocks + a.splits - 1) / a.splits;
+    const int b0 = split * per_split, b1 = min(n_blocks, b0 + per_split);
+
+    f32x16 acc[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+    float l = 0.f, l2 = 0.f, ref = -INFINITY, top = -INFINITY, sub = 0.f;  // top: the logit (scaled) from which on the reference is raised
+    bool huge = false;
+    const int row = row0 + 32 * rw + n, m_row = min(row, sp.rows - 1), tok = a.by_g.of(m_row);
+    const int64_t head = (int64_t)sp.h * a.G + m_row - tok * a.G;
+    const int last = sp.seen(a, m_row) - 1;
+    uint4 q[NS];
+    float row_c = a.c;  // factor of the row's logits
+    {
+        const bf16_t *qp = (const bf16_t *)a.q + sp.b * a.q_b + tok * a.q_t + head * a.q_h;
+        float most = 0.f;
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) {
+            q[sl] = *reinterpret_cast<const uint4 *>(qp + R::kVec * (2 * sl + h));
+            most = greatest_of(q[sl], most);
+        }
+        const float unit = unit_of(fmaxf(most, __shfl_xor(most, 32)));
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) q[sl] = to_f16(q[sl], 1.0f / unit);
+        row_c *= unit;
+    }
+    float mul = row_c;
+
+    const size_t base = (size_t)pair * a.capacity;
+    const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
+    const uint32_t *ks = a.ks + base * (D / GR), *vs = a.vs + base * (D / GR);
+    CodeStage<D, GR> stage;
+    stage.init(threadIdx.x);
+    auto load = [&](int b) {
+        if (b < b1) stage.load(kc, vc, ks, vs, b * kKeys, sp.held);
+    };
+    auto keep = [&](int b) {
+        if (b >= b1) return;
+        bool bad = false;
+        if (stage.store(sk(b), sv(b), units[b % kBufs], (b + 1) * kKeys > see_all, sp.held - b * kKeys, bad)) s_units = 1;
+        if (bad) s_bad = 1;
+    };
+    auto read_k = [&](u32x4(&x)[NS], const u32x4 *sk_) {
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) x[sl] = sk_[R::k_at(n, 2 * sl + h)];
+    };
+    auto logits = [&](f32x16 &s, const u32x4(&x)[NS]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) s = mma32_f16(__builtin_bit_cast(uint4, x[sl]), q[sl], s);
+    };
+    // units, masks, reference: what has to be known of the logits of the keys from kb on before their exponentials are formed
+    auto settle = [&](f32x16 &s, float mx, int kb) {
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(s_units), 0)) {
+            const float *u = units[kb / kKeys % kBufs] + (kb & 32);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] *= u[8 * (i >> 2) + 4 * h + (i & 3)];
+            mx = largest(s);
+        }
+        if (__builtin_expect(kb + 32 > see_all, 0)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (kb + 8 * (i >> 2) + 4 * h + (i & 3) > last) s[i] = -INFINITY;
+            mx = largest(s);
+        }
+        mx *= row_c;
+        if (__builtin_expect(__ballot(mx > top) != 0ull, 0)) {
+            const float now = fmaxf(ref, fmaxf(mx, __shfl_xor(mx, 32, 64)));
+            const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - now);  // no logit but -inf yet: nothing to scale
+            l *= f;
+            l2 *= f;
+            ref = now;
+            top = now + kSlack;
+            sub = finite_or_zero(now);
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+            huge = huge || __ballot(fabsf(sub) > kHuge) != 0ull;
+        }
+        if (__builtin_expect(huge, 0)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = rounded_exponent(s[i], row_c, finite_or_zero(ref));
+            mul = 1.f;
+            sub = 0.f;
+        }
+    };
+    const int v_at = v_lane(lane);
+    // The next 32 keys' logits into `next` (operands: kf), their largest into mx, while the values of this 32 keys are weighed; kf then
+    // takes the operands of the keys behind those.  meet: the tile that k_after points to is whole only behind a barrier.
+    auto turn = [&](f32x16 &s, f32x16 &next, float &mx, u32x4(&kf)[NS], const u32x4 *sv_, const u32x4 *k_after, bool meet) {
+        uint4 vf[2][ND], p[2];
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) vf[0][d] = read_v<D>(sv_, v_at, 0, d);
+        logits(next, kf);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            bf16x8 x;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[8 * half + i], mul, -sub));
+                if (WEIGH) l2 += e;
+                x[i] = (__bf16)e;
+            }
+            p[half] = __builtin_bit_cast(uint4, x);
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d) vf[1][d] = read_v<D>(sv_, v_at, 1, d);
+        if (meet) lds_barrier();
+        read_k(kf, k_after);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) acc[d] = mma32(vf[half][d], p[half], acc[d], bf16_t());
+        l = sum_of(p[1], sum_of(p[0], l));  // the sum of what the second product takes: the outputs' weights add up to one as they are used
+        mx = largest(next);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    if (threadIdx.x == 0) s_bad = s_units = 0;
+    __syncthreads();
+    if (b0 < b1) {
+        f32x16 sa, sb;
+        float mx;
+        u32x4 kf[NS];
+        load(b0);
+        keep(b0);
+        load(b0 + 1);
+        if constexpr (KW == 2) {
+            keep(b0 + 1);
+            load(b0 + 2);
+        }
+        lds_barrier();
+        read_k(kf, sk(b0) + kw * R::kKTile);
+        logits(sa, kf);
+        settle(sa, largest(sa), b0 * kKeys + 32 * kw);
+        // (behind the last block: logits of whatever lies there, not used)
+        if constexpr (KW == 1) {
+            read_k(kf, sk(b0) + R::kKTile);
+            for (int b = b0; b < b1; ++b) {
+                const u32x4 *v_now = sv(b), *k_next = sk(b + 1);
+                keep(b + 1);  // (into the buffer of block b - 2, which every wave has left before the last barrier)
+                load(b + 2);
+                turn(sa, sb, mx, kf, v_now, k_next, true);
+                settle(sb, mx, b * kKeys + 32);
+                turn(sb, sa, mx, kf, v_now + R::kVTile, k_next + R::kKTile, false);
+                if (b + 1 < b1) settle(sa, mx, (b + 1) * kKeys);
+            }
+        } else {
+            read_k(kf, sk(b0 + 1) + kw * R::kKTile);
+            auto block = [&](int b, f32x16 &s, f32x16 &next) {
+                keep(b + 2);  // (into the buffer of block b - 1: its values were read before the last barrier)
+                load(b + 3);
+                turn(s, next, mx, kf, sv(b) + kw * R::kVTile, sk(b + 2) + kw * R::kKTile, true);
+                if (b + 1 < b1) settle(next, mx, (b + 1) * kKeys + 32 * kw);
+            };
+            for (int b = b0; b < b1; b += 2) {
+                block(b, sa, sb);
+                if (b + 1 < b1) block(b + 1, sb, sa);
+            }
+        }
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (WEIGH) l2 += __shfl_xor(l2, 32, 64);
+    if constexpr (KW == 2) {  // the two waves of 32 rows: lane by lane
+        static_assert(sizeof(tiles) >= RW * 32 * D * sizeof(float), "the tiles' memory holds the sums of half the waves");
+        f32x4 *sums = reinterpret_cast<f32x4 *>(tiles) + rw * (4 * ND * 64) + lane;
+        lds_barrier();
+        if (kw == 1) {
+            if (h == 0) {
+                s_ml[rw * 32 + n] = make_float2(ref, l);
+                s_l2[rw * 32 + n] = l2;
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sums[(4 * d + i) * 64] = (f32x4){acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+        }
+        lds_barrier();
+        if (kw == 1) return;
+        const float2 other = s_ml[rw * 32 + n];
+        const float now = fmaxf(ref, other.x);
+        const float f0 = part_weight(ref, l, now), f1 = part_weight(other.x, other.y, now);
+        ref = now;
+        l = l * f0 + other.y * f1;
+        if (WEIGH) l2 = l2 * f0 + s_l2[rw * 32 + n] * f1;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 x = sums[(4 * d + i) * 64];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[d][4 * i + j] = acc[d][4 * i + j] * f0 + x[j] * f1;
+            }
+    }
+    if (s_bad) {  // groups of NaN that were taken out, for the rows that see them
+        for (int key = max(b0 * kKeys, see_all / kKeys * kKeys); key < min(b1 * kKeys, see_any) && key <= last; ++key)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                if ((vs[key * (D / GR) + 32 * d / GR] & 0x7f80u) == 0x7f80u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[d][i] = NAN;
+    }
+    const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
+    if (row < sp.rows && h == 0) {
+        if (a.part_ml) a.part_ml[part] = make_float2(ref, l);
+        if (WEIGH) a.part_l2[part] = l2;
+    }
+    if (a.splits == 1) {
+        if (!a.out) return;
+        // through LDS (clear of the sums above), so that a row leaves in whole lines
+        const float inv = 1.0f / l;
+        if (KW == 1) lds_barrier();
+        u32x4 *rows = (rw < 4 ? sv(1) : sk(1)) + (rw & 3) * (32 * R::kPieces);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f32x4 o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : acc[d][4 * i + j] * inv;
+                store4(reinterpret_cast<bf16_t *>(rows + n * R::kPieces + ((4 * d + i) ^ (n & (R::kPieces - 1)))) + 4 * h, o);
+            }
+        wave_sync();
+        bf16_t *out = (bf16_t *)a.out + sp.b * a.out_b + R::kVec * (lane % R::kPieces);
+#pragma unroll
+        for (int i = 0; i < R::kPieces / 2; ++i) {
+            const int r = lane / R::kPieces + (64 / R::kPieces) * i, m = row0 + 32 * rw + r;
+            const u32x4 o = rows[r * R::kPieces + ((lane % R::kPieces) ^ (r & (R::kPieces - 1)))];
+            const int to = a.by_g.of(m), hd = sp.h * a.G + m - to * a.G;
+            if (m < sp.rows) *reinterpret_cast<u32x4 *>(out + to * a.out_t + hd * a.out_h) = o;
+        }
+    } else if (row < sp.rows && a.out) {
+        float *po = a.part_o + part * D + 4 * h;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store4(po + 32 * d + 8 * i, (f32x4){acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]});
+    }
+}
+
+__global__ __launch_bounds__(256) void quant_join_kernel_128(QuantAttnArgs a) {
+    __shared__ float4 jl[256 + 8];
+    const int pair = blockIdx.y;
+    const QuantSpan sp(a, pair);
+    if (sp.rows > 0) join_rows<128, bf16_t>(a, sp, pair, jl);
+}
+__global__ __launch_bounds__(256) void quant_join_kernel_64(QuantAttnArgs a) {
+    __shared__ float4 jl[256 + 16 / 2];
+    const int pair = blockIdx.y;
+    const QuantSpan sp(a, pair);
+    if (sp.rows > 0) join_rows<64, bf16_t>(a, sp, pair, jl);
+}
+
+// The slots' weights: a wave has 64 slots, their keys as operands in registers, and meets all rows, 32 at a time, which the workgroup's
+// eight waves share in LDS.  S^T again: a lane has one row, its reference and sum, and adds up that row's share of 32 slots over all tiles of rows;
+// the lanes are added at the end, in a fixed order.
+template <int D, int GR>
+__global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArgs a) {
+    using R = Row<bf16_t, D>;
+    constexpr int NS = R::kSlices, NG = D / GR, kTiles = 4;  // tiles of rows at a time
+    __shared__ u32x4 qs[kTiles][R::kKTile];
+    __shared__ float4 rs[kTiles * 32];  // factor, reference, 1 / sum, slots seen
+    __shared__ float units[8][64];
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int y = a.by_pairs.of(blockIdx.x), pair = blockIdx.x - y * a.pairs;
+    const QuantSpan sp(a, pair);
+    const int slot0 = (y * 8 + wave) * 64;
+    if (y * 512 >= sp.held || sp.rows == 0) return;
+    const bool idle = slot0 >= sp.held;
+
+    const size_t base = (size_t)pair * a.capacity;
+    const uint8_t *kc = a.kc + base * (D / 2);
+    const uint32_t *ks = a.ks + base * NG;
+    // keys: lane (n, h) has elements 8 (2 sl + h) .. + 7 of slots slot0 + n and + 32
+    uint4 k[2][NS];
+    bool scaled = false;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int at = slot0 + 32 * t + n;
+        const uint32_t slot = at < sp.held ? at : sp.held - 1;
+        uint32_t w[2][D / 32], pr[NG];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint8_t *from = kc + (slot * (D / 2) + D / 8 * (h + 2 * i));
+            if (D == 128) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(from);
+                w[i][0] = x.x, w[i][1] = x.y, w[i][2 % (D / 32)] = x.z, w[i][3 % (D / 32)] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(from);
+                w[i][0] = x.x, w[i][1] = x.y;
+            }
+        }
+        float most = 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            pr[g] = ks[slot * NG + g];
+            most = fmaxf(most, fmaxf(fabsf(lo_of(pr[g])), fabsf(fmaf(15.0f, step_of(pr[g]), lo_of(pr[g])))));
+        }
+        const float u = unit_of(most), inv = 1.0f / u;
+        scaled = scaled || u != 1.0f;
+        if (h == 0) units[wave][32 * t + n] = u;
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) {  // piece 2 sl + h = 4 m + nq
+            const int m = sl >> 1;
+            const uint32_t p = pr[32 * m / GR];
+            k[t][sl] = key_values(w[sl & 1][m], lo_of(p) * inv, step_of(p) * inv);
+        }
+    }
+    scaled = __any(scaled);
+    f32x16 w[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[t][i] = 0.f;
+
+    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
+    const float *l2 = a.part_l2 + (size_t)pair * a.splits * a.n_rows;
+    constexpr int kLanes = D / 8, kPer = 512 / kLanes;  // threads of a row; rows of a round
+    for (int row0 = 0; row0 < sp.rows; row0 += 32 * kTiles) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 32 * kTiles / kPer; ++i) {
+            const int x = i * kPer + threadIdx.x / kLanes, piece = threadIdx.x % kLanes, row = row0 + x;
+            const int r = row < sp.rows ? row : sp.rows - 1, tok = a.by_g.of(r);
+            const bf16_t *qp = (const bf16_t *)a.q + sp.b * a.q_b + tok * a.q_t + ((int64_t)sp.h * a.G + r - tok * a.G) * a.q_h + 8 * piece;
+            const uint4 q = *reinterpret_cast<const uint4 *>(qp);
+            float most = greatest_of(q, 0.f);
+            most = kLanes == 16 ? max16(most) : max8(most);
+            const float unit = unit_of(most);
+            qs[x >> 5][R::k_at(x & 31, piece)] = __builtin_bit_cast(u32x4, to_f16(q, 1.0f / unit));
+            if (piece == 0) {
+                float top = -INFINITY, sum = 0.f;
+                for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[(size_t)s * a.n_rows + r].x);
+                for (int s = 0; s < a.splits; ++s) {
+                    const float v = l2[(size_t)s * a.n_rows + r];
+                    sum = fmaf(part_weight(ml[(size_t)s * a.n_rows + r].x, v, top), v, sum);
+                }
+                rs[x] = float4{a.c * unit, finite_or_zero(top), sum == 0.f || row >= sp.rows ? 0.f : 1.0f / sum, __int_as_float(sp.seen(a, r))};
+            }
+        }
+        __syncthreads();
+        if (idle) continue;
+        const int tiles = min(kTiles, (sp.rows - row0 + 31) / 32), all = sp.seen(a, row0);
+        for (int t = 0; t < tiles; ++t) {
+            const float4 ref = rs[32 * t + n];
+            u32x4 q[NS];
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) q[sl] = qs[t][R::k_at(n, 2 * sl + h)];
+            const bool huge = __any(fabsf(ref.y) > kHuge);
+            const int last = __float_as_int(ref.w) - 1;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                f32x16 s;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+                for (int sl = 0; sl < NS; ++sl) s = mma32_f16(k[x][sl], __builtin_bit_cast(uint4, q[sl]), s);
+                if (__builtin_expect(scaled, 0)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] *= units[wave][32 * x + 8 * (i >> 2) + 4 * h + (i & 3)];
+                }
+                if (__builtin_expect(slot0 + 32 * x + 32 > all, 0)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (slot0 + 32 * x + 8 * (i >> 2) + 4 * h + (i & 3) > last) s[i] = -INFINITY;
+                }
+                if (__builtin_expect(huge, 0)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[x][i] = fmaf(__builtin_amdgcn_exp2f(rounded_exponent(s[i], ref.x, ref.y)), ref.z, w[x][i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[x][i] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], ref.x, -ref.y)), ref.z, w[x][i]);
+                }
+            }
+        }
+    }
+    if (idle) return;
+    float *weights = a.weights + base;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        float mine = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float v = sum16(w[x][i]);
+            v += __shfl_xor(v, 16, 64);
+            mine = n == i ? v : mine;
+        }
+        const int slot = slot0 + 32 * x + 8 * (n >> 2) + 4 * h + (n & 3);
+        if (n < 16 && slot < sp.held) weights[slot] += mine;
+    }
+}
+
+template <int D, int GR>
+static hipError_t run_many(hipStream_t s, const QuantAttnArgs &a, const QuantPlan &p, int pairs) {
+    const dim3 grid((unsigned)((int64_t)p.splits * p.row_blocks * pairs));
+    if (p.tile_rows == 256) {
+        if (a.weights) quant_many_kernel<D, GR, 1, true><<<grid, 512, 0, s>>>(a);
+        else quant_many_kernel<D, GR, 1, false><<<grid, 512, 0, s>>>(a);
+    } else {
+        if (a.weights) quant_many_kernel<D, GR, 2, true><<<grid, 512, 0, s>>>(a);
+        else quant_many_kernel<D, GR, 2, false><<<grid, 512, 0, s>>>(a);
+    }
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && p.splits > 1 && a.out) {
+        if (D == 128) quant_join_kernel_128<<<dim3((unsigned)p.finish, (unsigned)pairs), 256, 0, s>>>(a);
+        else quant_join_kernel_64<<<dim3((unsigned)p.finish, (unsigned)pairs), 256, 0, s>>>(a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && a.weights) {
+        quant_many_weights_kernel<D, GR><<<dim3((unsigned)((int64_t)(p.max_len + 511) / 512 * pairs)), 512, 0, s>>>(a);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+hipError_t launch_quant_many(hipStream_t s, const QuantAttnArgs &a, const QuantPlan &p, int head_dim, int group, int pairs) {
+    if (head_dim == 128) return group == 32 ? run_many<128, 32>(s, a, p, pairs) : run_many<128, 64>(s, a, p, pairs);
+    return group == 32 ? run_many<64, 32>(s, a, p, pairs) : run_many<64, 64>(s, a, p, pairs);
+}
+
+}  // namespace air

@@ -50,7 +50,8 @@ def attention(cache, q, held, counts, causal, scale=None):
     Bounds: a logit is a sum of d products step q code and as many q lo, each exact or rounded to fp32, whose sums round once per term (bf16:
     codes have 16 added, and taken off again: 16 step q twice more); the exponent and the power of two (2^-22); sums of `held` terms; the factor
     p step keeps 11 bits (bf16: half a step 2^-11, and of numbers below 2^-14 the absolute 2^-25, in units of at most the greatest step of the
-    group in the sequence, times a code) or 24; outputs are rounded once."""
+    group in the sequence, times a code) or 24; outputs are rounded once.  bf16 calls of 65 rows and more: K in fp16 (half a step 2^-11, and 2^-25 of
+    rows of at least 2^-6), V, the probabilities and, by them, their sum in bf16."""
     import torch
 
     d, H = cache.head_dim, cache.n_kv_heads
@@ -75,12 +76,17 @@ def attention(cache, q, held, counts, causal, scale=None):
         p = p.masked_fill(~seen, 0.0)
         p = p / p.sum(-1, keepdim=True).clamp(min=1e-300)
         off = size.amax(-1, keepdim=True) * ((2 * d + 16) * 2.0 ** -24) + size.amax(-1, keepdim=True) * 2.0 ** -22 if n else p.sum(-1, keepdim=True)
+        if n and q.dtype == torch.bfloat16 and q.shape[2] * g >= 65:
+            dot = (qs.abs() @ t((kl + ks).abs()) * scale).masked_fill(~seen, 0.0)
+            least = qs.abs().sum(-1, keepdim=True) * (kl + ks).abs().amax((1, 2), keepdim=True) * scale * 2.0 ** -19
+            off = off + dot.amax(-1, keepdim=True) * 2.0 ** -11 + least
         rel = 2 * (torch.expm1(off) + 2.0 ** -22 + (n + 64) * 2.0 ** -24)
         vl_seen = torch.where(torch.isfinite(vl), vl, 0.0) if not bool(seen.all()) else vl
         o, a = p @ (vl_seen + vs), p @ (vl_seen.abs() + vs)
         low = half > 2.0 ** -20  # bf16
-        err = a * (rel + (2.0 ** -11 if low else 2.0 ** -22))
-        if low and n:
+        many = low and q.shape[2] * g >= 65
+        err = a * (rel + (3 * 2.0 ** -8 if many else 2.0 ** -11 if low else 2.0 ** -22))
+        if low and n and not many:
             err = err + vst1.amax(1, keepdim=True) * (n * 15 * 2.0 ** -25)
         bound = err * 1.01 + (o.abs() + err) * half + 1e-37
         w = p.reshape(H, g * c, n).sum(1)

@@ -197,6 +197,44 @@ def test_windows_and_pieces(dtype, d, group, causal):
     assert torch.equal(out, again) and torch.equal(w, w2)
 
 
+@pytest.mark.parametrize("d,group", [(64, 32), (64, 64), (128, 32), (128, 64)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("hq,hkv,counts,held", [
+    (8, 1, [9], [1500]),  # 72 rows: a tile of 128, splits
+    (14, 2, [150, 33, 0, 150], [150, 1201, 700, 2003]),  # ragged, whole prompts, behind other slots
+    (4, 4, [129], [257]), (24, 2, [300, 300], [640, 511]),
+    (64, 8, [96] * 8, [130, 97, 1, 200, 63, 64, 65, 128]),  # tiles of 256, more queries than slots
+])
+def test_many_rows(d, group, causal, hq, hkv, counts, held):
+    import paper_2503_23956_amd as A
+
+    cache = _filled(A, len(held), hkv, max(held) + 3, d, "bf16", group, held, 15)
+    q = (_randn(18, len(held), max(counts), hq, d) * 2.0).bfloat16().transpose(1, 2)
+    _check(A, cache, q, held, counts, causal, seed=6)
+    _check(A, cache, q, held, counts, causal, weigh=False)
+    _check(A, cache, q, held, counts, causal, seed=7, with_out=False)
+
+
+@pytest.mark.parametrize("rows", [1, 16, 32, 100])
+@pytest.mark.parametrize("k_size,q_size,v_size", [(1e6, 1e-6, 1e8), (1e-8, 1e7, 1e-9), (3e4, 1e-3, 2e5), (1e-12, 1e12, 1e30)])
+def test_magnitudes(rows, k_size, q_size, v_size):
+    """Any magnitude of queries, keys and values, next to each other in one batch row's heads and groups."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    cache = _new(A, 1, 2, 300, 128, "bf16", 32)
+    k, v = (_randn(i, 1, 2, 300, 128) for i in range(2))
+    k[:, 0] *= k_size
+    k[:, 0, :100] *= 1e-3
+    v[..., 32:64] *= v_size  # groups of other magnitudes beside it
+    v[:, :, 150:] *= 3.0
+    A.air_quant_append(cache, k.bfloat16(), v.bfloat16())
+    q = _randn(5, 1, 2, rows, 128)
+    q[:, 0] *= q_size
+    _check(A, cache, q.bfloat16(), [300], [rows], False)
+
+
 @pytest.mark.parametrize("dtype,d,group", KINDS)
 def test_append_and_attend(dtype, d, group):
     import torch
@@ -219,13 +257,14 @@ def test_append_and_attend(dtype, d, group):
 
 
 @pytest.mark.parametrize("dtype,d,group", KINDS)
-def test_slots_that_are_not_seen_count_for_nothing(dtype, d, group):
+@pytest.mark.parametrize("c", [3, 20, 60])
+def test_slots_that_are_not_seen_count_for_nothing(dtype, d, group, c):
     """Groups of NaN behind the causal border, and behind the slots held, reach no row; those that a row sees do, however little they weigh."""
     import torch
 
     import paper_2503_23956_amd as A
 
-    held, c = 140, 20
+    held = 140
     cache = _filled(A, 2, 2, 150, d, dtype, group, [held, held], 6)
     cache.planes[2][0, :, held - 1] = math.nan  # the last key of sequence 0, which the last query alone sees
     cache.planes[3][1, :, held - 3, 0] = math.nan  # lo of the first group of a value of sequence 1
