@@ -16,7 +16,10 @@ struct QuantAttnArgs {
     void *out;
     float *part_o;    // [pair][split][row][D]
     float2 *part_ml;  // [pair][split][row]
-    float *part_l2;   // the same, many rows with weights: sums of unrounded probabilities
+    // many rows with weights:
+    float *part_l2;    // [pair][split][row]: sums of the unrounded probabilities
+    float4 *row_ref;   // [pair][row]: factor of the logits, reference, 1 / sum, slots seen (whole number)
+    uint16_t *row_q;   // [pair][row][D]: queries in fp16, divided by their units
     float *weights;
     int64_t q_b, q_h, q_t, out_b, out_h, out_t;
     const int32_t *lens, *counts;

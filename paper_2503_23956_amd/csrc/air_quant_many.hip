@@ -196,6 +196,12 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
         row_c *= unit;
     }
     float mul = row_c;
+    if (WEIGH && split == 0 && kw == 0 && row < sp.rows) {
+        uint16_t *to = a.row_q + ((size_t)pair * a.n_rows + row) * D;
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) *reinterpret_cast<uint4 *>(to + R::kVec * (2 * sl + h)) = q[sl];
+        if (a.splits > 1 && h == 0) a.row_ref[(size_t)pair * a.n_rows + row] = make_float4(row_c, 0.f, 0.f, __int_as_float(last + 1));
+    }
 
     const size_t base = (size_t)pair * a.capacity;
     const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
@@ -375,8 +381,10 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     }
     const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
     if (row < sp.rows && h == 0) {
-        if (a.part_ml) a.part_ml[part] = make_float2(ref, l);
-        if (WEIGH) a.part_l2[part] = l2;
+        if (a.splits > 1) a.part_ml[part] = make_float2(ref, l);
+        if (WEIGH && a.splits > 1) a.part_l2[part] = l2;
+        if (WEIGH && a.splits == 1)
+            a.row_ref[part] = make_float4(row_c, finite_or_zero(ref), l2 == 0.f ? 0.f : 1.0f / l2, __int_as_float(last + 1));
     }
     if (a.splits == 1) {
         if (!a.out) return;
@@ -412,28 +420,40 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     }
 }
 
-__global__ __launch_bounds__(256) void quant_join_kernel_128(QuantAttnArgs a) {
+// Rows joined over the splits; their references for the weights
+template <int D>
+__global__ __launch_bounds__(256) void quant_many_join_kernel(QuantAttnArgs a) {
     __shared__ float4 jl[256 + 8];
     const int pair = blockIdx.y;
     const QuantSpan sp(a, pair);
-    if (sp.rows > 0) join_rows<128, bf16_t>(a, sp, pair, jl);
-}
-__global__ __launch_bounds__(256) void quant_join_kernel_64(QuantAttnArgs a) {
-    __shared__ float4 jl[256 + 16 / 2];
-    const int pair = blockIdx.y;
-    const QuantSpan sp(a, pair);
-    if (sp.rows > 0) join_rows<64, bf16_t>(a, sp, pair, jl);
+    if (sp.rows == 0) return;
+    if (a.weights)
+        for (int row = blockIdx.x * 256 + threadIdx.x; row < sp.rows; row += gridDim.x * 256) {
+            const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows + row;
+            const float *l2 = a.part_l2 + (size_t)pair * a.splits * a.n_rows + row;
+            float top = -INFINITY, sum = 0.f;
+            for (int s = 0; s < a.splits; ++s) {
+                const float m = ml[(size_t)s * a.n_rows].x, l = l2[(size_t)s * a.n_rows], now = fmaxf(top, m);
+                sum = part_weight(top, sum, now) * sum + part_weight(m, l, now) * l;
+                top = now;
+            }
+            float4 *ref = a.row_ref + (size_t)pair * a.n_rows + row;
+            ref->y = finite_or_zero(top);
+            ref->z = sum == 0.f ? 0.f : 1.0f / sum;
+        }
+    if (a.out) join_rows<D, bf16_t>(a, sp, pair, jl);
 }
 
 // The slots' weights: a wave has 64 slots, their keys as operands in registers, and meets all rows, 32 at a time, which the workgroup's
 // eight waves share in LDS.  S^T again: a lane has one row, its reference and sum, and adds up that row's share of 32 slots over all tiles of rows;
-// the lanes are added at the end, in a fixed order.
+// the lanes are added at the end, in a fixed order.  Two buffers: the next 128 rows are on their way under the products of the present ones.
+// 64 x 32 logits of a wave: 16 products of 32 clocks, 32 exponentials of 16 and two times as many other instructions of 4: the vector unit's time.
 template <int D, int GR>
 __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArgs a) {
     using R = Row<bf16_t, D>;
     constexpr int NS = R::kSlices, NG = D / GR, kTiles = 4;  // tiles of rows at a time
-    __shared__ u32x4 qs[kTiles][R::kKTile];
-    __shared__ float4 rs[kTiles * 32];  // factor, reference, 1 / sum, slots seen
+    __shared__ u32x4 qs[2][kTiles][R::kKTile];
+    __shared__ float4 rs[2][kTiles * 32];
     __shared__ float units[8][64];
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int y = a.by_pairs.of(blockIdx.x), pair = blockIdx.x - y * a.pairs;
@@ -487,63 +507,84 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
 #pragma unroll
         for (int i = 0; i < 16; ++i) w[t][i] = 0.f;
 
-    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
-    const float *l2 = a.part_l2 + (size_t)pair * a.splits * a.n_rows;
-    constexpr int kLanes = D / 8, kPer = 512 / kLanes;  // threads of a row; rows of a round
-    for (int row0 = 0; row0 < sp.rows; row0 += 32 * kTiles) {
-        __syncthreads();
+    constexpr int kLanes = D / 8, kPer = 512 / kLanes, kLoads = 32 * kTiles / kPer;  // threads of a row; rows of a round of loads
+    const uint16_t *row_q = a.row_q + (size_t)pair * a.n_rows * D + 8 * (threadIdx.x % kLanes);
+    const float4 *row_ref = a.row_ref + (size_t)pair * a.n_rows;
+    u32x4 next_q[kLoads];
+    float4 next_ref = {0.f, 0.f, 0.f, 0.f};
+    auto request = [&](int row0) {
 #pragma unroll
-        for (int i = 0; i < 32 * kTiles / kPer; ++i) {
-            const int x = i * kPer + threadIdx.x / kLanes, piece = threadIdx.x % kLanes, row = row0 + x;
-            const int r = row < sp.rows ? row : sp.rows - 1, tok = a.by_g.of(r);
-            const bf16_t *qp = (const bf16_t *)a.q + sp.b * a.q_b + tok * a.q_t + ((int64_t)sp.h * a.G + r - tok * a.G) * a.q_h + 8 * piece;
-            const uint4 q = *reinterpret_cast<const uint4 *>(qp);
-            float most = greatest_of(q, 0.f);
-            most = kLanes == 16 ? max16(most) : max8(most);
-            const float unit = unit_of(most);
-            qs[x >> 5][R::k_at(x & 31, piece)] = __builtin_bit_cast(u32x4, to_f16(q, 1.0f / unit));
-            if (piece == 0) {
-                float top = -INFINITY, sum = 0.f;
-                for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[(size_t)s * a.n_rows + r].x);
-                for (int s = 0; s < a.splits; ++s) {
-                    const float v = l2[(size_t)s * a.n_rows + r];
-                    sum = fmaf(part_weight(ml[(size_t)s * a.n_rows + r].x, v, top), v, sum);
-                }
-                rs[x] = float4{a.c * unit, finite_or_zero(top), sum == 0.f || row >= sp.rows ? 0.f : 1.0f / sum, __int_as_float(sp.seen(a, r))};
-            }
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = min(row0 + i * kPer + (int)threadIdx.x / kLanes, sp.rows - 1);
+            next_q[i] = *reinterpret_cast<const u32x4 *>(row_q + (size_t)row * D);
         }
-        __syncthreads();
+        if (threadIdx.x < 32 * kTiles) {
+            next_ref = row_ref[min(row0 + (int)threadIdx.x, sp.rows - 1)];
+            if (row0 + (int)threadIdx.x >= sp.rows) next_ref.z = 0.f;
+        }
+    };
+    request(0);
+    for (int row0 = 0, buf = 0; row0 < sp.rows; row0 += 32 * kTiles, buf ^= 1) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = i * kPer + threadIdx.x / kLanes;
+            qs[buf][x >> 5][R::k_at(x & 31, threadIdx.x % kLanes)] = next_q[i];
+        }
+        if (threadIdx.x < 32 * kTiles) rs[buf][threadIdx.x] = next_ref;
+        // (the buffer's readers of two rounds ago have passed the last round's barrier)
+        lds_barrier();
+        if (row0 + 32 * kTiles < sp.rows) request(row0 + 32 * kTiles);
         if (idle) continue;
         const int tiles = min(kTiles, (sp.rows - row0 + 31) / 32), all = sp.seen(a, row0);
-        for (int t = 0; t < tiles; ++t) {
-            const float4 ref = rs[32 * t + n];
-            u32x4 q[NS];
+        bool odd = scaled || slot0 + 64 > all;
 #pragma unroll
-            for (int sl = 0; sl < NS; ++sl) q[sl] = qs[t][R::k_at(n, 2 * sl + h)];
-            const bool huge = __any(fabsf(ref.y) > kHuge);
+        for (int t = 0; t < kTiles / 2; ++t) odd = odd || fabsf(rs[buf][64 * t + lane].y) > kHuge;
+        u32x4 q[NS];
+        auto read_q = [&](int t) {
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) q[sl] = qs[buf][t][R::k_at(n, 2 * sl + h)];
+        };
+        auto logits = [&](f32x16 &s, const uint4(&key)[NS]) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) s = mma32_f16(key[sl], __builtin_bit_cast(uint4, q[sl]), s);
+        };
+        if (__builtin_expect(!__any(odd), 1)) {
+            auto add = [&](f32x16 &to, const f32x16 &s, const float4 &ref) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) to[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], ref.x, -ref.y)), ref.z, to[i]);
+            };
+            // one half's products under the other's exponentials
+            f32x16 sa, sb;
+            read_q(0);
+            logits(sa, k[0]);
+            for (int t = 0; t < tiles; ++t) {
+                const float4 ref = rs[buf][32 * t + n];
+                logits(sb, k[1]);
+                add(w[0], sa, ref);
+                read_q(t + 1 < tiles ? t + 1 : t);
+                logits(sa, k[0]);  // (behind the last tile: not used)
+                add(w[1], sb, ref);
+            }
+            continue;
+        }
+        for (int t = 0; t < tiles; ++t) {
+            const float4 ref = rs[buf][32 * t + n];
             const int last = __float_as_int(ref.w) - 1;
+            const bool huge = __any(fabsf(ref.y) > kHuge);
+            read_q(t);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 f32x16 s;
+                logits(s, k[x]);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-                for (int sl = 0; sl < NS; ++sl) s = mma32_f16(k[x][sl], __builtin_bit_cast(uint4, q[sl]), s);
-                if (__builtin_expect(scaled, 0)) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] *= units[wave][32 * x + 8 * (i >> 2) + 4 * h + (i & 3)];
-                }
-                if (__builtin_expect(slot0 + 32 * x + 32 > all, 0)) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (slot0 + 32 * x + 8 * (i >> 2) + 4 * h + (i & 3) > last) s[i] = -INFINITY;
-                }
-                if (__builtin_expect(huge, 0)) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) w[x][i] = fmaf(__builtin_amdgcn_exp2f(rounded_exponent(s[i], ref.x, ref.y)), ref.z, w[x][i]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) w[x][i] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], ref.x, -ref.y)), ref.z, w[x][i]);
+                for (int i = 0; i < 16; ++i) {
+                    const int at = 32 * x + 8 * (i >> 2) + 4 * h + (i & 3);
+                    float v = s[i] * units[wave][at];
+                    if (slot0 + at > last) v = -INFINITY;
+                    v = huge ? rounded_exponent(v, ref.x, ref.y) : fmaf(v, ref.x, -ref.y);
+                    w[x][i] = fmaf(__builtin_amdgcn_exp2f(v), ref.z, w[x][i]);
                 }
             }
         }
@@ -575,9 +616,8 @@ static hipError_t run_many(hipStream_t s, const QuantAttnArgs &a, const QuantPla
         else quant_many_kernel<D, GR, 2, false><<<grid, 512, 0, s>>>(a);
     }
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && p.splits > 1 && a.out) {
-        if (D == 128) quant_join_kernel_128<<<dim3((unsigned)p.finish, (unsigned)pairs), 256, 0, s>>>(a);
-        else quant_join_kernel_64<<<dim3((unsigned)p.finish, (unsigned)pairs), 256, 0, s>>>(a);
+    if (e == hipSuccess && p.splits > 1) {
+        quant_many_join_kernel<D><<<dim3((unsigned)p.finish, (unsigned)pairs), 256, 0, s>>>(a);
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.weights) {
