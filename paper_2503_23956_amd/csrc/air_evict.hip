@@ -1,23 +1,28 @@
 // air_evict: the `keep` slots of a (sequence, head) that stay, and the rows that move to make them the first ones.
 //
-// One workgroup per (sequence, head) finds the keep-th largest of the slots' keys by digits of 11, 11 and 10 bits (histograms in LDS, the keys there too
-// where they fit), then ranks by counts of ballots: which slots below `keep` are given up, which from `keep` on stay; the i-th of the one takes
-// what the i-th of the other has.  Sources lie behind `keep` and destinations in front of it, so that rows move in any order.
-// Few rows are moved by the same workgroup; where there can be many, a second launch over all of the chip moves them by a list.
+// One workgroup per (sequence, head) finds the keep-th largest of the slots' keys by digits of 11, 11 and 10 bits (histograms in LDS); as soon as the
+// deciding digit has few slots they are ranked directly, each by comparing it with all of them.  Then counts of ballots rank which slots
+// below `keep` are given up and which from `keep` on stay; the i-th of the one takes what the i-th of the other has.  Sources lie behind `keep` and
+// destinations in front of it, so that rows move in any order.  Few rows are moved by the same workgroup; where there can be many, a
+// second launch over all of the chip moves them by a list.
+//
+// A wave has a run of the slots, a lane four of them at a time; keys stay in LDS (capacities up to 32768; beyond, they are formed
+// again, out of the L2 cache, wherever they are used).  What a call takes is dependent accesses, barriers and the instructions of
+// one pass over code that is new to the CU: loops are not unrolled (keys in registers, 16 to 32 slots unrolled: 18 us in place of 15, one sequence of
+// 7432 slots cut to 743).  16 x 4 heads of 2368 slots of which 64 go, K and V rows of 256 bytes with them: 10 us.
 #include "air_device.h"
 #include "air_internal.h"
 
 namespace air {
 
 constexpr int kEvictWaves = 16, kEvictThreads = 64 * kEvictWaves;
-constexpr int kLdsKeys = 8192, kLdsMoves = 2048, kBins = 2048;
+constexpr int kLdsMoves = 2048, kBins = 2048, kDirect = 256;  // kDirect: slots of the deciding digit that are ranked directly
 constexpr size_t kAlone = 128 << 10;  // bytes of rows that one workgroup moves by itself
 
 struct EvictPlane {
     uint8_t *rows;
     int64_t b, h, t;
-    int32_t words, wide;  // words of 16 (wide) or 4 bytes of a row
-    Div by_words;
+    int32_t start, wide;  // words of 16 (wide) or 4 bytes of a row lie behind those of the planes in front
 };
 struct EvictArgs {
     EvictPlane p[AIR_MAX_PLANES];
@@ -27,39 +32,84 @@ struct EvictArgs {
     int32_t *lens_out;
     int32_t *moves;  // [pair][1 + 2 most]: count, destinations, sources; null: one launch
     int32_t n_planes, n_heads, capacity, keep, limit, first, recent, most;
+    int32_t words, lanes;  // words of a slot's rows in all planes; lanes that share a slot, a power of two
     Div by_heads;
 };
 
 // Order of the slots: protected ones, NaN, then by weight (-0 like 0)
 __device__ __forceinline__ uint32_t rank_key(float w, bool safe) {
-    if (safe) return 0xffffffffu;
-    if (w != w) return 0xfffffffeu;
-    const uint32_t u = __float_as_uint(w + 0.0f);
-    return u >> 31 ? ~u : u | 0x80000000u;
+    const uint32_t u = __float_as_uint(w + 0.0f), k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return safe ? 0xffffffffu : w != w ? 0xfffffffeu : k;
 }
 
-__device__ __forceinline__ void move_rows(const EvictArgs &a, int b, int h, int count, const int32_t *to, const int32_t *from, int first, int step) {
-    for (int i = 0; i < a.n_planes; ++i) {
-        const EvictPlane &p = a.p[i];
-        uint8_t *rows = p.rows + b * p.b + h * p.h;
-        const int total = count * p.words;  // (at most half of 2^33 bytes, in words of 4: 2^30)
-        for (int x = first; x < total; x += step) {
-            const int r = p.by_words.of(x), w = x - r * p.words;
-            if (p.wide) {
-                *reinterpret_cast<uint4 *>(rows + to[r] * p.t + 16 * w) = *reinterpret_cast<const uint4 *>(rows + from[r] * p.t + 16 * w);
-            } else {
-                *reinterpret_cast<uint32_t *>(rows + to[r] * p.t + 4 * w) = *reinterpret_cast<const uint32_t *>(rows + from[r] * p.t + 4 * w);
-            }
+// Moves slots from[i] to to[i], `lanes` threads each
+struct Word {
+    uint8_t *to;  // null: none
+    bool wide;
+    uint4 x;
+};
+__device__ __forceinline__ Word request(const EvictArgs &a, int b, int h, int count, const int32_t *to, const int32_t *from, int r, int w) {
+    Word v = {nullptr, false, {0, 0, 0, 0}};
+    if (r >= count || w >= a.words) return v;
+    int64_t t = 0, off = 0;
+    uint8_t *rows = nullptr;
+    for (int p = 0; p < a.n_planes; ++p)
+        if (w >= a.p[p].start) {
+            v.wide = a.p[p].wide != 0;
+            rows = a.p[p].rows;
+            off = b * a.p[p].b + h * a.p[p].h + (w - a.p[p].start) * (v.wide ? 16 : 4);
+            t = a.p[p].t;
         }
+    rows += off;
+    v.to = rows + to[r] * t;
+    const uint8_t *at = rows + from[r] * t;
+    if (v.wide) v.x = *reinterpret_cast<const uint4 *>(at);
+    else v.x = uint4{*reinterpret_cast<const uint32_t *>(at), 0, 0, 0};
+    return v;
+}
+__device__ __forceinline__ void put(const Word &v) {
+    if (!v.to) return;
+    if (v.wide) *reinterpret_cast<uint4 *>(v.to) = v.x;
+    else *reinterpret_cast<uint32_t *>(v.to) = v.x.x;
+}
+// (six rows a thread at a time: what one workgroup moves by itself is that many fewer round trips to memory)
+__device__ __forceinline__ void move_rows(const EvictArgs &a, int b, int h, int count, const int32_t *to, const int32_t *from, int thread, int threads) {
+    const int step = threads / a.lanes;
+    for (int w = thread & (a.lanes - 1); w < a.words; w += a.lanes)
+        for (int r = thread / a.lanes; r < count; r += 6 * step) {
+            const Word v0 = request(a, b, h, count, to, from, r, w), v1 = request(a, b, h, count, to, from, r + step, w);
+            const Word v2 = request(a, b, h, count, to, from, r + 2 * step, w), v3 = request(a, b, h, count, to, from, r + 3 * step, w);
+            const Word v4 = request(a, b, h, count, to, from, r + 4 * step, w), v5 = request(a, b, h, count, to, from, r + 5 * step, w);
+            put(v0);
+            put(v1);
+            put(v2);
+            put(v3);
+            put(v4);
+            put(v5);
+        }
+}
+__device__ __forceinline__ void move_weights(float *weights, int32_t *positions, int count, const int32_t *to, const int32_t *from, int first, int step) {
+    for (int i = first; i < count; i += step) {
+        const int t = to[i], f = from[i];
+        weights[t] = weights[f];
+        if (positions) positions[t] = positions[f];
     }
 }
 
+// KEYS: slots whose keys LDS holds; 0: none
+template <int KEYS>
 __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a) {
-    __shared__ uint32_t keys[kLdsKeys];
-    __shared__ int32_t bins[kBins], moves[2 * kLdsMoves];
-    __shared__ int32_t wave_n[3][kEvictWaves], scan[kEvictWaves + 1], found[2], last_of[kEvictWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ __align__(16) uint32_t keys[KEYS ? KEYS : 4];
+    __shared__ int32_t bins[kBins], moves[2 * kLdsMoves], sums[kEvictWaves], found[3], last_of[kEvictWaves];
+    __shared__ uint64_t few[kDirect];  // (key, ~slot): larger goes first
+    __shared__ int32_t n_few;
+    __shared__ uint64_t border_at;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int pair = blockIdx.x, b = a.by_heads.of(pair), h = pair - b * a.n_heads;
+    float *weights = a.weights + (size_t)pair * a.capacity;
+    int32_t *positions = a.positions ? a.positions + (size_t)pair * a.capacity : nullptr;
+    for (int i = tid; i < kBins; i += kEvictThreads) bins[i] = 0;
+    if (tid == 0) n_few = 0;
     int n = a.lens[b];
     n = n < 0 ? 0 : n > a.capacity ? a.capacity : n;
     const bool over = n > a.limit;
@@ -69,123 +119,243 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a) {
         if (list && tid == 0) list[0] = 0;
         return;
     }
-    float *weights = a.weights + (size_t)pair * a.capacity;
-    int32_t *positions = a.positions ? a.positions + (size_t)pair * a.capacity : nullptr;
+    const int run = (n + 256 * kEvictWaves - 1) / (256 * kEvictWaves) * 256, begin = wave * run, end = min(begin + run, n);
 
-    int32_t last = INT32_MAX;  // (no position is less than 0 in front of it)
-    if (positions && a.recent > 0) {
-        last = INT32_MIN;
-        for (int i = tid; i < n; i += kEvictThreads) last = positions[i] > last ? positions[i] : last;
+    // ---- keys
+    struct Four {
+        uint32_t k[4];
+    };
+    // four words from slot s on, in one access where they all lie in the table
+    const auto fetch = [&](const void *table, int s) {
+        Four v = {{0, 0, 0, 0}};
+        const uint32_t *at = static_cast<const uint32_t *>(table) + s;
+        if (s + 4 <= a.capacity) __builtin_memcpy(&v, at, 16);
+        else
+            for (int i = 0; i < 4; ++i)
+                if (s + i < a.capacity) v.k[i] = at[i];
+        return v;
+    };
+    const bool any_recent = positions && a.recent > 0, any_first = positions != nullptr;
+    int32_t recent_from = 0;
+    const auto settle = [&](int32_t last) {  // of the wave's slots: the first of the most recent positions
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            const int32_t o = __shfl_xor(last, s, 64);
-            last = o > last ? o : last;
-        }
+        for (int d = 1; d < 64; d <<= 1) last = max(last, __shfl_xor(last, d, 64));
         if (lane == 0) last_of[wave] = last;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kEvictWaves; ++w) last = last_of[w] > last ? last_of[w] : last;
-    }
-    const auto fetch = [&](int i) {
-        bool safe = false;
-        if (positions) {
-            const int32_t pos = positions[i];
-            safe = pos < a.first || (int64_t)last - pos < a.recent;
-        }
-        return rank_key(weights[i], safe);
+        for (int w = 0; w < kEvictWaves; ++w) last = max(last, last_of[w]);
+        const int64_t from = (int64_t)last - a.recent + 1;
+        recent_from = from < INT32_MIN ? INT32_MIN : (int32_t)from;
     };
-    const bool held = n <= kLdsKeys;
-    if (held)
-        for (int i = tid; i < n; i += kEvictThreads) keys[i] = fetch(i);
-    const auto key_of = [&](int i) { return held ? keys[i] : fetch(i); };
-
-    // ---- the keep-th largest key, and how many equal to it stay
-    uint32_t value = 0, mask = 0;
-    int need = a.keep;
+    const auto form = [&](int s, const Four &w, const Four &pos) {  // 0 for slots that are not there
+        Four v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t at = (int32_t)pos.k[i];
+            const uint32_t k = rank_key(__uint_as_float(w.k[i]), (any_first && at < a.first) || (any_recent && at >= recent_from));
+            v.k[i] = s + i < end ? k : 0u;
+        }
+        return v;
+    };
+    if constexpr (KEYS > 0) {
+        constexpr int kTurns = KEYS / (256 * kEvictWaves);
+        Four w[kTurns], pos[kTurns];  // (everything requested at once)
+        int32_t last = INT32_MIN;
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int s = begin + 256 * t + 4 * lane;
+            if (256 * t < run && s < end) {
+                w[t] = fetch(weights, s);
+                if (positions) pos[t] = fetch(positions, s);
+                else pos[t] = Four{{0, 0, 0, 0}};
+            }
+        }
+        if (any_recent) {
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (256 * t < run && begin + 256 * t + 4 * lane + i < end) last = max(last, (int32_t)pos[t].k[i]);
+            settle(last);
+        }
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int s = begin + 256 * t + 4 * lane;
+            if (256 * t < run && s < end) {
+                const Four v = form(s, w[t], pos[t]);
+                *reinterpret_cast<uint4 *>(keys + s) = uint4{v.k[0], v.k[1], v.k[2], v.k[3]};
+            }
+        }
+    } else if (any_recent) {
+        int32_t last = INT32_MIN;
+        for (int s = tid; s < n; s += kEvictThreads) last = max(last, positions[s]);
+        settle(last);
+    }
+    __syncthreads();
+    // f(slot, keys of it and the next three) for the wave's slots, its lanes together (begin + 256 t + 4 lane)
+    const auto each = [&](auto &&f) {
 #pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
+        for (int s0 = begin; s0 < end; s0 += 256) {
+            const int s = s0 + 4 * lane;
+            Four v;
+            if constexpr (KEYS > 0) {
+                uint4 x = {0, 0, 0, 0};
+                if (s < end) x = *reinterpret_cast<const uint4 *>(keys + s);
+                v = Four{{x.x, x.y, x.z, x.w}};
+            } else {
+                v = form(s, fetch(weights, s), positions ? fetch(positions, s) : Four{{0, 0, 0, 0}});
+            }
+            f(s, v);
+        }
+    };
+
+    // ---- the last that stays: its key, and its slot among those of its key
+    uint32_t value = 0, mask = 0;
+    int need = a.keep, equal = 0;
+    bool direct = false;
+#pragma unroll 1
+    for (int pass = 0; pass < 3 && !direct; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
         const uint32_t digits = pass == 2 ? 0x3ffu : 0x7ffu;
-        for (int i = tid; i < kBins; i += kEvictThreads) bins[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += kEvictThreads) {
-            const uint32_t k = key_of(i);
-            if ((k & mask) == value) atomicAdd(&bins[k >> shift & digits], 1);
+        if (pass > 0) {
+            for (int i = tid; i < kBins; i += kEvictThreads) bins[i] = 0;
+            __syncthreads();
         }
+        each([&](int s, const Four &v) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s + i < end && (v.k[i] & mask) == value) atomicAdd(&bins[v.k[i] >> shift & digits], 1);
+        });
         __syncthreads();
         // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t
-        const int c0 = bins[kBins - 1 - 2 * tid], c1 = bins[kBins - 2 - 2 * tid];
-        int total;
-        const int above = block_excl_scan<kEvictWaves>(c0 + c1, scan, &total);
+        const int c0 = bins[kBins - 1 - 2 * tid], c1 = bins[kBins - 2 - 2 * tid], mine = wave_incl_scan(c0 + c1);
+        if (lane == 63) sums[wave] = mine;
+        __syncthreads();
+        int above = mine - c0 - c1;
+#pragma unroll
+        for (int w = 0; w < kEvictWaves; ++w) above += w < wave ? sums[w] : 0;
         if (above < need && need <= above + c0 + c1) {
             const bool second = need > above + c0;
             found[0] = kBins - 1 - 2 * tid - (second ? 1 : 0);
             found[1] = need - above - (second ? c0 : 0);
+            found[2] = second ? c1 : c0;
         }
         __syncthreads();
         value |= (uint32_t)found[0] << shift;
         mask |= digits << shift;
         need = found[1];
+        equal = found[2];
+        direct = equal <= kDirect;
     }
+    const auto order = [](int s, uint32_t k) { return (uint64_t)k << 32 | (uint32_t)~s; };
+    if (direct) {
+        each([&](int s, const Four &v) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s + i < end && (v.k[i] & mask) == value) few[atomicAdd(&n_few, 1)] = order(s + i, v.k[i]);
+        });
+        __syncthreads();
+        // four threads share a slot's comparisons
+        static_assert(4 * kDirect == kEvictThreads, "four threads a slot");
+        if (64 * wave < 4 * equal) {
+            const uint64_t own = tid >> 2 < equal ? few[tid >> 2] : ~0ull;
+            int ahead = 0;
+#pragma unroll 4
+            for (int i = tid & 3; i < equal; i += 4) ahead += few[i] > own;
+            ahead += __shfl_xor(ahead, 1, 64);
+            ahead += __shfl_xor(ahead, 2, 64);
+            if (tid >> 2 < equal && (tid & 3) == 0 && ahead == need - 1) border_at = own;
+        }
+    } else {  // more slots of one key: the first `need` of them stay
+        int same = 0;
+        const auto count_of = [&](int s, const Four &v) {
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c += s + i < end && v.k[i] == value;
+            return c;
+        };
+        each([&](int s, const Four &v) { same += count_of(s, v); });
+        same = wave_incl_scan(same);
+        if (lane == 63) sums[wave] = same;
+        __syncthreads();
+        int before = 0;
+        for (int w = 0; w < wave; ++w) before += sums[w];
+        if (before < need && need <= before + sums[wave])
+            each([&](int s, const Four &v) {
+                const int c = count_of(s, v), upto = before + wave_incl_scan(c);
+                int at = upto - c;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (s + i < end && v.k[i] == value && ++at == need) border_at = order(s + i, value);
+                before = __builtin_amdgcn_readlane(upto, 63);
+            });
+    }
+    __syncthreads();
+    const uint64_t border = border_at;
 
-    // ---- ranks: a wave has a run of the slots, 64 at a time
-    const int run = (n + 64 * kEvictWaves - 1) / (64 * kEvictWaves) * 64, begin = wave * run, end = begin + run < n ? begin + run : n;
-    int equal = 0;
-    for (int i = begin; i < end; i += 64) equal += __popcll(__ballot(i + lane < end && key_of(i + lane) == value));
-    if (lane == 0) wave_n[0][wave] = equal;
-    __syncthreads();
-    int before = 0;
-    for (int w = 0; w < wave; ++w) before += wave_n[0][w];
-    const uint64_t lower = (1ull << lane) - 1;
-    // calls with (slot, slots given up in front of `keep` so far, staying ones behind it so far, which of the two this one is)
-    const auto each = [&](auto &&f) {
-        int eq = before, holes = 0, comes = 0;
-        for (int i = begin; i < end; i += 64) {
-            const int s = i + lane;
-            const uint32_t k = s < end ? key_of(s) : 0u;
-            const bool same = s < end && k == value;
-            const uint64_t same_mask = __ballot(same);
-            const bool stays = s < end && (k > value || (same && eq + __popcll(same_mask & lower) < need));
-            const bool hole = s < end && s < a.keep && !stays, come = stays && s >= a.keep;
-            const uint64_t hole_mask = __ballot(hole), come_mask = __ballot(come);
-            f(s, holes + __popcll(hole_mask & lower), comes + __popcll(come_mask & lower), hole, come);
-            eq += __popcll(same_mask);
-            holes += __popcll(hole_mask);
-            comes += __popcll(come_mask);
+    // ---- slots given up in front of `keep`, staying ones from there on; counts of both in one word
+    const auto which = [&](int s, const Four &v, uint32_t &holes, uint32_t &comes) {
+        holes = comes = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool in = order(s + i, v.k[i]) >= border;
+            holes |= (s + i < end && s + i < a.keep && !in ? 1u : 0u) << i;
+            comes |= (s + i < end && s + i >= a.keep && in ? 1u : 0u) << i;
         }
-        if (lane == 0) {
-            wave_n[1][wave] = holes;
-            wave_n[2][wave] = comes;
-        }
+        return make_int2(__popc(holes), __popc(comes));
     };
-    each([](int, int, int, bool, bool) {});
-    __syncthreads();
-    int holes0 = 0, comes0 = 0, count = 0;
-    for (int w = 0; w < kEvictWaves; ++w) {
-        holes0 += w < wave ? wave_n[1][w] : 0;
-        comes0 += w < wave ? wave_n[2][w] : 0;
-        count += wave_n[1][w];
-    }
-    __syncthreads();
-    int32_t *to = list ? list + 1 : moves, *from = to + (list ? a.most : kLdsMoves);
-    each([&](int s, int holes, int comes, bool hole, bool come) {
-        if (hole) to[holes0 + holes] = s;
-        if (come) from[comes0 + comes] = s;
+    int2 mine = {0, 0};
+    each([&](int s, const Four &v) {
+        uint32_t holes, comes;
+        const int2 c = which(s, v, holes, comes);
+        mine.x += c.x;
+        mine.y += c.y;
     });
-    if (list && tid == 0) list[0] = count;
-    __syncthreads();  // (all keys have been read; the list is written)
-    for (int i = tid; i < count; i += kEvictThreads) {
-        const int t = to[i], f = from[i];
-        weights[t] = weights[f];
-        if (positions) positions[t] = positions[f];
+    mine.x = wave_incl_scan(mine.x);
+    mine.y = wave_incl_scan(mine.y);
+    if (lane == 63) {
+        sums[wave] = mine.x;
+        last_of[wave] = mine.y;
     }
-    if (!list) move_rows(a, b, h, count, to, from, tid, kEvictThreads);
+    __syncthreads();
+    int count = 0, hole_at = 0, come_at = 0;
+#pragma unroll
+    for (int w = 0; w < kEvictWaves; ++w) {
+        hole_at += w < wave ? sums[w] : 0;
+        come_at += w < wave ? last_of[w] : 0;
+        count += sums[w];
+    }
+    int32_t *to = list ? list + 1 : moves, *from = to + (list ? a.most : kLdsMoves);
+    each([&](int s, const Four &v) {
+        uint32_t holes, comes;
+        const int2 c = which(s, v, holes, comes);
+        if (!__any(holes | comes)) return;
+        const int h1 = hole_at + wave_incl_scan(c.x), c1 = come_at + wave_incl_scan(c.y);
+        int x = h1 - c.x, y = c1 - c.y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (holes >> i & 1) to[x++] = s + i;
+            if (comes >> i & 1) from[y++] = s + i;
+        }
+        hole_at = __builtin_amdgcn_readlane(h1, 63);
+        come_at = __builtin_amdgcn_readlane(c1, 63);
+    });
+    if (list) {
+        if (tid == 0) list[0] = count;
+        return;
+    }
+    __syncthreads();  // (all keys have been read; the list is written)
+    move_weights(weights, positions, count, to, from, tid, kEvictThreads);
+    move_rows(a, b, h, count, to, from, tid, kEvictThreads);
 }
 
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
     const int pair = blockIdx.y, b = a.by_heads.of(pair), h = pair - b * a.n_heads;
     const int32_t *list = a.moves + (size_t)pair * (1 + 2 * (size_t)a.most);
-    move_rows(a, b, h, list[0], list + 1, list + 1 + a.most, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+    const int thread = blockIdx.x * 256 + threadIdx.x, threads = gridDim.x * 256, count = list[0];
+    const size_t at = (size_t)pair * a.capacity;
+    move_weights(a.weights + at, a.positions ? a.positions + at : nullptr, count, list + 1, list + 1 + a.most, thread, threads);
+    move_rows(a, b, h, count, list + 1, list + 1 + a.most, thread, threads);
 }
 
 // rows that can move: no more than there are slots in front of `keep`, or behind it
@@ -219,16 +389,22 @@ hipError_t launch_evict(hipStream_t s, const air_evict_config &c, float *weights
     a.first = c.first;
     a.recent = c.recent;
     a.by_heads = div_by(c.n_heads);
+    a.words = 0;
     for (int i = 0; i < c.n_planes; ++i) {
         const air_evict_plane &p = c.planes[i];
         const bool wide = aligned(p.rows, 16) && p.b % 16 == 0 && p.h % 16 == 0 && p.t % 16 == 0 && p.row_bytes % 16 == 0;
-        a.p[i] = EvictPlane{static_cast<uint8_t *>(p.rows), p.b, p.h, p.t, p.row_bytes / (wide ? 16 : 4), wide, div_by(p.row_bytes / (wide ? 16 : 4))};
+        a.p[i] = EvictPlane{static_cast<uint8_t *>(p.rows), p.b, p.h, p.t, a.words, wide};
+        a.words += p.row_bytes / (wide ? 16 : 4);
     }
+    a.lanes = 1;
+    while (a.lanes < a.words && a.lanes < 64) a.lanes *= 2;
     const int pairs = c.batch * c.n_heads;
-    evict_kernel<<<pairs, kEvictThreads, 0, s>>>(a);
+    if (c.capacity <= 4096) evict_kernel<4096><<<pairs, kEvictThreads, 0, s>>>(a);
+    else if (c.capacity <= 32768) evict_kernel<32768><<<pairs, kEvictThreads, 0, s>>>(a);
+    else evict_kernel<0><<<pairs, kEvictThreads, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !a.moves || c.n_planes == 0) return e;
-    const int64_t words = ((int64_t)a.most * row_bytes(c) / 16 + 255) / 256, wgs = (2048 + pairs - 1) / pairs;
+    if (e != hipSuccess || !a.moves) return e;
+    const int64_t words = ((int64_t)a.most * a.lanes + 1023) / 1024, wgs = (2048 + pairs - 1) / pairs;
     evict_move_kernel<<<dim3((unsigned)(words < wgs ? (words < 1 ? 1 : words) : wgs), (unsigned)pairs), 256, 0, s>>>(a);
     return hipGetLastError();
 }

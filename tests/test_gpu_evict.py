@@ -116,15 +116,18 @@ def test_protected_tokens():
     _check(w, (pos - 300).astype(np.int32), [600, 600], 100, 100, first=0, recent=30)
 
 
-@pytest.mark.parametrize("n,keep", [(8192, 4000), (8193, 8000), (20001, 9000), (20001, 200), (70000, 33000)])
+@pytest.mark.parametrize("n,keep", [(4000, 3900), (4093, 700), (4094, 4000), (16381, 9000), (16382, 16000), (20001, 9000), (20001, 200), (32766, 5000), (70000, 33000)])
 def test_many_slots(n, keep):
-    """Keys that do not fit LDS, more moves than one workgroup takes."""
+    """Keys in 4, 16 and 32 registers a lane and in none, more moves than one workgroup takes, ties by the thousand."""
     rng = np.random.default_rng(n)
     cap = n + 3
     w = np.exp(2 * rng.standard_normal((2, 2, cap))).astype(np.float32)
     w[:, :, ::7] = 0.25
     pos = np.stack([[rng.permutation(cap) for _ in range(2)] for _ in range(2)]).astype(np.int32)
     assert _check(w, pos, [n, n - 5], keep, keep, first=3, recent=100, planes=_planes(2, 2, cap)[:3]) > 0
+    w[1] = np.float32(1.5)
+    w[1, :, -900:] = 2.0
+    assert _check(w, None, [n, n - 5], keep, keep, planes=_planes(2, 2, cap, 1)[:1]) > 0
 
 
 def test_other_streams_graphs_and_workspaces():
