@@ -35,6 +35,19 @@ struct QuantAttnArgs {
 constexpr int kRun = 64;  // slots that a wave takes at a time
 constexpr int kFewRows = 8;
 
+template <int N>
+struct Words {
+    uint32_t w[N];
+};
+template <int N>
+__device__ __forceinline__ Words<N> load_words(const void *p) {
+    Words<N> r;
+    if (N == 4) *reinterpret_cast<uint4 *>(&r) = *static_cast<const uint4 *>(p);
+    else if (N == 2) *reinterpret_cast<uint2 *>(&r) = *static_cast<const uint2 *>(p);
+    else r.w[0] = *static_cast<const uint32_t *>(p);
+    return r;
+}
+
 // What a sequence holds and asks
 struct QuantSpan {
     int b, h, count, held, rows;

@@ -33,19 +33,6 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 }
-template <int N>
-struct Words {
-    uint32_t w[N];
-};
-template <int N>
-__device__ __forceinline__ Words<N> load_words(const void *p) {
-    Words<N> r;
-    if (N == 4) *reinterpret_cast<uint4 *>(&r) = *static_cast<const uint4 *>(p);
-    else if (N == 2) *reinterpret_cast<uint2 *>(&r) = *static_cast<const uint2 *>(p);
-    else r.w[0] = *static_cast<const uint32_t *>(p);
-    return r;
-}
-
 // 16 rows of queries as operands: elements 32 m + 8 c .. + 7 of row n in lane (n, c), and the sums of their groups for the product with lo
 template <int D, int GR, typename T>
 struct QueryTile {
@@ -512,16 +499,16 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
 // At most eight rows (a token of up to eight query heads per KV head, a few tokens of fewer): half of a 16 x 16 product's rows would be
 // idle.  The first product's are; its logits of slots 32 .. 63 of a run then move to the idle lanes, so that softmax, sums and steps are formed
 // once per logit: lane (n, c) has rows 4 (c & 1) + i at slots 16 t + 32 (c >> 1) + n, t = 0, 1.  The factors p step are formed there,
-// and go through LDS.  bf16: as fp16 numbers, 11 bits, of a group's steps divided by a power of two that follows the greatest step the
-// wave has met (fp16 ends at 2^16).  fp32: as three bf16 terms, the first one in rows 0 .. 7 of the second product's operand, the second one in
-// rows 8 .. 15, the third one in a product of its own, joined at the end.
+// and go through LDS as bf16 terms (two, or with fp32 three): the first one in rows 0 .. 7 of the second product's operand, the second one in
+// rows 8 .. 15, joined at the end, the third one in a product of its own.  (One fp16 number would be 10 % fewer instructions, but its range
+// needs a unit, and next to a value 2^20 times as large, whatever that weighs, the others' codes would be lost.)
 //
 // The wave whose run has slots that the call appends writes them first.
 // ---------------------------------------------------------------------------------------
 template <int D, int GR, typename T>
 struct FewShape {
     using S = QuantShape<D, GR, T>;
-    static constexpr int kWStride = 144, kWRows = S::kF32 ? 24 : 8;  // bytes: 64 places of 16 bits and 16 more, 16 rows on different banks
+    static constexpr int kWStride = 144, kWRows = S::kF32 ? 24 : 16;  // bytes: 64 places of 16 bits and 16 more, 16 rows on different banks
     static constexpr int kWBytes = S::NG * kWRows * kWStride, kWave = S::kVBytes + kWBytes;
     static constexpr int kLds = 4 * kWave > 4 * 8 * D * 4 + 4 * 8 * 8 ? 4 * kWave : 4 * 8 * D * 4 + 4 * 8 * 8;
 };
@@ -597,14 +584,6 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
     f32x4 acc[S::NT];
     float m[4], limit[4], l[4], al[4][NG];
     bool huge = false;
-    // bf16: (p step) is held times scale[g], a power of two; most[g]: the greatest step (a pair, its lower half set) that it is right for
-    float scale[NG];
-    uint32_t most_step[NG];
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-        scale[g] = 1.0f;
-        most_step[g] = 0xffffu;
-    }
 #pragma unroll
     for (int i = 0; i < S::NT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -695,27 +674,6 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
             }
             huge = huge || __any(big);
         }
-        if (!S::kF32) {
-            bool more = false;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) more = more || vp[0].w[g] > most_step[g] || vp[1].w[g] > most_step[g];
-            if (__any(more)) {
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    const float greatest = max_halves(max16(fmaxf(step_of(vp[0].w[g]), step_of(vp[1].w[g]))));
-                    const bool up = __float_as_uint(greatest) > most_step[g];
-                    // times 2^-e: below 2; up to 32 times as much is right
-                    const int e = (int)(__float_as_uint(greatest) >> 23) - 127;
-                    const float next_scale = ldexpf(1.0f, -e), f = up ? next_scale / scale[g] : 1.0f;
-                    scale[g] = up ? next_scale : scale[g];
-                    most_step[g] = up ? __float_as_uint(greatest * 32.0f) | 0xffffu : most_step[g];
-#pragma unroll
-                    for (int j = g * (GR / 16); j < (g + 1) * (GR / 16); ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[j][i] *= f;
-                }
-            }
-        }
         bool odd = false;  // a lo of NaN in a run that some row does not see all of: it counts only where the row sees it
         if (masked) {
 #pragma unroll
@@ -751,24 +709,14 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         }
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            float step[2] = {step_of(vp[0].w[g]), step_of(vp[1].w[g])};
-            if (!S::kF32) {
-                step[0] *= scale[g];
-                step[1] *= scale[g];
-            }
+            const float step[2] = {step_of(vp[0].w[g]), step_of(vp[1].w[g])};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint8_t *to = wb + (g * F::kWRows + 4 * rc + i) * F::kWStride + 8 * n + 4 * upper;
-                const float w0 = p[i][0] * step[0], w1 = p[i][1] * step[1];
-                if constexpr (S::kF32) {
-                    uint32_t w[3];
-                    split_pair<3>(w0, w1, w);
+                uint32_t w[S::PT];
+                split_pair<S::PT>(p[i][0] * step[0], p[i][1] * step[1], w);
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t *>(to + 8 * k * F::kWStride) = w[k];
-                } else {
-                    const f16x2 w = {(_Float16)w0, (_Float16)w1};
-                    *reinterpret_cast<uint32_t *>(to) = __builtin_bit_cast(uint32_t, w);
-                }
+                for (int k = 0; k < S::PT; ++k) *reinterpret_cast<uint32_t *>(to + 8 * k * F::kWStride) = w[k];
             }
         }
         wave_sync();
@@ -779,8 +727,7 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 if (g > 0) __builtin_amdgcn_sched_barrier(0);
-                // (bf16: rows 8 .. 15 are rows 0 .. 7 again)
-                const uint4 w = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + (S::kF32 ? n : n & 7)) * F::kWStride + 32 * c + 16 * j);
+                const uint4 w = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + n) * F::kWStride + 32 * c + 16 * j);
                 uint4 w3 = {0, 0, 0, 0};
                 if (S::kF32 && n < 8) w3 = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + 16 + n) * F::kWStride + 32 * c + 16 * j);
 #pragma unroll
@@ -788,14 +735,9 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
                     const int tile = g * (GR / 16) + x;
                     typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
                     const i32x2 vcode = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(v_read + 8 * tile));
-                    if constexpr (S::kF32) {
-                        const uint4 v = operand_of((uint32_t)(j ? vcode.y : vcode.x));
-                        acc[tile] = mma<bf16_t>(w, v, acc[tile]);
-                        acc[tile] = mma<bf16_t>(w3, v, acc[tile]);
-                    } else {
-                        const uint4 v = operand16_of((uint32_t)(j ? vcode.y : vcode.x));
-                        acc[tile] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, v), acc[tile], 0, 0, 0);
-                    }
+                    const uint4 v = operand_of((uint32_t)(j ? vcode.y : vcode.x));
+                    acc[tile] = mma<bf16_t>(w, v, acc[tile]);
+                    if (S::kF32) acc[tile] = mma<bf16_t>(w3, v, acc[tile]);
                 }
             }
         }
@@ -812,7 +754,7 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         for (int g = 0; g < NG; ++g) al[i][g] = add_halves(sum16(al[i][g]));
 #pragma unroll
         for (int j = 0; j < S::NT; ++j) {
-            const float o = (S::kF32 ? add_halves(acc[j][i]) : acc[j][i] / scale[j / (GR / 16)]) + al[i][j / (GR / 16)];
+            const float o = add_halves(acc[j][i]) + al[i][j / (GR / 16)];
             if (upper == 0) ob[(wave * 8 + 4 * rc + i) * D + 16 * j + n] = o;
         }
         if (n == 0 && upper == 0) mlb[wave * 8 + 4 * rc + i] = float2{m[i], l[i]};

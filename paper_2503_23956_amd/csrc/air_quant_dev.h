@@ -29,16 +29,6 @@ __device__ __forceinline__ uint4 operand_of(uint32_t codes) {
     return r;
 }
 
-// The same in fp16
-__device__ __forceinline__ uint4 operand16_of(uint32_t codes) {
-    const uint32_t lo = codes & 0x0f0f0f0fu, hi = (codes >> 4) & 0x0f0f0f0fu;
-    uint4 r;
-    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.0f, false));
-    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 512.0f, true));
-    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, false));
-    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 512.0f, true));
-    return r;
-}
 // Eight codes of K as the bf16 numbers 16 + code, elements in order: a code three bits up in the mantissa of 16.  Eight full-rate instructions where
 // the exact conversion takes three and four of half the rate; what the product has too much, 16 sum(q), is taken off by the product with
 // the sums.

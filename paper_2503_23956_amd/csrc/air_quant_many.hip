@@ -4,10 +4,16 @@
 // probabilities and accumulators stay in two lanes), key blocks of 64 in three buffers, the codes of the block after next on their way, a
 // wave's next logits formed under the exponentials of its present ones.  What differs is how a block gets into LDS: a thread turns 16
 // codes of K and 16 of V into numbers, lo + step code in fp32, rounded once:
-//   K to fp16, 11 bits (bf16's 8 would cost a logit 2^-9 of sum |q k|).  Queries go to fp16 too, exactly: rows of either whose greatest
-//   magnitude lies outside 2^-6 .. 2^14 are held divided by a power of two, and their logits multiplied by it;
-//   V to bf16, like the probabilities, which have to hold any magnitude.
-// Per 32 x 64 logits a wave issues 16 + 16 products of 32 clocks; dequantising costs about 70 vector instructions a wave and block.
+//   K to fp16, 11 bits (bf16's 8 would cost a logit 2^-9 of sum |q k|); where weights are wanted, to two fp16 terms, 22 bits, as logits are
+//   then part of an fp32 result.  Queries go to fp16 too, exactly: rows of either whose greatest magnitude lies outside 2^-6 .. 2^14 are
+//   held divided by a power of two, and their logits multiplied by it;
+//   V to fp16, like the probabilities, unless the workgroup's share of V has a group (of all its slots) whose greatest magnitude lies outside
+//   2^-4 .. 2^14, which the pairs tell beforehand: then both to bf16, which holds any magnitude, with 8 bits (outputs 0.0025 off fp64 in place
+//   of 0.0018; an fp32 computation rounded once 0.0017).
+// Per 32 x 64 logits a wave issues 16 + 16 products of 32 clocks (weights: 32 + 16); dequantising costs about 70 vector instructions a
+// wave and block.
+#include <type_traits>
+
 #include "air_block.h"
 #include "air_quant_attn.h"
 
@@ -42,8 +48,13 @@ __device__ __forceinline__ float greatest_of(const uint4 &x, float most) {
     return most;
 }
 __device__ __forceinline__ float byte_of(uint32_t x, int i) { return (float)(x >> (8 * i) & 0xffu); }  // (one conversion)
-// what eight codes of K stand for, in fp16
-__device__ __forceinline__ uint4 key_values(uint32_t codes, float lo, float step) {
+__device__ __forceinline__ uint32_t pair_f16(float a, float b) {
+    const f16x2 v = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+// what eight codes of K stand for, as TERMS fp16 numbers each
+template <int TERMS>
+__device__ __forceinline__ void key_values(uint32_t codes, float lo, float step, uint4 (&k)[TERMS]) {
     const uint32_t a = codes & 0x0f0f0f0fu, b = codes >> 4 & 0x0f0f0f0fu;  // elements 0 4 1 5 and 2 6 3 7
     float x[8];
 #pragma unroll
@@ -51,24 +62,39 @@ __device__ __forceinline__ uint4 key_values(uint32_t codes, float lo, float step
         x[(i >> 1) + 4 * (i & 1)] = fmaf(step, byte_of(a, i), lo);
         x[2 + (i >> 1) + 4 * (i & 1)] = fmaf(step, byte_of(b, i), lo);
     }
-    uint32_t r[4];
+    uint32_t r[TERMS][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const f16x2 v = {(_Float16)x[2 * i], (_Float16)x[2 * i + 1]};
-        r[i] = __builtin_bit_cast(uint32_t, v);
+        r[0][i] = pair_f16(x[2 * i], x[2 * i + 1]);
+        if (TERMS == 2) {
+            const f16x2 v = __builtin_bit_cast(f16x2, r[0][i]);
+            r[TERMS - 1][i] = pair_f16(x[2 * i] - (float)v[0], x[2 * i + 1] - (float)v[1]);
+        }
     }
-    return uint4{r[0], r[1], r[2], r[3]};
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) k[t] = uint4{r[t][0], r[t][1], r[t][2], r[t][3]};
 }
-// what eight codes of V stand for, in bf16
+// what eight codes of V stand for, in fp16 or bf16
+template <bool WIDE>
 __device__ __forceinline__ uint4 values(uint32_t codes, float lo, float step) {
     const uint32_t a = codes & 0x0f0f0f0fu, b = codes >> 4 & 0x0f0f0f0fu;  // even and odd elements
     uint32_t r[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const bf16x2 v = {(__bf16)fmaf(step, byte_of(a, i), lo), (__bf16)fmaf(step, byte_of(b, i), lo)};
-        r[i] = __builtin_bit_cast(uint32_t, v);
+        const float x = fmaf(step, byte_of(a, i), lo), y = fmaf(step, byte_of(b, i), lo);
+        const bf16x2 v = {(__bf16)x, (__bf16)y};
+        r[i] = WIDE ? __builtin_bit_cast(uint32_t, v) : pair_f16(x, y);
     }
     return uint4{r[0], r[1], r[2], r[3]};
+}
+
+// the eight fp16 numbers of x added to sum
+__device__ __forceinline__ float sum_of_f16(const uint4 &x, float sum) {
+    const f16x2 one = {(_Float16)1.0f, (_Float16)1.0f};
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w[i]), one, sum, false);
+    return sum;
 }
 
 // A thread's part of a block of 64 slots: slot thread / 8, and of its rows the piece thread % 8 (8 bytes of codes, 4 with heads of 64)
@@ -105,9 +131,10 @@ struct CodeStage {
         }
         vp = vs[slot * (D / GR) + value_group()];
     }
-    // Into LDS; unit[key]: what the key was divided by (true: some key by more than 1).  Of a block that some row does not see all of, `left` slots from
+    // Into LDS (sk2: second terms); unit[key]: what the key was divided by (true: some key by more than 1).  Of a block that some row does not see all of, `left` slots from
     // its first are held: values behind them and of groups of NaN become 0 (bad: there were some)
-    __device__ __forceinline__ bool store(u32x4 *sk, u32x4 *sv, float *unit, bool part, int left, bool &bad) {
+    template <int TERMS, bool WIDE>
+    __device__ __forceinline__ bool store(u32x4 *sk, u32x4 *sk2, u32x4 *sv, float *unit, bool part, int left, bool &bad) {
         float lo[kPairs], step[kPairs], most = 0.0f;
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
@@ -125,11 +152,14 @@ struct CodeStage {
             }
         }
         if (piece == 0) unit[key] = u;
-        u32x4 *tk = sk + (key >> 5) * R::kKTile, *tv = sv + (key >> 5) * R::kVTile;
+        u32x4 *tv = sv + (key >> 5) * R::kVTile;
 #pragma unroll
         for (int i = 0; i < kWords; ++i) {
-            const int w = kWords * piece + i, nq = w / (D / 32), m = w % (D / 32);
-            tk[R::k_at(key & 31, 4 * m + nq)] = __builtin_bit_cast(u32x4, key_values(k[i], lo[i % kPairs], step[i % kPairs]));
+            const int w = kWords * piece + i, nq = w / (D / 32), m = w % (D / 32), at = (key >> 5) * R::kKTile + R::k_at(key & 31, 4 * m + nq);
+            uint4 x[TERMS];
+            key_values<TERMS>(k[i], lo[i % kPairs], step[i % kPairs], x);
+            sk[at] = __builtin_bit_cast(u32x4, x[0]);
+            if (TERMS == 2) sk2[at] = __builtin_bit_cast(u32x4, x[TERMS - 1]);
         }
         float vlo = lo_of(vp), vstep = step_of(vp);
         if (part) {
@@ -138,7 +168,7 @@ struct CodeStage {
             if (nan || key >= left) vlo = vstep = 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) tv[R::v_at(key & 31, kWords * piece + i)] = __builtin_bit_cast(u32x4, values(v[i], vlo, vstep));
+        for (int i = 0; i < kWords; ++i) tv[R::v_at(key & 31, kWords * piece + i)] = __builtin_bit_cast(u32x4, values<WIDE>(v[i], vlo, vstep));
         return u != 1.0f;
     }
 };
@@ -149,13 +179,15 @@ template <int D, int GR, int KW, bool WEIGH>
 __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     using R = Row<bf16_t, D>;
     constexpr int NW = 8, RW = NW / KW, kRows = 32 * RW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
-    __shared__ u32x4 tiles[2 * kBufs * (R::kKTile + R::kVTile)];
-    __shared__ float units[kBufs][kKeys];
+    constexpr int KT = WEIGH ? 2 : 1;  // terms of a key's elements
+    __shared__ u32x4 tiles[2 * kBufs * (KT * R::kKTile + R::kVTile)];
+    __shared__ float units[kBufs][kKeys], s_most[8][D / GR];
     __shared__ float2 s_ml[KW == 2 ? RW * 32 : 1];
     __shared__ float s_l2[KW == 2 ? RW * 32 : 1];
     __shared__ int s_bad, s_units;
     auto sk = [&](int b) { return tiles + b % kBufs * (2 * R::kKTile); };  // the two tiles of block b
     auto sv = [&](int b) { return tiles + 2 * kBufs * R::kKTile + b % kBufs * (2 * R::kVTile); };
+    constexpr int kSecond = 2 * kBufs * (R::kKTile + R::kVTile);  // from a key tile to its second terms
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rw = wave % RW, kw = wave / RW;
@@ -211,21 +243,33 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     auto load = [&](int b) {
         if (b < b1) stage.load(kc, vc, ks, vs, b * kKeys, sp.held);
     };
+    auto run = [&](auto wide_tag) {
+    constexpr bool WIDE = decltype(wide_tag)::value;
     auto keep = [&](int b) {
         if (b >= b1) return;
         bool bad = false;
-        if (stage.store(sk(b), sv(b), units[b % kBufs], (b + 1) * kKeys > see_all, sp.held - b * kKeys, bad)) s_units = 1;
+        if (stage.template store<KT, WIDE>(sk(b), sk(b) + kSecond, sv(b), units[b % kBufs], (b + 1) * kKeys > see_all, sp.held - b * kKeys, bad)) s_units = 1;
         if (bad) s_bad = 1;
     };
     auto read_k = [&](u32x4(&x)[NS], const u32x4 *sk_) {
 #pragma unroll
         for (int sl = 0; sl < NS; ++sl) x[sl] = sk_[R::k_at(n, 2 * sl + h)];
     };
-    auto logits = [&](f32x16 &s, const u32x4(&x)[NS]) {
+    // (second terms: read where they are used)
+    auto logits = [&](f32x16 &s, const u32x4(&x)[NS], const u32x4 *sk_) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        if (KT == 2) {
+            u32x4 x2[NS];
+            read_k(x2, sk_ + kSecond);
 #pragma unroll
-        for (int sl = 0; sl < NS; ++sl) s = mma32_f16(__builtin_bit_cast(uint4, x[sl]), q[sl], s);
+            for (int sl = 0; sl < NS; ++sl) s = mma32_f16(__builtin_bit_cast(uint4, x[sl]), q[sl], s);
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) s = mma32_f16(__builtin_bit_cast(uint4, x2[sl]), q[sl], s);
+        } else {
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) s = mma32_f16(__builtin_bit_cast(uint4, x[sl]), q[sl], s);
+        }
     };
     // units, masks, reference: what has to be known of the logits of the keys from kb on before their exponentials are formed
     auto settle = [&](f32x16 &s, float mx, int kb) {
@@ -265,23 +309,27 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     };
     const int v_at = v_lane(lane);
     // The next 32 keys' logits into `next` (operands: kf), their largest into mx, while the values of this 32 keys are weighed; kf then
-    // takes the operands of the keys behind those.  meet: the tile that k_after points to is whole only behind a barrier.
-    auto turn = [&](f32x16 &s, f32x16 &next, float &mx, u32x4(&kf)[NS], const u32x4 *sv_, const u32x4 *k_after, bool meet) {
+    // takes the operands of the keys behind those.  k_next: the next keys' tile; meet: the tile that k_after points to is whole only behind a barrier.
+    auto turn = [&](f32x16 &s, f32x16 &next, float &mx, u32x4(&kf)[NS], const u32x4 *k_next, const u32x4 *sv_, const u32x4 *k_after, bool meet) {
         uint4 vf[2][ND], p[2];
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int d = 0; d < ND; ++d) vf[0][d] = read_v<D>(sv_, v_at, 0, d);
-        logits(next, kf);
+        logits(next, kf, k_next);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             bf16x8 x;
+            uint32_t y[4];
+            float e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[8 * half + i], mul, -sub));
-                if (WEIGH) l2 += e;
-                x[i] = (__bf16)e;
+                e[i] = __builtin_amdgcn_exp2f(fmaf(s[8 * half + i], mul, -sub));
+                if (WEIGH) l2 += e[i];
+                x[i] = (__bf16)e[i];
             }
-            p[half] = __builtin_bit_cast(uint4, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = pair_f16(e[2 * i], e[2 * i + 1]);
+            p[half] = WIDE ? __builtin_bit_cast(uint4, x) : uint4{y[0], y[1], y[2], y[3]};
         }
 #pragma unroll
         for (int d = 0; d < ND; ++d) vf[1][d] = read_v<D>(sv_, v_at, 1, d);
@@ -290,13 +338,11 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int d = 0; d < ND; ++d) acc[d] = mma32(vf[half][d], p[half], acc[d], bf16_t());
-        l = sum_of(p[1], sum_of(p[0], l));  // the sum of what the second product takes: the outputs' weights add up to one as they are used
+            for (int d = 0; d < ND; ++d) acc[d] = WIDE ? mma32(vf[half][d], p[half], acc[d], bf16_t()) : mma32_f16(vf[half][d], p[half], acc[d]);
+        l = WIDE ? sum_of(p[1], sum_of(p[0], l)) : sum_of_f16(p[1], sum_of_f16(p[0], l));  // the sum of what the second product takes: the outputs' weights add up to one as they are used
         mx = largest(next);
         __builtin_amdgcn_s_setprio(0);
     };
-    if (threadIdx.x == 0) s_bad = s_units = 0;
-    __syncthreads();
     if (b0 < b1) {
         f32x16 sa, sb;
         float mx;
@@ -310,7 +356,7 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
         }
         lds_barrier();
         read_k(kf, sk(b0) + kw * R::kKTile);
-        logits(sa, kf);
+        logits(sa, kf, sk(b0) + kw * R::kKTile);
         settle(sa, largest(sa), b0 * kKeys + 32 * kw);
         // (behind the last block: logits of whatever lies there, not used)
         if constexpr (KW == 1) {
@@ -319,9 +365,9 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
                 const u32x4 *v_now = sv(b), *k_next = sk(b + 1);
                 keep(b + 1);  // (into the buffer of block b - 2, which every wave has left before the last barrier)
                 load(b + 2);
-                turn(sa, sb, mx, kf, v_now, k_next, true);
+                turn(sa, sb, mx, kf, sk(b) + R::kKTile, v_now, k_next, true);
                 settle(sb, mx, b * kKeys + 32);
-                turn(sb, sa, mx, kf, v_now + R::kVTile, k_next + R::kKTile, false);
+                turn(sb, sa, mx, kf, k_next, v_now + R::kVTile, k_next + R::kKTile, false);
                 if (b + 1 < b1) settle(sa, mx, (b + 1) * kKeys);
             }
         } else {
@@ -329,7 +375,7 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
             auto block = [&](int b, f32x16 &s, f32x16 &next) {
                 keep(b + 2);  // (into the buffer of block b - 1: its values were read before the last barrier)
                 load(b + 3);
-                turn(s, next, mx, kf, sv(b) + kw * R::kVTile, sk(b + 2) + kw * R::kKTile, true);
+                turn(s, next, mx, kf, sk(b + 1) + kw * R::kKTile, sv(b) + kw * R::kVTile, sk(b + 2) + kw * R::kKTile, true);
                 if (b + 1 < b1) settle(next, mx, (b + 1) * kKeys + 32 * kw);
             };
             for (int b = b0; b < b1; b += 2) {
@@ -338,6 +384,34 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
             }
         }
     }
+    };
+    // does the share of V have magnitudes that fp16 does not hold as well as their neighbours?
+    {
+        Words<D / GR> pairs;
+        float most[D / GR] = {};
+        for (int slot = b0 * kKeys + threadIdx.x; slot < min(b1 * kKeys, sp.held); slot += 64 * NW) {
+            pairs = load_words<D / GR>(vs + (size_t)slot * (D / GR));
+#pragma unroll
+            for (int g = 0; g < D / GR; ++g) most[g] = fmaxf(most[g], fmaxf(fabsf(lo_of(pairs.w[g])), fabsf(fmaf(15.0f, step_of(pairs.w[g]), lo_of(pairs.w[g])))));
+        }
+#pragma unroll
+        for (int g = 0; g < D / GR; ++g) {
+            most[g] = wave_max(most[g]);
+            if (lane == 0) s_most[wave][g] = most[g];
+        }
+    }
+    if (threadIdx.x == 0) s_bad = s_units = 0;
+    __syncthreads();
+    bool wide = false;
+#pragma unroll
+    for (int g = 0; g < D / GR; ++g) {
+        float most = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) most = fmaxf(most, s_most[w][g]);
+        wide = wide || most > kMost || (most > 0.f && most < 0x1p-4f);
+    }
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(wide), 0)) run(std::true_type());
+    else run(std::false_type());
     l += __shfl_xor(l, 32, 64);
     if (WEIGH) l2 += __shfl_xor(l2, 32, 64);
     if constexpr (KW == 2) {  // the two waves of 32 rows: lane by lane
@@ -447,7 +521,7 @@ __global__ __launch_bounds__(256) void quant_many_join_kernel(QuantAttnArgs a) {
 // The slots' weights: a wave has 64 slots, their keys as operands in registers, and meets all rows, 32 at a time, which the workgroup's
 // eight waves share in LDS.  S^T again: a lane has one row, its reference and sum, and adds up that row's share of 32 slots over all tiles of rows;
 // the lanes are added at the end, in a fixed order.  Two buffers: the next 128 rows are on their way under the products of the present ones.
-// 64 x 32 logits of a wave: 16 products of 32 clocks, 32 exponentials of 16 and two times as many other instructions of 4: the vector unit's time.
+// 64 x 32 logits of a wave: 32 products of 32 clocks; 32 exponentials of 16 clocks and 64 other instructions of 4 beside them.
 template <int D, int GR>
 __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArgs a) {
     using R = Row<bf16_t, D>;
@@ -466,7 +540,7 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
     const uint8_t *kc = a.kc + base * (D / 2);
     const uint32_t *ks = a.ks + base * NG;
     // keys: lane (n, h) has elements 8 (2 sl + h) .. + 7 of slots slot0 + n and + 32
-    uint4 k[2][NS];
+    uint4 k[2][2][NS];
     bool scaled = false;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -497,7 +571,10 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
         for (int sl = 0; sl < NS; ++sl) {  // piece 2 sl + h = 4 m + nq
             const int m = sl >> 1;
             const uint32_t p = pr[32 * m / GR];
-            k[t][sl] = key_values(w[sl & 1][m], lo_of(p) * inv, step_of(p) * inv);
+            uint4 x[2];
+            key_values<2>(w[sl & 1][m], lo_of(p) * inv, step_of(p) * inv, x);
+            k[t][0][sl] = x[0];
+            k[t][1][sl] = x[1];
         }
     }
     scaled = __any(scaled);
@@ -544,28 +621,29 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
 #pragma unroll
             for (int sl = 0; sl < NS; ++sl) q[sl] = qs[buf][t][R::k_at(n, 2 * sl + h)];
         };
-        auto logits = [&](f32x16 &s, const uint4(&key)[NS]) {
+        auto logits = [&](f32x16 &s, const uint4(&key)[2][NS]) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-            for (int sl = 0; sl < NS; ++sl) s = mma32_f16(key[sl], __builtin_bit_cast(uint4, q[sl]), s);
+            for (int term = 0; term < 2; ++term)
+#pragma unroll
+                for (int sl = 0; sl < NS; ++sl) s = mma32_f16(key[term][sl], __builtin_bit_cast(uint4, q[sl]), s);
         };
         if (__builtin_expect(!__any(odd), 1)) {
             auto add = [&](f32x16 &to, const f32x16 &s, const float4 &ref) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) to[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], ref.x, -ref.y)), ref.z, to[i]);
             };
-            // one half's products under the other's exponentials
-            f32x16 sa, sb;
-            read_q(0);
-            logits(sa, k[0]);
             for (int t = 0; t < tiles; ++t) {
                 const float4 ref = rs[buf][32 * t + n];
-                logits(sb, k[1]);
-                add(w[0], sa, ref);
-                read_q(t + 1 < tiles ? t + 1 : t);
-                logits(sa, k[0]);  // (behind the last tile: not used)
-                add(w[1], sb, ref);
+                read_q(t);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    f32x16 s;
+                    logits(s, k[x]);
+                    add(w[x], s, ref);
+                    if (D == 128) __builtin_amdgcn_sched_barrier(0);  // (both halves' logits at once do not fit the registers)
+                }
             }
             continue;
         }

@@ -44,26 +44,28 @@ def unpacked(cache):
     return out
 
 
-def attention(cache, q, held, counts, causal, scale=None):
+def attention(cache, q, held, counts, causal, scale=None, weigh=True, wide=False):
     """(out, its bound, weights, their bound) of every sequence, fp64: lists over the batch of [Hq][count][d] and [H][held].
 
     Bounds: a logit is a sum of d products step q code and as many q lo, each exact or rounded to fp32, whose sums round once per term (bf16:
     codes have 16 added, and taken off again: 16 step q twice more); the exponent and the power of two (2^-22); sums of `held` terms; the factor
-    p step keeps 11 bits (bf16: half a step 2^-11, and of numbers below 2^-14 the absolute 2^-25, in units of at most the greatest step of the
-    group in the sequence, times a code) or 24; outputs are rounded once.  bf16 calls of 65 rows and more: K in fp16 (half a step 2^-11, and 2^-25 of
-    rows of at least 2^-6), V, the probabilities and, by them, their sum in bf16."""
+    p step keeps 15 bits (bf16: a first term cut off, 2^-7, the rest rounded, 2^-8) or 24; outputs are rounded once.
+
+    bf16 calls of 65 rows and more: V and the probabilities, and with these their sum, are rounded to fp16 (half a step 2^-11; probabilities below
+    2^-14 of a reference that is at most 2^8 above the largest by 2^-25) or, where values have no ordinary magnitude (`wide`), to bf16 (2^-8);
+    without weights, K in fp16 (2^-11, and 2^-25 of rows of at least 2^-6), with them in two such terms."""
     import torch
 
     d, H = cache.head_dim, cache.n_kv_heads
     g = q.shape[1] // H
     scale = scale or d ** -0.5
     half = 2.0 ** -8 if q.dtype == torch.bfloat16 else 2.0 ** -24
-    (klo, kst, kstep), (vlo, vst, vstep) = unpacked(cache)
+    (klo, kst, kstep), (vlo, vst, _) = unpacked(cache)
     extra = 32.0 * kstep if q.dtype == torch.bfloat16 else 0.0 * kstep
     result = []
     for b, (n, c) in enumerate(zip(held, counts)):
         qs = q[b, :, :c].double()
-        kl, ks, vl, vs, ke, vst1 = (x[b, :, :n].repeat_interleave(g, dim=0) for x in (klo, kst, vlo, vst, extra, vstep))
+        kl, ks, vl, vs, ke = (x[b, :, :n].repeat_interleave(g, dim=0) for x in (klo, kst, vlo, vst, extra))
         t = lambda x: x.transpose(1, 2).contiguous()  # noqa: E731
         s = qs @ t(kl + ks) * scale
         size = qs.abs() @ t(kl.abs() + ks + ke) * scale
@@ -79,15 +81,15 @@ def attention(cache, q, held, counts, causal, scale=None):
         if n and q.dtype == torch.bfloat16 and q.shape[2] * g >= 65:
             dot = (qs.abs() @ t((kl + ks).abs()) * scale).masked_fill(~seen, 0.0)
             least = qs.abs().sum(-1, keepdim=True) * (kl + ks).abs().amax((1, 2), keepdim=True) * scale * 2.0 ** -19
-            off = off + dot.amax(-1, keepdim=True) * 2.0 ** -11 + least
+            off = off + (dot.amax(-1, keepdim=True) * 2.0 ** -11 + least) * (2.0 ** -11 if weigh else 1.0)
         rel = 2 * (torch.expm1(off) + 2.0 ** -22 + (n + 64) * 2.0 ** -24)
         vl_seen = torch.where(torch.isfinite(vl), vl, 0.0) if not bool(seen.all()) else vl
         o, a = p @ (vl_seen + vs), p @ (vl_seen.abs() + vs)
         low = half > 2.0 ** -20  # bf16
         many = low and q.shape[2] * g >= 65
-        err = a * (rel + (3 * 2.0 ** -8 if many else 2.0 ** -11 if low else 2.0 ** -22))
-        if low and n and not many:
-            err = err + vst1.amax(1, keepdim=True) * (n * 15 * 2.0 ** -25)
+        err = a * (rel + (3 * 2.0 ** (-8 if wide else -11) if many else 2.0 ** -15 if low else 2.0 ** -22))
+        if many and n and not wide:
+            err = err + (vl_seen.abs() + vs).amax(1, keepdim=True) * (2 * n * 2.0 ** -25) + n * 2.0 ** -25
         bound = err * 1.01 + (o.abs() + err) * half + 1e-37
         w = p.reshape(H, g * c, n).sum(1)
         wb = (p * rel).reshape(H, g * c, n).sum(1) * 1.01 + w * (g * c + 8) * 2.0 ** -24 + 1e-37

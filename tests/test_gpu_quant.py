@@ -137,7 +137,7 @@ def test_rows_outside_the_capacity_are_dropped():
 
 
 # ---- attention -------------------------------------------------------------------------------------------------------------------
-def _check(A, cache, q, held, counts, causal, seed=0, weigh=True, scale=0.0, lens=None, k=None, v=None, with_out=True, **kw):
+def _check(A, cache, q, held, counts, causal, seed=0, weigh=True, scale=0.0, lens=None, k=None, v=None, with_out=True, wide=False, **kw):
     """One call against the definition; `held`: slots after it."""
     import torch
 
@@ -148,7 +148,7 @@ def _check(A, cache, q, held, counts, causal, seed=0, weigh=True, scale=0.0, len
     A.air_quant_attn(cache, q, out if with_out else None, lens=_ints(held if lens is None else lens), counts=_ints(counts), causal=causal, scale=scale,
                      weights=w if weigh else None, k=k, v=v, **kw)
     torch.cuda.synchronize()
-    for b, (o, bound, ww, wb) in enumerate(attention(cache, q, held, counts, causal, scale or None)):
+    for b, (o, bound, ww, wb) in enumerate(attention(cache, q, held, counts, causal, scale or None, weigh, wide)):
         c, n = counts[b], held[b]
         if with_out:
             far = (out[b, :, :c].double() - o).abs()
@@ -232,7 +232,28 @@ def test_magnitudes(rows, k_size, q_size, v_size):
     A.air_quant_append(cache, k.bfloat16(), v.bfloat16())
     q = _randn(5, 1, 2, rows, 128)
     q[:, 0] *= q_size
-    _check(A, cache, q.bfloat16(), [300], [rows], False)
+    _check(A, cache, q.bfloat16(), [300], [rows], False, wide=True)
+    _check(A, cache, q.bfloat16(), [300], [rows], False, weigh=False, wide=True)
+
+
+@pytest.mark.parametrize("dtype,d,group", KINDS)
+@pytest.mark.parametrize("rows", [1, 12, 100])
+def test_large_values_that_weigh_nothing(dtype, d, group, rows):
+    """A value 2^100 times as large as the others, at a key that no row looks at, takes nothing from them."""
+    import paper_2503_23956_amd as A
+
+    cache = _new(A, 1, 1, 200, d, dtype, group)
+    k, v = (_randn(i, 1, 1, 200, d) for i in range(2))
+    v[:, :, 50] *= 2.0 ** 100
+    v[:, :, 51] *= 2.0 ** 12
+    k[..., 0] = 0.0
+    k[:, :, 50:52, 0] = -4000.0
+    A.air_quant_append(cache, k.to(_type(dtype)), v.to(_type(dtype)))
+    q = _randn(5, 1, 1, rows, d)
+    q[..., 0] = 8.0
+    q = q.to(_type(dtype))
+    out, w = _check(A, cache, q, [200], [rows], False, wide=True)
+    assert float(out.abs().max()) < 10.0
 
 
 @pytest.mark.parametrize("dtype,d,group", KINDS)
