@@ -6,7 +6,7 @@
 // destinations in front of it, so that rows move in any order.  Few rows are moved by the same workgroup; where there can be many, a
 // second launch over all of the chip moves them by a list.
 //
-// A wave has a run of the slots, a lane four of them at a time; keys stay in LDS (capacities up to 32768; beyond, they are formed
+// A wave has a run of the slots, a lane four of them at a time; keys stay in LDS (capacities up to 24576; beyond, they are formed
 // again, out of the L2 cache, wherever they are used).  What a call takes is dependent accesses, barriers and the instructions of
 // one pass over code that is new to the CU: loops are not unrolled (keys in registers, 16 to 32 slots unrolled: 18 us in place of 15, one sequence of
 // 7432 slots cut to 743).  16 x 4 heads of 2368 slots of which 64 go, K and V rows of 256 bytes with them: 10 us.
@@ -16,6 +16,7 @@
 namespace air {
 
 constexpr int kEvictWaves = 16, kEvictThreads = 64 * kEvictWaves;
+constexpr int kCopies = 4;  // of every bin: additions of one wave to one bin take turns (16910 equal weights 8 us a pass with one copy)
 constexpr int kLdsMoves = 2048, kBins = 2048, kDirect = 256;  // kDirect: slots of the deciding digit that are ranked directly
 constexpr size_t kAlone = 128 << 10;  // bytes of rows that one workgroup moves by itself
 
@@ -100,7 +101,8 @@ __device__ __forceinline__ void move_weights(float *weights, int32_t *positions,
 template <int KEYS>
 __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a) {
     __shared__ __align__(16) uint32_t keys[KEYS ? KEYS : 4];
-    __shared__ int32_t bins[kBins], moves[2 * kLdsMoves], sums[kEvictWaves], found[3], last_of[kEvictWaves];
+    __shared__ __align__(16) int32_t bins[kBins * kCopies];
+    __shared__ int32_t moves[2 * kLdsMoves], sums[kEvictWaves], found[3], last_of[kEvictWaves];
     __shared__ uint64_t few[kDirect];  // (key, ~slot): larger goes first
     __shared__ int32_t n_few;
     __shared__ uint64_t border_at;
@@ -108,7 +110,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a) {
     const int pair = blockIdx.x, b = a.by_heads.of(pair), h = pair - b * a.n_heads;
     float *weights = a.weights + (size_t)pair * a.capacity;
     int32_t *positions = a.positions ? a.positions + (size_t)pair * a.capacity : nullptr;
-    for (int i = tid; i < kBins; i += kEvictThreads) bins[i] = 0;
+    for (int i = tid; i < kBins; i += kEvictThreads) *reinterpret_cast<int4 *>(bins + kCopies * i) = int4{0, 0, 0, 0};
     if (tid == 0) n_few = 0;
     int n = a.lens[b];
     n = n < 0 ? 0 : n > a.capacity ? a.capacity : n;
@@ -218,17 +220,18 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
         const uint32_t digits = pass == 2 ? 0x3ffu : 0x7ffu;
         if (pass > 0) {
-            for (int i = tid; i < kBins; i += kEvictThreads) bins[i] = 0;
+            for (int i = tid; i < kBins; i += kEvictThreads) *reinterpret_cast<int4 *>(bins + kCopies * i) = int4{0, 0, 0, 0};
             __syncthreads();
         }
         each([&](int s, const Four &v) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (s + i < end && (v.k[i] & mask) == value) atomicAdd(&bins[v.k[i] >> shift & digits], 1);
+                if (s + i < end && (v.k[i] & mask) == value) atomicAdd(&bins[(v.k[i] >> shift & digits) * kCopies + (lane & (kCopies - 1))], 1);
         });
         __syncthreads();
         // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t
-        const int c0 = bins[kBins - 1 - 2 * tid], c1 = bins[kBins - 2 - 2 * tid], mine = wave_incl_scan(c0 + c1);
+        const int4 x0 = *reinterpret_cast<const int4 *>(bins + kCopies * (kBins - 1 - 2 * tid)), x1 = *reinterpret_cast<const int4 *>(bins + kCopies * (kBins - 2 - 2 * tid));
+        const int c0 = (x0.x + x0.y) + (x0.z + x0.w), c1 = (x1.x + x1.y) + (x1.z + x1.w), mine = wave_incl_scan(c0 + c1);
         if (lane == 63) sums[wave] = mine;
         __syncthreads();
         int above = mine - c0 - c1;
@@ -400,7 +403,7 @@ hipError_t launch_evict(hipStream_t s, const air_evict_config &c, float *weights
     while (a.lanes < a.words && a.lanes < 64) a.lanes *= 2;
     const int pairs = c.batch * c.n_heads;
     if (c.capacity <= 4096) evict_kernel<4096><<<pairs, kEvictThreads, 0, s>>>(a);
-    else if (c.capacity <= 32768) evict_kernel<32768><<<pairs, kEvictThreads, 0, s>>>(a);
+    else if (c.capacity <= 24576) evict_kernel<24576><<<pairs, kEvictThreads, 0, s>>>(a);
     else evict_kernel<0><<<pairs, kEvictThreads, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.moves) return e;

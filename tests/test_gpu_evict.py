@@ -116,9 +116,9 @@ def test_protected_tokens():
     _check(w, (pos - 300).astype(np.int32), [600, 600], 100, 100, first=0, recent=30)
 
 
-@pytest.mark.parametrize("n,keep", [(4000, 3900), (4093, 700), (4094, 4000), (16381, 9000), (16382, 16000), (20001, 9000), (20001, 200), (32766, 5000), (70000, 33000)])
+@pytest.mark.parametrize("n,keep", [(4000, 3900), (4093, 700), (4094, 4000), (16381, 9000), (16382, 16000), (20001, 9000), (20001, 200), (24573, 12000), (24574, 5000), (70000, 33000)])
 def test_many_slots(n, keep):
-    """Keys in 4, 16 and 32 registers a lane and in none, more moves than one workgroup takes, ties by the thousand."""
+    """Keys in LDS and formed again, more moves than one workgroup takes, ties by the thousand."""
     rng = np.random.default_rng(n)
     cap = n + 3
     w = np.exp(2 * rng.standard_normal((2, 2, cap))).astype(np.float32)
