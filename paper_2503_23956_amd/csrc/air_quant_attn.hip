@@ -39,20 +39,40 @@ struct QueryTile {
     using S = QuantShape<D, GR, T>;
     uint4 e[S::QT][S::KM], sums;
 
-    __device__ __forceinline__ void load(const QuantAttnArgs &a, const QuantSpan &sp, int row) {
+    uint4 raw[S::kF32 ? 2 * S::KM : 1];  // fp32: as they are read
+
+    __device__ __forceinline__ void request(const QuantAttnArgs &a, int b, int h, int row, int rows) {
         const int c = (threadIdx.x >> 4) & 3;
-        float part[S::NG] = {};
-        const bool real = row < sp.rows;
+        const bool real = row < rows;
         const int t = a.by_g.of(real ? row : 0), i = (real ? row : 0) - t * a.G;
-        const T *q = static_cast<const T *>(a.q) + sp.b * a.q_b + ((int64_t)sp.h * a.G + i) * a.q_h + t * a.q_t + 8 * c;
+        const T *q = static_cast<const T *>(a.q) + b * a.q_b + ((int64_t)h * a.G + i) * a.q_h + t * a.q_t + 8 * c;
 #pragma unroll
         for (int m = 0; m < S::KM; ++m) {
             uint4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
             if (real) x = *reinterpret_cast<const uint4 *>(q + 32 * m);
             if (S::kF32 && real) y = *reinterpret_cast<const uint4 *>(q + 32 * m + 4);
+            if (S::kF32) {
+                raw[2 * m % (S::kF32 ? 2 * S::KM : 1)] = x;
+                raw[(2 * m + 1) % (S::kF32 ? 2 * S::KM : 1)] = y;
+            } else {
+                e[0][m] = x;
+            }
+        }
+    }
+    // real: false makes it a row of zeros
+    __device__ __forceinline__ void form(bool real) {
+        const int c = (threadIdx.x >> 4) & 3;
+        float part[S::NG] = {};
+#pragma unroll
+        for (int m = 0; m < S::KM; ++m) {
             float sum = 0.0f;
             if constexpr (S::kF32) {
-                const f32x4 u = __builtin_bit_cast(f32x4, x), v = __builtin_bit_cast(f32x4, y);
+                f32x4 u = __builtin_bit_cast(f32x4, raw[2 * m]), v = __builtin_bit_cast(f32x4, raw[2 * m + 1]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    u[k] = real ? u[k] : 0.0f;
+                    v[k] = real ? v[k] : 0.0f;
+                }
                 uint32_t w[4][S::QT];
                 // (the order in which operand_of gives K's codes)
                 split_pair<S::QT>(u[0], v[0], w[0]);
@@ -63,10 +83,13 @@ struct QueryTile {
                 for (int k = 0; k < S::QT; ++k) e[k][m] = uint4{w[0][k], w[1][k], w[2][k], w[3][k]};
                 sum = ((u[0] + u[1]) + (u[2] + u[3])) + ((v[0] + v[1]) + (v[2] + v[3]));
             } else {
-                e[0][m] = x;
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                uint32_t w[4] = {e[0][m].x, e[0][m].y, e[0][m].z, e[0][m].w};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum += __uint_as_float(w[k] << 16) + __uint_as_float(w[k] & 0xffff0000u);
+                for (int k = 0; k < 4; ++k) {
+                    w[k] = real ? w[k] : 0u;
+                    sum += __uint_as_float(w[k] << 16) + __uint_as_float(w[k] & 0xffff0000u);
+                }
+                e[0][m] = uint4{w[0], w[1], w[2], w[3]};
             }
             part[m / S::KG] += sum;
         }
@@ -152,7 +175,7 @@ struct KeyRun {
     Words<D / 32> code[4];
     Words<D / GR> pair[4];
     // row: of the pair's first slot; slots from `held` on are read as the last one
-    __device__ __forceinline__ void load(const uint8_t *codes, const uint32_t *pairs, int slot0, int held) {
+    __device__ __forceinline__ void load(const uint8_t *codes, const uint32_t *pairs, int slot0, int held) {  // held: or the capacity, for slots that are masked later
         const int n = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -204,7 +227,10 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
 
     QueryTile<D, GR, T> q[RT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) q[r].load(a, sp, row0 + 16 * r + n);
+    for (int r = 0; r < RT; ++r) {
+        q[r].request(a, sp.b, sp.h, row0 + 16 * r + n, sp.rows);
+        q[r].form(true);
+    }
 
     f32x4 acc[RT][S::NT];
     float m[RT][4], l[RT][4], al[RT][4][NG];
@@ -434,7 +460,8 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
         __syncthreads();
         for (int r = wave; r < tiles; r += 4) {
             QueryTile<D, GR, T> q;
-            q.load(a, sp, row0 + 16 * r + n);
+            q.request(a, sp.b, sp.h, row0 + 16 * r + n, sp.rows);
+            q.form(true);
 #pragma unroll
             for (int k = 0; k < S::QT; ++k)
 #pragma unroll
@@ -503,14 +530,14 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
 // rows 8 .. 15, joined at the end, the third one in a product of its own.  (One fp16 number would be 10 % fewer instructions, but its range
 // needs a unit, and next to a value 2^20 times as large, whatever that weighs, the others' codes would be lost.)
 //
-// The wave whose run has slots that the call appends writes them first.
+// The wave whose run has slots that the call appends writes them, and takes them from LDS into what it has read of the run.
 // ---------------------------------------------------------------------------------------
 template <int D, int GR, typename T>
 struct FewShape {
     using S = QuantShape<D, GR, T>;
     static constexpr int kWStride = 144, kWRows = S::kF32 ? 24 : 16;  // bytes: 64 places of 16 bits and 16 more, 16 rows on different banks
     static constexpr int kWBytes = S::NG * kWRows * kWStride, kWave = S::kVBytes + kWBytes;
-    static constexpr int kLds = 4 * kWave > 4 * 8 * D * 4 + 4 * 8 * 8 ? 4 * kWave : 4 * 8 * D * 4 + 4 * 8 * 8;
+    static constexpr int kEnd = 4 * 16 * D * 4 + 4 * 16 * 8, kLds = 4 * kWave > kEnd ? 4 * kWave : kEnd;
 };
 
 // (x of lanes 0 .. 31, y of lanes 0 .. 31)
@@ -521,32 +548,45 @@ __device__ __forceinline__ float max_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float add_halves(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// the wave's rows of slots slot0 .. slot0 + 63 that the call appends
+// What the call appends, in codes, for the wave whose run has its slots: it does not wait for the cache's memory to have them
+template <int D, int GR>
+struct alignas(16) NewRow {
+    uint32_t k[D / 8], v[D / 8], kp[D / GR], vp[D / GR];
+};
+// rows of slots slot0 .. slot0 + 63 into the cache and, token by token of the call, into `rows`.  first: the eight elements of K and V that the lane
+// has requested of token lane / (D / 8)
 template <int D, int GR, typename T>
-__device__ __forceinline__ void append_run(const QuantAttnArgs &a, const QuantSpan &sp, int slot0) {
-    constexpr int kLanes = D / 8;
+__device__ __forceinline__ void append_run(const QuantAttnArgs &a, const QuantSpan &sp, int slot0, const float (&first)[2][8], NewRow<D, GR> *rows) {
+    constexpr int kLanes = D / 8, kRows = 64 / kLanes;
     const int lane = threadIdx.x & 63, p = lane & (kLanes - 1);
-    const int64_t len = (int64_t)sp.held_before;
-    for (int64_t t = slot0 - len + lane / kLanes; t < slot0 + kRun - len; t += 64 / kLanes) {
-        if (t < 0 || t >= sp.count || len + t >= sp.held) continue;
-        const int64_t cell = ((int64_t)sp.b * a.Hkv + sp.h) * a.capacity + len + t;
-        append_row<D, GR, T, true>(static_cast<const T *>(a.rows.rows[0]) + sp.b * a.rows.row_b[0] + sp.h * a.rows.row_h[0] + t * a.rows.row_t[0],
-                                   reinterpret_cast<uint32_t *>(a.rows.codes[0] + cell * (D / 2)), a.rows.scales[0] + cell * (D / GR), p);
-        append_row<D, GR, T, false>(static_cast<const T *>(a.rows.rows[1]) + sp.b * a.rows.row_b[1] + sp.h * a.rows.row_h[1] + t * a.rows.row_t[1],
-                                    reinterpret_cast<uint32_t *>(a.rows.codes[1] + cell * (D / 2)), a.rows.scales[1] + cell * (D / GR), p);
+    for (int t0 = 0; t0 < sp.count; t0 += kRows) {
+        const int t = t0 + lane / kLanes;
+        const int64_t slot = (int64_t)sp.held_before + t;
+        if (t >= sp.count || slot < slot0 || slot >= slot0 + kRun || slot >= sp.held) continue;
+        const int64_t cell = ((int64_t)sp.b * a.Hkv + sp.h) * a.capacity + slot;
+        float x[2][8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (t0 > 0) {
+                load8(static_cast<const T *>(a.rows.rows[i]) + sp.b * a.rows.row_b[i] + sp.h * a.rows.row_h[i] + t * a.rows.row_t[i] + 8 * p, x[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] = first[i][e];
+            }
+        }
+        uint32_t pair[2];
+        const uint32_t k = codes_of<GR, true>(x[0], pair[0]), v = codes_of<GR, false>(x[1], pair[1]);
+        reinterpret_cast<uint32_t *>(a.rows.codes[0] + cell * (D / 2))[dword_of<D, true>(p)] = rows[t].k[dword_of<D, true>(p)] = k;
+        reinterpret_cast<uint32_t *>(a.rows.codes[1] + cell * (D / 2))[p] = rows[t].v[p] = v;
+        if ((p & (GR / 8 - 1)) == 0) {
+            a.rows.scales[0][cell * (D / GR) + p / (GR / 8)] = rows[t].kp[p / (GR / 8)] = pair[0];
+            a.rows.scales[1][cell * (D / GR) + p / (GR / 8)] = rows[t].vp[p / (GR / 8)] = pair[1];
+        }
         if (p == 0) {
-            if (a.rows.positions) a.rows.positions[cell] = a.rows.first[sp.b] + (int)t;
+            if (a.rows.positions) a.rows.positions[cell] = a.rows.first[sp.b] + t;
             if (a.rows.weights) a.rows.weights[cell] = 0.0f;
         }
     }
-    // in this XCD's L2 before the wave reads them, and nothing older in the first-level cache
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
 }
 
 template <int D, int GR, typename T>
@@ -556,30 +596,42 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
     constexpr int NG = S::NG;
     __shared__ __align__(16) uint8_t lds[F::kLds];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4, upper = c >> 1, rc = c & 1;
-    const int pair = blockIdx.y, split = blockIdx.x;
-    const QuantSpan sp(a, pair);
+    __shared__ NewRow<D, GR> news[4][kFewRows];
+    const int pair = blockIdx.y, split = blockIdx.x, b = a.by_hkv.of(pair), h = pair - b * a.Hkv;
+
+    // requested before the sequence's length is there: the wave's first run (whatever lies in it), queries, new rows
+    const size_t base = (size_t)pair * a.capacity;
+    const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
+    const uint32_t *ks = a.ks + base * NG, *vs = a.vs + base * NG;
+    const int stride = 4 * a.splits;
+    int u = split * 4 + wave;
+    KeyRun<D, GR> key;
+    QueryTile<D, GR, T> q;
+    q.request(a, b, h, n, a.n_rows);
+    if (u * kRun < a.capacity) key.load(kc, ks, u * kRun, a.capacity);
     const bool append = a.rows.rows[0] != nullptr;
+    float first[2][8] = {};
+    if (append && lane / (D / 8) < a.n_tokens) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            load8(static_cast<const T *>(a.rows.rows[i]) + b * a.rows.row_b[i] + h * a.rows.row_h[i] + lane / (D / 8) * a.rows.row_t[i] + 8 * (lane & (D / 8 - 1)), first[i]);
+    }
+    const QuantSpan sp(a, pair);
     if (sp.rows == 0) return;
+    q.form(n < sp.rows);
     const int most = sp.seen(a, sp.rows - 1), least = sp.seen(a, 0);
+    const int runs = (most + kRun - 1) / kRun;
+    int new_run = -1;  // the wave's run with slots that the call appends: at most two runs have any
+    if (append) {
+        const int r0 = sp.held_before < 0 ? 0 : sp.held_before / kRun;
+        for (int r = r0; r < runs && r < r0 + 2; ++r)
+            if (r - a.by_stride.of(r) * stride == u) new_run = r;
+        if (new_run >= 0) append_run<D, GR, T>(a, sp, new_run * kRun, first, news[wave]);
+    }
 
     uint8_t *vb = lds + wave * F::kWave, *wb = vb + S::kVBytes;
     const int k_of = 16 * c + (n & 8) + ((n & 1) ? 4 + ((n & 7) >> 1) : (n & 7) >> 1);  // (as in the kernel for more rows)
     const uint8_t *v_read = vb + (16 * (k_of & 3) + (k_of >> 2)) * S::kVStride;
-
-    const size_t base = (size_t)pair * a.capacity;
-    const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
-    const uint32_t *ks = a.ks + base * NG, *vs = a.vs + base * NG;
-    const int runs = (most + kRun - 1) / kRun, stride = 4 * a.splits;
-    int u = split * 4 + wave;
-    KeyRun<D, GR> key;
-    if (append) {  // at most two runs have slots of its rows
-        const int first = sp.held_before < 0 ? 0 : sp.held_before / kRun;
-        for (int r = first; r < runs && r < first + 2; ++r)
-            if (r - a.by_stride.of(r) * stride == u) append_run<D, GR, T>(a, sp, r * kRun);
-    }
-    if (u < runs) key.load(kc, ks, u * kRun, sp.held);
-    QueryTile<D, GR, T> q;
-    q.load(a, sp, n);
 
     f32x4 acc[S::NT];
     float m[4], limit[4], l[4], al[4][NG];
@@ -601,13 +653,33 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         Words<NG> vp[2];
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int at = u * kRun + i * (64 / kPieces) + lane / kPieces, slot = at < sp.held ? at : sp.held - 1;
-            code[i] = *reinterpret_cast<const uint4 *>(vc + (size_t)(uint32_t)slot * (D / 2) + 16 * (lane % kPieces));
+            const int at = u * kRun + i * (64 / kPieces) + lane / kPieces, slot = at < a.capacity ? at : a.capacity - 1;
+            code[i] = *reinterpret_cast<const uint4 *>(vc + ((uint32_t)slot * (D / 2) + 16 * (lane % kPieces)));
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int at = u * kRun + 16 * t + 32 * upper + n, slot = at < sp.held ? at : sp.held - 1;
-            vp[t] = load_words<NG>(vs + (size_t)(uint32_t)slot * NG);
+            const int at = u * kRun + 16 * t + 32 * upper + n, slot = at < a.capacity ? at : a.capacity - 1;
+            vp[t] = load_words<NG>(reinterpret_cast<const uint8_t *>(vs) + (uint32_t)slot * (NG * 4));
+        }
+        if (u == new_run) {  // slots of the call's own rows: what was read there is not them yet
+            for (int t = 0; t < sp.count; ++t) {
+                const int slot = sp.held_before + t - u * kRun;
+                if (slot < 0 || slot >= kRun) continue;
+                const NewRow<D, GR> &row = news[wave][t];
+                wave_sync();
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (slot == 16 * x + n) {
+                        key.code[x] = load_words<D / 32>(row.k + D / 32 * c);
+                        key.pair[x] = load_words<NG>(row.kp);
+                    }
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i)
+                    if (slot == i * (64 / kPieces) + lane / kPieces) code[i] = *reinterpret_cast<const uint4 *>(row.v + 4 * (lane % kPieces));
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (slot == 16 * x + 32 * upper + n) vp[x] = load_words<NG>(row.vp);
+            }
         }
         const bool masked = (u + 1) * kRun > least;
         const int next = u + stride < runs ? u + stride : u;
@@ -621,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
             s4[t] = logits<D, GR, T>(q, k, key.pair[t], lo_operand<NG>(key.pair[t]));
             __builtin_amdgcn_sched_barrier(0);  // (operands of all four tiles at once do not fit the registers)
         }
-        key.load(kc, ks, next * kRun, sp.held);
+        key.load(kc, ks, next * kRun, a.capacity);
         f32x4 s[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -745,28 +817,26 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
 
     // ---- the lanes' sums, then the four waves'
     __syncthreads();
-    float *ob = reinterpret_cast<float *>(lds);  // [wave][8 rows][D]
-    float2 *mlb = reinterpret_cast<float2 *>(lds + 4 * 8 * D * 4);
+    float *ob = reinterpret_cast<float *>(lds);  // [wave][half of the lanes][8 rows][D]: the halves are added with the waves
+    float2 *mlb = reinterpret_cast<float2 *>(lds + 4 * 16 * D * 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        l[i] = add_halves(sum16(l[i]));
+        const int at = wave * 16 + 8 * upper + 4 * rc + i;
+        l[i] = sum16(l[i]);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) al[i][g] = add_halves(sum16(al[i][g]));
+        for (int g = 0; g < NG; ++g) al[i][g] = sum16(al[i][g]);
 #pragma unroll
-        for (int j = 0; j < S::NT; ++j) {
-            const float o = add_halves(acc[j][i]) + al[i][j / (GR / 16)];
-            if (upper == 0) ob[(wave * 8 + 4 * rc + i) * D + 16 * j + n] = o;
-        }
-        if (n == 0 && upper == 0) mlb[wave * 8 + 4 * rc + i] = float2{m[i], l[i]};
+        for (int j = 0; j < S::NT; ++j) ob[at * D + 16 * j + n] = acc[j][i] + al[i][j / (GR / 16)];
+        if (n == 0) mlb[at] = float2{m[i], l[i]};
     }
     __syncthreads();
     const int row = threadIdx.x >> 5, x = threadIdx.x & 31;
     if (row < sp.rows) {
-        float high = -INFINITY, f[4], sum = 0.0f;
+        float high = -INFINITY, f[8], sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) high = fmaxf(high, mlb[w * 8 + row].x);
+        for (int w = 0; w < 8; ++w) high = fmaxf(high, mlb[w * 8 + row].x);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < 8; ++w) {
             f[w] = part_weight(mlb[w * 8 + row].x, mlb[w * 8 + row].y, high);
             sum = fmaf(f[w], mlb[w * 8 + row].y, sum);
         }
@@ -780,7 +850,7 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
             for (int j = 0; j < D / 32; ++j) {
                 float o = 0.0f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) o = fmaf(f[w], ob[(w * 8 + row) * D + 32 * j + x], o);
+                for (int w = 0; w < 8; ++w) o = fmaf(f[w], ob[(w * 8 + row) * D + 32 * j + x], o);
                 if (a.splits > 1) a.part_o[part * D + 32 * j + x] = o;
                 else put(to + 32 * j + x, o * inv);
             }

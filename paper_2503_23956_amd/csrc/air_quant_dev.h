@@ -122,10 +122,9 @@ __device__ __forceinline__ int dword_of(int p) {
     return K ? D / 32 * (p & 3) + (p >> 2) : p;
 }
 
-template <int D, int GR, typename T, bool K>
-__device__ __forceinline__ void append_row(const T *src, uint32_t *codes, uint32_t *scales, int p) {
-    float x[8];
-    load8(src + 8 * p, x);
+// eight elements as codes; pair: (lo, step) of their group
+template <int GR, bool K>
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], uint32_t &pair) {
     float low = x[0], high = x[0];
     bool number = true;
 #pragma unroll
@@ -136,7 +135,7 @@ __device__ __forceinline__ void append_row(const T *src, uint32_t *codes, uint32
     }
     if (!number) high = INFINITY;
     range_of<GR / 8>(low, high);
-    const uint32_t pair = pair_of(low, high);
+    pair = pair_of(low, high);
     const float lo = lo_of(pair), step = step_of(pair), inv = 1.0f / step;
     uint32_t code = 0;
 #pragma unroll
@@ -147,7 +146,14 @@ __device__ __forceinline__ void append_row(const T *src, uint32_t *codes, uint32
         const uint32_t c = step > 0.0f ? (uint32_t)fminf(rintf(s), 15.0f) : 0u;
         code |= c << code_shift<K>(i);
     }
-    codes[dword_of<D, K>(p)] = code;
+    return code;
+}
+template <int D, int GR, typename T, bool K>
+__device__ __forceinline__ void append_row(const T *src, uint32_t *codes, uint32_t *scales, int p) {
+    float x[8];
+    load8(src + 8 * p, x);
+    uint32_t pair;
+    codes[dword_of<D, K>(p)] = codes_of<GR, K>(x, pair);
     if ((p & (GR / 8 - 1)) == 0) scales[p / (GR / 8)] = pair;
 }
 
