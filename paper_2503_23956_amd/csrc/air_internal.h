@@ -186,7 +186,7 @@ struct QuantPlan {
     int32_t max_runs;                       // runs of 64 slots per (sequence, KV head) whose logits are kept; 0: none
     int32_t tile_rows;                      // many rows: 128 or 256 a workgroup; else 0
     int32_t max_len;                        // slots that the launch is shaped for (many rows: that it covers, the capacity)
-    size_t l2_at, ref_at, q_at;             // many rows with weights: where second sums, references and queries in fp16 lie
+    size_t l2_at, ref_at, sums_at;          // many rows with weights: where second sums, references and sums of queries lie
     int32_t finish;                         // workgroups per (sequence, KV head) of the second launch; 0: none
     size_t ml_bytes, kept_at, bytes;        // workspace: (maximum, sum) pairs in front, where the logits lie, all of it
 };

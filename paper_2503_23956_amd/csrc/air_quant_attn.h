@@ -18,8 +18,8 @@ struct QuantAttnArgs {
     float2 *part_ml;  // [pair][split][row]
     // many rows with weights:
     float *part_l2;    // [pair][split][row]: sums of the unrounded probabilities
-    float4 *row_ref;   // [pair][row]: factor of the logits, reference, 1 / sum, slots seen (whole number)
-    uint16_t *row_q;   // [pair][row][D]: queries in fp16, divided by their units
+    float4 *row_ref;   // [pair][row]: reference, 1 / sum, slots seen (whole number), nothing
+    uint4 *row_sums;   // [pair][row][2]: sums of the queries' groups as bf16 terms, as the product with lo takes them
     float *weights;
     int64_t q_b, q_h, q_t, out_b, out_h, out_t;
     const int32_t *lens, *counts;

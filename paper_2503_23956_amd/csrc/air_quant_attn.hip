@@ -955,8 +955,8 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
         if (p.splits > 1) p.ml_bytes = whole(cells * sizeof(float2));
         p.l2_at = p.ml_bytes + (p.splits > 1 ? whole(cells * c.head_dim * sizeof(float)) : 0);
         p.ref_at = p.l2_at + (q.weights && p.splits > 1 ? whole(cells * sizeof(float)) : 0);
-        p.q_at = p.ref_at + (q.weights ? whole((size_t)pairs * rows * sizeof(float4)) : 0);
-        p.bytes = p.q_at + (q.weights ? whole((size_t)pairs * rows * c.head_dim * 2) : 0);
+        p.sums_at = p.ref_at + (q.weights ? whole((size_t)pairs * rows * sizeof(float4)) : 0);
+        p.bytes = p.sums_at + (q.weights ? whole((size_t)pairs * rows * 2 * sizeof(uint4)) : 0);
         p.max_len = c.capacity;
         const int places = 1024 / c.head_dim;
         int groups = 1;
@@ -1057,7 +1057,7 @@ hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const Quan
     uint8_t *space = static_cast<uint8_t *>(workspace);
     a.part_l2 = reinterpret_cast<float *>(space + p.l2_at);
     a.row_ref = reinterpret_cast<float4 *>(space + p.ref_at);
-    a.row_q = reinterpret_cast<uint16_t *>(space + p.q_at);
+    a.row_sums = reinterpret_cast<uint4 *>(space + p.sums_at);
     if (p.tile_rows) return launch_quant_many(s, a, p, c.head_dim, c.group, pairs);
 #define AIR_CASE(D, GR, T, F) \
     if (c.head_dim == D && c.group == GR && c.dtype == F) return run_quant_attn<D, GR, T>(s, a, p, pairs);

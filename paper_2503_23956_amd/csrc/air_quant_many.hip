@@ -173,6 +173,25 @@ struct CodeStage {
     }
 };
 
+// Sums of a query's groups as three bf16 terms each, for a product of 16 with the slots' lo: contraction indices 0 .. 7 and 8 .. 15
+template <int NG>
+__device__ __forceinline__ void write_sums(const float (&part)[NG], uint4 *to) {
+    uint32_t t[NG][3];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) split_pair<3>(part[g], 0.0f, t[g]);
+    if (NG == 4) {
+        const auto two = [&](int k, int g) { return t[g % NG][k] | t[(g + 1) % NG][k] << 16; };
+        to[0] = uint4{two(0, 0), two(0, 2), two(1, 0), two(1, 2)};
+        to[1] = uint4{two(2, 0), two(2, 2), 0, 0};
+    } else {
+        uint32_t w[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) w[k] = NG == 2 ? t[0][k] | t[NG - 1][k] << 16 : t[0][k] & 0xffffu;
+        to[0] = uint4{w[0], w[1], w[2], 0};
+        to[1] = uint4{0, 0, 0, 0};
+    }
+}
+
 // KW 1: 256 rows, every wave takes both halves of a block.  KW 2: 128 rows, two waves share 32 rows and take a half of every block each.
 // WEIGH: a second sum, of the probabilities as they were before they were rounded, for the weights of the slots.
 template <int D, int GR, int KW, bool WEIGH>
@@ -222,19 +241,20 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
             q[sl] = *reinterpret_cast<const uint4 *>(qp + R::kVec * (2 * sl + h));
             most = greatest_of(q[sl], most);
         }
+        if (WEIGH && split == 0 && kw == 0) {
+            float part[D / GR] = {};
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) part[16 * sl / GR] = sum_of(q[sl], part[16 * sl / GR]);
+#pragma unroll
+            for (int g = 0; g < D / GR; ++g) part[g] += __shfl_xor(part[g], 32, 64);
+            if (h == 0 && row < sp.rows) write_sums<D / GR>(part, a.row_sums + ((size_t)pair * a.n_rows + row) * 2);
+        }
         const float unit = unit_of(fmaxf(most, __shfl_xor(most, 32)));
 #pragma unroll
         for (int sl = 0; sl < NS; ++sl) q[sl] = to_f16(q[sl], 1.0f / unit);
         row_c *= unit;
     }
     float mul = row_c;
-    if (WEIGH && split == 0 && kw == 0 && row < sp.rows) {
-        uint16_t *to = a.row_q + ((size_t)pair * a.n_rows + row) * D;
-#pragma unroll
-        for (int sl = 0; sl < NS; ++sl) *reinterpret_cast<uint4 *>(to + R::kVec * (2 * sl + h)) = q[sl];
-        if (a.splits > 1 && h == 0) a.row_ref[(size_t)pair * a.n_rows + row] = make_float4(row_c, 0.f, 0.f, __int_as_float(last + 1));
-    }
-
     const size_t base = (size_t)pair * a.capacity;
     const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
     const uint32_t *ks = a.ks + base * (D / GR), *vs = a.vs + base * (D / GR);
@@ -458,7 +478,7 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
         if (a.splits > 1) a.part_ml[part] = make_float2(ref, l);
         if (WEIGH && a.splits > 1) a.part_l2[part] = l2;
         if (WEIGH && a.splits == 1)
-            a.row_ref[part] = make_float4(row_c, finite_or_zero(ref), l2 == 0.f ? 0.f : 1.0f / l2, __int_as_float(last + 1));
+            a.row_ref[part] = make_float4(finite_or_zero(ref), l2 == 0.f ? 0.f : 1.0f / l2, __int_as_float(last + 1), 0.f);
     }
     if (a.splits == 1) {
         if (!a.out) return;
@@ -511,24 +531,24 @@ __global__ __launch_bounds__(256) void quant_many_join_kernel(QuantAttnArgs a) {
                 sum = part_weight(top, sum, now) * sum + part_weight(m, l, now) * l;
                 top = now;
             }
-            float4 *ref = a.row_ref + (size_t)pair * a.n_rows + row;
-            ref->y = finite_or_zero(top);
-            ref->z = sum == 0.f ? 0.f : 1.0f / sum;
+            a.row_ref[(size_t)pair * a.n_rows + row] = make_float4(finite_or_zero(top), sum == 0.f ? 0.f : 1.0f / sum, __int_as_float(sp.seen(a, row)), 0.f);
         }
     if (a.out) join_rows<D, bf16_t>(a, sp, pair, jl);
 }
 
-// The slots' weights: a wave has 64 slots, their keys as operands in registers, and meets all rows, 32 at a time, which the workgroup's
-// eight waves share in LDS.  S^T again: a lane has one row, its reference and sum, and adds up that row's share of 32 slots over all tiles of rows;
-// the lanes are added at the end, in a fixed order.  Two buffers: the next 128 rows are on their way under the products of the present ones.
-// 64 x 32 logits of a wave: 32 products of 32 clocks; 32 exponentials of 16 clocks and 64 other instructions of 4 beside them.
+// The slots' weights: a wave has 64 slots, their codes as operands in registers, and meets all rows, 32 at a time, which the workgroup's
+// eight waves share in LDS.  Here S = Q K^T, so that a lane has one slot of a tile and 16 rows, and adds up their shares by itself; logits as in
+// the kernels of few rows: exact products of codes by group, times the slot's step, and a product of the queries' sums with lo.  Two
+// buffers: the next 128 rows are on their way under the products of the present ones.
+// 32 x 32 logits of a wave: 17 products of 32 clocks (16 and one for lo), 16 exponentials of 16 clocks and 32 + 16 D / GR other instructions of 4.
 template <int D, int GR>
 __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArgs a) {
     using R = Row<bf16_t, D>;
-    constexpr int NS = R::kSlices, NG = D / GR, kTiles = 4;  // tiles of rows at a time
+    constexpr int NS = R::kSlices, NG = D / GR, SG = GR / 16, kTiles = 4;  // tiles of rows at a time
     __shared__ u32x4 qs[2][kTiles][R::kKTile];
-    __shared__ float4 rs[2][kTiles * 32];
-    __shared__ float units[8][64];
+    __shared__ uint4 ss[2][kTiles][2][32];
+    __shared__ float2 rs[2][kTiles * 32];
+    __shared__ int seen_by[2][kTiles * 32];
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int y = a.by_pairs.of(blockIdx.x), pair = blockIdx.x - y * a.pairs;
     const QuantSpan sp(a, pair);
@@ -540,64 +560,45 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
     const uint8_t *kc = a.kc + base * (D / 2);
     const uint32_t *ks = a.ks + base * NG;
     // keys: lane (n, h) has elements 8 (2 sl + h) .. + 7 of slots slot0 + n and + 32
-    uint4 k[2][2][NS];
-    bool scaled = false;
+    uint4 k[2][NS];
+    Words<NG> pairs[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int at = slot0 + 32 * t + n;
         const uint32_t slot = at < sp.held ? at : sp.held - 1;
-        uint32_t w[2][D / 32], pr[NG];
+        Words<D / 32> w[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint8_t *from = kc + (slot * (D / 2) + D / 8 * (h + 2 * i));
-            if (D == 128) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(from);
-                w[i][0] = x.x, w[i][1] = x.y, w[i][2 % (D / 32)] = x.z, w[i][3 % (D / 32)] = x.w;
-            } else {
-                const uint2 x = *reinterpret_cast<const uint2 *>(from);
-                w[i][0] = x.x, w[i][1] = x.y;
-            }
-        }
-        float most = 0.f;
+        for (int i = 0; i < 2; ++i) w[i] = load_words<D / 32>(kc + (slot * (D / 2) + D / 8 * (h + 2 * i)));
+        pairs[t] = load_words<NG>(ks + (size_t)slot * NG);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            pr[g] = ks[slot * NG + g];
-            most = fmaxf(most, fmaxf(fabsf(lo_of(pr[g])), fabsf(fmaf(15.0f, step_of(pr[g]), lo_of(pr[g])))));
-        }
-        const float u = unit_of(most), inv = 1.0f / u;
-        scaled = scaled || u != 1.0f;
-        if (h == 0) units[wave][32 * t + n] = u;
-#pragma unroll
-        for (int sl = 0; sl < NS; ++sl) {  // piece 2 sl + h = 4 m + nq
-            const int m = sl >> 1;
-            const uint32_t p = pr[32 * m / GR];
-            uint4 x[2];
-            key_values<2>(w[sl & 1][m], lo_of(p) * inv, step_of(p) * inv, x);
-            k[t][0][sl] = x[0];
-            k[t][1][sl] = x[1];
+        for (int sl = 0; sl < NS; ++sl) {  // piece 2 sl + h = 4 m + nq; the codes in the order of the elements
+            const uint4 x = operand_of(w[sl & 1].w[sl >> 1]);
+            k[t][sl] = uint4{__builtin_amdgcn_perm(x.y, x.x, 0x05040100u), __builtin_amdgcn_perm(x.w, x.z, 0x05040100u),
+                             __builtin_amdgcn_perm(x.y, x.x, 0x07060302u), __builtin_amdgcn_perm(x.w, x.z, 0x07060302u)};
         }
     }
-    scaled = __any(scaled);
-    f32x16 w[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[t][i] = 0.f;
+    float w[2][2] = {};
 
     constexpr int kLanes = D / 8, kPer = 512 / kLanes, kLoads = 32 * kTiles / kPer;  // threads of a row; rows of a round of loads
-    const uint16_t *row_q = a.row_q + (size_t)pair * a.n_rows * D + 8 * (threadIdx.x % kLanes);
+    const int piece = threadIdx.x % kLanes;
+    const bf16_t *q0 = (const bf16_t *)a.q + sp.b * a.q_b + (int64_t)sp.h * a.G * a.q_h + 8 * piece;
     const float4 *row_ref = a.row_ref + (size_t)pair * a.n_rows;
+    const uint4 *row_sums = a.row_sums + (size_t)pair * a.n_rows * 2;
     u32x4 next_q[kLoads];
     float4 next_ref = {0.f, 0.f, 0.f, 0.f};
+    uint4 next_sums = {0, 0, 0, 0};
     auto request = [&](int row0) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int row = min(row0 + i * kPer + (int)threadIdx.x / kLanes, sp.rows - 1);
-            next_q[i] = *reinterpret_cast<const u32x4 *>(row_q + (size_t)row * D);
+            const int row = min(row0 + i * kPer + (int)threadIdx.x / kLanes, sp.rows - 1), tok = a.by_g.of(row);
+            next_q[i] = *reinterpret_cast<const u32x4 *>(q0 + tok * a.q_t + (int64_t)(row - tok * a.G) * a.q_h);
         }
         if (threadIdx.x < 32 * kTiles) {
             next_ref = row_ref[min(row0 + (int)threadIdx.x, sp.rows - 1)];
-            if (row0 + (int)threadIdx.x >= sp.rows) next_ref.z = 0.f;
+            if (row0 + (int)threadIdx.x >= sp.rows) next_ref.y = 0.f;
+        } else if (threadIdx.x < 96 * kTiles) {
+            const int x = threadIdx.x - 32 * kTiles;
+            next_sums = row_sums[2 * min(row0 + (x >> 1), sp.rows - 1) + (x & 1)];
         }
     };
     request(0);
@@ -605,64 +606,67 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int x = i * kPer + threadIdx.x / kLanes;
-            qs[buf][x >> 5][R::k_at(x & 31, threadIdx.x % kLanes)] = next_q[i];
+            qs[buf][x >> 5][R::k_at(x & 31, piece)] = next_q[i];
         }
-        if (threadIdx.x < 32 * kTiles) rs[buf][threadIdx.x] = next_ref;
+        if (threadIdx.x < 32 * kTiles) {
+            rs[buf][threadIdx.x] = make_float2(next_ref.x, next_ref.y);
+            seen_by[buf][threadIdx.x] = __float_as_int(next_ref.z);
+        } else if (threadIdx.x < 96 * kTiles) {
+            const int x = threadIdx.x - 32 * kTiles;
+            ss[buf][x >> 6][x & 1][x >> 1 & 31] = next_sums;
+        }
         // (the buffer's readers of two rounds ago have passed the last round's barrier)
         lds_barrier();
         if (row0 + 32 * kTiles < sp.rows) request(row0 + 32 * kTiles);
         if (idle) continue;
         const int tiles = min(kTiles, (sp.rows - row0 + 31) / 32), all = sp.seen(a, row0);
-        bool odd = scaled || slot0 + 64 > all;
+        bool odd = slot0 + 64 > all;
 #pragma unroll
-        for (int t = 0; t < kTiles / 2; ++t) odd = odd || fabsf(rs[buf][64 * t + lane].y) > kHuge;
-        u32x4 q[NS];
-        auto read_q = [&](int t) {
+        for (int t = 0; t < kTiles / 2; ++t) odd = odd || fabsf(rs[buf][64 * t + lane].x) > kHuge;
+        odd = __any(odd);
+        for (int t = 0; t < tiles; ++t) {
+            u32x4 q[NS];
 #pragma unroll
             for (int sl = 0; sl < NS; ++sl) q[sl] = qs[buf][t][R::k_at(n, 2 * sl + h)];
-        };
-        auto logits = [&](f32x16 &s, const uint4(&key)[2][NS]) {
+            const uint4 sums = ss[buf][t][h][n];
+            float2 ref[16];  // of rows 8 (i >> 2) + 4 h + (i & 3)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-            for (int term = 0; term < 2; ++term)
-#pragma unroll
-                for (int sl = 0; sl < NS; ++sl) s = mma32_f16(key[term][sl], __builtin_bit_cast(uint4, q[sl]), s);
-        };
-        if (__builtin_expect(!__any(odd), 1)) {
-            auto add = [&](f32x16 &to, const f32x16 &s, const float4 &ref) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) to[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], ref.x, -ref.y)), ref.z, to[i]);
-            };
-            for (int t = 0; t < tiles; ++t) {
-                const float4 ref = rs[buf][32 * t + n];
-                read_q(t);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    f32x16 s;
-                    logits(s, k[x]);
-                    add(w[x], s, ref);
-                    if (D == 128) __builtin_amdgcn_sched_barrier(0);  // (both halves' logits at once do not fit the registers)
-                }
-            }
-            continue;
-        }
-        for (int t = 0; t < tiles; ++t) {
-            const float4 ref = rs[buf][32 * t + n];
-            const int last = __float_as_int(ref.w) - 1;
-            const bool huge = __any(fabsf(ref.y) > kHuge);
-            read_q(t);
+            for (int i = 0; i < 16; ++i) ref[i] = rs[buf][32 * t + 8 * (i >> 2) + 4 * h + (i & 3)];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
+                uint4 lo;
+                {
+                    const uint32_t a01 = NG == 1 ? pairs[x].w[0] & 0xffffu : __builtin_amdgcn_perm(pairs[x].w[1 % NG], pairs[x].w[0], 0x05040100u);
+                    const uint32_t a23 = NG == 4 ? __builtin_amdgcn_perm(pairs[x].w[3 % NG], pairs[x].w[2 % NG], 0x05040100u) : a01;
+                    lo = uint4{a01, a23, a01, a23};
+                }
                 f32x16 s;
-                logits(s, k[x]);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int at = 32 * x + 8 * (i >> 2) + 4 * h + (i & 3);
-                    float v = s[i] * units[wave][at];
-                    if (slot0 + at > last) v = -INFINITY;
-                    v = huge ? rounded_exponent(v, ref.x, ref.y) : fmaf(v, ref.x, -ref.y);
-                    w[x][i] = fmaf(__builtin_amdgcn_exp2f(v), ref.z, w[x][i]);
+                for (int i = 0; i < 16; ++i) s[i] = 0.f;
+                s = mma32(sums, lo, s, bf16_t());
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    f32x16 z;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < SG; ++j) z = mma32(__builtin_bit_cast(uint4, q[g * SG + j]), k[x][g * SG + j], z, bf16_t());
+                    const float step = step_of(pairs[x].w[g]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = fmaf(step, z[i], s[i]);
+                }
+                if (__builtin_expect(odd, 0)) {
+                    const int slot = slot0 + 32 * x + n;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int seen = seen_by[buf][32 * t + 8 * (i >> 2) + 4 * h + (i & 3)];
+                        const float v = fabsf(ref[i].x) > kHuge ? rounded_exponent(s[i], a.c, ref[i].x) : fmaf(s[i], a.c, -ref[i].x);
+                        const float p = __builtin_amdgcn_exp2f(v) * ref[i].y;
+                        w[x][i & 1] += slot < seen ? p : 0.f;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[x][i & 1] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], a.c, -ref[i].x)), ref[i].y, w[x][i & 1]);
                 }
             }
         }
@@ -671,15 +675,10 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
     float *weights = a.weights + base;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        float mine = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float v = sum16(w[x][i]);
-            v += __shfl_xor(v, 16, 64);
-            mine = n == i ? v : mine;
-        }
-        const int slot = slot0 + 32 * x + 8 * (n >> 2) + 4 * h + (n & 3);
-        if (n < 16 && slot < sp.held) weights[slot] += mine;
+        float v = w[x][0] + w[x][1];
+        v += __shfl_xor(v, 32, 64);
+        const int slot = slot0 + 32 * x + n;
+        if (h == 0 && slot < sp.held) weights[slot] += v;
     }
 }
 
