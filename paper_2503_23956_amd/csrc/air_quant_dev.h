@@ -91,27 +91,40 @@ __device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
     *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
 }
 
-__device__ __forceinline__ float min_f(float a, float b) { return fminf(a, b); }
+// least and greatest that a NaN passes
+__device__ __forceinline__ float least_of(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+__device__ __forceinline__ float most_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 // over the 4 (LANES = 4) or 8 consecutive lanes of a group
 template <int LANES>
 __device__ __forceinline__ void range_of(float &low, float &high) {
-    low = AIR_DPP_STEP(min_f, low, 0xB1);
-    high = AIR_DPP_STEP(fmaxf, high, 0xB1);
-    low = AIR_DPP_STEP(min_f, low, 0x4E);
-    high = AIR_DPP_STEP(fmaxf, high, 0x4E);
+    low = AIR_DPP_STEP(least_of, low, 0xB1);
+    high = AIR_DPP_STEP(most_of, high, 0xB1);
+    low = AIR_DPP_STEP(least_of, low, 0x4E);
+    high = AIR_DPP_STEP(most_of, high, 0x4E);
     if (LANES == 8) {
-        low = AIR_DPP_STEP(min_f, low, 0x141);
-        high = AIR_DPP_STEP(fmaxf, high, 0x141);
+        low = AIR_DPP_STEP(least_of, low, 0x141);
+        high = AIR_DPP_STEP(most_of, high, 0x141);
     }
+}
+
+// a / b rounded correctly, out of 1 / b rounded correctly: the product, mended once by what it leaves (Markstein)
+__device__ __forceinline__ float quotient(float a, float b, float inv) {
+    const float q = a * inv;
+    return fmaf(fmaf(-q, b, a), inv, q);
+}
+// 1 / b rounded correctly, for b of eight significant bits in 2^-120 .. 2^124: the hardware's reciprocal, off by at most one step, mended once (all
+// 128 mantissas are tested)
+__device__ __forceinline__ float reciprocal(float b) {
+    const float y = __builtin_amdgcn_rcpf(b);
+    return fmaf(fmaf(-b, y, 1.0f), y, y);
 }
 
 // (lo, step) of a group from its least and greatest element
 __device__ __forceinline__ uint32_t pair_of(float low, float high) {
-    // (a NaN does not pass a minimum or maximum: the caller has put an infinity in its place)
-    if (!(fmaxf(-low, high) < 0x1p126f)) return 0x7fc0u;  // NaN, step 0
+    if (!(most_of(-low, high) < 0x1p126f)) return 0x7fc0u;  // NaN, step 0
     const uint32_t u = __float_as_uint(low);
     const uint32_t lo = (u + (u >> 31 ? 0xffffu : 0u)) & 0xffff0000u;  // down: away from zero below it
-    const float width = (high - __uint_as_float(lo)) / 15.0f;
+    const float width = quotient(high - __uint_as_float(lo), 15.0f, 1.0f / 15.0f);
     const uint32_t step = (__float_as_uint(width) + 0xffffu) & 0xffff0000u;
     return (__uint_as_float(step) < 0x1p-120f ? 0u : step) | lo >> 16;
 }
@@ -126,27 +139,25 @@ __device__ __forceinline__ int dword_of(int p) {
 template <int GR, bool K>
 __device__ __forceinline__ uint32_t codes_of(const float (&x)[8], uint32_t &pair) {
     float low = x[0], high = x[0];
-    bool number = true;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        low = fminf(low, x[i]);
-        high = fmaxf(high, x[i]);
-        number = number && x[i] == x[i];
+    for (int i = 1; i < 8; ++i) {
+        low = least_of(low, x[i]);
+        high = most_of(high, x[i]);
     }
-    if (!number) high = INFINITY;
     range_of<GR / 8>(low, high);
     pair = pair_of(low, high);
-    const float lo = lo_of(pair), step = step_of(pair), inv = 1.0f / step;
-    uint32_t code = 0;
+    const float lo = lo_of(pair), step = step_of(pair), inv = step > 0.0f ? reciprocal(step) : 0.0f;
+    // a quotient of 0 .. 15 (15 (1 + 2^-22) at most, as the step is no less than a fifteenth of the width but for its rounding) plus 1.5 2^23
+    // has its nearest whole number, ties to even, in its last bits; eight of them shifted and added leave a constant too much
+    constexpr uint32_t kBase = 0x4b400000u;
+    uint32_t code = 0, excess = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        // the quotient, rounded correctly: the product with the rounded reciprocal, mended once by what it leaves (Markstein)
-        const float d = x[i] - lo, q = d * inv;
-        const float s = fmaf(fmaf(-q, step, d), inv, q);
-        const uint32_t c = step > 0.0f ? (uint32_t)fminf(rintf(s), 15.0f) : 0u;
-        code |= c << code_shift<K>(i);
+        const float s = quotient(x[i] - lo, step, inv) + 0x1.8p23f;
+        code += __float_as_uint(s) << code_shift<K>(i);
+        excess += kBase << code_shift<K>(i);
     }
-    return code;
+    return step > 0.0f ? code - excess : 0u;
 }
 template <int D, int GR, typename T, bool K>
 __device__ __forceinline__ void append_row(const T *src, uint32_t *codes, uint32_t *scales, int p) {

@@ -110,6 +110,37 @@ def test_rows_that_are_not_numbers(dtype, d, group):
         assert torch.equal(torch.nan_to_num(o.double()), torch.nan_to_num(want.float().to(o.dtype).double()))
 
 
+@pytest.mark.parametrize("exponent", [-110, -20, 0, 3, 100])
+@pytest.mark.parametrize("group", [32, 64])
+def test_every_step_at_the_borders_of_its_codes(exponent, group):
+    """All 128 mantissas of a step, elements at and next to (n + 1/2) steps: the quotient's rounding decides."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    step = torch.ldexp(1.0 + torch.arange(128, dtype=torch.float64) / 128, torch.tensor(exponent)).cuda()
+    n = torch.arange(15, device="cuda:0") + 0.5
+    border = (step[:, None] * n).float()
+    up, down = torch.nextafter(border, torch.full_like(border, math.inf)), torch.nextafter(border, torch.zeros_like(border))
+    every = torch.cat([border, up, down, (step[:, None] * torch.rand((128, 17), generator=torch.Generator(device="cuda:0").manual_seed(3),
+                                                                    device="cuda:0") * 15).float()], dim=1)  # [128][62]
+    ends = torch.stack([torch.zeros_like(step), 15 * step], dim=1).float()
+    rows = torch.zeros((128, 64 if group == 64 else 96), device="cuda:0")
+    if group == 64:
+        rows[:, :2], rows[:, 2:] = ends, every
+    else:  # three groups of 30 elements and both ends
+        for i in range(3):
+            part = every[:, 30 * i: min(62, 30 * i + 30)]
+            rows[:, 32 * i: 32 * i + 2], rows[:, 32 * i + 2: 32 * i + 2 + part.shape[1]] = ends, part
+    k = torch.zeros((1, 1, 128, 128), device="cuda:0")
+    k[0, 0, :, : rows.shape[1]] = rows
+    cache = _new(A, 1, 1, 128, 128, "f32", group)
+    A.air_quant_append(cache, k, k)
+    want, _ = values_of(k, group)
+    for lo, up_, _ in unpacked(cache):
+        assert torch.equal(lo + up_, want)
+
+
 def test_rows_outside_the_capacity_are_dropped():
     """Lengths and counts from device memory that make no sense reach no memory outside the cache."""
     import torch
