@@ -187,6 +187,7 @@ struct QuantPlan {
     int32_t tile_rows;                      // many rows: 128 or 256 a workgroup; else 0
     int32_t max_len;                        // slots that the launch is shaped for (many rows: that it covers, the capacity)
     size_t l2_at, ref_at, sums_at;          // many rows with weights: where second sums, references and sums of queries lie
+    int32_t slot_tiles;                     // of 16 slots that a wave of the second launch takes: 4 or 1
     int32_t finish;                         // workgroups per (sequence, KV head) of the second launch; 0: none
     size_t ml_bytes, kept_at, bytes;        // workspace: (maximum, sum) pairs in front, where the logits lie, all of it
 };
