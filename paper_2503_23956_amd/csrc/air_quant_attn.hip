@@ -925,7 +925,10 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     const int64_t pairs = (int64_t)c.batch * c.n_kv_heads, rows = (int64_t)q.n_tokens * (q.n_q_heads / c.n_kv_heads);
     if (pairs == 0 || rows == 0) return p;
     const int64_t len = q.max_len > 0 && q.max_len < c.capacity ? q.max_len : c.capacity;
-    p.few = rows <= kFewRows;
+    // Logits kept for the weights: 2 KB a pair and 64 slots of the capacity, since the lengths are known on the device alone.  Forming them again costs 66
+    // us against 25 (16 x 8 heads, 4228 slots), so they are kept as long as that takes at most 1 GiB.
+    const int64_t cache_runs = (c.capacity + kRun - 1) / kRun, kept = q.weights ? pairs * cache_runs * kRun * kFewRows * (int64_t)sizeof(float) : 0;
+    p.few = rows <= kFewRows && kept <= (1ll << 30);
     p.row_tiles = rows > 16 && c.dtype == AIR_BF16 ? 2 : 1;  // (two tiles of fp32 queries, three terms each, do not fit the registers)
     p.row_blocks = (int)((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
     p.max_len = (int)len;
@@ -975,9 +978,9 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
         p.ml_bytes = (cells * sizeof(float2) + 255) / 256 * 256;
         p.bytes = p.ml_bytes + (p.splits > 1 ? (cells * c.head_dim * sizeof(float) + 255) / 256 * 256 : 0);
         if (p.few && q.weights) {
-            p.max_runs = (int)((c.capacity + kRun - 1) / kRun);
+            p.max_runs = (int)cache_runs;
             p.kept_at = p.bytes;
-            p.bytes += (size_t)pairs * p.max_runs * kRun * kFewRows * sizeof(float);
+            p.bytes += (size_t)kept;
         }
         const int places = 1024 / c.head_dim;  // rows of join_rows beside each other, times the splits taken side by side
         int groups = 1;

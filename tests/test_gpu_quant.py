@@ -418,6 +418,29 @@ def test_more_than_32_bits_of_cache():
     assert float((a[0, -1].double() - b[0, -1].double()).abs().max()) < 2.0 ** -7 * float(b[0, -1].abs().max())
 
 
+@pytest.mark.parametrize("max_len", [0, 700])
+def test_few_rows_of_a_long_cache_keep_no_logits(max_len):
+    """Three heads of 2^24 slots, where the logits of 8 rows would take 1.5 GiB: weights of a token are the definition's, appended or not."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    H, cap, n, T = 3, 1 << 24, 630, 3
+    big, small = A.QuantCache(1, H, cap, 64), A.QuantCache(1, H, n + T, 64)
+    k, v = (_randn(i, 1, H, n + T, 64).bfloat16() for i in range(2))
+    A.air_quant_append(small, k, v)
+    A.air_quant_append(big, k[:, :, :n], v[:, :, :n])
+    q = _randn(3, 1, 2 * H, T, 64).bfloat16()
+    out, w = torch.empty_like(q), torch.ones(1, H, cap, device="cuda:0")
+    A.air_quant_attn(big, q, out, lens=_ints([n]), weights=w, k=k[:, :, n:], v=v[:, :, n:], max_len=max_len)
+    o, bound, ww, wb = attention(small, q, [n + T], [T], True)[0]
+    assert bool(((out[0].double() - o).abs() <= bound).all())
+    was = torch.ones(H, n + T, device="cuda:0", dtype=torch.float64)
+    was[:, n:] = 0.0
+    assert bool(((w[0, :, :n + T].double() - was - ww).abs() <= wb + (was + ww) * 2.0 ** -23).all())
+    assert bool((w[0, :, n + T:] == 1.0).all())
+
+
 # ---- streams, graphs, workspaces ------------------------------------------------------------------------------------------------------
 def test_other_streams_workspaces_and_two_calls_at_once():
     import torch

@@ -100,6 +100,16 @@ def test_workspaces():
         assert lib.air_quant_attn(None, C.byref(big), C.byref(_query()), None, ws, n) == WORKSPACE
 
 
+def test_workspaces_of_few_rows_do_not_grow_without_bound():
+    lib = _lib()
+    size = lambda q, c: lib.air_quant_workspace_bytes(C.byref(c), C.byref(q))  # noqa: E731
+    most = 0
+    for log2 in range(8, 25):
+        for batch in (1, 3, 64):
+            most = max(most, size(_query(n_tokens=1, weights=P), _cache(batch=batch, capacity=1 << log2)))
+    assert 2 ** 29 < most < 2 ** 30 + 2 ** 24
+
+
 def _evict(n_planes=1, plane=None, w=P, pos=P, lens=P, out=2 * P, ws=None, nbytes=0, **kw):
     f = dict(batch=2, n_heads=2, capacity=100, keep=40, limit=50, first=2, recent=8)
     f.update(kw)
