@@ -159,7 +159,7 @@ air_status air_evict(void *stream, const air_evict_config *cfg, float *weights, 
     if (!positions && (c.first > 0 || c.recent > 0)) return refuse(AIR_ERR_INVALID_ARG, "air_evict: first and recent need positions");
     if (c.batch == 0) return AIR_OK;
     if (!weights || !lens || !lens_out) return refuse(AIR_ERR_INVALID_ARG, "air_evict: null argument");
-    if (lens == lens_out) return refuse(AIR_ERR_INVALID_ARG, "air_evict: lens_out must not be lens");
+    if (lens < lens_out + c.batch && lens_out < lens + c.batch) return refuse(AIR_ERR_INVALID_ARG, "air_evict: lens_out must not overlap lens");
     for (int i = 0; i < c.n_planes; ++i)
         if (!c.planes[i].rows) return refuse(AIR_ERR_INVALID_ARG, "air_evict: null plane");
     const size_t bytes = evict_bytes(c);

@@ -139,6 +139,10 @@ def test_bad_evictions(status, kw):
     assert lib.air_last_error(None).startswith(b"air_evict: ")
 
 
+def test_an_evictions_lengths_lie_apart():
+    assert all(_evict(lens=P, out=P + at)[0] == INVALID for at in (-4, 0, 4))  # two sequences
+
+
 def test_eviction_workspaces():
     assert _evict(capacity=40, n_planes=0, batch=0)[1] == 0 and _evict(batch=0)[1] == 0
     big = dict(capacity=20000, keep=9000, limit=9000, plane=dict(h=20000 * 256, b=20000 * 512))
