@@ -395,7 +395,8 @@ size_t air_quant_workspace_bytes(const air_quant_cache *cache, const air_quant_q
  * of NaN in a slot that it sees makes its part of the output (V) or all of it (K) NaN.  fp32: products of codes are exact, everything
  * else is held in fp32.  bf16: the same logits and sums, and factors p step of 15 bits for the second product; calls of 65 rows (queries
  * x query heads per KV head) and more round what V stands for and the probabilities to 11 bits (8 where a group of V has no magnitude between
- * 2^-4 and 2^14, or one above), and without weights what K stands for to 11 bits.  Outputs are rounded once.
+ * 2^-4 and 2^14, or one above), and without weights what K stands for to 11 bits.  Outputs are rounded once.  The sums of an output hold p up
+ * to 2^8 times the probability of the row's greatest logit, undivided: V of 2^95 and more can overflow them.
  * Causal queries belong to the last counts slots of the sequence: after air_evict slots have no order, so a call of
  * more than one causal query appends its own rows.  workspace: 256-byte aligned, free for another call when this one's work has run.
  * out must not overlap an input; output rows that overlap are refused (AIR_ERR_SHAPE). */
@@ -423,7 +424,7 @@ typedef struct {
  * or among the `recent` positions up to the largest one there; then those of the largest weights (NaN before every number, ties to the lower
  * slot), `keep` in all.  The i-th slot below `keep` that is given up takes what the i-th staying slot from `keep` on has: its rows of
  * all planes, its weight and its position.  Slots from `keep` on are left as they are.  lens_out[b] = keep, or lens[b] where
- * nothing is given up (not lens itself, which other calls of the launch's time may read).  positions: may be NULL with first =
+ * nothing is given up (memory of its own: every head reads lens).  positions: may be NULL with first =
  * recent = 0.  weights, positions: device [batch][n_heads][capacity].  workspace: 256-byte aligned, air_evict_workspace_bytes (0: none). */
 air_status air_evict(void *stream, const air_evict_config *cfg, float *weights, int32_t *positions, const int32_t *lens, int32_t *lens_out,
                      void *workspace, size_t workspace_bytes);

@@ -185,7 +185,6 @@ struct QuantPlan {
     bool few;                               // the kernel for few rows, which appends by itself
     int32_t max_runs;                       // runs of 64 slots per (sequence, KV head) whose logits are kept; 0: none
     int32_t tile_rows;                      // many rows: 128 or 256 a workgroup; else 0
-    int32_t max_len;                        // slots that the launch is shaped for (many rows: that it covers, the capacity)
     size_t l2_at, ref_at, sums_at;          // many rows with weights: where second sums, references and sums of queries lie
     int32_t slot_tiles;                     // of 16 slots that a wave of the second launch takes: 4 or 1
     int32_t finish;                         // workgroups per (sequence, KV head) of the second launch; 0: none

@@ -174,8 +174,8 @@ template <int D, int GR, int N = 4>
 struct KeyRun {
     Words<D / 32> code[N];
     Words<D / GR> pair[N];
-    // row: of the pair's first slot; slots from `held` on are read as the last one
-    __device__ __forceinline__ void load(const uint8_t *codes, const uint32_t *pairs, int slot0, int held) {  // held: or the capacity, for slots that are masked later
+    // held: slots held, or the capacity where the others are masked later; from there on they are read as the last one
+    __device__ __forceinline__ void load(const uint8_t *codes, const uint32_t *pairs, int slot0, int held) {
         const int n = threadIdx.x & 15, c = (threadIdx.x >> 4) & 3;
 #pragma unroll
         for (int t = 0; t < N; ++t) {
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
                 for (int j = 0; j < S::NT; ++j) {
                     float o = 0.0f;
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) o = f[w] == 0.0f ? o : fmaf(f[w], ob[(w * 16 + x) * D + 16 * j + n], o);
+                    for (int w = 0; w < 4; ++w) o = fmaf(f[w], ob[(w * 16 + x) * D + 16 * j + n], o);
                     if (a.splits > 1) a.part_o[part * D + 16 * j + n] = o;
                     else put(to + 16 * j + n, o * inv);
                 }
@@ -931,7 +931,6 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     p.few = rows <= kFewRows && kept <= (1ll << 30);
     p.row_tiles = rows > 16 && c.dtype == AIR_BF16 ? 2 : 1;  // (two tiles of fp32 queries, three terms each, do not fit the registers)
     p.row_blocks = (int)((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
-    p.max_len = (int)len;
     if (rows >= kManyRows && c.dtype == AIR_BF16) {
         // The least of what a call takes by a model, in us: rounds of 256 workgroups, the slots of each (all, or where there are several rounds of a
         // causal call the mean) at the nanoseconds a slot takes by tile and head size, and the splits' join with its launch and traffic.  Measured, 28 / 4
@@ -962,7 +961,6 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
         p.ref_at = p.l2_at + (q.weights && p.splits > 1 ? whole(cells * sizeof(float)) : 0);
         p.sums_at = p.ref_at + (q.weights ? whole((size_t)pairs * rows * sizeof(float4)) : 0);
         p.bytes = p.sums_at + (q.weights ? whole((size_t)pairs * rows * 2 * sizeof(uint4)) : 0);
-        p.max_len = c.capacity;
         const int places = 1024 / c.head_dim;
         int groups = 1;
         while (groups < p.splits && groups < places) groups *= 2;
@@ -1012,7 +1010,7 @@ static hipError_t run_quant_attn(hipStream_t s, const QuantAttnArgs &a, const Qu
     if (p.row_tiles == 1) quant_attn_kernel<D, GR, T, 1><<<grid, 256, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.finish == 0) return e;
-    constexpr int kMany = sizeof(T) == 4 ? 4 : 8;
+    constexpr int kMany = 4;  // tiles of 16 rows at a time: all of a bf16 call
     if (p.slot_tiles == 1) {
         if (a.n_rows <= 16) quant_finish_kernel<D, GR, T, 1, 1><<<finish, 256, 0, s>>>(a);
         else quant_finish_kernel<D, GR, T, kMany, 1><<<finish, 256, 0, s>>>(a);

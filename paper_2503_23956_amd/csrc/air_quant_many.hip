@@ -698,7 +698,7 @@ static hipError_t run_many(hipStream_t s, const QuantAttnArgs &a, const QuantPla
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.weights) {
-        quant_many_weights_kernel<D, GR><<<dim3((unsigned)((int64_t)(p.max_len + 511) / 512 * pairs)), 512, 0, s>>>(a);
+        quant_many_weights_kernel<D, GR><<<dim3((unsigned)((int64_t)(a.capacity + 511) / 512 * pairs)), 512, 0, s>>>(a);
         e = hipGetLastError();
     }
     return e;

@@ -288,6 +288,27 @@ def test_large_values_that_weigh_nothing(dtype, d, group, rows):
 
 
 @pytest.mark.parametrize("dtype,d,group", KINDS)
+@pytest.mark.parametrize("n", [40, 3000])
+@pytest.mark.parametrize("rows", [1, 12, 100])
+def test_values_that_are_not_numbers_reach_every_row_that_sees_them(dtype, d, group, n, rows):
+    """A group of NaN at a slot whose probability is zero in fp32: zero times NaN, wherever the other slots are summed up."""
+    import paper_2503_23956_amd as A
+
+    cache = _new(A, 1, 1, n, d, dtype, group)
+    k, v = (_randn(i, 1, 1, n, d) for i in range(2))
+    k[..., 0] = 0.0
+    k[:, :, n // 3, 0] = -4000.0
+    v[:, :, n // 3, 1] = math.nan
+    A.air_quant_append(cache, k.to(_type(dtype)), v.to(_type(dtype)))
+    q = _randn(5, 1, 1, rows, d)
+    q[..., 0] = 8.0
+    q = q.to(_type(dtype))
+    out = q.clone()
+    A.air_quant_attn(cache, q, out, lens=_ints([n]), causal=False)
+    assert bool(out[..., :group].isnan().all()) and not bool(out[..., group:].isnan().any())
+
+
+@pytest.mark.parametrize("dtype,d,group", KINDS)
 def test_append_and_attend(dtype, d, group):
     import torch
 
