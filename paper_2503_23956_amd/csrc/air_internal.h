@@ -183,7 +183,7 @@ hipError_t launch_quant_rows(hipStream_t s, const air_quant_cache &c, const air_
 struct QuantPlan {
     int32_t row_tiles, row_blocks, splits;  // row tiles of 16 per wave, workgroups along the rows, along the slots
     bool few;                               // the kernel for few rows, which appends by itself
-    int32_t max_runs;                       // runs of 64 slots per (sequence, KV head) whose logits are kept; 0: none
+    int32_t max_runs;                       // runs of 32 slots per (sequence, KV head) whose logits are kept; 0: none
     int32_t tile_rows;                      // many rows: 128 or 256 a workgroup; else 0
     size_t l2_at, ref_at, sums_at;          // many rows with weights: where second sums, references and sums of queries lie
     int32_t slot_tiles;                     // of 16 slots that a wave of the second launch takes: 4 or 1

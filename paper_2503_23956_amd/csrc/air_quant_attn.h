@@ -27,13 +27,13 @@ struct QuantAttnArgs {
     int32_t Hkv, G, n_tokens, capacity, n_rows, splits, causal, appended;
     Div by_g, by_hkv, by_splits, by_stride, by_pairs;  // by_stride: 4 splits
     int32_t pairs;
-    float4 *kept;      // [pair][run][2][lane]: logits, for the weights of calls with few rows; null: formed again
+    float4 *kept;      // [pair][run of 32][lane]: logits, for the weights of calls with few rows; null: formed again
     int32_t max_runs;  // runs of a pair there
     QuantAppendArgs rows;  // what the first launch appends (few rows), else rows[0] null
 };
 
 constexpr int kRun = 64;  // slots that a wave takes at a time
-constexpr int kFewRows = 8;
+constexpr int kFewRows = 8, kFewRun = 32;  // rows of a call of few, and slots of its waves
 
 template <int N>
 struct Words {
@@ -88,17 +88,17 @@ __device__ __forceinline__ void put4(bf16_t *p, const f32x4 &v) {
 
 // Second launch of a (sequence, KV head): rows joined over the splits, and what every slot was attended to - the logits once more, now against
 // every row's maximum and sum.  The partial results of a row are requested all at once: a lane per split for (maximum, sum), and
-// for the outputs D / 4 lanes a split.
-template <int D, typename T>
+// for the outputs D / 4 lanes a split.  AHEAD: requests do not wait for the sequence's rows to be known (what lies behind them is not used).
+template <int D, typename T, bool AHEAD = false>
 __device__ __forceinline__ void join_rows(const QuantAttnArgs &a, const QuantSpan &sp, int pair, float4 *lds) {
     constexpr int kLanes = D / 4, kPlaces = 256 / kLanes;  // places: splits of a row side by side, and rows
     int groups = 1;
     while (groups < a.splits && groups < kPlaces) groups *= 2;
     const int place = threadIdx.x / kLanes, x = threadIdx.x % kLanes, group = place & (groups - 1), lane = threadIdx.x & 63;
-    const int rows = kPlaces / groups;
+    const int rows = kPlaces / groups, all = AHEAD ? a.n_rows : sp.rows;
     const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
-    for (int first = blockIdx.x * rows; first < sp.rows; first += gridDim.x * rows) {
-        const int row = first + place / groups, r = row < sp.rows ? row : sp.rows - 1;
+    for (int first = blockIdx.x * rows; first < all; first += gridDim.x * rows) {
+        const int row = first + place / groups, r = row < all ? row : all - 1;
         const float4 *o = reinterpret_cast<const float4 *>(a.part_o + ((size_t)pair * a.splits * a.n_rows + r) * D) + x;
         const size_t step = (size_t)a.n_rows * (D / 4);
         float4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -167,23 +167,27 @@ __device__ __forceinline__ void join_rows(const QuantAttnArgs &a, const QuantSpa
 }
 
 // (maximum, 1 / sum) of a row over the splits; by 16 lanes, n of them
-__device__ __forceinline__ void row_reference(const QuantAttnArgs &a, const QuantSpan &sp, int pair, int row, int n, float2 *to) {
-    const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
+struct RowReference {
     float2 v[4];
-    float top = -INFINITY, sum = 0.0f;
+    __device__ __forceinline__ void request(const QuantAttnArgs &a, int pair, int row, int rows, int n) {
+        const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        v[k] = float2{-INFINITY, 0.f};
-        if (n + 16 * k < a.splits && row < sp.rows) v[k] = ml[(size_t)(n + 16 * k) * a.n_rows + row];
-        top = fmaxf(top, v[k].x);
+        for (int k = 0; k < 4; ++k) {
+            v[k] = float2{-INFINITY, 0.f};
+            if (n + 16 * k < a.splits && row < rows) v[k] = ml[(size_t)(n + 16 * k) * a.n_rows + row];
+        }
     }
-    top = max16(top);
+    __device__ __forceinline__ void form(int n, float2 *to) const {
+        float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top) * v[k].y;
-    sum = sum16(sum);
-    if (n == 0) *to = float2{finite_or_zero(top), sum == 0.0f ? 0.0f : 1.0f / sum};
-}
-
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, v[k].x);
+        top = max16(top);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top) * v[k].y;
+        sum = sum16(sum);
+        if (n == 0) *to = float2{finite_or_zero(top), sum == 0.0f ? 0.0f : 1.0f / sum};
+    }
+};
 
 hipError_t launch_quant_many(hipStream_t s, const QuantAttnArgs &a, const QuantPlan &p, int head_dim, int group, int pairs);
 

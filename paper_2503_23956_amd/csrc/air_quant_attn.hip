@@ -471,7 +471,9 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
             ql[r][kOperands - 1][lane] = q.sums;
         }
         for (int x = threadIdx.x >> 4; x < 16 * tiles; x += 16) {  // 16 lanes a row
-            row_reference(a, sp, pair, row0 + x, n, rl + x);
+            RowReference ref;
+            ref.request(a, pair, row0 + x, sp.rows, n);
+            ref.form(n, rl + x);
         }
         __syncthreads();
         for (int u = u0; u < runs; u += stride) {
@@ -525,26 +527,36 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------
-// At most eight rows (a token of up to eight query heads per KV head, a few tokens of fewer): half of a 16 x 16 product's rows would be
-// idle.  The first product's are; its logits of slots 32 .. 63 of a run then move to the idle lanes, so that softmax, sums and steps are formed
-// once per logit: lane (n, c) has rows 4 (c & 1) + i at slots 16 t + 32 (c >> 1) + n, t = 0, 1.  The factors p step are formed there,
-// and go through LDS as bf16 terms (two, or with fp32 three): the first one in rows 0 .. 7 of the second product's operand, the second one in
-// rows 8 .. 15, joined at the end, the third one in a product of its own.  (One fp16 number would be 10 % fewer instructions, but its range
-// needs a unit, and next to a value 2^20 times as large, whatever that weighs, the others' codes would be lost.)
+// At most eight rows (a token of up to eight query heads per KV head, a few tokens of fewer), 32 slots at a time: half of a 16 x 16 product's
+// rows would be idle.  The first product's are; its logits of slots 16 .. 31 of a run then move to the idle lanes, so that softmax, sums and steps are
+// formed once per logit: lane (n, c) has rows 4 (c & 1) + i at slot 16 (c >> 1) + n.  The factors p step are formed there, of two slots and
+// two rows after an exchange between lanes n and n ^ 1, and go through LDS as bf16 terms (two, or with fp32 three): the first one in rows 0 .. 7 of
+// the second product's operand, the second one in rows 8 .. 15, joined at the end, the third one in a product of its own.  (One fp16 number would be
+// 10 % fewer instructions, but its range needs a unit, and next to a value 2^20 times as large, whatever that weighs, the others' codes
+// would be lost.)
+//
+// Small calls are bound by the chain of dependent accesses and by the instructions of one pass over code that is new to the CU: one token over 7432
+// slots, 28 / 4 heads of 128, 12.2 us with the launch that joins 59 splits (13.8 with 64 slots at a time: twice the code of a pass, 200 registers in place of
+// 162); queries, first keys and new rows are requested before the length is there.  Large ones are bound by memory: 16 tokens over 14 to 17 k slots,
+// 64 / 8 heads of 128, with weights, 111 us, 88 of them here (404 MB with the logits kept, 4.6 TB/s).
 //
 // The wave whose run has slots that the call appends writes them, and takes them from LDS into what it has read of the run.
 // ---------------------------------------------------------------------------------------
 template <int D, int GR, typename T>
 struct FewShape {
     using S = QuantShape<D, GR, T>;
-    static constexpr int kWStride = 144, kWRows = S::kF32 ? 24 : 16;  // bytes: 64 places of 16 bits and 16 more, 16 rows on different banks
-    static constexpr int kWBytes = S::NG * kWRows * kWStride, kWave = S::kVBytes + kWBytes;
+    static constexpr int kWStride = 80, kWRows = S::kF32 ? 24 : 16;  // bytes: 32 places of 16 bits and 16 more, 16 rows on different banks
+    static constexpr int kVBytes = kFewRun * S::kVStride, kWBytes = S::NG * kWRows * kWStride, kWave = kVBytes + kWBytes;
     static constexpr int kEnd = 4 * 16 * D * 4 + 4 * 16 * 8, kLds = 4 * kWave > kEnd ? 4 * kWave : kEnd;
 };
 
 // (x of lanes 0 .. 31, y of lanes 0 .. 31)
 __device__ __forceinline__ float lower_halves(float x, float y) {
     return __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false)[0]);
+}
+// x of the lane beside: n ^ 1
+__device__ __forceinline__ float swap_pairs(float x) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xf, 0xf, true));
 }
 __device__ __forceinline__ float max_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -555,7 +567,7 @@ template <int D, int GR>
 struct alignas(16) NewRow {
     uint32_t k[D / 8], v[D / 8], kp[D / GR], vp[D / GR];
 };
-// rows of slots slot0 .. slot0 + 63 into the cache and, token by token of the call, into `rows`.  first: the eight elements of K and V that the lane
+// rows of slots slot0 .. slot0 + 31 into the cache and, token by token of the call, into `rows`.  first: the eight elements of K and V that the lane
 // has requested of token lane / (D / 8)
 template <int D, int GR, typename T>
 __device__ __forceinline__ void append_run(const QuantAttnArgs &a, const QuantSpan &sp, int slot0, const float (&first)[2][8], NewRow<D, GR> *rows) {
@@ -564,7 +576,7 @@ __device__ __forceinline__ void append_run(const QuantAttnArgs &a, const QuantSp
     for (int t0 = 0; t0 < sp.count; t0 += kRows) {
         const int t = t0 + lane / kLanes;
         const int64_t slot = (int64_t)sp.held_before + t;
-        if (t >= sp.count || slot < slot0 || slot >= slot0 + kRun || slot >= sp.held) continue;
+        if (t >= sp.count || slot < slot0 || slot >= slot0 + kFewRun || slot >= sp.held) continue;
         const int64_t cell = ((int64_t)sp.b * a.Hkv + sp.h) * a.capacity + slot;
         float x[2][8];
 #pragma unroll
@@ -607,10 +619,10 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
     const uint32_t *ks = a.ks + base * NG, *vs = a.vs + base * NG;
     const int stride = 4 * a.splits;
     int u = split * 4 + wave;
-    KeyRun<D, GR> key;
+    KeyRun<D, GR, 2> key;
     QueryTile<D, GR, T> q;
     q.request(a, b, h, n, a.n_rows);
-    if (u * kRun < a.capacity) key.load(kc, ks, u * kRun, a.capacity);
+    if (u * kFewRun < a.capacity) key.load(kc, ks, u * kFewRun, a.capacity);
     const bool append = a.rows.rows[0] != nullptr;
     float first[2][8] = {};
     if (append && lane / (D / 8) < a.n_tokens) {
@@ -622,18 +634,18 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
     if (sp.rows == 0) return;
     q.form(n < sp.rows);
     const int most = sp.seen(a, sp.rows - 1), least = sp.seen(a, 0);
-    const int runs = (most + kRun - 1) / kRun;
+    const int runs = (most + kFewRun - 1) / kFewRun;
     int new_run = -1;  // the wave's run with slots that the call appends: at most two runs have any
     if (append) {
-        const int r0 = sp.held_before < 0 ? 0 : sp.held_before / kRun;
+        const int r0 = sp.held_before < 0 ? 0 : sp.held_before / kFewRun;
         for (int r = r0; r < runs && r < r0 + 2; ++r)
             if (r - a.by_stride.of(r) * stride == u) new_run = r;
-        if (new_run >= 0) append_run<D, GR, T>(a, sp, new_run * kRun, first, news[wave]);
+        if (new_run >= 0) append_run<D, GR, T>(a, sp, new_run * kFewRun, first, news[wave]);
     }
 
-    uint8_t *vb = lds + wave * F::kWave, *wb = vb + S::kVBytes;
-    const int k_of = 16 * c + (n & 8) + ((n & 1) ? 4 + ((n & 7) >> 1) : (n & 7) >> 1);  // (as in the kernel for more rows)
-    const uint8_t *v_read = vb + (16 * (k_of & 3) + (k_of >> 2)) * S::kVStride;
+    uint8_t *vb = lds + wave * F::kWave, *wb = vb + F::kVBytes;
+    // rows of V that the lane gives to the transposed reads: slot 8 c + the place of code n & 7 in an operand, of two tiles of 16 elements
+    const uint8_t *v_read = vb + (8 * c + ((n & 1) ? 4 + ((n & 7) >> 1) : (n & 7) >> 1)) * S::kVStride + (n & 8);
 
     f32x4 acc[S::NT];
     float m[4], limit[4], l[4], al[4][NG];
@@ -649,79 +661,63 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
     }
 
     for (; u < runs; u += stride) {
-        // V on its way during the first product: the codes, and the pairs of the lane's two tiles
-        constexpr int kPieces = D / 32;
-        uint4 code[kPieces];
-        Words<NG> vp[2];
+        // V on its way during the first product: the codes, and the pairs of the lane's slot
+        constexpr int kPieces = D / 32, kLoads = kPieces / 2;
+        uint4 code[kLoads];
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int at = u * kRun + i * (64 / kPieces) + lane / kPieces, slot = at < a.capacity ? at : a.capacity - 1;
+        for (int i = 0; i < kLoads; ++i) {
+            const int at = u * kFewRun + i * (64 / kPieces) + lane / kPieces, slot = at < a.capacity ? at : a.capacity - 1;
             code[i] = *reinterpret_cast<const uint4 *>(vc + ((uint32_t)slot * (D / 2) + 16 * (lane % kPieces)));
         }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int at = u * kRun + 16 * t + 32 * upper + n, slot = at < a.capacity ? at : a.capacity - 1;
-            vp[t] = load_words<NG>(reinterpret_cast<const uint8_t *>(vs) + (uint32_t)slot * (NG * 4));
-        }
+        const int own = u * kFewRun + 16 * upper + n;
+        Words<NG> vp = load_words<NG>(reinterpret_cast<const uint8_t *>(vs) + (uint32_t)(own < a.capacity ? own : a.capacity - 1) * (NG * 4));
         if (u == new_run) {  // slots of the call's own rows: what was read there is not them yet
             for (int t = 0; t < sp.count; ++t) {
-                const int slot = sp.held_before + t - u * kRun;
-                if (slot < 0 || slot >= kRun) continue;
+                const int slot = sp.held_before + t - u * kFewRun;
+                if (slot < 0 || slot >= kFewRun) continue;
                 const NewRow<D, GR> &row = news[wave][t];
                 wave_sync();
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
+                for (int x = 0; x < 2; ++x)
                     if (slot == 16 * x + n) {
                         key.code[x] = load_words<D / 32>(row.k + D / 32 * c);
                         key.pair[x] = load_words<NG>(row.kp);
                     }
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i)
+                for (int i = 0; i < kLoads; ++i)
                     if (slot == i * (64 / kPieces) + lane / kPieces) code[i] = *reinterpret_cast<const uint4 *>(row.v + 4 * (lane % kPieces));
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (slot == 16 * x + 32 * upper + n) vp[x] = load_words<NG>(row.vp);
+                if (slot == 16 * upper + n) vp = load_words<NG>(row.vp);
             }
         }
-        const bool masked = (u + 1) * kRun > least;
+        const bool masked = (u + 1) * kFewRun > least;
         const int next = u + stride < runs ? u + stride : u;
         // ---- logits
-        f32x4 s4[4];
+        f32x4 s4[2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 2; ++t) {
             uint4 k[S::KM];
 #pragma unroll
             for (int i = 0; i < S::KM; ++i) k[i] = key_operand<S::kF32>(key.code[t].w[i]);
             s4[t] = logits<D, GR, T>(q, k, key.pair[t], lo_operand<NG>(key.pair[t]));
-            __builtin_amdgcn_sched_barrier(0);  // (operands of all four tiles at once do not fit the registers)
         }
-        key.load(kc, ks, next * kRun, a.capacity);
-        f32x4 s[2];
+        key.load(kc, ks, next * kFewRun, a.capacity);
+        f32x4 s;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[t][i] = lower_halves(s4[t][i], s4[t + 2][i]);
+        for (int i = 0; i < 4; ++i) s[i] = lower_halves(s4[0][i], s4[1][i]);
         if (masked) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int slot = u * kRun + 16 * t + 32 * upper + n;
+            for (int g = 0; g < NG; ++g) vp.w[g] = own < sp.held ? vp.w[g] : 0u;  // (whatever lies there)
 #pragma unroll
-                for (int g = 0; g < NG; ++g) vp[t].w[g] = slot < sp.held ? vp[t].w[g] : 0u;  // (whatever lies there)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = 4 * rc + i, seen = row < sp.rows ? sp.seen(a, row) : sp.held;
-                    s[t][i] = slot < seen ? s[t][i] : -INFINITY;
-                }
+            for (int i = 0; i < 4; ++i) {
+                const int row = 4 * rc + i, seen = row < sp.rows ? sp.seen(a, row) : sp.held;
+                s[i] = own < seen ? s[i] : -INFINITY;
             }
         }
-        if (a.kept) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) a.kept[(((size_t)pair * a.max_runs + u) * 2 + t) * 64 + lane] = float4{s[t][0], s[t][1], s[t][2], s[t][3]};
-        }
+        if (a.kept) a.kept[((size_t)pair * a.max_runs + u) * 64 + lane] = float4{s[0], s[1], s[2], s[3]};
         // ---- V to LDS
         wave_sync();
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
+        for (int i = 0; i < kLoads; ++i) {
             uint2 *to = reinterpret_cast<uint2 *>(vb + (i * (64 / kPieces) + lane / kPieces) * S::kVStride + 16 * (lane % kPieces));
             to[0] = uint2{code[i].x, code[i].y};
             to[1] = uint2{code[i].z, code[i].w};
@@ -729,12 +725,12 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         // ---- softmax against a running reference, raised when a logit lies more than kSlack above it
         bool raise = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raise = raise || s[0][i] > limit[i] || s[1][i] > limit[i];
+        for (int i = 0; i < 4; ++i) raise = raise || s[i] > limit[i];
         if (__any(raise)) {
             bool big = false;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float high = max_halves(max16(fmaxf(s[0][i], s[1][i]))), top = high * a.c;
+                const float high = max_halves(max16(s[i])), top = high * a.c;
                 const bool up = top > m[i];
                 const float f = up ? __builtin_amdgcn_exp2f(m[i] - top) : 1.0f;
                 m[i] = up ? top : m[i];
@@ -751,67 +747,65 @@ __global__ __launch_bounds__(256, 2) void quant_few_kernel(QuantAttnArgs a) {
         bool odd = false;  // a lo of NaN in a run that some row does not see all of: it counts only where the row sees it
         if (masked) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int g = 0; g < NG; ++g) odd = odd || (vp[t].w[g] & 0x7f80u) == 0x7f80u;
+            for (int g = 0; g < NG; ++g) odd = odd || (vp.w[g] & 0x7f80u) == 0x7f80u;
             odd = __any(odd);
         }
-        float p[4][2];
+        float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float ref = finite_or_zero(m[i]);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                p[i][t] = __builtin_amdgcn_exp2f(exponent(s[t][i], a.c, ref, huge));
-                l[i] += p[i][t];
-            }
+            p[i] = __builtin_amdgcn_exp2f(exponent(s[i], a.c, finite_or_zero(m[i]), huge));
+            l[i] += p[i];
         }
         if (__builtin_expect(odd, 0)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) al[i][g] = fmaf(p[i][t], s[t][i] == -INFINITY ? 0.0f : lo_of(vp[t].w[g]), al[i][g]);
+                for (int g = 0; g < NG; ++g) al[i][g] = fmaf(p[i], s[i] == -INFINITY ? 0.0f : lo_of(vp.w[g]), al[i][g]);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) al[i][g] = fmaf(p[i][t], lo_of(vp[t].w[g]), al[i][g]);
+                for (int g = 0; g < NG; ++g) al[i][g] = fmaf(p[i], lo_of(vp.w[g]), al[i][g]);
         }
+        // lanes n and n + 1 share their slots: the even one takes rows 0 and 1 of both, the odd one 2 and 3
+        const bool second = n & 1;
+        float two[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float other = swap_pairs(second ? p[i] : p[i + 2]);
+            two[i][0] = second ? other : p[i];
+            two[i][1] = second ? p[i + 2] : other;
+        }
+        uint8_t *to = wb + (4 * rc + (second ? 2 : 0)) * F::kWStride + 32 * upper + 2 * (n & 14);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const float step[2] = {step_of(vp[0].w[g]), step_of(vp[1].w[g])};
+            const float own_step = step_of(vp.w[g]), other = swap_pairs(own_step), step[2] = {second ? other : own_step, second ? own_step : other};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint8_t *to = wb + (g * F::kWRows + 4 * rc + i) * F::kWStride + 8 * n + 4 * upper;
+            for (int i = 0; i < 2; ++i) {
                 uint32_t w[S::PT];
-                split_pair<S::PT>(p[i][0] * step[0], p[i][1] * step[1], w);
+                split_pair<S::PT>(two[i][0] * step[0], two[i][1] * step[1], w);
 #pragma unroll
-                for (int k = 0; k < S::PT; ++k) *reinterpret_cast<uint32_t *>(to + 8 * k * F::kWStride) = w[k];
+                for (int k = 0; k < S::PT; ++k) *reinterpret_cast<uint32_t *>(to + (g * F::kWRows + 8 * k + i) * F::kWStride) = w[k];
             }
         }
         wave_sync();
-        __builtin_amdgcn_sched_barrier(0);
-        // ---- second product: two halves of 32 places
+        // ---- second product
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int g = 0; g < NG; ++g) {
+            const uint8_t *from = wb + (g * F::kWRows + n) * F::kWStride + 16 * c;
+            const uint4 w = *reinterpret_cast<const uint4 *>(from);
+            uint4 w3 = {0, 0, 0, 0};
+            if (S::kF32 && n < 8) w3 = *reinterpret_cast<const uint4 *>(from + 16 * F::kWStride);
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                if (g > 0) __builtin_amdgcn_sched_barrier(0);
-                const uint4 w = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + n) * F::kWStride + 32 * c + 16 * j);
-                uint4 w3 = {0, 0, 0, 0};
-                if (S::kF32 && n < 8) w3 = *reinterpret_cast<const uint4 *>(wb + (g * F::kWRows + 16 + n) * F::kWStride + 32 * c + 16 * j);
+            for (int x = 0; x < GR / 32; ++x) {
+                const int tile = g * (GR / 16) + 2 * x;
+                typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+                const i32x2 vcode = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(v_read + 8 * tile));
 #pragma unroll
-                for (int x = 0; x < GR / 16; ++x) {
-                    const int tile = g * (GR / 16) + x;
-                    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-                    const i32x2 vcode = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(v_read + 8 * tile));
+                for (int j = 0; j < 2; ++j) {
                     const uint4 v = operand_of((uint32_t)(j ? vcode.y : vcode.x));
-                    acc[tile] = mma<bf16_t>(w, v, acc[tile]);
-                    if (S::kF32) acc[tile] = mma<bf16_t>(w3, v, acc[tile]);
+                    acc[tile + j] = mma<bf16_t>(w, v, acc[tile + j]);
+                    if (S::kF32) acc[tile + j] = mma<bf16_t>(w3, v, acc[tile + j]);
                 }
             }
         }
@@ -866,12 +860,10 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
     __shared__ float4 jl[256 + 8];
     __shared__ float2 rl[8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
-    const int pair = blockIdx.y;
+    const int pair = blockIdx.y, stride = gridDim.x * 4;
     const QuantSpan sp(a, pair);
-    if (sp.rows == 0) return;
-    // (all rows together see all slots that the last one sees)
-    const int runs = a.weights ? (sp.seen(a, sp.rows - 1) + kRun - 1) / kRun : 0, stride = gridDim.x * 4;
-    const float4 *kept = a.kept + (size_t)pair * a.max_runs * 128 + lane;
+    // Two runs of 32 slots at a time; what is needed first is requested before the sequence's length is there
+    const float4 *kept = a.kept + (size_t)pair * a.max_runs * 64 + lane;
     float *weights = a.weights + (size_t)pair * a.capacity;
     int u = blockIdx.x * 4 + wave;
     float4 s[2] = {};
@@ -880,24 +872,27 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             s[t] = kept[((size_t)run * 2 + t) * 64];
-            const int slot = run * kRun + 16 * t + 32 * (c >> 1) + n;
-            was[t] = (c & 1) == t && slot < sp.held ? weights[slot] : 0.0f;
+            const int slot = run * kRun + 32 * t + 16 * (c >> 1) + n;
+            was[t] = (c & 1) == t && slot < a.capacity ? weights[slot] : 0.0f;
         }
     };
-    if (u < runs) request(u);
-    if (a.splits > 1 && a.out) join_rows<D, T>(a, sp, pair, jl);
-    if ((int)blockIdx.x * 4 >= runs) return;
-    if (threadIdx.x < 128) {  // 16 lanes a row
-        const int row = threadIdx.x >> 4;
-        row_reference(a, sp, pair, row, n, rl + row);
+    RowReference rows;  // 16 lanes a row
+    if (a.weights) {
+        if (u < a.max_runs / 2) request(u);
+        rows.request(a, pair, threadIdx.x >> 4, threadIdx.x < 128 ? a.n_rows : 0, n);
     }
+    if (a.splits > 1 && a.out) join_rows<D, T, true>(a, sp, pair, jl);
+    // (all rows together see all slots that the last one sees)
+    const int runs = a.weights && sp.rows > 0 ? (sp.seen(a, sp.rows - 1) + kRun - 1) / kRun : 0;
+    if ((int)blockIdx.x * 4 >= runs) return;
+    if (threadIdx.x < 128) rows.form(n, rl + (threadIdx.x >> 4));
     __syncthreads();
     float2 ref[4];
     bool huge = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         ref[i] = rl[4 * (c & 1) + i];
-        huge = huge || fabsf(ref[i].x) > kHuge;
+        huge = huge || (4 * (c & 1) + i < sp.rows && fabsf(ref[i].x) > kHuge);
     }
     huge = __any(huge);
     for (; u < runs; u += stride) {
@@ -913,7 +908,7 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int slot = u * kRun + 16 * t + 32 * (c >> 1) + n;
+            const int slot = u * kRun + 32 * t + 16 * (c >> 1) + n;
             if ((c & 1) == t && slot < sp.held) weights[slot] = was[t] + w[t];
         }
         if (u + stride < runs) request(u + stride);
@@ -926,7 +921,7 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     if (pairs == 0 || rows == 0) return p;
     const int64_t len = q.max_len > 0 && q.max_len < c.capacity ? q.max_len : c.capacity;
     // Logits kept for the weights: 2 KB a pair and 64 slots of the capacity, since the lengths are known on the device alone.  Forming them again costs 66
-    // us against 25 (16 x 8 heads, 4228 slots), so they are kept as long as that takes at most 1 GiB.
+    // us against 25 (16 x 8 heads of 14 to 17 k slots), so they are kept as long as that takes at most 1 GiB.
     const int64_t cache_runs = (c.capacity + kRun - 1) / kRun, kept = q.weights ? pairs * cache_runs * kRun * kFewRows * (int64_t)sizeof(float) : 0;
     p.few = rows <= kFewRows && kept <= (1ll << 30);
     p.row_tiles = rows > 16 && c.dtype == AIR_BF16 ? 2 : 1;  // (two tiles of fp32 queries, three terms each, do not fit the registers)
@@ -968,15 +963,16 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
         p.finish = (int)(n < most_wgs ? n : most_wgs);
         return p;
     }
-    const int64_t runs = (len + 4 * kRun - 1) / (4 * kRun), wanted = 512 / (pairs * p.row_blocks);  // two workgroups a CU
-    p.splits = (int)(wanted < 1 ? 1 : wanted < runs ? wanted : runs);
+    const int64_t runs = (len + 4 * kRun - 1) / (4 * kRun);
+    const int64_t shares = p.few ? (len + 4 * kFewRun - 1) / (4 * kFewRun) : runs, wanted = 512 / (pairs * p.row_blocks);  // two workgroups a CU
+    p.splits = (int)(wanted < 1 ? 1 : wanted < shares ? wanted : shares);
     if (p.splits > 64) p.splits = 64;
     if (p.splits > 1 || q.weights) {
         const size_t cells = (size_t)pairs * p.splits * rows;
         p.ml_bytes = (cells * sizeof(float2) + 255) / 256 * 256;
         p.bytes = p.ml_bytes + (p.splits > 1 ? (cells * c.head_dim * sizeof(float) + 255) / 256 * 256 : 0);
         if (p.few && q.weights) {
-            p.max_runs = (int)cache_runs;
+            p.max_runs = 2 * (int)cache_runs;
             p.kept_at = p.bytes;
             p.bytes += (size_t)kept;
         }
