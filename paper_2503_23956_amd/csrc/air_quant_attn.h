@@ -177,7 +177,8 @@ struct RowReference {
             if (n + 16 * k < a.splits && row < rows) v[k] = ml[(size_t)(n + 16 * k) * a.n_rows + row];
         }
     }
-    __device__ __forceinline__ void form(int n, float2 *to) const {
+    // real: false makes it that of a row without slots, whatever was read
+    __device__ __forceinline__ void form(int n, bool real, float2 *to) const {
         float top = -INFINITY, sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) top = fmaxf(top, v[k].x);
@@ -185,7 +186,7 @@ struct RowReference {
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum += part_weight(v[k].x, v[k].y, top) * v[k].y;
         sum = sum16(sum);
-        if (n == 0) *to = float2{finite_or_zero(top), sum == 0.0f ? 0.0f : 1.0f / sum};
+        if (n == 0) *to = real ? float2{finite_or_zero(top), sum == 0.0f ? 0.0f : 1.0f / sum} : float2{0.f, 0.f};
     }
 };
 

@@ -212,8 +212,18 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
     __shared__ __align__(16) uint8_t lds[S::kLds];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
     const int pair = blockIdx.y, block = a.by_splits.of(blockIdx.x), split = blockIdx.x - block * a.splits;
-    const QuantSpan sp(a, pair);
+    // requested before the sequence's length is there: queries, the wave's first run of keys (whatever lies in it)
+    const size_t base = (size_t)pair * a.capacity;
+    const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
+    const uint32_t *ks = a.ks + base * NG, *vs = a.vs + base * NG;
     const int row0 = block * 16 * RT;
+    int u = split * 4 + wave;
+    const QuantSpan sp(a, pair);
+    KeyRun<D, GR> key;
+    QueryTile<D, GR, T> q[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) q[r].request(a, sp.b, sp.h, row0 + 16 * r + n, a.n_rows);
+    if (u * kRun < a.capacity) key.load(kc, ks, u * kRun, a.capacity);
     if (row0 >= sp.rows) return;
     const int row_end = row0 + 16 * RT < sp.rows ? row0 + 16 * RT : sp.rows;
     const int most = sp.seen(a, row_end - 1), least = sp.seen(a, row0);
@@ -225,12 +235,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
     const int k_of = 16 * c + (n & 8) + ((n & 1) ? 4 + ((n & 7) >> 1) : (n & 7) >> 1);
     const uint8_t *v_read = vb + (16 * (k_of & 3) + (k_of >> 2)) * S::kVStride;
 
-    QueryTile<D, GR, T> q[RT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        q[r].request(a, sp.b, sp.h, row0 + 16 * r + n, sp.rows);
-        q[r].form(true);
-    }
+    for (int r = 0; r < RT; ++r) q[r].form(row0 + 16 * r + n < sp.rows);
 
     f32x4 acc[RT][S::NT];
     float m[RT][4], l[RT][4], al[RT][4][NG];
@@ -249,13 +255,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
         }
     }
 
-    const size_t base = (size_t)pair * a.capacity;
-    const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
-    const uint32_t *ks = a.ks + base * NG, *vs = a.vs + base * NG;
     const int runs = (most + kRun - 1) / kRun, stride = 4 * a.splits;
-    int u = split * 4 + wave;
-    KeyRun<D, GR> key;
-    if (u < runs) key.load(kc, ks, u * kRun, sp.held);
     for (; u < runs; u += stride) {
         ValueRun<D, GR> val;  // (on its way during the first product)
         val.load(vc, vs, u * kRun, sp.held);
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
             for (int r = 0; r < RT; ++r) s[r][t] = logits<D, GR, T>(q[r], k, key.pair[t], lo);
             if (NG == 4) __builtin_amdgcn_sched_barrier(0);  // (operands of all four tiles at once do not fit the registers)
         }
-        key.load(kc, ks, next * kRun, sp.held);
+        key.load(kc, ks, next * kRun, a.capacity);
         // ---- V to LDS, its steps beside it (group g by lanes c = g)
         wave_sync();
 #pragma unroll
@@ -445,35 +445,46 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, c = lane >> 4;
     const int pair = blockIdx.y;
     const QuantSpan sp(a, pair);
-    if (sp.rows == 0) return;
     const size_t base = (size_t)pair * a.capacity;
     const uint8_t *kc = a.kc + base * (D / 2);
     const uint32_t *ks = a.ks + base * NG;
-    const int runs = a.weights ? (sp.held + kSlots - 1) / kSlots : 0, stride = gridDim.x * 4;
-    const int u0 = blockIdx.x * 4 + wave;
+    const int stride = gridDim.x * 4, u0 = blockIdx.x * 4 + wave;
+    // what is needed first is requested before the sequence's length is there
+    static_assert(TILES <= 4, "a wave forms one tile of queries");
     KeyRun<D, GR, ST> key;
-    if (u0 < runs) key.load(kc, ks, u0 * kSlots, sp.held);
+    QueryTile<D, GR, T> own;
+    RowReference refs[TILES];  // 16 lanes a row
+    const auto request = [&](int row0, int rows) {
+        if (wave < TILES) own.request(a, sp.b, sp.h, row0 + 16 * wave + n, rows);
+#pragma unroll
+        for (int r = 0; r < TILES; ++r) refs[r].request(a, pair, row0 + 16 * r + (threadIdx.x >> 4), rows, n);
+    };
+    if (a.weights) {
+        if (u0 * kSlots < a.capacity) key.load(kc, ks, u0 * kSlots, a.capacity);
+        if (ST == 1) request(0, a.n_rows);  // (in larger calls the registers are needed in between)
+    }
+    if (sp.rows == 0) return;
+    const int runs = a.weights ? (sp.held + kSlots - 1) / kSlots : 0;
     if (a.splits > 1 && a.out) join_rows<D, T>(a, sp, pair, jl);
     if ((int)blockIdx.x * 4 >= runs) return;
 
     float *weights = a.weights + base;
     for (int row0 = 0; row0 < sp.rows; row0 += 16 * TILES) {
         const int left = (sp.rows - row0 + 15) / 16, tiles = left < TILES ? left : TILES;
+        if (ST > 1 || row0 > 0) request(row0, sp.rows);
         __syncthreads();
-        for (int r = wave; r < tiles; r += 4) {
-            QueryTile<D, GR, T> q;
-            q.request(a, sp.b, sp.h, row0 + 16 * r + n, sp.rows);
-            q.form(true);
+        if (wave < TILES) {
+            own.form(row0 + 16 * wave + n < sp.rows);
 #pragma unroll
             for (int k = 0; k < S::QT; ++k)
 #pragma unroll
-                for (int i = 0; i < S::KM; ++i) ql[r][k * S::KM + i][lane] = q.e[k][i];
-            ql[r][kOperands - 1][lane] = q.sums;
+                for (int i = 0; i < S::KM; ++i) ql[wave][k * S::KM + i][lane] = own.e[k][i];
+            ql[wave][kOperands - 1][lane] = own.sums;
         }
-        for (int x = threadIdx.x >> 4; x < 16 * tiles; x += 16) {  // 16 lanes a row
-            RowReference ref;
-            ref.request(a, pair, row0 + x, sp.rows, n);
-            ref.form(n, rl + x);
+#pragma unroll
+        for (int r = 0; r < TILES; ++r) {
+            const int x = 16 * r + (threadIdx.x >> 4);
+            refs[r].form(n, row0 + x < sp.rows, rl + x);
         }
         __syncthreads();
         for (int u = u0; u < runs; u += stride) {
@@ -487,7 +498,7 @@ __global__ __launch_bounds__(256, 2) void quant_finish_kernel(QuantAttnArgs a) {
                 pairs[t] = key.pair[t];
             }
             // the run after this one; behind the last one the first again, for the next rows
-            key.load(kc, ks, (u + stride < runs ? u + stride : u0) * kSlots, sp.held);
+            key.load(kc, ks, (u + stride < runs ? u + stride : u0) * kSlots, a.capacity);
             float w[ST] = {};
             for (int r = 0; r < tiles; ++r) {
                 QueryTile<D, GR, T> q;
@@ -885,14 +896,14 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
     // (all rows together see all slots that the last one sees)
     const int runs = a.weights && sp.rows > 0 ? (sp.seen(a, sp.rows - 1) + kRun - 1) / kRun : 0;
     if ((int)blockIdx.x * 4 >= runs) return;
-    if (threadIdx.x < 128) rows.form(n, rl + (threadIdx.x >> 4));
+    if (threadIdx.x < 128) rows.form(n, (int)(threadIdx.x >> 4) < sp.rows, rl + (threadIdx.x >> 4));
     __syncthreads();
     float2 ref[4];
     bool huge = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         ref[i] = rl[4 * (c & 1) + i];
-        huge = huge || (4 * (c & 1) + i < sp.rows && fabsf(ref[i].x) > kHuge);
+        huge = huge || fabsf(ref[i].x) > kHuge;
     }
     huge = __any(huge);
     for (; u < runs; u += stride) {
