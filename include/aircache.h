@@ -393,7 +393,7 @@ size_t air_quant_workspace_bytes(const air_quant_cache *cache, const air_quant_q
  * and, with weights, weights[b][KV head][j] += sum of p_j over the queries and the query heads of the KV head, in a fixed order.
  * A query that sees no slot gives zero.  What lies in slots that a query does not see counts for nothing, whatever it stands for; a group
  * of NaN in a slot that it sees makes its part of the output (V) or all of it (K) NaN.  fp32: products of codes are exact, everything
- * else is held in fp32.  bf16: the same logits and sums, and factors p step of 15 bits for the second product; calls of 65 rows (queries
+ * else is held in fp32.  bf16: the same logits and sums, and factors p step of 15 bits for the second product; large calls of 33 rows (queries
  * x query heads per KV head) and more round what V stands for and the probabilities to 11 bits (8 where a group of V has no magnitude between
  * 2^-4 and 2^14, or one above), and without weights what K stands for to 11 bits.  Outputs are rounded once.  The sums of an output hold p up
  * to 2^8 times the probability of the row's greatest logit, undivided: V of 2^95 and more can overflow them.

@@ -181,7 +181,7 @@ QuantAppendArgs quant_row_args(const air_quant_cache &c, const air_quant_rows &r
 hipError_t launch_quant_rows(hipStream_t s, const air_quant_cache &c, const air_quant_rows &r, bool append);
 // The shape of a quant attention call
 struct QuantPlan {
-    int32_t row_tiles, row_blocks, splits;  // row tiles of 16 per wave, workgroups along the rows, along the slots
+    int32_t row_blocks, splits;             // workgroups along the rows, along the slots
     bool few;                               // the kernel for few rows, which appends by itself
     int32_t max_runs;                       // runs of 32 slots per (sequence, KV head) whose logits are kept; 0: none
     int32_t tile_rows;                      // many rows: 128 or 256 a workgroup; else 0

@@ -1,7 +1,7 @@
 // air_quant_attn: attention over a cache held in 4 bits, and what every slot was attended to.
 //
 // The rows of one (sequence, KV head) are its queries times the G query heads that share the KV head, token by token: row t G + i.  A wave takes
-// 64 slots at a time, for 16 or 32 rows.  S = Q K^T by 16 x 16 products of codes, one group at a time; each group's product is
+// 64 slots at a time, for 16 rows.  S = Q K^T by 16 x 16 products of codes, one group at a time; each group's product is
 // scaled by the slot's step, and one product more adds sum(q)_g lo_g (three bf16 terms of the sums).  A lane (n, c) then has the logits of slots
 // 16 t + n, t = 0..3, and rows 4 c .. 4 c + 3.  Probabilities go through LDS in fp32, slot 16 t + n at place 4 n + t, and come back as the
 // operand of the second product: lane (n, c) takes row n and 16 places from 16 c on, times the group's steps, as bf16 terms.  The codes
@@ -14,7 +14,6 @@
 
 namespace air {
 
-constexpr int kManyRows = 65;  // bf16: tiles of 128 and 256 rows from here on
 constexpr float kSlack = 8.0f;  // how far (base 2) a logit may lie above the reference of its row
 
 template <int D, int GR, typename T>
@@ -205,8 +204,8 @@ struct ValueRun {
     }
 };
 
-template <int D, int GR, typename T, int RT>
-__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantAttnArgs a) {
+template <int D, int GR, typename T>
+__global__ __launch_bounds__(256, 2) void quant_attn_kernel(QuantAttnArgs a) {
     using S = QuantShape<D, GR, T>;
     constexpr int NG = S::NG;
     __shared__ __align__(16) uint8_t lds[S::kLds];
@@ -216,16 +215,15 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
     const size_t base = (size_t)pair * a.capacity;
     const uint8_t *kc = a.kc + base * (D / 2), *vc = a.vc + base * (D / 2);
     const uint32_t *ks = a.ks + base * NG, *vs = a.vs + base * NG;
-    const int row0 = block * 16 * RT;
+    const int row0 = block * 16;
     int u = split * 4 + wave;
     const QuantSpan sp(a, pair);
     KeyRun<D, GR> key;
-    QueryTile<D, GR, T> q[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) q[r].request(a, sp.b, sp.h, row0 + 16 * r + n, a.n_rows);
+    QueryTile<D, GR, T> q;
+    q.request(a, sp.b, sp.h, row0 + n, a.n_rows);
     if (u * kRun < a.capacity) key.load(kc, ks, u * kRun, a.capacity);
     if (row0 >= sp.rows) return;
-    const int row_end = row0 + 16 * RT < sp.rows ? row0 + 16 * RT : sp.rows;
+    const int row_end = row0 + 16 < sp.rows ? row0 + 16 : sp.rows;
     const int most = sp.seen(a, row_end - 1), least = sp.seen(a, row0);
 
     uint8_t *vb = lds + wave * S::kWave;
@@ -235,24 +233,20 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
     const int k_of = 16 * c + (n & 8) + ((n & 1) ? 4 + ((n & 7) >> 1) : (n & 7) >> 1);
     const uint8_t *v_read = vb + (16 * (k_of & 3) + (k_of >> 2)) * S::kVStride;
 
-#pragma unroll
-    for (int r = 0; r < RT; ++r) q[r].form(row0 + 16 * r + n < sp.rows);
+    q.form(row0 + n < sp.rows);
 
-    f32x4 acc[RT][S::NT];
-    float m[RT][4], l[RT][4], al[RT][4][NG];
-    float limit[RT][4];  // the logit above which the reference is raised
+    f32x4 acc[S::NT];
+    float m[4], l[4], al[4][NG];
+    float limit[4];  // the logit above which the reference is raised
     bool huge = false;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
+    for (int i = 0; i < S::NT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < S::NT; ++i) acc[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < 4; ++i) {
+        m[i] = limit[i] = -INFINITY;
+        l[i] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            m[r][i] = limit[r][i] = -INFINITY;
-            l[r][i] = 0.0f;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) al[r][i][g] = 0.0f;
-        }
+        for (int g = 0; g < NG; ++g) al[i][g] = 0.0f;
     }
 
     const int runs = (most + kRun - 1) / kRun, stride = 4 * a.splits;
@@ -262,15 +256,14 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
         const bool masked = (u + 1) * kRun > least;
         const int next = u + stride < runs ? u + stride : u;
         // ---- logits
-        f32x4 s[RT][4];
+        f32x4 s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             uint4 k[S::KM];
 #pragma unroll
             for (int i = 0; i < S::KM; ++i) k[i] = key_operand<S::kF32>(key.code[t].w[i]);
             const uint4 lo = lo_operand<NG>(key.pair[t]);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) s[r][t] = logits<D, GR, T>(q[r], k, key.pair[t], lo);
+            s[t] = logits<D, GR, T>(q, k, key.pair[t], lo);
             if (NG == 4) __builtin_amdgcn_sched_barrier(0);  // (operands of all four tiles at once do not fit the registers)
         }
         key.load(kc, ks, next * kRun, a.capacity);
@@ -300,88 +293,85 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
             }
             *reinterpret_cast<f32x4 *>(sb + c * kRun + 4 * n) = st;
         }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            // ---- softmax against a running reference, raised when a logit lies more than kSlack above it
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = row0 + 16 * r + 4 * c + i, seen = row < sp.rows ? sp.seen(a, row) : sp.held;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) s[r][t][i] = u * kRun + 16 * t + n < seen ? s[r][t][i] : -INFINITY;
-                }
-            }
-            bool raise = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) raise = raise || s[r][t][i] > limit[r][i];
-            if (__any(raise)) {
-                bool big = false;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float high = max16(fmaxf(fmaxf(s[r][0][i], s[r][1][i]), fmaxf(s[r][2][i], s[r][3][i]))), top = high * a.c;
-                    const bool up = top > m[r][i];
-                    const float f = up ? __builtin_amdgcn_exp2f(m[r][i] - top) : 1.0f;
-                    m[r][i] = up ? top : m[r][i];
-                    if (up) limit[r][i] = limit_of(high, top, a.c);
-                    big = big || fabsf(finite_or_zero(m[r][i])) > kHuge;
-                    l[r][i] *= f;
-#pragma unroll
-                    for (int g = 0; g < NG; ++g) al[r][i][g] *= f;
-#pragma unroll
-                    for (int j = 0; j < S::NT; ++j) acc[r][j][i] *= f;
-                }
-                huge = huge || __any(big);
-            }
-            wave_sync();  // (the probabilities of the tile in front have been read)
+        // ---- softmax against a running reference, raised when a logit lies more than kSlack above it
+        if (masked) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float ref = finite_or_zero(m[r][i]);
-                f32x4 p;
+                const int row = row0 + 4 * c + i, seen = row < sp.rows ? sp.seen(a, row) : sp.held;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    p[t] = __builtin_amdgcn_exp2f(exponent(s[r][t][i], a.c, ref, huge));
-                    l[r][i] += p[t];
-                }
-                if (masked) {
-                    // a lo of NaN counts only where the row sees it
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int g = 0; g < NG; ++g) al[r][i][g] = fmaf(p[t], s[r][t][i] == -INFINITY ? 0.0f : lo_of(vp[t].w[g]), al[r][i][g]);
-                } else {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int g = 0; g < NG; ++g) al[r][i][g] = fmaf(p[t], lo_of(vp[t].w[g]), al[r][i][g]);
-                }
-                *reinterpret_cast<f32x4 *>(pb + (4 * c + i) * S::kPStride + 4 * n) = p;
+                for (int t = 0; t < 4; ++t) s[t][i] = u * kRun + 16 * t + n < seen ? s[t][i] : -INFINITY;
             }
-            wave_sync();
-            // ---- second product: two halves of 32 places
+        }
+        bool raise = false;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float *pr = pb + n * S::kPStride + 16 * c + 8 * j;
-                const f32x4 p0 = *reinterpret_cast<const f32x4 *>(pr), p1 = *reinterpret_cast<const f32x4 *>(pr + 4);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    const float *sr = sb + g * kRun + 16 * c + 8 * j;
-                    const f32x4 s0 = *reinterpret_cast<const f32x4 *>(sr), s1 = *reinterpret_cast<const f32x4 *>(sr + 4);
-                    uint32_t w[4][S::PT];
-                    split_pair<S::PT>(p0[0] * s0[0], p0[1] * s0[1], w[0]);
-                    split_pair<S::PT>(p0[2] * s0[2], p0[3] * s0[3], w[1]);
-                    split_pair<S::PT>(p1[0] * s1[0], p1[1] * s1[1], w[2]);
-                    split_pair<S::PT>(p1[2] * s1[2], p1[3] * s1[3], w[3]);
+            for (int t = 0; t < 4; ++t) raise = raise || s[t][i] > limit[i];
+        if (__any(raise)) {
+            bool big = false;
 #pragma unroll
-                    for (int x = 0; x < GR / 16; ++x) {
-                        const int tile = g * (GR / 16) + x;
-                        typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-                        const i32x2 code = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(v_read + 8 * tile));
-                        const uint4 v = operand_of((uint32_t)(j ? code.y : code.x));
+            for (int i = 0; i < 4; ++i) {
+                const float high = max16(fmaxf(fmaxf(s[0][i], s[1][i]), fmaxf(s[2][i], s[3][i]))), top = high * a.c;
+                const bool up = top > m[i];
+                const float f = up ? __builtin_amdgcn_exp2f(m[i] - top) : 1.0f;
+                m[i] = up ? top : m[i];
+                if (up) limit[i] = limit_of(high, top, a.c);
+                big = big || fabsf(finite_or_zero(m[i])) > kHuge;
+                l[i] *= f;
 #pragma unroll
-                        for (int k = 0; k < S::PT; ++k) acc[r][tile] = mma<bf16_t>(uint4{w[0][k], w[1][k], w[2][k], w[3][k]}, v, acc[r][tile]);
-                    }
+                for (int g = 0; g < NG; ++g) al[i][g] *= f;
+#pragma unroll
+                for (int j = 0; j < S::NT; ++j) acc[j][i] *= f;
+            }
+            huge = huge || __any(big);
+        }
+        wave_sync();  // (the probabilities of the tile in front have been read)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float ref = finite_or_zero(m[i]);
+            f32x4 p;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                p[t] = __builtin_amdgcn_exp2f(exponent(s[t][i], a.c, ref, huge));
+                l[i] += p[t];
+            }
+            if (masked) {
+                // a lo of NaN counts only where the row sees it
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) al[i][g] = fmaf(p[t], s[t][i] == -INFINITY ? 0.0f : lo_of(vp[t].w[g]), al[i][g]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) al[i][g] = fmaf(p[t], lo_of(vp[t].w[g]), al[i][g]);
+            }
+            *reinterpret_cast<f32x4 *>(pb + (4 * c + i) * S::kPStride + 4 * n) = p;
+        }
+        wave_sync();
+        // ---- second product: two halves of 32 places
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float *pr = pb + n * S::kPStride + 16 * c + 8 * j;
+            const f32x4 p0 = *reinterpret_cast<const f32x4 *>(pr), p1 = *reinterpret_cast<const f32x4 *>(pr + 4);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const float *sr = sb + g * kRun + 16 * c + 8 * j;
+                const f32x4 s0 = *reinterpret_cast<const f32x4 *>(sr), s1 = *reinterpret_cast<const f32x4 *>(sr + 4);
+                uint32_t w[4][S::PT];
+                split_pair<S::PT>(p0[0] * s0[0], p0[1] * s0[1], w[0]);
+                split_pair<S::PT>(p0[2] * s0[2], p0[3] * s0[3], w[1]);
+                split_pair<S::PT>(p1[0] * s1[0], p1[1] * s1[1], w[2]);
+                split_pair<S::PT>(p1[2] * s1[2], p1[3] * s1[3], w[3]);
+#pragma unroll
+                for (int x = 0; x < GR / 16; ++x) {
+                    const int tile = g * (GR / 16) + x;
+                    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+                    const i32x2 code = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(v_read + 8 * tile));
+                    const uint4 v = operand_of((uint32_t)(j ? code.y : code.x));
+#pragma unroll
+                    for (int k = 0; k < S::PT; ++k) acc[tile] = mma<bf16_t>(uint4{w[0][k], w[1][k], w[2][k], w[3][k]}, v, acc[tile]);
                 }
             }
         }
@@ -392,42 +382,38 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void quant_attn_kernel(QuantA
     float *ob = reinterpret_cast<float *>(lds);  // [wave][row][D]
     float2 *mlb = reinterpret_cast<float2 *>(lds + 4 * 16 * D * 4);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        if (r > 0) __syncthreads();
+    for (int i = 0; i < 4; ++i) {
+        l[i] = sum16(l[i]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            l[r][i] = sum16(l[r][i]);
+        for (int g = 0; g < NG; ++g) al[i][g] = sum16(al[i][g]);
 #pragma unroll
-            for (int g = 0; g < NG; ++g) al[r][i][g] = sum16(al[r][i][g]);
+        for (int j = 0; j < S::NT; ++j) ob[(wave * 16 + 4 * c + i) * D + 16 * j + n] = acc[j][i] + al[i][j / (GR / 16)];
+        if (n == 0) mlb[wave * 16 + 4 * c + i] = float2{m[i], l[i]};
+    }
+    __syncthreads();
+    const int x = threadIdx.x >> 4, row = row0 + x;
+    if (row < sp.rows) {
+        float top = -INFINITY, f[4], sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < S::NT; ++j) ob[(wave * 16 + 4 * c + i) * D + 16 * j + n] = acc[r][j][i] + al[r][i][j / (GR / 16)];
-            if (n == 0) mlb[wave * 16 + 4 * c + i] = float2{m[r][i], l[r][i]};
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, mlb[w * 16 + x].x);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            f[w] = part_weight(mlb[w * 16 + x].x, mlb[w * 16 + x].y, top);
+            sum += f[w] * mlb[w * 16 + x].y;
         }
-        __syncthreads();
-        const int x = threadIdx.x >> 4, row = row0 + 16 * r + x;
-        if (row < sp.rows) {
-            float top = -INFINITY, f[4], sum = 0.0f;
+        const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
+        if (a.part_ml && n == 0) a.part_ml[part] = float2{top, sum};
+        if (a.splits > 1 || a.out) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const int t = a.by_g.of(row);
+            T *to = static_cast<T *>(a.out) + sp.b * a.out_b + ((int64_t)sp.h * a.G + row - t * a.G) * a.out_h + t * a.out_t;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmaxf(top, mlb[w * 16 + x].x);
+            for (int j = 0; j < S::NT; ++j) {
+                float o = 0.0f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                f[w] = part_weight(mlb[w * 16 + x].x, mlb[w * 16 + x].y, top);
-                sum += f[w] * mlb[w * 16 + x].y;
-            }
-            const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
-            if (a.part_ml && n == 0) a.part_ml[part] = float2{top, sum};
-            if (a.splits > 1 || a.out) {
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                const int t = a.by_g.of(row);
-                T *to = static_cast<T *>(a.out) + sp.b * a.out_b + ((int64_t)sp.h * a.G + row - t * a.G) * a.out_h + t * a.out_t;
-#pragma unroll
-                for (int j = 0; j < S::NT; ++j) {
-                    float o = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) o = fmaf(f[w], ob[(w * 16 + x) * D + 16 * j + n], o);
-                    if (a.splits > 1) a.part_o[part * D + 16 * j + n] = o;
-                    else put(to + 16 * j + n, o * inv);
-                }
+                for (int w = 0; w < 4; ++w) o = fmaf(f[w], ob[(w * 16 + x) * D + 16 * j + n], o);
+                if (a.splits > 1) a.part_o[part * D + 16 * j + n] = o;
+                else put(to + 16 * j + n, o * inv);
             }
         }
     }
@@ -926,6 +912,16 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
     }
 }
 
+// Tiles of 128 and 256 rows pay in bf16 calls of enough logits.  Measured, us, these kernels / those, heads of 128, 4 KV heads: one sequence, 112 rows
+// over 1000 slots 13.5 / 18.0, over 7432 22.8 / 22.8, 448 rows over 2500 27.1 / 26.2, over 7432 46.6 / 34.5; eight sequences, 48 rows over 4000 slots
+// 37.6 / 28.3, 32 rows 24.7 / 26.6 (sixteen, 16 k slots: 88 / 118), 448 rows over 200 23.1 / 15.3, 72 over 1500 26.9 / 23.2, with weights 43.5 / 36.6;
+// heads of 64: 224 rows over 700 13.3 / 17.9, 448 22.0 / 18.7.  With weights and few slots in all, where a wave of the weights' launch has 64 of
+// them, twice as many: 112 rows over one sequence of 7432 33.5 / 46.8, 448 89 / 71.
+static bool many_rows(const air_quant_cache &c, const air_quant_query &q, int64_t pairs, int64_t rows, int64_t len) {
+    if (c.dtype != AIR_BF16 || rows <= 32) return false;
+    const double least = (c.head_dim == 128 ? 2.6e6 : 6e6) * (q.weights && pairs * len < 32768 ? 2.0 : 1.0);
+    return (double)(pairs * rows) * (double)len >= least;
+}
 QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     QuantPlan p{};
     const int64_t pairs = (int64_t)c.batch * c.n_kv_heads, rows = (int64_t)q.n_tokens * (q.n_q_heads / c.n_kv_heads);
@@ -935,9 +931,8 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     // us against 25 (16 x 8 heads of 14 to 17 k slots), so they are kept as long as that takes at most 1 GiB.
     const int64_t cache_runs = (c.capacity + kRun - 1) / kRun, kept = q.weights ? pairs * cache_runs * kRun * kFewRows * (int64_t)sizeof(float) : 0;
     p.few = rows <= kFewRows && kept <= (1ll << 30);
-    p.row_tiles = rows > 16 && c.dtype == AIR_BF16 ? 2 : 1;  // (two tiles of fp32 queries, three terms each, do not fit the registers)
-    p.row_blocks = (int)((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
-    if (rows >= kManyRows && c.dtype == AIR_BF16) {
+    p.row_blocks = (int)((rows + 15) / 16);
+    if (many_rows(c, q, pairs, rows, len)) {
         // The least of what a call takes by a model, in us: rounds of 256 workgroups, the slots of each (all, or where there are several rounds of a
         // causal call the mean) at the nanoseconds a slot takes by tile and head size, and the splits' join with its launch and traffic.  Measured, 28 / 4
         // heads of 128, tiles of 128 rows / 256 rows with their best splits: 96 rows over 7432 slots 21 / 22, 448 33 / 34, 1792 68 / 62, 3500 124 / 97;
@@ -1011,13 +1006,10 @@ static hipError_t run_quant_attn(hipStream_t s, const QuantAttnArgs &a, const Qu
         quant_few_finish_kernel<D, T><<<finish, 256, 0, s>>>(a);
         return hipGetLastError();
     }
-    if constexpr (sizeof(T) == 2) {
-        if (p.row_tiles == 2) quant_attn_kernel<D, GR, T, 2><<<grid, 256, 0, s>>>(a);
-    }
-    if (p.row_tiles == 1) quant_attn_kernel<D, GR, T, 1><<<grid, 256, 0, s>>>(a);
+    quant_attn_kernel<D, GR, T><<<grid, 256, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.finish == 0) return e;
-    constexpr int kMany = 4;  // tiles of 16 rows at a time: all of a bf16 call
+    constexpr int kMany = 4;  // tiles of 16 rows at a time
     if (p.slot_tiles == 1) {
         if (a.n_rows <= 16) quant_finish_kernel<D, GR, T, 1, 1><<<finish, 256, 0, s>>>(a);
         else quant_finish_kernel<D, GR, T, kMany, 1><<<finish, 256, 0, s>>>(a);

@@ -51,7 +51,7 @@ def attention(cache, q, held, counts, causal, scale=None, weigh=True, wide=False
     codes have 16 added, and taken off again: 16 step q twice more); the exponent and the power of two (2^-22); sums of `held` terms; the factor
     p step keeps 15 bits (bf16: a first term cut off, 2^-7, the rest rounded, 2^-8) or 24; outputs are rounded once.
 
-    bf16 calls of 65 rows and more: V and the probabilities, and with these their sum, are rounded to fp16 (half a step 2^-11; probabilities below
+    bf16 calls of 33 rows and more, where they are large (the bound holds for both ways): V and the probabilities, and with these their sum, are rounded to fp16 (half a step 2^-11; probabilities below
     2^-14 of a reference that is at most 2^8 above the largest by 2^-25) or, where values have no ordinary magnitude (`wide`), to bf16 (2^-8);
     without weights, K in fp16 (2^-11, and 2^-25 of rows of at least 2^-6), with them in two such terms."""
     import torch
@@ -78,7 +78,7 @@ def attention(cache, q, held, counts, causal, scale=None, weigh=True, wide=False
         p = p.masked_fill(~seen, 0.0)
         p = p / p.sum(-1, keepdim=True).clamp(min=1e-300)
         off = size.amax(-1, keepdim=True) * ((2 * d + 16) * 2.0 ** -24) + size.amax(-1, keepdim=True) * 2.0 ** -22 if n else p.sum(-1, keepdim=True)
-        if n and q.dtype == torch.bfloat16 and q.shape[2] * g >= 65:
+        if n and q.dtype == torch.bfloat16 and q.shape[2] * g >= 33:
             dot = (qs.abs() @ t((kl + ks).abs()) * scale).masked_fill(~seen, 0.0)
             least = qs.abs().sum(-1, keepdim=True) * (kl + ks).abs().amax((1, 2), keepdim=True) * scale * 2.0 ** -19
             off = off + (dot.amax(-1, keepdim=True) * 2.0 ** -11 + least) * (2.0 ** -11 if weigh else 1.0)
@@ -86,7 +86,7 @@ def attention(cache, q, held, counts, causal, scale=None, weigh=True, wide=False
         vl_seen = torch.where(torch.isfinite(vl), vl, 0.0) if not bool(seen.all()) else vl
         o, a = p @ (vl_seen + vs), p @ (vl_seen.abs() + vs)
         low = half > 2.0 ** -20  # bf16
-        many = low and q.shape[2] * g >= 65
+        many = low and q.shape[2] * g >= 33
         err = a * (rel + (3 * 2.0 ** (-8 if wide else -11) if many else 2.0 ** -15 if low else 2.0 ** -22))
         if many and n and not wide:
             err = err + (vl_seen.abs() + vs).amax(1, keepdim=True) * (2 * n * 2.0 ** -25) + n * 2.0 ** -25

@@ -167,6 +167,9 @@ def test_rows_outside_the_capacity_are_dropped():
     assert bool((out[0][2:] == 42.0).all())
 
 
+ROOM = [0, 70000]  # more slots of capacity than are held: large calls, whose kernels and splits are others
+
+
 # ---- attention -------------------------------------------------------------------------------------------------------------------
 def _check(A, cache, q, held, counts, causal, seed=0, weigh=True, scale=0.0, lens=None, k=None, v=None, with_out=True, wide=False, **kw):
     """One call against the definition; `held`: slots after it."""
@@ -236,10 +239,13 @@ def test_windows_and_pieces(dtype, d, group, causal):
     (4, 4, [129], [257]), (24, 2, [300, 300], [640, 511]),
     (64, 8, [96] * 8, [130, 97, 1, 200, 63, 64, 65, 128]),  # tiles of 256, more queries than slots
 ])
-def test_many_rows(d, group, causal, hq, hkv, counts, held):
+@pytest.mark.parametrize("room", ROOM)
+def test_many_rows(d, group, causal, hq, hkv, counts, held, room):
     import paper_2503_23956_amd as A
 
-    cache = _filled(A, len(held), hkv, max(held) + 3, d, "bf16", group, held, 15)
+    if room and len(held) * hkv > 8:
+        pytest.skip("large as it is")
+    cache = _filled(A, len(held), hkv, max(held) + 3 + room, d, "bf16", group, held, 15)
     q = (_randn(18, len(held), max(counts), hq, d) * 2.0).bfloat16().transpose(1, 2)
     _check(A, cache, q, held, counts, causal, seed=6)
     _check(A, cache, q, held, counts, causal, weigh=False)
@@ -248,13 +254,14 @@ def test_many_rows(d, group, causal, hq, hkv, counts, held):
 
 @pytest.mark.parametrize("rows", [1, 16, 32, 100])
 @pytest.mark.parametrize("k_size,q_size,v_size", [(1e6, 1e-6, 1e8), (1e-8, 1e7, 1e-9), (3e4, 1e-3, 2e5), (1e-12, 1e12, 1e30)])
-def test_magnitudes(rows, k_size, q_size, v_size):
+@pytest.mark.parametrize("room", ROOM)
+def test_magnitudes(rows, k_size, q_size, v_size, room):
     """Any magnitude of queries, keys and values, next to each other in one batch row's heads and groups."""
     import torch
 
     import paper_2503_23956_amd as A
 
-    cache = _new(A, 1, 2, 300, 128, "bf16", 32)
+    cache = _new(A, 1, 2, 300 + room, 128, "bf16", 32)
     k, v = (_randn(i, 1, 2, 300, 128) for i in range(2))
     k[:, 0] *= k_size
     k[:, 0, :100] *= 1e-3
@@ -269,11 +276,12 @@ def test_magnitudes(rows, k_size, q_size, v_size):
 
 @pytest.mark.parametrize("dtype,d,group", KINDS)
 @pytest.mark.parametrize("rows", [1, 12, 100])
-def test_large_values_that_weigh_nothing(dtype, d, group, rows):
+@pytest.mark.parametrize("room", ROOM)
+def test_large_values_that_weigh_nothing(dtype, d, group, rows, room):
     """A value 2^100 times as large as the others, at a key that no row looks at, takes nothing from them."""
     import paper_2503_23956_amd as A
 
-    cache = _new(A, 1, 1, 200, d, dtype, group)
+    cache = _new(A, 1, 1, 200 + room, d, dtype, group)
     k, v = (_randn(i, 1, 1, 200, d) for i in range(2))
     v[:, :, 50] *= 2.0 ** 100
     v[:, :, 51] *= 2.0 ** 12
@@ -290,11 +298,12 @@ def test_large_values_that_weigh_nothing(dtype, d, group, rows):
 @pytest.mark.parametrize("dtype,d,group", KINDS)
 @pytest.mark.parametrize("n", [40, 3000])
 @pytest.mark.parametrize("rows", [1, 12, 100])
-def test_values_that_are_not_numbers_reach_every_row_that_sees_them(dtype, d, group, n, rows):
+@pytest.mark.parametrize("room", ROOM)
+def test_values_that_are_not_numbers_reach_every_row_that_sees_them(dtype, d, group, n, rows, room):
     """A group of NaN at a slot whose probability is zero in fp32: zero times NaN, wherever the other slots are summed up."""
     import paper_2503_23956_amd as A
 
-    cache = _new(A, 1, 1, n, d, dtype, group)
+    cache = _new(A, 1, 1, n + room, d, dtype, group)
     k, v = (_randn(i, 1, 1, n, d) for i in range(2))
     k[..., 0] = 0.0
     k[:, :, n // 3, 0] = -4000.0
@@ -331,19 +340,20 @@ def test_append_and_attend(dtype, d, group):
 
 @pytest.mark.parametrize("dtype,d,group", KINDS)
 @pytest.mark.parametrize("c", [3, 20, 60])
-def test_slots_that_are_not_seen_count_for_nothing(dtype, d, group, c):
+@pytest.mark.parametrize("room", ROOM)
+def test_slots_that_are_not_seen_count_for_nothing(dtype, d, group, c, room):
     """Groups of NaN behind the causal border, and behind the slots held, reach no row; those that a row sees do, however little they weigh."""
     import torch
 
     import paper_2503_23956_amd as A
 
     held = 140
-    cache = _filled(A, 2, 2, 150, d, dtype, group, [held, held], 6)
+    cache = _filled(A, 2, 2, 150 + room, d, dtype, group, [held, held], 6)
     cache.planes[2][0, :, held - 1] = math.nan  # the last key of sequence 0, which the last query alone sees
     cache.planes[3][1, :, held - 3, 0] = math.nan  # lo of the first group of a value of sequence 1
     q = (_randn(12, 2, 4, c, d) * 2.0).to(_type(dtype))
     out = torch.zeros_like(q)
-    w = torch.zeros((2, 2, 150), device="cuda:0")
+    w = torch.zeros((2, 2, 150 + room), device="cuda:0")
     A.air_quant_attn(cache, q, out, lens=_ints([held, held]), counts=_ints([c, c]), weights=w)
     nan = torch.isnan(out)
     assert bool(nan[0, :, c - 1].all()) and not bool(nan[0, :, : c - 1].any())
@@ -494,6 +504,38 @@ def test_other_streams_workspaces_and_two_calls_at_once():
         torch.cuda.synchronize()
         for o, w in zip(outs, want):
             assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("d,weigh", [(64, True), (128, False)])
+def test_recorded_pieces_of_a_large_call(d, weigh):
+    """40 and 17 tokens appended and attended at a time, recorded, over lengths that grow; every replay against the eager call."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    B, hq, hkv, cap, T, counts = 2, 12, 2, 20000, 40, [40, 17]
+    a, b = (_filled(A, B, hkv, cap, d, "bf16", 32, [3000, 3], 12) for _ in range(2))
+    q, k, v = (torch.zeros((B, h, T, d), dtype=torch.bfloat16, device="cuda:0") for h in (hq, hkv, hkv))
+    lens = {c: _ints([3000, 3]) for c in (a, b)}
+    out = {c: torch.full((B, hq, T, d), 42.0, dtype=torch.bfloat16, device="cuda:0") for c in (a, b)}
+    w = {c: torch.zeros((B, hkv, cap), device="cuda:0") for c in (a, b)}
+    n = _ints(counts)
+    calls = {c: A.prepare_quant_attn(c, q, out[c], lens=lens[c], counts=n, k=k, v=v, weights=w[c] if weigh else None) for c in (a, b)}
+    graph = torch.cuda.CUDAGraph()
+    space = torch.empty(calls[a].workspace_bytes, dtype=torch.uint8, device="cuda:0")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        calls[a](workspace=space)
+        lens[a].add_(n)
+    for step in range(6):
+        for i, x in enumerate((q, k, v)):
+            x.copy_(_randn(100 * step + i, *x.shape).bfloat16())
+        graph.replay()
+        calls[b]()
+        lens[b].add_(n)
+        torch.cuda.synchronize()
+        assert torch.equal(out[a], out[b]) and torch.equal(w[a], w[b])
+    assert bool((out[a][1, :, 17:] == 42.0).all()) and not bool((out[a][1, :, :17] == 42.0).any())
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
