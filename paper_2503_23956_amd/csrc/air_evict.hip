@@ -8,8 +8,9 @@
 //
 // A wave has a run of the slots, a lane four of them at a time; keys stay in LDS (capacities up to 24576; beyond, they are formed
 // again, out of the L2 cache, wherever they are used).  What a call takes is dependent accesses, barriers and the instructions of
-// one pass over code that is new to the CU: loops are not unrolled (keys in registers, 16 to 32 slots unrolled: 18 us in place of 15, one sequence of
-// 7432 slots cut to 743).  16 x 4 heads of 2368 slots of which 64 go, K and V rows of 256 bytes with them: 10 us.
+// one pass over code that is new to the CU: loops are not unrolled (keys in registers, 16 to 32 slots unrolled: 18 us in place of 15 at the time, one sequence of
+// 7432 slots cut to 743, now 13).  16 x 4 heads of 2368 slots of which 64 go, K and V rows of 256 bytes with them: 10 us.  2 x 8 heads of 16 k slots cut
+// to 8192: 21 us, and 9 for the rows.
 #include "air_device.h"
 #include "air_internal.h"
 

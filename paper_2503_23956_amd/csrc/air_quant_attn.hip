@@ -10,6 +10,11 @@
 //
 // Waves share nothing until their ends: each deals itself every (4 splits)-th run of 64 slots, K requested one run ahead, and the four
 // partial results of a workgroup are joined in LDS.
+//
+// Bound by the vector unit once a call fills the chip (codes into operands and factors into terms, for 16 rows at a time: 64 pairs of 12 rows over 16 k
+// slots, heads of 128, bf16 52 us, 4.2 TB/s), below that by one pass over code that is new to the CU and by dependent accesses (two windows of 64 fp32 rows
+// over 656 and 131 slots, heads of 64, with weights, 14.5 us in two launches).  32 rows a wave took 512 registers, one wave a SIMD: 8 x 4 pairs of 32
+// rows over 4000 slots 34.2 against 24.7 us.
 #include "air_quant_attn.h"
 
 namespace air {
