@@ -20,12 +20,14 @@ struct QuantAttnArgs {
     float *part_l2;    // [pair][split][row]: sums of the unrounded probabilities
     float4 *row_ref;   // [pair][row]: reference, 1 / sum, slots seen (whole number), nothing
     uint4 *row_sums;   // [pair][row][2]: sums of the queries' groups as bf16 terms, as the product with lo takes them
+    float *part_w;     // [share of the rows][pair][slot]: weights, where there are several shares
+    int32_t w_splits;
     float *weights;
     int64_t q_b, q_h, q_t, out_b, out_h, out_t;
     const int32_t *lens, *counts;
     float c;  // scale * log2(e)
     int32_t Hkv, G, n_tokens, capacity, n_rows, splits, causal, appended;
-    Div by_g, by_hkv, by_splits, by_stride, by_pairs;  // by_stride: 4 splits
+    Div by_g, by_hkv, by_splits, by_stride, by_pairs, by_shares;  // by_stride: 4 splits; by_shares: w_splits
     int32_t pairs;
     float4 *kept;      // [pair][run of 32][lane]: logits, for the weights of calls with few rows; null: formed again
     int32_t max_runs;  // runs of a pair there

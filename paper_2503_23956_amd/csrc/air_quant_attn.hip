@@ -920,12 +920,12 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
 // Tiles of 128 and 256 rows pay in bf16 calls of enough logits.  Measured, us, these kernels / those, heads of 128, 4 KV heads: one sequence, 112 rows
 // over 1000 slots 13.5 / 18.0, over 7432 22.8 / 22.8, 448 rows over 2500 27.1 / 26.2, over 7432 46.6 / 34.5; eight sequences, 48 rows over 4000 slots
 // 37.6 / 28.3, 32 rows 24.7 / 26.6 (sixteen, 16 k slots: 88 / 118), 448 rows over 200 23.1 / 15.3, 72 over 1500 26.9 / 23.2, with weights 43.5 / 36.6;
-// heads of 64: 224 rows over 700 13.3 / 17.9, 448 22.0 / 18.7.  With weights and few slots in all, where a wave of the weights' launch has 64 of
-// them, twice as many: 112 rows over one sequence of 7432 33.5 / 46.8, 448 89 / 71.
+// heads of 64: 224 rows over 700 13.3 / 17.9, 448 22.0 / 18.7.  With weights, whose launch there has few slots or few rows to deal, in calls of few slots: one sequence
+// of 7432, 112 rows 33.7 / 47.7, 224 54.4 / 52.3, 448 89 / 57; of 1000, 224 rows 31.7 / 36.7, 448 50 / 40.
 static bool many_rows(const air_quant_cache &c, const air_quant_query &q, int64_t pairs, int64_t rows, int64_t len) {
     if (c.dtype != AIR_BF16 || rows <= 32) return false;
-    const double least = (c.head_dim == 128 ? 2.6e6 : 6e6) * (q.weights && pairs * len < 32768 ? 2.0 : 1.0);
-    return (double)(pairs * rows) * (double)len >= least;
+    if (q.weights && (rows > 224 || pairs * len < 32768)) return rows > 224;
+    return (double)(pairs * rows) * (double)len >= (c.head_dim == 128 ? 2.6e6 : 6e6);
 }
 QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     QuantPlan p{};
@@ -966,7 +966,13 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
         p.l2_at = p.ml_bytes + (p.splits > 1 ? whole(cells * c.head_dim * sizeof(float)) : 0);
         p.ref_at = p.l2_at + (q.weights && p.splits > 1 ? whole(cells * sizeof(float)) : 0);
         p.sums_at = p.ref_at + (q.weights ? whole((size_t)pairs * rows * sizeof(float4)) : 0);
-        p.bytes = p.sums_at + (q.weights ? whole((size_t)pairs * rows * 2 * sizeof(uint4)) : 0);
+        p.w_at = p.sums_at + (q.weights ? whole((size_t)pairs * rows * 2 * sizeof(uint4)) : 0);
+        // The weights' workgroups have 512 slots each: where they would leave CUs without work, the rows are dealt to several, by whole turns of 128
+        // (7000 tokens of 28 / 4 heads over themselves 3720 us without, 877 so)
+        const int64_t wgs = pairs * ((len + 511) / 512), turns = (rows + 127) / 128;
+        const int64_t room = (64 << 20) / (pairs * c.capacity), dealt = 2 * kCUs / wgs, shares = dealt < room ? dealt : room;  // (at most 256 MiB)
+        p.w_splits = (int)(shares < 1 || turns < 2 ? 1 : shares < turns ? shares : turns);
+        p.bytes = p.w_at + (q.weights && p.w_splits > 1 ? whole((size_t)pairs * c.capacity * p.w_splits * sizeof(float)) : 0);
         const int places = 1024 / c.head_dim;
         int groups = 1;
         while (groups < p.splits && groups < places) groups *= 2;
@@ -1074,6 +1080,9 @@ hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const Quan
     a.part_l2 = reinterpret_cast<float *>(space + p.l2_at);
     a.row_ref = reinterpret_cast<float4 *>(space + p.ref_at);
     a.row_sums = reinterpret_cast<uint4 *>(space + p.sums_at);
+    a.part_w = reinterpret_cast<float *>(space + p.w_at);
+    a.w_splits = p.w_splits > 0 ? p.w_splits : 1;
+    a.by_shares = div_by(a.w_splits);
     if (p.tile_rows) return launch_quant_many(s, a, p, c.head_dim, c.group, pairs);
 #define AIR_CASE(D, GR, T, F) \
     if (c.head_dim == D && c.group == GR && c.dtype == F) return run_quant_attn<D, GR, T>(s, a, p, pairs);

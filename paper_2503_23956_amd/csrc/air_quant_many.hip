@@ -539,7 +539,7 @@ __global__ __launch_bounds__(256) void quant_many_join_kernel(QuantAttnArgs a) {
 }
 
 // The slots' weights: a wave has 64 slots, their codes as operands in registers, and meets all rows, 32 at a time, which the workgroup's
-// eight waves share in LDS.  Here S = Q K^T, so that a lane has one slot of a tile and 16 rows, and adds up their shares by itself; logits as in
+// eight waves share in LDS (a share of the rows where there are few slots in all).  Here S = Q K^T, so that a lane has one slot of a tile and 16 rows, and adds up their shares by itself; logits as in
 // the kernels of few rows: exact products of codes by group, times the slot's step, and a product of the queries' sums with lo.  Two
 // buffers: the next 128 rows are on their way under the products of the present ones.
 // 32 x 32 logits of a wave: 17 products of 32 clocks (16 and one for lo), 16 exponentials of 16 clocks and 32 + 16 D / GR other instructions of 4.
@@ -552,10 +552,15 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
     __shared__ float2 rs[2][kTiles * 32];
     __shared__ int seen_by[2][kTiles * 32];
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int y = a.by_pairs.of(blockIdx.x), pair = blockIdx.x - y * a.pairs;
+    const int yy = a.by_pairs.of(blockIdx.x), pair = blockIdx.x - yy * a.pairs, y = a.by_shares.of(yy), share = yy - y * a.w_splits;
     const QuantSpan sp(a, pair);
     const int slot0 = (y * 8 + wave) * 64;
     if (y * 512 >= sp.held || sp.rows == 0) return;
+    // rows, by whole turns: from the first that sees a slot of the workgroup on, a share of them
+    const int unseen = a.causal ? max(y * 512 - (sp.held - sp.count), 0) : 0;  // tokens that see no slot from y 512 on
+    const int all_from = min(unseen, sp.count - 1) * a.G / (32 * kTiles), turns = (sp.rows + 32 * kTiles - 1) / (32 * kTiles) - all_from;
+    const int per = (turns + a.w_splits - 1) / a.w_splits;
+    const int begin = (all_from + share * per) * (32 * kTiles), end = min(begin + per * (32 * kTiles), sp.rows);
     const bool idle = slot0 >= sp.held;
 
     const size_t base = (size_t)pair * a.capacity;
@@ -603,8 +608,8 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
             next_sums = row_sums[2 * min(row0 + (x >> 1), sp.rows - 1) + (x & 1)];
         }
     };
-    request(0);
-    for (int row0 = 0, buf = 0; row0 < sp.rows; row0 += 32 * kTiles, buf ^= 1) {
+    if (begin < end) request(begin);
+    for (int row0 = begin, buf = 0; row0 < end; row0 += 32 * kTiles, buf ^= 1) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int x = i * kPer + threadIdx.x / kLanes;
@@ -619,7 +624,7 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
         }
         // (the buffer's readers of two rounds ago have passed the last round's barrier)
         lds_barrier();
-        if (row0 + 32 * kTiles < sp.rows) request(row0 + 32 * kTiles);
+        if (row0 + 32 * kTiles < end) request(row0 + 32 * kTiles);
         if (idle) continue;
         const int tiles = min(kTiles, (sp.rows - row0 + 31) / 32), all = sp.seen(a, row0);
         bool odd = slot0 + 64 > all;
@@ -674,14 +679,28 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
         }
     }
     if (idle) return;
-    float *weights = a.weights + base;
+    float *weights = a.weights + base, *part = a.part_w + (size_t)share * a.pairs * a.capacity + base;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         float v = w[x][0] + w[x][1];
         v += __shfl_xor(v, 32, 64);
         const int slot = slot0 + 32 * x + n;
-        if (h == 0 && slot < sp.held) weights[slot] += v;
+        if (h == 0 && slot < sp.held) {
+            if (a.w_splits > 1) part[slot] = v;
+            else weights[slot] += v;
+        }
     }
+}
+// The shares of the rows added to the weights, in order
+__global__ __launch_bounds__(256) void quant_many_add_kernel(QuantAttnArgs a) {
+    const int pair = blockIdx.y;
+    const QuantSpan sp(a, pair);
+    const int slot = blockIdx.x * 256 + threadIdx.x;
+    if (slot >= sp.held || sp.rows == 0) return;
+    const size_t at = (size_t)pair * a.capacity + slot, step = (size_t)a.pairs * a.capacity;
+    float v = 0.0f;
+    for (int s = 0; s < a.w_splits; ++s) v += a.part_w[s * step + at];
+    a.weights[at] += v;
 }
 
 template <int D, int GR>
@@ -700,7 +719,11 @@ static hipError_t run_many(hipStream_t s, const QuantAttnArgs &a, const QuantPla
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.weights) {
-        quant_many_weights_kernel<D, GR><<<dim3((unsigned)((int64_t)(a.capacity + 511) / 512 * pairs)), 512, 0, s>>>(a);
+        quant_many_weights_kernel<D, GR><<<dim3((unsigned)((int64_t)(a.capacity + 511) / 512 * a.w_splits * pairs)), 512, 0, s>>>(a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && a.weights && a.w_splits > 1) {
+        quant_many_add_kernel<<<dim3((unsigned)((a.capacity + 255) / 256), (unsigned)pairs), 256, 0, s>>>(a);
         e = hipGetLastError();
     }
     return e;

@@ -110,6 +110,12 @@ def test_workspaces_of_few_rows_do_not_grow_without_bound():
     assert 2 ** 29 < most < 2 ** 30 + 2 ** 24
 
 
+def test_workspaces_of_many_rows_do_not_follow_the_capacity():
+    lib = _lib()
+    q = _query(n_tokens=2000, weights=P, max_len=100)
+    assert 0 < lib.air_quant_workspace_bytes(C.byref(_cache(capacity=1 << 24)), C.byref(q)) < 2 ** 29 + 2 ** 26
+
+
 def _evict(n_planes=1, plane=None, w=P, pos=P, lens=P, out=2 * P, ws=None, nbytes=0, **kw):
     f = dict(batch=2, n_heads=2, capacity=100, keep=40, limit=50, first=2, recent=8)
     f.update(kw)
