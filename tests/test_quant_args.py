@@ -112,7 +112,7 @@ def test_workspaces_of_few_rows_do_not_grow_without_bound():
 
 def test_workspaces_of_many_rows_do_not_follow_the_capacity():
     lib = _lib()
-    q = _query(n_tokens=2000, weights=P, max_len=100)
+    q = _query(n_tokens=2000, weights=P, max_len=100, q_b=2000 * 512, out_b=2000 * 512)
     assert 0 < lib.air_quant_workspace_bytes(C.byref(_cache(capacity=1 << 24)), C.byref(q)) < 2 ** 29 + 2 ** 26
 
 
