@@ -243,8 +243,8 @@ def test_windows_and_pieces(dtype, d, group, causal):
 def test_many_rows(d, group, causal, hq, hkv, counts, held, room):
     import paper_2503_23956_amd as A
 
-    if room and len(held) * hkv > 8:
-        pytest.skip("large as it is")
+    if len(held) * hkv > 8:
+        room //= 16
     cache = _filled(A, len(held), hkv, max(held) + 3 + room, d, "bf16", group, held, 15)
     q = (_randn(18, len(held), max(counts), hq, d) * 2.0).bfloat16().transpose(1, 2)
     _check(A, cache, q, held, counts, causal, seed=6)
