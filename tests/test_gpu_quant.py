@@ -191,7 +191,7 @@ def _check(A, cache, q, held, counts, causal, seed=0, weigh=True, scale=0.0, len
         if weigh:
             was = w0[b].double()
             if lens is not None and lens[b] < n:
-                was[:, lens[b]:n] = 0.0
+                was[:, max(lens[b], 0):n] = 0.0
             far = (w[b, :, :n].double() - was[:, :n] - ww).abs()
             assert bool((far <= wb + (was[:, :n] + ww) * 2.0 ** -23).all()), f"sequence {b}: weights {far.max().item()} off"
             assert torch.equal(w[b, :, n:], w0[b, :, n:])
@@ -315,6 +315,39 @@ def test_values_that_are_not_numbers_reach_every_row_that_sees_them(dtype, d, gr
     out = q.clone()
     A.air_quant_attn(cache, q, out, lens=_ints([n]), causal=False)
     assert bool(out[..., :group].isnan().all()) and not bool(out[..., group:].isnan().any())
+
+
+@pytest.mark.parametrize("dtype,d,group", KINDS)
+@pytest.mark.parametrize("T,G,causal", [(8, 1, True), (4, 2, False), (2, 4, True)])
+def test_append_and_attend_of_few_rows(dtype, d, group, T, G, causal):
+    """Up to eight rows, written and read by one wave each: over the runs' borders, in front of slot 0, behind the last, ragged."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    cap, hkv = 300, 2
+    lens = [0, 25, 31, 32, 60, 63, 254, 250, -1, cap - 2, cap, 95]
+    counts = [T, T, 2, T, T - 1, 1, T, 0, T, T, T, T]
+    B = len(lens)
+    held = [min(max(n + c, 0), cap) for n, c in zip(lens, counts)]
+    cache = _filled(A, B, hkv, cap, d, dtype, group, [max(n, 0) for n in lens], 5)
+    before = [p.clone() for p in cache.planes]
+    q = (_randn(9, B, hkv * G, T, d) * 2.0).to(_type(dtype))
+    k, v = (_randn(10 + i, B, hkv, T, d).to(_type(dtype)) for i in range(2))
+    pos = torch.full((B, hkv, cap), -1, dtype=torch.int32, device="cuda:0")
+    other = A.QuantCache(B, hkv, cap, d, cache.dtype, group)
+    for p, o in zip(before, other.planes):
+        o.copy_(p)
+    A.air_quant_append(other, k, v, lens=_ints(lens), counts=_ints(counts))
+    _check(A, cache, q, held, counts, causal, lens=lens, k=k, v=v, positions=pos, first_positions=_ints([7 * b for b in range(B)]))
+    for p, o in zip(cache.planes, other.planes):
+        assert torch.equal(p.view(torch.uint8), o.view(torch.uint8))
+    for b, (at, n) in enumerate(zip(lens, counts)):
+        want = torch.full((cap,), -1, dtype=torch.int32)
+        for t in range(n):
+            if 0 <= at + t < cap:
+                want[at + t] = 7 * b + t
+        assert torch.equal(pos[b, 1].cpu(), want)
 
 
 @pytest.mark.parametrize("dtype,d,group", KINDS)
