@@ -7,6 +7,7 @@
 //   K to fp16, 11 bits (bf16's 8 would cost a logit 2^-9 of sum |q k|); where weights are wanted, to two fp16 terms, 22 bits, as logits are
 //   then part of an fp32 result.  Queries go to fp16 too, exactly: rows of either whose greatest magnitude lies outside 2^-6 .. 2^14 are
 //   held divided by a power of two, and their logits multiplied by it;
+//   probabilities to fp16, times a power of two that follows the row (below);
 //   V to fp16, like the probabilities, unless the workgroup's share of V has a group (of all its slots) whose greatest magnitude lies outside
 //   2^-4 .. 2^14, which the pairs tell beforehand: then both to bf16, which holds any magnitude, with 8 bits (outputs 0.0025 off fp64 in place
 //   of 0.0018; an fp32 computation rounded once 0.0017).
@@ -22,6 +23,15 @@
 namespace air {
 
 constexpr float kLeast = 0x1p-6f, kMost = 0x1p14f;  // magnitudes held as they are
+
+// Probabilities in fp16, which has 11 bits down to 2^-14 and steps of 2^-24 below: against the reference they are held times 2^kLift (with the kSlack that
+// a logit may lie above the reference 2^15 at most), and the reference follows a row down as well as up.  Where the greatest logit of 32 slots lies more
+// than kDrop below it, it is lowered to that, and the row's sums, which are fp32, are multiplied: what is far below a row's greatest logit keeps its bits,
+// for it may be all that the row's outputs are made of, or be many.  Beside 11 bits a probability loses no more than 2^-25 2^(kDrop - kLift) = 2^-18 of the
+// greatest of its 32 slots, and 2^-31 of the row's greatest (references are rounded up to whole numbers, so that sums are multiplied by powers of two, without
+// rounding).  No reference lies further than kReach below the highest, so that no sum overflows (2^(kLift + kSlack + kReach), values of 2^16, 2^24 slots).
+// Rows whose logits reach from -7 to 7 lower it now and then: with kDrop 12 a window of 64 queries with weights took 671 us, with 14 664.
+constexpr float kLift = 7.0f, kDrop = 14.0f, kReach = 60.0f;
 
 __device__ __forceinline__ f32x16 mma32_f16(const uint4 &a, const uint4 &b, f32x16 acc) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
@@ -228,7 +238,8 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
-    float l = 0.f, l2 = 0.f, ref = -INFINITY, top = -INFINITY, sub = 0.f;  // top: the logit (scaled) from which on the reference is raised
+    float l = 0.f, l2 = 0.f, ref = -INFINITY, high = -INFINITY, sub = 0.f;  // high: the highest that the reference was
+    float top = -INFINITY, low = -INFINITY;  // logits (scaled) above and below which the reference is raised and lowered
     bool huge = false;
     const int row = row0 + 32 * rw + n, m_row = min(row, sp.rows - 1), tok = a.by_g.of(m_row);
     const int64_t head = (int64_t)sp.h * a.G + m_row - tok * a.G;
@@ -267,6 +278,7 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     };
     auto run = [&](auto wide_tag) {
     constexpr bool WIDE = decltype(wide_tag)::value;
+    constexpr float kUp = WIDE ? 0.0f : kLift;  // (bf16 holds probabilities of any size)
     auto keep = [&](int b) {
         if (b >= b1) return;
         bool bad = false;
@@ -308,25 +320,32 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
             mx = largest(s);
         }
         mx *= row_c;
-        if (__builtin_expect(__ballot(mx > top) != 0ull, 0)) {
-            const float now = fmaxf(ref, fmaxf(mx, __shfl_xor(mx, 32, 64)));
-            const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - now);  // no logit but -inf yet: nothing to scale
+        const uint64_t under = WIDE ? 0 : __ballot(mx < low);  // (both lanes of a row)
+        if (__builtin_expect(__ballot(mx > top) != 0ull || ((uint32_t)under & (uint32_t)(under >> 32)) != 0u, 0)) {
+            const float both = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            float now = ref;
+            if (both > ref) now = ceilf(both);
+            else if (both < low && both > -INFINITY) now = fmaxf(ceilf(both), high - kReach);
+            // (no logit but -inf yet: nothing to scale)
+            const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_ldexpf(1.0f, (int)fmaxf(ref - now, -300.0f));
             l *= f;
             l2 *= f;
             ref = now;
+            high = fmaxf(high, now);
             top = now + kSlack;
-            sub = finite_or_zero(now);
+            low = !WIDE && now > high - kReach ? now - kDrop : -INFINITY;
+            sub = finite_or_zero(now) - kUp;
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[d][i] *= f;
-            huge = huge || __ballot(fabsf(sub) > kHuge) != 0ull;
+            huge = huge || __ballot(fabsf(finite_or_zero(now)) > kHuge) != 0ull;
         }
         if (__builtin_expect(huge, 0)) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = rounded_exponent(s[i], row_c, finite_or_zero(ref));
             mul = 1.f;
-            sub = 0.f;
+            sub = -kUp;
         }
     };
     const int v_at = v_lane(lane);
@@ -405,6 +424,17 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
                 if (b + 1 < b1) block(b + 1, sb, sa);
             }
         }
+    }
+    // sums as they are against the highest reference, which tells what they weigh beside those of other workgroups
+    if (!WIDE && high > -INFINITY) {
+        const float f = __builtin_amdgcn_ldexpf(1.0f, (int)fmaxf(ref - high, -300.0f) - (int)kUp);
+        l *= f;
+        l2 *= f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+        ref = high;
     }
     };
     // does the share of V have magnitudes that fp16 does not hold as well as their neighbours?
