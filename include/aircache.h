@@ -394,10 +394,11 @@ size_t air_quant_workspace_bytes(const air_quant_cache *cache, const air_quant_q
  * A query that sees no slot gives zero.  What lies in slots that a query does not see counts for nothing, whatever it stands for; a group
  * of NaN in a slot that it sees makes its part of the output (V) or all of it (K) NaN.  fp32: products of codes are exact, everything
  * else is held in fp32.  bf16: the same logits and sums, and factors p step of 15 bits for the second product; large calls of 33 rows (queries
- * x query heads per KV head) and more round what V stands for and the probabilities to 11 bits (8 where a group of V has no magnitude between
- * 2^-4 and 2^14, or one above; a probability loses besides at most 2^-18 of the greatest among slots 32 i .. 32 i + 31, its own one of them, and 2^-31 of its
- * row's greatest), and without weights what K stands for to 11 bits.  Outputs are rounded once.  The sums of an output hold p up
- * to 2^8 times the probability of the row's greatest logit, undivided: V of 2^95 and more can overflow them.
+ * x query heads per KV head) and more round what V stands for and the probabilities to 11 bits, 8 where groups of a slot's V lie further than 2^24 below
+ * the same group of another slot (an element of V loses besides at most 2^-15 of the greatest of its group; a probability 2^-18 of the greatest
+ * among slots 32 i .. 32 i + 31, its own one of them, and at most 2^-31 of its row's greatest), and without weights what K stands for to 11 bits.
+ * Outputs are rounded once.  The sums of an output hold p up to 2^8 times the probability of the row's greatest logit, undivided: V of 2^95 and more can
+ * overflow them.
  * Causal queries belong to the last counts slots of the sequence: after air_evict slots have no order, so a call of
  * more than one causal query appends its own rows.  workspace: 256-byte aligned, free for another call when this one's work has run.
  * out must not overlap an input; output rows that overlap are refused (AIR_ERR_SHAPE). */

@@ -8,9 +8,10 @@
 //   then part of an fp32 result.  Queries go to fp16 too, exactly: rows of either whose greatest magnitude lies outside 2^-6 .. 2^14 are
 //   held divided by a power of two, and their logits multiplied by it;
 //   probabilities to fp16, times a power of two that follows the row (below);
-//   V to fp16, like the probabilities, unless the workgroup's share of V has a group (of all its slots) whose greatest magnitude lies outside
-//   2^-4 .. 2^14, which the pairs tell beforehand: then both to bf16, which holds any magnitude, with 8 bits (outputs 0.0025 off fp64 in place
-//   of 0.0018; an fp32 computation rounded once 0.0017).
+//   V to fp16, a group of columns at a time divided by the power of two that brings the greatest magnitude of the workgroup's share of V there to 2^14, as
+//   the pairs tell beforehand: a slot's group 2^24 times smaller still has 11 bits, and its smaller elements lose 2^-15 of its greatest.  Where some
+//   slot's group is smaller than that, V and the probabilities become bf16, which holds any magnitude, with 8 bits (outputs 0.0025 off fp64 in
+//   place of 0.0018; an fp32 computation rounded once 0.0017).
 // Per 32 x 64 logits a wave issues 16 + 16 products of 32 clocks (weights: 32 + 16); dequantising costs about 70 vector instructions a
 // wave and block.  500 queries of 28 / 4 heads behind 7432 slots: 92 us, 600 TFLOP/s (matrix unit busy 26 %: four splits of 28 blocks, prologue and
 // epilogue beside them; vector unit 39 %); 64 queries of 64 / 8 heads over eight caches of 16 k slots, with weights, 410 us (41 % and 53 %), the weights'
@@ -42,6 +43,12 @@ __device__ __forceinline__ float unit_of(float greatest) {
     const int e = (int)(__float_as_uint(greatest) >> 23);  // (a subnormal number counts as 2^-126, an infinity as 2^126)
     return __uint_as_float((uint32_t)(e < 1 ? 1 : e > 253 ? 253 : e) << 23);
 }
+// Exponent of the power of two that values of a group of columns are held divided by, of the greatest magnitude there (at least 2^-112): that becomes 2^14 .. 2^15
+__device__ __forceinline__ int value_exponent(float greatest) {
+    const int e = (int)(__float_as_uint(greatest) >> 23);
+    return (e < 15 ? 15 : e > 254 ? 254 : e) - 127 - 14;
+}
+constexpr float kSpread = 0x1p-24f, kTiny = 0x1p-112f;  // magnitudes of a group of columns that fp16 holds: of the greatest; the greatest
 // eight elements of a query divided by the row's unit
 __device__ __forceinline__ uint4 to_f16(const uint4 &x, float inv) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -143,10 +150,10 @@ struct CodeStage {
         }
         vp = vs[slot * (D / GR) + value_group()];
     }
-    // Into LDS (sk2: second terms); unit[key]: what the key was divided by (true: some key by more than 1).  Of a block that some row does not see all of, `left` slots from
+    // Into LDS (sk2: second terms), values times v_inv; unit[key]: what the key was divided by (true: some key by more than 1).  Of a block that some row does not see all of, `left` slots from
     // its first are held: values behind them and of groups of NaN become 0 (bad: there were some)
     template <int TERMS, bool WIDE>
-    __device__ __forceinline__ bool store(u32x4 *sk, u32x4 *sk2, u32x4 *sv, float *unit, bool part, int left, bool &bad) {
+    __device__ __forceinline__ bool store(u32x4 *sk, u32x4 *sk2, u32x4 *sv, float *unit, float v_inv, bool part, int left, bool &bad) {
         float lo[kPairs], step[kPairs], most = 0.0f;
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
@@ -174,6 +181,7 @@ struct CodeStage {
             if (TERMS == 2) sk2[at] = __builtin_bit_cast(u32x4, x[TERMS - 1]);
         }
         float vlo = lo_of(vp), vstep = step_of(vp);
+        if (!WIDE) vlo *= v_inv, vstep *= v_inv;
         if (part) {
             const bool nan = (vp & 0x7f80u) == 0x7f80u && key < left;
             bad = bad || nan;
@@ -212,7 +220,9 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     constexpr int NW = 8, RW = NW / KW, kRows = 32 * RW, kKeys = 64, ND = D / 32, NS = R::kSlices, kBufs = 3;
     constexpr int KT = WEIGH ? 2 : 1;  // terms of a key's elements
     __shared__ u32x4 tiles[2 * kBufs * (KT * R::kKTile + R::kVTile)];
-    __shared__ float units[kBufs][kKeys], s_most[8][D / GR];
+    __shared__ float units[kBufs][kKeys];
+    __shared__ __align__(16) Words<D / GR> s_most[NW];  // greatest magnitudes of V, by wave
+    __shared__ int s_exponent[D / GR], s_wide;
     __shared__ float2 s_ml[KW == 2 ? RW * 32 : 1];
     __shared__ float s_l2[KW == 2 ? RW * 32 : 1];
     __shared__ int s_bad, s_units;
@@ -276,13 +286,14 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     auto load = [&](int b) {
         if (b < b1) stage.load(kc, vc, ks, vs, b * kKeys, sp.held);
     };
+    float v_inv = 1.0f;  // what the thread's values are multiplied by
     auto run = [&](auto wide_tag) {
     constexpr bool WIDE = decltype(wide_tag)::value;
     constexpr float kUp = WIDE ? 0.0f : kLift;  // (bf16 holds probabilities of any size)
     auto keep = [&](int b) {
         if (b >= b1) return;
         bool bad = false;
-        if (stage.template store<KT, WIDE>(sk(b), sk(b) + kSecond, sv(b), units[b % kBufs], (b + 1) * kKeys > see_all, sp.held - b * kKeys, bad)) s_units = 1;
+        if (stage.template store<KT, WIDE>(sk(b), sk(b) + kSecond, sv(b), units[b % kBufs], v_inv, (b + 1) * kKeys > see_all, sp.held - b * kKeys, bad)) s_units = 1;
         if (bad) s_bad = 1;
     };
     auto read_k = [&](u32x4(&x)[NS], const u32x4 *sk_) {
@@ -388,7 +399,6 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
         f32x16 sa, sb;
         float mx;
         u32x4 kf[NS];
-        load(b0);
         keep(b0);
         load(b0 + 1);
         if constexpr (KW == 2) {
@@ -427,41 +437,56 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     }
     // sums as they are against the highest reference, which tells what they weigh beside those of other workgroups
     if (!WIDE && high > -INFINITY) {
-        const float f = __builtin_amdgcn_ldexpf(1.0f, (int)fmaxf(ref - high, -300.0f) - (int)kUp);
-        l *= f;
-        l2 *= f;
+        const int e = (int)fmaxf(ref - high, -300.0f) - (int)kUp;
+        l = __builtin_amdgcn_ldexpf(l, e);
+        l2 = __builtin_amdgcn_ldexpf(l2, e);
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d) {
+            const int ed = e + s_exponent[32 * d / GR];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+            for (int i = 0; i < 16; ++i) acc[d][i] = __builtin_amdgcn_ldexpf(acc[d][i], ed);
+        }
         ref = high;
     }
     };
-    // does the share of V have magnitudes that fp16 does not hold as well as their neighbours?
-    {
-        Words<D / GR> pairs;
-        float most[D / GR] = {};
-        for (int slot = b0 * kKeys + threadIdx.x; slot < min(b1 * kKeys, sp.held); slot += 64 * NW) {
-            pairs = load_words<D / GR>(vs + (size_t)slot * (D / GR));
+    load(b0);  // (on its way meanwhile)
+    // does the share of V have magnitudes that fp16 does not hold?
+    float most[D / GR] = {}, least[D / GR];  // magnitudes that are not 0
 #pragma unroll
-            for (int g = 0; g < D / GR; ++g) most[g] = fmaxf(most[g], fmaxf(fabsf(lo_of(pairs.w[g])), fabsf(fmaf(15.0f, step_of(pairs.w[g]), lo_of(pairs.w[g])))));
-        }
+    for (int g = 0; g < D / GR; ++g) least[g] = INFINITY;
+    for (int slot = b0 * kKeys + threadIdx.x; slot < min(b1 * kKeys, sp.held); slot += 64 * NW) {
+        const Words<D / GR> pairs = load_words<D / GR>(vs + (size_t)slot * (D / GR));
 #pragma unroll
         for (int g = 0; g < D / GR; ++g) {
-            most[g] = wave_max(most[g]);
-            if (lane == 0) s_most[wave][g] = most[g];
+            const float x = fmaxf(fabsf(lo_of(pairs.w[g])), fabsf(fmaf(15.0f, step_of(pairs.w[g]), lo_of(pairs.w[g]))));
+            most[g] = fmaxf(most[g], x);
+            least[g] = fminf(least[g], x > 0.f ? x : INFINITY);
         }
     }
-    if (threadIdx.x == 0) s_bad = s_units = 0;
-    __syncthreads();
-    bool wide = false;
 #pragma unroll
     for (int g = 0; g < D / GR; ++g) {
-        float most = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) most = fmaxf(most, s_most[w][g]);
-        wide = wide || most > kMost || (most > 0.f && most < 0x1p-4f);
+        const float x = wave_max(most[g]);
+        if (lane == 0) s_most[wave].w[g] = __float_as_uint(x);
     }
+    if (threadIdx.x == 0) s_bad = s_units = s_wide = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const Words<D / GR> x = load_words<D / GR>(&s_most[w]);
+#pragma unroll
+        for (int g = 0; g < D / GR; ++g) most[g] = fmaxf(most[g], __uint_as_float(x.w[g]));
+    }
+    bool spread = false;
+#pragma unroll
+    for (int g = 0; g < D / GR; ++g) {
+        spread = spread || (most[g] > 0.f && (most[g] < kTiny || least[g] < most[g] * kSpread));
+        const int e = value_exponent(most[g]);
+        if (g == stage.value_group()) v_inv = __builtin_amdgcn_ldexpf(1.0f, -e);
+        if ((int)threadIdx.x == g) s_exponent[g] = e;
+    }
+    if (spread) s_wide = 1;
+    __syncthreads();
+    const int wide = s_wide;
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(wide), 0)) run(std::true_type());
     else run(std::false_type());
     l += __shfl_xor(l, 32, 64);

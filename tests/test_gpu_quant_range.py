@@ -51,12 +51,12 @@ def _floor(p):
 
 
 # ---- probabilities ---------------------------------------------------------------------------------------------------------------
-def _check_out(got, size, p, val, group, terms):
+def _check_out(got, size, p, val, group, terms, bits=11):
     """Outputs against sum p v: 11 bits of a probability, of their sum and of a value, 2^-15 of the greatest of a value's group, the floor."""
     want, a = p @ val, p @ val.abs()
     great = val.abs().unflatten(-1, (-1, group)).amax(-1).repeat_interleave(group, -1)
     off = _logit_error(size, val.shape[-1], terms)
-    bound = (p * off) @ val.abs() + a * off.amax(-1, keepdim=True) + 3 * 2.0 ** -11 * a + p @ great * 2.0 ** -15 + _floor(p) @ val.abs()
+    bound = (p * off) @ val.abs() + a * off.amax(-1, keepdim=True) + 3 * 2.0 ** -bits * a + p @ great * 2.0 ** -15 + _floor(p) @ val.abs()
     bound = bound * 1.01 + (want.abs() + bound) * 2.0 ** -8
     far = (got.double() - want).abs()
     assert bool((far <= bound).all()), f"{(far / bound).max().item()} of the bound, {(far / a).max().item()} of sum p |v|"
@@ -151,3 +151,37 @@ def test_logits_that_rise_and_fall(rows, weigh):
     _check_out(out[0, 0], size, p, val, 32, 2 if weigh else 1)
     if weigh:
         _check_weights(w[0, 0, :n], size, p, d)
+
+
+# ---- values ----------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("below", [10, 16, 20, 23, 30, 100])
+@pytest.mark.parametrize("rows", [4, 20, 48, 300])
+@pytest.mark.parametrize("d,group", [(64, 32), (64, 64), (128, 32), (128, 64)])
+@pytest.mark.parametrize("weighs", [False, True])
+@pytest.mark.parametrize("pieces", [1, 2])
+def test_values_beside_larger_ones(below, rows, d, group, weighs, pieces):
+    """A slot of ordinary values, at which no row looks, or which weighs 2^-below, beside others 2^-below as large; in every group of columns the same at
+    another size.  A row looks at few slots.  Read in one piece (many heads) or many."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    n, H, room, scale = (1500, 256, 0, 0.5) if pieces == 1 else (1500, 1, 70000, 0.5)
+    cache = A.QuantCache(1, H, n + room, d, group=group)
+    k, v = 0.5 * _randn(1, 1, H, n, d), _randn(2, 1, H, n, d) * 2.0 ** -below
+    k[..., 0] = 0.0
+    k[:, :, 700, 0] = -below * math.log(2.0) / (scale * 16.0) if weighs else -4000.0
+    v[:, :, 700] *= 2.0 ** below
+    for g in range(d // group):
+        v[..., g * group:(g + 1) * group] *= 10.0 ** (3 * g)
+    A.air_quant_append(cache, k.bfloat16(), v.bfloat16())
+    q = _randn(3, 1, H, rows, d)
+    q[..., 0] = 16.0
+    q = q.bfloat16()
+    out, w = torch.empty_like(q), torch.zeros((1, H, n + room), device="cuda:0")
+    A.air_quant_attn(cache, q, out, lens=_ints([n]), causal=False, scale=scale, weights=w)
+    for h in (0, H // 2):
+        size, p, val = _formula(cache, q, n, scale, h)
+        # (the slot's own logit is far from the others': its error, larger than theirs, is not that of their probabilities)
+        size[:, 700] = torch.where(p[:, 700] > 2.0 ** -126, size[:, 700], 0.0)
+        _check_out(out[0, h], size, p, val, group, 2, 11 if below < 24 else 8)
