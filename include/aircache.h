@@ -396,7 +396,8 @@ size_t air_quant_workspace_bytes(const air_quant_cache *cache, const air_quant_q
  * else is held in fp32.  bf16: the same logits and sums, and factors p step of 15 bits for the second product; large calls of 33 rows (queries
  * x query heads per KV head) and more round what V stands for and the probabilities to 11 bits, 8 where groups of a slot's V lie further than 2^24 below
  * the same group of another slot (an element of V loses besides at most 2^-15 of the greatest of its group; a probability 2^-18 of the greatest
- * among slots 32 i .. 32 i + 31, its own one of them, and at most 2^-31 of its row's greatest), and without weights what K stands for to 11 bits.
+ * among slots 32 i .. 32 i + 31, its own one of them, and at most 2^-31 of its row's greatest), and without weights what K stands for to 11 bits
+ * (with them to 22; elements of K and of queries lose besides at most 2^-22 of their row's greatest).
  * Outputs are rounded once.  The sums of an output hold p up to 2^8 times the probability of the row's greatest logit, undivided: V of 2^95 and more can
  * overflow them.
  * Causal queries belong to the last counts slots of the sequence: after air_evict slots have no order, so a call of

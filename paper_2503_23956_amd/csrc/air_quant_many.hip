@@ -5,8 +5,9 @@
 // wave's next logits formed under the exponentials of its present ones.  What differs is how a block gets into LDS: a thread turns 16
 // codes of K and 16 of V into numbers, lo + step code in fp32, rounded once:
 //   K to fp16, 11 bits (bf16's 8 would cost a logit 2^-9 of sum |q k|); where weights are wanted, to two fp16 terms, 22 bits, as logits are
-//   then part of an fp32 result.  Queries go to fp16 too, exactly: rows of either whose greatest magnitude lies outside 2^-6 .. 2^14 are
-//   held divided by a power of two, and their logits multiplied by it;
+//   then part of an fp32 result.  Queries go to fp16 too, their eight bits exactly.  Rows of either are held times 16, and where their greatest magnitude
+//   lies outside 2^-7 .. 2^11 divided by a power of two that their logits are multiplied by: the greatest held is at least 2^-3, and what lies below
+//   fp16's normal numbers loses at most 2^-25, 2^-22 of it;
 //   probabilities to fp16, times a power of two that follows the row (below);
 //   V to fp16, a group of columns at a time divided by the power of two that brings the greatest magnitude of the workgroup's share of V there to 2^14, as
 //   the pairs tell beforehand: a slot's group 2^24 times smaller still has 11 bits, and its smaller elements lose 2^-15 of its greatest.  Where some
@@ -23,7 +24,7 @@
 
 namespace air {
 
-constexpr float kLeast = 0x1p-6f, kMost = 0x1p14f;  // magnitudes held as they are
+constexpr float kLeast = 0x1p-7f, kMost = 0x1p11f, kHeld = 16.0f;  // greatest magnitudes of rows of K and queries that need no unit; what all are held times
 
 // Probabilities in fp16, which has 11 bits down to 2^-14 and steps of 2^-24 below: against the reference they are held times 2^kLift (with the kSlack that
 // a logit may lie above the reference 2^15 at most), and the reference follows a row down as well as up.  Where the greatest logit of 32 slots lies more
@@ -40,9 +41,12 @@ __device__ __forceinline__ f32x16 mma32_f16(const uint4 &a, const uint4 &b, f32x
 // the power of two that brings a greatest magnitude outside the bounds to 1 .. 2; else 1
 __device__ __forceinline__ float unit_of(float greatest) {
     if (!(greatest > kMost || greatest < kLeast) || greatest == 0.0f) return 1.0f;
-    const int e = (int)(__float_as_uint(greatest) >> 23);  // (a subnormal number counts as 2^-126, an infinity as 2^126)
-    return __uint_as_float((uint32_t)(e < 1 ? 1 : e > 253 ? 253 : e) << 23);
+    const int e = (int)(__float_as_uint(greatest) >> 23);  // (less than 2^-123 counts as that, an infinity as 2^126)
+    return __uint_as_float((uint32_t)(e < 4 ? 4 : e > 253 ? 253 : e) << 23);
 }
+// kHeld / unit
+__device__ __forceinline__ float held_over(float unit) { return __uint_as_float(((127u + 127u + 4u) << 23) - __float_as_uint(unit)); }
+static_assert(kHeld == 16.0f, "2^4");
 // Exponent of the power of two that values of a group of columns are held divided by, of the greatest magnitude there (at least 2^-112): that becomes 2^14 .. 2^15
 __device__ __forceinline__ int value_exponent(float greatest) {
     const int e = (int)(__float_as_uint(greatest) >> 23);
@@ -163,12 +167,11 @@ struct CodeStage {
         }
         most = max8(most);
         const float u = unit_of(most);
-        if (u != 1.0f) {
+        const float f = held_over(u);
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                lo[i] /= u;
-                step[i] /= u;
-            }
+        for (int i = 0; i < kPairs; ++i) {
+            lo[i] *= f;
+            step[i] *= f;
         }
         if (piece == 0) unit[key] = u;
         u32x4 *tv = sv + (key >> 5) * R::kVTile;
@@ -274,8 +277,8 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
         }
         const float unit = unit_of(fmaxf(most, __shfl_xor(most, 32)));
 #pragma unroll
-        for (int sl = 0; sl < NS; ++sl) q[sl] = to_f16(q[sl], 1.0f / unit);
-        row_c *= unit;
+        for (int sl = 0; sl < NS; ++sl) q[sl] = to_f16(q[sl], held_over(unit));
+        row_c = row_c * unit / (kHeld * kHeld);
     }
     float mul = row_c;
     const size_t base = (size_t)pair * a.capacity;

@@ -185,3 +185,29 @@ def test_values_beside_larger_ones(below, rows, d, group, weighs, pieces):
         # (the slot's own logit is far from the others': its error, larger than theirs, is not that of their probabilities)
         size[:, 700] = torch.where(p[:, 700] > 2.0 ** -126, size[:, 700], 0.0)
         _check_out(out[0, h], size, p, val, group, 2, 11 if below < 24 else 8)
+
+
+# ---- keys ------------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [4, 20, 48, 300])
+@pytest.mark.parametrize("size", [-20, -8, -7, -6, -5, 0, 10, 11, 12, 40])
+def test_weights_of_small_and_large_keys(rows, size):
+    """Equal keys lo + 8 step = 2^size (1 + 255 2^-19), whose low bits lie 2^-19 and less below: the rows' logits are 600 (base 2), and every slot has its share.
+    K has 22 bits, sums round 16 times (of the products of two terms) and 6 times (by group) to 24."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    n, d, room = 40, 128, 70000
+    cache = A.QuantCache(1, 1, n + room, d)
+    for p in cache.planes[:2]:
+        p.fill_(0x88)
+    for p in cache.planes[2:]:
+        p[..., ::2], p[..., 1::2] = 2.0 ** size, 255 * 2.0 ** (size - 22)
+    q = torch.full((1, 1, rows, d), 2304.0 * 2.0 ** (-6 - size), device="cuda:0").bfloat16()
+    w = torch.zeros((1, 1, n + room), device="cuda:0")
+    A.air_quant_attn(cache, q, None, lens=_ints([n]), causal=False, weights=w)
+    want = rows / n
+    bound = math.log(2.0) * 600 * (2.0 ** -22 + 22 * 2.0 ** -24) + 2.0 ** -21 + (n + rows + 72) * 2.0 ** -24
+    far = (w[0, 0, :n].double() - want).abs().max().item() / want
+    assert far <= bound, f"{far} off, {bound} allowed"
+    assert not bool(w[0, 0, n:].any())
