@@ -185,7 +185,7 @@ struct QuantPlan {
     bool few;                               // the kernel for few rows, which appends by itself
     int32_t max_runs;                       // runs of 32 slots per (sequence, KV head) whose logits are kept; 0: none
     int32_t tile_rows;                      // many rows: 128 or 256 a workgroup; else 0
-    size_t l2_at, ref_at, sums_at, w_at;    // many rows with weights: where second sums, references, sums of queries and shares of the weights lie
+    size_t norm_at, ref_at, sums_at, w_at;  // many rows with weights: where the splits' references and sums, the rows', sums of queries and shares of the weights lie
     int32_t w_splits;                       // of the rows in the weights' launch
     int32_t slot_tiles;                     // of 16 slots that a wave of the second launch takes: 4 or 1
     int32_t finish;                         // workgroups per (sequence, KV head) of the second launch; 0: none

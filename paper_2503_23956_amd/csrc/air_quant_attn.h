@@ -17,7 +17,7 @@ struct QuantAttnArgs {
     float *part_o;    // [pair][split][row][D]
     float2 *part_ml;  // [pair][split][row]
     // many rows with weights:
-    float *part_l2;    // [pair][split][row]: sums of the unrounded probabilities
+    float2 *part_norm; // [pair][split][row]: reference and sum that the weights are formed with
     float4 *row_ref;   // [pair][row]: reference, 1 / sum, slots seen (whole number), nothing
     uint4 *row_sums;   // [pair][row][2]: sums of the queries' groups as bf16 terms, as the product with lo takes them
     float *part_w;     // [share of the rows][pair][slot]: weights, where there are several shares

@@ -963,8 +963,8 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
         const size_t cells = (size_t)pairs * p.splits * rows;
         const auto whole = [](size_t n) { return (n + 255) / 256 * 256; };
         if (p.splits > 1) p.ml_bytes = whole(cells * sizeof(float2));
-        p.l2_at = p.ml_bytes + (p.splits > 1 ? whole(cells * c.head_dim * sizeof(float)) : 0);
-        p.ref_at = p.l2_at + (q.weights && p.splits > 1 ? whole(cells * sizeof(float)) : 0);
+        p.norm_at = p.ml_bytes + (p.splits > 1 ? whole(cells * c.head_dim * sizeof(float)) : 0);
+        p.ref_at = p.norm_at + (q.weights && p.splits > 1 ? whole(cells * sizeof(float2)) : 0);
         p.sums_at = p.ref_at + (q.weights ? whole((size_t)pairs * rows * sizeof(float4)) : 0);
         p.w_at = p.sums_at + (q.weights ? whole((size_t)pairs * rows * 2 * sizeof(uint4)) : 0);
         // The weights' workgroups have 512 slots each: where they would leave CUs without work, the rows are dealt to several, by whole turns of 128
@@ -1077,7 +1077,7 @@ hipError_t launch_quant_attn(hipStream_t s, const air_quant_cache &c, const Quan
     a.pairs = pairs;
     a.by_pairs = div_by(pairs);
     uint8_t *space = static_cast<uint8_t *>(workspace);
-    a.part_l2 = reinterpret_cast<float *>(space + p.l2_at);
+    a.part_norm = reinterpret_cast<float2 *>(space + p.norm_at);
     a.row_ref = reinterpret_cast<float4 *>(space + p.ref_at);
     a.row_sums = reinterpret_cast<uint4 *>(space + p.sums_at);
     a.part_w = reinterpret_cast<float *>(space + p.w_at);

@@ -127,6 +127,7 @@ struct CodeStage {
     static constexpr int kWords = D / 64, kPairs = GR == 32 ? kWords : 1;  // dwords of codes; pairs of K that belong to them
     int key, piece;
     uint32_t k[kWords], v[kWords], kp[kPairs], vp;
+    float k_most[kPairs] = {};  // greatest magnitudes of the thread's groups of K
 
     __device__ __forceinline__ void init(int thread) {
         key = thread >> 3;
@@ -163,7 +164,9 @@ struct CodeStage {
         for (int i = 0; i < kPairs; ++i) {
             lo[i] = lo_of(kp[i]);
             step[i] = step_of(kp[i]);
-            most = fmaxf(most, fmaxf(fabsf(lo[i]), fabsf(fmaf(15.0f, step[i], lo[i]))));
+            const float x = fmaxf(fabsf(lo[i]), fabsf(fmaf(15.0f, step[i], lo[i])));
+            most = fmaxf(most, x);
+            if (TERMS == 2) k_most[i] = fmaxf(k_most[i], x);
         }
         most = max8(most);
         const float u = unit_of(most);
@@ -215,6 +218,52 @@ __device__ __forceinline__ void write_sums(const float (&part)[NG], uint4 *to) {
     }
 }
 
+// Logits of weights: exact products of codes.  A lane (n, h) has elements 8 (2 sl + h) .. + 7 of a slot's codes as numbers,
+template <int D, int GR>
+struct CodeKeys {
+    static constexpr int NS = D / 16, NG = D / GR;
+    uint4 k[NS];
+    Words<NG> pairs;
+    __device__ __forceinline__ void load(const uint8_t *kc, const uint32_t *ks, uint32_t slot, int h) {
+        Words<D / 32> w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] = load_words<D / 32>(kc + (slot * (D / 2) + D / 8 * (h + 2 * i)));
+        pairs = load_words<NG>(ks + (size_t)slot * NG);
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) {  // piece 2 sl + h = 4 m + nq; the codes in the order of the elements
+            const uint4 x = operand_of(w[sl & 1].w[sl >> 1]);
+            k[sl] = uint4{__builtin_amdgcn_perm(x.y, x.x, 0x05040100u), __builtin_amdgcn_perm(x.w, x.z, 0x05040100u),
+                          __builtin_amdgcn_perm(x.y, x.x, 0x07060302u), __builtin_amdgcn_perm(x.w, x.z, 0x07060302u)};
+        }
+    }
+    // before the factor: slot n, rows 8 (i >> 2) + 4 h + (i & 3) of 32, whose elements (as the codes' lie) and sums are q and sums
+    __device__ __forceinline__ f32x16 logits(const u32x4 (&q)[NS], const uint4 &sums) const {
+        const uint32_t a01 = NG == 1 ? pairs.w[0] & 0xffffu : __builtin_amdgcn_perm(pairs.w[1 % NG], pairs.w[0], 0x05040100u);
+        const uint32_t a23 = NG == 4 ? __builtin_amdgcn_perm(pairs.w[3 % NG], pairs.w[2 % NG], 0x05040100u) : a01;
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        s = mma32(sums, uint4{a01, a23, a01, a23}, s, bf16_t());
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < GR / 16; ++j) z = mma32(__builtin_bit_cast(uint4, q[g * (GR / 16) + j]), k[g * (GR / 16) + j], z, bf16_t());
+            const float step = step_of(pairs.w[g]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = fmaf(step, z[i], s[i]);
+        }
+        return s;
+    }
+};
+// The logits of the outputs are off those of the weights by fp32 steps of what they are sums of, so that the sum of a row's probabilities in the one is no measure
+// for the other where these are large: a logit beyond kLarge (base 2), or magnitudes (by group: the query's, times the greatest of K) that add up to more
+// than kLargeSum.  The reference and sum of such rows are formed once more, with the weights' own logits (beyond kLarge with the product with the factor rounded, as
+// there), so that equal logits share equally and a row's weights add up to one at any size.
+constexpr float kLarge = 256.0f, kLargeSum = 4096.0f;
+
 // KW 1: 256 rows, every wave takes both halves of a block.  KW 2: 128 rows, two waves share 32 rows and take a half of every block each.
 // WEIGH: a second sum, of the probabilities as they were before they were rounded, for the weights of the slots.
 template <int D, int GR, int KW, bool WEIGH>
@@ -228,6 +277,8 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     __shared__ int s_exponent[D / GR], s_wide;
     __shared__ float2 s_ml[KW == 2 ? RW * 32 : 1];
     __shared__ float s_l2[KW == 2 ? RW * 32 : 1];
+    __shared__ float2 s_norm[WEIGH ? RW * 32 : 1];
+    __shared__ uint32_t s_k_most[D / GR];
     __shared__ int s_bad, s_units;
     auto sk = [&](int b) { return tiles + b % kBufs * (2 * R::kKTile); };  // the two tiles of block b
     auto sv = [&](int b) { return tiles + 2 * kBufs * R::kKTile + b % kBufs * (2 * R::kVTile); };
@@ -472,6 +523,7 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
         if (lane == 0) s_most[wave].w[g] = __float_as_uint(x);
     }
     if (threadIdx.x == 0) s_bad = s_units = s_wide = 0;
+    if (threadIdx.x < D / GR) s_k_most[threadIdx.x] = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
@@ -493,7 +545,17 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(wide), 0)) run(std::true_type());
     else run(std::false_type());
     l += __shfl_xor(l, 32, 64);
-    if (WEIGH) l2 += __shfl_xor(l2, 32, 64);
+    if constexpr (WEIGH) {
+        l2 += __shfl_xor(l2, 32, 64);
+#pragma unroll
+        for (int i = 0; i < stage.kPairs; ++i) {
+            float x = stage.k_most[i];
+#pragma unroll
+            for (int m = 2; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m, 64));
+            if (lane < 2) atomicMax(&s_k_most[stage.key_group() + i], __float_as_uint(x));
+        }
+        if (KW == 1) lds_barrier();
+    }
     if constexpr (KW == 2) {  // the two waves of 32 rows: lane by lane
         static_assert(sizeof(tiles) >= RW * 32 * D * sizeof(float), "the tiles' memory holds the sums of half the waves");
         f32x4 *sums = reinterpret_cast<f32x4 *>(tiles) + rw * (4 * ND * 64) + lane;
@@ -533,12 +595,77 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[d][i] = NAN;
     }
+    float2 norm = make_float2(ref, l2);  // what the weights are formed with
+    if constexpr (WEIGH) {
+        float size = 0.f;
+#pragma unroll
+        for (int g = 0; g < D / GR; ++g) {
+            float x = 0.f;
+#pragma unroll
+            for (int sl = 0; sl < GR / 16; ++sl) {
+                const uint4 y = q[g * (GR / 16) + sl];
+                x = sum_of_f16(uint4{y.x & 0x7fff7fffu, y.y & 0x7fff7fffu, y.z & 0x7fff7fffu, y.w & 0x7fff7fffu}, x);
+            }
+            size = fmaf(x, __uint_as_float(s_k_most[g]), size);
+        }
+        size = (size + __shfl_xor(size, 32, 64)) * (row_c * kHeld);
+        const bool large = row < sp.rows && ref > -INFINITY && (fabsf(ref) > kLarge || size > kLargeSum);
+        if (__builtin_expect(__any(large), 0)) {
+            u32x4 x[NS];
+            uint4 sums[2];
+            float total[D / GR] = {};
+            const bf16_t *qp = (const bf16_t *)a.q + sp.b * a.q_b + tok * a.q_t + head * a.q_h;
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) {
+                x[sl] = *reinterpret_cast<const u32x4 *>(qp + R::kVec * (2 * sl + h));
+                total[16 * sl / GR] = sum_of(__builtin_bit_cast(uint4, x[sl]), total[16 * sl / GR]);
+            }
+#pragma unroll
+            for (int g = 0; g < D / GR; ++g) total[g] += __shfl_xor(total[g], 32, 64);
+            write_sums<D / GR>(total, sums);
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {  // (eight rows of a lane at a time: the registers)
+                float most[8], sum[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most[i] = -INFINITY, sum[i] = 0.f;
+#pragma unroll 1
+                for (int slot0 = b0 * kKeys; slot0 < min(b1 * kKeys, see_any); slot0 += 32) {
+                    const int slot = slot0 + n;
+                    CodeKeys<D, GR> key;
+                    key.load(kc, ks, slot < sp.held ? slot : sp.held - 1, h);
+                    const f32x16 s = key.logits(x, h ? sums[1] : sums[0]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int seen = sp.seen(a, min(row0 + 32 * rw + 16 * half + 8 * (i >> 2) + 4 * h + (i & 3), sp.rows - 1));
+                        const float v = rounded_exponent(half ? s[8 + i] : s[i], a.c, 0.f);
+                        if (slot < seen && v != -INFINITY) {
+                            const float now = fmaxf(most[i], v);
+                            sum[i] = sum[i] * __builtin_amdgcn_exp2f(most[i] - now) + __builtin_amdgcn_exp2f(v - now);
+                            most[i] = now;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                    for (int m = 1; m < 32; m <<= 1) {
+                        const float other = __shfl_xor(most[i], m, 64), l_other = __shfl_xor(sum[i], m, 64), now = fmaxf(most[i], other);
+                        sum[i] = part_weight(most[i], sum[i], now) * sum[i] + part_weight(other, l_other, now) * l_other;
+                        most[i] = now;
+                    }
+                    if (n == 0) s_norm[32 * rw + 16 * half + 8 * (i >> 2) + 4 * h + (i & 3)] = make_float2(most[i], sum[i]);
+                }
+            }
+            wave_sync();
+            if (large) norm = s_norm[32 * rw + n];
+        }
+    }
     const size_t part = ((size_t)pair * a.splits + split) * a.n_rows + row;
     if (row < sp.rows && h == 0) {
         if (a.splits > 1) a.part_ml[part] = make_float2(ref, l);
-        if (WEIGH && a.splits > 1) a.part_l2[part] = l2;
+        if (WEIGH && a.splits > 1) a.part_norm[part] = norm;
         if (WEIGH && a.splits == 1)
-            a.row_ref[part] = make_float4(finite_or_zero(ref), l2 == 0.f ? 0.f : 1.0f / l2, __int_as_float(last + 1), 0.f);
+            a.row_ref[part] = make_float4(finite_or_zero(norm.x), norm.y == 0.f ? 0.f : 1.0f / norm.y, __int_as_float(last + 1), 0.f);
     }
     if (a.splits == 1) {
         if (!a.out) return;
@@ -583,12 +710,12 @@ __global__ __launch_bounds__(256) void quant_many_join_kernel(QuantAttnArgs a) {
     if (sp.rows == 0) return;
     if (a.weights)
         for (int row = blockIdx.x * 256 + threadIdx.x; row < sp.rows; row += gridDim.x * 256) {
-            const float2 *ml = a.part_ml + (size_t)pair * a.splits * a.n_rows + row;
-            const float *l2 = a.part_l2 + (size_t)pair * a.splits * a.n_rows + row;
+            const float2 *norm = a.part_norm + (size_t)pair * a.splits * a.n_rows + row;
             float top = -INFINITY, sum = 0.f;
             for (int s = 0; s < a.splits; ++s) {
-                const float m = ml[(size_t)s * a.n_rows].x, l = l2[(size_t)s * a.n_rows], now = fmaxf(top, m);
-                sum = part_weight(top, sum, now) * sum + part_weight(m, l, now) * l;
+                const float2 x = norm[(size_t)s * a.n_rows];
+                const float now = fmaxf(top, x.x);
+                sum = part_weight(top, sum, now) * sum + part_weight(x.x, x.y, now) * x.y;
                 top = now;
             }
             a.row_ref[(size_t)pair * a.n_rows + row] = make_float4(finite_or_zero(top), sum == 0.f ? 0.f : 1.0f / sum, __int_as_float(sp.seen(a, row)), 0.f);
@@ -604,7 +731,7 @@ __global__ __launch_bounds__(256) void quant_many_join_kernel(QuantAttnArgs a) {
 template <int D, int GR>
 __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArgs a) {
     using R = Row<bf16_t, D>;
-    constexpr int NS = R::kSlices, NG = D / GR, SG = GR / 16, kTiles = 4;  // tiles of rows at a time
+    constexpr int NS = R::kSlices, NG = D / GR, kTiles = 4;  // tiles of rows at a time
     __shared__ u32x4 qs[2][kTiles][R::kKTile];
     __shared__ uint4 ss[2][kTiles][2][32];
     __shared__ float2 rs[2][kTiles * 32];
@@ -624,23 +751,11 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
     const size_t base = (size_t)pair * a.capacity;
     const uint8_t *kc = a.kc + base * (D / 2);
     const uint32_t *ks = a.ks + base * NG;
-    // keys: lane (n, h) has elements 8 (2 sl + h) .. + 7 of slots slot0 + n and + 32
-    uint4 k[2][NS];
-    Words<NG> pairs[2];
+    CodeKeys<D, GR> key[2];  // slots slot0 + n and + 32
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int at = slot0 + 32 * t + n;
-        const uint32_t slot = at < sp.held ? at : sp.held - 1;
-        Words<D / 32> w[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) w[i] = load_words<D / 32>(kc + (slot * (D / 2) + D / 8 * (h + 2 * i)));
-        pairs[t] = load_words<NG>(ks + (size_t)slot * NG);
-#pragma unroll
-        for (int sl = 0; sl < NS; ++sl) {  // piece 2 sl + h = 4 m + nq; the codes in the order of the elements
-            const uint4 x = operand_of(w[sl & 1].w[sl >> 1]);
-            k[t][sl] = uint4{__builtin_amdgcn_perm(x.y, x.x, 0x05040100u), __builtin_amdgcn_perm(x.w, x.z, 0x05040100u),
-                             __builtin_amdgcn_perm(x.y, x.x, 0x07060302u), __builtin_amdgcn_perm(x.w, x.z, 0x07060302u)};
-        }
+        key[t].load(kc, ks, at < sp.held ? at : sp.held - 1, h);
     }
     float w[2][2] = {};
 
@@ -687,7 +802,7 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
         const int tiles = min(kTiles, (sp.rows - row0 + 31) / 32), all = sp.seen(a, row0);
         bool odd = slot0 + 64 > all;
 #pragma unroll
-        for (int t = 0; t < kTiles / 2; ++t) odd = odd || fabsf(rs[buf][64 * t + lane].x) > kHuge;
+        for (int t = 0; t < kTiles / 2; ++t) odd = odd || fabsf(rs[buf][64 * t + lane].x) > kLarge;
         odd = __any(odd);
         for (int t = 0; t < tiles; ++t) {
             u32x4 q[NS];
@@ -699,33 +814,13 @@ __global__ __launch_bounds__(512, 2) void quant_many_weights_kernel(QuantAttnArg
             for (int i = 0; i < 16; ++i) ref[i] = rs[buf][32 * t + 8 * (i >> 2) + 4 * h + (i & 3)];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                uint4 lo;
-                {
-                    const uint32_t a01 = NG == 1 ? pairs[x].w[0] & 0xffffu : __builtin_amdgcn_perm(pairs[x].w[1 % NG], pairs[x].w[0], 0x05040100u);
-                    const uint32_t a23 = NG == 4 ? __builtin_amdgcn_perm(pairs[x].w[3 % NG], pairs[x].w[2 % NG], 0x05040100u) : a01;
-                    lo = uint4{a01, a23, a01, a23};
-                }
-                f32x16 s;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = 0.f;
-                s = mma32(sums, lo, s, bf16_t());
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    f32x16 z;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < SG; ++j) z = mma32(__builtin_bit_cast(uint4, q[g * SG + j]), k[x][g * SG + j], z, bf16_t());
-                    const float step = step_of(pairs[x].w[g]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = fmaf(step, z[i], s[i]);
-                }
+                const f32x16 s = key[x].logits(q, sums);
                 if (__builtin_expect(odd, 0)) {
                     const int slot = slot0 + 32 * x + n;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int seen = seen_by[buf][32 * t + 8 * (i >> 2) + 4 * h + (i & 3)];
-                        const float v = fabsf(ref[i].x) > kHuge ? rounded_exponent(s[i], a.c, ref[i].x) : fmaf(s[i], a.c, -ref[i].x);
+                        const float v = fabsf(ref[i].x) > kLarge ? rounded_exponent(s[i], a.c, ref[i].x) : fmaf(s[i], a.c, -ref[i].x);
                         const float p = __builtin_amdgcn_exp2f(v) * ref[i].y;
                         w[x][i & 1] += slot < seen ? p : 0.f;
                     }

@@ -211,3 +211,51 @@ def test_weights_of_small_and_large_keys(rows, size):
     far = (w[0, 0, :n].double() - want).abs().max().item() / want
     assert far <= bound, f"{far} off, {bound} allowed"
     assert not bool(w[0, 0, n:].any())
+
+
+# ---- logits of any size ----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("d,group", [(64, 32), (64, 64), (128, 32), (128, 64)])
+@pytest.mark.parametrize("rows", [1, 6, 20, 48, 300])
+@pytest.mark.parametrize("size", [1e2, 3e3, 1e6, 1e9])
+@pytest.mark.parametrize("pieces", [1, 2])
+def test_equal_logits_share_a_row_at_any_size(d, group, rows, size, pieces):
+    """Equal keys of any elements: equal logits, so that the slots share a row equally however large these are, in the outputs and in the weights: sums
+    of as many terms, and a product with one over the sum."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    n, H, room = (300, 32, 9000) if pieces == 1 else (300, 1, 70000)
+    cache = A.QuantCache(1, H, n + room, d, group=group)
+    k, v = _randn(1, 1, H, 1, d).bfloat16().expand(1, H, n, d), _randn(2, 1, H, n, d).bfloat16()
+    A.air_quant_append(cache, k, v)
+    q = (size * _randn(3, 1, H, rows, d)).bfloat16()
+    out, w = torch.empty_like(q), torch.zeros((1, H, n + room), device="cuda:0")
+    A.air_quant_attn(cache, q, out, lens=_ints([n]), causal=False, weights=w)
+    far = (w[:, :, :n].double() * n / rows - 1.0).abs().max().item()
+    assert far <= (n + rows + 72) * 2.0 ** -24 + 2.0 ** -21, f"weights {far} off"
+    assert not bool(w[:, :, n:].any())
+    _, (vl, vs, _) = unpacked(cache)
+    val = (vl + vs)[:, :, :n]
+    want, a = val.mean(2, keepdim=True), val.abs().mean(2, keepdim=True)
+    assert bool(((out.double() - want).abs() <= a * 3 * 2.0 ** -11 + 2.0 ** -8 * want.abs() + 1e-6).all())
+
+
+@pytest.mark.parametrize("d,group", [(64, 32), (128, 64)])
+@pytest.mark.parametrize("rows", [1, 20, 48, 300])
+@pytest.mark.parametrize("size", [30.0, 1e3, 1e5, 1e7])
+@pytest.mark.parametrize("causal", [False, True])
+def test_weights_of_a_row_add_up_to_one_at_any_size(d, group, rows, size, causal):
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    n, room = 2000, 70000
+    cache = A.QuantCache(1, 1, n + room, d, group=group)
+    A.air_quant_append(cache, _randn(1, 1, 1, n, d).bfloat16(), _randn(2, 1, 1, n, d).bfloat16())
+    q = (size * _randn(3, 1, 1, rows, d)).bfloat16()
+    w = torch.zeros((1, 1, n + room), device="cuda:0")
+    A.air_quant_attn(cache, q, None, lens=_ints([n]), causal=causal, weights=w)
+    far = abs(w.double().sum().item() / rows - 1.0)
+    # the sums of 2000 probabilities, their factor, and weights of up to `rows` terms
+    assert far <= (n + rows + 72) * 2.0 ** -24 + 2.0 ** -20, f"{far} off"
