@@ -890,13 +890,15 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
     if (threadIdx.x < 128) rows.form(n, (int)(threadIdx.x >> 4) < sp.rows, rl + (threadIdx.x >> 4));
     __syncthreads();
     float2 ref[4];
-    bool huge = false;
+    bool huge = false, odd = false;  // odd: a row of NaN, which counts in slots that it sees alone (elsewhere a probability of 0 times NaN)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         ref[i] = rl[4 * (c & 1) + i];
         huge = huge || fabsf(ref[i].x) > kHuge;
+        odd = odd || ref[i].y != ref[i].y;
     }
     huge = __any(huge);
+    odd = __any(odd);
     for (; u < runs; u += stride) {
         float w[2];
 #pragma unroll
@@ -904,8 +906,11 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
             const float x[4] = {s[t].x, s[t].y, s[t].z, s[t].w};
             w[t] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (4 * (c & 1) + i < sp.rows) w[t] = fmaf(__builtin_amdgcn_exp2f(exponent(x[i], a.c, ref[i].x, huge)), ref[i].y, w[t]);
+            for (int i = 0; i < 4; ++i) {
+                const int row = 4 * (c & 1) + i;
+                if (row < sp.rows && (!odd || u * kRun + 32 * t + 16 * (c >> 1) + n < sp.seen(a, row)))
+                    w[t] = fmaf(__builtin_amdgcn_exp2f(exponent(x[i], a.c, ref[i].x, huge)), ref[i].y, w[t]);
+            }
             w[t] += __shfl_xor(w[t], 16, 64);
         }
 #pragma unroll

@@ -259,3 +259,30 @@ def test_weights_of_a_row_add_up_to_one_at_any_size(d, group, rows, size, causal
     far = abs(w.double().sum().item() / rows - 1.0)
     # the sums of 2000 probabilities, their factor, and weights of up to `rows` terms
     assert far <= (n + rows + 72) * 2.0 ** -24 + 2.0 ** -20, f"{far} off"
+
+
+# ---- rows that are not numbers ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d,group", [("bf16", 64, 32), ("bf16", 128, 64), ("f32", 64, 64), ("f32", 128, 32)])
+@pytest.mark.parametrize("T,bad", [(2, 0), (8, 0), (8, 3), (12, 5), (60, 0), (60, 31), (300, 150)])
+@pytest.mark.parametrize("room", [0, 70000])
+def test_a_row_of_nan_weighs_only_slots_that_it_sees(dtype, d, group, T, bad, room):
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    n = 400
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    cache = A.QuantCache(1, 1, n + room, d, A.AIR_BF16 if dtype == "bf16" else A.AIR_F32, group=group)
+    A.air_quant_append(cache, _randn(1, 1, 1, n, d).to(dt), _randn(2, 1, 1, n, d).to(dt))
+    q = _randn(3, 1, 1, T, d).to(dt)
+    q[0, 0, bad, 1] = math.nan
+    out, w = torch.empty_like(q), torch.zeros((1, 1, n + room), device="cuda:0")
+    A.air_quant_attn(cache, q, out, lens=_ints([n]), causal=True, weights=w)
+    seen = n - T + 1 + bad  # slots that the row sees
+    assert bool(w[0, 0, :seen].isnan().all()) and not bool(w[0, 0, seen:].isnan().any())
+    assert bool(out[0, 0, bad].isnan().all()) and not bool(out[0, 0, :bad].isnan().any()) and not bool(out[0, 0, bad + 1:].isnan().any())
+    # what the others give to the slots that it does not see
+    q2, w2 = q.clone(), torch.zeros_like(w)
+    q2[0, 0, bad] = 0.0
+    A.air_quant_attn(cache, q2, None, lens=_ints([n]), causal=True, weights=w2)
+    assert torch.equal(w[0, 0, seen:], w2[0, 0, seen:])
