@@ -374,7 +374,8 @@ typedef struct {
     int32_t n_q_heads, n_tokens; /* a multiple of the KV heads, at most 16384; queries of a sequence, with padding (0: nothing is done).
                                     n_tokens x n_q_heads below 2^26, times batch below 2^31                                     */
     int32_t causal;              /* 0: every query sees all slots held; 1: query t of n sees all but the last n - 1 - t        */
-    int32_t max_len;             /* most slots that a sequence will hold when the call runs: only the launch's shape goes by it; 0: capacity */
+    int32_t max_len;             /* most slots that a sequence will hold when the call runs (0: capacity).  More are attended to all the same: the
+                                    launch's shape goes by it, and whether a call is a large one (air_quant_attn)                */
     float scale;                 /* of the logits, > 0, at most 2^127; 0: 1 / sqrt(head_dim)                                  */
     const void *q;               /* [batch][n_q_heads][n_tokens][head_dim]                                                     */
     void *out;                   /* the same, or NULL: weights only                                                            */
@@ -393,15 +394,18 @@ size_t air_quant_workspace_bytes(const air_quant_cache *cache, const air_quant_q
  * and, with weights, weights[b][KV head][j] += sum of p_j over the queries and the query heads of the KV head, in a fixed order.
  * A query that sees no slot gives zero.  What lies in slots that a query does not see counts for nothing, whatever it stands for; a group
  * of NaN in a slot that it sees makes its part of the output (V) or all of it (K) NaN.  fp32: products of codes are exact, everything
- * else is held in fp32.  bf16: the same logits and sums, and factors p step of 15 bits for the second product; large calls of 33 rows (queries
- * x query heads per KV head) and more round what V stands for and the probabilities to 11 bits, 8 where groups of a slot's V lie further than 2^24 below
- * the same group of another slot (an element of V loses besides at most 2^-15 of the greatest of its group; a probability 2^-18 of the greatest
- * among slots 32 i .. 32 i + 31, its own one of them, and at most 2^-31 of its row's greatest), and without weights what K stands for to 11 bits
- * (with them to 22; elements of K and of queries lose besides at most 2^-22 of their row's greatest).
+ * else is held in fp32.  bf16: the same logits and sums, and factors p step of 15 bits for the second product.
+ * Large bf16 calls round more, so that the same rows in a cache of another capacity, or with another max_len, may come out otherwise within these bounds:
+ * V and the probabilities to 11 bits, 8 where groups of a slot's V lie further than 2^24 below the same group of another slot (an element of V
+ * loses besides at most 2^-15 of the greatest of its group; a probability 2^-18 of the greatest among slots 32 i .. 32 i + 31, its own one of
+ * them, and at most 2^-31 of its row's greatest), and without weights what K stands for to 11 bits (with them to 22; elements of K and of queries lose
+ * besides at most 2^-22 of their row's greatest).  Large: with rows = n_tokens x n_q_heads / n_kv_heads above 32, slots = batch x n_kv_heads x max_len (or
+ * capacity), rows x slots at least 2.6e6 (heads of 128; of 64: 6e6); with weights, of up to 224 rows, where slots are at least 32768 too, of more always.
  * Outputs are rounded once.  The sums of an output hold p up to 2^8 times the probability of the row's greatest logit, undivided: V of 2^95 and more can
  * overflow them.
  * Causal queries belong to the last counts slots of the sequence: after air_evict slots have no order, so a call of
- * more than one causal query appends its own rows.  workspace: 256-byte aligned, free for another call when this one's work has run.
+ * more than one causal query appends its own rows.  Where lens + counts exceed the capacity, rows that have no slot are dropped, but the border still
+ * counts back from the last slot: query t of n sees the first capacity - (n - 1 - t), which may lack its own.  workspace: 256-byte aligned, free for another call when this one's work has run.
  * out must not overlap an input; output rows that overlap are refused (AIR_ERR_SHAPE). */
 air_status air_quant_attn(void *stream, const air_quant_cache *cache, const air_quant_query *query, const air_quant_rows *append,
                           void *workspace, size_t workspace_bytes);
