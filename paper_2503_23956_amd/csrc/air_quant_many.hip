@@ -218,7 +218,7 @@ __device__ __forceinline__ void write_sums(const float (&part)[NG], uint4 *to) {
     }
 }
 
-// Logits of weights: exact products of codes.  A lane (n, h) has elements 8 (2 sl + h) .. + 7 of a slot's codes as numbers,
+// Logits of weights: exact products of codes.  A lane (n, h) has elements 8 (2 sl + h) .. + 7 of slot n, as numbers
 template <int D, int GR>
 struct CodeKeys {
     static constexpr int NS = D / 16, NG = D / GR;
@@ -329,7 +329,8 @@ __global__ __launch_bounds__(512, 2) void quant_many_kernel(QuantAttnArgs a) {
         const float unit = unit_of(fmaxf(most, __shfl_xor(most, 32)));
 #pragma unroll
         for (int sl = 0; sl < NS; ++sl) q[sl] = to_f16(q[sl], held_over(unit));
-        row_c = row_c * unit / (kHeld * kHeld);
+        // (a factor of 0 or infinity would make no number of a masked logit, or of a logit of 0; at the ends of the range all logits are 0 or infinite)
+        row_c = fminf(fmaxf(row_c * unit * (1.0f / (kHeld * kHeld)), 0x1p-126f), 0x1.fffffep127f);
     }
     float mul = row_c;
     const size_t base = (size_t)pair * a.capacity;

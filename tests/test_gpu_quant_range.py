@@ -286,3 +286,33 @@ def test_a_row_of_nan_weighs_only_slots_that_it_sees(dtype, d, group, T, bad, ro
     q2[0, 0, bad] = 0.0
     A.air_quant_attn(cache, q2, None, lens=_ints([n]), causal=True, weights=w2)
     assert torch.equal(w[0, 0, seen:], w2[0, 0, seen:])
+
+
+# ---- scales ----------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("scale", [1.5e-45, 1e-42, 1e-38, 1e-30, 1e30, 1e38])
+@pytest.mark.parametrize("rows", [1, 8, 20, 48, 300])
+@pytest.mark.parametrize("room", [0, 70000])
+@pytest.mark.parametrize("q_size", [1e-12, 1.0, 1e12])
+def test_scales_at_the_ends_of_their_range(scale, rows, room, q_size):
+    """Logits that all vanish, of rows that see all slots, some or none: the mean of what they see; and logits of 0 at any scale."""
+    import torch
+
+    import paper_2503_23956_amd as A
+
+    n, d = 200, 128
+    cache = A.QuantCache(1, 1, n + room, d)
+    k, v = _randn(1, 1, 1, n, d), _randn(2, 1, 1, n, d) + 1.0
+    q = q_size * _randn(3, 1, 1, rows, d)
+    if scale * q_size > 1e-10:  # keys of 0
+        k.zero_()
+    A.air_quant_append(cache, k.bfloat16(), v.bfloat16())
+    q = q.bfloat16()
+    out, w = torch.empty_like(q), torch.zeros((1, 1, n + room), device="cuda:0")
+    A.air_quant_attn(cache, q, out, lens=_ints([n]), causal=True, scale=scale, weights=w)
+    _, (vl, vs, _) = unpacked(cache)
+    val = (vl + vs)[0, 0, :n]
+    seen = (torch.arange(rows, device="cuda:0") + 1 + n - rows).clamp(min=0)
+    p = (torch.arange(n, device="cuda:0") < seen[:, None]).double() / seen[:, None].clamp(min=1)
+    want, a = p @ val, p @ val.abs()
+    assert bool(((out[0, 0].double() - want).abs() <= a * (3 * 2.0 ** -11 + 2.0 ** -8) + 1e-6).all())
+    assert bool(((w[0, 0, :n].double() - p.sum(0)).abs() <= p.sum(0) * ((n + rows + 72) * 2.0 ** -24 + 2.0 ** -20)).all())
