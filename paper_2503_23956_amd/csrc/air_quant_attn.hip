@@ -923,10 +923,10 @@ __global__ __launch_bounds__(256) void quant_few_finish_kernel(QuantAttnArgs a) 
 }
 
 // Tiles of 128 and 256 rows pay in bf16 calls of enough logits.  Measured, us, these kernels / those, heads of 128, 4 KV heads: one sequence, 112 rows
-// over 1000 slots 13.5 / 18.0, over 7432 22.8 / 22.8, 448 rows over 2500 27.1 / 26.2, over 7432 46.6 / 34.5; eight sequences, 48 rows over 4000 slots
-// 37.6 / 28.3, 32 rows 24.7 / 26.6 (sixteen, 16 k slots: 88 / 118), 448 rows over 200 23.1 / 15.3, 72 over 1500 26.9 / 23.2, with weights 43.5 / 36.6;
-// heads of 64: 224 rows over 700 13.3 / 17.9, 448 22.0 / 18.7.  With weights, whose launch there has few slots or few rows to deal, in calls of few slots: one sequence
-// of 7432, 112 rows 33.7 / 47.7, 224 54.4 / 52.3, 448 89 / 57; of 1000, 224 rows 31.7 / 36.7, 448 50 / 40.
+// over 1000 slots 13.9 / 18.5, over 7432 22.8 / 23.1, 448 rows over 2500 26.4 / 25.9, over 7432 46.4 / 34.1; eight sequences, 48 rows over 4000 slots
+// 36.4 / 28.1, 32 rows 23.2 / 26.2 (sixteen, 16 k slots: 88 / 114), 448 rows over 200 22.5 / 15.7, 72 over 1500 26.5 / 23.6, with weights 43.0 / 38.4;
+// heads of 64: 224 rows over 700 10.6 / 13.9, 448 12.1 / 14.8.  With weights, whose launch there has few slots or few rows to deal, in calls of few slots: one sequence
+// of 7432, 112 rows 33.0 / 48.6, 224 54.0 / 53.0, 448 89 / 58; of 1000, 224 rows 30.9 / 37.9, 448 50 / 41.
 static bool many_rows(const air_quant_cache &c, const air_quant_query &q, int64_t pairs, int64_t rows, int64_t len) {
     if (c.dtype != AIR_BF16 || rows <= 32) return false;
     if (q.weights && (rows > 224 || pairs * len < 32768)) return rows > 224;
@@ -945,8 +945,8 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
     if (many_rows(c, q, pairs, rows, len)) {
         // The least of what a call takes by a model, in us: rounds of 256 workgroups, the slots of each (all, or where there are several rounds of a
         // causal call the mean) at the nanoseconds a slot takes by tile and head size, and the splits' join with its launch and traffic.  Measured, 28 / 4
-        // heads of 128, tiles of 128 rows / 256 rows with their best splits: 96 rows over 7432 slots 21 / 22, 448 33 / 34, 1792 68 / 62, 3500 124 / 97;
-        // prompts of 1000 tokens 32 / 41, 3000 132 / 109, 7000 548 / 425; 64 pairs of 512 rows over 16 k slots 692 / 640.
+        // heads of 128, tiles of 128 rows / 256 rows with their best splits: 96 rows over 7432 slots 22 / 23, 448 34 / 35, 1792 69 / 63, 3500 113 / 91;
+        // prompts of 1000 tokens 35 / 46, 2999 136 / 112, 7000 579 / 441; 64 pairs of 512 rows over 16 k slots 414 / 322.
         double least = 1e30;
         for (int tile = 128; tile <= 256; tile += 128) {
             const double ns = c.head_dim == 128 ? (tile == 128 ? 24.0 : 32.0) : (tile == 128 ? 12.7 : 20.6);
@@ -973,7 +973,7 @@ QuantPlan quant_plan(const air_quant_cache &c, const air_quant_query &q) {
         p.sums_at = p.ref_at + (q.weights ? whole((size_t)pairs * rows * sizeof(float4)) : 0);
         p.w_at = p.sums_at + (q.weights ? whole((size_t)pairs * rows * 2 * sizeof(uint4)) : 0);
         // The weights' workgroups have 512 slots each: where they would leave CUs without work, the rows are dealt to several, by whole turns of 128
-        // (7000 tokens of 28 / 4 heads over themselves 3720 us without, 877 so)
+        // (7000 tokens of 28 / 4 heads over themselves 3720 us without, 884 so)
         const int64_t wgs = pairs * ((len + 511) / 512), turns = (rows + 127) / 128;
         const int64_t room = (64 << 20) / (pairs * c.capacity), dealt = 2 * kCUs / wgs, shares = dealt < room ? dealt : room;  // (at most 256 MiB)
         p.w_splits = (int)(shares < 1 || turns < 2 ? 1 : shares < turns ? shares : turns);

@@ -14,9 +14,9 @@
 //   slot's group is smaller than that, V and the probabilities become bf16, which holds any magnitude, with 8 bits (outputs 0.0025 off fp64 in
 //   place of 0.0018; an fp32 computation rounded once 0.0017).
 // Per 32 x 64 logits a wave issues 16 + 16 products of 32 clocks (weights: 32 + 16); dequantising costs about 70 vector instructions a
-// wave and block.  500 queries of 28 / 4 heads behind 7432 slots: 92 us, 600 TFLOP/s (matrix unit busy 26 %: four splits of 28 blocks, prologue and
-// epilogue beside them; vector unit 39 %); 64 queries of 64 / 8 heads over eight caches of 16 k slots, with weights, 410 us (41 % and 53 %), the weights'
-// launch 230 (25 % and 59 %).  Between them the unit that is busy alternates with the one that waits: two waves a SIMD.
+// wave and block.  500 queries of 28 / 4 heads behind 7432 slots: 95 us, 580 TFLOP/s (matrix unit busy 25 %: four splits of 28 blocks, prologue and
+// epilogue beside them; vector unit 40 %); 64 queries of 64 / 8 heads over eight caches of 16 k slots, with weights, 415 to 428 us (38 % and 53 %), the weights'
+// launch 230 to 237 (25 % and 59 %).  Between them the unit that is busy alternates with the one that waits: two waves a SIMD.
 #include <type_traits>
 
 #include "air_block.h"
@@ -261,7 +261,7 @@ struct CodeKeys {
 // The logits of the outputs are off those of the weights by fp32 steps of what they are sums of, so that the sum of a row's probabilities in the one is no measure
 // for the other where these are large: a logit beyond kLarge (base 2), or magnitudes (by group: the query's, times the greatest of K) that add up to more
 // than kLargeSum.  The reference and sum of such rows are formed once more, with the weights' own logits (beyond kLarge with the product with the factor rounded, as
-// there), so that equal logits share equally and a row's weights add up to one at any size.
+// there), so that equal logits share equally and a row's weights add up to one at any size.  (The window above with queries 100 times as large: 1380 us.)
 constexpr float kLarge = 256.0f, kLargeSum = 4096.0f;
 
 // KW 1: 256 rows, every wave takes both halves of a block.  KW 2: 128 rows, two waves share 32 rows and take a half of every block each.
