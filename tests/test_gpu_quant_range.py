@@ -192,7 +192,7 @@ def test_values_beside_larger_ones(below, rows, d, group, weighs, pieces):
 @pytest.mark.parametrize("size", [-20, -8, -7, -6, -5, 0, 10, 11, 12, 40])
 def test_weights_of_small_and_large_keys(rows, size):
     """Equal keys lo + 8 step = 2^size (1 + 255 2^-19), whose low bits lie 2^-19 and less below: the rows' logits are 600 (base 2), and every slot has its share.
-    K has 22 bits, sums round 16 times (of the products of two terms) and 6 times (by group) to 24."""
+    K has 22 bits; sums are rounded to 24 sixteen times (products of two terms) and six times (by group)."""
     import torch
 
     import paper_2503_23956_amd as A
